@@ -312,6 +312,68 @@ mw_status mw_bca_cache_fwd_noalloc(const void* q, const void* k_new, const void*
                                    int H, int n_q_chunks, int T_chunk, int d, float scale,
                                    void* stream);
 
+/* ---- Conditioning: cross attention to an encoder's states, layer norm ---- */
+
+/*
+ * Cross attention: queries of a video's tokens against the states of an encoder
+ * (a prompt, images, a reference video), whose number is another one:
+ *
+ *     s_ij = scale * <q_i, k_j> for j < len_b,   LSE_i = ln sum_j exp(s_ij),
+ *     P_ij = exp(s_ij - LSE_i),   O_i = sum_j P_ij v_j
+ *
+ * q, o [B, H, M, d]; k, v [B, Hkv, S, d], H a multiple of Hkv: query heads
+ * h H/Hkv ... (h+1) H/Hkv - 1 share head h of K and V.  kv_len: device array of B
+ * int32, the valid states of each sample (the first kv_len[b]; below 0 counts as
+ * 0, above S as S), or NULL: all S.  What K and V hold in the other places does
+ * not matter (NaN included).  A row that sees no state has O = 0, LSE = -inf.
+ * lse (fp32 [B, H, M]) may be NULL.  M = 0 and S = 0 are valid.
+ * workspace: mw_xattn_workspace_size() bytes, 256-byte aligned (NULL if 0).
+ */
+size_t mw_xattn_workspace_size(int B, int H, int Hkv, int M, int S, int d);
+mw_status mw_xattn_fwd(const void* q, const void* k, const void* v, const int* kv_len, void* o,
+                       float* lse, void* workspace, size_t ws_bytes, int B, int H, int Hkv, int M,
+                       int S, int d, float scale, void* stream);
+
+/*
+ * Its gradients: with D_i = <dO_i, O_i> and dS = P (dO V^T - D),
+ *     dV = P^T dO,   dK = scale dS^T Q,   dQ = scale dS K,
+ * those of K and V summed over the query heads that share them, and 0 in the
+ * places past kv_len.  o and lse are the forward's.
+ */
+size_t mw_xattn_bwd_workspace_size(int B, int H, int Hkv, int M, int S, int d);
+mw_status mw_xattn_bwd(const void* q, const void* k, const void* v, const int* kv_len, const void* o,
+                       const float* lse, const void* dout, void* dq, void* dk, void* dv,
+                       void* workspace, size_t ws_bytes, int B, int H, int Hkv, int M, int S, int d,
+                       float scale, void* stream);
+
+/* Element types of the layer norm's arrays. */
+enum { MW_BF16 = 0, MW_F32 = 1 };
+
+/*
+ * Layer norm over the C <= 8192 channels of each of `rows` rows:
+ *     xh = (x - mean) rstd,   rstd = 1 / sqrt(var + eps),   y = xh w_g + b_g
+ * with one weight and bias for each of `groups` equal groups of consecutive rows
+ * (weight, bias [groups, C]; 1: the usual layer norm; more: the modulation of
+ * samples or frames; NULL: 1 and 0).  x and y may be bf16 or fp32 (y fp32 only
+ * with x fp32), weight and bias either.  mean, rstd (fp32 [rows]) are written for
+ * the backward, or NULL.  Pointers need the alignment of their elements only; with
+ * C a multiple of 8 and all of them 16-byte aligned, memory is accessed 16 bytes at
+ * a time.
+ */
+mw_status mw_layernorm_fwd(const void* x, const void* weight, const void* bias, void* y, float* mean,
+                           float* rstd, long long rows, int C, int groups, float eps, int x_dtype,
+                           int y_dtype, int param_dtype, void* stream);
+
+/*
+ * Its gradients, dy in y's type: dx in x's, dweight and dbias (either NULL) in the
+ * parameters', summed over each group's rows in fp32 in a fixed order.
+ */
+size_t mw_layernorm_bwd_workspace_size(long long rows, int C, int groups);
+mw_status mw_layernorm_bwd(const void* dy, const void* x, const float* mean, const float* rstd,
+                           const void* weight, void* dx, void* dweight, void* dbias, void* workspace,
+                           size_t ws_bytes, long long rows, int C, int groups, int x_dtype,
+                           int y_dtype, int param_dtype, void* stream);
+
 /* Human-readable name of a status code (static string). */
 const char* mw_status_string(mw_status s);
 

@@ -14,8 +14,12 @@ Entry points (same names as the C ABI, taking torch tensors):
                         cache_head, cache_len, T_chunk, ...) -> (o, lse)
   mw_bca_cache_fwd_rope(..., rope_dims, rope_base, shift_frames)
   mw_bca_cache_commit(k_cache, v_cache, slot_start, k_src, v_src)
+  mw_xattn_fwd(q, k, v, kv_len=None, scale=None, need_lse=True) -> (o, lse)
+  mw_xattn_bwd(q, k, v, o, lse, dout, kv_len=None, scale=None) -> (dq, dk, dv)
+  mw_layernorm_fwd(x, weight=None, bias=None, eps=1e-5) -> (y, mean, rstd)
+  mw_layernorm_bwd(dy, x, mean, rstd, weight, bias) -> (dx, dweight, dbias)
   mw_device_status(clear=True), mw_set_option(name, value)
-Tensors are contiguous bf16 [B, H, rows, d] on the current CUDA device.
+Attention tensors are contiguous bf16 [B, H, rows, d] on the current CUDA device.
 """
 from __future__ import annotations
 
@@ -36,6 +40,9 @@ __all__ = [
     "mw_bca_cache_commit", "mw_bca_bwd_workspace_size", "mw_bca_bwd_head_groups",
     "mw_bca_cache_workspace_size",
     "mw_device_status", "mw_set_option", "mw_qkv_rope_split", "BlockCausalAttention",
+    "mw_xattn_fwd", "mw_xattn_bwd", "mw_xattn_workspace_size", "mw_xattn_bwd_workspace_size",
+    "mw_layernorm_fwd", "mw_layernorm_bwd", "mw_layernorm_bwd_workspace_size", "CrossAttention",
+    "LayerNorm",
     "EXPORTED_SYMBOLS",
     "RingState",
 ]
@@ -50,6 +57,8 @@ EXPORTED_SYMBOLS = (
     "mw_bca_cache_fwd", "mw_bca_cache_commit", "mw_status_string", "mw_last_error",
     "mw_device_status", "mw_set_option", "mw_bca_cache_fwd_noalloc", "mw_bca_cache_fwd_sink",
     "mw_bca_cache_fwd_rope", "mw_qkv_rope_split", "mw_bca_cache_step", "mw_bca_bwd_head_groups",
+    "mw_xattn_workspace_size", "mw_xattn_fwd", "mw_xattn_bwd_workspace_size", "mw_xattn_bwd",
+    "mw_layernorm_fwd", "mw_layernorm_bwd_workspace_size", "mw_layernorm_bwd",
 )
 
 STATUS = {0: "MW_OK", 1: "MW_ERR_INVALID_ARG", 2: "MW_ERR_UNSUPPORTED", 3: "MW_ERR_CUDA",
@@ -78,6 +87,7 @@ _P = ctypes.c_void_p
 _I = ctypes.c_int
 _F = ctypes.c_float
 _Z = ctypes.c_size_t
+_L = ctypes.c_longlong
 
 
 def library() -> ctypes.CDLL:
@@ -111,6 +121,15 @@ def library() -> ctypes.CDLL:
                                    _I, _I, _I, _I, _I, _F, _P]),
         "mw_bca_cache_fwd_noalloc": (_I, [_P, _P, _P, _P, _P, _I, _I, _I, _P, _P,
                                           _I, _I, _I, _I, _I, _F, _P]),
+        "mw_xattn_workspace_size": (_Z, [_I, _I, _I, _I, _I, _I]),
+        "mw_xattn_fwd": (_I, [_P, _P, _P, _P, _P, _P, _P, _Z, _I, _I, _I, _I, _I, _I, _F, _P]),
+        "mw_xattn_bwd_workspace_size": (_Z, [_I, _I, _I, _I, _I, _I]),
+        "mw_xattn_bwd": (_I, [_P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _Z,
+                              _I, _I, _I, _I, _I, _I, _F, _P]),
+        "mw_layernorm_fwd": (_I, [_P, _P, _P, _P, _P, _P, _L, _I, _I, _F, _I, _I, _I, _P]),
+        "mw_layernorm_bwd_workspace_size": (_Z, [_L, _I, _I]),
+        "mw_layernorm_bwd": (_I, [_P, _P, _P, _P, _P, _P, _P, _P, _P, _Z, _L, _I, _I,
+                                  _I, _I, _I, _P]),
         "mw_status_string": (ctypes.c_char_p, [_I]),
         "mw_last_error": (ctypes.c_char_p, []),
         "mw_device_status": (_I, [_P, _I]),
@@ -149,7 +168,9 @@ def _load_native(lib: ctypes.CDLL) -> None:
                        f"{running[0]} and Python {running[1]:#x}")
     module.bind(*(ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in (
         "mw_bca_fwd", "mw_bca_bwd", "mw_bca_bwd_workspace_size", "mw_bca_cache_workspace_size",
-        "mw_bca_cache_fwd_rope", "mw_bca_cache_step", "mw_qkv_rope_split")))
+        "mw_bca_cache_fwd_rope", "mw_bca_cache_step", "mw_qkv_rope_split",
+        "mw_xattn_workspace_size", "mw_xattn_fwd", "mw_xattn_bwd_workspace_size", "mw_xattn_bwd",
+        "mw_layernorm_fwd", "mw_layernorm_bwd_workspace_size", "mw_layernorm_bwd")))
     _native = module
 
 
@@ -490,6 +511,201 @@ def mw_qkv_rope_split(qkv: torch.Tensor, rope_dims: int = 0, rope_base: float = 
     return q, k, v
 
 
+def _xattn_shapes(q, k, v, kv_len):
+    """B, H, Hkv, M, S, d of a cross attention call."""
+    B, H, M, d = _bhnd(q, "q")
+    Bk, Hkv, S, dk = _bhnd(k, "k")
+    if _bhnd(v, "v") != (Bk, Hkv, S, dk):
+        raise ValueError(f"v shape {tuple(v.shape)} != k shape {tuple(k.shape)}")
+    if (Bk, dk) != (B, d):
+        raise ValueError(f"k shape {tuple(k.shape)} does not match q shape {tuple(q.shape)}")
+    if Hkv < 1 or H % Hkv != 0:
+        raise ValueError(f"q has {H} heads, not a multiple of k's {Hkv}")
+    if kv_len is not None:
+        _expect(kv_len, "kv_len", (B,), torch.int32)
+    return B, H, Hkv, M, S, d
+
+
+def mw_xattn_workspace_size(B: int, H: int, Hkv: int, M: int, S: int, d: int) -> int:
+    return int(library().mw_xattn_workspace_size(B, H, Hkv, M, S, d))
+
+
+def mw_xattn_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                 kv_len: Optional[torch.Tensor] = None, scale: Optional[float] = None,
+                 need_lse: bool = True, workspace: Optional[torch.Tensor] = None,
+                 out: Optional[Tuple[torch.Tensor, Optional[torch.Tensor]]] = None
+                 ) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """Cross attention of q [B, H, M, d] to an encoder's states k, v
+    [B, Hkv, S, d]: H / Hkv query heads share a head of K and V, and of a sample's
+    states the first ``kv_len`` [B] (int32, on the device) count; returns (O, LSE
+    or None), O = 0 and LSE = -inf for a sample without states.
+
+    ``out`` = (o, lse) reuses caller buffers (lse may be None)."""
+    if out is None and _native is not None:
+        r = _native.xattn_fwd(q, k, v, kv_len, scale, need_lse, workspace)
+        if r is not None:
+            return r if type(r) is tuple else _check(r)
+    B, H, Hkv, M, S, d = _xattn_shapes(q, k, v, kv_len)
+    o, lse = out if out is not None else (None, None)
+    if out is not None:
+        _expect(o, "o", (B, H, M, d))
+        if lse is not None:
+            _expect(lse, "lse", (B, H, M), torch.float32)
+    _on_device(q, (("k", k), ("v", v), ("kv_len", kv_len), ("o", o), ("lse", lse),
+                   ("workspace", workspace)))
+    ws_bytes = mw_xattn_workspace_size(B, H, Hkv, M, S, d)
+    workspace = _workspace(workspace, ws_bytes, q.device)
+    if out is None:
+        o = torch.empty_like(q)
+        lse = torch.empty((B, H, M), dtype=torch.float32, device=q.device) if need_lse else None
+    _no_alias((("o", o), ("lse", lse), ("workspace", workspace)),
+              (("q", q), ("k", k), ("v", v), ("kv_len", kv_len)))
+    _check(library().mw_xattn_fwd(_ptr(q), _ptr(k), _ptr(v), _ptr(kv_len), _ptr(o), _ptr(lse),
+                                  _ptr(workspace), ws_bytes, B, H, Hkv, M, S, d,
+                                  _scale(scale, d), _stream()))
+    return o, lse
+
+
+def mw_xattn_bwd_workspace_size(B: int, H: int, Hkv: int, M: int, S: int, d: int) -> int:
+    return int(library().mw_xattn_bwd_workspace_size(B, H, Hkv, M, S, d))
+
+
+def mw_xattn_bwd(q, k, v, o, lse, dout, kv_len: Optional[torch.Tensor] = None,
+                 scale: Optional[float] = None, workspace: Optional[torch.Tensor] = None, out=None):
+    """Gradients (dQ, dK, dV) of sum(O * dout) through mw_xattn_fwd; those of K and
+    V are sums over the query heads that share them, and 0 past ``kv_len``.
+
+    ``out`` = (dq, dk, dv) preallocated outputs."""
+    if out is None and workspace is None and _native is not None:
+        r = _native.xattn_bwd(q, k, v, o, lse, dout, kv_len, scale)
+        if r is not None:
+            return r if type(r) is tuple else _check(r)
+    B, H, Hkv, M, S, d = _xattn_shapes(q, k, v, kv_len)
+    for t, n in ((o, "o"), (dout, "dout")):
+        if _bhnd(t, n) != (B, H, M, d):
+            raise ValueError(f"{n} shape {tuple(t.shape)} != q shape {(B, H, M, d)}")
+    _expect(lse, "lse", (B, H, M), torch.float32)
+    dq, dk, dv = out if out is not None else (None, None, None)
+    if out is not None:
+        _expect(dq, "dq", (B, H, M, d))
+        _expect(dk, "dk", (B, Hkv, S, d))
+        _expect(dv, "dv", (B, Hkv, S, d))
+    _on_device(q, (("k", k), ("v", v), ("kv_len", kv_len), ("o", o), ("lse", lse), ("dout", dout),
+                   ("dq", dq), ("dk", dk), ("dv", dv), ("workspace", workspace)))
+    ws_bytes = mw_xattn_bwd_workspace_size(B, H, Hkv, M, S, d)
+    workspace = _workspace(workspace, ws_bytes, q.device)
+    if out is None:
+        dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+    _no_alias((("dq", dq), ("dk", dk), ("dv", dv), ("workspace", workspace)),
+              (("q", q), ("k", k), ("v", v), ("o", o), ("lse", lse), ("dout", dout),
+               ("kv_len", kv_len)))
+    _check(library().mw_xattn_bwd(_ptr(q), _ptr(k), _ptr(v), _ptr(kv_len), _ptr(o), _ptr(lse),
+                                  _ptr(dout), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(workspace),
+                                  ws_bytes, B, H, Hkv, M, S, d, _scale(scale, d), _stream()))
+    return dq, dk, dv
+
+
+_NORM_TYPES = {torch.bfloat16: 0, torch.float32: 1}
+
+
+def _norm_type(t, name: str) -> int:
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor, got {type(t).__name__}")
+    if t.dtype not in _NORM_TYPES:
+        raise TypeError(f"{name} must be bfloat16 or float32, got {t.dtype}")
+    return _NORM_TYPES[t.dtype]
+
+
+def _norm_params(x, weight, bias):
+    """Rows, channels, groups and the parameters' type of a layer norm call."""
+    if x.dim() < 1 or not x.is_contiguous():
+        raise ValueError("x must be a contiguous [..., C] tensor")
+    C = x.shape[-1]
+    rows = x.numel() // C if C else 0
+    groups, ptype, shape = 1, 1, None
+    for t, name in ((weight, "weight"), (bias, "bias")):
+        if t is None:
+            continue
+        kind = _norm_type(t, name)
+        if t.dim() not in (1, 2) or t.shape[-1] != C or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous [C] or [groups, C] tensor, C = {C}, "
+                             f"got {tuple(t.shape)}")
+        if shape is not None and (tuple(t.shape) != shape or kind != ptype):
+            raise ValueError("weight and bias must have one shape and type")
+        shape, ptype = tuple(t.shape), kind
+        groups = t.shape[0] if t.dim() == 2 else 1
+    if groups < 1 or rows % groups:
+        raise ValueError(f"{rows} rows are not a multiple of the {groups} groups of weight or bias")
+    return rows, C, groups, ptype
+
+
+def mw_layernorm_fwd(x: torch.Tensor, weight: Optional[torch.Tensor] = None,
+                     bias: Optional[torch.Tensor] = None, eps: float = 1e-5,
+                     out_dtype: Optional[torch.dtype] = None, need_stats: bool = True,
+                     out: Optional[torch.Tensor] = None):
+    """Layer norm over the last dimension of x [..., C] (bf16 or fp32); returns
+    (y, mean, rstd), the latter two fp32 [...] or None.
+
+    ``weight`` and ``bias``: [C], or [groups, C] with one of each for every one of
+    ``groups`` equal runs of consecutive rows (samples, frames), or None.  y has
+    ``out_dtype`` (None: x's; fp32 only with x in fp32)."""
+    if out is None and _native is not None:
+        r = _native.norm_fwd(x, weight, bias, eps, out_dtype, need_stats)
+        if r is not None:
+            return r if type(r) is tuple else _check(r)
+    xt = _norm_type(x, "x")
+    rows, C, groups, ptype = _norm_params(x, weight, bias)
+    out_dtype = x.dtype if out_dtype is None else out_dtype
+    if out_dtype not in _NORM_TYPES:
+        raise TypeError(f"out_dtype must be bfloat16 or float32, got {out_dtype}")
+    if out is not None:
+        _expect(out, "out", tuple(x.shape), out_dtype)
+    _on_device(x, (("weight", weight), ("bias", bias), ("out", out)))
+    y = torch.empty(x.shape, dtype=out_dtype, device=x.device) if out is None else out
+    mean = rstd = None
+    if need_stats:
+        mean, rstd = (torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+                      for _ in range(2))
+    _no_alias((("out", y),), (("x", x), ("weight", weight), ("bias", bias)))
+    _check(library().mw_layernorm_fwd(_ptr(x), _ptr(weight), _ptr(bias), _ptr(y), _ptr(mean),
+                                      _ptr(rstd), rows, C, groups, float(eps), xt,
+                                      _NORM_TYPES[out_dtype], ptype, _stream()))
+    return y, mean, rstd
+
+
+def mw_layernorm_bwd_workspace_size(rows: int, C: int, groups: int) -> int:
+    return int(library().mw_layernorm_bwd_workspace_size(rows, C, groups))
+
+
+def mw_layernorm_bwd(dy, x, mean, rstd, weight: Optional[torch.Tensor] = None,
+                     bias: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """Gradients (dx, dweight, dbias) of sum(y * dy) through mw_layernorm_fwd, None
+    in the place of a parameter that is None (bias: only its shape is used)."""
+    if workspace is None and _native is not None:
+        r = _native.norm_bwd(dy, x, mean, rstd, weight, bias)
+        if r is not None:
+            return r if type(r) is tuple else _check(r)
+    xt, yt = _norm_type(x, "x"), _norm_type(dy, "dy")
+    rows, C, groups, ptype = _norm_params(x, weight, bias)
+    _expect(dy, "dy", tuple(x.shape), dy.dtype)
+    for t, name in ((mean, "mean"), (rstd, "rstd")):
+        _expect(t, name, tuple(x.shape[:-1]), torch.float32)
+    _on_device(x, (("dy", dy), ("mean", mean), ("rstd", rstd), ("weight", weight), ("bias", bias),
+                   ("workspace", workspace)))
+    params = weight is not None or bias is not None
+    ws_bytes = mw_layernorm_bwd_workspace_size(rows, C, groups) if params else 0
+    workspace = _workspace(workspace, ws_bytes, x.device)
+    dx = torch.empty_like(x)
+    dw = None if weight is None else torch.empty_like(weight)
+    db = None if bias is None else torch.empty_like(bias)
+    _no_alias((("workspace", workspace),), (("dy", dy), ("x", x), ("mean", mean), ("rstd", rstd),
+                                            ("weight", weight)))
+    _check(library().mw_layernorm_bwd(_ptr(dy), _ptr(x), _ptr(mean), _ptr(rstd), _ptr(weight),
+                                      _ptr(dx), _ptr(dw), _ptr(db), _ptr(workspace), ws_bytes,
+                                      rows, C, groups, xt, yt, ptype, _stream()))
+    return dx, dw, db
+
+
 def mw_device_status(clear: bool = True) -> int:
     """Synchronises the current stream and returns the device status code."""
     return int(library().mw_device_status(_stream(), 1 if clear else 0))
@@ -538,3 +754,41 @@ class BlockCausalAttention(torch.autograd.Function):
         q, k, v, o, lse = ctx.saved_tensors
         dq, dk, dv = mw_bca_bwd(q, k, v, o, lse, do.contiguous(), ctx.T_chunk, ctx.scale)
         return dq, dk, dv, None, None
+
+
+class CrossAttention(torch.autograd.Function):
+    """Autograd wrapper: O = cross attention(q, k, v) over the first kv_len states of
+    each sample (None: all)."""
+
+    @staticmethod
+    def forward(ctx, q, k, v, kv_len: Optional[torch.Tensor] = None,
+                scale: Optional[float] = None):
+        o, lse = mw_xattn_fwd(q, k, v, kv_len, scale, need_lse=True)
+        ctx.save_for_backward(q, k, v, o, lse, kv_len)
+        ctx.scale = scale
+        return o
+
+    @staticmethod
+    def backward(ctx, do):
+        q, k, v, o, lse, kv_len = ctx.saved_tensors
+        dq, dk, dv = mw_xattn_bwd(q, k, v, o, lse, do.contiguous(), kv_len, ctx.scale)
+        return dq, dk, dv, None, None
+
+
+class LayerNorm(torch.autograd.Function):
+    """Autograd wrapper: y = layer norm(x) * weight + bias, weight and bias [C], one of
+    each for every group of rows ([groups, C]), or None."""
+
+    @staticmethod
+    def forward(ctx, x, weight: Optional[torch.Tensor] = None,
+                bias: Optional[torch.Tensor] = None, eps: float = 1e-5,
+                out_dtype: Optional[torch.dtype] = None):
+        y, mean, rstd = mw_layernorm_fwd(x, weight, bias, eps, out_dtype)
+        ctx.save_for_backward(x, weight, bias, mean, rstd)
+        return y
+
+    @staticmethod
+    def backward(ctx, dy):
+        x, weight, bias, mean, rstd = ctx.saved_tensors
+        dx, dw, db = mw_layernorm_bwd(dy.contiguous(), x, mean, rstd, weight, bias)
+        return dx, dw, db, None, None

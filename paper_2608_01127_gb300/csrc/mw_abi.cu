@@ -19,6 +19,7 @@
 #include <vector>
 
 #include "mw_bca.h"
+#include "mw_host.h"
 #include "mw_internal.h"
 #include "mw_ptx.cuh"
 
@@ -39,6 +40,10 @@ long long g_opt_budget_ms = 2000;
 long long g_opt_skip_q = 0;
 long long g_opt_group_waves = 3;
 long long g_opt_bwd_group_heads = 0;
+
+}  // namespace
+
+namespace mw {
 
 mw_status fail(mw_status s, const char* fmt, ...) {
   char buf[512];
@@ -103,11 +108,7 @@ mw_status check_tokens(long long BH, long long rows) {
   return MW_OK;
 }
 
-#define MW_TRY(expr)                 \
-  do {                               \
-    mw_status _s = (expr);           \
-    if (_s != MW_OK) return _s;      \
-  } while (0)
+namespace {
 
 PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
   static PFN_cuTensorMapEncodeTiled_v12000 fn = [] {
@@ -164,8 +165,10 @@ thread_local MapKey t_map_keys[kMapCache];
 thread_local CUtensorMap t_maps[kMapCache];
 thread_local int t_map_next = 0;
 
+}  // namespace
+
 mw_status make_map(CUtensorMap* m, const void* ptr, int rows, int BH, int d, const char* name,
-                   int box_rows = mw::kTileRows, bool f32 = false, int cols = 0) {
+                   int box_rows, bool f32, int cols) {
   if (cols == 0) cols = d;
   const MapKey key{ptr, rows, BH, d, box_rows, f32, cols};
   for (int i = 0; i < kMapCache; ++i) {
@@ -208,11 +211,31 @@ int sm_count() {
   return n;
 }
 
+// 3-D map over the bias rows [BH, N_pad, 8] f32: 8 x box_rows boxes with the
+// 32-byte swizzle the tf32 MMA descriptors read
+mw_status encode_bias_map(CUtensorMap* m, const float* bias, int N_pad, int BH, int box_rows) {
+  auto fn = encode_fn();
+  if (!fn) return fail(MW_ERR_CUDA, "cuTensorMapEncodeTiled is unavailable (no CUDA driver?)");
+  cuuint64_t dims[3] = {8, static_cast<cuuint64_t>(N_pad), static_cast<cuuint64_t>(BH)};
+  cuuint64_t strides[2] = {32, static_cast<cuuint64_t>(N_pad) * 32};
+  cuuint32_t box[3] = {8, static_cast<cuuint32_t>(box_rows), 1};
+  cuuint32_t estr[3] = {1, 1, 1};
+  CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, const_cast<float*>(bias), dims, strides,
+                  box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_32B,
+                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) return fail(MW_ERR_CUDA, "cuTensorMapEncodeTiled(bias) failed: %d", (int)r);
+  return MW_OK;
+}
+
 unsigned long long budget_ns() { return static_cast<unsigned long long>(g_opt_budget_ms) * 1000000ull; }
 
-size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
+int debug_skip_q() { return static_cast<int>(g_opt_skip_q); }
 
-int ceil_div(long long a, long long b) { return static_cast<int>((a + b - 1) / b); }
+}  // namespace mw
+
+namespace {
+
+using namespace mw;
 
 // Split-KV count for the cache path: balances (query blocks x splits) CTAs
 // over the SMs against the per-split key-tile count plus a fixed cost.
@@ -341,60 +364,6 @@ BwdWs bwd_ws_layout(int BH, int N_pad, int d) {
   return w;
 }
 
-// 3-D map over the bias rows [BH, N_pad, 8] f32: 8 x box_rows boxes with the
-// 32-byte swizzle the tf32 MMA descriptors read
-mw_status encode_bias_map(CUtensorMap* m, const float* bias, int N_pad, int BH, int box_rows) {
-  auto fn = encode_fn();
-  if (!fn) return fail(MW_ERR_CUDA, "cuTensorMapEncodeTiled is unavailable (no CUDA driver?)");
-  cuuint64_t dims[3] = {8, static_cast<cuuint64_t>(N_pad), static_cast<cuuint64_t>(BH)};
-  cuuint64_t strides[2] = {32, static_cast<cuuint64_t>(N_pad) * 32};
-  cuuint32_t box[3] = {8, static_cast<cuuint32_t>(box_rows), 1};
-  cuuint32_t estr[3] = {1, 1, 1};
-  CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, const_cast<float*>(bias), dims, strides,
-                  box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_32B,
-                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  if (r != CUDA_SUCCESS) return fail(MW_ERR_CUDA, "cuTensorMapEncodeTiled(bias) failed: %d", (int)r);
-  return MW_OK;
-}
-
-// Makes the device of `stream` current on the calling thread for the scope
-// of one entry point (binding its primary context, which driver calls such
-// as cuTensorMapEncodeTiled need on threads where nothing else did), and
-// restores the caller's device afterwards.
-class DeviceScope {
- public:
-  explicit DeviceScope(cudaStream_t stream) {
-    if (cudaGetDevice(&prev_) != cudaSuccess) prev_ = -1;
-    int dev = prev_;
-    // (cudaStreamGetDevice is not allowed on a stream under graph capture,
-    // and a capturing stream belongs to the current device anyway)
-    cudaStreamCaptureStatus cs = cudaStreamCaptureStatusNone;
-    if (stream != nullptr && cudaStreamIsCapturing(stream, &cs) == cudaSuccess &&
-        cs == cudaStreamCaptureStatusNone && cudaStreamGetDevice(stream, &dev) != cudaSuccess)
-      dev = prev_;
-    if (dev < 0) dev = 0;
-    err_ = cudaSetDevice(dev);
-    dev_ = dev;
-  }
-  ~DeviceScope() {
-    if (prev_ >= 0 && prev_ != dev_) cudaSetDevice(prev_);
-  }
-  mw_status status() const {
-    if (err_ != cudaSuccess) return fail(MW_ERR_CUDA, "cudaSetDevice: %s", cudaGetErrorString(err_));
-    return MW_OK;
-  }
-  int device() const { return dev_; }
-
- private:
-  int prev_ = -1, dev_ = 0;
-  cudaError_t err_ = cudaSuccess;
-};
-
-mw_status launch_status(cudaError_t e, const char* what) {
-  if (e != cudaSuccess) return fail(MW_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
-  return ok();
-}
-
 struct RopeArgs {
   int dims = 0;          // 0: off
   mw::RopeFreq omega{};
@@ -471,7 +440,7 @@ mw_status fwd_common(const void* q, const void* k, const void* v, const void* kr
   p.lse = lse;
   p.status = status;
   p.budget_ns = budget_ns();
-  p.debug_skip_q = static_cast<int>(g_opt_skip_q);
+  p.debug_skip_q = debug_skip_q();
   CUtensorMap top = tq;  // the split partials (TMA stores); unused with one split
   if (p.num_splits > 1) {
     const size_t need = cache_ws_bytes(p.num_splits, BH, rows_q, D);
@@ -657,7 +626,7 @@ mw_status mw_bca_bwd_stage(int stage, const void* q, const void* k, const void* 
     p.wide_out = wide_rows(dk, d) && wide_rows(dv, d);
     p.status = status;
     p.budget_ns = budget_ns();
-    p.debug_skip_q = static_cast<int>(g_opt_skip_q);
+    p.debug_skip_q = debug_skip_q();
     MW_TRY(launch_status(mw::launch_bwd_main(D, mma_d(d), tq, tk, tv, tdo, tdq, tbias, p, scope.device(), s),
                          "backward kernel launch"));
   }

@@ -1,0 +1,273 @@
+// C ABI of the conditioning path (declared in include/mw_bca.h): cross attention
+// to an encoder's states and layer norm.  As in mw_abi.cu, arguments are checked
+// on the host before any CUDA call.
+#include <climits>
+#include <cmath>
+
+#include "mw_bca.h"
+#include "mw_host.h"
+#include "mw_internal.h"
+
+using namespace mw;
+
+namespace {
+
+// Sizes of a cross attention call, with the query heads that share a head of K
+// and V as one sequence of rows (they lie one after another in [B, H, M, d]).
+struct XattnSizes {
+  int BH = 0, rows = 0;  // heads of K and V over the batch; query rows of each
+};
+
+mw_status xattn_sizes(XattnSizes* out, int B, int H, int Hkv, int M, int S, int d) {
+  MW_TRY(check_dims(B, H, d));
+  if (Hkv < 1 || H % Hkv != 0)
+    return fail(MW_ERR_INVALID_ARG, "H=%d is not a multiple of Hkv=%d", H, Hkv);
+  if (M < 0 || S < 0 || S > (1 << 24))
+    return fail(MW_ERR_INVALID_ARG, "M=%d and S=%d must be >= 0 and S <= 2^24", M, S);
+  const long long rows = static_cast<long long>(H / Hkv) * M;
+  if (rows > (1 << 24))
+    return fail(MW_ERR_INVALID_ARG, "H/Hkv*M=%lld exceeds 2^24", rows);
+  MW_TRY(check_tokens(static_cast<long long>(B) * Hkv, rows));
+  MW_TRY(check_tokens(static_cast<long long>(B) * Hkv, S));
+  out->BH = B * Hkv;
+  out->rows = static_cast<int>(rows);
+  return MW_OK;
+}
+
+mw_status check_f32(const void* p, const char* name) {
+  if (reinterpret_cast<uintptr_t>(p) & 3u)
+    return fail(MW_ERR_INVALID_ARG, "%s is not 4-byte aligned", name);
+  return MW_OK;
+}
+
+mw_status check_scale(float scale) {
+  if (!(scale > 0.f) || !std::isfinite(scale))
+    return fail(MW_ERR_INVALID_ARG, "scale must be > 0 and finite");
+  return MW_OK;
+}
+
+bool dtype_ok(int t) { return t == MW_BF16 || t == MW_F32; }
+
+mw_status norm_sizes(long long rows, int C, int groups, float eps) {
+  if (C < 1 || C > kNormMaxC)
+    return fail(MW_ERR_UNSUPPORTED, "C=%d channels (supported: 1 to %d)", C, kNormMaxC);
+  if (rows < 0 || rows > INT_MAX)
+    return fail(MW_ERR_INVALID_ARG, "rows=%lld out of range [0, 2^31)", rows);
+  if (groups < 1 || groups > (1 << 24) || rows % groups != 0)
+    return fail(MW_ERR_INVALID_ARG, "rows=%lld is not a multiple of groups=%d", rows, groups);
+  if (!(eps >= 0.f) || !std::isfinite(eps))
+    return fail(MW_ERR_INVALID_ARG, "eps must be >= 0 and finite");
+  return MW_OK;
+}
+
+// Every row of every array can be read and written 16 bytes at a time.
+template <class... P>
+bool vector_rows(int C, P... ptrs) {
+  return C % 8 == 0 && (aligned16(ptrs) && ...);
+}
+
+mw_status check_elems(const void* p, int dtype, const char* name) {
+  if (p == nullptr) return fail(MW_ERR_INVALID_ARG, "%s is NULL", name);
+  if (reinterpret_cast<uintptr_t>(p) & (dtype == MW_F32 ? 3u : 1u))
+    return fail(MW_ERR_INVALID_ARG, "%s is not aligned to its elements", name);
+  return MW_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t mw_xattn_workspace_size(int B, int H, int Hkv, int M, int S, int d) {
+  XattnSizes z;
+  if (xattn_sizes(&z, B, H, Hkv, M, S, d) != MW_OK) return 0;
+  return 0;
+}
+
+mw_status mw_xattn_fwd(const void* q, const void* k, const void* v, const int* kv_len, void* o,
+                       float* lse, void* workspace, size_t ws_bytes, int B, int H, int Hkv, int M,
+                       int S, int d, float scale, void* stream) {
+  XattnSizes z;
+  MW_TRY(xattn_sizes(&z, B, H, Hkv, M, S, d));
+  MW_TRY(check_scale(scale));
+  if (M == 0) return ok();
+  MW_TRY(check_ptr(q, "q"));
+  MW_TRY(check_ptr(o, "o"));
+  if (S > 0) {
+    MW_TRY(check_ptr(k, "k"));
+    MW_TRY(check_ptr(v, "v"));
+  }
+  MW_TRY(check_f32(kv_len, "kv_len"));
+  MW_TRY(check_f32(lse, "lse"));
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  DeviceScope scope(s);
+  MW_TRY(scope.status());
+  XattnParams p{};
+  p.q = static_cast<const __nv_bfloat16*>(q);
+  p.k = static_cast<const __nv_bfloat16*>(k);
+  p.v = static_cast<const __nv_bfloat16*>(v);
+  p.kv_len = kv_len;
+  p.o = static_cast<__nv_bfloat16*>(o);
+  p.lse = lse;
+  p.BH = z.BH;
+  p.heads = Hkv;
+  p.M = z.rows;
+  p.S = S;
+  p.d = d;
+  p.scale = scale;
+  p.scale_log2 = scale * 1.4426950408889634f;
+  return launch_status(launch_xattn_fwd(p, s), "cross attention forward launch");
+}
+
+size_t mw_xattn_bwd_workspace_size(int B, int H, int Hkv, int M, int S, int d) {
+  XattnSizes z;
+  if (xattn_sizes(&z, B, H, Hkv, M, S, d) != MW_OK) return 0;
+  return 0;
+}
+
+mw_status mw_xattn_bwd(const void* q, const void* k, const void* v, const int* kv_len, const void* o,
+                       const float* lse, const void* dout, void* dq, void* dk, void* dv,
+                       void* workspace, size_t ws_bytes, int B, int H, int Hkv, int M, int S, int d,
+                       float scale, void* stream) {
+  XattnSizes z;
+  MW_TRY(xattn_sizes(&z, B, H, Hkv, M, S, d));
+  MW_TRY(check_scale(scale));
+  if (M > 0) {
+    MW_TRY(check_ptr(q, "q"));
+    MW_TRY(check_ptr(o, "o"));
+    MW_TRY(check_ptr(dout, "dout"));
+    MW_TRY(check_ptr(dq, "dq"));
+    if (lse == nullptr) return fail(MW_ERR_INVALID_ARG, "lse is NULL");
+    MW_TRY(check_f32(lse, "lse"));
+  }
+  if (S > 0) {
+    MW_TRY(check_ptr(k, "k"));
+    MW_TRY(check_ptr(v, "v"));
+    MW_TRY(check_ptr(dk, "dk"));
+    MW_TRY(check_ptr(dv, "dv"));
+  }
+  MW_TRY(check_f32(kv_len, "kv_len"));
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  DeviceScope scope(s);
+  MW_TRY(scope.status());
+  XattnParams p{};
+  p.q = static_cast<const __nv_bfloat16*>(q);
+  p.k = static_cast<const __nv_bfloat16*>(k);
+  p.v = static_cast<const __nv_bfloat16*>(v);
+  p.kv_len = kv_len;
+  p.o = static_cast<__nv_bfloat16*>(const_cast<void*>(o));
+  p.lse = const_cast<float*>(lse);
+  p.BH = z.BH;
+  p.heads = Hkv;
+  p.M = z.rows;
+  p.S = S;
+  p.d = d;
+  p.scale = scale;
+  p.scale_log2 = scale * 1.4426950408889634f;
+  p.dout = static_cast<const __nv_bfloat16*>(dout);
+  p.dq = static_cast<__nv_bfloat16*>(dq);
+  p.dk = static_cast<__nv_bfloat16*>(dk);
+  p.dv = static_cast<__nv_bfloat16*>(dv);
+  return launch_status(launch_xattn_bwd(p, s), "cross attention backward launch");
+}
+
+mw_status mw_layernorm_fwd(const void* x, const void* weight, const void* bias, void* y, float* mean,
+                           float* rstd, long long rows, int C, int groups, float eps, int x_dtype,
+                           int y_dtype, int param_dtype, void* stream) {
+  MW_TRY(norm_sizes(rows, C, groups, eps));
+  if (!dtype_ok(x_dtype) || !dtype_ok(y_dtype) || !dtype_ok(param_dtype))
+    return fail(MW_ERR_INVALID_ARG, "types must be MW_BF16 or MW_F32");
+  if (x_dtype == MW_BF16 && y_dtype == MW_F32)
+    return fail(MW_ERR_UNSUPPORTED, "y in fp32 needs x in fp32");
+  if (rows == 0) return ok();
+  MW_TRY(check_elems(x, x_dtype, "x"));
+  MW_TRY(check_elems(y, y_dtype, "y"));
+  if (weight) MW_TRY(check_elems(weight, param_dtype, "weight"));
+  if (bias) MW_TRY(check_elems(bias, param_dtype, "bias"));
+  MW_TRY(check_f32(mean, "mean"));
+  MW_TRY(check_f32(rstd, "rstd"));
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  DeviceScope scope(s);
+  MW_TRY(scope.status());
+  NormParams p{};
+  p.x = x;
+  p.weight = weight;
+  p.bias = bias;
+  p.y = y;
+  p.mean = mean;
+  p.rstd = rstd;
+  p.rows = rows;
+  p.rows_per_group = rows / groups;
+  p.C = C;
+  p.groups = groups;
+  p.eps = eps;
+  p.x_f32 = x_dtype == MW_F32;
+  p.y_f32 = y_dtype == MW_F32;
+  p.param_f32 = param_dtype == MW_F32;
+  return launch_status(launch_norm_fwd(p, vector_rows(C, x, weight, bias, y), sm_count(), s),
+                       "layer norm forward launch");
+}
+
+size_t mw_layernorm_bwd_workspace_size(long long rows, int C, int groups) {
+  if (norm_sizes(rows, C, groups, 0.f) != MW_OK || rows == 0) return 0;
+  const int parts = norm_parts(rows / groups, groups, kNormSms);
+  return parts > 1 ? align256(static_cast<size_t>(groups) * parts * 2 * C * sizeof(float)) : 0;
+}
+
+mw_status mw_layernorm_bwd(const void* dy, const void* x, const float* mean, const float* rstd,
+                           const void* weight, void* dx, void* dweight, void* dbias, void* workspace,
+                           size_t ws_bytes, long long rows, int C, int groups, int x_dtype,
+                           int y_dtype, int param_dtype, void* stream) {
+  MW_TRY(norm_sizes(rows, C, groups, 0.f));
+  if (!dtype_ok(x_dtype) || !dtype_ok(y_dtype) || !dtype_ok(param_dtype))
+    return fail(MW_ERR_INVALID_ARG, "types must be MW_BF16 or MW_F32");
+  if (x_dtype == MW_BF16 && y_dtype == MW_F32)
+    return fail(MW_ERR_UNSUPPORTED, "y in fp32 needs x in fp32");
+  if (weight) MW_TRY(check_elems(weight, param_dtype, "weight"));
+  if (dweight) MW_TRY(check_elems(dweight, param_dtype, "dweight"));
+  if (dbias) MW_TRY(check_elems(dbias, param_dtype, "dbias"));
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (rows == 0) {
+    DeviceScope scope(s);
+    MW_TRY(scope.status());
+    const size_t bytes = static_cast<size_t>(groups) * C * (param_dtype == MW_F32 ? 4 : 2);
+    for (void* g : {dweight, dbias})
+      if (g) MW_TRY(launch_status(cudaMemsetAsync(g, 0, bytes, s), "clearing a gradient"));
+    return ok();
+  }
+  MW_TRY(check_elems(dy, y_dtype, "dy"));
+  MW_TRY(check_elems(x, x_dtype, "x"));
+  MW_TRY(check_elems(dx, x_dtype, "dx"));
+  MW_TRY(check_elems(mean, MW_F32, "mean"));
+  MW_TRY(check_elems(rstd, MW_F32, "rstd"));
+  const size_t need = dweight || dbias ? mw_layernorm_bwd_workspace_size(rows, C, groups) : 0;
+  if (need > 0) {
+    if (workspace == nullptr || ws_bytes < need)
+      return fail(MW_ERR_WORKSPACE, "workspace %zu bytes, need %zu", ws_bytes, need);
+    if (reinterpret_cast<uintptr_t>(workspace) & 255u)
+      return fail(MW_ERR_INVALID_ARG, "workspace is not 256-byte aligned");
+  }
+  DeviceScope scope(s);
+  MW_TRY(scope.status());
+  NormParams p{};
+  p.dy = dy;
+  p.x = x;
+  p.mean = const_cast<float*>(mean);
+  p.rstd = const_cast<float*>(rstd);
+  p.weight = weight;
+  p.dx = dx;
+  p.dweight = dweight;
+  p.dbias = dbias;
+  p.partial = static_cast<float*>(workspace);
+  p.rows = rows;
+  p.rows_per_group = rows / groups;
+  p.C = C;
+  p.groups = groups;
+  p.parts = norm_parts(rows / groups, groups, kNormSms);
+  p.x_f32 = x_dtype == MW_F32;
+  p.y_f32 = y_dtype == MW_F32;
+  p.param_f32 = param_dtype == MW_F32;
+  return launch_status(launch_norm_bwd(p, vector_rows(C, dy, x, weight, dx), scope.device(), s),
+                       "layer norm backward launch");
+}
+
+}  // extern "C"

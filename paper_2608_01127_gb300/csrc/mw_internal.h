@@ -190,4 +190,56 @@ cudaError_t launch_qkv_rope(const __nv_bfloat16* qkv, __nv_bfloat16* q, __nv_bfl
                             const RopeFreq& omega, int per_frame, int first_frame,
                             cudaStream_t s);
 
+
+// Layer norm (mw_norm.cu).
+constexpr int kNormMaxC = 8192;
+// The SMs that the backward's parts are planned for (a GB300's, so that the plan
+// needs no device).
+constexpr int kNormSms = 152;
+struct NormParams {
+  const void* x;       // [rows, C], bf16 or fp32
+  const void* weight;  // [groups, C] or null (all 1)
+  const void* bias;    // [groups, C] or null (all 0)
+  void* y;             // forward: [rows, C], bf16 or fp32
+  float* mean;         // [rows]; forward: nullable
+  float* rstd;
+  const void* dy;      // backward: y's type
+  void* dx;            // x's type
+  void* dweight;       // the parameters' type, nullable
+  void* dbias;
+  float* partial;      // [groups * parts, 2, C] where parts > 1
+  long long rows, rows_per_group;
+  int C, groups;
+  int parts;           // backward: blocks that share a group's rows
+  int W;               // warps that share a row (set by the launcher)
+  float eps;
+  bool x_f32, y_f32, param_f32;
+};
+// Blocks a group of the backward.
+int norm_parts(long long rows_per_group, int groups, int sms);
+// vec: C is a multiple of 8 and every pointer 16-byte aligned
+cudaError_t launch_norm_fwd(NormParams p, bool vec, int sms, cudaStream_t s);
+cudaError_t launch_norm_bwd(NormParams p, bool vec, int dev, cudaStream_t s);
+
+// Cross attention (mw_xattn.cu): BH heads of K and V [BH, S, d], each with M rows of
+// Q (those of all the query heads that share it, which lie one after another);
+// head bh belongs to sample bh / heads, whose first kv_len[...] keys count.
+struct XattnParams {
+  const __nv_bfloat16* q;
+  const __nv_bfloat16* k;
+  const __nv_bfloat16* v;
+  const int* kv_len;   // [BH / heads], nullable: all S
+  __nv_bfloat16* o;
+  float* lse;          // nullable
+  int BH, heads, M, S, d;
+  float scale, scale_log2;
+  // backward
+  const __nv_bfloat16* dout;
+  __nv_bfloat16* dq;
+  __nv_bfloat16* dk;
+  __nv_bfloat16* dv;
+};
+cudaError_t launch_xattn_fwd(const XattnParams& p, cudaStream_t s);
+cudaError_t launch_xattn_bwd(const XattnParams& p, cudaStream_t s);
+
 }  // namespace mw

@@ -1,0 +1,376 @@
+// Layer norm over the channels of a row, forward and backward, with one weight
+// and bias for every group of rows (one group: the usual layer norm; a group a
+// sample or a frame: the adaptive modulation of Sec. 4.1's blocks).
+//
+//   mean = sum x / C, rstd = 1 / sqrt(sum (x - mean)^2 / C + eps),
+//   xh = (x - mean) rstd, y = xh w_g + b_g
+//   g = dy w_g, dx = rstd (g - sum g / C - xh sum(g xh) / C),
+//   dw_g = sum of dy xh over the group's rows, db_g = sum of dy
+//
+// Bound by HBM: a row is read once into registers and stays there (the variance
+// is the second pass over the registers, in fp32 as all sums).  W warps share a
+// row, so that a thread holds at most V accesses of VEC elements: VEC = 8 where
+// rows start at multiples of 16 bytes, else 1 (any width, any alignment).
+// Backward: a block takes a range of one group's rows, its threads keep the
+// sums of their columns in registers over all of them, and leave one partial
+// [2, C] a block; a second kernel adds the blocks' partials of a group in their
+// order, so that results do not depend on timing.
+#include "mw_internal.h"
+#include "mw_ptx.cuh"
+
+namespace mw {
+namespace {
+
+using bf16 = __nv_bfloat16;
+
+template <int VEC>
+__device__ __forceinline__ void load(const float* p, float (&v)[VEC]) {
+  if constexpr (VEC == 8) {
+    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w;
+    v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+  } else {
+    v[0] = *p;
+  }
+}
+template <int VEC>
+__device__ __forceinline__ void load(const bf16* p, float (&v)[VEC]) {
+  if constexpr (VEC == 8) {
+    const uint4 a = *reinterpret_cast<const uint4*>(p);
+    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      v[2 * k] = __uint_as_float(w[k] << 16);
+      v[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
+    }
+  } else {
+    v[0] = __bfloat162float(*p);
+  }
+}
+template <int VEC>
+__device__ __forceinline__ void store(float* p, const float (&v)[VEC]) {
+  if constexpr (VEC == 8) {
+    reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+    reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+  } else {
+    *p = v[0];
+  }
+}
+template <int VEC>
+__device__ __forceinline__ void store(bf16* p, const float (&v)[VEC]) {
+  if constexpr (VEC == 8)
+    *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]),
+                                              pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+  else
+    *p = __float2bfloat16(v[0]);
+}
+// a weight, bias or a gradient of one: fp32 or bf16
+template <int VEC>
+__device__ __forceinline__ void load_param(const void* base, bool f32, size_t i, float (&v)[VEC]) {
+  if (f32)
+    load<VEC>(static_cast<const float*>(base) + i, v);
+  else
+    load<VEC>(static_cast<const bf16*>(base) + i, v);
+}
+__device__ __forceinline__ void store_param(void* base, bool f32, size_t i, float v) {
+  if (f32)
+    static_cast<float*>(base)[i] = v;
+  else
+    static_cast<bf16*>(base)[i] = __float2bfloat16(v);
+}
+
+// A block's threads: teams of W warps, a row each.
+struct Team {
+  int W, index, count, t, warp;  // t: thread of the team
+  __device__ explicit Team(int W_) : W(W_) {
+    const int w = threadIdx.x >> 5;
+    index = w / W;
+    count = (blockDim.x >> 5) / W;
+    warp = w % W;
+    t = warp * 32 + (threadIdx.x & 31);
+  }
+  // Sums over the team in a fixed order; red: two floats a warp of the block.
+  // (A barrier a call is enough where calls alternate between two buffers.)
+  __device__ float2 sum(float2 v, float2* red) const {
+#pragma unroll
+    for (int s = 16; s > 0; s >>= 1) {
+      v.x += __shfl_xor_sync(0xffffffffu, v.x, s);
+      v.y += __shfl_xor_sync(0xffffffffu, v.y, s);
+    }
+    if (W == 1) return v;
+    if ((threadIdx.x & 31) == 0) red[index * W + warp] = v;
+    asm volatile("bar.sync %0, %1;" ::"r"(index + 1), "r"(W * 32) : "memory");
+    float2 s = red[index * W];
+    for (int w = 1; w < W; ++w) {
+      const float2 a = red[index * W + w];
+      s.x += a.x;
+      s.y += a.y;
+    }
+    return s;
+  }
+};
+
+template <class TX, class TY, int VEC, int V>
+__global__ void __launch_bounds__(512) norm_fwd_kernel(const NormParams p) {
+  __shared__ float2 red[2][16];
+  const Team team(p.W);
+  const TX* x = static_cast<const TX*>(p.x);
+  TY* y = static_cast<TY*>(p.y);
+  const float inv_c = 1.f / static_cast<float>(p.C);
+  pdl_wait();
+  pdl_trigger();
+  for (long long row = static_cast<long long>(blockIdx.x) * team.count + team.index; row < p.rows;
+       row += static_cast<long long>(gridDim.x) * team.count) {
+    float v[V][VEC];
+    float s = 0.f;
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      const int c = (k * team.W * 32 + team.t) * VEC;
+      if (c < p.C) {
+        load<VEC>(x + row * p.C + c, v[k]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) v[k][e] = 0.f;
+      }
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) s += v[k][e];
+    }
+    const float mean = team.sum(make_float2(s, 0.f), red[0]).x * inv_c;
+    float q = 0.f;
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      const int c = (k * team.W * 32 + team.t) * VEC;
+      if (c >= p.C) continue;
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        v[k][e] -= mean;
+        q = fmaf(v[k][e], v[k][e], q);
+      }
+    }
+    const float rstd = rsqrtf(team.sum(make_float2(q, 0.f), red[1]).x * inv_c + p.eps);
+    const size_t g = p.groups == 1 ? 0 : static_cast<size_t>(row / p.rows_per_group) * p.C;
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      const int c = (k * team.W * 32 + team.t) * VEC;
+      if (c >= p.C) continue;
+      float w[VEC], b[VEC];
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) w[e] = 1.f, b[e] = 0.f;
+      if (p.weight) load_param<VEC>(p.weight, p.param_f32, g + c, w);
+      if (p.bias) load_param<VEC>(p.bias, p.param_f32, g + c, b);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) v[k][e] = fmaf(v[k][e] * rstd, w[e], b[e]);
+      store<VEC>(y + row * p.C + c, v[k]);
+    }
+    if (team.t == 0) {
+      if (p.mean) p.mean[row] = mean;
+      if (p.rstd) p.rstd[row] = rstd;
+    }
+  }
+}
+
+// Block (part, group): rows [part n / parts, (part + 1) n / parts) of the group.
+template <class TX, class TY, int VEC, int V>
+__global__ void __launch_bounds__(512) norm_bwd_kernel(const NormParams p) {
+  __shared__ float2 red[2][16];
+  extern __shared__ float sums[];  // [2][C]
+  const Team team(p.W);
+  const TX* x = static_cast<const TX*>(p.x);
+  const TY* dy = static_cast<const TY*>(p.dy);
+  TX* dx = static_cast<TX*>(p.dx);
+  const float inv_c = 1.f / static_cast<float>(p.C);
+  const int part = blockIdx.x % p.parts;
+  const long long group = blockIdx.x / p.parts;
+  const long long n = p.rows_per_group;
+  const long long r0 = group * n + part * n / p.parts, r1 = group * n + (part + 1) * n / p.parts;
+  const size_t g = static_cast<size_t>(group) * p.C;
+  float aw[V][VEC], ab[V][VEC];
+#pragma unroll
+  for (int k = 0; k < V; ++k)
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) aw[k][e] = ab[k][e] = 0.f;
+  int turn = 0;
+  for (long long row = r0 + team.index; row < r1; row += team.count, turn ^= 1) {
+    const float mean = p.mean[row], rstd = p.rstd[row];
+    float xh[V][VEC], gr[V][VEC];
+    float2 s = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      const int c = (k * team.W * 32 + team.t) * VEC;
+      if (c < p.C) {
+        load<VEC>(x + row * p.C + c, xh[k]);
+        load<VEC>(dy + row * p.C + c, gr[k]);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      const int c = (k * team.W * 32 + team.t) * VEC;
+      if (c >= p.C) continue;
+      float w[VEC];
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) w[e] = 1.f;
+      if (p.weight) load_param<VEC>(p.weight, p.param_f32, g + c, w);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        xh[k][e] = (xh[k][e] - mean) * rstd;
+        aw[k][e] = fmaf(gr[k][e], xh[k][e], aw[k][e]);
+        ab[k][e] += gr[k][e];
+        gr[k][e] *= w[e];
+        s.x += gr[k][e];
+        s.y = fmaf(gr[k][e], xh[k][e], s.y);
+      }
+    }
+    s = team.sum(s, red[turn]);
+    const float m1 = s.x * inv_c, m2 = s.y * inv_c;
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      const int c = (k * team.W * 32 + team.t) * VEC;
+      if (c >= p.C) continue;
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) gr[k][e] = rstd * (gr[k][e] - m1 - xh[k][e] * m2);
+      store<VEC>(dx + row * p.C + c, gr[k]);
+    }
+  }
+  if (!p.dweight && !p.dbias) return;
+  for (int t = 0; t < team.count; ++t) {
+    if (team.index == t) {
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        const int c = (k * team.W * 32 + team.t) * VEC;
+        if (c >= p.C) continue;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          sums[c + e] = t == 0 ? aw[k][e] : sums[c + e] + aw[k][e];
+          sums[p.C + c + e] = t == 0 ? ab[k][e] : sums[p.C + c + e] + ab[k][e];
+        }
+      }
+    }
+    __syncthreads();
+  }
+  for (int c = threadIdx.x; c < 2 * p.C; c += blockDim.x) {
+    if (p.parts > 1)
+      p.partial[static_cast<size_t>(blockIdx.x) * 2 * p.C + c] = sums[c];
+    else if (c < p.C ? p.dweight != nullptr : p.dbias != nullptr)
+      store_param(c < p.C ? p.dweight : p.dbias, p.param_f32, g + (c < p.C ? c : c - p.C), sums[c]);
+  }
+}
+
+// dw and db of a group from its blocks' partials: 32 columns a block, the parts
+// over its 16 warps.
+__global__ void __launch_bounds__(512) norm_params_kernel(const NormParams p) {
+  __shared__ float sums[16][33];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int c = blockIdx.x * 32 + lane;
+  for (int g = blockIdx.y; g < p.groups; g += gridDim.y) {
+    float s = 0.f;
+    if (c < 2 * p.C) {
+      const float* in = p.partial + static_cast<size_t>(g) * p.parts * 2 * p.C + c;
+#pragma unroll 4
+      for (int i = warp; i < p.parts; i += 16) s += in[static_cast<size_t>(i) * 2 * p.C];
+    }
+    sums[warp][lane] = s;
+    __syncthreads();
+    if (warp == 0 && c < 2 * p.C) {
+      for (int w = 1; w < 16; ++w) s += sums[w][lane];
+      void* out = c < p.C ? p.dweight : p.dbias;
+      if (out) store_param(out, p.param_f32, static_cast<size_t>(g) * p.C + (c < p.C ? c : c - p.C), s);
+    }
+    __syncthreads();
+  }
+}
+
+// Warps a row and accesses a thread: the fewest slots that hold the row (the
+// fewest warps of those), VEC = 8 up to 4 accesses, VEC = 1 up to 16.
+struct Shape {
+  int W, V, threads;
+};
+Shape shape_of(int C, bool vec) {
+  const int elems = vec ? 256 : 32, max_v = vec ? 4 : 16, max_w = vec ? 8 : 16;
+  Shape best{0, 0, 0};
+  for (int W = 1; W <= max_w; ++W) {
+    int V = (C + elems * W - 1) / (elems * W);
+    if (!vec) V = V <= 2 ? 2 : V <= 4 ? 4 : V <= 8 ? 8 : V;
+    if (!vec && V > 8) V = V <= 16 ? 16 : V;
+    if (V > max_v) continue;
+    if (best.W == 0 || W * V < best.W * best.V) best = {W, V, 0};
+  }
+  best.threads = 32 * best.W * (best.W < 8 ? 8 / best.W : 1);
+  return best;
+}
+
+template <class X, class Y, int VEC, int V>
+struct Kernels {
+  static constexpr auto fwd = norm_fwd_kernel<X, Y, VEC, V>;
+  static constexpr auto bwd = norm_bwd_kernel<X, Y, VEC, V>;
+};
+
+// f of the kernels for these types and accesses a thread.
+template <class F>
+cudaError_t by_shape(const NormParams& p, bool vec, int V, F&& f) {
+  auto types = [&](auto tx, auto ty) {
+    using X = decltype(tx);
+    using Y = decltype(ty);
+    if (vec) {
+      switch (V) {
+        case 1: return f(Kernels<X, Y, 8, 1>{});
+        case 2: return f(Kernels<X, Y, 8, 2>{});
+        case 3: return f(Kernels<X, Y, 8, 3>{});
+        default: return f(Kernels<X, Y, 8, 4>{});
+      }
+    }
+    switch (V) {
+      case 2: return f(Kernels<X, Y, 1, 2>{});
+      case 4: return f(Kernels<X, Y, 1, 4>{});
+      case 8: return f(Kernels<X, Y, 1, 8>{});
+      default: return f(Kernels<X, Y, 1, 16>{});
+    }
+  };
+  if (!p.x_f32) return types(bf16{}, bf16{});
+  if (!p.y_f32) return types(float{}, bf16{});
+  return types(float{}, float{});
+}
+
+}  // namespace
+
+int norm_parts(long long rows_per_group, int groups, int sms) {
+  long long parts = 2ll * sms / groups;
+  if (parts > rows_per_group) parts = rows_per_group;
+  return parts < 1 ? 1 : static_cast<int>(parts);
+}
+
+cudaError_t launch_norm_fwd(NormParams p, bool vec, int sms, cudaStream_t s) {
+  const Shape sh = shape_of(p.C, vec);
+  p.W = sh.W;
+  const int teams = sh.threads / 32 / sh.W;
+  const long long blocks = (p.rows + teams - 1) / teams;
+  const unsigned grid = static_cast<unsigned>(blocks < (1 << 20) ? blocks : (1 << 20));
+  cudaLaunchConfig_t cfg;
+  cudaLaunchAttribute attr;
+  pdl_config(cfg, attr, dim3(grid), dim3(sh.threads), 0, s);
+  return by_shape(p, vec, sh.V, [&](auto k) { return cudaLaunchKernelEx(&cfg, k.fwd, p); });
+}
+
+cudaError_t launch_norm_bwd(NormParams p, bool vec, int dev, cudaStream_t s) {
+  const Shape sh = shape_of(p.C, vec);
+  p.W = sh.W;
+  const size_t smem = static_cast<size_t>(2) * p.C * sizeof(float);
+  const unsigned grid = static_cast<unsigned>(p.groups) * p.parts;
+  cudaError_t e = by_shape(p, vec, sh.V, [&](auto k) {
+    constexpr auto bwd = decltype(k)::bwd;
+    if (smem > 48 * 1024) {
+      static OncePerDevice prepared;
+      const cudaError_t e0 = prepared(dev, [&] {
+        return cudaFuncSetAttribute(bwd, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                    2 * kNormMaxC * static_cast<int>(sizeof(float)));
+      });
+      if (e0 != cudaSuccess) return e0;
+    }
+    bwd<<<grid, sh.threads, smem, s>>>(p);
+    return cudaGetLastError();
+  });
+  if (e != cudaSuccess || p.parts == 1 || (!p.dweight && !p.dbias)) return e;
+  norm_params_kernel<<<dim3((2 * p.C + 31) / 32, p.groups < 65535 ? p.groups : 65535), 512, 0, s>>>(p);
+  return cudaGetLastError();
+}
+
+}  // namespace mw

@@ -21,6 +21,7 @@
 #include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -28,6 +29,7 @@
 #include <climits>
 #include <cmath>
 #include <initializer_list>
+#include <vector>
 
 #include "mw_bca.h"
 
@@ -40,6 +42,13 @@ decltype(&mw_bca_cache_workspace_size) p_cache_ws = nullptr;
 decltype(&mw_bca_cache_fwd_rope) p_cache = nullptr;
 decltype(&mw_bca_cache_step) p_step = nullptr;
 decltype(&mw_qkv_rope_split) p_qkv = nullptr;
+decltype(&mw_xattn_workspace_size) p_xattn_ws = nullptr;
+decltype(&mw_xattn_fwd) p_xattn = nullptr;
+decltype(&mw_xattn_bwd_workspace_size) p_xattn_bwd_ws = nullptr;
+decltype(&mw_xattn_bwd) p_xattn_bwd = nullptr;
+decltype(&mw_layernorm_fwd) p_norm = nullptr;
+decltype(&mw_layernorm_bwd_workspace_size) p_norm_bwd_ws = nullptr;
+decltype(&mw_layernorm_bwd) p_norm_bwd = nullptr;
 
 // A tensor this module may look into: exactly a torch.Tensor or Parameter,
 // strided, with storage of its own (no fake, batched or other wrapper).
@@ -175,12 +184,13 @@ auto call(F&& f) {
 }
 
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (n != 7) {
-    PyErr_SetString(PyExc_TypeError, "bind takes 7 addresses");
+  constexpr int kEntries = 14;
+  if (n != kEntries) {
+    PyErr_SetString(PyExc_TypeError, "bind takes 14 addresses");
     return nullptr;
   }
-  void* p[7];
-  for (int i = 0; i < 7; ++i) {
+  void* p[kEntries];
+  for (int i = 0; i < kEntries; ++i) {
     p[i] = PyLong_AsVoidPtr(a[i]);
     if (!p[i]) {
       if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "null address");
@@ -194,6 +204,13 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
   p_cache = reinterpret_cast<decltype(p_cache)>(p[4]);
   p_step = reinterpret_cast<decltype(p_step)>(p[5]);
   p_qkv = reinterpret_cast<decltype(p_qkv)>(p[6]);
+  p_xattn_ws = reinterpret_cast<decltype(p_xattn_ws)>(p[7]);
+  p_xattn = reinterpret_cast<decltype(p_xattn)>(p[8]);
+  p_xattn_bwd_ws = reinterpret_cast<decltype(p_xattn_bwd_ws)>(p[9]);
+  p_xattn_bwd = reinterpret_cast<decltype(p_xattn_bwd)>(p[10]);
+  p_norm = reinterpret_cast<decltype(p_norm)>(p[11]);
+  p_norm_bwd_ws = reinterpret_cast<decltype(p_norm_bwd_ws)>(p[12]);
+  p_norm_bwd = reinterpret_cast<decltype(p_norm_bwd)>(p[13]);
   Py_RETURN_NONE;
 }
 
@@ -397,6 +414,223 @@ PyObject* qkv(PyObject*, PyObject* const* a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// K and V of a cross attention and the valid states of its samples (null: all).
+struct States {
+  const at::Tensor *k = nullptr, *v = nullptr, *len = nullptr;
+  bool read(const at::Tensor* q, PyObject* ko, PyObject* vo, PyObject* lo) {
+    k = bf16(ko, 4);
+    v = bf16(vo, 4);
+    if (!q || !k || !v || k->sizes() != v->sizes() || !fits(*q) || !fits(*k) ||
+        k->size(0) != q->size(0) || k->size(3) != q->size(3) || k->size(1) < 1 ||
+        q->size(1) % k->size(1))
+      return false;
+    if (lo == Py_None) return true;
+    len = tensor(lo);
+    return len && len->scalar_type() == at::kInt && len->dim() == 1 && len->size(0) == q->size(0);
+  }
+  const int* lens() const { return len ? static_cast<const int*>(len->const_data_ptr()) : nullptr; }
+};
+
+// xattn_fwd(q, k, v, kv_len, scale, need_lse, workspace) -> (o, lse or None)
+PyObject* xattn_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 7 || !p_xattn || a[6] != Py_None) return none();
+  const at::Tensor* q = bf16(a[0], 4);
+  States st;
+  c10::DeviceIndex dev;
+  float scale;
+  if (!st.read(q, a[1], a[2], a[3]) || !one_device({q, st.k, st.v, st.len}, &dev) ||
+      !softmax_scale(a[4], q->size(3), &scale) || !PyBool_Check(a[5]))
+    return none();
+  const Shape sh = shape(*q);
+  const at::TensorOptions options = q->options();
+  const int B = static_cast<int>(sh[0]), H = static_cast<int>(sh[1]), M = static_cast<int>(sh[2]);
+  const int Hkv = static_cast<int>(st.k->size(1)), S = static_cast<int>(st.k->size(2));
+  const int d = static_cast<int>(sh[3]);
+  const size_t bytes = p_xattn_ws(B, H, Hkv, M, S, d);
+  const void *pq = q->const_data_ptr(), *pk = st.k->const_data_ptr(), *pv = st.v->const_data_ptr();
+  const int* lens = st.lens();
+  const bool need_lse = a[5] == Py_True;
+  at::Tensor o, lse, ws;
+  mw_status s = MW_OK;
+  const bool real = call([&] {
+    o = at::empty(sh, options);
+    if (need_lse) lse = rows_f32(sh, options);
+    if (bytes) ws = scratch(bytes, options);
+    if (!is_real(o) || (need_lse && !is_real(lse)) || (bytes && !is_real(ws))) return false;
+    s = p_xattn(pq, pk, pv, lens, o.mutable_data_ptr(),
+                need_lse ? static_cast<float*>(lse.mutable_data_ptr()) : nullptr,
+                bytes ? ws.mutable_data_ptr() : nullptr, bytes, B, H, Hkv, M, S, d, scale,
+                c10::cuda::getCurrentCUDAStream(dev).stream());
+    return true;
+  });
+  if (!real) return none();
+  if (s != MW_OK) return PyLong_FromLong(s);
+  return result({&o, &lse});
+  END_HANDLE_TH_ERRORS
+}
+
+// xattn_bwd(q, k, v, o, lse, dout, kv_len, scale) -> (dq, dk, dv)
+PyObject* xattn_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 8 || !p_xattn_bwd) return none();
+  const at::Tensor *q = bf16(a[0], 4), *o = bf16(a[3], 4), *lse = tensor(a[4]), *dout = bf16(a[5], 4);
+  States st;
+  c10::DeviceIndex dev;
+  float scale;
+  if (!st.read(q, a[1], a[2], a[6]) || !o || !lse || !dout || o->sizes() != q->sizes() ||
+      dout->sizes() != q->sizes() || lse->scalar_type() != at::kFloat ||
+      lse->sizes() != q->sizes().slice(0, 3) ||
+      !one_device({q, st.k, st.v, st.len, o, lse, dout}, &dev) ||
+      !softmax_scale(a[7], q->size(3), &scale))
+    return none();
+  const Shape sh = shape(*q), ks = shape(*st.k);
+  const at::TensorOptions options = q->options();
+  const int B = static_cast<int>(sh[0]), H = static_cast<int>(sh[1]), M = static_cast<int>(sh[2]);
+  const int Hkv = static_cast<int>(ks[1]), S = static_cast<int>(ks[2]), d = static_cast<int>(sh[3]);
+  const size_t bytes = p_xattn_bwd_ws(B, H, Hkv, M, S, d);
+  const void *pq = q->const_data_ptr(), *pk = st.k->const_data_ptr(), *pv = st.v->const_data_ptr();
+  const void *po = o->const_data_ptr(), *pdo = dout->const_data_ptr();
+  const float* pl = static_cast<const float*>(lse->const_data_ptr());
+  const int* lens = st.lens();
+  at::Tensor ws, dq, dk, dv;
+  mw_status s = MW_OK;
+  const bool real = call([&] {
+    if (bytes) ws = scratch(bytes, options);
+    dq = at::empty(sh, options);
+    dk = at::empty(ks, options);
+    dv = at::empty(ks, options);
+    if ((bytes && !is_real(ws)) || !is_real(dq) || !is_real(dk) || !is_real(dv)) return false;
+    s = p_xattn_bwd(pq, pk, pv, lens, po, pl, pdo, dq.mutable_data_ptr(), dk.mutable_data_ptr(),
+                    dv.mutable_data_ptr(), bytes ? ws.mutable_data_ptr() : nullptr, bytes, B, H,
+                    Hkv, M, S, d, scale, c10::cuda::getCurrentCUDAStream(dev).stream());
+    return true;
+  });
+  if (!real) return none();
+  if (s != MW_OK) return PyLong_FromLong(s);
+  return result({&dq, &dk, &dv});
+  END_HANDLE_TH_ERRORS
+}
+
+// Type codes of the layer norm's arrays (-1: another type).
+int norm_type(at::ScalarType t) { return t == at::kBFloat16 ? MW_BF16 : t == at::kFloat ? MW_F32 : -1; }
+
+// The arrays of a layer norm call.
+struct Norm {
+  const at::Tensor *x = nullptr, *w = nullptr, *b = nullptr;
+  int xt = -1, pt = MW_F32, C = 0, groups = 1;
+  int64_t rows = 0;
+  bool read(PyObject* xo, PyObject* wo, PyObject* bo) {
+    x = tensor(xo);
+    if (!x || x->dim() < 1 || (xt = norm_type(x->scalar_type())) < 0) return false;
+    const int64_t c = x->size(-1);
+    if (c < 1 || c > INT_MAX) return false;
+    C = static_cast<int>(c);
+    rows = x->numel() / c;
+    if (wo != Py_None && !(w = tensor(wo))) return false;
+    if (bo != Py_None && !(b = tensor(bo))) return false;
+    for (const at::Tensor* t : {w, b}) {
+      if (!t) continue;
+      pt = norm_type(t->scalar_type());
+      if (pt < 0 || t->dim() < 1 || t->dim() > 2 || t->size(-1) != c) return false;
+      const int64_t g = t->dim() == 2 ? t->size(0) : 1;
+      if (g < 1 || g > INT_MAX) return false;
+      groups = static_cast<int>(g);
+    }
+    if (w && b && (w->scalar_type() != b->scalar_type() || w->sizes() != b->sizes())) return false;
+    return rows % groups == 0;
+  }
+};
+
+// norm_fwd(x, weight, bias, eps, out_dtype, need_stats) -> (y, mean or None, rstd or None)
+PyObject* norm_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 6 || !p_norm) return none();
+  Norm t;
+  c10::DeviceIndex dev;
+  float eps;
+  if (!t.read(a[0], a[1], a[2]) || !one_device({t.x, t.w, t.b}, &dev) || !real_number(a[3], &eps) ||
+      !PyBool_Check(a[5]))
+    return none();
+  int yt = t.xt;
+  if (a[4] != Py_None) {
+    if (!THPDtype_Check(a[4])) return none();
+    yt = norm_type(reinterpret_cast<THPDtype*>(a[4])->scalar_type);
+    if (yt < 0) return none();
+  }
+  const at::TensorOptions options = t.x->options();
+  const std::vector<int64_t> full(t.x->sizes().begin(), t.x->sizes().end());
+  const at::IntArrayRef lead(full.data(), full.size() - 1);
+  const void* px = t.x->const_data_ptr();
+  const void *pw = t.w ? t.w->const_data_ptr() : nullptr, *pb = t.b ? t.b->const_data_ptr() : nullptr;
+  const bool stats = a[5] == Py_True;
+  at::Tensor y, mean, rstd;
+  mw_status s = MW_OK;
+  const bool real = call([&] {
+    y = at::empty(full, options.dtype(yt == MW_F32 ? at::kFloat : at::kBFloat16));
+    if (stats) {
+      mean = at::empty(lead, options.dtype(at::kFloat));
+      rstd = at::empty(lead, options.dtype(at::kFloat));
+    }
+    if (!is_real(y) || (stats && (!is_real(mean) || !is_real(rstd)))) return false;
+    s = p_norm(px, pw, pb, y.mutable_data_ptr(),
+               stats ? static_cast<float*>(mean.mutable_data_ptr()) : nullptr,
+               stats ? static_cast<float*>(rstd.mutable_data_ptr()) : nullptr, t.rows, t.C, t.groups,
+               eps, t.xt, yt, t.pt, c10::cuda::getCurrentCUDAStream(dev).stream());
+    return true;
+  });
+  if (!real) return none();
+  if (s != MW_OK) return PyLong_FromLong(s);
+  return result({&y, &mean, &rstd});
+  END_HANDLE_TH_ERRORS
+}
+
+// norm_bwd(dy, x, mean, rstd, weight, bias) -> (dx, dweight or None, dbias or None)
+PyObject* norm_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 6 || !p_norm_bwd) return none();
+  Norm t;
+  const at::Tensor *dy = tensor(a[0]), *mean = tensor(a[2]), *rstd = tensor(a[3]);
+  c10::DeviceIndex dev;
+  if (!t.read(a[1], a[4], a[5]) || !dy || !mean || !rstd || dy->sizes() != t.x->sizes() ||
+      !one_device({t.x, t.w, t.b, dy, mean, rstd}, &dev))
+    return none();
+  const int yt = norm_type(dy->scalar_type());
+  const at::IntArrayRef lead = t.x->sizes().slice(0, t.x->dim() - 1);
+  if (yt < 0 || mean->scalar_type() != at::kFloat || rstd->scalar_type() != at::kFloat ||
+      mean->sizes() != lead || rstd->sizes() != lead)
+    return none();
+  const size_t bytes = t.w || t.b ? p_norm_bwd_ws(t.rows, t.C, t.groups) : 0;
+  const at::TensorOptions options = t.x->options();
+  const std::vector<int64_t> full(t.x->sizes().begin(), t.x->sizes().end());
+  const at::Tensor* some = t.w ? t.w : t.b;
+  const std::vector<int64_t> ps = some ? some->sizes().vec() : std::vector<int64_t>();
+  const at::TensorOptions poptions = some ? some->options() : options;
+  const void *px = t.x->const_data_ptr(), *pdy = dy->const_data_ptr();
+  const void* pw = t.w ? t.w->const_data_ptr() : nullptr;
+  const float *pm = static_cast<const float*>(mean->const_data_ptr()),
+              *pr = static_cast<const float*>(rstd->const_data_ptr());
+  at::Tensor ws, dx, dw, db;
+  mw_status s = MW_OK;
+  const bool real = call([&] {
+    if (bytes) ws = scratch(bytes, options);
+    dx = at::empty(full, options);
+    if (t.w) dw = at::empty(ps, poptions);
+    if (t.b) db = at::empty(ps, poptions);
+    for (const at::Tensor* r : {&ws, &dx, &dw, &db})
+      if (r->defined() && !is_real(*r)) return false;
+    s = p_norm_bwd(pdy, px, pm, pr, pw, dx.mutable_data_ptr(), t.w ? dw.mutable_data_ptr() : nullptr,
+                   t.b ? db.mutable_data_ptr() : nullptr, bytes ? ws.mutable_data_ptr() : nullptr, bytes,
+                   t.rows, t.C, t.groups, t.xt, yt, t.pt,
+                   c10::cuda::getCurrentCUDAStream(dev).stream());
+    return true;
+  });
+  if (!real) return none();
+  if (s != MW_OK) return PyLong_FromLong(s);
+  return result({&dx, &dw, &db});
+  END_HANDLE_TH_ERRORS
+}
+
 #define MW_FAST(f) reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL
 PyMethodDef methods[] = {
     {"bind", MW_FAST(bind), "addresses of the C entry points"},
@@ -404,6 +638,10 @@ PyMethodDef methods[] = {
     {"bwd", MW_FAST(bwd), "mw_bca_bwd"},
     {"cache", MW_FAST(cache), "mw_bca_cache_fwd in its forms, mw_bca_cache_step"},
     {"qkv", MW_FAST(qkv), "mw_qkv_rope_split"},
+    {"xattn_fwd", MW_FAST(xattn_fwd), "mw_xattn_fwd"},
+    {"xattn_bwd", MW_FAST(xattn_bwd), "mw_xattn_bwd"},
+    {"norm_fwd", MW_FAST(norm_fwd), "mw_layernorm_fwd"},
+    {"norm_bwd", MW_FAST(norm_bwd), "mw_layernorm_bwd"},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_mw_torch", nullptr, -1, methods,
                       nullptr, nullptr, nullptr, nullptr};
