@@ -34,6 +34,35 @@ mw_status xattn_sizes(XattnSizes* out, int B, int H, int Hkv, int M, int S, int 
   return MW_OK;
 }
 
+// Rows of a head up to which the forward runs on CUDA cores.
+constexpr int kFewRows = 8;
+
+// Key ranges of the forward on tensor cores: enough that the blocks fill the SMs,
+// against the cost of a range (about three key tiles' time).
+int xattn_splits(int BH, int rows, int S) {
+  const long long blocks = static_cast<long long>(BH) * ceil_div(rows, kFwdBlockRows);
+  const int tiles = ceil_div(S, kTileRows);
+  int best = 1;
+  long long best_cost = LLONG_MAX;
+  for (int s = 1; s <= kMaxSplits && s <= tiles; ++s) {
+    const long long waves = ceil_div(blocks * s, kNormSms);
+    const long long cost = waves * (ceil_div(tiles, s) + (s > 1 ? 3 : 0)) + (s > 1 ? 6 : 0);
+    if (cost < best_cost) {
+      best_cost = cost;
+      best = s;
+    }
+  }
+  return best;
+}
+
+size_t xattn_ws(const XattnSizes& z, int S, int d) {
+  if (z.rows <= kFewRows) return 0;
+  const int splits = xattn_splits(z.BH, z.rows, S);
+  if (splits == 1) return 0;
+  const size_t rows = static_cast<size_t>(splits) * z.BH * z.rows;
+  return align256(rows * kernel_d(d) * sizeof(float)) + align256(rows * sizeof(float));
+}
+
 mw_status check_f32(const void* p, const char* name) {
   if (reinterpret_cast<uintptr_t>(p) & 3u)
     return fail(MW_ERR_INVALID_ARG, "%s is not 4-byte aligned", name);
@@ -80,7 +109,7 @@ extern "C" {
 size_t mw_xattn_workspace_size(int B, int H, int Hkv, int M, int S, int d) {
   XattnSizes z;
   if (xattn_sizes(&z, B, H, Hkv, M, S, d) != MW_OK) return 0;
-  return 0;
+  return xattn_ws(z, S, d);
 }
 
 mw_status mw_xattn_fwd(const void* q, const void* k, const void* v, const int* kv_len, void* o,
@@ -98,9 +127,53 @@ mw_status mw_xattn_fwd(const void* q, const void* k, const void* v, const int* k
   }
   MW_TRY(check_f32(kv_len, "kv_len"));
   MW_TRY(check_f32(lse, "lse"));
+  const size_t need = xattn_ws(z, S, d);
+  if (need > 0) {
+    if (workspace == nullptr || ws_bytes < need)
+      return fail(MW_ERR_WORKSPACE, "workspace %zu bytes, need %zu", ws_bytes, need);
+    if (reinterpret_cast<uintptr_t>(workspace) & 255u)
+      return fail(MW_ERR_INVALID_ARG, "workspace is not 256-byte aligned");
+  }
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   DeviceScope scope(s);
   MW_TRY(scope.status());
+  if (z.rows > kFewRows && S > 0) {
+    const int D = kernel_d(d);
+    XattnTcParams p{};
+    MW_TRY(status_ptr(scope.device(), &p.status));
+    CUtensorMap tq, tk, tv;
+    MW_TRY(make_map(&tq, q, z.rows, z.BH, d, "q"));
+    MW_TRY(make_map(&tk, k, S, z.BH, d, "k"));
+    MW_TRY(make_map(&tv, v, S, z.BH, d, "v"));
+    p.kv_len = kv_len;
+    p.o = static_cast<__nv_bfloat16*>(o);
+    p.lse = lse;
+    p.BH = z.BH;
+    p.heads = Hkv;
+    p.M = z.rows;
+    p.S = S;
+    p.d = d;
+    p.n_qblocks = ceil_div(z.rows, kFwdBlockRows);
+    p.num_splits = need > 0 ? xattn_splits(z.BH, z.rows, S) : 1;
+    p.items = z.BH * p.n_qblocks * p.num_splits;
+    p.wide_out = wide_rows(o, d);
+    p.scale_log2 = scale * 1.4426950408889634f;
+    p.budget_ns = budget_ns();
+    p.debug_skip_q = debug_skip_q();
+    if (p.num_splits > 1) {
+      p.o_part = static_cast<float*>(workspace);
+      p.lse_part = reinterpret_cast<float*>(
+          static_cast<char*>(workspace) +
+          align256(static_cast<size_t>(p.num_splits) * z.BH * z.rows * D * sizeof(float)));
+    }
+    MW_TRY(launch_status(launch_xattn_tc(D, mma_d(d), tq, tk, tv, p, scope.device(), sm_count(), s),
+                         "cross attention forward launch"));
+    if (p.num_splits > 1)
+      MW_TRY(launch_status(launch_combine(D, d, p.o_part, p.lse_part, p.o, lse, p.num_splits, z.BH,
+                                          z.rows, CommitJob{}, s),
+                           "combine kernel launch"));
+    return ok();
+  }
   XattnParams p{};
   p.q = static_cast<const __nv_bfloat16*>(q);
   p.k = static_cast<const __nv_bfloat16*>(k);

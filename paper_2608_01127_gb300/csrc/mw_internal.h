@@ -239,6 +239,27 @@ struct XattnParams {
   __nv_bfloat16* dk;
   __nv_bfloat16* dv;
 };
+// Forward on tensor cores (mw_xattn_fwd.cu): blocks of kFwdBlockRows rows of one
+// head against one of num_splits ranges of its key tiles.
+struct XattnTcParams {
+  const int* kv_len;
+  __nv_bfloat16* o;
+  float* lse;          // nullable
+  float* o_part;       // [num_splits, BH * M, D] where num_splits > 1
+  float* lse_part;     // [num_splits, BH * M]
+  int BH, heads, M, S, d;
+  int n_qblocks, num_splits;
+  int items;           // BH * n_qblocks * num_splits
+  bool wide_out;       // every row of o starts at a multiple of 32 bytes
+  float scale_log2;
+  unsigned* status;
+  unsigned long long budget_ns;
+  int debug_skip_q;    // test hook: never load Q, so the issuers' wait expires
+};
+// d, dm: tile and MMA width as for launch_fwd; sms: CTAs at most
+cudaError_t launch_xattn_tc(int d, int dm, const CUtensorMap& tq, const CUtensorMap& tk,
+                            const CUtensorMap& tv, const XattnTcParams& p, int dev, int sms, cudaStream_t s);
+// Forward of few rows a head on CUDA cores (mw_xattn.cu).
 cudaError_t launch_xattn_fwd(const XattnParams& p, cudaStream_t s);
 cudaError_t launch_xattn_bwd(const XattnParams& p, cudaStream_t s);
 

@@ -1,0 +1,697 @@
+// Cross attention forward on sm_103a: blocks of 2 x 128 query rows against an
+// encoder's states, all of which (up to the sample's valid number) every row sees.
+//
+//   S = Q K^T, P = exp2(scale log2e S - m), O = sum over key tiles of P V / l,
+//   LSE = (m + log2 l) ln 2
+//
+// There is no order among the rows, so the query heads that share a head of K
+// and V are one sequence of rows.  An encoder's states are few next to a video's
+// tokens (a prompt is one to four key tiles), so a block is short and what
+// surrounds its key tiles counts: the CTAs are persistent, one an SM, and every
+// role runs through the blocks without a stop.  The next block's Q and K/V tiles
+// are loaded, and its first S is computed, while the softmax warps finish the
+// last one; they take O into registers, hand its tensor memory back, and store
+// rows while the next block's MMAs run.
+//
+// Roles (384 threads):
+//   warps 0-3 / 4-7  softmax of query tile 0 / 1 (one thread per row = TMEM lane)
+//   warp 8           TMA producer
+//   warp 9           tcgen05 issuer; d = 64: of query tile 0, and warp 10 of tile 1
+//   the rest of 9-11 V tiles that end inside the valid states: rows past them are
+//                    zeroed (their weights are 0, but what they hold may be NaN);
+//                    80-wide MMAs: also the ones columns of every V tile
+// TMEM as in the block-causal forward: S_t at column 128 t, O_t at 256 + OW t with
+// 16 row-sum columns where V has ones columns; P_t, bf16, over S_t, its second
+// half in columns of its own where there is room.
+#include <type_traits>
+
+#include "mw_internal.h"
+#include "mw_ptx.cuh"
+
+namespace mw {
+namespace {
+
+// D: width of the shared-memory tiles; DM <= D: the columns the MMAs cover
+template <int D, int DM>
+struct Layout {
+  static constexpr int QT = kFwdQTiles;
+  static constexpr int REG = D / 64;  // 64-column swizzle regions per row
+  static constexpr int REGION_BYTES = kTileRows * 128;
+  static constexpr int TILE_BYTES = REG * REGION_BYTES;
+  static constexpr int STAGES = (D == 64) ? 4 : 2;
+  static constexpr int QBUFS = (D == 64) ? 2 : 1;  // blocks of Q in shared memory
+  static constexpr int OFF_Q = 0;
+  static constexpr int OFF_K = OFF_Q + QBUFS * QT * TILE_BYTES;
+  static constexpr int OFF_V = OFF_K + STAGES * TILE_BYTES;
+  // The row sum of P as 16 more columns of the PV MMA: ones in a region of their
+  // own (d = 64) or in columns 80..95 of each V tile (80-wide MMAs)
+  static constexpr bool ONES_IN_V = (D == 128 && DM == 80);
+  static constexpr bool SUM_MMA = (D == 64) || ONES_IN_V;
+  static constexpr int OW = SUM_MMA ? DM + 16 : DM;
+  static constexpr int OFF_ONES = OFF_V + STAGES * TILE_BYTES;
+  static constexpr int ONES_BYTES = (D == 64) ? REGION_BYTES : 0;
+  static constexpr int OFF_BAR = OFF_ONES + ONES_BYTES;
+  static constexpr bool SPLIT_P = 256 + OW * QT + 32 * QT <= 512;
+  static constexpr int ISSUERS = D == 64 ? QT : 1;
+  static constexpr int HELPERS = 3 - ISSUERS;
+  static constexpr int NBAR = 2 * QBUFS + 5 * STAGES + 5 * QT;
+  static constexpr int OFF_MISC = OFF_BAR + NBAR * 8;
+  static constexpr int BYTES = OFF_MISC + 16;
+  static_assert(BYTES <= 232448, "shared memory");
+  static constexpr uint32_t S_COL(int t) { return 128u * t; }
+  static constexpr uint32_t O_COL(int t) { return 256u + OW * t; }
+  static constexpr uint32_t P_COL(int t, int half) {
+    return half == 0 ? S_COL(t) : SPLIT_P ? 256u + OW * QT + 32u * t : S_COL(t) + 32u;
+  }
+  static constexpr int THREADS = 384;
+  // registers per thread after the re-split: 2 * 128 * S + 128 * C is exactly the
+  // launch's 384 * 168
+  static constexpr int REGS_LAUNCH = 168;
+  static constexpr int REGS_SOFTMAX = (D == 64) ? 224 : 208;
+  static constexpr int REGS_CONTROL = (D == 64) ? 56 : 88;
+  static_assert(2 * 128 * REGS_SOFTMAX + 128 * REGS_CONTROL == THREADS * REGS_LAUNCH,
+                "register re-split must hand out exactly the launch's registers");
+};
+
+// The blocks of a CTA in turn; every role walks through the same ones.
+struct Walk {
+  const XattnTcParams& p;
+  int next;        // index of the next block
+  int sample, len; // the last block's sample and its valid states
+  int bh, r0, split;
+  int j0, n;       // its key tiles: n from the j0-th on
+  __device__ explicit Walk(const XattnTcParams& p_) : p(p_), next(blockIdx.x), sample(-1), len(p_.S) {}
+  __device__ __forceinline__ bool step() {
+    if (next >= p.items) return false;
+    int x = next;
+    next += gridDim.x;
+    split = x % p.num_splits;
+    x /= p.num_splits;
+    bh = x / p.n_qblocks;
+    r0 = (x - bh * p.n_qblocks) * kFwdBlockRows;
+    if (p.kv_len) {
+      const int s = bh / p.heads;
+      if (s != sample) {
+        sample = s;
+        len = min(max(p.kv_len[s], 0), p.S);
+      }
+    }
+    const int all = (len + kTileRows - 1) / kTileRows;
+    j0 = static_cast<int>(static_cast<long long>(split) * all / p.num_splits);
+    n = static_cast<int>(static_cast<long long>(split + 1) * all / p.num_splits) - j0;
+    return true;
+  }
+  // the next block that has keys
+  __device__ __forceinline__ bool step_nonempty() {
+    while (step())
+      if (n > 0) return true;
+    return false;
+  }
+  __device__ __forceinline__ bool present(int t) const { return r0 + kTileRows * t < p.M; }
+  // V tile i of the block passes through the helper warps: all of them, or those
+  // with rows that count as nothing but may hold anything (past S are zeros)
+  __device__ __forceinline__ bool helped(int i, bool all) const {
+    return all || ((j0 + i + 1) * kTileRows > len && len < p.S);
+  }
+};
+
+template <int D, int DM>
+__global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
+    xattn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
+                     const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ XattnTcParams p) {
+  using L = Layout<D, DM>;
+  constexpr int QT = L::QT, NS = L::STAGES, NQ = L::QBUFS;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const int warp = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31;
+
+  // Row `row` of head bh gets its value: bf16 O and LSE, or a split's partials.
+  auto store_lse = [&](const Walk& w, int row, float lse) {
+    const size_t at = static_cast<size_t>(w.bh) * p.M + row;
+    if (p.num_splits > 1)
+      p.lse_part[static_cast<size_t>(w.split) * p.BH * p.M + at] = lse;
+    else if (p.lse)
+      p.lse[at] = lse;
+  };
+  auto store_nothing = [&](const Walk& w, int row) {
+    if (p.num_splits == 1) {  // (the combine skips a split whose LSE is -inf)
+      uint4* dst = reinterpret_cast<uint4*>(p.o + (static_cast<size_t>(w.bh) * p.M + row) * p.d);
+      for (int c = 0; c < p.d / 8; ++c) dst[c] = make_uint4(0u, 0u, 0u, 0u);
+    }
+    store_lse(w, row, -INFINITY);
+  };
+
+  if ((smem_u32(smem) & 1023u) != 0u) {
+    // nothing runs without aligned shared memory: report it, and give this CTA's
+    // rows a defined result
+    if (threadIdx.x == 0) atomicOr(p.status, kDevMisaligned);
+    Walk w(p);
+    while (w.step()) {
+      const int row = w.r0 + static_cast<int>(threadIdx.x);
+      if (threadIdx.x < kFwdBlockRows && row < p.M) store_nothing(w, row);
+    }
+    return;  // uniform across the CTA, before any barrier or TMEM use
+  }
+  uint64_t* q_full = reinterpret_cast<uint64_t*>(smem + L::OFF_BAR);
+  uint64_t* q_empty = q_full + NQ;
+  uint64_t* k_full = q_empty + NQ;
+  uint64_t* k_empty = k_full + NS;
+  uint64_t* v_full = k_empty + NS;
+  uint64_t* v_empty = v_full + NS;
+  uint64_t* v_raw = v_empty + NS;   // V tile that a helper warp makes ready, then v_full
+  uint64_t* s_full = v_raw + NS;
+  uint64_t* p_half = s_full + QT;   // first 64 keys of P in TMEM
+  uint64_t* p_full = p_half + QT;
+  uint64_t* pv_done = p_full + QT;  // PV of a key tile (SPLIT_P), of a block's last one (else)
+  uint64_t* o_free = pv_done + QT;  // O of a block is in registers
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + L::OFF_MISC);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + L::OFF_MISC + 4);
+
+  if (threadIdx.x == 0) {
+    for (int b = 0; b < NQ; ++b) {
+      mbar_init(&q_full[b], 1);
+      mbar_init(&q_empty[b], L::ISSUERS);
+    }
+    for (int s = 0; s < NS; ++s) {
+      mbar_init(&k_full[s], 1);
+      mbar_init(&k_empty[s], L::ISSUERS);
+      mbar_init(&v_full[s], L::ONES_IN_V ? L::HELPERS : 1);
+      mbar_init(&v_empty[s], L::ISSUERS);
+      mbar_init(&v_raw[s], 1);
+    }
+    for (int t = 0; t < QT; ++t) {
+      mbar_init(&s_full[t], 1);
+      mbar_init(&p_half[t], 4);
+      mbar_init(&p_full[t], 4);
+      mbar_init(&pv_done[t], 1);
+      mbar_init(&o_free[t], 4);
+    }
+    *abort_flag = 0;
+    fence_mbar_init();
+  }
+  if (warp == 8 && lane == 0) {
+    prefetch_tmap(&tm_q);
+    prefetch_tmap(&tm_k);
+    prefetch_tmap(&tm_v);
+  }
+  if (warp == 9) {
+    tmem_alloc(tmem_slot, 512);
+    tmem_relinquish();
+  }
+  if constexpr (L::ONES_BYTES > 0) {
+    uint4* ones = reinterpret_cast<uint4*>(smem + L::OFF_ONES);
+    const uint32_t one2 = 0x3F803F80u;  // bf16 1.0 twice
+    for (int k = threadIdx.x; k < L::ONES_BYTES / 16; k += L::THREADS)
+      ones[k] = make_uint4(one2, one2, one2, one2);
+    fence_proxy_async_smem();  // read by the tensor core (async proxy)
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  constexpr uint32_t tmem = 0;  // the allocation of all 512 columns can only start at 0
+  const WaitCtl ctl{abort_flag, p.status, p.budget_ns};
+  pdl_wait();  // global memory only from here on
+
+  uint8_t* sQ = smem + L::OFF_Q;
+  uint8_t* sK = smem + L::OFF_K;
+  uint8_t* sV = smem + L::OFF_V;
+  Walk w(p);
+
+  if (warp >= 8) {
+  regs_dec<L::REGS_CONTROL>();
+  if (warp == 8) {
+    // ------------------------------------------------------------ TMA producer
+    if (lane == 0) {
+      int nq = 0, nk = 0, nv = 0;  // blocks, K and V tiles so far
+      uint32_t raw = 0, turn = 0;  // per stage: its last V tile went to a helper; parity of those
+      bool ok = true;
+      while (ok && w.step_nonempty()) {
+        const int qb = nq % NQ;
+        if (!(ok = mbar_wait(&q_empty[qb], ((nq / NQ) & 1) ^ 1, ctl))) break;
+        if (!p.debug_skip_q) {
+          const int tiles = w.present(1) ? QT : 1;
+          mbar_arrive_expect_tx(&q_full[qb], tiles * L::TILE_BYTES);
+          for (int t = 0; t < tiles; ++t)
+            for (int r = 0; r < L::REG; ++r)
+              tma_load_3d(sQ + (qb * QT + t) * L::TILE_BYTES + r * L::REGION_BYTES, &tm_q, &q_full[qb],
+                          64 * r, w.r0 + kTileRows * t, w.bh);
+          ++nq;
+        }
+        for (int i = 0; i < w.n; ++i) {
+          const int st = nk % NS;
+          const uint32_t ph = ((nk / NS) & 1) ^ 1;
+          const int row0 = (w.j0 + i) * kTileRows;
+          if (!(ok = mbar_wait(&k_empty[st], ph, ctl))) break;
+          mbar_arrive_expect_tx(&k_full[st], L::TILE_BYTES);
+          for (int r = 0; r < L::REG; ++r)
+            tma_load_3d(sK + st * L::TILE_BYTES + r * L::REGION_BYTES, &tm_k, &k_full[st], 64 * r, row0, w.bh);
+          ++nk;
+          if (!(ok = mbar_wait(&v_empty[st], ph, ctl))) break;
+          const bool help = w.helped(i, L::ONES_IN_V);
+          uint64_t* bar = help ? &v_raw[st] : &v_full[st];
+          mbar_arrive_expect_tx(bar, L::TILE_BYTES);
+          for (int r = 0; r < L::REG; ++r)
+            tma_load_3d(sV + st * L::TILE_BYTES + r * L::REGION_BYTES, &tm_v, bar, 64 * r, row0, w.bh);
+          raw = (raw & ~(1u << st)) | (help ? 1u << st : 0u);
+          turn ^= help ? 1u << st : 0u;
+          ++nv;
+        }
+      }
+      if (*abort_flag || !ok) {
+        // let every copy this CTA started land before shared memory goes away
+        for (int i = max(0, nq - NQ); i < nq; ++i) drain_wait(&q_full[i % NQ], (i / NQ) & 1, p.budget_ns);
+        for (int i = max(0, nk - NS); i < nk; ++i) drain_wait(&k_full[i % NS], (i / NS) & 1, p.budget_ns);
+        for (int i = max(0, nv - NS); i < nv; ++i) {
+          const int st = i % NS;
+          if ((raw >> st) & 1)
+            drain_wait(&v_raw[st], ((turn >> st) & 1) ^ 1, p.budget_ns);
+          else
+            drain_wait(&v_full[st], (i / NS) & 1, p.budget_ns);
+        }
+      }
+    }
+  } else if (warp == 9 || (L::ISSUERS > 1 && warp == 10)) {
+    // ------------------------------------------------------------ MMA issuers (whole warps)
+    constexpr uint32_t idesc_qk = idesc_bf16_f32(128, 128, false, false);
+    constexpr uint32_t idesc_pv = idesc_bf16_f32(128, L::OW, false, true);
+    const uint32_t q_desc = sdesc_sw128(smem_u32(sQ), 16);
+    const uint32_t k_desc = sdesc_sw128(smem_u32(sK), 16);
+    const uint32_t v_addr = smem_u32(sV);
+    const uint32_t ones_addr = smem_u32(smem + L::OFF_ONES);
+    auto issue_qk = [&](int t, int qb, int st) {
+      const uint32_t qa = sdesc_add(q_desc, (qb * QT + t) * L::TILE_BYTES);
+      const uint32_t kb = sdesc_add(k_desc, st * L::TILE_BYTES);
+#pragma unroll
+      for (int kk = 0; kk < DM / 16; ++kk) {
+        const uint32_t off = (kk >> 2) * L::REGION_BYTES + (kk & 3) * 32;
+        umma_ss(tmem + L::S_COL(t), sdesc_add(qa, off), sdesc_add(kb, off), idesc_qk, kk > 0 ? 1u : 0u);
+      }
+    };
+    auto issue_pv = [&](int t, int st, bool acc, int half) {
+      const uint32_t vs = v_addr + st * L::TILE_BYTES;
+      const uint32_t vb = sdesc_sw128(vs, L::ONES_BYTES > 0 ? ones_addr - vs : L::REGION_BYTES);
+#pragma unroll
+      for (int k4 = 0; k4 < 4; ++k4) {
+        const int kk = 4 * half + k4;
+        umma_ts(tmem + L::O_COL(t), tmem + L::P_COL(t, half) + k4 * 8, sdesc_add(vb, kk * 2048), idesc_pv,
+                (acc || kk > 0) ? 1u : 0u);
+      }
+    };
+    // query tiles [T0, T1): one issuer's, or all of them
+    auto issue = [&](auto first, auto last) {
+      constexpr int T0 = decltype(first)::value, T1 = decltype(last)::value;
+      int nq = 0, nk = 0;       // blocks and key tiles whose S is issued
+      int done[QT] = {0, 0};    // key tiles of a query tile whose PV is issued
+      int blocks[QT] = {0, 0};  // blocks of a query tile begun
+      if (!w.step_nonempty()) return;
+      bool ok = warp_wait(&q_full[0], 0, ctl) && warp_wait(&k_full[0], 0, ctl);
+      tc_fence_after();
+      if (ok) {
+#pragma unroll
+        for (int t = T0; t < T1; ++t)
+          if (w.present(t)) {
+            issue_qk(t, 0, 0);
+            umma_commit(&s_full[t]);
+          }
+        umma_commit(&k_empty[0]);
+        if (w.n == 1) umma_commit(&q_empty[0]);
+        nk = 1;
+        nq = 1;
+      }
+      int i = 0;
+      while (ok) {
+        // tile i of this block, of which S is issued, and the tile after it
+        const int st = (nk - 1) % NS;
+        const uint32_t ph = ((nk - 1) / NS) & 1;
+        const bool have[QT] = {w.present(0), w.present(1)};
+        const bool first_tile = i == 0, last_tile = i + 1 == w.n;
+        bool more = true;
+        if (last_tile) {
+          more = w.step_nonempty();
+          i = 0;
+        } else {
+          ++i;
+        }
+        const int st1 = nk % NS, qb1 = (i == 0 ? nq : nq - 1) % NQ;
+        bool waited = false;
+        auto wait_next = [&]() {  // Q (of a new block) and K of the next tile
+          if (waited) return true;
+          waited = true;
+          if (i == 0 && !warp_wait(&q_full[qb1], (nq / NQ) & 1, ctl)) return false;
+          if (!warp_wait(&k_full[st1], (nk / NS) & 1, ctl)) return false;
+          tc_fence_after();
+          return true;
+        };
+        // S of the next tile between the halves of this one's PV where P leaves
+        // it free, but not at the risk of waiting for a new block's Q
+        const bool early = L::SPLIT_P && (NQ > 1 || i > 0);
+        if (!(ok = warp_wait(&v_full[st], ph, ctl))) break;
+        tc_fence_after();
+#pragma unroll
+        for (int t = T0; t < T1; ++t) {
+          if (have[t]) {
+            if (!(ok = warp_wait(&p_half[t], done[t] & 1, ctl))) break;
+            if (first_tile) {
+              // the last block's O is in the softmax warps' registers
+              if (blocks[t] > 0 && !(ok = warp_wait(&o_free[t], (blocks[t] - 1) & 1, ctl))) break;
+              ++blocks[t];
+            }
+            tc_fence_after();
+            issue_pv(t, st, !first_tile, 0);
+          }
+          if (early && more && w.present(t)) {
+            if (!(ok = wait_next())) break;
+            issue_qk(t, qb1, st1);
+            umma_commit(&s_full[t]);
+          }
+          if (have[t]) {
+            if (!(ok = warp_wait(&p_full[t], done[t] & 1, ctl))) break;
+            tc_fence_after();
+            issue_pv(t, st, true, 1);
+            ++done[t];
+            if (L::SPLIT_P || last_tile) umma_commit(&pv_done[t]);
+          }
+          if (!early && more && w.present(t)) {
+            if (!(ok = wait_next())) break;
+            issue_qk(t, qb1, st1);
+            umma_commit(&s_full[t]);
+          }
+        }
+        if (!ok) break;
+        umma_commit(&v_empty[st]);
+        if (!more) break;
+        if (!(ok = wait_next())) break;  // (an issuer without a tile here looks, too)
+        umma_commit(&k_empty[st1]);
+        if (i + 1 == w.n) umma_commit(&q_empty[qb1]);
+        if (i == 0) ++nq;
+        ++nk;
+      }
+    };
+    if constexpr (L::ISSUERS == 1) {
+      issue(std::integral_constant<int, 0>{}, std::integral_constant<int, QT>{});
+    } else {
+      if (warp == 9)
+        issue(std::integral_constant<int, 0>{}, std::integral_constant<int, 1>{});
+      else
+        issue(std::integral_constant<int, 1>{}, std::integral_constant<int, 2>{});
+    }
+  } else {
+    // ------------------------------------------------------------ V tiles made ready
+    // With ones columns every tile passes through all helpers, else only the
+    // ragged ones, through the first.  A stage's v_raw cannot complete again
+    // before the helper has looked: the stage is free for another tile only once
+    // the MMAs, which wait for the helper, have read this one.
+    const int part = warp - 9 - L::ISSUERS;
+    constexpr int kParts = L::ONES_IN_V ? L::HELPERS : 1;
+    constexpr int kRows = kTileRows / kParts;  // of a helper
+    int nv = 0;
+    uint32_t turn = 0;  // parity of each stage's uses
+    bool ok = part < kParts;
+    while (ok && w.step_nonempty()) {
+      for (int i = 0; i < w.n; ++i, ++nv) {
+        if (!w.helped(i, L::ONES_IN_V)) continue;
+        const int st = nv % NS;
+        if (!(ok = warp_wait(&v_raw[st], (turn >> st) & 1, ctl))) break;
+        turn ^= 1u << st;
+        uint8_t* tile = sV + st * L::TILE_BYTES;
+        const int limit = w.len - (w.j0 + i) * kTileRows;
+#pragma unroll
+        for (int k = 0; k < kRows / 32; ++k) {
+          const int r = kRows * part + 32 * k + lane;
+          if constexpr (L::ONES_IN_V) {
+            const uint4 ones = make_uint4(0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u);
+            uint8_t* row = tile + L::REGION_BYTES + r * 128;
+            *reinterpret_cast<uint4*>(row + (((DM - 64) / 8 ^ (r & 7)) << 4)) = ones;
+            *reinterpret_cast<uint4*>(row + (((DM - 64) / 8 + 1 ^ (r & 7)) << 4)) = ones;
+          }
+          if (r >= limit) {
+            const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+            for (int c = 0; c < DM / 8; ++c)
+              *reinterpret_cast<uint4*>(tile + (c >> 3) * L::REGION_BYTES + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = zero;
+          }
+        }
+        fence_proxy_async_smem();  // the tensor core reads the tile next
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&v_full[st]);
+      }
+    }
+  }
+  } else {
+    regs_inc<L::REGS_SOFTMAX>();
+    // ------------------------------------------------------------ softmax
+    const int t = warp >> 2;
+    const int wq = warp & 3;
+    const int row_local = wq * 32 + lane;
+    const uint32_t lane_base = tmem + (static_cast<uint32_t>(wq * 32) << 16);
+    const uint32_t s_addr = lane_base + L::S_COL(t);
+    const uint32_t o_addr = lane_base + L::O_COL(t);
+    const float sl2 = p.scale_log2;
+    int done = 0;    // key tiles so far
+    int blocks = 0;  // blocks with keys so far
+    bool ok = true;
+    while (w.step()) {
+      const int row = w.r0 + t * kTileRows + row_local;
+      const bool row_valid = row < p.M;
+      if (w.n == 0 || !ok) {  // no keys, or a wait gave up: a defined result
+        if (row_valid) store_nothing(w, row);
+        __syncwarp();
+        continue;
+      }
+      if (!w.present(t)) continue;
+      float m_used = -INFINITY;
+      float l = 0.f;
+      const bool idle = w.r0 + t * kTileRows + wq * 32 >= p.M;  // a warp without rows only keeps step
+      for (int i = 0; i < w.n; ++i, ++done) {
+        if (!(ok = warp_wait(&s_full[t], done & 1, ctl))) break;
+        if (idle) {
+          if (lane == 0) {
+            mbar_arrive(&p_half[t]);
+            mbar_arrive(&p_full[t]);
+          }
+          // (the block's end shows that its PVs are done)
+          if (L::SPLIT_P && !(ok = warp_wait(&pv_done[t], done & 1, ctl))) break;
+          continue;
+        }
+        tc_fence_after();
+        float s[128];
+        if constexpr (L::SPLIT_P) {
+          uint32_t r[4][32];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) tmem_ld32(s_addr + 32 * c, r[c]);
+          tmem_wait_ld();
+#pragma unroll
+          for (int c = 0; c < 128; ++c) s[c] = __uint_as_float(r[c / 32][c % 32]);
+        } else {
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            uint32_t r[32];
+            tmem_ld32(s_addr + 32 * c, r);
+            tmem_wait_ld();
+#pragma unroll
+            for (int k = 0; k < 32; ++k) s[32 * c + k] = __uint_as_float(r[k]);
+          }
+        }
+        const int limit = w.len - (w.j0 + i) * kTileRows;
+        if (limit < kTileRows) {
+#pragma unroll
+          for (int c = 0; c < 128; ++c)
+            if (c >= limit) s[c] = -INFINITY;
+        }
+        const float2 sl2x2 = make_float2(sl2, sl2);
+        auto minus = [](float m) {
+          const float m_eff = (m == -INFINITY) ? 0.f : m;
+          return make_float2(-m_eff, -m_eff);
+        };
+        // P of keys 32 g4 + 2 k and + 1, as a bf16 pair, relative to a maximum
+        auto weights = [&](int g4, int k, float2 negm) {
+          const float2 x = fma2(make_float2(s[32 * g4 + 2 * k], s[32 * g4 + 2 * k + 1]), sl2x2, negm);
+          return pack_bf16x2(ex2_approx(x.x), ex2_approx(x.y));
+        };
+        // the first groups against the maximum so far, which a tile hardly ever
+        // replaces (a block's first one always does)
+        constexpr int kEarly = L::SPLIT_P ? 2 : 0;
+        [[maybe_unused]] uint32_t early[kEarly > 0 ? kEarly : 1][16];
+        auto set_early = [&](float2 negm) {
+#pragma unroll
+          for (int g4 = 0; g4 < kEarly; ++g4)
+#pragma unroll
+            for (int k = 0; k < 16; ++k) early[g4][k] = weights(g4, k, negm);
+        };
+        if (i > 0) set_early(minus(m_used));
+        float mq[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) mq[k] = fmaxf(s[k], s[k + 4]);
+#pragma unroll
+        for (int c = 8; c < 128; c += 8) {
+          mq[0] = max3(mq[0], s[c], s[c + 1]);
+          mq[1] = max3(mq[1], s[c + 2], s[c + 3]);
+          mq[2] = max3(mq[2], s[c + 4], s[c + 5]);
+          mq[3] = max3(mq[3], s[c + 6], s[c + 7]);
+        }
+        const float mx = max3(fmaxf(mq[0], mq[1]), mq[2], mq[3]);
+        const float m_tile = mx * sl2;  // scale > 0
+        const float m_cand = fmaxf(m_used, m_tile);
+        // rescale only when the running maximum grew by more than 2^8: P stays
+        // below 256 in between, and the final O / l is exact either way
+        const bool need = m_cand > m_used + 8.0f;
+        if (i == 0 || __any_sync(0xffffffffu, need)) {
+          float alpha = 1.f;
+          if (need) {
+            alpha = ex2_approx(m_used - m_cand);
+            m_used = m_cand;
+          }
+          set_early(minus(m_used));
+          l *= alpha;
+          if (i > 0) {
+            if constexpr (L::SPLIT_P) {  // (else S of this tile implies it)
+              if (!(ok = warp_wait(&pv_done[t], (done - 1) & 1, ctl))) break;
+              tc_fence_after();
+            }
+            // exactly the tile's O columns, row sums included
+#pragma unroll
+            for (int c = 0; c < L::OW / 16; ++c) {
+              uint32_t r[16];
+              tmem_ld16(o_addr + 16 * c, r);
+              tmem_wait_ld();
+#pragma unroll
+              for (int k = 0; k < 16; ++k) r[k] = __float_as_uint(__uint_as_float(r[k]) * alpha);
+              tmem_st16(o_addr + 16 * c, r);
+            }
+            tmem_wait_st();
+          }
+        }
+        const float2 negm = minus(m_used);
+        float2 acc = make_float2(0.f, 0.f);
+        // P in four 32-key groups, each stored as soon as it is packed; the first
+        // two are announced while the third is stored
+#pragma unroll
+        for (int g4 = 0; g4 < 4; ++g4) {
+          uint32_t packed[16];
+#pragma unroll
+          for (int k = 0; k < 16; ++k) {
+            const uint32_t pk = g4 < kEarly ? early[g4 < kEarly ? g4 : 0][k] : weights(g4, k, negm);
+            // the row sum uses the bf16 weights the PV MMA consumes, so O is an
+            // exact convex combination of them
+            if constexpr (!L::SUM_MMA)
+              acc = add2(acc, make_float2(__uint_as_float(pk << 16), __uint_as_float(pk & 0xffff0000u)));
+            packed[k] = pk;
+          }
+          if (g4 == 2) {
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&p_half[t]);
+            // the previous tile's PV has read the columns of the second half
+            if (L::SPLIT_P && i > 0) {
+              if (!(ok = warp_wait(&pv_done[t], (done - 1) & 1, ctl))) break;
+              tc_fence_after();
+            }
+          }
+          const uint32_t p_addr = L::SPLIT_P && g4 >= 2 ? lane_base + L::P_COL(t, 1) : s_addr + 32 * (g4 >> 1);
+          tmem_st16(p_addr + 16 * (g4 & 1), packed);
+        }
+        if (!ok) break;
+        l += acc.x + acc.y;
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&p_full[t]);
+      }
+
+      // ---- epilogue
+      if (ok) ok = warp_wait(&pv_done[t], (L::SPLIT_P ? done - 1 : blocks) & 1, ctl);
+      ++blocks;
+      if (!ok) {
+        if (row_valid) store_nothing(w, row);
+        __syncwarp();
+        continue;
+      }
+      tc_fence_after();
+      uint32_t r[(DM + 31) / 32][32];
+#pragma unroll
+      for (int c = 0; c < DM / 32; ++c) tmem_ld32(o_addr + 32 * c, r[c]);
+      if constexpr (DM % 32 != 0) {
+        uint32_t h[16];
+        tmem_ld16(o_addr + DM - 16, h);
+        tmem_wait_ld();
+#pragma unroll
+        for (int k = 0; k < 16; ++k) r[DM / 32][k] = h[k], r[DM / 32][16 + k] = 0u;
+      }
+      if constexpr (L::SUM_MMA) {
+        uint32_t h[16];
+        tmem_ld16(o_addr + DM, h);
+        tmem_wait_ld();
+        l = __uint_as_float(h[0]);
+      }
+      tmem_wait_ld();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&o_free[t]);
+      if (row_valid) {
+        const bool nonzero = l > 0.f;
+        const float inv_l = nonzero ? 1.f / l : 0.f;
+        const float m_eff = (m_used == -INFINITY) ? 0.f : m_used;
+        const size_t at = static_cast<size_t>(w.bh) * p.M + row;
+#pragma unroll
+        for (int c = 0; c < (DM + 31) / 32; ++c) {
+          float v[32];
+#pragma unroll
+          for (int k = 0; k < 32; ++k) v[k] = nonzero ? __uint_as_float(r[c][k]) * inv_l : 0.f;
+          if (p.num_splits == 1) {
+            const int d_io = (D == 64) ? D : p.d;
+            if (32 * c < d_io) store_row32(p.o + at * d_io + 32 * c, v, min(4, (d_io - 32 * c) / 8), p.wide_out);
+          } else {
+            float4* dst = reinterpret_cast<float4*>(
+                p.o_part + (static_cast<size_t>(w.split) * p.BH * p.M + at) * D + 32 * c);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) dst[k] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+          }
+        }
+        store_lse(w, row, nonzero ? (m_eff + __log2f(l)) * 0.69314718055994530942f : -INFINITY);
+      }
+      __syncwarp();
+    }
+    pdl_trigger();  // the next kernel (the split combine) may be scheduled now
+  }
+
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 9) {
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+template <int D, int DM>
+cudaError_t launch(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv,
+                   const XattnTcParams& p, int dev, int sms, cudaStream_t s) {
+  using L = Layout<D, DM>;
+  static OncePerDevice prepared;
+  const cudaError_t e = prepared(dev, [] {
+    // the in-kernel register re-split assumes the launch register count; with any
+    // other its setmaxnreg.inc could never be satisfied, so refuse
+    cudaFuncAttributes fa;
+    const cudaError_t e0 = cudaFuncGetAttributes(&fa, xattn_fwd_kernel<D, DM>);
+    if (e0 != cudaSuccess) return e0;
+    if (fa.numRegs != L::REGS_LAUNCH) return cudaErrorInvalidKernelImage;
+    return cudaFuncSetAttribute(xattn_fwd_kernel<D, DM>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::BYTES);
+  });
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg;
+  cudaLaunchAttribute attr;
+  pdl_config(cfg, attr, dim3(p.items < sms ? p.items : sms), dim3(L::THREADS), L::BYTES, s);
+  return cudaLaunchKernelEx(&cfg, xattn_fwd_kernel<D, DM>, tq, tk, tv, p);
+}
+
+}  // namespace
+
+cudaError_t launch_xattn_tc(int d, int dm, const CUtensorMap& tq, const CUtensorMap& tk,
+                            const CUtensorMap& tv, const XattnTcParams& p, int dev, int sms, cudaStream_t s) {
+  if (d == 64) return launch<64, 64>(tq, tk, tv, p, dev, sms, s);
+  if (dm == 80) return launch<128, 80>(tq, tk, tv, p, dev, sms, s);
+  return launch<128, 128>(tq, tk, tv, p, dev, sms, s);
+}
+
+}  // namespace mw
