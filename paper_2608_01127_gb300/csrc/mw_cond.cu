@@ -63,6 +63,44 @@ size_t xattn_ws(const XattnSizes& z, int S, int d) {
   return align256(rows * kernel_d(d) * sizeof(float)) + align256(rows * sizeof(float));
 }
 
+// Ranges of a head's query tiles in the backward: pieces of work that fill the
+// SMs, against what a sweep costs besides its steps (about two).
+int xattn_bwd_ranges(int BH, int q_tiles, int k_tiles) {
+  int best = 1;
+  long long best_cost = LLONG_MAX;
+  for (int r = 1; r <= q_tiles; ++r) {
+    const long long waves = ceil_div(static_cast<long long>(BH) * r, kNormSms);
+    const long long cost = waves * k_tiles * (ceil_div(q_tiles, r) + 2);
+    if (cost < best_cost) {
+      best_cost = cost;
+      best = r;
+    }
+    if (waves > 64) break;
+  }
+  return best;
+}
+
+// The backward's workspace: byte offsets of its fp32 arrays.
+struct XattnBwdWs {
+  int M_pad = 0, S_pad = 0;
+  size_t dq = 0, dk = 0, dv = 0, lse2 = 0, delta = 0, bias = 0, total = 0;
+};
+
+XattnBwdWs xattn_bwd_ws(const XattnSizes& z, int S, int d) {
+  XattnBwdWs w;
+  const int D = kernel_d(d);
+  w.M_pad = ceil_div(z.rows, kTileRows) * kTileRows;
+  w.S_pad = ceil_div(S, kTileRows) * kTileRows;
+  const size_t rows = static_cast<size_t>(z.BH) * w.M_pad, keys = static_cast<size_t>(z.BH) * w.S_pad;
+  w.dk = align256(rows * D * 4);
+  w.dv = w.dk + align256(keys * D * 4);
+  w.lse2 = w.dv + align256(keys * D * 4);
+  w.delta = w.lse2 + align256(rows * 4);
+  w.bias = w.delta + align256(rows * 4);
+  w.total = w.bias + (D == 64 ? align256(rows * 32) : 0);
+  return w;
+}
+
 mw_status check_f32(const void* p, const char* name) {
   if (reinterpret_cast<uintptr_t>(p) & 3u)
     return fail(MW_ERR_INVALID_ARG, "%s is not 4-byte aligned", name);
@@ -186,15 +224,14 @@ mw_status mw_xattn_fwd(const void* q, const void* k, const void* v, const int* k
   p.M = z.rows;
   p.S = S;
   p.d = d;
-  p.scale = scale;
   p.scale_log2 = scale * 1.4426950408889634f;
   return launch_status(launch_xattn_fwd(p, s), "cross attention forward launch");
 }
 
 size_t mw_xattn_bwd_workspace_size(int B, int H, int Hkv, int M, int S, int d) {
   XattnSizes z;
-  if (xattn_sizes(&z, B, H, Hkv, M, S, d) != MW_OK) return 0;
-  return 0;
+  if (xattn_sizes(&z, B, H, Hkv, M, S, d) != MW_OK || M == 0 || S == 0) return 0;
+  return xattn_bwd_ws(z, S, d).total;
 }
 
 mw_status mw_xattn_bwd(const void* q, const void* k, const void* v, const int* kv_len, const void* o,
@@ -219,28 +256,73 @@ mw_status mw_xattn_bwd(const void* q, const void* k, const void* v, const int* k
     MW_TRY(check_ptr(dv, "dv"));
   }
   MW_TRY(check_f32(kv_len, "kv_len"));
+  const bool empty = M == 0 || S == 0;
+  const XattnBwdWs ws = empty ? XattnBwdWs{} : xattn_bwd_ws(z, S, d);
+  if (!empty) {
+    if (workspace == nullptr || ws_bytes < ws.total)
+      return fail(MW_ERR_WORKSPACE, "workspace %zu bytes, need %zu", ws_bytes, ws.total);
+    if (reinterpret_cast<uintptr_t>(workspace) & 255u)
+      return fail(MW_ERR_INVALID_ARG, "workspace is not 256-byte aligned");
+  }
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   DeviceScope scope(s);
   MW_TRY(scope.status());
-  XattnParams p{};
-  p.q = static_cast<const __nv_bfloat16*>(q);
-  p.k = static_cast<const __nv_bfloat16*>(k);
-  p.v = static_cast<const __nv_bfloat16*>(v);
+  if (empty) {  // no pairs: zero gradients
+    const size_t row = static_cast<size_t>(d) * 2;
+    if (M > 0) MW_TRY(launch_status(cudaMemsetAsync(dq, 0, z.BH * row * z.rows, s), "clearing dq"));
+    if (S > 0) {
+      MW_TRY(launch_status(cudaMemsetAsync(dk, 0, z.BH * row * S, s), "clearing dk"));
+      MW_TRY(launch_status(cudaMemsetAsync(dv, 0, z.BH * row * S, s), "clearing dv"));
+    }
+    return ok();
+  }
+  const int D = kernel_d(d);
+  char* base = static_cast<char*>(workspace);
+  auto at = [&](size_t off) { return reinterpret_cast<float*>(base + off); };
+  XattnBwdParams p{};
+  MW_TRY(status_ptr(scope.device(), &p.status));
   p.kv_len = kv_len;
-  p.o = static_cast<__nv_bfloat16*>(const_cast<void*>(o));
-  p.lse = const_cast<float*>(lse);
   p.BH = z.BH;
   p.heads = Hkv;
   p.M = z.rows;
+  p.M_pad = ws.M_pad;
   p.S = S;
   p.d = d;
-  p.scale = scale;
+  p.ranges = xattn_bwd_ranges(z.BH, ws.M_pad / kTileRows, ws.S_pad / kTileRows);
+  p.pieces = z.BH * p.ranges;
   p.scale_log2 = scale * 1.4426950408889634f;
-  p.dout = static_cast<const __nv_bfloat16*>(dout);
-  p.dq = static_cast<__nv_bfloat16*>(dq);
-  p.dk = static_cast<__nv_bfloat16*>(dk);
-  p.dv = static_cast<__nv_bfloat16*>(dv);
-  return launch_status(launch_xattn_bwd(p, s), "cross attention backward launch");
+  p.lse2 = at(ws.lse2);
+  p.delta = at(ws.delta);
+  p.budget_ns = budget_ns();
+  p.debug_skip_q = debug_skip_q();
+  float* bias = D == 64 ? at(ws.bias) : nullptr;
+  XattnBwdMaps m;
+  MW_TRY(make_map(&m.q, q, z.rows, z.BH, d, "q"));
+  MW_TRY(make_map(&m.k, k, S, z.BH, d, "k"));
+  MW_TRY(make_map(&m.v, v, S, z.BH, d, "v"));
+  MW_TRY(make_map(&m.dout, dout, z.rows, z.BH, d, "dout"));
+  MW_TRY(make_map(&m.dq, at(ws.dq), ws.M_pad, z.BH, D, "dq_acc", 32, true, d));
+  MW_TRY(make_map(&m.dk, at(ws.dk), ws.S_pad, z.BH, D, "dk_acc", 32, true, d));
+  MW_TRY(make_map(&m.dv, at(ws.dv), ws.S_pad, z.BH, D, "dv_acc", 32, true, d));
+  m.bias = m.dq;  // d = 128: unused
+  if (bias) MW_TRY(encode_bias_map(&m.bias, bias, ws.M_pad, z.BH, kTileRows));
+  MW_TRY(launch_status(launch_bwd_pre(D, d, static_cast<const __nv_bfloat16*>(o),
+                                      static_cast<const __nv_bfloat16*>(dout), lse, at(ws.lse2),
+                                      at(ws.delta), at(ws.dq), bias, 1.f / scale, z.BH, z.rows,
+                                      ws.M_pad, s),
+                       "cross attention backward pre kernel launch"));
+  MW_TRY(launch_status(cudaMemsetAsync(at(ws.dk), 0, ws.lse2 - ws.dk, s), "clearing dK and dV"));
+  MW_TRY(launch_status(launch_xattn_bwd_main(D, mma_d(d), m, p, scope.device(), sm_count(), s),
+                       "cross attention backward launch"));
+  MW_TRY(launch_status(launch_bwd_post(D, d, at(ws.dq), static_cast<__nv_bfloat16*>(dq), scale, z.BH,
+                                       z.rows, ws.M_pad, s),
+                       "dQ post kernel launch"));
+  MW_TRY(launch_status(launch_bwd_post(D, d, at(ws.dk), static_cast<__nv_bfloat16*>(dk), scale, z.BH, S,
+                                       ws.S_pad, s),
+                       "dK post kernel launch"));
+  return launch_status(launch_bwd_post(D, d, at(ws.dv), static_cast<__nv_bfloat16*>(dv), 1.f, z.BH, S,
+                                       ws.S_pad, s),
+                       "dV post kernel launch");
 }
 
 mw_status mw_layernorm_fwd(const void* x, const void* weight, const void* bias, void* y, float* mean,

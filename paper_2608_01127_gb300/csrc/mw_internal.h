@@ -232,12 +232,7 @@ struct XattnParams {
   __nv_bfloat16* o;
   float* lse;          // nullable
   int BH, heads, M, S, d;
-  float scale, scale_log2;
-  // backward
-  const __nv_bfloat16* dout;
-  __nv_bfloat16* dq;
-  __nv_bfloat16* dk;
-  __nv_bfloat16* dv;
+  float scale_log2;
 };
 // Forward on tensor cores (mw_xattn_fwd.cu): blocks of kFwdBlockRows rows of one
 // head against one of num_splits ranges of its key tiles.
@@ -261,6 +256,26 @@ cudaError_t launch_xattn_tc(int d, int dm, const CUtensorMap& tq, const CUtensor
                             const CUtensorMap& tv, const XattnTcParams& p, int dev, int sms, cudaStream_t s);
 // Forward of few rows a head on CUDA cores (mw_xattn.cu).
 cudaError_t launch_xattn_fwd(const XattnParams& p, cudaStream_t s);
-cudaError_t launch_xattn_bwd(const XattnParams& p, cudaStream_t s);
+
+// Backward on tensor cores (mw_xattn_bwd.cu); its D, LSE and bias rows come from
+// launch_bwd_pre, its accumulators become bf16 with launch_bwd_post.
+struct XattnBwdParams {
+  const int* kv_len;
+  int BH, heads, M, M_pad, S, d;  // M_pad: M rounded up to kTileRows
+  int ranges, pieces;  // ranges of a head's query tiles; BH * ranges
+  float scale_log2;
+  const float* lse2;   // [BH, M_pad]
+  const float* delta;  // [BH, M_pad]
+  unsigned* status;
+  unsigned long long budget_ns;
+  int debug_skip_q;
+};
+// dq [BH, M_pad, D], dk, dv [BH, S_pad, D]: f32 accumulators, 32 x 32 boxes; bias as
+// for launch_bwd_main
+struct XattnBwdMaps {
+  CUtensorMap q, k, v, dout, dq, dk, dv, bias;
+};
+cudaError_t launch_xattn_bwd_main(int d, int dm, const XattnBwdMaps& m, const XattnBwdParams& p, int dev, int sms,
+                                  cudaStream_t s);
 
 }  // namespace mw

@@ -1,13 +1,11 @@
-// Cross attention on CUDA cores: queries against an encoder's states of another
-// length, of which a sample has some number valid (Sec. 4.1's conditioning).
+// Cross attention of few query rows a head on CUDA cores: single new tokens against
+// an encoder's states, of which a sample has some number valid.
 //
 //   s_ij = scale <q_i, k_j> for j < len; LSE_i = ln sum_j exp(s_ij);
 //   P = exp(s - LSE), O = P V; len = 0: O = 0, LSE = -inf
-//   D_i = <dO_i, O_i>; dS = P (dO V^T - D); dV = P^T dO,
-//   dQ = scale dS K, dK = scale dS^T Q
 //
-// L lanes hold one key's (or query's) d channels, 8 each, so that a warp works
-// on 32 / L of them at once; a dot product is 8 FMAs and log2(L) shuffles.
+// L lanes hold one key's d channels, 8 each, so that a warp works on 32 / L keys at
+// once; a dot product is 8 FMAs and log2(L) shuffles.
 #include "mw_internal.h"
 #include "mw_ptx.cuh"
 
@@ -24,12 +22,6 @@ __device__ __forceinline__ void load8(const __nv_bfloat16* p, bool there, float 
     v[2 * k] = __uint_as_float(w[k] << 16);
     v[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
   }
-}
-
-__device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&v)[8], float mul) {
-  *reinterpret_cast<uint4*>(p) =
-      make_uint4(pack_bf16x2(v[0] * mul, v[1] * mul), pack_bf16x2(v[2] * mul, v[3] * mul),
-                 pack_bf16x2(v[4] * mul, v[5] * mul), pack_bf16x2(v[6] * mul, v[7] * mul));
 }
 
 // <a, b> over the channels of L lanes, in each of them.
@@ -126,92 +118,6 @@ __global__ void __launch_bounds__(kWarps * 32) xattn_fwd_kernel(const XattnParam
   }
 }
 
-// dQ: a row a warp, its keys 32 / L at a time.
-template <int L>
-__global__ void __launch_bounds__(kWarps * 32) xattn_dq_kernel(const XattnParams p) {
-  constexpr int G = 32 / L;
-  const int lane = threadIdx.x & 31, c = 8 * (lane % L);
-  const bool in = c < p.d;
-  const long long row = static_cast<long long>(blockIdx.x) * kWarps + (threadIdx.x >> 5);
-  if (row >= static_cast<long long>(p.BH) * p.M) return;
-  const int bh = static_cast<int>(row / p.M), len = valid_keys(p, bh);
-  const size_t at = static_cast<size_t>(row) * p.d + c;
-  float q[8], g[8], o[8], dq[8] = {};
-  load8(p.q + at, in, q);
-  load8(p.dout + at, in, g);
-  load8(p.o + at, in, o);
-  const float D = dot<L>(g, o), lse2 = p.lse[row] * 1.4426950408889634f;
-  for (int j0 = 0; j0 < len; j0 += G) {
-    const int j = j0 + lane / L;
-    const size_t kt = (static_cast<size_t>(bh) * p.S + j) * p.d + c;
-    float k8[8], v8[8];
-    load8(p.k + kt, in && j < len, k8);
-    load8(p.v + kt, in && j < len, v8);
-    const float s = dot<L>(q, k8), dp = dot<L>(g, v8);
-    const float ds = j < len ? ex2_approx(fmaf(s, p.scale_log2, -lse2)) * (dp - D) : 0.f;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) dq[k] = fmaf(ds, k8[k], dq[k]);
-  }
-#pragma unroll
-  for (int s = L; s < 32; s <<= 1)
-#pragma unroll
-    for (int k = 0; k < 8; ++k) dq[k] += __shfl_xor_sync(0xffffffffu, dq[k], s);
-  if (lane < L && in) store8(p.dq + at, dq, p.scale);
-}
-
-// dK, dV: a key a warp, its head's rows 32 / L at a time.
-template <int L>
-__global__ void __launch_bounds__(kWarps * 32) xattn_dkv_kernel(const XattnParams p) {
-  constexpr int G = 32 / L;
-  const int lane = threadIdx.x & 31, c = 8 * (lane % L);
-  const bool in = c < p.d;
-  const long long key = static_cast<long long>(blockIdx.x) * kWarps + (threadIdx.x >> 5);
-  if (key >= static_cast<long long>(p.BH) * p.S) return;
-  const int bh = static_cast<int>(key / p.S), j = static_cast<int>(key % p.S);
-  const bool seen = j < valid_keys(p, bh);
-  const size_t kt = static_cast<size_t>(key) * p.d + c;
-  float k8[8], v8[8], dk[8] = {}, dv[8] = {};
-  load8(p.k + kt, in && seen, k8);
-  load8(p.v + kt, in && seen, v8);
-  for (int i0 = 0; seen && i0 < p.M; i0 += G) {
-    const int i = i0 + lane / L;
-    const size_t row = static_cast<size_t>(bh) * p.M + i, at = row * p.d + c;
-    float q[8], g[8], o[8];
-    load8(p.q + at, in && i < p.M, q);
-    load8(p.dout + at, in && i < p.M, g);
-    load8(p.o + at, in && i < p.M, o);
-    const float s = dot<L>(q, k8), dp = dot<L>(g, v8), D = dot<L>(g, o);
-    const float w = i < p.M ? ex2_approx(fmaf(s, p.scale_log2, -p.lse[row] * 1.4426950408889634f)) : 0.f;
-    const float ds = w * (dp - D);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      dv[k] = fmaf(w, g[k], dv[k]);
-      dk[k] = fmaf(ds, q[k], dk[k]);
-    }
-  }
-#pragma unroll
-  for (int s = L; s < 32; s <<= 1)
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      dk[k] += __shfl_xor_sync(0xffffffffu, dk[k], s);
-      dv[k] += __shfl_xor_sync(0xffffffffu, dv[k], s);
-    }
-  if (lane < L && in) {
-    store8(p.dk + kt, dk, p.scale);
-    store8(p.dv + kt, dv, 1.f);
-  }
-}
-
-template <int L>
-cudaError_t bwd(const XattnParams& p, cudaStream_t s) {
-  const long long rows = static_cast<long long>(p.BH) * p.M, keys = static_cast<long long>(p.BH) * p.S;
-  if (rows > 0)
-    xattn_dq_kernel<L><<<static_cast<unsigned>((rows + kWarps - 1) / kWarps), kWarps * 32, 0, s>>>(p);
-  if (keys > 0)
-    xattn_dkv_kernel<L><<<static_cast<unsigned>((keys + kWarps - 1) / kWarps), kWarps * 32, 0, s>>>(p);
-  return cudaGetLastError();
-}
-
 template <int L, int R>
 cudaError_t fwd(const XattnParams& p, cudaStream_t s) {
   const unsigned grid = static_cast<unsigned>(p.BH) * ((p.M + R - 1) / R);
@@ -224,10 +130,6 @@ cudaError_t fwd(const XattnParams& p, cudaStream_t s) {
 cudaError_t launch_xattn_fwd(const XattnParams& p, cudaStream_t s) {
   if (p.M == 1) return p.d == 64 ? fwd<8, 1>(p, s) : fwd<16, 1>(p, s);
   return p.d == 64 ? fwd<8, 4>(p, s) : fwd<16, 4>(p, s);
-}
-
-cudaError_t launch_xattn_bwd(const XattnParams& p, cudaStream_t s) {
-  return p.d == 64 ? bwd<8>(p, s) : bwd<16>(p, s);
 }
 
 }  // namespace mw

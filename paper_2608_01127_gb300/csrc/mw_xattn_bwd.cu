@@ -1,0 +1,722 @@
+// Cross attention backward on sm_103a: the gradients of queries against an
+// encoder's states.
+//
+// The block-causal backward gives every key tile a CTA that visits all query
+// rows that see it.  An encoder's states are often only a few key tiles, too few
+// CTAs, so here a piece of work is a range of query tiles of one head, and a CTA
+// (persistent, one an SM) takes its pieces through all key tiles of the head:
+// one sweep over the range a key tile, in which dK and dV of the tile stay in
+// tensor memory.  At the end of a sweep they are added to fp32 accumulators, as dQ is
+// after every step.  Per step (128 keys x 128 queries), as in the block-causal
+// backward, whose arrangement of tensor memory and roles this kernel shares:
+//   S^T = K Q^T, dP^T = V dO^T              (tcgen05 -> TMEM)
+//   P^T = exp2(scale log2e S^T - LSE2), dS^T = P^T (dP^T - D)   (registers)
+//   dV += P^T dO, dK += dS^T Q, dQ = dS K   (tcgen05)
+//   dQacc += dQ                             (TMA reduce-add of fp32 boxes)
+// d = 64: LSE and D enter S^T and dP^T through a tf32 MMA each.
+//
+// Roles (512 threads): warps 0-7 P/dS (two warpgroups, one half of the query
+// columns each, one key row per thread), warps 8-11 drain (dQ after every step, dK
+// and dV after a sweep, while the next one starts), warp 12 TMA producer, warps 13
+// and 14 MMA issuers (13: S^T, dV, dP^T; 14: dK, dQ), warp 15 K and V tiles that end
+// inside the valid states (what the rows past them hold, NaN included, becomes 0).
+#include "mw_internal.h"
+#include "mw_ptx.cuh"
+
+namespace mw {
+namespace {
+
+// D: width of the shared-memory tiles; DM <= D: the columns the MMAs cover
+template <int D, int DM>
+struct Layout {
+  static constexpr int QN = bwd_q_rows(D);           // query rows per step
+  static constexpr bool DQT = (D == 128);            // dQ produced transposed
+  static constexpr int CW = QN / 2;                  // query columns per P/dS warpgroup
+  static constexpr int REG = D / 64;                 // 64-column swizzle regions per row
+  static constexpr int KREGION = kTileRows * 128;
+  static constexpr int QREGION = QN * 128;
+  static constexpr int KTILE = REG * KREGION;
+  static constexpr int QTILE = REG * QREGION;
+  static constexpr int QSTAGES = (D == 64) ? 3 : 2;
+  static constexpr int DOSTAGES = (D == 64) ? 3 : 1;
+  static constexpr int DS_BYTES = (QN / 64) * KREGION;  // dS^T: 128 key rows x QN columns
+  static constexpr int DS_BUFS = (D == 64) ? 2 : 1;
+  static constexpr int BOX_BYTES = 32 * 32 * 4;
+  static constexpr int BOXES = DQT ? 2 : 1;          // staging boxes per drain warp
+  static constexpr bool FOLD = (D == 64);            // LSE and D through tf32 MMAs
+  static constexpr int BIAS_BYTES = FOLD ? QN * 32 : 0;
+  static constexpr int QSTRIDE = QTILE + BIAS_BYTES;
+  static constexpr int VEC_BYTES = FOLD ? 0 : QN * 4;
+  static constexpr int ONES_BYTES = FOLD ? 512 : 0;
+  static constexpr int OFF_K = 0;
+  static constexpr int OFF_V = OFF_K + KTILE;
+  static constexpr int OFF_Q = OFF_V + KTILE;
+  static constexpr int OFF_DO = OFF_Q + QSTAGES * QSTRIDE;
+  static constexpr int OFF_DS = OFF_DO + DOSTAGES * QTILE;
+  static constexpr int OFF_STG = OFF_DS + DS_BUFS * DS_BYTES;
+  static constexpr int OFF_LSE = OFF_STG + BOXES * 4 * BOX_BYTES;
+  static constexpr int OFF_DELTA = OFF_LSE + QSTAGES * VEC_BYTES;
+  static constexpr int OFF_ONES = OFF_DELTA + 2 * VEC_BYTES;
+  static constexpr int OFF_BAR = OFF_ONES + ONES_BYTES;
+  static constexpr int NBAR = 3 + 2 * (QSTAGES + DOSTAGES) + 9 + 2 * DS_BUFS;
+  static constexpr int OFF_MISC = OFF_BAR + NBAR * 8;
+  static constexpr int BYTES = OFF_MISC + 16;
+  // d = 128 has no room for S^T, dP^T, P^T and dQ^T in columns of their own: P^T
+  // overwrites S^T and dQ^T overwrites dP^T (each is in registers by then)
+  static constexpr bool PAIRED = (D == 128);
+  static constexpr uint32_t DV_COL = 0;
+  static constexpr uint32_t DK_COL = D;
+  static constexpr uint32_t S_COL = 2 * D;
+  static constexpr uint32_t DP_COL = 2 * D + QN;
+  static constexpr uint32_t P_COL = PAIRED ? S_COL : 384u;
+  static constexpr uint32_t DQ_COL = PAIRED ? DP_COL : 448u;
+  static constexpr int THREADS = 512;
+  // registers after the re-split between the P/dS warpgroups, the drain and the
+  // control warpgroup: exactly the launch's 512 x 128
+  static constexpr int REGS_LAUNCH = 128;
+  static constexpr int REGS_PDS = (D == 64) ? 168 : 144;
+  static constexpr int REGS_DRAIN = (D == 64) ? 88 : 144;
+  static constexpr int REGS_CONTROL = (D == 64) ? 88 : 80;
+  static_assert(256 * REGS_PDS + 128 * REGS_DRAIN + 128 * REGS_CONTROL == THREADS * REGS_LAUNCH,
+                "register re-split must hand out exactly the launch's registers");
+  static_assert(BYTES <= 232448, "shared memory");
+};
+
+// The sweeps of a CTA in turn: its pieces' key tiles.  Every role walks through
+// the same ones.
+struct Walk {
+  const XattnBwdParams& p;
+  int next;         // index of the next piece
+  int bh, q0, n_q;  // head, first query tile and query tiles of the piece
+  int len, sample;  // valid states of the head's sample
+  int kt, n_kt;     // key tile, key tiles
+  __device__ explicit Walk(const XattnBwdParams& p_)
+      : p(p_), next(blockIdx.x), len(p_.S), sample(-1), kt(0), n_kt(0) {}
+  __device__ __forceinline__ bool step() {
+    if (++kt < n_kt) return true;
+    while (next < p.pieces) {
+      const int x = next;
+      next += gridDim.x;
+      bh = x / p.ranges;
+      const int r = x - bh * p.ranges;
+      if (p.kv_len) {
+        const int s = bh / p.heads;
+        if (s != sample) {
+          sample = s;
+          len = min(max(p.kv_len[s], 0), p.S);
+        }
+      }
+      const int tiles = p.M_pad / 128;
+      q0 = static_cast<int>(static_cast<long long>(r) * tiles / p.ranges);
+      n_q = static_cast<int>(static_cast<long long>(r + 1) * tiles / p.ranges) - q0;
+      n_kt = (len + kTileRows - 1) / kTileRows;
+      kt = 0;
+      if (n_kt > 0) return true;
+    }
+    return false;
+  }
+  // the key tile has rows that count as nothing but may hold anything
+  __device__ __forceinline__ bool ragged() const { return (kt + 1) * kTileRows > len && len < p.S; }
+};
+
+template <int D, int DM>
+__global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
+    xattn_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
+                     const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_do,
+                     const __grid_constant__ CUtensorMap tm_dq, const __grid_constant__ CUtensorMap tm_dk,
+                     const __grid_constant__ CUtensorMap tm_dv, const __grid_constant__ CUtensorMap tm_bias,
+                     const __grid_constant__ XattnBwdParams p) {
+  using L = Layout<D, DM>;
+  constexpr int NQ = L::QSTAGES;
+  constexpr int ND = L::DOSTAGES;
+  constexpr int QN = L::QN;
+  constexpr int CW = L::CW;
+  constexpr int NB = L::DS_BUFS;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  if ((smem_u32(smem) & 1023u) != 0u) {
+    // nothing runs without aligned shared memory: report it (the accumulators
+    // keep the zeros they start with)
+    if (threadIdx.x == 0) atomicOr(p.status, kDevMisaligned);
+    return;  // uniform across the CTA, before any barrier or TMEM use
+  }
+  uint64_t* kv_full = reinterpret_cast<uint64_t*>(smem + L::OFF_BAR);
+  uint64_t* kv_raw = kv_full + 1;   // K and V that warp 15 makes ready, then kv_full
+  uint64_t* kv_empty = kv_raw + 1;
+  uint64_t* q_full = kv_empty + 1;
+  uint64_t* q_empty = q_full + NQ;
+  uint64_t* do_full = q_empty + NQ;
+  uint64_t* do_empty = do_full + ND;
+  uint64_t* s_full = do_empty + ND;
+  uint64_t* s_free = s_full + 1;
+  uint64_t* dp_full = s_free + 1;
+  uint64_t* dp_free = dp_full + 1;
+  uint64_t* pt_ready = dp_free + 1;
+  uint64_t* dq_full = pt_ready + 1;
+  uint64_t* dq_free = dq_full + 1;
+  uint64_t* dkv_full = dq_free + 1;
+  uint64_t* dkv_free = dkv_full + 1;
+  uint64_t* p_ready = dkv_free + 1;
+  uint64_t* ds_free = p_ready + NB;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + L::OFF_MISC);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + L::OFF_MISC + 4);
+
+  const int warp = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31;
+  if constexpr (L::FOLD) {
+    // A rows of the bias MMAs: [1 1 0 0 | 1 1 0 0] picks the LSE pair of a bias
+    // row, [0 0 1 1 | 0 0 1 1] its D pair; both 16-byte halves alike, so the
+    // 32-byte swizzle leaves them unchanged (8 rows of each)
+    if (threadIdx.x < 128) {
+      const int a = threadIdx.x >> 6, c = threadIdx.x & 7;
+      reinterpret_cast<float*>(smem + L::OFF_ONES)[threadIdx.x] = (((c & 3) < 2) == (a == 0)) ? 1.f : 0.f;
+      fence_proxy_async_smem();
+    }
+  }
+  if (threadIdx.x == 0) {
+    mbar_init(kv_full, 1);
+    mbar_init(kv_raw, 1);
+    mbar_init(kv_empty, 2);
+    for (int s = 0; s < NQ; ++s) {
+      mbar_init(&q_full[s], 1);
+      mbar_init(&q_empty[s], 1);
+    }
+    for (int s = 0; s < ND; ++s) {
+      mbar_init(&do_full[s], 1);
+      mbar_init(&do_empty[s], 1);
+    }
+    mbar_init(s_full, 1);
+    mbar_init(s_free, 8);
+    mbar_init(dp_full, 1);
+    mbar_init(dp_free, 8);
+    mbar_init(pt_ready, 8);
+    mbar_init(dq_full, 1);
+    mbar_init(dq_free, 4);
+    mbar_init(dkv_full, 2);
+    mbar_init(dkv_free, 4);
+    for (int b = 0; b < NB; ++b) {
+      mbar_init(&p_ready[b], 8);
+      mbar_init(&ds_free[b], 1);
+    }
+    *abort_flag = 0;
+    fence_mbar_init();
+  }
+  if (warp == 13) {
+    tmem_alloc(tmem_slot, 512);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  const WaitCtl ctl{abort_flag, p.status, p.budget_ns};
+
+  uint8_t* sK = smem + L::OFF_K;
+  uint8_t* sV = smem + L::OFF_V;
+  uint8_t* sQ = smem + L::OFF_Q;
+  uint8_t* sDO = smem + L::OFF_DO;
+  uint8_t* sDS = smem + L::OFF_DS;
+  float* sLSE = reinterpret_cast<float*>(smem + L::OFF_LSE);
+  float* sDelta = reinterpret_cast<float*>(smem + L::OFF_DELTA);
+  Walk w(p);
+
+  if (warp >= 12) {
+  regs_dec<L::REGS_CONTROL>();
+  if (warp == 12) {
+    // ------------------------------------------------------------ TMA producer
+    if (lane == 0) {
+      prefetch_tmap(&tm_q);
+      prefetch_tmap(&tm_do);
+      int sw = 0, raws = 0, n_q = 0, n_do = 0;  // sweeps, those through warp 15, Q and dO tiles so far
+      bool ok = true, raw = false;
+      auto load_q = [&](int q) {
+        const int st = n_q % NQ;
+        if (!mbar_wait(&q_empty[st], ((n_q / NQ) & 1) ^ 1, ctl)) return false;
+        if (p.debug_skip_q) return true;
+        mbar_arrive_expect_tx(&q_full[st], L::QTILE + L::BIAS_BYTES + L::VEC_BYTES);
+        for (int r = 0; r < L::REG; ++r)
+          tma_load_3d(sQ + st * L::QSTRIDE + r * L::QREGION, &tm_q, &q_full[st], 64 * r, q, w.bh);
+        if constexpr (L::FOLD)
+          tma_load_3d(sQ + st * L::QSTRIDE + L::QTILE, &tm_bias, &q_full[st], 0, q, w.bh);
+        else
+          bulk_load(sLSE + st * QN, p.lse2 + static_cast<size_t>(w.bh) * p.M_pad + q, L::VEC_BYTES, &q_full[st]);
+        ++n_q;
+        return true;
+      };
+      auto load_do = [&](int q) {
+        const int sd = n_do % ND;
+        if (!mbar_wait(&do_empty[sd], ((n_do / ND) & 1) ^ 1, ctl)) return false;
+        mbar_arrive_expect_tx(&do_full[sd], L::QTILE + L::VEC_BYTES);
+        for (int r = 0; r < L::REG; ++r)
+          tma_load_3d(sDO + sd * L::QTILE + r * L::QREGION, &tm_do, &do_full[sd], 64 * r, q, w.bh);
+        if constexpr (!L::FOLD)
+          bulk_load(sDelta + (n_do & 1) * QN, p.delta + static_cast<size_t>(w.bh) * p.M_pad + q, L::VEC_BYTES,
+                    &do_full[sd]);
+        ++n_do;
+        return true;
+      };
+      while (ok && w.step()) {
+        // the first query tile ahead of K and V, which wait for the last sweep's end
+        if (!(ok = load_q(w.q0 * QN))) break;
+        if (!(ok = mbar_wait(kv_empty, (sw & 1) ^ 1, ctl))) break;
+        raw = w.ragged();
+        uint64_t* bar = raw ? kv_raw : kv_full;
+        mbar_arrive_expect_tx(bar, 2 * L::KTILE);
+        for (int r = 0; r < L::REG; ++r) {
+          tma_load_3d(sK + r * L::KREGION, &tm_k, bar, 64 * r, w.kt * kTileRows, w.bh);
+          tma_load_3d(sV + r * L::KREGION, &tm_v, bar, 64 * r, w.kt * kTileRows, w.bh);
+        }
+        ++sw;
+        raws += raw;
+        if (!(ok = load_do(w.q0 * QN))) break;
+        for (int j = 1; ok && j < w.n_q; ++j) ok = load_q((w.q0 + j) * QN) && load_do((w.q0 + j) * QN);
+      }
+      if (*abort_flag || !ok) {
+        // let every copy this CTA started land before shared memory goes away
+        if (sw > 0) drain_wait(raw ? kv_raw : kv_full, ((raw ? raws : sw) - 1) & 1, p.budget_ns);
+        for (int j = max(0, n_q - NQ); j < n_q; ++j) drain_wait(&q_full[j % NQ], (j / NQ) & 1, p.budget_ns);
+        for (int j = max(0, n_do - ND); j < n_do; ++j) drain_wait(&do_full[j % ND], (j / ND) & 1, p.budget_ns);
+      }
+    }
+  } else if (warp == 13 || warp == 14) {
+    // ------------------------------------------------------------ MMA issuers (whole warps)
+    const bool role_a = warp == 13;  // S^T, dV, dP^T
+    constexpr uint32_t idesc_s = idesc_bf16_f32(128, QN, false, false);    // S^T, dP^T
+    constexpr uint32_t idesc_tn = idesc_bf16_f32(128, DM, false, true);    // dV, dK
+    // d = 64: dQ = dS K (M = query rows); d = 128: dQ^T = K^T dS^T (M = head dim)
+    constexpr uint32_t idesc_dq = L::DQT ? idesc_bf16_f32(128, QN, true, true)
+                                         : idesc_bf16_f32(128, D, true, true);
+    const uint32_t k_kmaj = sdesc_sw128(smem_u32(sK), 16);
+    const uint32_t v_kmaj = sdesc_sw128(smem_u32(sV), 16);
+    const uint32_t k_mn = sdesc_sw128(smem_u32(sK), L::KREGION);
+    const uint32_t q_kmaj0 = sdesc_sw128(smem_u32(sQ), 16);
+    const uint32_t do_kmaj0 = sdesc_sw128(smem_u32(sDO), 16);
+    const uint32_t q_mn0 = sdesc_sw128(smem_u32(sQ), L::QREGION);
+    const uint32_t do_mn0 = sdesc_sw128(smem_u32(sDO), L::QREGION);
+    const uint32_t ds_mn0 = sdesc_sw128(smem_u32(sDS), L::KREGION);
+    const uint32_t ds_kmaj0 = sdesc_sw128(smem_u32(sDS), 16);
+    const uint64_t ones_l = sdesc_sw32(smem_u32(smem + L::OFF_ONES), 0);
+    const uint64_t ones_d = sdesc_sw32(smem_u32(smem + L::OFF_ONES + 256), 0);
+    const uint64_t bias0 = sdesc_sw32(smem_u32(sQ + L::QTILE), 256);
+    auto add_bias = [&](uint32_t d_col, uint64_t ones, int stage) {
+      if constexpr (L::FOLD)
+        umma_ss_tf32(tmem + d_col, ones, sdesc_add(bias0, stage * L::QSTRIDE), idesc_tf32_f32(128, QN), 1u);
+    };
+    // X = A B^T, both K-major over d
+    auto issue_kmajor = [&](uint32_t d_col, uint32_t a, uint32_t b) {
+#pragma unroll
+      for (int kk = 0; kk < DM / 16; ++kk) {
+        const uint32_t ka = (kk >> 2) * L::KREGION + (kk & 3) * 32;
+        const uint32_t kq = (kk >> 2) * L::QREGION + (kk & 3) * 32;
+        umma_ss(tmem + d_col, sdesc_add(a, ka), sdesc_add(b, kq), idesc_s, kk > 0 ? 1u : 0u);
+      }
+    };
+    auto issue_s = [&](int g) {
+      issue_kmajor(L::S_COL, k_kmaj, sdesc_add(q_kmaj0, (g % NQ) * L::QSTRIDE));
+      add_bias(L::S_COL, ones_l, g % NQ);
+      umma_commit(s_full);
+    };
+    auto issue_dp = [&](int g) {
+      issue_kmajor(L::DP_COL, v_kmaj, sdesc_add(do_kmaj0, (g % ND) * L::QTILE));
+      add_bias(L::DP_COL, ones_d, g % NQ);
+      umma_commit(dp_full);
+    };
+    // TMEM column of the k-th 16-query slice of P^T (d = 128: each warpgroup's
+    // half in its own 64 columns of S^T)
+    auto pt_col = [](int kk) -> uint32_t {
+      return L::PAIRED ? L::P_COL + (kk >> 2) * 64 + (kk & 3) * 8 : L::P_COL + kk * 8;
+    };
+    auto issue_dv = [&](int g, bool acc) {  // dV += P^T dO
+      const uint32_t do_mn = sdesc_add(do_mn0, (g % ND) * L::QTILE);
+#pragma unroll
+      for (int kk = 0; kk < QN / 16; ++kk)
+        umma_ts(tmem + L::DV_COL, tmem + pt_col(kk), sdesc_add(do_mn, kk * 2048), idesc_tn,
+                (acc || kk > 0) ? 1u : 0u);
+    };
+    auto issue_dk = [&](int g, bool acc) {  // dK += dS^T Q
+      const uint32_t ds_kmaj = sdesc_add(ds_kmaj0, (g % NB) * L::DS_BYTES);
+      const uint32_t q_mn = sdesc_add(q_mn0, (g % NQ) * L::QSTRIDE);
+#pragma unroll
+      for (int kk = 0; kk < QN / 16; ++kk)
+        umma_ss(tmem + L::DK_COL, sdesc_add(ds_kmaj, (kk >> 2) * L::KREGION + (kk & 3) * 32),
+                sdesc_add(q_mn, kk * 2048), idesc_tn, (acc || kk > 0) ? 1u : 0u);
+    };
+    auto issue_dq = [&](int g) {
+      const uint32_t ds_mn = sdesc_add(ds_mn0, (g % NB) * L::DS_BYTES);
+#pragma unroll
+      for (int kk = 0; kk < kTileRows / 16; ++kk) {
+        if constexpr (L::DQT)
+          umma_ss(tmem + L::DQ_COL, sdesc_add(k_mn, kk * 2048), sdesc_add(ds_mn, kk * 2048), idesc_dq,
+                  kk > 0 ? 1u : 0u);
+        else
+          umma_ss(tmem + L::DQ_COL, sdesc_add(ds_mn, kk * 2048), sdesc_add(k_mn, kk * 2048), idesc_dq,
+                  kk > 0 ? 1u : 0u);
+      }
+    };
+    bool ok = true;
+    int g = 0, sw = 0;  // steps and sweeps so far
+    while (ok && w.step()) {
+      if (!(ok = warp_wait(kv_full, sw & 1, ctl))) break;
+      // the last sweep's dK and dV are out of tensor memory
+      auto wait_dkv = [&]() { return sw == 0 || warp_wait(dkv_free, (sw - 1) & 1, ctl); };
+      if (role_a) {
+        if (!(ok = warp_wait(&q_full[g % NQ], (g / NQ) & 1, ctl))) break;
+        if constexpr (!L::PAIRED)
+          if (g > 0 && !(ok = warp_wait(s_free, (g - 1) & 1, ctl))) break;
+        tc_fence_after();
+        issue_s(g);
+        if constexpr (!L::PAIRED) {
+          if (!(ok = warp_wait(&do_full[g % ND], (g / ND) & 1, ctl))) break;
+          if (g > 0 && !(ok = warp_wait(dp_free, (g - 1) & 1, ctl))) break;
+          tc_fence_after();
+          issue_dp(g);
+        }
+        for (int j = 0; j < w.n_q; ++j, ++g) {
+          const bool more = j + 1 < w.n_q;
+          if constexpr (L::PAIRED) {
+            // dP, dV, the next S: MMAs of one issuer run in order, so the next S may
+            // land on P once dV is issued
+            if (!(ok = warp_wait(&do_full[g % ND], (g / ND) & 1, ctl))) break;
+            // the last dQ is in the drain's registers: its columns take dP
+            if (g > 0 && !(ok = warp_wait(dq_free, (g - 1) & 1, ctl))) break;
+            tc_fence_after();
+            issue_dp(g);
+          } else if (more) {
+            // S^T of the next step as soon as the P/dS warps hold this one's
+            if (!(ok = warp_wait(s_free, g & 1, ctl))) break;
+            if (!(ok = warp_wait(&q_full[(g + 1) % NQ], ((g + 1) / NQ) & 1, ctl))) break;
+            tc_fence_after();
+            issue_s(g + 1);
+          }
+          if (!(ok = warp_wait(pt_ready, g & 1, ctl))) break;
+          if (j == 0 && !(ok = wait_dkv())) break;
+          tc_fence_after();
+          issue_dv(g, j > 0);
+          umma_commit(&do_empty[g % ND]);
+          if (!more) continue;
+          if constexpr (L::PAIRED) {
+            if (!(ok = warp_wait(&q_full[(g + 1) % NQ], ((g + 1) / NQ) & 1, ctl))) break;
+            tc_fence_after();
+            issue_s(g + 1);
+          } else {
+            // dP^T of the next step once the P/dS warps hold this one's
+            if (!(ok = warp_wait(dp_free, g & 1, ctl))) break;
+            if (!(ok = warp_wait(&do_full[(g + 1) % ND], ((g + 1) / ND) & 1, ctl))) break;
+            tc_fence_after();
+            issue_dp(g + 1);
+          }
+        }
+      } else {
+        for (int j = 0; j < w.n_q; ++j, ++g) {
+          // dS is in shared memory (and so dP in registers)
+          if (!(ok = warp_wait(&p_ready[g % NB], (g / NB) & 1, ctl))) break;
+          // dQ first, so the drain starts while dK runs
+          if constexpr (!L::PAIRED)
+            if (g > 0 && !(ok = warp_wait(dq_free, (g - 1) & 1, ctl))) break;
+          tc_fence_after();
+          issue_dq(g);
+          umma_commit(dq_full);
+          if (j == 0) {
+            if (!(ok = wait_dkv())) break;
+            tc_fence_after();
+          }
+          issue_dk(g, j > 0);
+          umma_commit(&q_empty[g % NQ]);
+          umma_commit(&ds_free[g % NB]);
+        }
+      }
+      if (!ok) break;
+      umma_commit(dkv_full);  // one arrival per issuing warp
+      umma_commit(kv_empty);
+      ++sw;
+    }
+  } else {
+    // ------------------------------------------------------------ ragged K and V tiles
+    int raws = 0;
+    while (w.step()) {
+      if (!w.ragged()) continue;
+      if (!warp_wait(kv_raw, raws & 1, ctl)) break;
+      ++raws;
+      const int limit = w.len - w.kt * kTileRows;
+      const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+      for (int i = limit * 8 + lane; i < kTileRows * 8; i += 32)
+        for (int r = 0; r < L::REG; ++r) {
+          *reinterpret_cast<uint4*>(sK + r * L::KREGION + i * 16) = zero;
+          *reinterpret_cast<uint4*>(sV + r * L::KREGION + i * 16) = zero;
+        }
+      fence_proxy_async_smem();  // the tensor core reads the tiles next
+      __syncwarp();
+      if (lane == 0) mbar_arrive(kv_full);
+    }
+  }
+  } else if (warp < 8) {
+    regs_inc<L::REGS_PDS>();
+    // ------------------------------------------------------------ P / dS (thread = key row)
+    const int wg = warp >> 2;            // query columns [CW wg, CW wg + CW)
+    const int wq = warp & 3;             // TMEM lane quadrant
+    const int j_local = wq * 32 + lane;
+    const uint32_t lane_base = tmem + (static_cast<uint32_t>(wq * 32) << 16);
+    const uint32_t s_addr = lane_base + L::S_COL + CW * wg;
+    const uint32_t dp_addr = lane_base + L::DP_COL + CW * wg;
+    const uint32_t p_addr = lane_base + L::P_COL + (L::PAIRED ? 64 : 32) * wg;
+    const float sl2 = p.scale_log2;
+    const int c0 = CW * wg;
+    const int ds_off = (c0 >> 6) * L::KREGION + j_local * 128;
+    const int chunk0 = (c0 & 63) >> 3;
+    const int sw = j_local & 7;
+    bool ok = true;
+    int g = 0;
+    while (ok && w.step()) {
+    const bool k_valid = w.kt * kTileRows + j_local < w.len;
+    const bool some_invalid = !__all_sync(0xffffffffu, k_valid);
+    for (int j = 0; j < w.n_q; ++j, ++g) {
+      const float* lse2 = sLSE + (g % NQ) * QN + c0;
+      const float* delta = sDelta + (g & 1) * QN + c0;
+      if (!(ok = warp_wait(s_full, g & 1, ctl))) break;
+      tc_fence_after();
+      float2 nl[CW / 2];
+      auto load_lse = [&]() {
+#pragma unroll
+        for (int c = 0; c < CW / 4; ++c) {
+          const float4 v = reinterpret_cast<const float4*>(lse2)[c];
+          nl[2 * c] = make_float2(-v.x, -v.y);
+          nl[2 * c + 1] = make_float2(-v.z, -v.w);
+        }
+      };
+      float pr[CW];
+      {
+        uint32_t r[CW / 32][32];
+#pragma unroll
+        for (int h = 0; h < CW / 32; ++h) tmem_ld32(s_addr + 32 * h, r[h]);
+        tmem_wait_ld();
+#pragma unroll
+        for (int h = 0; h < CW / 32; ++h)
+#pragma unroll
+          for (int k = 0; k < 32; ++k) pr[32 * h + k] = __uint_as_float(r[h][k]);
+      }
+      if constexpr (!L::PAIRED) {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(s_free);
+      }
+      if constexpr (!L::FOLD) load_lse();
+      const float2 sl2x2 = make_float2(sl2, sl2);
+#pragma unroll
+      for (int c = 0; c < CW / 2; ++c) {
+        // d = 64: the MMA already subtracted LSE/scale
+        const float2 x = L::FOLD ? mul2(make_float2(pr[2 * c], pr[2 * c + 1]), sl2x2)
+                                 : fma2(make_float2(pr[2 * c], pr[2 * c + 1]), sl2x2, nl[c]);
+        pr[2 * c] = ex2_approx(x.x);
+        pr[2 * c + 1] = ex2_approx(x.y);
+      }
+      if (some_invalid) {
+#pragma unroll
+        for (int c = 0; c < CW; ++c)
+          if (!k_valid) pr[c] = 0.f;
+      }
+      // P^T (bf16 pairs) -> TMEM right away, so that dV starts while dS is computed
+      uint32_t r[32];  // 32 columns of dP^T
+      if constexpr (!L::PAIRED) {
+        // dP^T is issued after the last dV: once it is there, that has read P^T.
+        // Its first half loads while P^T is stored.
+        if (!(ok = warp_wait(dp_full, g & 1, ctl))) break;
+        tc_fence_after();
+        tmem_ld32(dp_addr, r);
+      }
+      {
+        uint32_t pe[CW / 2];
+#pragma unroll
+        for (int c = 0; c < CW / 2; ++c) pe[c] = pack_bf16x2(pr[2 * c], pr[2 * c + 1]);
+        tmem_st32(p_addr, pe);
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(pt_ready);
+      }
+      if constexpr (L::PAIRED) {
+        if (!(ok = warp_wait(dp_full, g & 1, ctl))) break;
+        tc_fence_after();
+        tmem_ld32(dp_addr, r);
+      }
+      // the wait for the dS^T buffer passes while dP^T loads
+      const int buf = g % NB;
+      if (g >= NB && !(ok = warp_wait(&ds_free[buf], ((g / NB) - 1) & 1, ctl))) break;
+      uint32_t dk[CW / 2];
+#pragma unroll
+      for (int h = 0; h < CW / 32; ++h) {
+        if (h > 0) tmem_ld32(dp_addr + 32 * h, r);
+        tmem_wait_ld();
+        if (!L::PAIRED && h == CW / 32 - 1) {
+          // dP^T is in registers: its columns can take the next step's
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(dp_free);
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          // d = 64: the MMA already subtracted D
+          const float4 dv = L::FOLD ? make_float4(0.f, 0.f, 0.f, 0.f)
+                                    : reinterpret_cast<const float4*>(delta)[8 * h + k];
+          const int c = 32 * h + 4 * k;
+          const float2 dp0 = make_float2(__uint_as_float(r[4 * k]), __uint_as_float(r[4 * k + 1]));
+          const float2 dp1 = make_float2(__uint_as_float(r[4 * k + 2]), __uint_as_float(r[4 * k + 3]));
+          const float2 t0 = L::FOLD ? dp0 : add2(dp0, make_float2(-dv.x, -dv.y));
+          const float2 t1 = L::FOLD ? dp1 : add2(dp1, make_float2(-dv.z, -dv.w));
+          const float2 s0 = mul2(make_float2(pr[c], pr[c + 1]), t0);
+          const float2 s1 = mul2(make_float2(pr[c + 2], pr[c + 3]), t1);
+          dk[16 * h + 2 * k] = pack_bf16x2(s0.x, s0.y);
+          dk[16 * h + 2 * k + 1] = pack_bf16x2(s1.x, s1.y);
+        }
+      }
+      // dS^T row segment -> shared memory (swizzled like a TMA 128-byte tile)
+      uint8_t* ds_row = sDS + buf * L::DS_BYTES + ds_off;
+#pragma unroll
+      for (int q = 0; q < CW / 8; ++q)
+        *reinterpret_cast<uint4*>(ds_row + (((chunk0 + q) ^ sw) << 4)) =
+            make_uint4(dk[4 * q], dk[4 * q + 1], dk[4 * q + 2], dk[4 * q + 3]);
+      fence_proxy_async_smem();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&p_ready[buf]);
+    }
+    }
+  } else {
+    if constexpr (L::REGS_DRAIN > L::REGS_LAUNCH)
+      regs_inc<L::REGS_DRAIN>();
+    else
+      regs_dec<L::REGS_DRAIN>();
+    // ------------------------------------------------------------ drain
+    const int wq = warp & 3;
+    const uint32_t lane_base = tmem + (static_cast<uint32_t>(wq * 32) << 16);
+    int box = 0;  // the staging box whose turn it is
+    // 32 lanes x 32 columns as a box of 32 rows (128 bytes, 16-byte chunk c of row r
+    // at c ^ (r mod 8)) that the TMA unit adds to `map` at column c0, row `row`
+    auto add_rows = [&](const CUtensorMap* map, const uint32_t (&r)[32], int c0, int row) {
+      uint8_t* stg = smem + L::OFF_STG + (L::BOXES * wq + box) * L::BOX_BYTES;
+      if (lane == 0) bulk_wait_read<L::BOXES - 1>();  // the TMA unit has read this box
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        *reinterpret_cast<uint4*>(stg + lane * 128 + ((i ^ (lane & 7)) << 4)) =
+            make_uint4(r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]);
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) {
+        tma_reduce_add_3d(map, stg, c0, row, w.bh);
+        bulk_commit_group();
+      }
+      box ^= L::BOXES - 1;
+    };
+    bool ok = true;
+    int g = 0, sw = 0;
+    while (ok && w.step()) {
+      for (int j = 0; j < w.n_q; ++j, ++g) {
+        const int q0 = (w.q0 + j) * QN;
+        if (!(ok = warp_wait(dq_full, g & 1, ctl))) break;
+        tc_fence_after();
+        if constexpr (L::DQT) {
+          // lanes = head-dim columns, TMEM columns = the QN query rows: boxes of 32
+          // queries, each store instruction one of its rows.  The map clips columns
+          // past the caller's; warps with none skip.
+          uint32_t r[QN / 32][32];
+#pragma unroll
+          for (int c = 0; c < QN / 32; ++c) tmem_ld32(lane_base + L::DQ_COL + 32 * c, r[c]);
+          tmem_wait_ld();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(dq_free);  // dQ is in registers
+          if (32 * wq < p.d) {
+#pragma unroll
+            for (int c = 0; c < QN / 32; ++c) {
+              uint8_t* stg = smem + L::OFF_STG + (2 * wq + box) * L::BOX_BYTES;
+              if (lane == 0) bulk_wait_read<1>();
+              __syncwarp();
+#pragma unroll
+              for (int k = 0; k < 32; ++k)
+                *reinterpret_cast<uint32_t*>(stg + k * 128 + (((lane >> 2) ^ (k & 7)) << 4) + (lane & 3) * 4) =
+                    r[c][k];
+              fence_proxy_async_smem();
+              __syncwarp();
+              if (lane == 0) {
+                tma_reduce_add_3d(&tm_dq, stg, 32 * wq, q0 + 32 * c, w.bh);
+                bulk_commit_group();
+              }
+              box ^= 1;
+            }
+          }
+        } else {
+          // lanes = query rows
+          static_assert(D == 64 || L::DQT, "the drain below covers two 32-column boxes");
+          uint32_t r[2][32];
+          tmem_ld32(lane_base + L::DQ_COL, r[0]);
+          tmem_ld32(lane_base + L::DQ_COL + 32, r[1]);
+          tmem_wait_ld();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(dq_free);  // dQ is in registers
+          add_rows(&tm_dq, r[0], 0, q0 + wq * 32);
+          add_rows(&tm_dq, r[1], 32, q0 + wq * 32);
+        }
+      }
+      // the sweep's dK and dV (lanes = key rows)
+      if (!ok || !(ok = warp_wait(dkv_full, sw & 1, ctl))) break;
+      tc_fence_after();
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+#pragma unroll
+        for (int c = 0; c < (DM + 31) / 32; ++c) {
+          uint32_t r[32];
+          tmem_ld32(lane_base + (m == 0 ? L::DV_COL : L::DK_COL) + 32 * c, r);
+          tmem_wait_ld();
+          if (m == 1 && c == (DM + 31) / 32 - 1) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(dkv_free);
+          }
+          if (32 * c < p.d) add_rows(m == 0 ? &tm_dv : &tm_dk, r, 32 * c, w.kt * kTileRows + wq * 32);
+        }
+      }
+      ++sw;
+    }
+    // every reduce-add has completed before the CTA's shared memory goes away
+    if (lane == 0) bulk_wait_all();
+    __syncwarp();
+  }
+
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 13) {
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+template <int D, int DM>
+cudaError_t launch(const XattnBwdMaps& m, const XattnBwdParams& p, int dev, int sms, cudaStream_t s) {
+  using L = Layout<D, DM>;
+  static OncePerDevice prepared;
+  const cudaError_t e = prepared(dev, [] {
+    // the in-kernel register re-split assumes the launch register count; with any
+    // other its setmaxnreg.inc could never be satisfied, so refuse
+    cudaFuncAttributes fa;
+    const cudaError_t e0 = cudaFuncGetAttributes(&fa, xattn_bwd_kernel<D, DM>);
+    if (e0 != cudaSuccess) return e0;
+    if (fa.numRegs != L::REGS_LAUNCH) return cudaErrorInvalidKernelImage;
+    return cudaFuncSetAttribute(xattn_bwd_kernel<D, DM>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::BYTES);
+  });
+  if (e != cudaSuccess) return e;
+  const unsigned grid = static_cast<unsigned>(p.pieces < sms ? p.pieces : sms);
+  xattn_bwd_kernel<D, DM><<<grid, L::THREADS, L::BYTES, s>>>(m.q, m.k, m.v, m.dout, m.dq, m.dk, m.dv, m.bias, p);
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_xattn_bwd_main(int d, int dm, const XattnBwdMaps& m, const XattnBwdParams& p, int dev, int sms,
+                                  cudaStream_t s) {
+  if (d == 64) return launch<64, 64>(m, p, dev, sms, s);
+  if (dm == 80) return launch<128, 80>(m, p, dev, sms, s);
+  return launch<128, 128>(m, p, dev, sms, s);
+}
+
+}  // namespace mw
