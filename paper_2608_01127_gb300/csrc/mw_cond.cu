@@ -63,27 +63,44 @@ size_t xattn_ws(const XattnSizes& z, int S, int d) {
   return align256(rows * kernel_d(d) * sizeof(float)) + align256(rows * sizeof(float));
 }
 
-// Ranges of a head's query tiles in the backward: pieces of work that fill the
-// SMs, against what a sweep costs besides its steps (about two).
-int xattn_bwd_ranges(int BH, int q_tiles, int k_tiles) {
-  int best = 1;
-  long long best_cost = LLONG_MAX;
-  for (int r = 1; r <= q_tiles; ++r) {
-    const long long waves = ceil_div(static_cast<long long>(BH) * r, kNormSms);
-    const long long cost = waves * k_tiles * (ceil_div(q_tiles, r) + 2);
+// The order of the backward's work and the ranges of a head's query tiles, from a
+// model of the time (us): steps of t, a sweep's start and end, waves of pieces over
+// the SMs, and the accumulators' way through HBM.
+struct XattnBwdPlan {
+  bool key_major = false;
+  int ranges = 1;
+};
+
+XattnBwdPlan xattn_bwd_plan(int BH, int q_tiles, int k_tiles, int D) {
+  const double t = D == 64 ? 1.25 : 2.2, sweep = 2.0;
+  const double acc = 4e-6 * BH * static_cast<double>(q_tiles) * kTileRows * D / 6.5;  // us a pass
+  XattnBwdPlan best;
+  double best_cost = 1e30;
+  auto consider = [&](bool key_major, int r, double extra) {
+    const long long pieces = static_cast<long long>(BH) * r * (key_major ? k_tiles : 1);
+    const double sweeps = key_major ? 1 : k_tiles;
+    const double cost = ceil_div(pieces, kNormSms) * sweeps * (ceil_div(q_tiles, r) * t + sweep) + extra;
     if (cost < best_cost) {
       best_cost = cost;
-      best = r;
+      best.key_major = key_major;
+      best.ranges = r;
     }
-    if (waves > 64) break;
+  };
+  // query-major: the dQ of the ranges in work has to stay in L2 (about 40 MB)
+  const int most = k_tiles == 1 ? q_tiles : D == 64 ? 8 : 4;
+  for (int r = ceil_div(q_tiles, most); r <= q_tiles; ++r) {
+    consider(false, r, k_tiles == 1 ? 0 : 2.5 * acc);
+    if (static_cast<long long>(BH) * r > 64ll * kNormSms) break;
   }
+  for (int r = 1; k_tiles > 1 && r <= q_tiles && r <= 64; ++r) consider(true, r, 3.5 * acc);
   return best;
 }
 
 // The backward's workspace: byte offsets of its fp32 arrays.
 struct XattnBwdWs {
   int M_pad = 0, S_pad = 0;
-  size_t dq = 0, dk = 0, dv = 0, lse2 = 0, delta = 0, bias = 0, total = 0;
+  XattnBwdPlan plan;
+  size_t dq = 0, dkv = 0, dkv_bytes = 0, lse2 = 0, delta = 0, bias = 0, total = 0;
 };
 
 XattnBwdWs xattn_bwd_ws(const XattnSizes& z, int S, int d) {
@@ -91,12 +108,13 @@ XattnBwdWs xattn_bwd_ws(const XattnSizes& z, int S, int d) {
   const int D = kernel_d(d);
   w.M_pad = ceil_div(z.rows, kTileRows) * kTileRows;
   w.S_pad = ceil_div(S, kTileRows) * kTileRows;
+  w.plan = xattn_bwd_plan(z.BH, w.M_pad / kTileRows, w.S_pad / kTileRows, D);
   const size_t rows = static_cast<size_t>(z.BH) * w.M_pad, keys = static_cast<size_t>(z.BH) * w.S_pad;
-  w.dk = align256(rows * D * 4);
-  w.dv = w.dk + align256(keys * D * 4);
-  w.lse2 = w.dv + align256(keys * D * 4);
-  w.delta = w.lse2 + align256(rows * 4);
-  w.bias = w.delta + align256(rows * 4);
+  w.dkv = w.S_pad > kTileRows ? align256(rows * D * 4) : 0;
+  w.dkv_bytes = w.plan.ranges > 1 ? 2 * keys * D * 4 : 0;
+  w.lse2 = w.dkv + align256(w.dkv_bytes);
+  w.delta = w.lse2 + (D == 64 ? 0 : align256(rows * 4));
+  w.bias = w.delta + (D == 64 ? 0 : align256(rows * 4));
   w.total = w.bias + (D == 64 ? align256(rows * 32) : 0);
   return w;
 }
@@ -282,47 +300,55 @@ mw_status mw_xattn_bwd(const void* q, const void* k, const void* v, const int* k
   XattnBwdParams p{};
   MW_TRY(status_ptr(scope.device(), &p.status));
   p.kv_len = kv_len;
+  p.o = static_cast<const __nv_bfloat16*>(o);
+  p.dout = static_cast<const __nv_bfloat16*>(dout);
+  p.lse = lse;
+  p.dq = static_cast<__nv_bfloat16*>(dq);
+  p.dk = static_cast<__nv_bfloat16*>(dk);
+  p.dv = static_cast<__nv_bfloat16*>(dv);
   p.BH = z.BH;
   p.heads = Hkv;
   p.M = z.rows;
   p.M_pad = ws.M_pad;
   p.S = S;
+  p.S_pad = ws.S_pad;
   p.d = d;
-  p.ranges = xattn_bwd_ranges(z.BH, ws.M_pad / kTileRows, ws.S_pad / kTileRows);
-  p.pieces = z.BH * p.ranges;
+  p.key_major = ws.plan.key_major;
+  p.ranges = ws.plan.ranges;
+  p.k_tiles = ws.S_pad / kTileRows;
+  p.pieces = z.BH * p.ranges * (p.key_major ? p.k_tiles : 1);
+  p.zero_dq = p.key_major;
+  p.wide_dq = wide_rows(dq, d);
+  p.wide_dkv = wide_rows(dk, d) && wide_rows(dv, d);
+  p.scale = scale;
   p.scale_log2 = scale * 1.4426950408889634f;
   p.lse2 = at(ws.lse2);
   p.delta = at(ws.delta);
+  p.bias = at(ws.bias);
+  p.dq_acc = at(ws.dq);
+  p.dkv_acc = at(ws.dkv);
+  p.dkv_float4s = static_cast<long long>(ws.dkv_bytes / 16);
   p.budget_ns = budget_ns();
   p.debug_skip_q = debug_skip_q();
-  float* bias = D == 64 ? at(ws.bias) : nullptr;
   XattnBwdMaps m;
   MW_TRY(make_map(&m.q, q, z.rows, z.BH, d, "q"));
   MW_TRY(make_map(&m.k, k, S, z.BH, d, "k"));
   MW_TRY(make_map(&m.v, v, S, z.BH, d, "v"));
   MW_TRY(make_map(&m.dout, dout, z.rows, z.BH, d, "dout"));
-  MW_TRY(make_map(&m.dq, at(ws.dq), ws.M_pad, z.BH, D, "dq_acc", 32, true, d));
-  MW_TRY(make_map(&m.dk, at(ws.dk), ws.S_pad, z.BH, D, "dk_acc", 32, true, d));
-  MW_TRY(make_map(&m.dv, at(ws.dv), ws.S_pad, z.BH, D, "dv_acc", 32, true, d));
-  m.bias = m.dq;  // d = 128: unused
-  if (bias) MW_TRY(encode_bias_map(&m.bias, bias, ws.M_pad, z.BH, kTileRows));
-  MW_TRY(launch_status(launch_bwd_pre(D, d, static_cast<const __nv_bfloat16*>(o),
-                                      static_cast<const __nv_bfloat16*>(dout), lse, at(ws.lse2),
-                                      at(ws.delta), at(ws.dq), bias, 1.f / scale, z.BH, z.rows,
-                                      ws.M_pad, s),
-                       "cross attention backward pre kernel launch"));
-  MW_TRY(launch_status(cudaMemsetAsync(at(ws.dk), 0, ws.lse2 - ws.dk, s), "clearing dK and dV"));
-  MW_TRY(launch_status(launch_xattn_bwd_main(D, mma_d(d), m, p, scope.device(), sm_count(), s),
-                       "cross attention backward launch"));
-  MW_TRY(launch_status(launch_bwd_post(D, d, at(ws.dq), static_cast<__nv_bfloat16*>(dq), scale, z.BH,
-                                       z.rows, ws.M_pad, s),
-                       "dQ post kernel launch"));
-  MW_TRY(launch_status(launch_bwd_post(D, d, at(ws.dk), static_cast<__nv_bfloat16*>(dk), scale, z.BH, S,
-                                       ws.S_pad, s),
-                       "dK post kernel launch"));
-  return launch_status(launch_bwd_post(D, d, at(ws.dv), static_cast<__nv_bfloat16*>(dv), 1.f, z.BH, S,
-                                       ws.S_pad, s),
-                       "dV post kernel launch");
+  // (maps that no launch of these sizes uses stand in for one another)
+  m.dq = m.dk = m.dv = m.bias = m.dq_out = m.q;
+  if (ws.dkv > 0) MW_TRY(make_map(&m.dq, p.dq_acc, ws.M_pad, z.BH, D, "dq_acc", 32, true, d));
+  if (ws.dkv_bytes > 0) {
+    MW_TRY(make_map(&m.dk, p.dkv_acc, ws.S_pad, z.BH, D, "dk_acc", 32, true, d));
+    MW_TRY(make_map(&m.dv, p.dkv_acc + static_cast<size_t>(z.BH) * ws.S_pad * D, ws.S_pad, z.BH, D, "dv_acc", 32,
+                    true, d));
+  }
+  if (D == 64)
+    MW_TRY(encode_bias_map(&m.bias, p.bias, ws.M_pad, z.BH, kTileRows));
+  else
+    MW_TRY(encode_rows_map(&m.dq_out, dq, z.rows, z.BH, d));
+  return launch_status(launch_xattn_bwd(D, mma_d(d), m, p, scope.device(), sm_count(), s),
+                       "cross attention backward launch");
 }
 
 mw_status mw_layernorm_fwd(const void* x, const void* weight, const void* bias, void* y, float* mean,

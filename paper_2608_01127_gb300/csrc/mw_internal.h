@@ -257,25 +257,38 @@ cudaError_t launch_xattn_tc(int d, int dm, const CUtensorMap& tq, const CUtensor
 // Forward of few rows a head on CUDA cores (mw_xattn.cu).
 cudaError_t launch_xattn_fwd(const XattnParams& p, cudaStream_t s);
 
-// Backward on tensor cores (mw_xattn_bwd.cu); its D, LSE and bias rows come from
-// launch_bwd_pre, its accumulators become bf16 with launch_bwd_post.
+// Backward on tensor cores (mw_xattn_bwd.cu).
 struct XattnBwdParams {
   const int* kv_len;
-  int BH, heads, M, M_pad, S, d;  // M_pad: M rounded up to kTileRows
-  int ranges, pieces;  // ranges of a head's query tiles; BH * ranges
-  float scale_log2;
-  const float* lse2;   // [BH, M_pad]
-  const float* delta;  // [BH, M_pad]
+  const __nv_bfloat16* o;
+  const __nv_bfloat16* dout;
+  const float* lse;
+  __nv_bfloat16* dq;
+  __nv_bfloat16* dk;
+  __nv_bfloat16* dv;
+  int BH, heads, M, M_pad, S, S_pad, d;  // _pad: rounded up to kTileRows
+  bool key_major;      // a piece of work is one key tile, else a range of query tiles
+  int ranges, k_tiles; // ranges of a head's query tiles; key tiles of S states
+  int pieces;          // BH * ranges, key-major times k_tiles
+  bool zero_dq;        // dq_acc is only added to
+  bool wide_dq, wide_dkv;  // every row of the outputs starts at a multiple of 32 bytes
+  float scale, scale_log2;
+  float* lse2;         // [BH, M_pad] (d = 64: unused, as delta)
+  float* delta;        // [BH, M_pad]
+  float* bias;         // [BH, M_pad, 8] (d = 64)
+  float* dq_acc;       // [BH, M_pad, D]
+  float* dkv_acc;      // [2, BH, S_pad, D] where ranges > 1: dK, then dV
+  long long dkv_float4s;  // its size
   unsigned* status;
   unsigned long long budget_ns;
   int debug_skip_q;
 };
 // dq [BH, M_pad, D], dk, dv [BH, S_pad, D]: f32 accumulators, 32 x 32 boxes; bias as
-// for launch_bwd_main
+// for launch_bwd_main; dq_out: the caller's dQ, 32 x 32 boxes without swizzle
 struct XattnBwdMaps {
-  CUtensorMap q, k, v, dout, dq, dk, dv, bias;
+  CUtensorMap q, k, v, dout, dq, dk, dv, bias, dq_out;
 };
-cudaError_t launch_xattn_bwd_main(int d, int dm, const XattnBwdMaps& m, const XattnBwdParams& p, int dev, int sms,
-                                  cudaStream_t s);
+cudaError_t launch_xattn_bwd(int d, int dm, const XattnBwdMaps& m, const XattnBwdParams& p, int dev, int sms,
+                             cudaStream_t s);
 
 }  // namespace mw

@@ -1,14 +1,18 @@
 // Cross attention backward on sm_103a: the gradients of queries against an
 // encoder's states.
 //
-// The block-causal backward gives every key tile a CTA that visits all query
-// rows that see it.  An encoder's states are often only a few key tiles, too few
-// CTAs, so here a piece of work is a range of query tiles of one head, and a CTA
-// (persistent, one an SM) takes its pieces through all key tiles of the head:
-// one sweep over the range a key tile, in which dK and dV of the tile stay in
-// tensor memory.  At the end of a sweep they are added to fp32 accumulators, as dQ is
-// after every step.  Per step (128 keys x 128 queries), as in the block-causal
-// backward, whose arrangement of tensor memory and roles this kernel shares:
+// A sweep takes one key tile through a range of query tiles, with dK and dV of the
+// tile in tensor memory; dQ of every step goes out.  Two orders:
+//   query-major  a piece of work is a range of query tiles, taken through all key tiles
+//                of its head: few states, whose key tiles alone would not fill the
+//                SMs.  The first key tile's dQ is stored, the others' added while the
+//                range is still in L2 (and with one key tile dQ is written as it is);
+//                dK and dV are added to accumulators at the end of a sweep.
+//   key-major    a piece is one key tile, taken through all query tiles (or a few
+//                ranges of them): many states.  The key tiles of a head run side by side,
+//                so that dQ is added up in L2; dK and dV are written as they are.
+// Per step (128 keys x 128 queries), as in the block-causal backward, whose arrangement
+// of tensor memory and roles this kernel shares:
 //   S^T = K Q^T, dP^T = V dO^T              (tcgen05 -> TMEM)
 //   P^T = exp2(scale log2e S^T - LSE2), dS^T = P^T (dP^T - D)   (registers)
 //   dV += P^T dO, dK += dS^T Q, dQ = dS K   (tcgen05)
@@ -58,7 +62,7 @@ struct Layout {
   static constexpr int OFF_DELTA = OFF_LSE + QSTAGES * VEC_BYTES;
   static constexpr int OFF_ONES = OFF_DELTA + 2 * VEC_BYTES;
   static constexpr int OFF_BAR = OFF_ONES + ONES_BYTES;
-  static constexpr int NBAR = 3 + 2 * (QSTAGES + DOSTAGES) + 9 + 2 * DS_BUFS;
+  static constexpr int NBAR = 6 + 2 * (QSTAGES + DOSTAGES) + 9 + 2 * DS_BUFS;
   static constexpr int OFF_MISC = OFF_BAR + NBAR * 8;
   static constexpr int BYTES = OFF_MISC + 16;
   // d = 128 has no room for S^T, dP^T, P^T and dQ^T in columns of their own: P^T
@@ -82,38 +86,58 @@ struct Layout {
   static_assert(BYTES <= 232448, "shared memory");
 };
 
-// The sweeps of a CTA in turn: its pieces' key tiles.  Every role walks through
-// the same ones.
+// The sweeps of a CTA in turn: a key tile against a range of query tiles each.
+// Every role walks through the same ones.  A piece of work is, query-major, a range
+// of query tiles with all key tiles of its head; key-major, one key tile.
 struct Walk {
   const XattnBwdParams& p;
   int next;         // index of the next piece
   int bh, q0, n_q;  // head, first query tile and query tiles of the piece
   int len, sample;  // valid states of the head's sample
-  int kt, n_kt;     // key tile, key tiles
+  int kt, k_end;    // key tile; where the piece's end
+  int n_kt;         // key tiles of the sample
   __device__ explicit Walk(const XattnBwdParams& p_)
-      : p(p_), next(blockIdx.x), len(p_.S), sample(-1), kt(0), n_kt(0) {}
-  __device__ __forceinline__ bool step() {
-    if (++kt < n_kt) return true;
-    while (next < p.pieces) {
-      const int x = next;
-      next += gridDim.x;
-      bh = x / p.ranges;
-      const int r = x - bh * p.ranges;
-      if (p.kv_len) {
-        const int s = bh / p.heads;
-        if (s != sample) {
-          sample = s;
-          len = min(max(p.kv_len[s], 0), p.S);
-        }
-      }
-      const int tiles = p.M_pad / 128;
-      q0 = static_cast<int>(static_cast<long long>(r) * tiles / p.ranges);
-      n_q = static_cast<int>(static_cast<long long>(r + 1) * tiles / p.ranges) - q0;
-      n_kt = (len + kTileRows - 1) / kTileRows;
-      kt = 0;
-      if (n_kt > 0) return true;
+      : p(p_), next(blockIdx.x), len(p_.S), sample(-1), kt(0), k_end(0) {}
+  // the next piece, with keys or not
+  __device__ __forceinline__ bool piece() {
+    if (next >= p.pieces) return false;
+    int x = next;
+    next += gridDim.x;
+    kt = 0;
+    if (p.key_major) {
+      kt = x % p.k_tiles;
+      x /= p.k_tiles;
     }
+    bh = x / p.ranges;
+    const int r = x - bh * p.ranges;
+    if (p.kv_len) {
+      const int s = bh / p.heads;
+      if (s != sample) {
+        sample = s;
+        len = min(max(p.kv_len[s], 0), p.S);
+      }
+    }
+    const int tiles = p.M_pad / kTileRows;
+    q0 = static_cast<int>(static_cast<long long>(r) * tiles / p.ranges);
+    n_q = static_cast<int>(static_cast<long long>(r + 1) * tiles / p.ranges) - q0;
+    n_kt = (len + kTileRows - 1) / kTileRows;
+    k_end = p.key_major ? min(kt + 1, n_kt) : n_kt;
+    return true;
+  }
+  __device__ __forceinline__ bool step() {
+    if (++kt < k_end) return true;
+    while (piece())
+      if (kt < k_end) return true;
     return false;
+  }
+  // first row of the sweep's j-th query tile: key-major, each key tile starts at its
+  // own offset, so that those of one head side by side reduce into different dQ
+  // tiles instead of contending for the same L2 lines
+  __device__ __forceinline__ int query_row(int j) const {
+    const int rot = p.key_major ? kt % n_q : 0;
+    int t = j + rot;
+    if (t >= n_q) t -= n_q;
+    return (q0 + t) * kTileRows;
   }
   // the key tile has rows that count as nothing but may hold anything
   __device__ __forceinline__ bool ragged() const { return (kt + 1) * kTileRows > len && len < p.S; }
@@ -125,6 +149,7 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
                      const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_do,
                      const __grid_constant__ CUtensorMap tm_dq, const __grid_constant__ CUtensorMap tm_dk,
                      const __grid_constant__ CUtensorMap tm_dv, const __grid_constant__ CUtensorMap tm_bias,
+                     const __grid_constant__ CUtensorMap tm_dqo,
                      const __grid_constant__ XattnBwdParams p) {
   using L = Layout<D, DM>;
   constexpr int NQ = L::QSTAGES;
@@ -139,10 +164,13 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
     if (threadIdx.x == 0) atomicOr(p.status, kDevMisaligned);
     return;  // uniform across the CTA, before any barrier or TMEM use
   }
-  uint64_t* kv_full = reinterpret_cast<uint64_t*>(smem + L::OFF_BAR);
-  uint64_t* kv_raw = kv_full + 1;   // K and V that warp 15 makes ready, then kv_full
-  uint64_t* kv_empty = kv_raw + 1;
-  uint64_t* q_full = kv_empty + 1;
+  uint64_t* k_full = reinterpret_cast<uint64_t*>(smem + L::OFF_BAR);
+  uint64_t* k_raw = k_full + 1;   // a K tile that warp 15 makes ready, then k_full
+  uint64_t* k_empty = k_raw + 1;
+  uint64_t* v_full = k_empty + 1;
+  uint64_t* v_raw = v_full + 1;
+  uint64_t* v_empty = v_raw + 1;
+  uint64_t* q_full = v_empty + 1;
   uint64_t* q_empty = q_full + NQ;
   uint64_t* do_full = q_empty + NQ;
   uint64_t* do_empty = do_full + ND;
@@ -173,9 +201,12 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
     }
   }
   if (threadIdx.x == 0) {
-    mbar_init(kv_full, 1);
-    mbar_init(kv_raw, 1);
-    mbar_init(kv_empty, 2);
+    mbar_init(k_full, 1);
+    mbar_init(k_raw, 1);
+    mbar_init(k_empty, 2);
+    mbar_init(v_full, 1);
+    mbar_init(v_raw, 1);
+    mbar_init(v_empty, 1);
     for (int s = 0; s < NQ; ++s) {
       mbar_init(&q_full[s], 1);
       mbar_init(&q_empty[s], 1);
@@ -227,6 +258,7 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
       prefetch_tmap(&tm_q);
       prefetch_tmap(&tm_do);
       int sw = 0, raws = 0, n_q = 0, n_do = 0;  // sweeps, those through warp 15, Q and dO tiles so far
+      int n_v = 0;                              // V tiles (one a sweep, loaded ahead of K)
       bool ok = true, raw = false;
       auto load_q = [&](int q) {
         const int st = n_q % NQ;
@@ -255,24 +287,29 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
         return true;
       };
       while (ok && w.step()) {
-        // the first query tile ahead of K and V, which wait for the last sweep's end
-        if (!(ok = load_q(w.q0 * QN))) break;
-        if (!(ok = mbar_wait(kv_empty, (sw & 1) ^ 1, ctl))) break;
         raw = w.ragged();
-        uint64_t* bar = raw ? kv_raw : kv_full;
-        mbar_arrive_expect_tx(bar, 2 * L::KTILE);
-        for (int r = 0; r < L::REG; ++r) {
-          tma_load_3d(sK + r * L::KREGION, &tm_k, bar, 64 * r, w.kt * kTileRows, w.bh);
-          tma_load_3d(sV + r * L::KREGION, &tm_v, bar, 64 * r, w.kt * kTileRows, w.bh);
-        }
-        ++sw;
+        // Q, dO and V of the sweep's first step ahead of K, which waits for the last dQ
+        // of the sweep before
+        if (!(ok = load_q(w.query_row(0)))) break;
+        if (!(ok = mbar_wait(v_empty, (sw & 1) ^ 1, ctl))) break;
+        auto load_tile = [&](uint8_t* dst, const CUtensorMap* map, uint64_t* bar) {
+          mbar_arrive_expect_tx(bar, L::KTILE);
+          for (int r = 0; r < L::REG; ++r)
+            tma_load_3d(dst + r * L::KREGION, map, bar, 64 * r, w.kt * kTileRows, w.bh);
+        };
+        load_tile(sV, &tm_v, raw ? v_raw : v_full);
+        ++n_v;
         raws += raw;
-        if (!(ok = load_do(w.q0 * QN))) break;
-        for (int j = 1; ok && j < w.n_q; ++j) ok = load_q((w.q0 + j) * QN) && load_do((w.q0 + j) * QN);
+        if (!(ok = load_do(w.query_row(0)))) break;
+        if (!(ok = mbar_wait(k_empty, (sw & 1) ^ 1, ctl))) break;
+        load_tile(sK, &tm_k, raw ? k_raw : k_full);
+        ++sw;
+        for (int j = 1; ok && j < w.n_q; ++j) ok = load_q(w.query_row(j)) && load_do(w.query_row(j));
       }
       if (*abort_flag || !ok) {
         // let every copy this CTA started land before shared memory goes away
-        if (sw > 0) drain_wait(raw ? kv_raw : kv_full, ((raw ? raws : sw) - 1) & 1, p.budget_ns);
+        if (n_v > 0) drain_wait(raw ? v_raw : v_full, ((raw ? raws : n_v) - 1) & 1, p.budget_ns);
+        if (sw > 0 && sw == n_v) drain_wait(raw ? k_raw : k_full, ((raw ? raws : sw) - 1) & 1, p.budget_ns);
         for (int j = max(0, n_q - NQ); j < n_q; ++j) drain_wait(&q_full[j % NQ], (j / NQ) & 1, p.budget_ns);
         for (int j = max(0, n_do - ND); j < n_do; ++j) drain_wait(&do_full[j % ND], (j / ND) & 1, p.budget_ns);
       }
@@ -355,7 +392,7 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
     bool ok = true;
     int g = 0, sw = 0;  // steps and sweeps so far
     while (ok && w.step()) {
-      if (!(ok = warp_wait(kv_full, sw & 1, ctl))) break;
+      if (!(ok = warp_wait(k_full, sw & 1, ctl))) break;
       // the last sweep's dK and dV are out of tensor memory
       auto wait_dkv = [&]() { return sw == 0 || warp_wait(dkv_free, (sw - 1) & 1, ctl); };
       if (role_a) {
@@ -364,11 +401,13 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
           if (g > 0 && !(ok = warp_wait(s_free, (g - 1) & 1, ctl))) break;
         tc_fence_after();
         issue_s(g);
+        if (!(ok = warp_wait(v_full, sw & 1, ctl))) break;
         if constexpr (!L::PAIRED) {
           if (!(ok = warp_wait(&do_full[g % ND], (g / ND) & 1, ctl))) break;
           if (g > 0 && !(ok = warp_wait(dp_free, (g - 1) & 1, ctl))) break;
           tc_fence_after();
           issue_dp(g);
+          if (w.n_q == 1) umma_commit(v_empty);
         }
         for (int j = 0; j < w.n_q; ++j, ++g) {
           const bool more = j + 1 < w.n_q;
@@ -380,6 +419,7 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
             if (g > 0 && !(ok = warp_wait(dq_free, (g - 1) & 1, ctl))) break;
             tc_fence_after();
             issue_dp(g);
+            if (!more) umma_commit(v_empty);
           } else if (more) {
             // S^T of the next step as soon as the P/dS warps hold this one's
             if (!(ok = warp_wait(s_free, g & 1, ctl))) break;
@@ -403,6 +443,7 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
             if (!(ok = warp_wait(&do_full[(g + 1) % ND], ((g + 1) / ND) & 1, ctl))) break;
             tc_fence_after();
             issue_dp(g + 1);
+            if (j + 2 == w.n_q) umma_commit(v_empty);
           }
         }
       } else {
@@ -426,26 +467,45 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
       }
       if (!ok) break;
       umma_commit(dkv_full);  // one arrival per issuing warp
-      umma_commit(kv_empty);
+      umma_commit(k_empty);
       ++sw;
     }
   } else {
+    // ------------------------------------------------------------ what has no key to it
+    // Gradients that no sweep writes: dQ of samples without states, and dK and dV of
+    // tiles past them where each tile's one sweep writes them whole.
+    Walk z(p);
+    auto zero_rows = [&](__nv_bfloat16* out, int rows, int row0, int count) {
+      const int n = min(count, rows - row0) * (p.d / 8);
+      uint4* dst = reinterpret_cast<uint4*>(out + (static_cast<size_t>(z.bh) * rows + row0) * p.d);
+      for (int i = lane; i < n; i += 32) dst[i] = make_uint4(0u, 0u, 0u, 0u);
+    };
+    while (z.piece()) {
+      if (z.n_kt == 0 && z.kt == 0) zero_rows(p.dq, p.M, z.q0 * kTileRows, z.n_q * kTileRows);
+      if (p.ranges == 1)
+        for (int t = p.key_major ? z.kt : 0; t < (p.key_major ? z.kt + 1 : p.k_tiles); ++t)
+          if (t >= z.n_kt) {
+            zero_rows(p.dk, p.S, t * kTileRows, kTileRows);
+            zero_rows(p.dv, p.S, t * kTileRows, kTileRows);
+          }
+    }
     // ------------------------------------------------------------ ragged K and V tiles
     int raws = 0;
-    while (w.step()) {
+    bool ok = true;
+    while (ok && w.step()) {
       if (!w.ragged()) continue;
-      if (!warp_wait(kv_raw, raws & 1, ctl)) break;
-      ++raws;
       const int limit = w.len - w.kt * kTileRows;
-      const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-      for (int i = limit * 8 + lane; i < kTileRows * 8; i += 32)
-        for (int r = 0; r < L::REG; ++r) {
-          *reinterpret_cast<uint4*>(sK + r * L::KREGION + i * 16) = zero;
-          *reinterpret_cast<uint4*>(sV + r * L::KREGION + i * 16) = zero;
-        }
-      fence_proxy_async_smem();  // the tensor core reads the tiles next
-      __syncwarp();
-      if (lane == 0) mbar_arrive(kv_full);
+      for (int m = 0; ok && m < 2; ++m) {  // V is loaded first
+        if (!(ok = warp_wait(m == 0 ? v_raw : k_raw, raws & 1, ctl))) break;
+        uint8_t* tile = m == 0 ? sV : sK;
+        for (int i = limit * 8 + lane; i < kTileRows * 8; i += 32)
+          for (int r = 0; r < L::REG; ++r)
+            *reinterpret_cast<uint4*>(tile + r * L::KREGION + i * 16) = make_uint4(0u, 0u, 0u, 0u);
+        fence_proxy_async_smem();  // the tensor core reads the tile next
+        __syncwarp();
+        if (lane == 0) mbar_arrive(m == 0 ? v_full : k_full);
+      }
+      ++raws;
     }
   }
   } else if (warp < 8) {
@@ -589,8 +649,9 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
     const uint32_t lane_base = tmem + (static_cast<uint32_t>(wq * 32) << 16);
     int box = 0;  // the staging box whose turn it is
     // 32 lanes x 32 columns as a box of 32 rows (128 bytes, 16-byte chunk c of row r
-    // at c ^ (r mod 8)) that the TMA unit adds to `map` at column c0, row `row`
-    auto add_rows = [&](const CUtensorMap* map, const uint32_t (&r)[32], int c0, int row) {
+    // at c ^ (r mod 8)) that the TMA unit adds to `map` at column c0, row `row`, or
+    // stores there
+    auto put_rows = [&](const CUtensorMap* map, const uint32_t (&r)[32], int c0, int row, bool add) {
       uint8_t* stg = smem + L::OFF_STG + (L::BOXES * wq + box) * L::BOX_BYTES;
       if (lane == 0) bulk_wait_read<L::BOXES - 1>();  // the TMA unit has read this box
       __syncwarp();
@@ -601,7 +662,10 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) {
-        tma_reduce_add_3d(map, stg, c0, row, w.bh);
+        if (add)
+          tma_reduce_add_3d(map, stg, c0, row, w.bh);
+        else
+          tma_store_3d(map, stg, c0, row, w.bh);
         bulk_commit_group();
       }
       box ^= L::BOXES - 1;
@@ -609,14 +673,22 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
     bool ok = true;
     int g = 0, sw = 0;
     while (ok && w.step()) {
+      // dQ of a step: whole, where the sample has one key tile; else, query-major, the
+      // first key tile's is stored and the others' added (the stores are complete by
+      // then); key-major all are added to zeros
+      const bool whole = w.n_kt == 1;
+      const bool add = p.key_major || w.kt > 0;
+      if (!p.key_major && w.kt == 1) {
+        if (lane == 0) bulk_wait_all();
+        __syncwarp();
+      }
       for (int j = 0; j < w.n_q; ++j, ++g) {
-        const int q0 = (w.q0 + j) * QN;
+        const int q0 = w.query_row(j);
         if (!(ok = warp_wait(dq_full, g & 1, ctl))) break;
         tc_fence_after();
         if constexpr (L::DQT) {
           // lanes = head-dim columns, TMEM columns = the QN query rows: boxes of 32
-          // queries, each store instruction one of its rows.  The map clips columns
-          // past the caller's; warps with none skip.
+          // queries.  The maps clip columns past the caller's; warps with none skip.
           uint32_t r[QN / 32][32];
 #pragma unroll
           for (int c = 0; c < QN / 32; ++c) tmem_ld32(lane_base + L::DQ_COL + 32 * c, r[c]);
@@ -630,14 +702,31 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
               uint8_t* stg = smem + L::OFF_STG + (2 * wq + box) * L::BOX_BYTES;
               if (lane == 0) bulk_wait_read<1>();
               __syncwarp();
+              if (whole) {
+                // bf16 rows of 64 bytes: of two queries, even lanes take the first and
+                // odd ones the second, a pair of columns each
 #pragma unroll
-              for (int k = 0; k < 32; ++k)
-                *reinterpret_cast<uint32_t*>(stg + k * 128 + (((lane >> 2) ^ (k & 7)) << 4) + (lane & 3) * 4) =
-                    r[c][k];
+                for (int k = 0; k < 32; k += 2) {
+                  const float a = __uint_as_float(r[c][k]) * p.scale, b = __uint_as_float(r[c][k + 1]) * p.scale;
+                  const float other = __shfl_xor_sync(0xffffffffu, lane & 1 ? a : b, 1);
+                  const uint32_t pair = lane & 1 ? pack_bf16x2(other, b) : pack_bf16x2(a, other);
+                  *reinterpret_cast<uint32_t*>(stg + (k + (lane & 1)) * 64 + (lane >> 1) * 4) = pair;
+                }
+              } else {
+#pragma unroll
+                for (int k = 0; k < 32; ++k)  // each instruction one row, 16-byte chunks swizzled
+                  *reinterpret_cast<uint32_t*>(stg + k * 128 + (((lane >> 2) ^ (k & 7)) << 4) + (lane & 3) * 4) =
+                      r[c][k];
+              }
               fence_proxy_async_smem();
               __syncwarp();
               if (lane == 0) {
-                tma_reduce_add_3d(&tm_dq, stg, 32 * wq, q0 + 32 * c, w.bh);
+                if (whole)
+                  tma_store_3d(&tm_dqo, stg, 32 * wq, q0 + 32 * c, w.bh);
+                else if (add)
+                  tma_reduce_add_3d(&tm_dq, stg, 32 * wq, q0 + 32 * c, w.bh);
+                else
+                  tma_store_3d(&tm_dq, stg, 32 * wq, q0 + 32 * c, w.bh);
                 bulk_commit_group();
               }
               box ^= 1;
@@ -653,13 +742,25 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
           tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(dq_free);  // dQ is in registers
-          add_rows(&tm_dq, r[0], 0, q0 + wq * 32);
-          add_rows(&tm_dq, r[1], 32, q0 + wq * 32);
+          const int row = q0 + wq * 32;
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            if (!whole) {
+              put_rows(&tm_dq, r[c], 32 * c, row, add);
+            } else if (row + lane < p.M) {
+              float v[32];
+#pragma unroll
+              for (int k = 0; k < 32; ++k) v[k] = __uint_as_float(r[c][k]) * p.scale;
+              store_row32(p.dq + (static_cast<size_t>(w.bh) * p.M + row + lane) * D + 32 * c, v, 4, p.wide_dq);
+            }
+          }
+          __syncwarp();
         }
       }
       // the sweep's dK and dV (lanes = key rows)
       if (!ok || !(ok = warp_wait(dkv_full, sw & 1, ctl))) break;
       tc_fence_after();
+      const int row = w.kt * kTileRows + wq * 32;
 #pragma unroll
       for (int m = 0; m < 2; ++m) {
 #pragma unroll
@@ -672,7 +773,18 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
             __syncwarp();
             if (lane == 0) mbar_arrive(dkv_free);
           }
-          if (32 * c < p.d) add_rows(m == 0 ? &tm_dv : &tm_dk, r, 32 * c, w.kt * kTileRows + wq * 32);
+          if (32 * c < p.d) {
+            if (p.ranges > 1) {
+              put_rows(m == 0 ? &tm_dv : &tm_dk, r, 32 * c, row, true);
+            } else if (row + lane < p.S) {
+              float v[32];
+#pragma unroll
+              for (int k = 0; k < 32; ++k) v[k] = __uint_as_float(r[k]) * (m == 0 ? 1.f : p.scale);
+              store_row32((m == 0 ? p.dv : p.dk) + (static_cast<size_t>(w.bh) * p.S + row + lane) * p.d + 32 * c, v,
+                          min(4, (p.d - 32 * c) / 8), p.wide_dkv);
+            }
+          }
+          __syncwarp();
         }
       }
       ++sw;
@@ -691,6 +803,93 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
   }
 }
 
+// D_i = <dO_i, O_i> and LSE_i log2(e) (padding rows 0 and +inf, so that their P is
+// exactly 0); d = 64: both again as bias rows, -LSE/scale and -D as tf32 high and
+// low parts.  D / 8 lanes a row, 16 bytes each.  Key-major also zeroes dQacc.  The
+// blocks after the rows' zero the dK and dV accumulators.
+template <int D>
+__global__ void __launch_bounds__(256) xattn_pre_kernel(const XattnBwdParams p) {
+  constexpr int G = D / 8;
+  constexpr int kBlockRows = 256 / G;
+  const int d_io = (D == 64) ? D : p.d;
+  const long long rows = static_cast<long long>(p.BH) * p.M_pad;
+  const long long row_blocks = (rows + kBlockRows - 1) / kBlockRows;
+  if (blockIdx.x >= row_blocks) {
+    float4* acc = reinterpret_cast<float4*>(p.dkv_acc);
+    const long long i = (blockIdx.x - row_blocks) * 1024ll + threadIdx.x;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (i + 256 * k < p.dkv_float4s) acc[i + 256 * k] = make_float4(0.f, 0.f, 0.f, 0.f);
+    return;
+  }
+  const long long gr = blockIdx.x * static_cast<long long>(kBlockRows) + threadIdx.x / G;
+  const int sub = threadIdx.x % G;
+  const bool valid = gr < rows;
+  const int bh = static_cast<int>(gr / p.M_pad);
+  const int i = static_cast<int>(gr - static_cast<long long>(bh) * p.M_pad);
+  if (valid && p.zero_dq) {
+    float4* acc = reinterpret_cast<float4*>(p.dq_acc + gr * D);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) acc[sub + k * G] = make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+  float sum = 0.f;
+  if (valid && i < p.M && 8 * sub < d_io) {
+    const size_t off = (static_cast<size_t>(bh) * p.M + i) * d_io + 8 * sub;
+    const uint4 a = *reinterpret_cast<const uint4*>(p.o + off);
+    const uint4 b = *reinterpret_cast<const uint4*>(p.dout + off);
+    const uint32_t av[4] = {a.x, a.y, a.z, a.w}, bv[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      sum = fmaf(__uint_as_float(av[k] << 16), __uint_as_float(bv[k] << 16), sum);
+      sum = fmaf(__uint_as_float(av[k] & 0xffff0000u), __uint_as_float(bv[k] & 0xffff0000u), sum);
+    }
+  }
+#pragma unroll
+  for (int s = G / 2; s > 0; s >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, s);
+  if (valid && sub == 0) {
+    const float lse = i < p.M ? p.lse[static_cast<size_t>(bh) * p.M + i] : INFINITY;
+    if constexpr (D == 64) {
+      const float lb = i < p.M ? -lse / p.scale : -1e30f;
+      const float lh = __uint_as_float(__float_as_uint(lb) & 0xffffe000u);
+      const float dh = __uint_as_float(__float_as_uint(-sum) & 0xffffe000u);
+      float4* row = reinterpret_cast<float4*>(p.bias + gr * 8);
+      row[0] = make_float4(lh, lb - lh, dh, -sum - dh);
+      row[1] = make_float4(0.f, 0.f, 0.f, 0.f);
+    } else {
+      p.delta[gr] = sum;
+      p.lse2[gr] = lse * 1.4426950408889634f;
+    }
+  }
+}
+
+// bf16 rows from the accumulators: dQ of samples with several key tiles (the others'
+// is written already), dK and dV where several ranges add to them.  8 columns a
+// thread; blockIdx.y 0: dQ, 1: dK, 2: dV.
+template <int D>
+__global__ void __launch_bounds__(256) xattn_post_kernel(const XattnBwdParams p, int first) {
+  const int which = blockIdx.y + first;
+  const int d_io = (D == 64) ? D : p.d;
+  const int pieces = d_io / 8;
+  const int rows = which == 0 ? p.M : p.S;
+  const int padded = which == 0 ? p.M_pad : p.S_pad;
+  const float* acc = which == 0 ? p.dq_acc : which == 1 ? p.dkv_acc : p.dkv_acc + static_cast<size_t>(p.BH) * p.S_pad * D;
+  __nv_bfloat16* out = which == 0 ? p.dq : which == 1 ? p.dk : p.dv;
+  const float mul = which == 2 ? 1.f : p.scale;
+  const long long total = static_cast<long long>(p.BH) * rows * pieces;
+  for (long long i = blockIdx.x * 256ll + threadIdx.x; i < total; i += gridDim.x * 256ll) {
+    const long long row = i / pieces;
+    const int c = static_cast<int>(i - row * pieces) * 8;
+    const int bh = static_cast<int>(row / rows);
+    const int r = static_cast<int>(row - static_cast<long long>(bh) * rows);
+    if (which == 0 && p.kv_len && p.kv_len[bh / p.heads] <= kTileRows) continue;
+    const float4* src = reinterpret_cast<const float4*>(acc + (static_cast<size_t>(bh) * padded + r) * D + c);
+    const float4 a = src[0], b = src[1];
+    *reinterpret_cast<uint4*>(out + row * d_io + c) =
+        make_uint4(pack_bf16x2(a.x * mul, a.y * mul), pack_bf16x2(a.z * mul, a.w * mul),
+                   pack_bf16x2(b.x * mul, b.y * mul), pack_bf16x2(b.z * mul, b.w * mul));
+  }
+}
+
 template <int D, int DM>
 cudaError_t launch(const XattnBwdMaps& m, const XattnBwdParams& p, int dev, int sms, cudaStream_t s) {
   using L = Layout<D, DM>;
@@ -706,13 +905,27 @@ cudaError_t launch(const XattnBwdMaps& m, const XattnBwdParams& p, int dev, int 
   });
   if (e != cudaSuccess) return e;
   const unsigned grid = static_cast<unsigned>(p.pieces < sms ? p.pieces : sms);
-  xattn_bwd_kernel<D, DM><<<grid, L::THREADS, L::BYTES, s>>>(m.q, m.k, m.v, m.dout, m.dq, m.dk, m.dv, m.bias, p);
+  const long long rows = static_cast<long long>(p.BH) * p.M_pad;
+  constexpr int kBlockRows = 256 / (D / 8);
+  const long long pre = (rows + kBlockRows - 1) / kBlockRows + (p.dkv_float4s + 1023) / 1024;
+  xattn_pre_kernel<D><<<static_cast<unsigned>(pre), 256, 0, s>>>(p);
+  xattn_bwd_kernel<D, DM><<<grid, L::THREADS, L::BYTES, s>>>(m.q, m.k, m.v, m.dout, m.dq, m.dk, m.dv, m.bias,
+                                                             m.dq_out, p);
+  // what several sweeps add to becomes bf16
+  const int first = p.k_tiles > 1 ? 0 : 1, last = p.ranges > 1 ? 3 : 1;
+  if (first < last) {
+    const long long most = static_cast<long long>(p.BH) * (first == 0 && p.M > p.S ? p.M : last > 1 ? p.S : p.M) *
+                           (p.d / 8);
+    const long long blocks = (most + 255) / 256;
+    xattn_post_kernel<D><<<dim3(static_cast<unsigned>(blocks < 1 << 20 ? blocks : 1 << 20), last - first), 256, 0, s>>>(
+        p, first);
+  }
   return cudaGetLastError();
 }
 
 }  // namespace
 
-cudaError_t launch_xattn_bwd_main(int d, int dm, const XattnBwdMaps& m, const XattnBwdParams& p, int dev, int sms,
+cudaError_t launch_xattn_bwd(int d, int dm, const XattnBwdMaps& m, const XattnBwdParams& p, int dev, int sms,
                                   cudaStream_t s) {
   if (d == 64) return launch<64, 64>(m, p, dev, sms, s);
   if (dm == 80) return launch<128, 80>(m, p, dev, sms, s);
