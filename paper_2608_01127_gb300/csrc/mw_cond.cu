@@ -315,6 +315,8 @@ mw_status mw_xattn_bwd(const void* q, const void* k, const void* v, const int* k
   p.d = d;
   p.key_major = ws.plan.key_major;
   p.ranges = ws.plan.ranges;
+  p.range_tiles = ws.M_pad / kTileRows / p.ranges;
+  p.range_rest = ws.M_pad / kTileRows % p.ranges;
   p.k_tiles = ws.S_pad / kTileRows;
   p.pieces = z.BH * p.ranges * (p.key_major ? p.k_tiles : 1);
   p.zero_dq = p.key_major;

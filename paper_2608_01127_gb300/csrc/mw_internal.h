@@ -269,6 +269,7 @@ struct XattnBwdParams {
   int BH, heads, M, M_pad, S, S_pad, d;  // _pad: rounded up to kTileRows
   bool key_major;      // a piece of work is one key tile, else a range of query tiles
   int ranges, k_tiles; // ranges of a head's query tiles; key tiles of S states
+  int range_tiles, range_rest;  // query tiles of a range, one more in the first range_rest
   int pieces;          // BH * ranges, key-major times k_tiles
   bool zero_dq;        // dq_acc is only added to
   bool wide_dq, wide_dkv;  // every row of the outputs starts at a multiple of 32 bytes

@@ -114,12 +114,13 @@ struct Walk {
       const int s = bh / p.heads;
       if (s != sample) {
         sample = s;
-        len = min(max(p.kv_len[s], 0), p.S);
+        // (all lanes read the same; the reduction tells the compiler, which then
+        // holds what follows from it in uniform registers: 100 -> 87 KB of code)
+        len = min(max(__reduce_max_sync(__activemask(), p.kv_len[s]), 0), p.S);
       }
     }
-    const int tiles = p.M_pad / kTileRows;
-    q0 = static_cast<int>(static_cast<long long>(r) * tiles / p.ranges);
-    n_q = static_cast<int>(static_cast<long long>(r + 1) * tiles / p.ranges) - q0;
+    q0 = r * p.range_tiles + min(r, p.range_rest);
+    n_q = p.range_tiles + (r < p.range_rest);
     n_kt = (len + kTileRows - 1) / kTileRows;
     k_end = p.key_major ? min(kt + 1, n_kt) : n_kt;
     return true;
@@ -396,53 +397,49 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
       // the last sweep's dK and dV are out of tensor memory
       auto wait_dkv = [&]() { return sw == 0 || warp_wait(dkv_free, (sw - 1) & 1, ctl); };
       if (role_a) {
-        if (!(ok = warp_wait(&q_full[g % NQ], (g / NQ) & 1, ctl))) break;
-        if constexpr (!L::PAIRED)
-          if (g > 0 && !(ok = warp_wait(s_free, (g - 1) & 1, ctl))) break;
-        tc_fence_after();
-        issue_s(g);
-        if (!(ok = warp_wait(v_full, sw & 1, ctl))) break;
-        if constexpr (!L::PAIRED) {
-          if (!(ok = warp_wait(&do_full[g % ND], (g / ND) & 1, ctl))) break;
-          if (g > 0 && !(ok = warp_wait(dp_free, (g - 1) & 1, ctl))) break;
-          tc_fence_after();
-          issue_dp(g);
-          if (w.n_q == 1) umma_commit(v_empty);
-        }
-        for (int j = 0; j < w.n_q; ++j, ++g) {
+        // j = -1: the sweep's first S (and dP); g counts the steps whose S is issued
+        for (int j = -1; j < w.n_q; ++j) {
           const bool more = j + 1 < w.n_q;
+          auto next_dp = [&](int x) {  // dP^T of step x, the (j + 1)-th of the sweep (PAIRED: the j-th)
+            if (!warp_wait(&do_full[x % ND], (x / ND) & 1, ctl)) return false;
+            // d = 64: the P/dS warps hold the last dP^T; else the drain holds the last
+            // dQ, whose columns this takes
+            if (x > 0 && !warp_wait(L::PAIRED ? dq_free : dp_free, (x - 1) & 1, ctl)) return false;
+            tc_fence_after();
+            issue_dp(x);
+            return true;
+          };
           if constexpr (L::PAIRED) {
             // dP, dV, the next S: MMAs of one issuer run in order, so the next S may
             // land on P once dV is issued
-            if (!(ok = warp_wait(&do_full[g % ND], (g / ND) & 1, ctl))) break;
-            // the last dQ is in the drain's registers: its columns take dP
-            if (g > 0 && !(ok = warp_wait(dq_free, (g - 1) & 1, ctl))) break;
-            tc_fence_after();
-            issue_dp(g);
-            if (!more) umma_commit(v_empty);
+            if (j >= 0) {
+              if (j == 0 && !(ok = warp_wait(v_full, sw & 1, ctl))) break;
+              if (!(ok = next_dp(g - 1))) break;
+              if (!more) umma_commit(v_empty);
+            }
           } else if (more) {
-            // S^T of the next step as soon as the P/dS warps hold this one's
-            if (!(ok = warp_wait(s_free, g & 1, ctl))) break;
-            if (!(ok = warp_wait(&q_full[(g + 1) % NQ], ((g + 1) / NQ) & 1, ctl))) break;
+            // S^T of the next step as soon as the P/dS warps hold the last one
+            if (!(ok = warp_wait(&q_full[g % NQ], (g / NQ) & 1, ctl))) break;
+            if (g > 0 && !(ok = warp_wait(s_free, (g - 1) & 1, ctl))) break;
             tc_fence_after();
-            issue_s(g + 1);
+            issue_s(g++);
           }
-          if (!(ok = warp_wait(pt_ready, g & 1, ctl))) break;
-          if (j == 0 && !(ok = wait_dkv())) break;
-          tc_fence_after();
-          issue_dv(g, j > 0);
-          umma_commit(&do_empty[g % ND]);
+          if (j >= 0) {
+            const int x = L::PAIRED || !more ? g - 1 : g - 2;  // the step in work
+            if (!(ok = warp_wait(pt_ready, x & 1, ctl))) break;
+            if (j == 0 && !(ok = wait_dkv())) break;
+            tc_fence_after();
+            issue_dv(x, j > 0);
+            umma_commit(&do_empty[x % ND]);
+          }
           if (!more) continue;
           if constexpr (L::PAIRED) {
-            if (!(ok = warp_wait(&q_full[(g + 1) % NQ], ((g + 1) / NQ) & 1, ctl))) break;
+            if (!(ok = warp_wait(&q_full[g % NQ], (g / NQ) & 1, ctl))) break;
             tc_fence_after();
-            issue_s(g + 1);
+            issue_s(g++);
           } else {
-            // dP^T of the next step once the P/dS warps hold this one's
-            if (!(ok = warp_wait(dp_free, g & 1, ctl))) break;
-            if (!(ok = warp_wait(&do_full[(g + 1) % ND], ((g + 1) / ND) & 1, ctl))) break;
-            tc_fence_after();
-            issue_dp(g + 1);
+            if (j < 0 && !(ok = warp_wait(v_full, sw & 1, ctl))) break;
+            if (!(ok = next_dp(g - 1))) break;
             if (j + 2 == w.n_q) umma_commit(v_empty);
           }
         }
@@ -689,47 +686,67 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
         if constexpr (L::DQT) {
           // lanes = head-dim columns, TMEM columns = the QN query rows: boxes of 32
           // queries.  The maps clip columns past the caller's; warps with none skip.
-          uint32_t r[QN / 32][32];
-#pragma unroll
-          for (int c = 0; c < QN / 32; ++c) tmem_ld32(lane_base + L::DQ_COL + 32 * c, r[c]);
-          tmem_wait_ld();
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(dq_free);  // dQ is in registers
-          if (32 * wq < p.d) {
-#pragma unroll
+          auto hand_over = [&]() {  // dQ is in registers
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(dq_free);
+          };
+          auto next_box = [&]() {
+            uint8_t* stg = smem + L::OFF_STG + (2 * wq + box) * L::BOX_BYTES;
+            if (lane == 0) bulk_wait_read<1>();  // the TMA unit has read this box
+            __syncwarp();
+            box ^= 1;
+            return stg;
+          };
+          if (whole) {
+#pragma unroll 1
             for (int c = 0; c < QN / 32; ++c) {
-              uint8_t* stg = smem + L::OFF_STG + (2 * wq + box) * L::BOX_BYTES;
-              if (lane == 0) bulk_wait_read<1>();
-              __syncwarp();
-              if (whole) {
-                // bf16 rows of 64 bytes: of two queries, even lanes take the first and
-                // odd ones the second, a pair of columns each
+              uint32_t r[32];
+              tmem_ld32(lane_base + L::DQ_COL + 32 * c, r);
+              tmem_wait_ld();
+              if (c == QN / 32 - 1) hand_over();
+              if (32 * wq >= p.d) continue;
+              uint8_t* stg = next_box();
+              // bf16 rows of 64 bytes: of two queries, even lanes take the first and odd
+              // ones the second, a pair of columns each
 #pragma unroll
-                for (int k = 0; k < 32; k += 2) {
-                  const float a = __uint_as_float(r[c][k]) * p.scale, b = __uint_as_float(r[c][k + 1]) * p.scale;
-                  const float other = __shfl_xor_sync(0xffffffffu, lane & 1 ? a : b, 1);
-                  const uint32_t pair = lane & 1 ? pack_bf16x2(other, b) : pack_bf16x2(a, other);
-                  *reinterpret_cast<uint32_t*>(stg + (k + (lane & 1)) * 64 + (lane >> 1) * 4) = pair;
-                }
-              } else {
-#pragma unroll
-                for (int k = 0; k < 32; ++k)  // each instruction one row, 16-byte chunks swizzled
-                  *reinterpret_cast<uint32_t*>(stg + k * 128 + (((lane >> 2) ^ (k & 7)) << 4) + (lane & 3) * 4) =
-                      r[c][k];
+              for (int k = 0; k < 32; k += 2) {
+                const float a = __uint_as_float(r[k]) * p.scale, b = __uint_as_float(r[k + 1]) * p.scale;
+                const float other = __shfl_xor_sync(0xffffffffu, lane & 1 ? a : b, 1);
+                const uint32_t pair = lane & 1 ? pack_bf16x2(other, b) : pack_bf16x2(a, other);
+                *reinterpret_cast<uint32_t*>(stg + (k + (lane & 1)) * 64 + (lane >> 1) * 4) = pair;
               }
               fence_proxy_async_smem();
               __syncwarp();
               if (lane == 0) {
-                if (whole)
-                  tma_store_3d(&tm_dqo, stg, 32 * wq, q0 + 32 * c, w.bh);
-                else if (add)
-                  tma_reduce_add_3d(&tm_dq, stg, 32 * wq, q0 + 32 * c, w.bh);
-                else
-                  tma_store_3d(&tm_dq, stg, 32 * wq, q0 + 32 * c, w.bh);
+                tma_store_3d(&tm_dqo, stg, 32 * wq, q0 + 32 * c, w.bh);
                 bulk_commit_group();
               }
-              box ^= 1;
+            }
+          } else {
+            uint32_t r[QN / 32][32];
+#pragma unroll
+            for (int c = 0; c < QN / 32; ++c) tmem_ld32(lane_base + L::DQ_COL + 32 * c, r[c]);
+            tmem_wait_ld();
+            hand_over();
+            if (32 * wq < p.d) {
+#pragma unroll
+              for (int c = 0; c < QN / 32; ++c) {
+                uint8_t* stg = next_box();
+#pragma unroll
+                for (int k = 0; k < 32; ++k)  // each instruction one row, 16-byte chunks swizzled
+                  *reinterpret_cast<uint32_t*>(stg + k * 128 + (((lane >> 2) ^ (k & 7)) << 4) + (lane & 3) * 4) =
+                      r[c][k];
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) {
+                  if (add)
+                    tma_reduce_add_3d(&tm_dq, stg, 32 * wq, q0 + 32 * c, w.bh);
+                  else
+                    tma_store_3d(&tm_dq, stg, 32 * wq, q0 + 32 * c, w.bh);
+                  bulk_commit_group();
+                }
+              }
             }
           }
         } else {
@@ -761,31 +778,31 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
       if (!ok || !(ok = warp_wait(dkv_full, sw & 1, ctl))) break;
       tc_fence_after();
       const int row = w.kt * kTileRows + wq * 32;
-#pragma unroll
-      for (int m = 0; m < 2; ++m) {
-#pragma unroll
-        for (int c = 0; c < (DM + 31) / 32; ++c) {
-          uint32_t r[32];
-          tmem_ld32(lane_base + (m == 0 ? L::DV_COL : L::DK_COL) + 32 * c, r);
-          tmem_wait_ld();
-          if (m == 1 && c == (DM + 31) / 32 - 1) {
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(dkv_free);
-          }
-          if (32 * c < p.d) {
-            if (p.ranges > 1) {
-              put_rows(m == 0 ? &tm_dv : &tm_dk, r, 32 * c, row, true);
-            } else if (row + lane < p.S) {
-              float v[32];
-#pragma unroll
-              for (int k = 0; k < 32; ++k) v[k] = __uint_as_float(r[k]) * (m == 0 ? 1.f : p.scale);
-              store_row32((m == 0 ? p.dv : p.dk) + (static_cast<size_t>(w.bh) * p.S + row + lane) * p.d + 32 * c, v,
-                          min(4, (p.d - 32 * c) / 8), p.wide_dkv);
-            }
-          }
+      constexpr int kChunks = (DM + 31) / 32;
+#pragma unroll 1
+      for (int i = 0; i < 2 * kChunks; ++i) {
+        const bool is_dk = i >= kChunks;
+        const int c = is_dk ? i - kChunks : i;
+        uint32_t r[32];
+        tmem_ld32(lane_base + (is_dk ? L::DK_COL : L::DV_COL) + 32 * c, r);
+        tmem_wait_ld();
+        if (i == 2 * kChunks - 1) {
+          tc_fence_before();
           __syncwarp();
+          if (lane == 0) mbar_arrive(dkv_free);
         }
+        if (32 * c >= p.d) continue;
+        if (p.ranges > 1) {
+          put_rows(is_dk ? &tm_dk : &tm_dv, r, 32 * c, row, true);
+        } else if (row + lane < p.S) {
+          const float mul = is_dk ? p.scale : 1.f;
+          float v[32];
+#pragma unroll
+          for (int k = 0; k < 32; ++k) v[k] = __uint_as_float(r[k]) * mul;
+          store_row32((is_dk ? p.dk : p.dv) + (static_cast<size_t>(w.bh) * p.S + row + lane) * p.d + 32 * c, v,
+                      min(4, (p.d - 32 * c) / 8), p.wide_dkv);
+        }
+        __syncwarp();
       }
       ++sw;
     }

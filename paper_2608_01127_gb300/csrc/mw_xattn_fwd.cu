@@ -54,8 +54,10 @@ struct Layout {
   static constexpr bool SPLIT_P = 256 + OW * QT + 32 * QT <= 512;
   static constexpr int ISSUERS = D == 64 ? QT : 1;
   static constexpr int HELPERS = 3 - ISSUERS;
-  static constexpr int NBAR = 2 * QBUFS + 5 * STAGES + 5 * QT;
-  static constexpr int OFF_MISC = OFF_BAR + NBAR * 8;
+  static constexpr int SLOTS = 4;  // blocks announced ahead
+  static constexpr int NBAR = 2 * QBUFS + 5 * STAGES + 5 * QT + 2 * SLOTS;
+  static constexpr int OFF_SLOTS = (OFF_BAR + NBAR * 8 + 15) / 16 * 16;
+  static constexpr int OFF_MISC = OFF_SLOTS + SLOTS * 32;
   static constexpr int BYTES = OFF_MISC + 16;
   static_assert(BYTES <= 232448, "shared memory");
   static constexpr uint32_t S_COL(int t) { return 128u * t; }
@@ -73,47 +75,42 @@ struct Layout {
                 "register re-split must hand out exactly the launch's registers");
 };
 
-// The blocks of a CTA in turn; every role walks through the same ones.
-struct Walk {
-  const XattnTcParams& p;
-  int next;        // index of the next block
-  int sample, len; // the last block's sample and its valid states
-  int bh, r0, split;
-  int j0, n;       // its key tiles: n from the j0-th on
-  __device__ explicit Walk(const XattnTcParams& p_) : p(p_), next(blockIdx.x), sample(-1), len(p_.S) {}
-  __device__ __forceinline__ bool step() {
-    if (next >= p.items) return false;
-    int x = next;
-    next += gridDim.x;
-    split = x % p.num_splits;
-    x /= p.num_splits;
-    bh = x / p.n_qblocks;
-    r0 = (x - bh * p.n_qblocks) * kFwdBlockRows;
-    if (p.kv_len) {
-      const int s = bh / p.heads;
-      if (s != sample) {
-        sample = s;
-        len = min(max(p.kv_len[s], 0), p.S);
-      }
-    }
-    const int all = (len + kTileRows - 1) / kTileRows;
-    j0 = static_cast<int>(static_cast<long long>(split) * all / p.num_splits);
-    n = static_cast<int>(static_cast<long long>(split + 1) * all / p.num_splits) - j0;
-    return true;
-  }
-  // the next block that has keys
-  __device__ __forceinline__ bool step_nonempty() {
-    while (step())
-      if (n > 0) return true;
-    return false;
-  }
-  __device__ __forceinline__ bool present(int t) const { return r0 + kTileRows * t < p.M; }
+// A block of a CTA, as the producer announces it to the other roles.
+struct Block {
+  int bh;        // head; below 0: no more blocks
+  int r0;        // first row
+  int split;     // range of key tiles
+  int row0, n;   // its first key row, its key tiles
+  int len;       // valid states
+  __device__ __forceinline__ bool present(int t, int M) const { return r0 + kTileRows * t < M; }
   // V tile i of the block passes through the helper warps: all of them, or those
   // with rows that count as nothing but may hold anything (past S are zeros)
-  __device__ __forceinline__ bool helped(int i, bool all) const {
-    return all || ((j0 + i + 1) * kTileRows > len && len < p.S);
+  __device__ __forceinline__ bool helped(int i, bool all, int S) const {
+    return all || (row0 + (i + 1) * kTileRows > len && len < S);
   }
 };
+
+// Block x of the launch.
+__device__ __forceinline__ Block block_of(const XattnTcParams& p, int x) {
+  Block b;
+  b.split = 0;
+  if (p.num_splits > 1) {
+    const int y = x / p.num_splits;
+    b.split = x - y * p.num_splits;
+    x = y;
+  }
+  b.bh = x / p.n_qblocks;
+  b.r0 = (x - b.bh * p.n_qblocks) * kFwdBlockRows;
+  b.len = p.kv_len ? min(max(p.kv_len[b.bh / p.heads], 0), p.S) : p.S;
+  b.n = (b.len + kTileRows - 1) / kTileRows;
+  b.row0 = 0;
+  if (p.num_splits > 1) {  // ranges that differ by a tile at most
+    const int base = b.n / p.num_splits, rest = b.n - base * p.num_splits;
+    b.row0 = (b.split * base + min(b.split, rest)) * kTileRows;
+    b.n = base + (b.split < rest);
+  }
+  return b;
+}
 
 template <int D, int DM>
 __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
@@ -126,14 +123,14 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
   const int lane = threadIdx.x & 31;
 
   // Row `row` of head bh gets its value: bf16 O and LSE, or a split's partials.
-  auto store_lse = [&](const Walk& w, int row, float lse) {
+  auto store_lse = [&](const Block& w, int row, float lse) {
     const size_t at = static_cast<size_t>(w.bh) * p.M + row;
     if (p.num_splits > 1)
       p.lse_part[static_cast<size_t>(w.split) * p.BH * p.M + at] = lse;
     else if (p.lse)
       p.lse[at] = lse;
   };
-  auto store_nothing = [&](const Walk& w, int row) {
+  auto store_nothing = [&](const Block& w, int row) {
     if (p.num_splits == 1) {  // (the combine skips a split whose LSE is -inf)
       uint4* dst = reinterpret_cast<uint4*>(p.o + (static_cast<size_t>(w.bh) * p.M + row) * p.d);
       for (int c = 0; c < p.d / 8; ++c) dst[c] = make_uint4(0u, 0u, 0u, 0u);
@@ -145,8 +142,8 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
     // nothing runs without aligned shared memory: report it, and give this CTA's
     // rows a defined result
     if (threadIdx.x == 0) atomicOr(p.status, kDevMisaligned);
-    Walk w(p);
-    while (w.step()) {
+    for (int x = blockIdx.x; x < p.items; x += gridDim.x) {
+      const Block w = block_of(p, x);
       const int row = w.r0 + static_cast<int>(threadIdx.x);
       if (threadIdx.x < kFwdBlockRows && row < p.M) store_nothing(w, row);
     }
@@ -164,6 +161,8 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
   uint64_t* p_full = p_half + QT;
   uint64_t* pv_done = p_full + QT;  // PV of a key tile (SPLIT_P), of a block's last one (else)
   uint64_t* o_free = pv_done + QT;  // O of a block is in registers
+  uint64_t* b_full = o_free + QT;   // a block is announced, and
+  uint64_t* b_empty = b_full + L::SLOTS;  // read by all roles
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + L::OFF_MISC);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + L::OFF_MISC + 4);
 
@@ -185,6 +184,10 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
       mbar_init(&p_full[t], 4);
       mbar_init(&pv_done[t], 1);
       mbar_init(&o_free[t], 4);
+    }
+    for (int b = 0; b < L::SLOTS; ++b) {
+      mbar_init(&b_full[b], 1);
+      mbar_init(&b_empty[b], 11);  // the other warps
     }
     *abort_flag = 0;
     fence_mbar_init();
@@ -215,7 +218,32 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
   uint8_t* sQ = smem + L::OFF_Q;
   uint8_t* sK = smem + L::OFF_K;
   uint8_t* sV = smem + L::OFF_V;
-  Walk w(p);
+  int4* slots = reinterpret_cast<int4*>(smem + L::OFF_SLOTS);
+  // The next block, for a whole warp (its fields agree over the lanes: the shuffles
+  // tell the compiler, which then works in uniform registers).
+  int turn = 0;
+  Block w;
+  auto next_block = [&]() {
+    const int slot = turn % L::SLOTS;
+    if (!warp_wait(&b_full[slot], (turn / L::SLOTS) & 1, ctl)) return false;
+    ++turn;
+    const int4 a = slots[2 * slot], b = slots[2 * slot + 1];
+    w.bh = __shfl_sync(0xffffffffu, a.x, 0);
+    w.r0 = __shfl_sync(0xffffffffu, a.y, 0);
+    w.split = __shfl_sync(0xffffffffu, a.z, 0);
+    w.row0 = __shfl_sync(0xffffffffu, a.w, 0);
+    w.n = __shfl_sync(0xffffffffu, b.x, 0);
+    w.len = __shfl_sync(0xffffffffu, b.y, 0);
+    if (lane == 0) mbar_arrive(&b_empty[slot]);
+    return w.bh >= 0;
+  };
+  // the next one that has keys
+  auto next_keys = [&]() {
+    do {
+      if (!next_block()) return false;
+    } while (w.n == 0);
+    return true;
+  };
 
   if (warp >= 8) {
   regs_dec<L::REGS_CONTROL>();
@@ -223,13 +251,22 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
     // ------------------------------------------------------------ TMA producer
     if (lane == 0) {
       int nq = 0, nk = 0, nv = 0;  // blocks, K and V tiles so far
-      uint32_t raw = 0, turn = 0;  // per stage: its last V tile went to a helper; parity of those
+      uint32_t raw = 0, raws = 0;  // per stage: its last V tile went to a helper; parity of those
       bool ok = true;
-      while (ok && w.step_nonempty()) {
+      for (int x = blockIdx.x; ok; x += gridDim.x, ++turn) {
+        const int slot = turn % L::SLOTS;
+        if (!(ok = mbar_wait(&b_empty[slot], ((turn / L::SLOTS) & 1) ^ 1, ctl))) break;
+        w.bh = -1;
+        if (x < p.items) w = block_of(p, x);
+        slots[2 * slot] = make_int4(w.bh, w.r0, w.split, w.row0);
+        slots[2 * slot + 1] = make_int4(w.n, w.len, 0, 0);
+        mbar_arrive(&b_full[slot]);  // (releases the stores above)
+        if (w.bh < 0) break;
+        if (w.n == 0) continue;
         const int qb = nq % NQ;
         if (!(ok = mbar_wait(&q_empty[qb], ((nq / NQ) & 1) ^ 1, ctl))) break;
         if (!p.debug_skip_q) {
-          const int tiles = w.present(1) ? QT : 1;
+          const int tiles = w.present(1, p.M) ? QT : 1;
           mbar_arrive_expect_tx(&q_full[qb], tiles * L::TILE_BYTES);
           for (int t = 0; t < tiles; ++t)
             for (int r = 0; r < L::REG; ++r)
@@ -240,20 +277,20 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
         for (int i = 0; i < w.n; ++i) {
           const int st = nk % NS;
           const uint32_t ph = ((nk / NS) & 1) ^ 1;
-          const int row0 = (w.j0 + i) * kTileRows;
+          const int row0 = w.row0 + i * kTileRows;
           if (!(ok = mbar_wait(&k_empty[st], ph, ctl))) break;
           mbar_arrive_expect_tx(&k_full[st], L::TILE_BYTES);
           for (int r = 0; r < L::REG; ++r)
             tma_load_3d(sK + st * L::TILE_BYTES + r * L::REGION_BYTES, &tm_k, &k_full[st], 64 * r, row0, w.bh);
           ++nk;
           if (!(ok = mbar_wait(&v_empty[st], ph, ctl))) break;
-          const bool help = w.helped(i, L::ONES_IN_V);
+          const bool help = w.helped(i, L::ONES_IN_V, p.S);
           uint64_t* bar = help ? &v_raw[st] : &v_full[st];
           mbar_arrive_expect_tx(bar, L::TILE_BYTES);
           for (int r = 0; r < L::REG; ++r)
             tma_load_3d(sV + st * L::TILE_BYTES + r * L::REGION_BYTES, &tm_v, bar, 64 * r, row0, w.bh);
           raw = (raw & ~(1u << st)) | (help ? 1u << st : 0u);
-          turn ^= help ? 1u << st : 0u;
+          raws ^= help ? 1u << st : 0u;
           ++nv;
         }
       }
@@ -264,7 +301,7 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
         for (int i = max(0, nv - NS); i < nv; ++i) {
           const int st = i % NS;
           if ((raw >> st) & 1)
-            drain_wait(&v_raw[st], ((turn >> st) & 1) ^ 1, p.budget_ns);
+            drain_wait(&v_raw[st], ((raws >> st) & 1) ^ 1, p.budget_ns);
           else
             drain_wait(&v_full[st], (i / NS) & 1, p.budget_ns);
         }
@@ -297,103 +334,78 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
                 (acc || kk > 0) ? 1u : 0u);
       }
     };
-    // query tiles [T0, T1): one issuer's, or all of them
-    auto issue = [&](auto first, auto last) {
-      constexpr int T0 = decltype(first)::value, T1 = decltype(last)::value;
-      int nq = 0, nk = 0;       // blocks and key tiles whose S is issued
-      int done[QT] = {0, 0};    // key tiles of a query tile whose PV is issued
-      int blocks[QT] = {0, 0};  // blocks of a query tile begun
-      if (!w.step_nonempty()) return;
-      bool ok = warp_wait(&q_full[0], 0, ctl) && warp_wait(&k_full[0], 0, ctl);
-      tc_fence_after();
-      if (ok) {
-#pragma unroll
-        for (int t = T0; t < T1; ++t)
-          if (w.present(t)) {
-            issue_qk(t, 0, 0);
-            umma_commit(&s_full[t]);
-          }
-        umma_commit(&k_empty[0]);
-        if (w.n == 1) umma_commit(&q_empty[0]);
-        nk = 1;
-        nq = 1;
+    int nq = 0, nk = 0;       // blocks and key tiles whose S is issued
+    // of this warp's query tiles (all; d = 64: one, tile t0)
+    constexpr int NT = QT / L::ISSUERS;
+    const int t0 = L::ISSUERS == 1 ? 0 : warp - 9;
+    int done[NT] = {};    // key tiles whose PV is issued
+    int blocks[NT] = {};  // blocks begun
+    int i = -1;               // tile of the block in work (none yet)
+    bool have[NT] = {};
+    w.n = 0;
+    bool ok = true, more = true;
+    // In turn: S of the next tile, and PV of this one, of which S is there.  Where P
+    // leaves S free in time, the next S goes between the halves of the PV.
+    while (ok && more) {
+      const int st = (nk + NS - 1) % NS;
+      const uint32_t ph = ((nk - 1) / NS) & 1;
+      const bool any = i >= 0, first_tile = i == 0, last_tile = i + 1 == w.n;
+      if (last_tile) {
+        more = next_keys();
+        i = 0;
+      } else {
+        ++i;
       }
-      int i = 0;
-      while (ok) {
-        // tile i of this block, of which S is issued, and the tile after it
-        const int st = (nk - 1) % NS;
-        const uint32_t ph = ((nk - 1) / NS) & 1;
-        const bool have[QT] = {w.present(0), w.present(1)};
-        const bool first_tile = i == 0, last_tile = i + 1 == w.n;
-        bool more = true;
-        if (last_tile) {
-          more = w.step_nonempty();
-          i = 0;
-        } else {
-          ++i;
-        }
-        const int st1 = nk % NS, qb1 = (i == 0 ? nq : nq - 1) % NQ;
-        bool waited = false;
-        auto wait_next = [&]() {  // Q (of a new block) and K of the next tile
-          if (waited) return true;
+      const int st1 = nk % NS;
+      const int qb1 = (i == 0 ? nq : nq - 1) % NQ;
+      bool waited = false;
+      auto next_s = [&](int t) {
+        if (!waited) {  // Q (of a new block) and K of the next tile
           waited = true;
           if (i == 0 && !warp_wait(&q_full[qb1], (nq / NQ) & 1, ctl)) return false;
           if (!warp_wait(&k_full[st1], (nk / NS) & 1, ctl)) return false;
           tc_fence_after();
-          return true;
-        };
-        // S of the next tile between the halves of this one's PV where P leaves
-        // it free, but not at the risk of waiting for a new block's Q
-        const bool early = L::SPLIT_P && (NQ > 1 || i > 0);
-        if (!(ok = warp_wait(&v_full[st], ph, ctl))) break;
-        tc_fence_after();
-#pragma unroll
-        for (int t = T0; t < T1; ++t) {
-          if (have[t]) {
-            if (!(ok = warp_wait(&p_half[t], done[t] & 1, ctl))) break;
-            if (first_tile) {
-              // the last block's O is in the softmax warps' registers
-              if (blocks[t] > 0 && !(ok = warp_wait(&o_free[t], (blocks[t] - 1) & 1, ctl))) break;
-              ++blocks[t];
-            }
-            tc_fence_after();
-            issue_pv(t, st, !first_tile, 0);
-          }
-          if (early && more && w.present(t)) {
-            if (!(ok = wait_next())) break;
-            issue_qk(t, qb1, st1);
-            umma_commit(&s_full[t]);
-          }
-          if (have[t]) {
-            if (!(ok = warp_wait(&p_full[t], done[t] & 1, ctl))) break;
-            tc_fence_after();
-            issue_pv(t, st, true, 1);
-            ++done[t];
-            if (L::SPLIT_P || last_tile) umma_commit(&pv_done[t]);
-          }
-          if (!early && more && w.present(t)) {
-            if (!(ok = wait_next())) break;
-            issue_qk(t, qb1, st1);
-            umma_commit(&s_full[t]);
-          }
         }
-        if (!ok) break;
-        umma_commit(&v_empty[st]);
-        if (!more) break;
-        if (!(ok = wait_next())) break;  // (an issuer without a tile here looks, too)
+        if (w.present(t, p.M)) {
+          issue_qk(t, qb1, st1);
+          umma_commit(&s_full[t]);
+        }
+        return true;
+      };
+      if (any && !(ok = warp_wait(&v_full[st], ph, ctl))) break;
+#pragma unroll
+      for (int u = 0; u < NT; ++u) {
+        const int t = t0 + u;
+        if (have[u]) {
+          if (!(ok = warp_wait(&p_half[t], done[u] & 1, ctl))) break;
+          if (first_tile) {
+            // the last block's O is in the softmax warps' registers
+            if (blocks[u] > 0 && !(ok = warp_wait(&o_free[t], (blocks[u] - 1) & 1, ctl))) break;
+            ++blocks[u];
+          }
+          tc_fence_after();
+          issue_pv(t, st, !first_tile, 0);
+        }
+        if (L::SPLIT_P && more && !(ok = next_s(t))) break;
+        if (have[u]) {
+          if (!(ok = warp_wait(&p_full[t], done[u] & 1, ctl))) break;
+          tc_fence_after();
+          issue_pv(t, st, true, 1);
+          ++done[u];
+          if (L::SPLIT_P || last_tile) umma_commit(&pv_done[t]);
+        }
+        if (!L::SPLIT_P && more && !(ok = next_s(t))) break;
+      }
+      if (!ok) break;
+      if (any) umma_commit(&v_empty[st]);
+      if (more) {
         umma_commit(&k_empty[st1]);
         if (i + 1 == w.n) umma_commit(&q_empty[qb1]);
-        if (i == 0) ++nq;
+#pragma unroll
+        for (int u = 0; u < NT; ++u) have[u] = w.present(t0 + u, p.M);
+        nq += i == 0;
         ++nk;
       }
-    };
-    if constexpr (L::ISSUERS == 1) {
-      issue(std::integral_constant<int, 0>{}, std::integral_constant<int, QT>{});
-    } else {
-      if (warp == 9)
-        issue(std::integral_constant<int, 0>{}, std::integral_constant<int, 1>{});
-      else
-        issue(std::integral_constant<int, 1>{}, std::integral_constant<int, 2>{});
     }
   } else {
     // ------------------------------------------------------------ V tiles made ready
@@ -405,16 +417,16 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
     constexpr int kParts = L::ONES_IN_V ? L::HELPERS : 1;
     constexpr int kRows = kTileRows / kParts;  // of a helper
     int nv = 0;
-    uint32_t turn = 0;  // parity of each stage's uses
-    bool ok = part < kParts;
-    while (ok && w.step_nonempty()) {
+    uint32_t raws = 0;  // parity of each stage's uses
+    bool ok = true;
+    while (ok && next_keys()) {
       for (int i = 0; i < w.n; ++i, ++nv) {
-        if (!w.helped(i, L::ONES_IN_V)) continue;
+        if (part >= kParts || !w.helped(i, L::ONES_IN_V, p.S)) continue;
         const int st = nv % NS;
-        if (!(ok = warp_wait(&v_raw[st], (turn >> st) & 1, ctl))) break;
-        turn ^= 1u << st;
+        if (!(ok = warp_wait(&v_raw[st], (raws >> st) & 1, ctl))) break;
+        raws ^= 1u << st;
         uint8_t* tile = sV + st * L::TILE_BYTES;
-        const int limit = w.len - (w.j0 + i) * kTileRows;
+        const int limit = w.len - w.row0 - i * kTileRows;
 #pragma unroll
         for (int k = 0; k < kRows / 32; ++k) {
           const int r = kRows * part + 32 * k + lane;
@@ -442,26 +454,31 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
     // ------------------------------------------------------------ softmax
     const int t = warp >> 2;
     const int wq = warp & 3;
-    const int row_local = wq * 32 + lane;
+    const int row_local = t * kTileRows + wq * 32 + lane;
     const uint32_t lane_base = tmem + (static_cast<uint32_t>(wq * 32) << 16);
     const uint32_t s_addr = lane_base + L::S_COL(t);
     const uint32_t o_addr = lane_base + L::O_COL(t);
     const float sl2 = p.scale_log2;
-    int done = 0;    // key tiles so far
-    int blocks = 0;  // blocks with keys so far
+    int blocks = 0;  // blocks dealt with
+    int begun = 0;   // blocks of this query tile that have keys
+    int done = 0;    // their key tiles
     bool ok = true;
-    while (w.step()) {
-      const int row = w.r0 + t * kTileRows + row_local;
-      const bool row_valid = row < p.M;
-      if (w.n == 0 || !ok) {  // no keys, or a wait gave up: a defined result
-        if (row_valid) store_nothing(w, row);
+    while ((ok = next_block())) {
+      const int row = w.r0 + row_local;
+      if (w.n == 0) {  // no keys
+        if (row < p.M) store_nothing(w, row);
         __syncwarp();
+        ++blocks;
         continue;
       }
-      if (!w.present(t)) continue;
+      if (!w.present(t, p.M)) {
+        ++blocks;
+        continue;
+      }
       float m_used = -INFINITY;
       float l = 0.f;
       const bool idle = w.r0 + t * kTileRows + wq * 32 >= p.M;  // a warp without rows only keeps step
+#pragma unroll 1
       for (int i = 0; i < w.n; ++i, ++done) {
         if (!(ok = warp_wait(&s_full[t], done & 1, ctl))) break;
         if (idle) {
@@ -469,56 +486,26 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
             mbar_arrive(&p_half[t]);
             mbar_arrive(&p_full[t]);
           }
-          // (the block's end shows that its PVs are done)
+          // (not a tile ahead of the others: their arrivals for this one count first)
           if (L::SPLIT_P && !(ok = warp_wait(&pv_done[t], done & 1, ctl))) break;
           continue;
         }
         tc_fence_after();
         float s[128];
-        if constexpr (L::SPLIT_P) {
-          uint32_t r[4][32];
 #pragma unroll
-          for (int c = 0; c < 4; ++c) tmem_ld32(s_addr + 32 * c, r[c]);
+        for (int c = 0; c < 4; ++c) {
+          uint32_t r[32];
+          tmem_ld32(s_addr + 32 * c, r);
           tmem_wait_ld();
 #pragma unroll
-          for (int c = 0; c < 128; ++c) s[c] = __uint_as_float(r[c / 32][c % 32]);
-        } else {
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            uint32_t r[32];
-            tmem_ld32(s_addr + 32 * c, r);
-            tmem_wait_ld();
-#pragma unroll
-            for (int k = 0; k < 32; ++k) s[32 * c + k] = __uint_as_float(r[k]);
-          }
+          for (int k = 0; k < 32; ++k) s[32 * c + k] = __uint_as_float(r[k]);
         }
-        const int limit = w.len - (w.j0 + i) * kTileRows;
+        const int limit = w.len - w.row0 - i * kTileRows;
         if (limit < kTileRows) {
 #pragma unroll
           for (int c = 0; c < 128; ++c)
             if (c >= limit) s[c] = -INFINITY;
         }
-        const float2 sl2x2 = make_float2(sl2, sl2);
-        auto minus = [](float m) {
-          const float m_eff = (m == -INFINITY) ? 0.f : m;
-          return make_float2(-m_eff, -m_eff);
-        };
-        // P of keys 32 g4 + 2 k and + 1, as a bf16 pair, relative to a maximum
-        auto weights = [&](int g4, int k, float2 negm) {
-          const float2 x = fma2(make_float2(s[32 * g4 + 2 * k], s[32 * g4 + 2 * k + 1]), sl2x2, negm);
-          return pack_bf16x2(ex2_approx(x.x), ex2_approx(x.y));
-        };
-        // the first groups against the maximum so far, which a tile hardly ever
-        // replaces (a block's first one always does)
-        constexpr int kEarly = L::SPLIT_P ? 2 : 0;
-        [[maybe_unused]] uint32_t early[kEarly > 0 ? kEarly : 1][16];
-        auto set_early = [&](float2 negm) {
-#pragma unroll
-          for (int g4 = 0; g4 < kEarly; ++g4)
-#pragma unroll
-            for (int k = 0; k < 16; ++k) early[g4][k] = weights(g4, k, negm);
-        };
-        if (i > 0) set_early(minus(m_used));
         float mq[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) mq[k] = fmaxf(s[k], s[k + 4]);
@@ -529,19 +516,17 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
           mq[2] = max3(mq[2], s[c + 4], s[c + 5]);
           mq[3] = max3(mq[3], s[c + 6], s[c + 7]);
         }
-        const float mx = max3(fmaxf(mq[0], mq[1]), mq[2], mq[3]);
-        const float m_tile = mx * sl2;  // scale > 0
+        const float m_tile = max3(fmaxf(mq[0], mq[1]), mq[2], mq[3]) * sl2;  // scale > 0
         const float m_cand = fmaxf(m_used, m_tile);
         // rescale only when the running maximum grew by more than 2^8: P stays
         // below 256 in between, and the final O / l is exact either way
         const bool need = m_cand > m_used + 8.0f;
-        if (i == 0 || __any_sync(0xffffffffu, need)) {
+        if (__any_sync(0xffffffffu, need)) {
           float alpha = 1.f;
           if (need) {
             alpha = ex2_approx(m_used - m_cand);
             m_used = m_cand;
           }
-          set_early(minus(m_used));
           l *= alpha;
           if (i > 0) {
             if constexpr (L::SPLIT_P) {  // (else S of this tile implies it)
@@ -549,19 +534,20 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
               tc_fence_after();
             }
             // exactly the tile's O columns, row sums included
-#pragma unroll
-            for (int c = 0; c < L::OW / 16; ++c) {
+#pragma unroll 1
+            for (int c = 0; c < L::OW; c += 16) {
               uint32_t r[16];
-              tmem_ld16(o_addr + 16 * c, r);
+              tmem_ld16(o_addr + c, r);
               tmem_wait_ld();
 #pragma unroll
               for (int k = 0; k < 16; ++k) r[k] = __float_as_uint(__uint_as_float(r[k]) * alpha);
-              tmem_st16(o_addr + 16 * c, r);
+              tmem_st16(o_addr + c, r);
             }
             tmem_wait_st();
           }
         }
-        const float2 negm = minus(m_used);
+        const float m_eff = m_used == -INFINITY ? 0.f : m_used;
+        const float2 sl2x2 = make_float2(sl2, sl2), negm = make_float2(-m_eff, -m_eff);
         float2 acc = make_float2(0.f, 0.f);
         // P in four 32-key groups, each stored as soon as it is packed; the first
         // two are announced while the third is stored
@@ -570,7 +556,8 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
           uint32_t packed[16];
 #pragma unroll
           for (int k = 0; k < 16; ++k) {
-            const uint32_t pk = g4 < kEarly ? early[g4 < kEarly ? g4 : 0][k] : weights(g4, k, negm);
+            const float2 x = fma2(make_float2(s[32 * g4 + 2 * k], s[32 * g4 + 2 * k + 1]), sl2x2, negm);
+            const uint32_t pk = pack_bf16x2(ex2_approx(x.x), ex2_approx(x.y));
             // the row sum uses the bf16 weights the PV MMA consumes, so O is an
             // exact convex combination of them
             if constexpr (!L::SUM_MMA)
@@ -599,48 +586,39 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
         if (lane == 0) mbar_arrive(&p_full[t]);
       }
 
-      // ---- epilogue
-      if (ok) ok = warp_wait(&pv_done[t], (L::SPLIT_P ? done - 1 : blocks) & 1, ctl);
-      ++blocks;
-      if (!ok) {
-        if (row_valid) store_nothing(w, row);
-        __syncwarp();
-        continue;
-      }
+      // ---- epilogue: a loop of 32 columns a turn (it runs once a block, and what
+      // runs once waits for its instructions: unrolled, it took longer)
+      if (ok) ok = warp_wait(&pv_done[t], (L::SPLIT_P ? done - 1 : begun) & 1, ctl);
+      if (!ok) break;
+      ++begun;
       tc_fence_after();
-      uint32_t r[(DM + 31) / 32][32];
-#pragma unroll
-      for (int c = 0; c < DM / 32; ++c) tmem_ld32(o_addr + 32 * c, r[c]);
-      if constexpr (DM % 32 != 0) {
-        uint32_t h[16];
-        tmem_ld16(o_addr + DM - 16, h);
-        tmem_wait_ld();
-#pragma unroll
-        for (int k = 0; k < 16; ++k) r[DM / 32][k] = h[k], r[DM / 32][16 + k] = 0u;
-      }
       if constexpr (L::SUM_MMA) {
         uint32_t h[16];
         tmem_ld16(o_addr + DM, h);
         tmem_wait_ld();
         l = __uint_as_float(h[0]);
       }
-      tmem_wait_ld();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&o_free[t]);
-      if (row_valid) {
-        const bool nonzero = l > 0.f;
-        const float inv_l = nonzero ? 1.f / l : 0.f;
-        const float m_eff = (m_used == -INFINITY) ? 0.f : m_used;
-        const size_t at = static_cast<size_t>(w.bh) * p.M + row;
-#pragma unroll
-        for (int c = 0; c < (DM + 31) / 32; ++c) {
+      const bool nonzero = l > 0.f;
+      const float inv_l = nonzero ? 1.f / l : 0.f;
+      const size_t at = static_cast<size_t>(w.bh) * p.M + row;
+      constexpr int kChunks = (DM + 31) / 32;
+#pragma unroll 1
+      for (int c = 0; c < kChunks; ++c) {
+        uint32_t r[32];  // (the last chunk's columns past the caller's are not stored)
+        tmem_ld32(o_addr + 32 * c, r);
+        tmem_wait_ld();
+        if (c == kChunks - 1) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&o_free[t]);
+        }
+        const int n16 = min(4, (p.d - 32 * c) / 8);  // 16-byte pieces of the caller's columns
+        if (row < p.M && n16 > 0) {
           float v[32];
 #pragma unroll
-          for (int k = 0; k < 32; ++k) v[k] = nonzero ? __uint_as_float(r[c][k]) * inv_l : 0.f;
+          for (int k = 0; k < 32; ++k) v[k] = nonzero ? __uint_as_float(r[k]) * inv_l : 0.f;
           if (p.num_splits == 1) {
-            const int d_io = (D == 64) ? D : p.d;
-            if (32 * c < d_io) store_row32(p.o + at * d_io + 32 * c, v, min(4, (d_io - 32 * c) / 8), p.wide_out);
+            store_row32(p.o + at * p.d + 32 * c, v, n16, p.wide_out);
           } else {
             float4* dst = reinterpret_cast<float4*>(
                 p.o_part + (static_cast<size_t>(w.split) * p.BH * p.M + at) * D + 32 * c);
@@ -648,7 +626,20 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
             for (int k = 0; k < 8; ++k) dst[k] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
           }
         }
+        __syncwarp();
+      }
+      if (row < p.M) {
+        const float m_eff = m_used == -INFINITY ? 0.f : m_used;
         store_lse(w, row, nonzero ? (m_eff + __log2f(l)) * 0.69314718055994530942f : -INFINITY);
+      }
+      __syncwarp();
+      ++blocks;
+    }
+    if (!ok && *abort_flag) {
+      // a wait gave up: this query tile's rows of the blocks left get a defined result
+      for (int x = blockIdx.x + blocks * gridDim.x; x < p.items; x += gridDim.x) {
+        const Block b = block_of(p, x);
+        if (b.r0 + row_local < p.M) store_nothing(b, b.r0 + row_local);
       }
       __syncwarp();
     }
