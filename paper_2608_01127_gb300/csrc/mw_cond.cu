@@ -197,10 +197,11 @@ mw_status mw_xattn_fwd(const void* q, const void* k, const void* v, const int* k
     const int D = kernel_d(d);
     XattnTcParams p{};
     MW_TRY(status_ptr(scope.device(), &p.status));
-    CUtensorMap tq, tk, tv;
+    CUtensorMap tq, tk, tv, to;
     MW_TRY(make_map(&tq, q, z.rows, z.BH, d, "q"));
     MW_TRY(make_map(&tk, k, S, z.BH, d, "k"));
     MW_TRY(make_map(&tv, v, S, z.BH, d, "v"));
+    MW_TRY(encode_rows_map(&to, o, z.rows, z.BH, d, true));
     p.kv_len = kv_len;
     p.o = static_cast<__nv_bfloat16*>(o);
     p.lse = lse;
@@ -212,7 +213,6 @@ mw_status mw_xattn_fwd(const void* q, const void* k, const void* v, const int* k
     p.n_qblocks = ceil_div(z.rows, kFwdBlockRows);
     p.num_splits = need > 0 ? xattn_splits(z.BH, z.rows, S) : 1;
     p.items = z.BH * p.n_qblocks * p.num_splits;
-    p.wide_out = wide_rows(o, d);
     p.scale_log2 = scale * 1.4426950408889634f;
     p.budget_ns = budget_ns();
     p.debug_skip_q = debug_skip_q();
@@ -222,7 +222,7 @@ mw_status mw_xattn_fwd(const void* q, const void* k, const void* v, const int* k
           static_cast<char*>(workspace) +
           align256(static_cast<size_t>(p.num_splits) * z.BH * z.rows * D * sizeof(float)));
     }
-    MW_TRY(launch_status(launch_xattn_tc(D, mma_d(d), tq, tk, tv, p, scope.device(), sm_count(), s),
+    MW_TRY(launch_status(launch_xattn_tc(D, mma_d(d), tq, tk, tv, to, p, scope.device(), sm_count(), s),
                          "cross attention forward launch"));
     if (p.num_splits > 1)
       MW_TRY(launch_status(launch_combine(D, d, p.o_part, p.lse_part, p.o, lse, p.num_splits, z.BH,
@@ -348,7 +348,7 @@ mw_status mw_xattn_bwd(const void* q, const void* k, const void* v, const int* k
   if (D == 64)
     MW_TRY(encode_bias_map(&m.bias, p.bias, ws.M_pad, z.BH, kTileRows));
   else
-    MW_TRY(encode_rows_map(&m.dq_out, dq, z.rows, z.BH, d));
+    MW_TRY(encode_rows_map(&m.dq_out, dq, z.rows, z.BH, d, false));
   return launch_status(launch_xattn_bwd(D, mma_d(d), m, p, scope.device(), sm_count(), s),
                        "cross attention backward launch");
 }

@@ -245,15 +245,16 @@ struct XattnTcParams {
   int BH, heads, M, S, d;
   int n_qblocks, num_splits;
   int items;           // BH * n_qblocks * num_splits
-  bool wide_out;       // every row of o starts at a multiple of 32 bytes
   float scale_log2;
   unsigned* status;
   unsigned long long budget_ns;
   int debug_skip_q;    // test hook: never load Q, so the issuers' wait expires
 };
-// d, dm: tile and MMA width as for launch_fwd; sms: CTAs at most
+// d, dm: tile and MMA width as for launch_fwd; to: o in 32 x 32 boxes with the 64-byte
+// swizzle; sms: CTAs at most
 cudaError_t launch_xattn_tc(int d, int dm, const CUtensorMap& tq, const CUtensorMap& tk,
-                            const CUtensorMap& tv, const XattnTcParams& p, int dev, int sms, cudaStream_t s);
+                            const CUtensorMap& tv, const CUtensorMap& to, const XattnTcParams& p, int dev, int sms,
+                            cudaStream_t s);
 // Forward of few rows a head on CUDA cores (mw_xattn.cu).
 cudaError_t launch_xattn_fwd(const XattnParams& p, cudaStream_t s);
 

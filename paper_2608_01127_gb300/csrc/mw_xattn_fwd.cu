@@ -38,7 +38,7 @@ struct Layout {
   static constexpr int REG = D / 64;  // 64-column swizzle regions per row
   static constexpr int REGION_BYTES = kTileRows * 128;
   static constexpr int TILE_BYTES = REG * REGION_BYTES;
-  static constexpr int STAGES = (D == 64) ? 4 : 2;
+  static constexpr int STAGES = (D == 64) ? 3 : 2;
   static constexpr int QBUFS = (D == 64) ? 2 : 1;  // blocks of Q in shared memory
   static constexpr int OFF_Q = 0;
   static constexpr int OFF_K = OFF_Q + QBUFS * QT * TILE_BYTES;
@@ -50,7 +50,10 @@ struct Layout {
   static constexpr int OW = SUM_MMA ? DM + 16 : DM;
   static constexpr int OFF_ONES = OFF_V + STAGES * TILE_BYTES;
   static constexpr int ONES_BYTES = (D == 64) ? REGION_BYTES : 0;
-  static constexpr int OFF_BAR = OFF_ONES + ONES_BYTES;
+  // O leaves through TMA stores of 32 x 32 boxes, two a warp in turn
+  static constexpr int BOX_BYTES = 32 * 64;
+  static constexpr int OFF_BOX = OFF_ONES + ONES_BYTES;
+  static constexpr int OFF_BAR = OFF_BOX + 8 * 2 * BOX_BYTES;
   static constexpr bool SPLIT_P = 256 + OW * QT + 32 * QT <= 512;
   static constexpr int ISSUERS = D == 64 ? QT : 1;
   static constexpr int HELPERS = 3 - ISSUERS;
@@ -115,7 +118,8 @@ __device__ __forceinline__ Block block_of(const XattnTcParams& p, int x) {
 template <int D, int DM>
 __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
     xattn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
-                     const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ XattnTcParams p) {
+                     const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_o,
+                     const __grid_constant__ XattnTcParams p) {
   using L = Layout<D, DM>;
   constexpr int QT = L::QT, NS = L::STAGES, NQ = L::QBUFS;
   extern __shared__ __align__(1024) uint8_t smem[];
@@ -196,6 +200,7 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
     prefetch_tmap(&tm_q);
     prefetch_tmap(&tm_k);
     prefetch_tmap(&tm_v);
+    prefetch_tmap(&tm_o);
   }
   if (warp == 9) {
     tmem_alloc(tmem_slot, 512);
@@ -253,15 +258,25 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
       int nq = 0, nk = 0, nv = 0;  // blocks, K and V tiles so far
       uint32_t raw = 0, raws = 0;  // per stage: its last V tile went to a helper; parity of those
       bool ok = true;
+      Block next = block_of(p, blockIdx.x);
       for (int x = blockIdx.x; ok; x += gridDim.x, ++turn) {
         const int slot = turn % L::SLOTS;
         if (!(ok = mbar_wait(&b_empty[slot], ((turn / L::SLOTS) & 1) ^ 1, ctl))) break;
-        w.bh = -1;
-        if (x < p.items) w = block_of(p, x);
+        w = next;
+        if (x >= p.items) w.bh = -1;
         slots[2 * slot] = make_int4(w.bh, w.r0, w.split, w.row0);
         slots[2 * slot + 1] = make_int4(w.n, w.len, 0, 0);
         mbar_arrive(&b_full[slot]);  // (releases the stores above)
         if (w.bh < 0) break;
+        // the block after it, its Q on the way into L2 (a block of one key tile is over
+        // in less than HBM's latency)
+        if (x + static_cast<int>(gridDim.x) < p.items) {
+          next = block_of(p, x + gridDim.x);
+          if (next.n > 0)
+            for (int t = 0; t < QT; ++t)
+              if (next.present(t, p.M))
+                for (int r = 0; r < L::REG; ++r) tma_prefetch_3d(&tm_q, 64 * r, next.r0 + kTileRows * t, next.bh);
+        }
         if (w.n == 0) continue;
         const int qb = nq % NQ;
         if (!(ok = mbar_wait(&q_empty[qb], ((nq / NQ) & 1) ^ 1, ctl))) break;
@@ -462,6 +477,7 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
     int blocks = 0;  // blocks dealt with
     int begun = 0;   // blocks of this query tile that have keys
     int done = 0;    // their key tiles
+    int box = 0;     // the staging box whose turn it is
     bool ok = true;
     while ((ok = next_block())) {
       const int row = w.r0 + row_local;
@@ -612,19 +628,33 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
           __syncwarp();
           if (lane == 0) mbar_arrive(&o_free[t]);
         }
-        const int n16 = min(4, (p.d - 32 * c) / 8);  // 16-byte pieces of the caller's columns
-        if (row < p.M && n16 > 0) {
-          float v[32];
+        if (idle || 32 * c >= p.d) continue;
+        float v[32];
 #pragma unroll
-          for (int k = 0; k < 32; ++k) v[k] = nonzero ? __uint_as_float(r[k]) * inv_l : 0.f;
-          if (p.num_splits == 1) {
-            store_row32(p.o + at * p.d + 32 * c, v, n16, p.wide_out);
-          } else {
-            float4* dst = reinterpret_cast<float4*>(
-                p.o_part + (static_cast<size_t>(w.split) * p.BH * p.M + at) * D + 32 * c);
+        for (int k = 0; k < 32; ++k) v[k] = nonzero ? __uint_as_float(r[k]) * inv_l : 0.f;
+        if (p.num_splits == 1) {
+          // 32 rows of 64 bytes with the 64-byte swizzle: 16-byte chunk k of row i at
+          // k ^ ((i >> 1) & 3).  The map clips rows and columns past the caller's.
+          uint8_t* stg = smem + L::OFF_BOX + (2 * warp + box) * L::BOX_BYTES;
+          box ^= 1;
+          if (lane == 0) bulk_wait_read<1>();  // the TMA unit has read this box
+          __syncwarp();
 #pragma unroll
-            for (int k = 0; k < 8; ++k) dst[k] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+          for (int k = 0; k < 4; ++k)
+            *reinterpret_cast<uint4*>(stg + lane * 64 + ((k ^ ((lane >> 1) & 3)) << 4)) =
+                make_uint4(pack_bf16x2(v[8 * k], v[8 * k + 1]), pack_bf16x2(v[8 * k + 2], v[8 * k + 3]),
+                           pack_bf16x2(v[8 * k + 4], v[8 * k + 5]), pack_bf16x2(v[8 * k + 6], v[8 * k + 7]));
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) {
+            tma_store_3d(&tm_o, stg, 32 * c, row - lane, w.bh);
+            bulk_commit_group();
           }
+        } else if (row < p.M) {
+          float4* dst = reinterpret_cast<float4*>(
+              p.o_part + (static_cast<size_t>(w.split) * p.BH * p.M + at) * D + 32 * c);
+#pragma unroll
+          for (int k = 0; k < 8; ++k) dst[k] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
         }
         __syncwarp();
       }
@@ -643,6 +673,8 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
       }
       __syncwarp();
     }
+    if (lane == 0) bulk_wait_read<0>();  // the boxes are read before shared memory goes
+    __syncwarp();
     pdl_trigger();  // the next kernel (the split combine) may be scheduled now
   }
 
@@ -657,7 +689,7 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
 
 template <int D, int DM>
 cudaError_t launch(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv,
-                   const XattnTcParams& p, int dev, int sms, cudaStream_t s) {
+                   const CUtensorMap& to, const XattnTcParams& p, int dev, int sms, cudaStream_t s) {
   using L = Layout<D, DM>;
   static OncePerDevice prepared;
   const cudaError_t e = prepared(dev, [] {
@@ -673,16 +705,16 @@ cudaError_t launch(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorM
   cudaLaunchConfig_t cfg;
   cudaLaunchAttribute attr;
   pdl_config(cfg, attr, dim3(p.items < sms ? p.items : sms), dim3(L::THREADS), L::BYTES, s);
-  return cudaLaunchKernelEx(&cfg, xattn_fwd_kernel<D, DM>, tq, tk, tv, p);
+  return cudaLaunchKernelEx(&cfg, xattn_fwd_kernel<D, DM>, tq, tk, tv, to, p);
 }
 
 }  // namespace
 
 cudaError_t launch_xattn_tc(int d, int dm, const CUtensorMap& tq, const CUtensorMap& tk,
-                            const CUtensorMap& tv, const XattnTcParams& p, int dev, int sms, cudaStream_t s) {
-  if (d == 64) return launch<64, 64>(tq, tk, tv, p, dev, sms, s);
-  if (dm == 80) return launch<128, 80>(tq, tk, tv, p, dev, sms, s);
-  return launch<128, 128>(tq, tk, tv, p, dev, sms, s);
+                            const CUtensorMap& tv, const CUtensorMap& to, const XattnTcParams& p, int dev, int sms, cudaStream_t s) {
+  if (d == 64) return launch<64, 64>(tq, tk, tv, to, p, dev, sms, s);
+  if (dm == 80) return launch<128, 80>(tq, tk, tv, to, p, dev, sms, s);
+  return launch<128, 128>(tq, tk, tv, to, p, dev, sms, s);
 }
 
 }  // namespace mw
