@@ -305,14 +305,7 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
         if (!(ok = mbar_wait(k_empty, (sw & 1) ^ 1, ctl))) break;
         load_tile(sK, &tm_k, raw ? k_raw : k_full);
         ++sw;
-        for (int j = 1; ok && j < w.n_q; ++j) {
-          if (j + 1 < w.n_q)  // into L2 (few key tiles: every load would wait for HBM)
-            for (int r = 0; r < L::REG; ++r) {
-              tma_prefetch_3d(&tm_q, 64 * r, w.query_row(j + 1), w.bh);
-              tma_prefetch_3d(&tm_do, 64 * r, w.query_row(j + 1), w.bh);
-            }
-          ok = load_q(w.query_row(j)) && load_do(w.query_row(j));
-        }
+        for (int j = 1; ok && j < w.n_q; ++j) ok = load_q(w.query_row(j)) && load_do(w.query_row(j));
       }
       if (*abort_flag || !ok) {
         // let every copy this CTA started land before shared memory goes away

@@ -228,9 +228,8 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
   // tell the compiler, which then works in uniform registers).
   int turn = 0;
   Block w;
-  auto next_block = [&]() {
+  auto read_block = [&]() {  // (announced)
     const int slot = turn % L::SLOTS;
-    if (!warp_wait(&b_full[slot], (turn / L::SLOTS) & 1, ctl)) return false;
     ++turn;
     const int4 a = slots[2 * slot], b = slots[2 * slot + 1];
     w.bh = __shfl_sync(0xffffffffu, a.x, 0);
@@ -241,6 +240,9 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
     w.len = __shfl_sync(0xffffffffu, b.y, 0);
     if (lane == 0) mbar_arrive(&b_empty[slot]);
     return w.bh >= 0;
+  };
+  auto next_block = [&]() {
+    return warp_wait(&b_full[turn % L::SLOTS], (turn / L::SLOTS) & 1, ctl) && read_block();
   };
   // the next one that has keys
   auto next_keys = [&]() {
@@ -360,16 +362,27 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
     w.n = 0;
     bool ok = true, more = true;
     // In turn: S of the next tile, and PV of this one, of which S is there.  Where P
-    // leaves S free in time, the next S goes between the halves of the PV.
+    // leaves S free in time, the next S goes between the halves of the PV.  A block that
+    // is not announced yet is waited for only after this PV (a turn without one): blocks
+    // without keys may lie in between, which the softmax warps pass only once they have
+    // the O that this PV makes.
     while (ok && more) {
       const int st = (nk + NS - 1) % NS;
       const uint32_t ph = ((nk - 1) / NS) & 1;
       const bool any = i >= 0, first_tile = i == 0, last_tile = i + 1 == w.n;
-      if (last_tile) {
+      bool known = true;
+      if (!last_tile) {
+        ++i;
+      } else if (!any) {
         more = next_keys();
         i = 0;
       } else {
-        ++i;
+        w.n = 0;
+        while (more && w.n == 0 && known) {
+          known = __all_sync(0xffffffffu, mbar_try_wait(&b_full[turn % L::SLOTS], (turn / L::SLOTS) & 1));
+          if (known) more = read_block();
+        }
+        i = known ? 0 : -1;
       }
       const int st1 = nk % NS;
       const int qb1 = (i == 0 ? nq : nq - 1) % NQ;
@@ -401,7 +414,7 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
           tc_fence_after();
           issue_pv(t, st, !first_tile, 0);
         }
-        if (L::SPLIT_P && more && !(ok = next_s(t))) break;
+        if (L::SPLIT_P && more && known && !(ok = next_s(t))) break;
         if (have[u]) {
           if (!(ok = warp_wait(&p_full[t], done[u] & 1, ctl))) break;
           tc_fence_after();
@@ -409,15 +422,15 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
           ++done[u];
           if (L::SPLIT_P || last_tile) umma_commit(&pv_done[t]);
         }
-        if (!L::SPLIT_P && more && !(ok = next_s(t))) break;
+        if (!L::SPLIT_P && more && known && !(ok = next_s(t))) break;
       }
       if (!ok) break;
       if (any) umma_commit(&v_empty[st]);
-      if (more) {
+#pragma unroll
+      for (int u = 0; u < NT; ++u) have[u] = more && known && w.present(t0 + u, p.M);
+      if (more && known) {
         umma_commit(&k_empty[st1]);
         if (i + 1 == w.n) umma_commit(&q_empty[qb1]);
-#pragma unroll
-        for (int u = 0; u < NT; ++u) have[u] = w.present(t0 + u, p.M);
         nq += i == 0;
         ++nk;
       }

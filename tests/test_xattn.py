@@ -258,6 +258,32 @@ def test_no_rows_and_no_states(mw, M, S):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 72, 128])
+@pytest.mark.parametrize("lens", [[200, 0, 130], [0, 0, 40], [129, 0, 0], [1, 0, 300]])
+def test_long_runs_of_blocks_without_states(mw, d, lens):
+    """A dropped sample between others, with more blocks than the launch has CTAs times
+    the blocks announced ahead: the result of every sample alone."""
+    B, H, M, S = 3, 6, 256 * 152 + 77, 300
+    g = torch.Generator("cuda").manual_seed(1)
+    q, do = (torch.randn(B, H, M, d, device="cuda", generator=g).to(torch.bfloat16) for _ in range(2))
+    k, v = (torch.randn(B, H, S, d, device="cuda", generator=g).to(torch.bfloat16) for _ in range(2))
+    kv_len = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    o, lse = mw.mw_xattn_fwd(q, k, v, kv_len)
+    dq, dk, dv = mw.mw_xattn_bwd(q, k, v, o, lse, do, kv_len)
+    torch.cuda.synchronize()
+    assert mw.mw_device_status() == OK
+    for b, n in enumerate(lens):
+        one = [t[b:b + 1] for t in (q, k[:, :, :n].contiguous(), v[:, :, :n].contiguous())]
+        ob, lb = mw.mw_xattn_fwd(*one)
+        assert torch.equal(o[b:b + 1], ob) and torch.equal(lse[b:b + 1], lb)
+        grads = mw.mw_xattn_bwd(*one, ob, lb, do[b:b + 1])
+        for got, ref in zip((dq[b:b + 1], dk[b:b + 1], dv[b:b + 1]), grads):
+            rows = ref.shape[2]
+            assert rel(got[:, :, :rows], ref.double().cpu()) <= 2e-3  # the order of fp32 sums
+            assert torch.count_nonzero(got[:, :, rows:]) == 0
+
+
+@pytest.mark.gpu
 def test_autograd_and_shared_heads(mw):
     """The gradients of shared heads are the sums over the query heads that share
     them: the same as those of the heads repeated, added up."""
