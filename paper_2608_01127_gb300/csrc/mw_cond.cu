@@ -34,9 +34,6 @@ mw_status xattn_sizes(XattnSizes* out, int B, int H, int Hkv, int M, int S, int 
   return MW_OK;
 }
 
-// Rows of a head up to which the forward runs on CUDA cores.
-constexpr int kFewRows = 8;
-
 // Key ranges of the forward on tensor cores: enough that the blocks fill the SMs,
 // against the cost of a range (about three key tiles' time).
 int xattn_splits(int BH, int rows, int S) {
@@ -56,7 +53,7 @@ int xattn_splits(int BH, int rows, int S) {
 }
 
 size_t xattn_ws(const XattnSizes& z, int S, int d) {
-  if (z.rows <= kFewRows) return 0;
+  if (z.rows <= kXattnFewRows) return 0;
   const int splits = xattn_splits(z.BH, z.rows, S);
   if (splits == 1) return 0;
   const size_t rows = static_cast<size_t>(splits) * z.BH * z.rows;
@@ -193,14 +190,17 @@ mw_status mw_xattn_fwd(const void* q, const void* k, const void* v, const int* k
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   DeviceScope scope(s);
   MW_TRY(scope.status());
-  if (z.rows > kFewRows && S > 0) {
+  if (z.rows > kXattnFewRows) {
     const int D = kernel_d(d);
     XattnTcParams p{};
     MW_TRY(status_ptr(scope.device(), &p.status));
     CUtensorMap tq, tk, tv, to;
     MW_TRY(make_map(&tq, q, z.rows, z.BH, d, "q"));
-    MW_TRY(make_map(&tk, k, S, z.BH, d, "k"));
-    MW_TRY(make_map(&tv, v, S, z.BH, d, "v"));
+    tk = tv = tq;  // (no states: never read)
+    if (S > 0) {
+      MW_TRY(make_map(&tk, k, S, z.BH, d, "k"));
+      MW_TRY(make_map(&tv, v, S, z.BH, d, "v"));
+    }
     MW_TRY(encode_rows_map(&to, o, z.rows, z.BH, d, true));
     p.kv_len = kv_len;
     p.o = static_cast<__nv_bfloat16*>(o);
@@ -242,8 +242,9 @@ mw_status mw_xattn_fwd(const void* q, const void* k, const void* v, const int* k
   p.M = z.rows;
   p.S = S;
   p.d = d;
+  p.sms = sm_count();
   p.scale_log2 = scale * 1.4426950408889634f;
-  return launch_status(launch_xattn_fwd(p, s), "cross attention forward launch");
+  return launch_status(launch_xattn_few(p, scope.device(), s), "cross attention forward launch");
 }
 
 size_t mw_xattn_bwd_workspace_size(int B, int H, int Hkv, int M, int S, int d) {

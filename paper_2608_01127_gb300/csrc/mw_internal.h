@@ -232,6 +232,7 @@ struct XattnParams {
   __nv_bfloat16* o;
   float* lse;          // nullable
   int BH, heads, M, S, d;
+  int sms;
   float scale_log2;
 };
 // Forward on tensor cores (mw_xattn_fwd.cu): blocks of kFwdBlockRows rows of one
@@ -255,8 +256,10 @@ struct XattnTcParams {
 cudaError_t launch_xattn_tc(int d, int dm, const CUtensorMap& tq, const CUtensorMap& tk,
                             const CUtensorMap& tv, const CUtensorMap& to, const XattnTcParams& p, int dev, int sms,
                             cudaStream_t s);
-// Forward of few rows a head on CUDA cores (mw_xattn.cu).
-cudaError_t launch_xattn_fwd(const XattnParams& p, cudaStream_t s);
+// Forward of at most kXattnFewRows rows a head (or of no states) on CUDA cores
+// (mw_xattn.cu).
+constexpr int kXattnFewRows = 8;
+cudaError_t launch_xattn_few(const XattnParams& p, int dev, cudaStream_t s);
 
 // Backward on tensor cores (mw_xattn_bwd.cu).
 struct XattnBwdParams {
