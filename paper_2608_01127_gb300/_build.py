@@ -28,7 +28,7 @@ TORCH_SOURCE = "mw_torch.cpp"
 TORCH_LIB_PATH = os.path.join(LIB_DIR, "_mw_torch.so")
 
 SOURCES = ["mw_abi.cu", "mw_fwd.cu", "mw_bwd.cu", "mw_commit.cu", "mw_qkv.cu", "mw_cond.cu",
-           "mw_xattn.cu", "mw_xattn_fwd.cu", "mw_xattn_bwd.cu", "mw_norm.cu"]
+           "mw_xattn_few.cu", "mw_xattn_fwd.cu", "mw_xattn_bwd.cu", "mw_norm.cu"]
 HEADERS = ["mw_ptx.cuh", "mw_internal.h", "mw_host.h"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 CFLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-Xcompiler", "-Wall",

@@ -230,10 +230,17 @@ mw_status mw_xattn_fwd(const void* q, const void* k, const void* v, const int* k
                            "combine kernel launch"));
     return ok();
   }
-  XattnParams p{};
+  XattnFewParams p{};
+  MW_TRY(status_ptr(scope.device(), &p.status));
+  CUtensorMap tk, tv;
+  if (S > 0) {
+    MW_TRY(make_map(&tk, k, S, z.BH, d, "k", kXattnFewKeys));
+    MW_TRY(make_map(&tv, v, S, z.BH, d, "v", kXattnFewKeys));
+  } else {  // never read
+    MW_TRY(make_map(&tk, q, z.rows, z.BH, d, "q"));
+    tv = tk;
+  }
   p.q = static_cast<const __nv_bfloat16*>(q);
-  p.k = static_cast<const __nv_bfloat16*>(k);
-  p.v = static_cast<const __nv_bfloat16*>(v);
   p.kv_len = kv_len;
   p.o = static_cast<__nv_bfloat16*>(o);
   p.lse = lse;
@@ -244,7 +251,9 @@ mw_status mw_xattn_fwd(const void* q, const void* k, const void* v, const int* k
   p.d = d;
   p.sms = sm_count();
   p.scale_log2 = scale * 1.4426950408889634f;
-  return launch_status(launch_xattn_few(p, scope.device(), s), "cross attention forward launch");
+  p.budget_ns = budget_ns();
+  return launch_status(launch_xattn_few(kernel_d(d), tk, tv, p, scope.device(), s),
+                       "cross attention forward launch");
 }
 
 size_t mw_xattn_bwd_workspace_size(int B, int H, int Hkv, int M, int S, int d) {

@@ -221,20 +221,9 @@ int norm_parts(long long rows_per_group, int groups, int sms);
 cudaError_t launch_norm_fwd(NormParams p, bool vec, int sms, cudaStream_t s);
 cudaError_t launch_norm_bwd(NormParams p, bool vec, int dev, cudaStream_t s);
 
-// Cross attention (mw_xattn.cu): BH heads of K and V [BH, S, d], each with M rows of
-// Q (those of all the query heads that share it, which lie one after another);
-// head bh belongs to sample bh / heads, whose first kv_len[...] keys count.
-struct XattnParams {
-  const __nv_bfloat16* q;
-  const __nv_bfloat16* k;
-  const __nv_bfloat16* v;
-  const int* kv_len;   // [BH / heads], nullable: all S
-  __nv_bfloat16* o;
-  float* lse;          // nullable
-  int BH, heads, M, S, d;
-  int sms;
-  float scale_log2;
-};
+// Cross attention: BH heads of K and V [BH, S, d], each with M rows of Q (those of all
+// the query heads that share it, which lie one after another); head bh belongs to
+// sample bh / heads, whose first kv_len[...] keys count (null: all S).
 // Forward on tensor cores (mw_xattn_fwd.cu): blocks of kFwdBlockRows rows of one
 // head against one of num_splits ranges of its key tiles.
 struct XattnTcParams {
@@ -256,10 +245,23 @@ struct XattnTcParams {
 cudaError_t launch_xattn_tc(int d, int dm, const CUtensorMap& tq, const CUtensorMap& tk,
                             const CUtensorMap& tv, const CUtensorMap& to, const XattnTcParams& p, int dev, int sms,
                             cudaStream_t s);
-// Forward of at most kXattnFewRows rows a head (or of no states) on CUDA cores
-// (mw_xattn.cu).
-constexpr int kXattnFewRows = 8;
-cudaError_t launch_xattn_few(const XattnParams& p, int dev, cudaStream_t s);
+// Forward of at most kXattnFewRows rows a head (mw_xattn_few.cu).
+constexpr int kXattnFewRows = 16;
+constexpr int kXattnFewKeys = 64;  // of a copy: the rows of tk's and tv's boxes
+struct XattnFewParams {
+  const __nv_bfloat16* q;
+  const int* kv_len;
+  __nv_bfloat16* o;
+  float* lse;          // nullable
+  int BH, heads, M, S, d;
+  int sms;
+  float scale_log2;
+  unsigned* status;
+  unsigned long long budget_ns;
+};
+// d: tile width (64 or 128); without states any maps
+cudaError_t launch_xattn_few(int d, const CUtensorMap& tk, const CUtensorMap& tv, const XattnFewParams& p, int dev,
+                             cudaStream_t s);
 
 // Backward on tensor cores (mw_xattn_bwd.cu).
 struct XattnBwdParams {
