@@ -170,7 +170,8 @@ def _load_native(lib: ctypes.CDLL) -> None:
         "mw_bca_fwd", "mw_bca_bwd", "mw_bca_bwd_workspace_size", "mw_bca_cache_workspace_size",
         "mw_bca_cache_fwd_rope", "mw_bca_cache_step", "mw_qkv_rope_split",
         "mw_xattn_workspace_size", "mw_xattn_fwd", "mw_xattn_bwd_workspace_size", "mw_xattn_bwd",
-        "mw_layernorm_fwd", "mw_layernorm_bwd_workspace_size", "mw_layernorm_bwd")))
+        "mw_layernorm_fwd", "mw_layernorm_bwd_workspace_size", "mw_layernorm_bwd",
+        "mw_last_error")), MWError)
     _native = module
 
 
@@ -760,6 +761,15 @@ class CrossAttention(torch.autograd.Function):
     """Autograd wrapper: O = cross attention(q, k, v) over the first kv_len states of
     each sample (None: all)."""
 
+    @classmethod
+    def apply(cls, q, k, v, kv_len: Optional[torch.Tensor] = None,
+              scale: Optional[float] = None):
+        if _native is not None:
+            r = _native.xattn_apply(q, k, v, kv_len, scale)
+            if r is not None:
+                return _check(r) if type(r) is int else r
+        return super().apply(q, k, v, kv_len, scale)
+
     @staticmethod
     def forward(ctx, q, k, v, kv_len: Optional[torch.Tensor] = None,
                 scale: Optional[float] = None):
@@ -778,6 +788,16 @@ class CrossAttention(torch.autograd.Function):
 class LayerNorm(torch.autograd.Function):
     """Autograd wrapper: y = layer norm(x) * weight + bias, weight and bias [C], one of
     each for every group of rows ([groups, C]), or None."""
+
+    @classmethod
+    def apply(cls, x, weight: Optional[torch.Tensor] = None,
+              bias: Optional[torch.Tensor] = None, eps: float = 1e-5,
+              out_dtype: Optional[torch.dtype] = None):
+        if _native is not None:
+            r = _native.norm_apply(x, weight, bias, eps, out_dtype)
+            if r is not None:
+                return _check(r) if type(r) is int else r
+        return super().apply(x, weight, bias, eps, out_dtype)
 
     @staticmethod
     def forward(ctx, x, weight: Optional[torch.Tensor] = None,

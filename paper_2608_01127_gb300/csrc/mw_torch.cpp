@@ -21,9 +21,13 @@
 #include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
+#include <ATen/core/grad_mode.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
+#include <torch/csrc/autograd/function.h>
+#include <torch/csrc/autograd/functions/utils.h>
 #include <torch/csrc/autograd/python_variable.h>
+#include <torch/csrc/autograd/saved_variable.h>
 
 #include <array>
 #include <climits>
@@ -49,6 +53,8 @@ decltype(&mw_xattn_bwd) p_xattn_bwd = nullptr;
 decltype(&mw_layernorm_fwd) p_norm = nullptr;
 decltype(&mw_layernorm_bwd_workspace_size) p_norm_bwd_ws = nullptr;
 decltype(&mw_layernorm_bwd) p_norm_bwd = nullptr;
+decltype(&mw_last_error) p_last_error = nullptr;
+PyObject* error_type = nullptr;  // MWError(code, message)
 
 // A tensor this module may look into: exactly a torch.Tensor or Parameter,
 // strided, with storage of its own (no fake, batched or other wrapper).
@@ -184,9 +190,9 @@ auto call(F&& f) {
 }
 
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  constexpr int kEntries = 14;
-  if (n != kEntries) {
-    PyErr_SetString(PyExc_TypeError, "bind takes 14 addresses");
+  constexpr int kEntries = 15;
+  if (n != kEntries + 1) {
+    PyErr_SetString(PyExc_TypeError, "bind takes 15 addresses and the error type");
     return nullptr;
   }
   void* p[kEntries];
@@ -211,6 +217,9 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
   p_norm = reinterpret_cast<decltype(p_norm)>(p[11]);
   p_norm_bwd_ws = reinterpret_cast<decltype(p_norm_bwd_ws)>(p[12]);
   p_norm_bwd = reinterpret_cast<decltype(p_norm_bwd)>(p[13]);
+  p_last_error = reinterpret_cast<decltype(p_last_error)>(p[14]);
+  Py_XDECREF(error_type);
+  error_type = Py_NewRef(a[kEntries]);
   Py_RETURN_NONE;
 }
 
@@ -431,95 +440,114 @@ struct States {
   const int* lens() const { return len ? static_cast<const int*>(len->const_data_ptr()) : nullptr; }
 };
 
+// A cross attention call: its tensors and sizes, and the results of its forward.
+struct Xattn {
+  const at::Tensor* q = nullptr;
+  States st;
+  c10::DeviceIndex dev = -1;
+  float scale = 0.f;
+  at::Tensor o, lse;
+  bool read(PyObject* qo, PyObject* ko, PyObject* vo, PyObject* lo, PyObject* so) {
+    q = bf16(qo, 4);
+    return st.read(q, ko, vo, lo) && one_device({q, st.k, st.v, st.len}, &dev) &&
+           softmax_scale(so, q->size(3), &scale);
+  }
+  // false: outputs that are not real tensors
+  bool forward(bool need_lse, mw_status* s) {
+    const Shape sh = shape(*q);
+    const at::TensorOptions options = q->options();
+    const int B = static_cast<int>(sh[0]), H = static_cast<int>(sh[1]), M = static_cast<int>(sh[2]);
+    const int Hkv = static_cast<int>(st.k->size(1)), S = static_cast<int>(st.k->size(2));
+    const int d = static_cast<int>(sh[3]);
+    const size_t bytes = p_xattn_ws(B, H, Hkv, M, S, d);
+    const void *pq = q->const_data_ptr(), *pk = st.k->const_data_ptr(), *pv = st.v->const_data_ptr();
+    const int* lens = st.lens();
+    return call([&] {
+      at::Tensor ws;
+      o = at::empty(sh, options);
+      if (need_lse) lse = rows_f32(sh, options);
+      if (bytes) ws = scratch(bytes, options);
+      if (!is_real(o) || (need_lse && !is_real(lse)) || (bytes && !is_real(ws))) return false;
+      *s = p_xattn(pq, pk, pv, lens, o.mutable_data_ptr(),
+                   need_lse ? static_cast<float*>(lse.mutable_data_ptr()) : nullptr,
+                   bytes ? ws.mutable_data_ptr() : nullptr, bytes, B, H, Hkv, M, S, d, scale,
+                   c10::cuda::getCurrentCUDAStream(dev).stream());
+      return true;
+    });
+  }
+};
+
 // xattn_fwd(q, k, v, kv_len, scale, need_lse, workspace) -> (o, lse or None)
 PyObject* xattn_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
-  if (n != 7 || !p_xattn || a[6] != Py_None) return none();
-  const at::Tensor* q = bf16(a[0], 4);
-  States st;
-  c10::DeviceIndex dev;
-  float scale;
-  if (!st.read(q, a[1], a[2], a[3]) || !one_device({q, st.k, st.v, st.len}, &dev) ||
-      !softmax_scale(a[4], q->size(3), &scale) || !PyBool_Check(a[5]))
+  Xattn x;
+  if (n != 7 || !p_xattn || a[6] != Py_None || !PyBool_Check(a[5]) || !x.read(a[0], a[1], a[2], a[3], a[4]))
     return none();
-  const Shape sh = shape(*q);
-  const at::TensorOptions options = q->options();
-  const int B = static_cast<int>(sh[0]), H = static_cast<int>(sh[1]), M = static_cast<int>(sh[2]);
-  const int Hkv = static_cast<int>(st.k->size(1)), S = static_cast<int>(st.k->size(2));
-  const int d = static_cast<int>(sh[3]);
-  const size_t bytes = p_xattn_ws(B, H, Hkv, M, S, d);
-  const void *pq = q->const_data_ptr(), *pk = st.k->const_data_ptr(), *pv = st.v->const_data_ptr();
-  const int* lens = st.lens();
-  const bool need_lse = a[5] == Py_True;
-  at::Tensor o, lse, ws;
   mw_status s = MW_OK;
-  const bool real = call([&] {
-    o = at::empty(sh, options);
-    if (need_lse) lse = rows_f32(sh, options);
-    if (bytes) ws = scratch(bytes, options);
-    if (!is_real(o) || (need_lse && !is_real(lse)) || (bytes && !is_real(ws))) return false;
-    s = p_xattn(pq, pk, pv, lens, o.mutable_data_ptr(),
-                need_lse ? static_cast<float*>(lse.mutable_data_ptr()) : nullptr,
-                bytes ? ws.mutable_data_ptr() : nullptr, bytes, B, H, Hkv, M, S, d, scale,
-                c10::cuda::getCurrentCUDAStream(dev).stream());
-    return true;
-  });
-  if (!real) return none();
+  if (!x.forward(a[5] == Py_True, &s)) return none();
   if (s != MW_OK) return PyLong_FromLong(s);
-  return result({&o, &lse});
+  return result({&x.o, &x.lse});
   END_HANDLE_TH_ERRORS
+}
+
+// The gradients of a cross attention into new tensors; false: not real ones.  Called
+// without the interpreter lock.
+bool xattn_gradients(const at::Tensor& q, const at::Tensor& k, const at::Tensor& v, const int* lens,
+                     const at::Tensor& o, const at::Tensor& lse, const at::Tensor& dout, float scale,
+                     c10::DeviceIndex dev, std::array<at::Tensor, 3>* grads, mw_status* s) {
+  const Shape sh = shape(q), ks = shape(k);
+  const at::TensorOptions options = q.options();
+  const int B = static_cast<int>(sh[0]), H = static_cast<int>(sh[1]), M = static_cast<int>(sh[2]);
+  const int Hkv = static_cast<int>(ks[1]), S = static_cast<int>(ks[2]), d = static_cast<int>(sh[3]);
+  const size_t bytes = p_xattn_bwd_ws(B, H, Hkv, M, S, d);
+  at::Tensor ws;
+  if (bytes) ws = scratch(bytes, options);
+  (*grads)[0] = at::empty(sh, options);
+  (*grads)[1] = at::empty(ks, options);
+  (*grads)[2] = at::empty(ks, options);
+  if (bytes && !is_real(ws)) return false;
+  for (const at::Tensor& t : *grads)
+    if (!is_real(t)) return false;
+  *s = p_xattn_bwd(q.const_data_ptr(), k.const_data_ptr(), v.const_data_ptr(), lens, o.const_data_ptr(),
+                   static_cast<const float*>(lse.const_data_ptr()), dout.const_data_ptr(),
+                   (*grads)[0].mutable_data_ptr(), (*grads)[1].mutable_data_ptr(),
+                   (*grads)[2].mutable_data_ptr(), bytes ? ws.mutable_data_ptr() : nullptr, bytes, B, H,
+                   Hkv, M, S, d, scale, c10::cuda::getCurrentCUDAStream(dev).stream());
+  return true;
 }
 
 // xattn_bwd(q, k, v, o, lse, dout, kv_len, scale) -> (dq, dk, dv)
 PyObject* xattn_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   if (n != 8 || !p_xattn_bwd) return none();
-  const at::Tensor *q = bf16(a[0], 4), *o = bf16(a[3], 4), *lse = tensor(a[4]), *dout = bf16(a[5], 4);
-  States st;
+  Xattn x;
+  const at::Tensor *o = bf16(a[3], 4), *lse = tensor(a[4]), *dout = bf16(a[5], 4);
   c10::DeviceIndex dev;
-  float scale;
-  if (!st.read(q, a[1], a[2], a[6]) || !o || !lse || !dout || o->sizes() != q->sizes() ||
-      dout->sizes() != q->sizes() || lse->scalar_type() != at::kFloat ||
-      lse->sizes() != q->sizes().slice(0, 3) ||
-      !one_device({q, st.k, st.v, st.len, o, lse, dout}, &dev) ||
-      !softmax_scale(a[7], q->size(3), &scale))
+  if (!x.read(a[0], a[1], a[2], a[6], a[7]) || !o || !lse || !dout || o->sizes() != x.q->sizes() ||
+      dout->sizes() != x.q->sizes() || lse->scalar_type() != at::kFloat ||
+      lse->sizes() != x.q->sizes().slice(0, 3) || !one_device({x.q, o, lse, dout}, &dev))
     return none();
-  const Shape sh = shape(*q), ks = shape(*st.k);
-  const at::TensorOptions options = q->options();
-  const int B = static_cast<int>(sh[0]), H = static_cast<int>(sh[1]), M = static_cast<int>(sh[2]);
-  const int Hkv = static_cast<int>(ks[1]), S = static_cast<int>(ks[2]), d = static_cast<int>(sh[3]);
-  const size_t bytes = p_xattn_bwd_ws(B, H, Hkv, M, S, d);
-  const void *pq = q->const_data_ptr(), *pk = st.k->const_data_ptr(), *pv = st.v->const_data_ptr();
-  const void *po = o->const_data_ptr(), *pdo = dout->const_data_ptr();
-  const float* pl = static_cast<const float*>(lse->const_data_ptr());
-  const int* lens = st.lens();
-  at::Tensor ws, dq, dk, dv;
+  std::array<at::Tensor, 3> g;
   mw_status s = MW_OK;
-  const bool real = call([&] {
-    if (bytes) ws = scratch(bytes, options);
-    dq = at::empty(sh, options);
-    dk = at::empty(ks, options);
-    dv = at::empty(ks, options);
-    if ((bytes && !is_real(ws)) || !is_real(dq) || !is_real(dk) || !is_real(dv)) return false;
-    s = p_xattn_bwd(pq, pk, pv, lens, po, pl, pdo, dq.mutable_data_ptr(), dk.mutable_data_ptr(),
-                    dv.mutable_data_ptr(), bytes ? ws.mutable_data_ptr() : nullptr, bytes, B, H,
-                    Hkv, M, S, d, scale, c10::cuda::getCurrentCUDAStream(dev).stream());
-    return true;
-  });
+  const int* lens = x.st.lens();
+  const bool real =
+      call([&] { return xattn_gradients(*x.q, *x.st.k, *x.st.v, lens, *o, *lse, *dout, x.scale, dev, &g, &s); });
   if (!real) return none();
   if (s != MW_OK) return PyLong_FromLong(s);
-  return result({&dq, &dk, &dv});
+  return result({&g[0], &g[1], &g[2]});
   END_HANDLE_TH_ERRORS
 }
 
 // Type codes of the layer norm's arrays (-1: another type).
 int norm_type(at::ScalarType t) { return t == at::kBFloat16 ? MW_BF16 : t == at::kFloat ? MW_F32 : -1; }
 
-// The arrays of a layer norm call.
+// A layer norm call: its tensors and sizes, and the results of its forward.
 struct Norm {
   const at::Tensor *x = nullptr, *w = nullptr, *b = nullptr;
   int xt = -1, pt = MW_F32, C = 0, groups = 1;
   int64_t rows = 0;
+  c10::DeviceIndex dev = -1;
+  at::Tensor y, mean, rstd;
   bool read(PyObject* xo, PyObject* wo, PyObject* bo) {
     x = tensor(xo);
     if (!x || x->dim() < 1 || (xt = norm_type(x->scalar_type())) < 0) return false;
@@ -538,51 +566,88 @@ struct Norm {
       groups = static_cast<int>(g);
     }
     if (w && b && (w->scalar_type() != b->scalar_type() || w->sizes() != b->sizes())) return false;
-    return rows % groups == 0;
+    return rows % groups == 0 && one_device({x, w, b}, &dev);
+  }
+  bool out_type(PyObject* o, int* yt) const {
+    *yt = xt;
+    if (o == Py_None) return true;
+    if (!THPDtype_Check(o)) return false;
+    *yt = norm_type(reinterpret_cast<THPDtype*>(o)->scalar_type);
+    return *yt >= 0;
+  }
+  bool forward(float eps, int yt, bool stats, mw_status* s) {
+    const at::TensorOptions options = x->options();
+    const std::vector<int64_t> full = x->sizes().vec();
+    const at::IntArrayRef lead(full.data(), full.size() - 1);
+    const void* px = x->const_data_ptr();
+    const void *pw = w ? w->const_data_ptr() : nullptr, *pb = b ? b->const_data_ptr() : nullptr;
+    return call([&] {
+      y = at::empty(full, options.dtype(yt == MW_F32 ? at::kFloat : at::kBFloat16));
+      if (stats) {
+        mean = at::empty(lead, options.dtype(at::kFloat));
+        rstd = at::empty(lead, options.dtype(at::kFloat));
+      }
+      if (!is_real(y) || (stats && (!is_real(mean) || !is_real(rstd)))) return false;
+      *s = p_norm(px, pw, pb, y.mutable_data_ptr(),
+                  stats ? static_cast<float*>(mean.mutable_data_ptr()) : nullptr,
+                  stats ? static_cast<float*>(rstd.mutable_data_ptr()) : nullptr, rows, C, groups, eps, xt,
+                  yt, pt, c10::cuda::getCurrentCUDAStream(dev).stream());
+      return true;
+    });
   }
 };
 
 // norm_fwd(x, weight, bias, eps, out_dtype, need_stats) -> (y, mean or None, rstd or None)
 PyObject* norm_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
-  if (n != 6 || !p_norm) return none();
   Norm t;
-  c10::DeviceIndex dev;
   float eps;
-  if (!t.read(a[0], a[1], a[2]) || !one_device({t.x, t.w, t.b}, &dev) || !real_number(a[3], &eps) ||
+  int yt;
+  if (n != 6 || !p_norm || !t.read(a[0], a[1], a[2]) || !real_number(a[3], &eps) || !t.out_type(a[4], &yt) ||
       !PyBool_Check(a[5]))
     return none();
-  int yt = t.xt;
-  if (a[4] != Py_None) {
-    if (!THPDtype_Check(a[4])) return none();
-    yt = norm_type(reinterpret_cast<THPDtype*>(a[4])->scalar_type);
-    if (yt < 0) return none();
-  }
-  const at::TensorOptions options = t.x->options();
-  const std::vector<int64_t> full(t.x->sizes().begin(), t.x->sizes().end());
-  const at::IntArrayRef lead(full.data(), full.size() - 1);
-  const void* px = t.x->const_data_ptr();
-  const void *pw = t.w ? t.w->const_data_ptr() : nullptr, *pb = t.b ? t.b->const_data_ptr() : nullptr;
-  const bool stats = a[5] == Py_True;
-  at::Tensor y, mean, rstd;
   mw_status s = MW_OK;
-  const bool real = call([&] {
-    y = at::empty(full, options.dtype(yt == MW_F32 ? at::kFloat : at::kBFloat16));
-    if (stats) {
-      mean = at::empty(lead, options.dtype(at::kFloat));
-      rstd = at::empty(lead, options.dtype(at::kFloat));
-    }
-    if (!is_real(y) || (stats && (!is_real(mean) || !is_real(rstd)))) return false;
-    s = p_norm(px, pw, pb, y.mutable_data_ptr(),
-               stats ? static_cast<float*>(mean.mutable_data_ptr()) : nullptr,
-               stats ? static_cast<float*>(rstd.mutable_data_ptr()) : nullptr, t.rows, t.C, t.groups,
-               eps, t.xt, yt, t.pt, c10::cuda::getCurrentCUDAStream(dev).stream());
-    return true;
-  });
-  if (!real) return none();
+  if (!t.forward(eps, yt, a[5] == Py_True, &s)) return none();
   if (s != MW_OK) return PyLong_FromLong(s);
-  return result({&y, &mean, &rstd});
+  return result({&t.y, &t.mean, &t.rstd});
   END_HANDLE_TH_ERRORS
+}
+
+// The gradients of a layer norm into new tensors (of x, weight, bias; the latter two
+// where `w` and `b` say so); false: not real ones.  Called without the interpreter lock.
+struct NormSizes {
+  int64_t rows;
+  int C, groups, xt, yt, pt;
+  bool w, b;
+  std::vector<int64_t> params;  // shape of weight and bias
+};
+bool norm_gradients(const at::Tensor& dy, const at::Tensor& x, const at::Tensor& mean, const at::Tensor& rstd,
+                    const void* weight, const NormSizes& z, c10::DeviceIndex dev,
+                    std::array<at::Tensor, 3>* grads, mw_status* s) {
+  const size_t bytes = z.w || z.b ? p_norm_bwd_ws(z.rows, z.C, z.groups) : 0;
+  const at::TensorOptions options = x.options();
+  const at::TensorOptions poptions = options.dtype(z.pt == MW_F32 ? at::kFloat : at::kBFloat16);
+  at::Tensor ws;
+  if (bytes) ws = scratch(bytes, options);
+  (*grads)[0] = at::empty(x.sizes(), options);
+  if (z.w) (*grads)[1] = at::empty(z.params, poptions);
+  if (z.b) (*grads)[2] = at::empty(z.params, poptions);
+  if (bytes && !is_real(ws)) return false;
+  for (const at::Tensor& t : *grads)
+    if (t.defined() && !is_real(t)) return false;
+  *s = p_norm_bwd(dy.const_data_ptr(), x.const_data_ptr(), static_cast<const float*>(mean.const_data_ptr()),
+                  static_cast<const float*>(rstd.const_data_ptr()), weight, (*grads)[0].mutable_data_ptr(),
+                  z.w ? (*grads)[1].mutable_data_ptr() : nullptr,
+                  z.b ? (*grads)[2].mutable_data_ptr() : nullptr, bytes ? ws.mutable_data_ptr() : nullptr,
+                  bytes, z.rows, z.C, z.groups, z.xt, z.yt, z.pt,
+                  c10::cuda::getCurrentCUDAStream(dev).stream());
+  return true;
+}
+
+NormSizes norm_sizes(const Norm& t, int yt) {
+  const at::Tensor* some = t.w ? t.w : t.b;
+  return {t.rows, t.C, t.groups, t.xt, yt, t.pt, t.w != nullptr, t.b != nullptr,
+          some ? some->sizes().vec() : std::vector<int64_t>()};
 }
 
 // norm_bwd(dy, x, mean, rstd, weight, bias) -> (dx, dweight or None, dbias or None)
@@ -593,41 +658,175 @@ PyObject* norm_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const at::Tensor *dy = tensor(a[0]), *mean = tensor(a[2]), *rstd = tensor(a[3]);
   c10::DeviceIndex dev;
   if (!t.read(a[1], a[4], a[5]) || !dy || !mean || !rstd || dy->sizes() != t.x->sizes() ||
-      !one_device({t.x, t.w, t.b, dy, mean, rstd}, &dev))
+      !one_device({t.x, dy, mean, rstd}, &dev))
     return none();
   const int yt = norm_type(dy->scalar_type());
   const at::IntArrayRef lead = t.x->sizes().slice(0, t.x->dim() - 1);
   if (yt < 0 || mean->scalar_type() != at::kFloat || rstd->scalar_type() != at::kFloat ||
       mean->sizes() != lead || rstd->sizes() != lead)
     return none();
-  const size_t bytes = t.w || t.b ? p_norm_bwd_ws(t.rows, t.C, t.groups) : 0;
-  const at::TensorOptions options = t.x->options();
-  const std::vector<int64_t> full(t.x->sizes().begin(), t.x->sizes().end());
-  const at::Tensor* some = t.w ? t.w : t.b;
-  const std::vector<int64_t> ps = some ? some->sizes().vec() : std::vector<int64_t>();
-  const at::TensorOptions poptions = some ? some->options() : options;
-  const void *px = t.x->const_data_ptr(), *pdy = dy->const_data_ptr();
+  const NormSizes z = norm_sizes(t, yt);
   const void* pw = t.w ? t.w->const_data_ptr() : nullptr;
-  const float *pm = static_cast<const float*>(mean->const_data_ptr()),
-              *pr = static_cast<const float*>(rstd->const_data_ptr());
-  at::Tensor ws, dx, dw, db;
+  std::array<at::Tensor, 3> g;
   mw_status s = MW_OK;
-  const bool real = call([&] {
-    if (bytes) ws = scratch(bytes, options);
-    dx = at::empty(full, options);
-    if (t.w) dw = at::empty(ps, poptions);
-    if (t.b) db = at::empty(ps, poptions);
-    for (const at::Tensor* r : {&ws, &dx, &dw, &db})
-      if (r->defined() && !is_real(*r)) return false;
-    s = p_norm_bwd(pdy, px, pm, pr, pw, dx.mutable_data_ptr(), t.w ? dw.mutable_data_ptr() : nullptr,
-                   t.b ? db.mutable_data_ptr() : nullptr, bytes ? ws.mutable_data_ptr() : nullptr, bytes,
-                   t.rows, t.C, t.groups, t.xt, yt, t.pt,
-                   c10::cuda::getCurrentCUDAStream(dev).stream());
-    return true;
-  });
-  if (!real) return none();
+  if (!call([&] { return norm_gradients(*dy, *t.x, *mean, *rstd, pw, z, dev, &g, &s); })) return none();
   if (s != MW_OK) return PyLong_FromLong(s);
-  return result({&dx, &dw, &db});
+  return result({&g[0], &g[1], &g[2]});
+  END_HANDLE_TH_ERRORS
+}
+
+// ---- the same with gradients: nodes of PyTorch's graph, whose backward pass runs
+// without the interpreter (a Python function's takes 60 us on the autograd thread,
+// more than the kernels of many layers).
+
+using torch::autograd::SavedVariable;
+using torch::autograd::variable_list;
+
+// A failed call on the autograd thread, as the Python binding raises it.
+[[noreturn]] void raise(mw_status s) {
+  const std::string what = p_last_error();
+  const PyGILState_STATE gil = PyGILState_Ensure();
+  PyObject* e = PyObject_CallFunction(error_type, "is", static_cast<int>(s), what.c_str());
+  if (e) PyErr_SetObject(reinterpret_cast<PyObject*>(Py_TYPE(e)), e);
+  Py_XDECREF(e);
+  python_error err;
+  err.persist();
+  PyGILState_Release(gil);
+  throw err;  // NOLINT
+}
+
+// The gradient of an output as the kernels read it.
+at::Tensor plain_gradient(const at::Tensor& g, const at::Tensor& like, at::ScalarType type) {
+  TORCH_CHECK(is_real(g) && g.scalar_type() == type && g.sizes() == like.sizes() && g.device() == like.device(),
+              "the gradient must be a plain CUDA tensor like the output");
+  return g.contiguous();
+}
+
+struct CrossAttentionBackward : public torch::autograd::Node {
+  SavedVariable q, k, v, o, lse, len;
+  float scale = 0.f;
+  c10::DeviceIndex dev = 0;
+
+  std::string name() const override { return "CrossAttentionBackward"; }
+  void release_variables() override {
+    for (SavedVariable* s : {&q, &k, &v, &o, &lse, &len}) s->reset_data();
+  }
+  variable_list apply(variable_list&& grads) override {
+    variable_list out(3);
+    if (!grads[0].defined()) return out;
+    const at::NoGradGuard no_grad;
+    const at::Tensor tq = q.unpack(), tk = k.unpack(), tv = v.unpack(), to = o.unpack(shared_from_this());
+    const at::Tensor tl = lse.unpack(), tn = len.unpack();
+    const at::Tensor dout = plain_gradient(grads[0], tq, at::kBFloat16);
+    for (const at::Tensor* t : {&tq, &tk, &tv, &to, &tl})
+      TORCH_CHECK(is_real(*t) && t->is_contiguous(), "a saved tensor is no plain CUDA tensor any more");
+    const int* lens = tn.defined() ? static_cast<const int*>(tn.const_data_ptr()) : nullptr;
+    std::array<at::Tensor, 3> g;
+    mw_status s = MW_OK;
+    TORCH_CHECK(xattn_gradients(tq, tk, tv, lens, to, tl, dout, scale, dev, &g, &s), "no plain CUDA tensors");
+    if (s != MW_OK) raise(s);
+    for (size_t i = 0; i < 3; ++i)
+      if (task_should_compute_output(i)) out[i] = g[i];
+    return out;
+  }
+};
+
+// A tensor with a forward-mode gradient, which only the Python function refuses.
+bool dual(const at::Tensor* t) { return t && t->_fw_grad(0).defined(); }
+
+// xattn_apply(q, k, v, kv_len, scale) -> o
+PyObject* xattn_apply(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Xattn x;
+  if (n != 5 || !p_xattn || !x.read(a[0], a[1], a[2], a[3], a[4]) || dual(x.q) || dual(x.st.k) || dual(x.st.v))
+    return none();
+  const at::Tensor &q = *x.q, &k = *x.st.k, &v = *x.st.v;
+  mw_status s = MW_OK;
+  const bool graph = torch::autograd::compute_requires_grad(q, k, v);
+  {
+    const at::NoGradGuard no_grad;
+    if (!x.forward(graph, &s)) return none();
+  }
+  if (s != MW_OK) return PyLong_FromLong(s);
+  if (graph) {
+    auto node = std::shared_ptr<CrossAttentionBackward>(new CrossAttentionBackward(), torch::autograd::deleteNode);
+    node->set_next_edges(torch::autograd::collect_next_edges(q, k, v));
+    node->q = SavedVariable(q, false);
+    node->k = SavedVariable(k, false);
+    node->v = SavedVariable(v, false);
+    node->lse = SavedVariable(x.lse, false);
+    if (x.st.len) node->len = SavedVariable(*x.st.len, false);
+    node->scale = x.scale;
+    node->dev = x.dev;
+    torch::autograd::set_history(x.o, node);
+    node->o = SavedVariable(x.o, true);
+  }
+  return THPVariable_Wrap(x.o);
+  END_HANDLE_TH_ERRORS
+}
+
+struct LayerNormBackward : public torch::autograd::Node {
+  SavedVariable x, weight, mean, rstd;
+  NormSizes z{};
+  c10::DeviceIndex dev = 0;
+
+  std::string name() const override { return "LayerNormBackward"; }
+  void release_variables() override {
+    for (SavedVariable* s : {&x, &weight, &mean, &rstd}) s->reset_data();
+  }
+  variable_list apply(variable_list&& grads) override {
+    variable_list out(3);
+    if (!grads[0].defined()) return out;
+    const at::NoGradGuard no_grad;
+    const at::Tensor tx = x.unpack(), tw = weight.unpack(), tm = mean.unpack(), tr = rstd.unpack();
+    const at::Tensor dy = plain_gradient(grads[0], tx, z.yt == MW_F32 ? at::kFloat : at::kBFloat16);
+    for (const at::Tensor* t : {&tx, &tm, &tr})
+      TORCH_CHECK(is_real(*t) && t->is_contiguous(), "a saved tensor is no plain CUDA tensor any more");
+    // (gradients of parameters that nothing asks for are left out)
+    NormSizes need = z;
+    need.w = z.w && task_should_compute_output(1);
+    need.b = z.b && task_should_compute_output(2);
+    std::array<at::Tensor, 3> g;
+    mw_status s = MW_OK;
+    TORCH_CHECK(norm_gradients(dy, tx, tm, tr, tw.defined() ? tw.const_data_ptr() : nullptr, need, dev, &g, &s),
+                "no plain CUDA tensors");
+    if (s != MW_OK) raise(s);
+    for (size_t i = 0; i < 3; ++i)
+      if (g[i].defined() && task_should_compute_output(i)) out[i] = g[i];
+    return out;
+  }
+};
+
+// norm_apply(x, weight, bias, eps, out_dtype) -> y
+PyObject* norm_apply(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Norm t;
+  float eps;
+  int yt;
+  if (n != 5 || !p_norm || !t.read(a[0], a[1], a[2]) || !real_number(a[3], &eps) || !t.out_type(a[4], &yt) ||
+      dual(t.x) || dual(t.w) || dual(t.b))
+    return none();
+  const at::Tensor none_given;
+  const at::Tensor &x = *t.x, &w = t.w ? *t.w : none_given, &b = t.b ? *t.b : none_given;
+  const bool graph = torch::autograd::compute_requires_grad(x, w, b);
+  mw_status s = MW_OK;
+  {
+    const at::NoGradGuard no_grad;
+    if (!t.forward(eps, yt, graph, &s)) return none();
+  }
+  if (s != MW_OK) return PyLong_FromLong(s);
+  if (graph) {
+    auto node = std::shared_ptr<LayerNormBackward>(new LayerNormBackward(), torch::autograd::deleteNode);
+    node->set_next_edges(torch::autograd::collect_next_edges(x, w, b));
+    node->x = SavedVariable(x, false);
+    if (t.w) node->weight = SavedVariable(w, false);
+    node->mean = SavedVariable(t.mean, false);
+    node->rstd = SavedVariable(t.rstd, false);
+    node->z = norm_sizes(t, yt);
+    node->dev = t.dev;
+    torch::autograd::set_history(t.y, node);
+  }
+  return THPVariable_Wrap(t.y);
   END_HANDLE_TH_ERRORS
 }
 
@@ -642,6 +841,8 @@ PyMethodDef methods[] = {
     {"xattn_bwd", MW_FAST(xattn_bwd), "mw_xattn_bwd"},
     {"norm_fwd", MW_FAST(norm_fwd), "mw_layernorm_fwd"},
     {"norm_bwd", MW_FAST(norm_bwd), "mw_layernorm_bwd"},
+    {"xattn_apply", MW_FAST(xattn_apply), "CrossAttention.apply"},
+    {"norm_apply", MW_FAST(norm_apply), "LayerNorm.apply"},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_mw_torch", nullptr, -1, methods,
                       nullptr, nullptr, nullptr, nullptr};

@@ -286,9 +286,11 @@ __global__ void __launch_bounds__(Layout<D, R>::THREADS)
 template <int D, int R>
 cudaError_t launch(const CUtensorMap& tk, const CUtensorMap& tv, const XattnFewParams& p, int dev, cudaStream_t s) {
   using L = Layout<D, R>;
-  // CTAs a head: two an SM at most, each with some stages
+  // CTAs a head: as many as the SMs hold at once (their shared memory: two, or four of
+  // 64 channels), each with some stages.  (Two stages and more CTAs: 160 heads of 128,
+  // 4096 keys 66 -> 80 us.  160 heads of 64 with two CTAs an SM 44 us, four 37.)
   int ranks = 1;
-  while (ranks < 16 && p.BH * ranks * 2 <= 2 * p.sms && p.S > 2 * ranks * kKeys) ranks *= 2;
+  while (ranks < 16 && p.BH * ranks * 2 <= (D == 64 ? 4 : 2) * p.sms && p.S > 2 * ranks * kKeys) ranks *= 2;
   static OncePerDevice prepared;
   const cudaError_t e = prepared(dev, [] {
     const cudaError_t e0 =
