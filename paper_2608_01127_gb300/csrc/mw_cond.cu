@@ -402,7 +402,7 @@ mw_status mw_layernorm_fwd(const void* x, const void* weight, const void* bias, 
 
 size_t mw_layernorm_bwd_workspace_size(long long rows, int C, int groups) {
   if (norm_sizes(rows, C, groups, 0.f) != MW_OK || rows == 0) return 0;
-  const int parts = norm_parts(rows / groups, groups, kNormSms);
+  const int parts = norm_parts(rows / groups, C, groups);
   return parts > 1 ? align256(static_cast<size_t>(groups) * parts * 2 * C * sizeof(float)) : 0;
 }
 
@@ -455,7 +455,7 @@ mw_status mw_layernorm_bwd(const void* dy, const void* x, const float* mean, con
   p.rows_per_group = rows / groups;
   p.C = C;
   p.groups = groups;
-  p.parts = norm_parts(rows / groups, groups, kNormSms);
+  p.parts = norm_parts(rows / groups, C, groups);
   p.x_f32 = x_dtype == MW_F32;
   p.y_f32 = y_dtype == MW_F32;
   p.param_f32 = param_dtype == MW_F32;

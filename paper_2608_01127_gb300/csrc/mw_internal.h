@@ -216,7 +216,7 @@ struct NormParams {
   bool x_f32, y_f32, param_f32;
 };
 // Blocks a group of the backward.
-int norm_parts(long long rows_per_group, int groups, int sms);
+int norm_parts(long long rows_per_group, int C, int groups);
 // vec: C is a multiple of 8 and every pointer 16-byte aligned
 cudaError_t launch_norm_fwd(NormParams p, bool vec, int sms, cudaStream_t s);
 cudaError_t launch_norm_bwd(NormParams p, bool vec, int dev, cudaStream_t s);

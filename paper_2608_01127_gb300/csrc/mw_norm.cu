@@ -23,30 +23,41 @@ namespace {
 
 using bf16 = __nv_bfloat16;
 
-template <int VEC>
-__device__ __forceinline__ void load(const float* p, float (&v)[VEC]) {
-  if constexpr (VEC == 8) {
-    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+// VEC elements as they lie in memory, so that a row on its way takes few registers.
+template <class T, int VEC>
+struct Raw;
+template <>
+struct Raw<float, 8> {
+  float4 a, b;
+  __device__ __forceinline__ void load(const float* p) {
+    a = reinterpret_cast<const float4*>(p)[0];
+    b = reinterpret_cast<const float4*>(p)[1];
+  }
+  __device__ __forceinline__ void get(float (&v)[8]) const {
     v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w;
     v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-  } else {
-    v[0] = *p;
   }
-}
-template <int VEC>
-__device__ __forceinline__ void load(const bf16* p, float (&v)[VEC]) {
-  if constexpr (VEC == 8) {
-    const uint4 a = *reinterpret_cast<const uint4*>(p);
+};
+template <>
+struct Raw<bf16, 8> {
+  uint4 a;
+  __device__ __forceinline__ void load(const bf16* p) { a = *reinterpret_cast<const uint4*>(p); }
+  __device__ __forceinline__ void get(float (&v)[8]) const {
     const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       v[2 * k] = __uint_as_float(w[k] << 16);
       v[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
     }
-  } else {
-    v[0] = __bfloat162float(*p);
   }
-}
+};
+template <class T>
+struct Raw<T, 1> {
+  T a;
+  __device__ __forceinline__ void load(const T* p) { a = *p; }
+  __device__ __forceinline__ void get(float (&v)[1]) const { v[0] = static_cast<float>(a); }
+};
+
 template <int VEC>
 __device__ __forceinline__ void store(float* p, const float (&v)[VEC]) {
   if constexpr (VEC == 8) {
@@ -67,10 +78,15 @@ __device__ __forceinline__ void store(bf16* p, const float (&v)[VEC]) {
 // a weight, bias or a gradient of one: fp32 or bf16
 template <int VEC>
 __device__ __forceinline__ void load_param(const void* base, bool f32, size_t i, float (&v)[VEC]) {
-  if (f32)
-    load<VEC>(static_cast<const float*>(base) + i, v);
-  else
-    load<VEC>(static_cast<const bf16*>(base) + i, v);
+  if (f32) {
+    Raw<float, VEC> r;
+    r.load(static_cast<const float*>(base) + i);
+    r.get(v);
+  } else {
+    Raw<bf16, VEC> r;
+    r.load(static_cast<const bf16*>(base) + i);
+    r.get(v);
+  }
 }
 __device__ __forceinline__ void store_param(void* base, bool f32, size_t i, float v) {
   if (f32)
@@ -110,37 +126,69 @@ struct Team {
   }
 };
 
+// Threads of a block at most, and the blocks of 256 threads that an SM holds for the
+// registers that a thread's columns take (x: bytes of an element of x).
+constexpr int max_threads(int VEC, int V) { return VEC == 1 && V > 8 ? 512 : 256; }
+constexpr int fwd_blocks(int VEC, int V, int x) {
+  return VEC == 1 ? (V <= 4 ? 4 : V <= 8 ? 3 : 1) : V == 1 ? 4 : V == 2 && x == 2 ? 3 : V <= 3 ? 2 : 1;
+}
+constexpr int bwd_blocks(int VEC, int V, int x) {
+  return VEC == 1 ? (V <= 4 ? 3 : V <= 8 ? 2 : 1) : V == 1 ? 3 : V == 2 && x == 2 ? 2 : 1;
+}
+
+// Each team takes a run of rows, the next row on its way while it works on one.
 template <class TX, class TY, int VEC, int V>
-__global__ void __launch_bounds__(512) norm_fwd_kernel(const NormParams p) {
+__global__ void __launch_bounds__(max_threads(VEC, V), fwd_blocks(VEC, V, sizeof(TX))) norm_fwd_kernel(const NormParams p) {
   __shared__ float2 red[2][16];
   const Team team(p.W);
   const TX* x = static_cast<const TX*>(p.x);
   TY* y = static_cast<TY*>(p.y);
   const float inv_c = 1.f / static_cast<float>(p.C);
+  const long long teams = static_cast<long long>(gridDim.x) * team.count;
+  const long long mine = static_cast<long long>(blockIdx.x) * team.count + team.index;
+  const long long r0 = p.rows * mine / teams, r1 = p.rows * (mine + 1) / teams;
+  auto column = [&](int k) { return (k * team.W * 32 + team.t) * VEC; };
   pdl_wait();
   pdl_trigger();
-  for (long long row = static_cast<long long>(blockIdx.x) * team.count + team.index; row < p.rows;
-       row += static_cast<long long>(gridDim.x) * team.count) {
+  Raw<TX, VEC> raw[V];
+  auto fetch = [&](long long row) {
+#pragma unroll
+    for (int k = 0; k < V; ++k)
+      if (column(k) < p.C) raw[k].load(x + row * p.C + column(k));
+  };
+  if (r0 < r1) fetch(r0);
+  float w[V][VEC], b[V][VEC];
+  long long group = -1;
+  for (long long row = r0; row < r1; ++row) {
+    const long long g = p.groups == 1 ? 0 : row / p.rows_per_group;
+    if (g != group) {
+      group = g;
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) w[k][e] = 1.f, b[k][e] = 0.f;
+        if (column(k) >= p.C) continue;
+        if (p.weight) load_param<VEC>(p.weight, p.param_f32, static_cast<size_t>(g) * p.C + column(k), w[k]);
+        if (p.bias) load_param<VEC>(p.bias, p.param_f32, static_cast<size_t>(g) * p.C + column(k), b[k]);
+      }
+    }
     float v[V][VEC];
     float s = 0.f;
 #pragma unroll
     for (int k = 0; k < V; ++k) {
-      const int c = (k * team.W * 32 + team.t) * VEC;
-      if (c < p.C) {
-        load<VEC>(x + row * p.C + c, v[k]);
-      } else {
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) v[k][e] = 0.f;
-      }
+      for (int e = 0; e < VEC; ++e) v[k][e] = 0.f;
+      if (column(k) >= p.C) continue;
+      raw[k].get(v[k]);
 #pragma unroll
       for (int e = 0; e < VEC; ++e) s += v[k][e];
     }
+    if (row + 1 < r1) fetch(row + 1);
     const float mean = team.sum(make_float2(s, 0.f), red[0]).x * inv_c;
     float q = 0.f;
 #pragma unroll
     for (int k = 0; k < V; ++k) {
-      const int c = (k * team.W * 32 + team.t) * VEC;
-      if (c >= p.C) continue;
+      if (column(k) >= p.C) continue;
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
         v[k][e] -= mean;
@@ -148,19 +196,12 @@ __global__ void __launch_bounds__(512) norm_fwd_kernel(const NormParams p) {
       }
     }
     const float rstd = rsqrtf(team.sum(make_float2(q, 0.f), red[1]).x * inv_c + p.eps);
-    const size_t g = p.groups == 1 ? 0 : static_cast<size_t>(row / p.rows_per_group) * p.C;
 #pragma unroll
     for (int k = 0; k < V; ++k) {
-      const int c = (k * team.W * 32 + team.t) * VEC;
-      if (c >= p.C) continue;
-      float w[VEC], b[VEC];
+      if (column(k) >= p.C) continue;
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) w[e] = 1.f, b[e] = 0.f;
-      if (p.weight) load_param<VEC>(p.weight, p.param_f32, g + c, w);
-      if (p.bias) load_param<VEC>(p.bias, p.param_f32, g + c, b);
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) v[k][e] = fmaf(v[k][e] * rstd, w[e], b[e]);
-      store<VEC>(y + row * p.C + c, v[k]);
+      for (int e = 0; e < VEC; ++e) v[k][e] = fmaf(v[k][e] * rstd, w[k][e], b[k][e]);
+      store<VEC>(y + row * p.C + column(k), v[k]);
     }
     if (team.t == 0) {
       if (p.mean) p.mean[row] = mean;
@@ -171,7 +212,7 @@ __global__ void __launch_bounds__(512) norm_fwd_kernel(const NormParams p) {
 
 // Block (part, group): rows [part n / parts, (part + 1) n / parts) of the group.
 template <class TX, class TY, int VEC, int V>
-__global__ void __launch_bounds__(512) norm_bwd_kernel(const NormParams p) {
+__global__ void __launch_bounds__(max_threads(VEC, V), bwd_blocks(VEC, V, sizeof(TX))) norm_bwd_kernel(const NormParams p) {
   __shared__ float2 red[2][16];
   extern __shared__ float sums[];  // [2][C]
   const Team team(p.W);
@@ -184,51 +225,59 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(const NormParams p) {
   const long long n = p.rows_per_group;
   const long long r0 = group * n + part * n / p.parts, r1 = group * n + (part + 1) * n / p.parts;
   const size_t g = static_cast<size_t>(group) * p.C;
-  float aw[V][VEC], ab[V][VEC];
+  auto column = [&](int k) { return (k * team.W * 32 + team.t) * VEC; };
+  pdl_wait();
+  pdl_trigger();
+  Raw<TX, VEC> rx[V];
+  Raw<TY, VEC> rg[V];
+  float mean = 0.f, rstd = 0.f;
+  auto fetch = [&](long long row) {
+    mean = p.mean[row];
+    rstd = p.rstd[row];
 #pragma unroll
-  for (int k = 0; k < V; ++k)
+    for (int k = 0; k < V; ++k)
+      if (column(k) < p.C) {
+        rx[k].load(x + row * p.C + column(k));
+        rg[k].load(dy + row * p.C + column(k));
+      }
+  };
+  if (r0 + team.index < r1) fetch(r0 + team.index);
+  float w[V][VEC], aw[V][VEC], ab[V][VEC];
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) aw[k][e] = ab[k][e] = 0.f;
+  for (int k = 0; k < V; ++k) {
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) aw[k][e] = ab[k][e] = 0.f, w[k][e] = 1.f;
+    if (p.weight && column(k) < p.C) load_param<VEC>(p.weight, p.param_f32, g + column(k), w[k]);
+  }
   int turn = 0;
   for (long long row = r0 + team.index; row < r1; row += team.count, turn ^= 1) {
-    const float mean = p.mean[row], rstd = p.rstd[row];
     float xh[V][VEC], gr[V][VEC];
     float2 s = make_float2(0.f, 0.f);
+    const float rs = rstd;
 #pragma unroll
     for (int k = 0; k < V; ++k) {
-      const int c = (k * team.W * 32 + team.t) * VEC;
-      if (c < p.C) {
-        load<VEC>(x + row * p.C + c, xh[k]);
-        load<VEC>(dy + row * p.C + c, gr[k]);
-      }
-    }
-#pragma unroll
-    for (int k = 0; k < V; ++k) {
-      const int c = (k * team.W * 32 + team.t) * VEC;
-      if (c >= p.C) continue;
-      float w[VEC];
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) w[e] = 1.f;
-      if (p.weight) load_param<VEC>(p.weight, p.param_f32, g + c, w);
+      if (column(k) >= p.C) continue;
+      rx[k].get(xh[k]);
+      rg[k].get(gr[k]);
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
-        xh[k][e] = (xh[k][e] - mean) * rstd;
+        xh[k][e] = (xh[k][e] - mean) * rs;
         aw[k][e] = fmaf(gr[k][e], xh[k][e], aw[k][e]);
         ab[k][e] += gr[k][e];
-        gr[k][e] *= w[e];
+        gr[k][e] *= w[k][e];
         s.x += gr[k][e];
         s.y = fmaf(gr[k][e], xh[k][e], s.y);
       }
     }
+    if (row + team.count < r1) fetch(row + team.count);
     s = team.sum(s, red[turn]);
     const float m1 = s.x * inv_c, m2 = s.y * inv_c;
 #pragma unroll
     for (int k = 0; k < V; ++k) {
-      const int c = (k * team.W * 32 + team.t) * VEC;
-      if (c >= p.C) continue;
+      if (column(k) >= p.C) continue;
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) gr[k][e] = rstd * (gr[k][e] - m1 - xh[k][e] * m2);
-      store<VEC>(dx + row * p.C + c, gr[k]);
+      for (int e = 0; e < VEC; ++e) gr[k][e] = rs * (gr[k][e] - m1 - xh[k][e] * m2);
+      store<VEC>(dx + row * p.C + column(k), gr[k]);
     }
   }
   if (!p.dweight && !p.dbias) return;
@@ -236,7 +285,7 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(const NormParams p) {
     if (team.index == t) {
 #pragma unroll
       for (int k = 0; k < V; ++k) {
-        const int c = (k * team.W * 32 + team.t) * VEC;
+        const int c = column(k);
         if (c >= p.C) continue;
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
@@ -255,23 +304,29 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(const NormParams p) {
   }
 }
 
-// dw and db of a group from its blocks' partials: 32 columns a block, the parts
-// over its 16 warps.
-__global__ void __launch_bounds__(512) norm_params_kernel(const NormParams p) {
-  __shared__ float sums[16][33];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int c = blockIdx.x * 32 + lane;
+// dw and db of a group from its blocks' partials: `split` threads a column, each an
+// equal share of the parts in their order.
+__global__ void __launch_bounds__(256) norm_params_kernel(const NormParams p, int split) {
+  __shared__ float sums[256];
+  const int columns = 256 / split;
+  const int lane = threadIdx.x / columns, at = threadIdx.x % columns;
+  const int c = blockIdx.x * columns + at;
+  pdl_wait();
+  pdl_trigger();
   for (int g = blockIdx.y; g < p.groups; g += gridDim.y) {
     float s = 0.f;
     if (c < 2 * p.C) {
       const float* in = p.partial + static_cast<size_t>(g) * p.parts * 2 * p.C + c;
-#pragma unroll 4
-      for (int i = warp; i < p.parts; i += 16) s += in[static_cast<size_t>(i) * 2 * p.C];
+      const int i1 = p.parts * (lane + 1) / split;
+#pragma unroll 8
+      for (int i = p.parts * lane / split; i < i1; ++i) s += in[static_cast<size_t>(i) * 2 * p.C];
     }
-    sums[warp][lane] = s;
-    __syncthreads();
-    if (warp == 0 && c < 2 * p.C) {
-      for (int w = 1; w < 16; ++w) s += sums[w][lane];
+    if (split > 1) {
+      sums[threadIdx.x] = s;
+      __syncthreads();
+      for (int k = 1; lane == 0 && k < split; ++k) s += sums[k * columns + at];
+    }
+    if (lane == 0 && c < 2 * p.C) {
       void* out = c < p.C ? p.dweight : p.dbias;
       if (out) store_param(out, p.param_f32, static_cast<size_t>(g) * p.C + (c < p.C ? c : c - p.C), s);
     }
@@ -280,17 +335,18 @@ __global__ void __launch_bounds__(512) norm_params_kernel(const NormParams p) {
 }
 
 // Warps a row and accesses a thread: the fewest slots that hold the row (the
-// fewest warps of those), VEC = 8 up to 4 accesses, VEC = 1 up to 16.
+// fewest warps of those).  VEC = 8: up to 4 accesses forward, 2 backward, which holds
+// three times as much a column; VEC = 1: up to 8, or 16 of the widest rows.
 struct Shape {
   int W, V, threads;
 };
-Shape shape_of(int C, bool vec) {
-  const int elems = vec ? 256 : 32, max_v = vec ? 4 : 16, max_w = vec ? 8 : 16;
+Shape shape_of(int C, bool vec, bool backward) {
+  const int elems = vec ? 256 : 32, max_v = vec ? (backward && C <= 4096 ? 2 : 4) : (C <= 2048 ? 8 : 16);
+  const int max_w = vec || C <= 2048 ? 8 : 16;
   Shape best{0, 0, 0};
   for (int W = 1; W <= max_w; ++W) {
     int V = (C + elems * W - 1) / (elems * W);
-    if (!vec) V = V <= 2 ? 2 : V <= 4 ? 4 : V <= 8 ? 8 : V;
-    if (!vec && V > 8) V = V <= 16 ? 16 : V;
+    if (!vec) V = V <= 2 ? 2 : V <= 4 ? 4 : V <= 8 ? 8 : V <= 16 ? 16 : V;
     if (V > max_v) continue;
     if (best.W == 0 || W * V < best.W * best.V) best = {W, V, 0};
   }
@@ -302,6 +358,7 @@ template <class X, class Y, int VEC, int V>
 struct Kernels {
   static constexpr auto fwd = norm_fwd_kernel<X, Y, VEC, V>;
   static constexpr auto bwd = norm_bwd_kernel<X, Y, VEC, V>;
+  static constexpr int blocks = fwd_blocks(VEC, V, sizeof(X));
 };
 
 // f of the kernels for these types and accesses a thread.
@@ -332,30 +389,39 @@ cudaError_t by_shape(const NormParams& p, bool vec, int V, F&& f) {
 
 }  // namespace
 
-int norm_parts(long long rows_per_group, int groups, int sms) {
-  long long parts = 2ll * sms / groups;
+int norm_parts(long long rows_per_group, int C, int groups) {
+  // as many blocks as the SMs hold, by the form that aligned rows take
+  const bool vec = C % 8 == 0;
+  const Shape sh = shape_of(C, vec, true);
+  long long parts = static_cast<long long>(kNormSms) * bwd_blocks(vec ? 8 : 1, sh.V, 2) * max_threads(vec ? 8 : 1, sh.V) /
+                    sh.threads / groups;
   if (parts > rows_per_group) parts = rows_per_group;
   return parts < 1 ? 1 : static_cast<int>(parts);
 }
 
 cudaError_t launch_norm_fwd(NormParams p, bool vec, int sms, cudaStream_t s) {
-  const Shape sh = shape_of(p.C, vec);
+  const Shape sh = shape_of(p.C, vec, false);
   p.W = sh.W;
   const int teams = sh.threads / 32 / sh.W;
   const long long blocks = (p.rows + teams - 1) / teams;
-  const unsigned grid = static_cast<unsigned>(blocks < (1 << 20) ? blocks : (1 << 20));
-  cudaLaunchConfig_t cfg;
-  cudaLaunchAttribute attr;
-  pdl_config(cfg, attr, dim3(grid), dim3(sh.threads), 0, s);
-  return by_shape(p, vec, sh.V, [&](auto k) { return cudaLaunchKernelEx(&cfg, k.fwd, p); });
+  return by_shape(p, vec, sh.V, [&](auto k) {
+    // as many blocks as the SMs hold (of fewer threads, more)
+    const long long most = static_cast<long long>(sms) * decltype(k)::blocks * 256 / sh.threads;
+    cudaLaunchConfig_t cfg;
+    cudaLaunchAttribute attr;
+    pdl_config(cfg, attr, dim3(static_cast<unsigned>(blocks < most ? blocks : most)), dim3(sh.threads), 0, s);
+    return cudaLaunchKernelEx(&cfg, k.fwd, p);
+  });
 }
 
 cudaError_t launch_norm_bwd(NormParams p, bool vec, int dev, cudaStream_t s) {
-  const Shape sh = shape_of(p.C, vec);
+  const Shape sh = shape_of(p.C, vec, true);
   p.W = sh.W;
   const size_t smem = static_cast<size_t>(2) * p.C * sizeof(float);
-  const unsigned grid = static_cast<unsigned>(p.groups) * p.parts;
-  cudaError_t e = by_shape(p, vec, sh.V, [&](auto k) {
+  cudaLaunchConfig_t cfg;
+  cudaLaunchAttribute attr;
+  pdl_config(cfg, attr, dim3(static_cast<unsigned>(p.groups) * p.parts), dim3(sh.threads), smem, s);
+  const cudaError_t e = by_shape(p, vec, sh.V, [&](auto k) {
     constexpr auto bwd = decltype(k)::bwd;
     if (smem > 48 * 1024) {
       static OncePerDevice prepared;
@@ -365,12 +431,14 @@ cudaError_t launch_norm_bwd(NormParams p, bool vec, int dev, cudaStream_t s) {
       });
       if (e0 != cudaSuccess) return e0;
     }
-    bwd<<<grid, sh.threads, smem, s>>>(p);
-    return cudaGetLastError();
+    return cudaLaunchKernelEx(&cfg, bwd, p);
   });
   if (e != cudaSuccess || p.parts == 1 || (!p.dweight && !p.dbias)) return e;
-  norm_params_kernel<<<dim3((2 * p.C + 31) / 32, p.groups < 65535 ? p.groups : 65535), 512, 0, s>>>(p);
-  return cudaGetLastError();
+  int split = 1;
+  while (split < 32 && p.parts >= 16 * split) split *= 2;
+  const int columns = 256 / split;
+  pdl_config(cfg, attr, dim3((2 * p.C + columns - 1) / columns, p.groups < 65535 ? p.groups : 65535), dim3(256), 0, s);
+  return cudaLaunchKernelEx(&cfg, norm_params_kernel, p, split);
 }
 
 }  // namespace mw
