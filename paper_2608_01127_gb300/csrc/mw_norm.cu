@@ -95,6 +95,12 @@ __device__ __forceinline__ void store_param(void* base, bool f32, size_t i, floa
     static_cast<bf16*>(base)[i] = __float2bfloat16(v);
 }
 
+// Sums that a team makes at once.
+template <int N>
+struct Sums {
+  float v[N];
+};
+
 // A block's threads: teams of W warps, a row each.
 struct Team {
   int W, index, count, t, warp;  // t: thread of the team
@@ -105,24 +111,32 @@ struct Team {
     warp = w % W;
     t = warp * 32 + (threadIdx.x & 31);
   }
-  // Sums over the team in a fixed order; red: two floats a warp of the block.
-  // (A barrier a call is enough where calls alternate between two buffers.)
-  __device__ float2 sum(float2 v, float2* red) const {
+  // Sums over the team in a fixed order; red: a value a warp of the block.  (A barrier
+  // a call is enough where calls alternate between two buffers.)
+  template <int N>
+  __device__ __forceinline__ Sums<N> sum(Sums<N> v, Sums<N>* red) const {
 #pragma unroll
-    for (int s = 16; s > 0; s >>= 1) {
-      v.x += __shfl_xor_sync(0xffffffffu, v.x, s);
-      v.y += __shfl_xor_sync(0xffffffffu, v.y, s);
-    }
+    for (int s = 16; s > 0; s >>= 1) v = plus(v, shuffled(v, s));
     if (W == 1) return v;
     if ((threadIdx.x & 31) == 0) red[index * W + warp] = v;
     asm volatile("bar.sync %0, %1;" ::"r"(index + 1), "r"(W * 32) : "memory");
-    float2 s = red[index * W];
-    for (int w = 1; w < W; ++w) {
-      const float2 a = red[index * W + w];
-      s.x += a.x;
-      s.y += a.y;
-    }
+    Sums<N> s = red[index * W];
+    for (int w = 1; w < W; ++w) s = plus(s, red[index * W + w]);
     return s;
+  }
+
+ private:
+  template <int N>
+  static __device__ __forceinline__ Sums<N> plus(Sums<N> a, const Sums<N>& b) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) a.v[i] += b.v[i];
+    return a;
+  }
+  template <int N>
+  static __device__ __forceinline__ Sums<N> shuffled(Sums<N> a, int s) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) a.v[i] = __shfl_xor_sync(0xffffffffu, a.v[i], s);
+    return a;
   }
 };
 
@@ -130,16 +144,26 @@ struct Team {
 // registers that a thread's columns take (x: bytes of an element of x).
 constexpr int max_threads(int VEC, int V) { return VEC == 1 && V > 8 ? 512 : 256; }
 constexpr int fwd_blocks(int VEC, int V, int x) {
-  return VEC == 1 ? (V <= 4 ? 4 : V <= 8 ? 3 : 1) : V == 1 ? 4 : V == 2 && x == 2 ? 3 : V <= 3 ? 2 : 1;
+  return VEC == 1 ? (V <= 4 ? 5 : V <= 8 ? 3 : 1) : V <= 2 ? 4 : V <= 4 ? 3 : V <= 6 && x == 2 ? 3 : 2;
 }
 constexpr int bwd_blocks(int VEC, int V, int x) {
   return VEC == 1 ? (V <= 4 ? 3 : V <= 8 ? 2 : 1) : V == 1 ? 3 : V == 2 && x == 2 ? 2 : 1;
 }
 
-// Each team takes a run of rows, the next row on its way while it works on one.
+// Rows that a team of the forward works on at once: their loads, sums and barriers
+// overlap, and they share what a group's weight and bias cost (read from L1 for every
+// turn: in registers they would take the room of rows).  14080 rows of 2560 bf16: one
+// row with the next on its way, five warps a row 59 us; one warp, one row 43; two 39.
+template <class TX, int VEC, int V>
+constexpr int kRows = VEC == 8 && V >= 3 && sizeof(TX) == 2 ? 2 : 1;
+
+// Each team takes a run of rows.  A warp alone holds rows of up to 2560 elements: no
+// barrier, and many rows on their way at once.
 template <class TX, class TY, int VEC, int V>
-__global__ void __launch_bounds__(max_threads(VEC, V), fwd_blocks(VEC, V, sizeof(TX))) norm_fwd_kernel(const NormParams p) {
-  __shared__ float2 red[2][16];
+__global__ void __launch_bounds__(max_threads(VEC, V), fwd_blocks(VEC, V, sizeof(TX)))
+    norm_fwd_kernel(const NormParams p) {
+  constexpr int R = kRows<TX, VEC, V>;
+  __shared__ Sums<R> red[2][16];
   const Team team(p.W);
   const TX* x = static_cast<const TX*>(p.x);
   TY* y = static_cast<TY*>(p.y);
@@ -148,64 +172,115 @@ __global__ void __launch_bounds__(max_threads(VEC, V), fwd_blocks(VEC, V, sizeof
   const long long mine = static_cast<long long>(blockIdx.x) * team.count + team.index;
   const long long r0 = p.rows * mine / teams, r1 = p.rows * (mine + 1) / teams;
   auto column = [&](int k) { return (k * team.W * 32 + team.t) * VEC; };
+  long long left = 0;  // rows of the group from this one on
+  size_t params = 0;   // where the group's weight and bias start
+  if (p.groups > 1 && r0 < r1) {
+    const long long group = r0 / p.rows_per_group;
+    left = (group + 1) * p.rows_per_group - r0;
+    params = static_cast<size_t>(group) * p.C;
+  }
   pdl_wait();
   pdl_trigger();
-  Raw<TX, VEC> raw[V];
-  auto fetch = [&](long long row) {
+  auto fetch = [&](long long row, int n, Raw<TX, VEC> (&to)[R][V]) {
 #pragma unroll
-    for (int k = 0; k < V; ++k)
-      if (column(k) < p.C) raw[k].load(x + row * p.C + column(k));
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int k = 0; k < V; ++k)
+        if (r < n && column(k) < p.C) to[r][k].load(x + (row + r) * p.C + column(k));
   };
-  if (r0 < r1) fetch(r0);
-  float w[V][VEC], b[V][VEC];
-  long long group = -1;
-  for (long long row = r0; row < r1; ++row) {
-    const long long g = p.groups == 1 ? 0 : row / p.rows_per_group;
-    if (g != group) {
-      group = g;
+  auto load_params = [&](int k, float (&w)[VEC], float (&b)[VEC]) {
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) w[e] = 1.f, b[e] = 0.f;
+    if (column(k) >= p.C) return;
+    if (p.weight) load_param<VEC>(p.weight, p.param_f32, params + column(k), w);
+    if (p.bias) load_param<VEC>(p.bias, p.param_f32, params + column(k), b);
+  };
+  // (single elements: 5003 rows of 1155 fp32 33 us with weights read for every row)
+  constexpr int kHeld = VEC == 1 ? V : 1;
+  [[maybe_unused]] float hw[kHeld][VEC], hb[kHeld][VEC];
+  auto hold_params = [&]() {
+    if constexpr (VEC == 1) {
+#pragma unroll
+      for (int k = 0; k < V; ++k) load_params(k, hw[k], hb[k]);
+    }
+  };
+  hold_params();
+  Raw<TX, VEC> raw[R][V];
+  [[maybe_unused]] Raw<TX, VEC> next[R][V];  // a row at a time: the next one on its way
+  if (R == 1 && r0 < r1) fetch(r0, 1, raw);
+  for (long long row = r0; row < r1;) {
+    // rows of one group
+    int n = static_cast<int>(min(static_cast<long long>(R), r1 - row));
+    if (p.groups > 1) n = static_cast<int>(min(static_cast<long long>(n), left));
+    if constexpr (R == 1) {
+      if (row + 1 < r1) fetch(row + 1, 1, next);
+    } else {
+      fetch(row, n, raw);
+    }
+    Sums<R> mean, rstd;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      mean.v[r] = 0.f;
 #pragma unroll
       for (int k = 0; k < V; ++k) {
+        if (r >= n || column(k) >= p.C) continue;
+        float v[VEC];
+        raw[r][k].get(v);
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) w[k][e] = 1.f, b[k][e] = 0.f;
-        if (column(k) >= p.C) continue;
-        if (p.weight) load_param<VEC>(p.weight, p.param_f32, static_cast<size_t>(g) * p.C + column(k), w[k]);
-        if (p.bias) load_param<VEC>(p.bias, p.param_f32, static_cast<size_t>(g) * p.C + column(k), b[k]);
+        for (int e = 0; e < VEC; ++e) mean.v[r] += v[e];
       }
     }
-    float v[V][VEC];
-    float s = 0.f;
+    mean = team.sum(mean, red[0]);
 #pragma unroll
-    for (int k = 0; k < V; ++k) {
+    for (int r = 0; r < R; ++r) {
+      mean.v[r] *= inv_c;
+      rstd.v[r] = 0.f;
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) v[k][e] = 0.f;
-      if (column(k) >= p.C) continue;
-      raw[k].get(v[k]);
+      for (int k = 0; k < V; ++k) {
+        if (r >= n || column(k) >= p.C) continue;
+        float v[VEC];
+        raw[r][k].get(v);
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) s += v[k][e];
-    }
-    if (row + 1 < r1) fetch(row + 1);
-    const float mean = team.sum(make_float2(s, 0.f), red[0]).x * inv_c;
-    float q = 0.f;
-#pragma unroll
-    for (int k = 0; k < V; ++k) {
-      if (column(k) >= p.C) continue;
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-        v[k][e] -= mean;
-        q = fmaf(v[k][e], v[k][e], q);
+        for (int e = 0; e < VEC; ++e) rstd.v[r] = fmaf(v[e] - mean.v[r], v[e] - mean.v[r], rstd.v[r]);
       }
     }
-    const float rstd = rsqrtf(team.sum(make_float2(q, 0.f), red[1]).x * inv_c + p.eps);
+    rstd = team.sum(rstd, red[1]);
+#pragma unroll
+    for (int r = 0; r < R; ++r) rstd.v[r] = rsqrtf(rstd.v[r] * inv_c + p.eps);
 #pragma unroll
     for (int k = 0; k < V; ++k) {
       if (column(k) >= p.C) continue;
+      float w[VEC], b[VEC];
+      if constexpr (VEC == 1)
+        w[0] = hw[k][0], b[0] = hb[k][0];
+      else
+        load_params(k, w, b);
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) v[k][e] = fmaf(v[k][e] * rstd, w[k][e], b[k][e]);
-      store<VEC>(y + row * p.C + column(k), v[k]);
+      for (int r = 0; r < R; ++r) {
+        if (r >= n) continue;
+        float v[VEC];
+        raw[r][k].get(v);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) v[e] = fmaf((v[e] - mean.v[r]) * rstd.v[r], w[e], b[e]);
+        store<VEC>(y + (row + r) * p.C + column(k), v);
+      }
     }
-    if (team.t == 0) {
-      if (p.mean) p.mean[row] = mean;
-      if (p.rstd) p.rstd[row] = rstd;
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+      if (r < n && team.t == 0) {
+        if (p.mean) p.mean[row + r] = mean.v[r];
+        if (p.rstd) p.rstd[row + r] = rstd.v[r];
+      }
+    if constexpr (R == 1) {
+#pragma unroll
+      for (int k = 0; k < V; ++k) raw[0][k] = next[0][k];
+    }
+    row += n;
+    left -= n;
+    if (p.groups > 1 && left == 0) {
+      left = p.rows_per_group;
+      params += p.C;
+      if (row < r1) hold_params();
     }
   }
 }
@@ -213,7 +288,7 @@ __global__ void __launch_bounds__(max_threads(VEC, V), fwd_blocks(VEC, V, sizeof
 // Block (part, group): rows [part n / parts, (part + 1) n / parts) of the group.
 template <class TX, class TY, int VEC, int V>
 __global__ void __launch_bounds__(max_threads(VEC, V), bwd_blocks(VEC, V, sizeof(TX))) norm_bwd_kernel(const NormParams p) {
-  __shared__ float2 red[2][16];
+  __shared__ Sums<2> red[2][16];
   extern __shared__ float sums[];  // [2][C]
   const Team team(p.W);
   const TX* x = static_cast<const TX*>(p.x);
@@ -252,7 +327,7 @@ __global__ void __launch_bounds__(max_threads(VEC, V), bwd_blocks(VEC, V, sizeof
   int turn = 0;
   for (long long row = r0 + team.index; row < r1; row += team.count, turn ^= 1) {
     float xh[V][VEC], gr[V][VEC];
-    float2 s = make_float2(0.f, 0.f);
+    Sums<2> s = {{0.f, 0.f}};
     const float rs = rstd;
 #pragma unroll
     for (int k = 0; k < V; ++k) {
@@ -265,13 +340,13 @@ __global__ void __launch_bounds__(max_threads(VEC, V), bwd_blocks(VEC, V, sizeof
         aw[k][e] = fmaf(gr[k][e], xh[k][e], aw[k][e]);
         ab[k][e] += gr[k][e];
         gr[k][e] *= w[k][e];
-        s.x += gr[k][e];
-        s.y = fmaf(gr[k][e], xh[k][e], s.y);
+        s.v[0] += gr[k][e];
+        s.v[1] = fmaf(gr[k][e], xh[k][e], s.v[1]);
       }
     }
     if (row + team.count < r1) fetch(row + team.count);
     s = team.sum(s, red[turn]);
-    const float m1 = s.x * inv_c, m2 = s.y * inv_c;
+    const float m1 = s.v[0] * inv_c, m2 = s.v[1] * inv_c;
 #pragma unroll
     for (int k = 0; k < V; ++k) {
       if (column(k) >= p.C) continue;
@@ -334,21 +409,28 @@ __global__ void __launch_bounds__(256) norm_params_kernel(const NormParams p, in
   }
 }
 
-// Warps a row and accesses a thread: the fewest slots that hold the row (the
-// fewest warps of those).  VEC = 8: up to 4 accesses forward, 2 backward, which holds
-// three times as much a column; VEC = 1: up to 8, or 16 of the widest rows.
+// Warps a row and accesses a thread.  VEC = 8: forward the fewest warps that hold the
+// row in ten accesses; backward, which holds three times as much a column and sums
+// over rows, the fewest slots with two accesses a thread (four of the widest rows).
+// VEC = 1: the fewest slots with 8 accesses, 16 of the widest rows.
 struct Shape {
   int W, V, threads;
 };
-Shape shape_of(int C, bool vec, bool backward) {
-  const int elems = vec ? 256 : 32, max_v = vec ? (backward && C <= 4096 ? 2 : 4) : (C <= 2048 ? 8 : 16);
+int form(int V, bool vec, bool backward) {  // the least V that is compiled
+  if (!vec) return V <= 2 ? 2 : V <= 4 ? 4 : V <= 8 ? 8 : V <= 16 ? 16 : 99;
+  if (backward) return V <= 4 ? V : 99;
+  return V <= 4 ? V : V <= 6 ? 6 : V <= 10 ? 10 : 99;
+}
+// Few rows (forward): all SMs' warps for them, a thread's part of a row as short as can be.
+Shape shape_of(int C, bool vec, bool backward, bool few) {
+  const int elems = vec ? 256 : 32;
+  const int max_v = vec ? (!backward && !few ? 10 : C <= 4096 ? 2 : 4) : (C <= 2048 ? 8 : 16);
   const int max_w = vec || C <= 2048 ? 8 : 16;
   Shape best{0, 0, 0};
   for (int W = 1; W <= max_w; ++W) {
-    int V = (C + elems * W - 1) / (elems * W);
-    if (!vec) V = V <= 2 ? 2 : V <= 4 ? 4 : V <= 8 ? 8 : V <= 16 ? 16 : V;
+    const int V = form((C + elems * W - 1) / (elems * W), vec, backward);
     if (V > max_v) continue;
-    if (best.W == 0 || W * V < best.W * best.V) best = {W, V, 0};
+    if (best.W == 0 || (W * V < best.W * best.V && (backward || few || !vec))) best = {W, V, 0};
   }
   best.threads = 32 * best.W * (best.W < 8 ? 8 / best.W : 1);
   return best;
@@ -356,31 +438,31 @@ Shape shape_of(int C, bool vec, bool backward) {
 
 template <class X, class Y, int VEC, int V>
 struct Kernels {
-  static constexpr auto fwd = norm_fwd_kernel<X, Y, VEC, V>;
-  static constexpr auto bwd = norm_bwd_kernel<X, Y, VEC, V>;
+  static constexpr auto fwd() { return norm_fwd_kernel<X, Y, VEC, V>; }
+  static constexpr auto bwd() { return norm_bwd_kernel<X, Y, VEC, V>; }
   static constexpr int blocks = fwd_blocks(VEC, V, sizeof(X));
 };
 
 // f of the kernels for these types and accesses a thread.
-template <class F>
+template <bool BACKWARD, class F>
 cudaError_t by_shape(const NormParams& p, bool vec, int V, F&& f) {
   auto types = [&](auto tx, auto ty) {
     using X = decltype(tx);
     using Y = decltype(ty);
     if (vec) {
-      switch (V) {
-        case 1: return f(Kernels<X, Y, 8, 1>{});
-        case 2: return f(Kernels<X, Y, 8, 2>{});
-        case 3: return f(Kernels<X, Y, 8, 3>{});
-        default: return f(Kernels<X, Y, 8, 4>{});
+      if (V == 1) return f(Kernels<X, Y, 8, 1>{});
+      if (V == 2) return f(Kernels<X, Y, 8, 2>{});
+      if (V == 3) return f(Kernels<X, Y, 8, 3>{});
+      if constexpr (!BACKWARD) {
+        if (V == 6) return f(Kernels<X, Y, 8, 6>{});
+        if (V == 10) return f(Kernels<X, Y, 8, 10>{});
       }
+      return f(Kernels<X, Y, 8, 4>{});
     }
-    switch (V) {
-      case 2: return f(Kernels<X, Y, 1, 2>{});
-      case 4: return f(Kernels<X, Y, 1, 4>{});
-      case 8: return f(Kernels<X, Y, 1, 8>{});
-      default: return f(Kernels<X, Y, 1, 16>{});
-    }
+    if (V == 2) return f(Kernels<X, Y, 1, 2>{});
+    if (V == 4) return f(Kernels<X, Y, 1, 4>{});
+    if (V == 8) return f(Kernels<X, Y, 1, 8>{});
+    return f(Kernels<X, Y, 1, 16>{});
   };
   if (!p.x_f32) return types(bf16{}, bf16{});
   if (!p.y_f32) return types(float{}, bf16{});
@@ -392,7 +474,7 @@ cudaError_t by_shape(const NormParams& p, bool vec, int V, F&& f) {
 int norm_parts(long long rows_per_group, int C, int groups) {
   // as many blocks as the SMs hold, by the form that aligned rows take
   const bool vec = C % 8 == 0;
-  const Shape sh = shape_of(C, vec, true);
+  const Shape sh = shape_of(C, vec, true, false);
   long long parts = static_cast<long long>(kNormSms) * bwd_blocks(vec ? 8 : 1, sh.V, 2) * max_threads(vec ? 8 : 1, sh.V) /
                     sh.threads / groups;
   if (parts > rows_per_group) parts = rows_per_group;
@@ -400,29 +482,29 @@ int norm_parts(long long rows_per_group, int C, int groups) {
 }
 
 cudaError_t launch_norm_fwd(NormParams p, bool vec, int sms, cudaStream_t s) {
-  const Shape sh = shape_of(p.C, vec, false);
+  const Shape sh = shape_of(p.C, vec, false, p.rows <= 8ll * sms);
   p.W = sh.W;
   const int teams = sh.threads / 32 / sh.W;
   const long long blocks = (p.rows + teams - 1) / teams;
-  return by_shape(p, vec, sh.V, [&](auto k) {
+  return by_shape<false>(p, vec, sh.V, [&](auto k) {
     // as many blocks as the SMs hold (of fewer threads, more)
     const long long most = static_cast<long long>(sms) * decltype(k)::blocks * 256 / sh.threads;
     cudaLaunchConfig_t cfg;
     cudaLaunchAttribute attr;
     pdl_config(cfg, attr, dim3(static_cast<unsigned>(blocks < most ? blocks : most)), dim3(sh.threads), 0, s);
-    return cudaLaunchKernelEx(&cfg, k.fwd, p);
+    return cudaLaunchKernelEx(&cfg, decltype(k)::fwd(), p);
   });
 }
 
 cudaError_t launch_norm_bwd(NormParams p, bool vec, int dev, cudaStream_t s) {
-  const Shape sh = shape_of(p.C, vec, true);
+  const Shape sh = shape_of(p.C, vec, true, false);
   p.W = sh.W;
   const size_t smem = static_cast<size_t>(2) * p.C * sizeof(float);
   cudaLaunchConfig_t cfg;
   cudaLaunchAttribute attr;
   pdl_config(cfg, attr, dim3(static_cast<unsigned>(p.groups) * p.parts), dim3(sh.threads), smem, s);
-  const cudaError_t e = by_shape(p, vec, sh.V, [&](auto k) {
-    constexpr auto bwd = decltype(k)::bwd;
+  const cudaError_t e = by_shape<true>(p, vec, sh.V, [&](auto k) {
+    constexpr auto bwd = decltype(k)::bwd();
     if (smem > 48 * 1024) {
       static OncePerDevice prepared;
       const cudaError_t e0 = prepared(dev, [&] {
