@@ -60,42 +60,40 @@ size_t xattn_ws(const XattnSizes& z, int S, int d) {
   return align256(rows * kernel_d(d) * sizeof(float)) + align256(rows * sizeof(float));
 }
 
-// The order of the backward's work and the ranges of a head's query tiles, from a
-// model of the time (us): steps of t, a sweep's start and end, waves of pieces over
-// the SMs, and the accumulators' way through HBM.
+// The order of the backward's work, from a model of the time (us): steps of t, a sweep's
+// start and end, and the accumulators' way through HBM.
 struct XattnBwdPlan {
   bool key_major = false;
-  int ranges = 1;
+  int ranges = 1;  // key-major: of a head's query tiles
+  int run = 1;     // query-major: query tiles of a run, so that the dQ of all runs in work stays in L2
 };
 
 XattnBwdPlan xattn_bwd_plan(int BH, int q_tiles, int k_tiles, int D) {
-  const double t = D == 64 ? 1.25 : 2.2, sweep = 2.0;
+  const double t = D == 64 ? 1.25 : 2.2, sweep = D == 64 ? 1.0 : 2.0;
   const double acc = 4e-6 * BH * static_cast<double>(q_tiles) * kTileRows * D / 6.5;  // us a pass
   XattnBwdPlan best;
-  double best_cost = 1e30;
-  auto consider = [&](bool key_major, int r, double extra) {
-    const long long pieces = static_cast<long long>(BH) * r * (key_major ? k_tiles : 1);
-    const double sweeps = key_major ? 1 : k_tiles;
-    const double cost = ceil_div(pieces, kNormSms) * sweeps * (ceil_div(q_tiles, r) * t + sweep) + extra;
+  best.run = D == 64 ? 8 : 4;
+  // query-major: equal shares of all steps (dQ in bf16 leaves with the last key tile at
+  // d = 64, through a pass of its own else)
+  const double tiles = std::ceil(static_cast<double>(BH) * q_tiles / kNormSms);
+  double best_cost = tiles * k_tiles * t + (k_tiles == 1 ? 1 : k_tiles * std::ceil(tiles / best.run)) * sweep +
+                     (k_tiles == 1 ? 0 : D == 64 ? 0.5 : 2.5) * acc;
+  for (int r = 1; k_tiles > 1 && r <= q_tiles && r <= 64; ++r) {
+    const double cost = ceil_div(static_cast<long long>(BH) * r * k_tiles, kNormSms) * (ceil_div(q_tiles, r) * t + sweep) +
+                        3.5 * acc;
     if (cost < best_cost) {
       best_cost = cost;
-      best.key_major = key_major;
+      best.key_major = true;
       best.ranges = r;
     }
-  };
-  // query-major: the dQ of the ranges in work has to stay in L2 (about 40 MB)
-  const int most = k_tiles == 1 ? q_tiles : D == 64 ? 8 : 4;
-  for (int r = ceil_div(q_tiles, most); r <= q_tiles; ++r) {
-    consider(false, r, k_tiles == 1 ? 0 : 2.5 * acc);
-    if (static_cast<long long>(BH) * r > 64ll * kNormSms) break;
   }
-  for (int r = 1; k_tiles > 1 && r <= q_tiles && r <= 64; ++r) consider(true, r, 3.5 * acc);
   return best;
 }
 
 // The backward's workspace: byte offsets of its fp32 arrays.
 struct XattnBwdWs {
   int M_pad = 0, S_pad = 0;
+  bool dkv_whole = false;  // no accumulators of dK and dV
   XattnBwdPlan plan;
   size_t dq = 0, dkv = 0, dkv_bytes = 0, lse2 = 0, delta = 0, bias = 0, total = 0;
 };
@@ -108,7 +106,8 @@ XattnBwdWs xattn_bwd_ws(const XattnSizes& z, int S, int d) {
   w.plan = xattn_bwd_plan(z.BH, w.M_pad / kTileRows, w.S_pad / kTileRows, D);
   const size_t rows = static_cast<size_t>(z.BH) * w.M_pad, keys = static_cast<size_t>(z.BH) * w.S_pad;
   w.dkv = w.S_pad > kTileRows ? align256(rows * D * 4) : 0;
-  w.dkv_bytes = w.plan.ranges > 1 ? 2 * keys * D * 4 : 0;
+  w.dkv_whole = w.plan.key_major && w.plan.ranges == 1;
+  w.dkv_bytes = w.dkv_whole ? 0 : 2 * keys * D * 4;
   w.lse2 = w.dkv + align256(w.dkv_bytes);
   w.delta = w.lse2 + (D == 64 ? 0 : align256(rows * 4));
   w.bias = w.delta + (D == 64 ? 0 : align256(rows * 4));
@@ -323,12 +322,17 @@ mw_status mw_xattn_bwd(const void* q, const void* k, const void* v, const int* k
   p.S = S;
   p.S_pad = ws.S_pad;
   p.d = d;
-  p.key_major = ws.plan.key_major;
-  p.ranges = ws.plan.ranges;
-  p.range_tiles = ws.M_pad / kTileRows / p.ranges;
-  p.range_rest = ws.M_pad / kTileRows % p.ranges;
+  if (kv_len == nullptr) p.heads = z.BH;  // one sample of all heads
+  p.samples = z.BH / p.heads;
+  p.q_tiles = ws.M_pad / kTileRows;
   p.k_tiles = ws.S_pad / kTileRows;
-  p.pieces = z.BH * p.ranges * (p.key_major ? p.k_tiles : 1);
+  p.key_major = ws.plan.key_major;
+  p.run = ws.plan.run;
+  p.ranges = ws.plan.ranges;
+  p.range_tiles = p.q_tiles / p.ranges;
+  p.range_rest = p.q_tiles % p.ranges;
+  p.pieces = p.key_major ? z.BH * p.ranges * p.k_tiles : 0;
+  p.dkv_whole = ws.dkv_whole;
   p.zero_dq = p.key_major;
   p.wide_dq = wide_rows(dq, d);
   p.wide_dkv = wide_rows(dk, d) && wide_rows(dv, d);

@@ -273,10 +273,14 @@ struct XattnBwdParams {
   __nv_bfloat16* dk;
   __nv_bfloat16* dv;
   int BH, heads, M, M_pad, S, S_pad, d;  // _pad: rounded up to kTileRows
-  bool key_major;      // a piece of work is one key tile, else a range of query tiles
-  int ranges, k_tiles; // ranges of a head's query tiles; key tiles of S states
-  int range_tiles, range_rest;  // query tiles of a range, one more in the first range_rest
-  int pieces;          // BH * ranges, key-major times k_tiles
+  int samples;         // BH / heads (without kv_len one of BH heads, which is the same)
+  int q_tiles, k_tiles;  // of a head's rows; of S states
+  bool key_major;      // a piece of work is one key tile, else a run of query tiles
+  int run;             // query-major: query tiles of a run at most
+  int ranges;          // key-major: ranges of a head's query tiles,
+  int range_tiles, range_rest;  // of range_tiles each, one more in the first range_rest
+  int pieces;          // key-major: BH * ranges * k_tiles
+  bool dkv_whole;      // one sweep makes all of a key tile's dK and dV
   bool zero_dq;        // dq_acc is only added to
   bool wide_dq, wide_dkv;  // every row of the outputs starts at a multiple of 32 bytes
   float scale, scale_log2;
@@ -284,7 +288,7 @@ struct XattnBwdParams {
   float* delta;        // [BH, M_pad]
   float* bias;         // [BH, M_pad, 8] (d = 64)
   float* dq_acc;       // [BH, M_pad, D]
-  float* dkv_acc;      // [2, BH, S_pad, D] where ranges > 1: dK, then dV
+  float* dkv_acc;      // [2, BH, S_pad, D] unless dkv_whole: dK, then dV
   long long dkv_float4s;  // its size
   unsigned* status;
   unsigned long long budget_ns;

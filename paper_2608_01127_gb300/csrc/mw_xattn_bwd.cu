@@ -3,11 +3,13 @@
 //
 // A sweep takes one key tile through a range of query tiles, with dK and dV of the
 // tile in tensor memory; dQ of every step goes out.  Two orders:
-//   query-major  a piece of work is a range of query tiles, taken through all key tiles
-//                of its head: few states, whose key tiles alone would not fill the
-//                SMs.  The first key tile's dQ is stored, the others' added while the
-//                range is still in L2 (and with one key tile dQ is written as it is);
-//                dK and dV are added to accumulators at the end of a sweep.
+//   query-major  a piece of work is a run of query tiles, taken through all key tiles of
+//                its head: few states, whose key tiles alone would not fill the SMs.
+//                Every CTA takes an equal share of all steps.  The first key tile's
+//                dQ is stored, the others' added while the run is still in L2, the
+//                last one's (d = 64) written in bf16 (with one key tile dQ is
+//                written as it is); dK and dV are added to accumulators at the end of
+//                a sweep.
 //   key-major    a piece is one key tile, taken through all query tiles (or a few
 //                ranges of them): many states.  The key tiles of a head run side by side,
 //                so that dQ is added up in L2; dK and dV are written as they are.
@@ -42,7 +44,8 @@ struct Layout {
   static constexpr int KTILE = REG * KREGION;
   static constexpr int QTILE = REG * QREGION;
   static constexpr int QSTAGES = (D == 64) ? 3 : 2;
-  static constexpr int DOSTAGES = (D == 64) ? 3 : 1;
+  static constexpr int DOSTAGES = (D == 64) ? 2 : 1;
+  static constexpr int KBUFS = (D == 64) ? 2 : 1;    // K tiles: the next sweep's S while dQ ends this one
   static constexpr int DS_BYTES = (QN / 64) * KREGION;  // dS^T: 128 key rows x QN columns
   static constexpr int DS_BUFS = (D == 64) ? 2 : 1;
   static constexpr int BOX_BYTES = 32 * 32 * 4;
@@ -53,7 +56,7 @@ struct Layout {
   static constexpr int VEC_BYTES = FOLD ? 0 : QN * 4;
   static constexpr int ONES_BYTES = FOLD ? 512 : 0;
   static constexpr int OFF_K = 0;
-  static constexpr int OFF_V = OFF_K + KTILE;
+  static constexpr int OFF_V = OFF_K + KBUFS * KTILE;
   static constexpr int OFF_Q = OFF_V + KTILE;
   static constexpr int OFF_DO = OFF_Q + QSTAGES * QSTRIDE;
   static constexpr int OFF_DS = OFF_DO + DOSTAGES * QTILE;
@@ -62,8 +65,10 @@ struct Layout {
   static constexpr int OFF_DELTA = OFF_LSE + QSTAGES * VEC_BYTES;
   static constexpr int OFF_ONES = OFF_DELTA + 2 * VEC_BYTES;
   static constexpr int OFF_BAR = OFF_ONES + ONES_BYTES;
-  static constexpr int NBAR = 6 + 2 * (QSTAGES + DOSTAGES) + 9 + 2 * DS_BUFS;
-  static constexpr int OFF_MISC = OFF_BAR + NBAR * 8;
+  static constexpr int SLOTS = 4;  // sweeps announced ahead
+  static constexpr int NBAR = 3 * KBUFS + 3 + 2 * (QSTAGES + DOSTAGES) + 9 + 2 * DS_BUFS + 2 * SLOTS;
+  static constexpr int OFF_SLOTS = (OFF_BAR + NBAR * 8 + 15) / 16 * 16;
+  static constexpr int OFF_MISC = OFF_SLOTS + SLOTS * 32;
   static constexpr int BYTES = OFF_MISC + 16;
   // d = 128 has no room for S^T, dP^T, P^T and dQ^T in columns of their own: P^T
   // overwrites S^T and dQ^T overwrites dP^T (each is in registers by then)
@@ -86,62 +91,99 @@ struct Layout {
   static_assert(BYTES <= 232448, "shared memory");
 };
 
-// The sweeps of a CTA in turn: a key tile against a range of query tiles each.
-// Every role walks through the same ones.  A piece of work is, query-major, a range
-// of query tiles with all key tiles of its head; key-major, one key tile.
-struct Walk {
-  const XattnBwdParams& p;
-  int next;         // index of the next piece
-  int bh, q0, n_q;  // head, first query tile and query tiles of the piece
-  int len, sample;  // valid states of the head's sample
-  int kt, k_end;    // key tile; where the piece's end
-  int n_kt;         // key tiles of the sample
-  __device__ explicit Walk(const XattnBwdParams& p_)
-      : p(p_), next(blockIdx.x), len(p_.S), sample(-1), kt(0), k_end(0) {}
-  // the next piece, with keys or not
-  __device__ __forceinline__ bool piece() {
-    if (next >= p.pieces) return false;
-    int x = next;
-    next += gridDim.x;
-    kt = 0;
-    if (p.key_major) {
-      kt = x % p.k_tiles;
-      x /= p.k_tiles;
-    }
-    bh = x / p.ranges;
-    const int r = x - bh * p.ranges;
-    if (p.kv_len) {
-      const int s = bh / p.heads;
-      if (s != sample) {
-        sample = s;
-        // (all lanes read the same; the reduction tells the compiler, which then
-        // holds what follows from it in uniform registers: 100 -> 87 KB of code)
-        len = min(max(__reduce_max_sync(__activemask(), p.kv_len[s]), 0), p.S);
-      }
-    }
-    q0 = r * p.range_tiles + min(r, p.range_rest);
-    n_q = p.range_tiles + (r < p.range_rest);
-    n_kt = (len + kTileRows - 1) / kTileRows;
-    k_end = p.key_major ? min(kt + 1, n_kt) : n_kt;
-    return true;
-  }
-  __device__ __forceinline__ bool step() {
-    if (++kt < k_end) return true;
-    while (piece())
-      if (kt < k_end) return true;
-    return false;
-  }
-  // first row of the sweep's j-th query tile: key-major, each key tile starts at its
-  // own offset, so that those of one head side by side reduce into different dQ
-  // tiles instead of contending for the same L2 lines
-  __device__ __forceinline__ int query_row(int j) const {
-    const int rot = p.key_major ? kt % n_q : 0;
+// A sweep as the producer announces it to the other roles: a key tile against a run of
+// query tiles.
+struct Sweep {
+  int bh;           // head; below 0: no more
+  int q0, n_q;      // first query tile, query tiles
+  int kt, n_kt;     // key tile; key tiles of the head's sample
+  int len;          // its valid states
+  // first row of the j-th query tile: key-major, each key tile starts at its own
+  // offset, so that those of one head side by side reduce into different dQ tiles
+  // instead of contending for the same L2 lines
+  __device__ __forceinline__ int query_row(int j, bool key_major) const {
+    const int rot = key_major ? kt % n_q : 0;
     int t = j + rot;
     if (t >= n_q) t -= n_q;
     return (q0 + t) * kTileRows;
   }
   // the key tile has rows that count as nothing but may hold anything
-  __device__ __forceinline__ bool ragged() const { return (kt + 1) * kTileRows > len && len < p.S; }
+  __device__ __forceinline__ bool ragged(int S) const { return (kt + 1) * kTileRows > len && len < S; }
+};
+
+__device__ __forceinline__ int valid_states(const XattnBwdParams& p, int sample) {
+  return p.kv_len ? min(max(p.kv_len[sample], 0), p.S) : p.S;
+}
+
+// The sweeps of this CTA in turn (one thread).
+struct Plan {
+  const XattnBwdParams& p;
+  Sweep w;
+  int k_end = 0;       // of the piece in work
+  // query-major: units (query tiles of heads) of a sample count as its key tiles; the
+  // CTA's share of all that is [at, end), from unit `unit` of `sample` on
+  long long at = 0, end = 0, before = 0;  // before: what the samples before count
+  int sample = 0, unit = 0, unit_end = 0;
+  bool begun = false;
+  // key-major: pieces of (head, range, key tile)
+  int next;
+  __device__ explicit Plan(const XattnBwdParams& p_) : p(p_), next(blockIdx.x) {
+    w.kt = 0;
+    if (p.key_major) return;
+    long long total = 0;
+    for (int b = 0; b < p.samples; ++b) total += weight(b);
+    at = total * blockIdx.x / gridDim.x;
+    end = total * (blockIdx.x + 1) / gridDim.x;
+  }
+  __device__ __forceinline__ int units() const { return p.heads * p.q_tiles; }
+  __device__ __forceinline__ int key_tiles(int b) const { return (valid_states(p, b) + kTileRows - 1) / kTileRows; }
+  __device__ __forceinline__ long long weight(int b) const { return static_cast<long long>(units()) * key_tiles(b); }
+  __device__ bool query_piece() {
+    while (unit >= unit_end) {  // on to the sample in which the share goes on
+      if (begun) {
+        before += weight(sample);
+        ++sample;
+      }
+      begun = true;
+      if (sample >= p.samples || before >= end) return false;
+      const int n = key_tiles(sample);
+      const long long all = weight(sample);
+      if (n == 0 || before + all <= at) continue;
+      unit = at > before ? static_cast<int>((at - before) / n) : 0;
+      unit_end = end < before + all ? static_cast<int>((end - before) / n) : units();
+    }
+    const int h = unit / p.q_tiles;
+    w.bh = sample * p.heads + h;
+    w.q0 = unit - h * p.q_tiles;
+    w.len = valid_states(p, sample);
+    w.n_kt = (w.len + kTileRows - 1) / kTileRows;
+    // what is left of the head, in equal runs that stay in L2
+    const int left = min(p.q_tiles - w.q0, unit_end - unit);
+    const int runs = w.n_kt == 1 ? 1 : (left + p.run - 1) / p.run;
+    w.n_q = (left + runs - 1) / runs;
+    unit += w.n_q;
+    w.kt = 0;
+    k_end = w.n_kt;
+    return true;
+  }
+  __device__ bool key_piece() {
+    while (next < p.pieces) {
+      int x = next;
+      next += gridDim.x;
+      w.kt = x % p.k_tiles;
+      x /= p.k_tiles;
+      w.bh = x / p.ranges;
+      const int r = x - w.bh * p.ranges;
+      w.q0 = r * p.range_tiles + min(r, p.range_rest);
+      w.n_q = p.range_tiles + (r < p.range_rest);
+      w.len = valid_states(p, w.bh / p.heads);
+      w.n_kt = (w.len + kTileRows - 1) / kTileRows;
+      k_end = w.kt + 1;
+      if (w.kt < w.n_kt) return true;
+    }
+    return false;
+  }
+  __device__ bool step() { return ++w.kt < k_end || (p.key_major ? key_piece() : query_piece()); }
 };
 
 template <int D, int DM>
@@ -165,10 +207,11 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
     if (threadIdx.x == 0) atomicOr(p.status, kDevMisaligned);
     return;  // uniform across the CTA, before any barrier or TMEM use
   }
+  constexpr int NK = L::KBUFS;
   uint64_t* k_full = reinterpret_cast<uint64_t*>(smem + L::OFF_BAR);
-  uint64_t* k_raw = k_full + 1;   // a K tile that warp 15 makes ready, then k_full
-  uint64_t* k_empty = k_raw + 1;
-  uint64_t* v_full = k_empty + 1;
+  uint64_t* k_raw = k_full + NK;   // a K tile that warp 15 makes ready, then k_full
+  uint64_t* k_empty = k_raw + NK;
+  uint64_t* v_full = k_empty + NK;
   uint64_t* v_raw = v_full + 1;
   uint64_t* v_empty = v_raw + 1;
   uint64_t* q_full = v_empty + 1;
@@ -186,6 +229,8 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
   uint64_t* dkv_free = dkv_full + 1;
   uint64_t* p_ready = dkv_free + 1;
   uint64_t* ds_free = p_ready + NB;
+  uint64_t* w_full = ds_free + NB;         // a sweep is announced, and
+  uint64_t* w_empty = w_full + L::SLOTS;   // read by all roles
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + L::OFF_MISC);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + L::OFF_MISC + 4);
 
@@ -202,9 +247,15 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
     }
   }
   if (threadIdx.x == 0) {
-    mbar_init(k_full, 1);
-    mbar_init(k_raw, 1);
-    mbar_init(k_empty, 2);
+    for (int b = 0; b < NK; ++b) {
+      mbar_init(&k_full[b], 1);
+      mbar_init(&k_raw[b], 1);
+      mbar_init(&k_empty[b], 2);
+    }
+    for (int b = 0; b < L::SLOTS; ++b) {
+      mbar_init(&w_full[b], 1);
+      mbar_init(&w_empty[b], 15);  // the other warps
+    }
     mbar_init(v_full, 1);
     mbar_init(v_raw, 1);
     mbar_init(v_empty, 1);
@@ -249,7 +300,25 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
   uint8_t* sDS = smem + L::OFF_DS;
   float* sLSE = reinterpret_cast<float*>(smem + L::OFF_LSE);
   float* sDelta = reinterpret_cast<float*>(smem + L::OFF_DELTA);
-  Walk w(p);
+  int4* slots = reinterpret_cast<int4*>(smem + L::OFF_SLOTS);
+  // The next sweep, for a whole warp (its fields agree over the lanes: the shuffles tell
+  // the compiler, which then works in uniform registers).
+  int turn = 0;
+  Sweep w;
+  auto next_sweep = [&]() {
+    const int slot = turn % L::SLOTS;
+    if (!warp_wait(&w_full[slot], (turn / L::SLOTS) & 1, ctl)) return false;
+    ++turn;
+    const int4 a = slots[2 * slot], b = slots[2 * slot + 1];
+    w.bh = __shfl_sync(0xffffffffu, a.x, 0);
+    w.q0 = __shfl_sync(0xffffffffu, a.y, 0);
+    w.n_q = __shfl_sync(0xffffffffu, a.z, 0);
+    w.kt = __shfl_sync(0xffffffffu, a.w, 0);
+    w.n_kt = __shfl_sync(0xffffffffu, b.x, 0);
+    w.len = __shfl_sync(0xffffffffu, b.y, 0);
+    if (lane == 0) mbar_arrive(&w_empty[slot]);
+    return w.bh >= 0;
+  };
 
   if (warp >= 12) {
   regs_dec<L::REGS_CONTROL>();
@@ -258,9 +327,11 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
     if (lane == 0) {
       prefetch_tmap(&tm_q);
       prefetch_tmap(&tm_do);
-      int sw = 0, raws = 0, n_q = 0, n_do = 0;  // sweeps, those through warp 15, Q and dO tiles so far
+      int sw = 0, raws = 0, n_q = 0, n_do = 0;  // K tiles, V tiles through warp 15, Q and dO tiles so far
       int n_v = 0;                              // V tiles (one a sweep, loaded ahead of K)
+      uint32_t k_raws = 0, k_was_raw = 0;       // per K buffer: parity of those through warp 15; the last one was
       bool ok = true, raw = false;
+      Plan plan(p);
       auto load_q = [&](int q) {
         const int st = n_q % NQ;
         if (!mbar_wait(&q_empty[st], ((n_q / NQ) & 1) ^ 1, ctl)) return false;
@@ -287,30 +358,56 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
         ++n_do;
         return true;
       };
-      while (ok && w.step()) {
-        raw = w.ragged();
-        // Q, dO and V of the sweep's first step ahead of K, which waits for the last dQ
-        // of the sweep before
-        if (!(ok = load_q(w.query_row(0)))) break;
-        if (!(ok = mbar_wait(v_empty, (sw & 1) ^ 1, ctl))) break;
+      for (;; ++turn) {
+        const int slot = turn % L::SLOTS;
+        if (!(ok = mbar_wait(&w_empty[slot], ((turn / L::SLOTS) & 1) ^ 1, ctl))) break;
+        const bool more = plan.step();
+        if (!more) plan.w.bh = -1;
+        w = plan.w;
+        slots[2 * slot] = make_int4(w.bh, w.q0, w.n_q, w.kt);
+        slots[2 * slot + 1] = make_int4(w.n_kt, w.len, 0, 0);
+        mbar_arrive(&w_full[slot]);  // (releases the stores above)
+        if (!more) break;
+        raw = w.ragged(p.S);
+        const int kb = sw % NK;
+        // Q, dO and V of the sweep's first step; K (one buffer) waits for the last dQ of
+        // the sweep before
+        if (!(ok = load_q(w.query_row(0, p.key_major)))) break;
         auto load_tile = [&](uint8_t* dst, const CUtensorMap* map, uint64_t* bar) {
           mbar_arrive_expect_tx(bar, L::KTILE);
           for (int r = 0; r < L::REG; ++r)
             tma_load_3d(dst + r * L::KREGION, map, bar, 64 * r, w.kt * kTileRows, w.bh);
         };
+        auto load_k = [&]() {
+          if (!mbar_wait(&k_empty[kb], ((sw / NK) & 1) ^ 1, ctl)) return false;
+          load_tile(sK + kb * L::KTILE, &tm_k, raw ? &k_raw[kb] : &k_full[kb]);
+          if (raw) k_raws ^= 1u << kb;
+          k_was_raw = (k_was_raw & ~(1u << kb)) | (raw ? 1u << kb : 0u);
+          ++sw;
+          return true;
+        };
+        if (NK > 1 && !(ok = load_k())) break;
+        if (!(ok = mbar_wait(v_empty, (n_v & 1) ^ 1, ctl))) break;
         load_tile(sV, &tm_v, raw ? v_raw : v_full);
         ++n_v;
         raws += raw;
-        if (!(ok = load_do(w.query_row(0)))) break;
-        if (!(ok = mbar_wait(k_empty, (sw & 1) ^ 1, ctl))) break;
-        load_tile(sK, &tm_k, raw ? k_raw : k_full);
-        ++sw;
-        for (int j = 1; ok && j < w.n_q; ++j) ok = load_q(w.query_row(j)) && load_do(w.query_row(j));
+        if (!(ok = load_do(w.query_row(0, p.key_major)))) break;
+        if (NK == 1 && !(ok = load_k())) break;
+        for (int j = 1; ok && j < w.n_q; ++j)
+          ok = load_q(w.query_row(j, p.key_major)) && load_do(w.query_row(j, p.key_major));
+        if (!ok) break;
       }
       if (*abort_flag || !ok) {
         // let every copy this CTA started land before shared memory goes away
-        if (n_v > 0) drain_wait(raw ? v_raw : v_full, ((raw ? raws : n_v) - 1) & 1, p.budget_ns);
-        if (sw > 0 && sw == n_v) drain_wait(raw ? k_raw : k_full, ((raw ? raws : sw) - 1) & 1, p.budget_ns);
+        for (int i = max(0, sw - NK); i < sw; ++i) {
+          const int kb = i % NK;
+          if ((k_was_raw >> kb) & 1)
+            drain_wait(&k_raw[kb], ((k_raws >> kb) & 1) ^ 1, p.budget_ns);
+          else
+            drain_wait(&k_full[kb], (i / NK) & 1, p.budget_ns);
+        }
+        // (a sweep whose V is not loaded yet leaves the one before, which has been read)
+        if (n_v > 0 && (NK == 1 || n_v == sw)) drain_wait(raw ? v_raw : v_full, ((raw ? raws : n_v) - 1) & 1, p.budget_ns);
         for (int j = max(0, n_q - NQ); j < n_q; ++j) drain_wait(&q_full[j % NQ], (j / NQ) & 1, p.budget_ns);
         for (int j = max(0, n_do - ND); j < n_do; ++j) drain_wait(&do_full[j % ND], (j / ND) & 1, p.budget_ns);
       }
@@ -348,8 +445,8 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
         umma_ss(tmem + d_col, sdesc_add(a, ka), sdesc_add(b, kq), idesc_s, kk > 0 ? 1u : 0u);
       }
     };
-    auto issue_s = [&](int g) {
-      issue_kmajor(L::S_COL, k_kmaj, sdesc_add(q_kmaj0, (g % NQ) * L::QSTRIDE));
+    auto issue_s = [&](int g, uint32_t k_off) {
+      issue_kmajor(L::S_COL, sdesc_add(k_kmaj, k_off), sdesc_add(q_kmaj0, (g % NQ) * L::QSTRIDE));
       add_bias(L::S_COL, ones_l, g % NQ);
       umma_commit(s_full);
     };
@@ -378,22 +475,24 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
         umma_ss(tmem + L::DK_COL, sdesc_add(ds_kmaj, (kk >> 2) * L::KREGION + (kk & 3) * 32),
                 sdesc_add(q_mn, kk * 2048), idesc_tn, (acc || kk > 0) ? 1u : 0u);
     };
-    auto issue_dq = [&](int g) {
+    auto issue_dq = [&](int g, uint32_t k_off) {
+      const uint32_t k_mn0 = sdesc_add(k_mn, k_off);
       const uint32_t ds_mn = sdesc_add(ds_mn0, (g % NB) * L::DS_BYTES);
 #pragma unroll
       for (int kk = 0; kk < kTileRows / 16; ++kk) {
         if constexpr (L::DQT)
-          umma_ss(tmem + L::DQ_COL, sdesc_add(k_mn, kk * 2048), sdesc_add(ds_mn, kk * 2048), idesc_dq,
+          umma_ss(tmem + L::DQ_COL, sdesc_add(k_mn0, kk * 2048), sdesc_add(ds_mn, kk * 2048), idesc_dq,
                   kk > 0 ? 1u : 0u);
         else
-          umma_ss(tmem + L::DQ_COL, sdesc_add(ds_mn, kk * 2048), sdesc_add(k_mn, kk * 2048), idesc_dq,
+          umma_ss(tmem + L::DQ_COL, sdesc_add(ds_mn, kk * 2048), sdesc_add(k_mn0, kk * 2048), idesc_dq,
                   kk > 0 ? 1u : 0u);
       }
     };
     bool ok = true;
     int g = 0, sw = 0;  // steps and sweeps so far
-    while (ok && w.step()) {
-      if (!(ok = warp_wait(k_full, sw & 1, ctl))) break;
+    while (ok && next_sweep()) {
+      const uint32_t k_off = (sw % NK) * L::KTILE;  // this sweep's K
+      if (!(ok = warp_wait(&k_full[sw % NK], (sw / NK) & 1, ctl))) break;
       // the last sweep's dK and dV are out of tensor memory
       auto wait_dkv = [&]() { return sw == 0 || warp_wait(dkv_free, (sw - 1) & 1, ctl); };
       if (role_a) {
@@ -422,7 +521,7 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
             if (!(ok = warp_wait(&q_full[g % NQ], (g / NQ) & 1, ctl))) break;
             if (g > 0 && !(ok = warp_wait(s_free, (g - 1) & 1, ctl))) break;
             tc_fence_after();
-            issue_s(g++);
+            issue_s(g++, k_off);
           }
           if (j >= 0) {
             const int x = L::PAIRED || !more ? g - 1 : g - 2;  // the step in work
@@ -436,7 +535,7 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
           if constexpr (L::PAIRED) {
             if (!(ok = warp_wait(&q_full[g % NQ], (g / NQ) & 1, ctl))) break;
             tc_fence_after();
-            issue_s(g++);
+            issue_s(g++, k_off);
           } else {
             if (j < 0 && !(ok = warp_wait(v_full, sw & 1, ctl))) break;
             if (!(ok = next_dp(g - 1))) break;
@@ -451,7 +550,7 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
           if constexpr (!L::PAIRED)
             if (g > 0 && !(ok = warp_wait(dq_free, (g - 1) & 1, ctl))) break;
           tc_fence_after();
-          issue_dq(g);
+          issue_dq(g, k_off);
           umma_commit(dq_full);
           if (j == 0) {
             if (!(ok = wait_dkv())) break;
@@ -464,45 +563,51 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
       }
       if (!ok) break;
       umma_commit(dkv_full);  // one arrival per issuing warp
-      umma_commit(k_empty);
+      umma_commit(&k_empty[sw % NK]);
       ++sw;
     }
   } else {
     // ------------------------------------------------------------ what has no key to it
-    // Gradients that no sweep writes: dQ of samples without states, and dK and dV of
-    // tiles past them where each tile's one sweep writes them whole.
-    Walk z(p);
-    auto zero_rows = [&](__nv_bfloat16* out, int rows, int row0, int count) {
-      const int n = min(count, rows - row0) * (p.d / 8);
-      uint4* dst = reinterpret_cast<uint4*>(out + (static_cast<size_t>(z.bh) * rows + row0) * p.d);
-      for (int i = lane; i < n; i += 32) dst[i] = make_uint4(0u, 0u, 0u, 0u);
+    // Gradients that no sweep writes: dQ of samples without states, and dK and dV past
+    // the key tiles where each tile's one sweep writes them whole.  Row by row of
+    // pieces, over all CTAs.
+    auto zero_rows = [&](__nv_bfloat16* out, long long row0, long long row1) {
+      uint4* dst = reinterpret_cast<uint4*>(out);
+      const long long i1 = row1 * (p.d / 8);
+      for (long long i = row0 * (p.d / 8) + blockIdx.x * 32 + lane; i < i1; i += gridDim.x * 32)
+        dst[i] = make_uint4(0u, 0u, 0u, 0u);
     };
-    while (z.piece()) {
-      if (z.n_kt == 0 && z.kt == 0) zero_rows(p.dq, p.M, z.q0 * kTileRows, z.n_q * kTileRows);
-      if (p.ranges == 1)
-        for (int t = p.key_major ? z.kt : 0; t < (p.key_major ? z.kt + 1 : p.k_tiles); ++t)
-          if (t >= z.n_kt) {
-            zero_rows(p.dk, p.S, t * kTileRows, kTileRows);
-            zero_rows(p.dv, p.S, t * kTileRows, kTileRows);
-          }
+    for (int b = 0; b < p.samples; ++b) {
+      const int n = (valid_states(p, b) + kTileRows - 1) / kTileRows;
+      const long long h0 = static_cast<long long>(b) * p.heads, h1 = h0 + p.heads;
+      if (n == 0) zero_rows(p.dq, h0 * p.M, h1 * p.M);
+      if (p.dkv_whole && n < p.k_tiles)
+        for (long long h = h0; h < h1; ++h) {
+          zero_rows(p.dk, h * p.S + n * kTileRows, (h + 1) * p.S);
+          zero_rows(p.dv, h * p.S + n * kTileRows, (h + 1) * p.S);
+        }
     }
     // ------------------------------------------------------------ ragged K and V tiles
-    int raws = 0;
+    int v_raws = 0, sw = 0;
+    uint32_t k_raws = 0;
     bool ok = true;
-    while (ok && w.step()) {
-      if (!w.ragged()) continue;
+    for (; ok && next_sweep(); ++sw) {
+      if (!w.ragged(p.S)) continue;
+      const int kb = sw % NK;
       const int limit = w.len - w.kt * kTileRows;
-      for (int m = 0; ok && m < 2; ++m) {  // V is loaded first
-        if (!(ok = warp_wait(m == 0 ? v_raw : k_raw, raws & 1, ctl))) break;
-        uint8_t* tile = m == 0 ? sV : sK;
+      for (int m = 0; ok && m < 2; ++m) {  // in the order of the loads
+        const bool is_k = (m == 0) == (NK > 1);
+        if (!(ok = is_k ? warp_wait(&k_raw[kb], (k_raws >> kb) & 1, ctl) : warp_wait(v_raw, v_raws & 1, ctl))) break;
+        uint8_t* tile = is_k ? sK + kb * L::KTILE : sV;
         for (int i = limit * 8 + lane; i < kTileRows * 8; i += 32)
           for (int r = 0; r < L::REG; ++r)
             *reinterpret_cast<uint4*>(tile + r * L::KREGION + i * 16) = make_uint4(0u, 0u, 0u, 0u);
         fence_proxy_async_smem();  // the tensor core reads the tile next
         __syncwarp();
-        if (lane == 0) mbar_arrive(m == 0 ? v_full : k_full);
+        if (lane == 0) mbar_arrive(is_k ? &k_full[kb] : v_full);
       }
-      ++raws;
+      k_raws ^= 1u << kb;
+      ++v_raws;
     }
   }
   } else if (warp < 8) {
@@ -522,7 +627,7 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
     const int sw = j_local & 7;
     bool ok = true;
     int g = 0;
-    while (ok && w.step()) {
+    while (ok && next_sweep()) {
     const bool k_valid = w.kt * kTileRows + j_local < w.len;
     const bool some_invalid = !__all_sync(0xffffffffu, k_valid);
     for (int j = 0; j < w.n_q; ++j, ++g) {
@@ -669,18 +774,20 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
     };
     bool ok = true;
     int g = 0, sw = 0;
-    while (ok && w.step()) {
+    while (ok && next_sweep()) {
       // dQ of a step: whole, where the sample has one key tile; else, query-major, the
       // first key tile's is stored and the others' added (the stores are complete by
-      // then); key-major all are added to zeros
+      // then), the last one's on its way out (d = 64); key-major all are added to zeros
       const bool whole = w.n_kt == 1;
       const bool add = p.key_major || w.kt > 0;
-      if (!p.key_major && w.kt == 1) {
+      const bool finish = !L::DQT && !p.key_major && !whole && w.kt == w.n_kt - 1;
+      if (!p.key_major && (w.kt == 1 || finish)) {
         if (lane == 0) bulk_wait_all();
+        fence_proxy_async();  // what the TMA unit has written is read below
         __syncwarp();
       }
       for (int j = 0; j < w.n_q; ++j, ++g) {
-        const int q0 = w.query_row(j);
+        const int q0 = w.query_row(j, p.key_major);
         if (!(ok = warp_wait(dq_full, g & 1, ctl))) break;
         tc_fence_after();
         if constexpr (L::DQT) {
@@ -752,6 +859,14 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
         } else {
           // lanes = query rows
           static_assert(D == 64 || L::DQT, "the drain below covers two 32-column boxes");
+          const int row = q0 + wq * 32;
+          auto store_rows = [&](const uint32_t (&r)[32], int c) {
+            float v[32];
+#pragma unroll
+            for (int k = 0; k < 32; ++k) v[k] = __uint_as_float(r[k]) * p.scale;
+            if (row + lane < p.M)
+              store_row32(p.dq + (static_cast<size_t>(w.bh) * p.M + row + lane) * D + 32 * c, v, 4, p.wide_dq);
+          };
           uint32_t r[2][32];
           tmem_ld32(lane_base + L::DQ_COL, r[0]);
           tmem_ld32(lane_base + L::DQ_COL + 32, r[1]);
@@ -759,17 +874,30 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
           tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(dq_free);  // dQ is in registers
-          const int row = q0 + wq * 32;
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
-            if (!whole) {
-              put_rows(&tm_dq, r[c], 32 * c, row, add);
-            } else if (row + lane < p.M) {
-              float v[32];
+            if (finish) {
+              const float4* acc = reinterpret_cast<const float4*>(
+                  p.dq_acc + (static_cast<size_t>(w.bh) * p.M_pad + row + lane) * D + 32 * c);
 #pragma unroll
-              for (int k = 0; k < 32; ++k) v[k] = __uint_as_float(r[c][k]) * p.scale;
-              store_row32(p.dq + (static_cast<size_t>(w.bh) * p.M + row + lane) * D + 32 * c, v, 4, p.wide_dq);
+              for (int h = 0; h < 2; ++h) {
+                float4 x[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) x[k] = __ldcg(acc + 4 * h + k);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                  const int e = 16 * h + 4 * k;
+                  r[c][e] = __float_as_uint(__uint_as_float(r[c][e]) + x[k].x);
+                  r[c][e + 1] = __float_as_uint(__uint_as_float(r[c][e + 1]) + x[k].y);
+                  r[c][e + 2] = __float_as_uint(__uint_as_float(r[c][e + 2]) + x[k].z);
+                  r[c][e + 3] = __float_as_uint(__uint_as_float(r[c][e + 3]) + x[k].w);
+                }
+              }
             }
+            if (whole || finish)
+              store_rows(r[c], c);
+            else
+              put_rows(&tm_dq, r[c], 32 * c, row, add);
           }
           __syncwarp();
         }
@@ -792,7 +920,7 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
           if (lane == 0) mbar_arrive(dkv_free);
         }
         if (32 * c >= p.d) continue;
-        if (p.ranges > 1) {
+        if (!p.dkv_whole) {
           put_rows(is_dk ? &tm_dk : &tm_dv, r, 32 * c, row, true);
         } else if (row + lane < p.S) {
           const float mul = is_dk ? p.scale : 1.f;
@@ -880,7 +1008,7 @@ __global__ void __launch_bounds__(256) xattn_pre_kernel(const XattnBwdParams p) 
 }
 
 // bf16 rows from the accumulators: dQ of samples with several key tiles (the others'
-// is written already), dK and dV where several ranges add to them.  8 columns a
+// is written already), dK and dV where several sweeps add to them.  8 columns a
 // thread; blockIdx.y 0: dQ, 1: dK, 2: dV.
 template <int D>
 __global__ void __launch_bounds__(256) xattn_post_kernel(const XattnBwdParams p, int first) {
@@ -921,7 +1049,8 @@ cudaError_t launch(const XattnBwdMaps& m, const XattnBwdParams& p, int dev, int 
     return cudaFuncSetAttribute(xattn_bwd_kernel<D, DM>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::BYTES);
   });
   if (e != cudaSuccess) return e;
-  const unsigned grid = static_cast<unsigned>(p.pieces < sms ? p.pieces : sms);
+  const long long work = p.key_major ? p.pieces : static_cast<long long>(p.BH) * p.q_tiles;
+  const unsigned grid = static_cast<unsigned>(work < sms ? work : sms);
   const long long rows = static_cast<long long>(p.BH) * p.M_pad;
   constexpr int kBlockRows = 256 / (D / 8);
   const long long pre = (rows + kBlockRows - 1) / kBlockRows + (p.dkv_float4s + 1023) / 1024;
@@ -929,7 +1058,7 @@ cudaError_t launch(const XattnBwdMaps& m, const XattnBwdParams& p, int dev, int 
   xattn_bwd_kernel<D, DM><<<grid, L::THREADS, L::BYTES, s>>>(m.q, m.k, m.v, m.dout, m.dq, m.dk, m.dv, m.bias,
                                                              m.dq_out, p);
   // what several sweeps add to becomes bf16
-  const int first = p.k_tiles > 1 ? 0 : 1, last = p.ranges > 1 ? 3 : 1;
+  const int first = p.k_tiles > 1 && (p.key_major || D == 128) ? 0 : 1, last = p.dkv_whole ? 1 : 3;
   if (first < last) {
     const long long most = static_cast<long long>(p.BH) * (first == 0 && p.M > p.S ? p.M : last > 1 ? p.S : p.M) *
                            (p.d / 8);
