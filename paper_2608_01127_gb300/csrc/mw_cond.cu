@@ -1,6 +1,7 @@
 // C ABI of the conditioning path (declared in include/mw_bca.h): cross attention
 // to an encoder's states and layer norm.  As in mw_abi.cu, arguments are checked
 // on the host before any CUDA call.
+#include <algorithm>
 #include <climits>
 #include <cmath>
 
@@ -60,8 +61,15 @@ size_t xattn_ws(const XattnSizes& z, int S, int d) {
   return align256(rows * kernel_d(d) * sizeof(float)) + align256(rows * sizeof(float));
 }
 
-// The order of the backward's work, from a model of the time (us): steps of t, a sweep's
-// start and end, and the accumulators' way through HBM.
+// The order of the backward's work, from a model of the time (us): steps of t and a
+// sweep's start and end; key-major also two passes and a quarter over dQ in HBM (zeroed,
+// read, bf16 written; written once in bf16 query-major).  Query-major a run ends after
+// few tiles, and its dQ waits for copies: a step costs more, and the first ones 6 us.  Heads x query tiles x key
+// tiles, us of all kernels, query-/key-major: d = 64 48 x 110 x 2 186 / 216, 152 x 40 x 2
+// 213 / 218, 100 x 24 x 5 202 / 190, 16 x 110 x 9 231 / 186, 64 x 3 x 2 28 / 20; d = 128,
+// where dQ could not leave with the last sweep (no shared memory for it): 48 x 110 x 2
+// 420 / 420, 152 x 40 x 2 522 / 424, 16 x 110 x 9 395 / 305, so that it is key-major from
+// two key tiles on.
 struct XattnBwdPlan {
   bool key_major = false;
   int ranges = 1;  // key-major: of a head's query tiles
@@ -69,18 +77,15 @@ struct XattnBwdPlan {
 };
 
 XattnBwdPlan xattn_bwd_plan(int BH, int q_tiles, int k_tiles, int D) {
-  const double t = D == 64 ? 1.25 : 2.2, sweep = D == 64 ? 1.0 : 2.0;
-  const double acc = 4e-6 * BH * static_cast<double>(q_tiles) * kTileRows * D / 6.5;  // us a pass
   XattnBwdPlan best;
-  best.run = D == 64 ? 8 : 4;
-  // query-major: equal shares of all steps (dQ in bf16 leaves with the last key tile at
-  // d = 64, through a pass of its own else)
-  const double tiles = std::ceil(static_cast<double>(BH) * q_tiles / kNormSms);
-  double best_cost = tiles * k_tiles * t + (k_tiles == 1 ? 1 : k_tiles * std::ceil(tiles / best.run)) * sweep +
-                     (k_tiles == 1 ? 0 : D == 64 ? 0.5 : 2.5) * acc;
-  for (int r = 1; k_tiles > 1 && r <= q_tiles && r <= 64; ++r) {
+  best.run = 16;  // 48 x 110 x 2: runs of 4 227, of 8 201, of 16 186 us
+  if (k_tiles == 1) return best;
+  const double t = D == 64 ? 1.55 : 2.25, sweep = D == 64 ? 1.0 : 2.0;
+  const double acc = 4e-6 * BH * static_cast<double>(q_tiles) * kTileRows * D / 6.5;  // us a pass
+  double best_cost = D == 64 ? ceil_div(static_cast<long long>(BH) * q_tiles, kNormSms) * k_tiles * 2.05 + 6 : INFINITY;
+  for (int r = 1; r <= q_tiles && r <= 64; ++r) {
     const double cost = ceil_div(static_cast<long long>(BH) * r * k_tiles, kNormSms) * (ceil_div(q_tiles, r) * t + sweep) +
-                        3.5 * acc;
+                        2.25 * acc;
     if (cost < best_cost) {
       best_cost = cost;
       best.key_major = true;
@@ -95,7 +100,7 @@ struct XattnBwdWs {
   int M_pad = 0, S_pad = 0;
   bool dkv_whole = false;  // no accumulators of dK and dV
   XattnBwdPlan plan;
-  size_t dq = 0, dkv = 0, dkv_bytes = 0, lse2 = 0, delta = 0, bias = 0, total = 0;
+  size_t shares = 0, dq = 0, dkv = 0, dkv_bytes = 0, lse2 = 0, delta = 0, bias = 0, total = 0;
 };
 
 XattnBwdWs xattn_bwd_ws(const XattnSizes& z, int S, int d) {
@@ -105,7 +110,9 @@ XattnBwdWs xattn_bwd_ws(const XattnSizes& z, int S, int d) {
   w.S_pad = ceil_div(S, kTileRows) * kTileRows;
   w.plan = xattn_bwd_plan(z.BH, w.M_pad / kTileRows, w.S_pad / kTileRows, D);
   const size_t rows = static_cast<size_t>(z.BH) * w.M_pad, keys = static_cast<size_t>(z.BH) * w.S_pad;
-  w.dkv = w.S_pad > kTileRows ? align256(rows * D * 4) : 0;
+  w.dq = align256((kXattnMaxCtas + 1) * sizeof(int2));
+  const bool dq_acc = w.S_pad > kTileRows;
+  w.dkv = w.dq + (dq_acc ? align256(rows * D * 4) : 0);
   w.dkv_whole = w.plan.key_major && w.plan.ranges == 1;
   w.dkv_bytes = w.dkv_whole ? 0 : 2 * keys * D * 4;
   w.lse2 = w.dkv + align256(w.dkv_bytes);
@@ -341,6 +348,7 @@ mw_status mw_xattn_bwd(const void* q, const void* k, const void* v, const int* k
   p.lse2 = at(ws.lse2);
   p.delta = at(ws.delta);
   p.bias = at(ws.bias);
+  p.shares = reinterpret_cast<int2*>(base + ws.shares);
   p.dq_acc = at(ws.dq);
   p.dkv_acc = at(ws.dkv);
   p.dkv_float4s = static_cast<long long>(ws.dkv_bytes / 16);
@@ -353,7 +361,7 @@ mw_status mw_xattn_bwd(const void* q, const void* k, const void* v, const int* k
   MW_TRY(make_map(&m.dout, dout, z.rows, z.BH, d, "dout"));
   // (maps that no launch of these sizes uses stand in for one another)
   m.dq = m.dk = m.dv = m.bias = m.dq_out = m.q;
-  if (ws.dkv > 0) MW_TRY(make_map(&m.dq, p.dq_acc, ws.M_pad, z.BH, D, "dq_acc", 32, true, d));
+  if (ws.dkv > ws.dq) MW_TRY(make_map(&m.dq, p.dq_acc, ws.M_pad, z.BH, D, "dq_acc", 32, true, d));
   if (ws.dkv_bytes > 0) {
     MW_TRY(make_map(&m.dk, p.dkv_acc, ws.S_pad, z.BH, D, "dk_acc", 32, true, d));
     MW_TRY(make_map(&m.dv, p.dkv_acc + static_cast<size_t>(z.BH) * ws.S_pad * D, ws.S_pad, z.BH, D, "dv_acc", 32,
@@ -363,7 +371,7 @@ mw_status mw_xattn_bwd(const void* q, const void* k, const void* v, const int* k
     MW_TRY(encode_bias_map(&m.bias, p.bias, ws.M_pad, z.BH, kTileRows));
   else
     MW_TRY(encode_rows_map(&m.dq_out, dq, z.rows, z.BH, d, false));
-  return launch_status(launch_xattn_bwd(D, mma_d(d), m, p, scope.device(), sm_count(), s),
+  return launch_status(launch_xattn_bwd(D, mma_d(d), m, p, scope.device(), std::min(sm_count(), kXattnMaxCtas), s),
                        "cross attention backward launch");
 }
 

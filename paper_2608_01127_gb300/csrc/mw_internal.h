@@ -264,6 +264,7 @@ cudaError_t launch_xattn_few(int d, const CUtensorMap& tk, const CUtensorMap& tv
                              cudaStream_t s);
 
 // Backward on tensor cores (mw_xattn_bwd.cu).
+constexpr int kXattnMaxCtas = 1023;
 struct XattnBwdParams {
   const int* kv_len;
   const __nv_bfloat16* o;
@@ -287,6 +288,7 @@ struct XattnBwdParams {
   float* lse2;         // [BH, M_pad] (d = 64: unused, as delta)
   float* delta;        // [BH, M_pad]
   float* bias;         // [BH, M_pad, 8] (d = 64)
+  int2* shares;        // query-major: where each CTA's share begins, and the end (sample, unit)
   float* dq_acc;       // [BH, M_pad, D]
   float* dkv_acc;      // [2, BH, S_pad, D] unless dkv_whole: dK, then dV
   long long dkv_float4s;  // its size

@@ -335,7 +335,7 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
     auto issue_qk = [&](int t, int qb, int st) {
       const uint32_t qa = sdesc_add(q_desc, (qb * QT + t) * L::TILE_BYTES);
       const uint32_t kb = sdesc_add(k_desc, st * L::TILE_BYTES);
-#pragma unroll
+#pragma unroll 4
       for (int kk = 0; kk < DM / 16; ++kk) {
         const uint32_t off = (kk >> 2) * L::REGION_BYTES + (kk & 3) * 32;
         umma_ss(tmem + L::S_COL(t), sdesc_add(qa, off), sdesc_add(kb, off), idesc_qk, kk > 0 ? 1u : 0u);
