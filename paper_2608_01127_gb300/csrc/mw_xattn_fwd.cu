@@ -11,7 +11,11 @@
 // role runs through the blocks without a stop.  The next block's Q and K/V tiles
 // are loaded, and its first S is computed, while the softmax warps finish the
 // last one; they take O into registers, hand its tensor memory back, and store
-// rows while the next block's MMAs run.
+// rows while the next block's MMAs run.  What bounds a step is the chain from S through
+// softmax and P to the next S (d = 64: 2230 cycles, of which S to registers 350, P 1600),
+// not the exponentials (1024 cycles at 32 a clock) or the MMAs (1150; d = 128 2048 of
+// 3170).  Steps of 64 keys with two S in flight were slower (d = 64 1.16 -> 1.59 us, 128
+// 1.65 -> 1.88): half of the softmax is latency that does not shrink with the step.
 //
 // Roles (384 threads):
 //   warps 0-3 / 4-7  softmax of query tile 0 / 1 (one thread per row = TMEM lane)
@@ -57,6 +61,11 @@ struct Layout {
   static constexpr bool SPLIT_P = 256 + OW * QT + 32 * QT <= 512;
   static constexpr int ISSUERS = D == 64 ? QT : 1;
   static constexpr int HELPERS = 3 - ISSUERS;
+  // A block's O leaves after the first softmax of the next block, while that one's MMAs
+  // run.  Where P overwrites all of S, S of the tile after that would wait for it: there
+  // O leaves at the end of its own block (us a step of 2 x 128 rows, blocks of two key
+  // tiles: d = 64 2.31 -> 2.18, 72 2.98 -> 2.75; 128 2.81, 2.95 if deferred)
+  static constexpr bool DEFER = SPLIT_P;
   static constexpr int SLOTS = 4;  // blocks announced ahead
   static constexpr int NBAR = 2 * QBUFS + 5 * STAGES + 5 * QT + 2 * SLOTS;
   static constexpr int OFF_SLOTS = (OFF_BAR + NBAR * 8 + 15) / 16 * 16;
@@ -335,21 +344,20 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
     auto issue_qk = [&](int t, int qb, int st) {
       const uint32_t qa = sdesc_add(q_desc, (qb * QT + t) * L::TILE_BYTES);
       const uint32_t kb = sdesc_add(k_desc, st * L::TILE_BYTES);
-#pragma unroll 4
-      for (int kk = 0; kk < DM / 16; ++kk) {
-        const uint32_t off = (kk >> 2) * L::REGION_BYTES + (kk & 3) * 32;
-        umma_ss(tmem + L::S_COL(t), sdesc_add(qa, off), sdesc_add(kb, off), idesc_qk, kk > 0 ? 1u : 0u);
+#pragma unroll
+      for (int r = 0; r < DM / 64; ++r)
+        umma_ss4<2, 2>(tmem + L::S_COL(t), sdesc_add(qa, r * L::REGION_BYTES), sdesc_add(kb, r * L::REGION_BYTES),
+                       idesc_qk, r > 0 ? 1u : 0u);
+      if constexpr (DM % 64 != 0) {
+        static_assert(DM % 64 == 0 || DM == 80, "one more slice");
+        umma_ss(tmem + L::S_COL(t), sdesc_add(qa, L::REGION_BYTES), sdesc_add(kb, L::REGION_BYTES), idesc_qk, 1u);
       }
     };
     auto issue_pv = [&](int t, int st, bool acc, int half) {
       const uint32_t vs = v_addr + st * L::TILE_BYTES;
       const uint32_t vb = sdesc_sw128(vs, L::ONES_BYTES > 0 ? ones_addr - vs : L::REGION_BYTES);
-#pragma unroll
-      for (int k4 = 0; k4 < 4; ++k4) {
-        const int kk = 4 * half + k4;
-        umma_ts(tmem + L::O_COL(t), tmem + L::P_COL(t, half) + k4 * 8, sdesc_add(vb, kk * 2048), idesc_pv,
-                (acc || kk > 0) ? 1u : 0u);
-      }
+      umma_ts4<8, 128>(tmem + L::O_COL(t), tmem + L::P_COL(t, half), sdesc_add(vb, half * 8192), idesc_pv,
+                       (acc || half > 0) ? 1u : 0u);
     };
     int nq = 0, nk = 0;       // blocks and key tiles whose S is issued
     // of this warp's query tiles (all; d = 64: one, tile t0)
@@ -488,199 +496,222 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
     const uint32_t o_addr = lane_base + L::O_COL(t);
     const float sl2 = p.scale_log2;
     int blocks = 0;  // blocks dealt with
-    int begun = 0;   // blocks of this query tile that have keys
-    int done = 0;    // their key tiles
+    int begun = 0;   // blocks of this query tile whose O is out
+    int done = 0;    // key tiles of this query tile
     int box = 0;     // the staging box whose turn it is
-    bool ok = true;
-    while ((ok = next_block())) {
+    // the block whose O has to leave, and its statistics
+    bool pending = false;
+    Block pw;
+    float pm = 0.f, pl = 0.f;
+    int pblock = 0;
+    while (true) {
+      bool ok = true;
+      const bool more = next_block();  // (at the end one more turn, for the last block's O)
+      if (!more && (*abort_flag || !pending)) break;
       const int row = w.r0 + row_local;
-      if (w.n == 0) {  // no keys
+      if (more && w.n == 0) {  // no keys
         if (row < p.M) store_nothing(w, row);
         __syncwarp();
         ++blocks;
         continue;
       }
-      if (!w.present(t, p.M)) {
+      if (more && !w.present(t, p.M)) {
         ++blocks;
         continue;
       }
+      if (!more) w.n = 1;
       float m_used = -INFINITY;
       float l = 0.f;
-      const bool idle = w.r0 + t * kTileRows + wq * 32 >= p.M;  // a warp without rows only keeps step
+      const bool idle = !more || w.r0 + t * kTileRows + wq * 32 >= p.M;  // a warp without rows only keeps step
 #pragma unroll 1
       for (int i = 0; i < w.n; ++i, ++done) {
-        if (!(ok = warp_wait(&s_full[t], done & 1, ctl))) break;
-        if (idle) {
-          if (lane == 0) {
-            mbar_arrive(&p_half[t]);
-            mbar_arrive(&p_full[t]);
+        if (more && !(ok = warp_wait(&s_full[t], done & 1, ctl))) break;
+        if (!idle) {
+          tc_fence_after();
+          float s[128];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            uint32_t r[32];
+            tmem_ld32(s_addr + 32 * c, r);
+            tmem_wait_ld();
+#pragma unroll
+            for (int k = 0; k < 32; ++k) s[32 * c + k] = __uint_as_float(r[k]);
           }
-          // (not a tile ahead of the others: their arrivals for this one count first)
-          if (L::SPLIT_P && !(ok = warp_wait(&pv_done[t], done & 1, ctl))) break;
-          continue;
-        }
-        tc_fence_after();
-        float s[128];
+          const int limit = w.len - w.row0 - i * kTileRows;
+          if (limit < kTileRows) {
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          uint32_t r[32];
-          tmem_ld32(s_addr + 32 * c, r);
-          tmem_wait_ld();
-#pragma unroll
-          for (int k = 0; k < 32; ++k) s[32 * c + k] = __uint_as_float(r[k]);
-        }
-        const int limit = w.len - w.row0 - i * kTileRows;
-        if (limit < kTileRows) {
-#pragma unroll
-          for (int c = 0; c < 128; ++c)
-            if (c >= limit) s[c] = -INFINITY;
-        }
-        float mq[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) mq[k] = fmaxf(s[k], s[k + 4]);
-#pragma unroll
-        for (int c = 8; c < 128; c += 8) {
-          mq[0] = max3(mq[0], s[c], s[c + 1]);
-          mq[1] = max3(mq[1], s[c + 2], s[c + 3]);
-          mq[2] = max3(mq[2], s[c + 4], s[c + 5]);
-          mq[3] = max3(mq[3], s[c + 6], s[c + 7]);
-        }
-        const float m_tile = max3(fmaxf(mq[0], mq[1]), mq[2], mq[3]) * sl2;  // scale > 0
-        const float m_cand = fmaxf(m_used, m_tile);
-        // rescale only when the running maximum grew by more than 2^8: P stays
-        // below 256 in between, and the final O / l is exact either way
-        const bool need = m_cand > m_used + 8.0f;
-        if (__any_sync(0xffffffffu, need)) {
-          float alpha = 1.f;
-          if (need) {
-            alpha = ex2_approx(m_used - m_cand);
-            m_used = m_cand;
+            for (int c = 0; c < 128; ++c)
+              if (c >= limit) s[c] = -INFINITY;
           }
-          l *= alpha;
-          if (i > 0) {
-            if constexpr (L::SPLIT_P) {  // (else S of this tile implies it)
-              if (!(ok = warp_wait(&pv_done[t], (done - 1) & 1, ctl))) break;
-              tc_fence_after();
+          float mq[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) mq[k] = fmaxf(s[k], s[k + 4]);
+#pragma unroll
+          for (int c = 8; c < 128; c += 8) {
+            mq[0] = max3(mq[0], s[c], s[c + 1]);
+            mq[1] = max3(mq[1], s[c + 2], s[c + 3]);
+            mq[2] = max3(mq[2], s[c + 4], s[c + 5]);
+            mq[3] = max3(mq[3], s[c + 6], s[c + 7]);
+          }
+          const float m_tile = max3(fmaxf(mq[0], mq[1]), mq[2], mq[3]) * sl2;  // scale > 0
+          const float m_cand = fmaxf(m_used, m_tile);
+          // rescale only when the running maximum grew by more than 2^8: P stays
+          // below 256 in between, and the final O / l is exact either way
+          const bool need = m_cand > m_used + 8.0f;
+          if (__any_sync(0xffffffffu, need)) {
+            float alpha = 1.f;
+            if (need) {
+              alpha = ex2_approx(m_used - m_cand);
+              m_used = m_cand;
             }
-            // exactly the tile's O columns, row sums included
+            l *= alpha;
+            if (i > 0) {
+              if constexpr (L::SPLIT_P) {  // (else S of this tile implies it)
+                if (!(ok = warp_wait(&pv_done[t], (done - 1) & 1, ctl))) break;
+                tc_fence_after();
+              }
+              // exactly the tile's O columns, row sums included
 #pragma unroll 1
-            for (int c = 0; c < L::OW; c += 16) {
-              uint32_t r[16];
-              tmem_ld16(o_addr + c, r);
-              tmem_wait_ld();
+              for (int c = 0; c < L::OW; c += 16) {
+                uint32_t r[16];
+                tmem_ld16(o_addr + c, r);
+                tmem_wait_ld();
 #pragma unroll
-              for (int k = 0; k < 16; ++k) r[k] = __float_as_uint(__uint_as_float(r[k]) * alpha);
-              tmem_st16(o_addr + c, r);
-            }
-            tmem_wait_st();
-          }
-        }
-        const float m_eff = m_used == -INFINITY ? 0.f : m_used;
-        const float2 sl2x2 = make_float2(sl2, sl2), negm = make_float2(-m_eff, -m_eff);
-        float2 acc = make_float2(0.f, 0.f);
-        // P in four 32-key groups, each stored as soon as it is packed; the first
-        // two are announced while the third is stored
-#pragma unroll
-        for (int g4 = 0; g4 < 4; ++g4) {
-          uint32_t packed[16];
-#pragma unroll
-          for (int k = 0; k < 16; ++k) {
-            const float2 x = fma2(make_float2(s[32 * g4 + 2 * k], s[32 * g4 + 2 * k + 1]), sl2x2, negm);
-            const uint32_t pk = pack_bf16x2(ex2_approx(x.x), ex2_approx(x.y));
-            // the row sum uses the bf16 weights the PV MMA consumes, so O is an
-            // exact convex combination of them
-            if constexpr (!L::SUM_MMA)
-              acc = add2(acc, make_float2(__uint_as_float(pk << 16), __uint_as_float(pk & 0xffff0000u)));
-            packed[k] = pk;
-          }
-          if (g4 == 2) {
-            tmem_wait_st();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&p_half[t]);
-            // the previous tile's PV has read the columns of the second half
-            if (L::SPLIT_P && i > 0) {
-              if (!(ok = warp_wait(&pv_done[t], (done - 1) & 1, ctl))) break;
-              tc_fence_after();
+                for (int k = 0; k < 16; ++k) r[k] = __float_as_uint(__uint_as_float(r[k]) * alpha);
+                tmem_st16(o_addr + c, r);
+              }
+              tmem_wait_st();
             }
           }
-          const uint32_t p_addr = L::SPLIT_P && g4 >= 2 ? lane_base + L::P_COL(t, 1) : s_addr + 32 * (g4 >> 1);
-          tmem_st16(p_addr + 16 * (g4 & 1), packed);
-        }
-        if (!ok) break;
-        l += acc.x + acc.y;
-        tmem_wait_st();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&p_full[t]);
-      }
-
-      // ---- epilogue: a loop of 32 columns a turn (it runs once a block, and what
-      // runs once waits for its instructions: unrolled, it took longer)
-      if (ok) ok = warp_wait(&pv_done[t], (L::SPLIT_P ? done - 1 : begun) & 1, ctl);
-      if (!ok) break;
-      ++begun;
-      tc_fence_after();
-      if constexpr (L::SUM_MMA) {
-        uint32_t h[16];
-        tmem_ld16(o_addr + DM, h);
-        tmem_wait_ld();
-        l = __uint_as_float(h[0]);
-      }
-      const bool nonzero = l > 0.f;
-      const float inv_l = nonzero ? 1.f / l : 0.f;
-      const size_t at = static_cast<size_t>(w.bh) * p.M + row;
-      constexpr int kChunks = (DM + 31) / 32;
-#pragma unroll 1
-      for (int c = 0; c < kChunks; ++c) {
-        uint32_t r[32];  // (the last chunk's columns past the caller's are not stored)
-        tmem_ld32(o_addr + 32 * c, r);
-        tmem_wait_ld();
-        if (c == kChunks - 1) {
+          const float m_eff = m_used == -INFINITY ? 0.f : m_used;
+          const float2 sl2x2 = make_float2(sl2, sl2), negm = make_float2(-m_eff, -m_eff);
+          float2 acc = make_float2(0.f, 0.f);
+          // P in four 32-key groups, each stored as soon as it is packed; the first
+          // two are announced while the third is stored
+#pragma unroll
+          for (int g4 = 0; g4 < 4; ++g4) {
+            uint32_t packed[16];
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+              const float2 x = fma2(make_float2(s[32 * g4 + 2 * k], s[32 * g4 + 2 * k + 1]), sl2x2, negm);
+              const uint32_t pk = pack_bf16x2(ex2_approx(x.x), ex2_approx(x.y));
+              // the row sum uses the bf16 weights the PV MMA consumes, so O is an
+              // exact convex combination of them
+              if constexpr (!L::SUM_MMA)
+                acc = add2(acc, make_float2(__uint_as_float(pk << 16), __uint_as_float(pk & 0xffff0000u)));
+              packed[k] = pk;
+            }
+            if (g4 == 2) {
+              tmem_wait_st();
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(&p_half[t]);
+              // the previous tile's PV has read the columns of the second half
+              if (L::SPLIT_P && done > 0) {
+                if (!(ok = warp_wait(&pv_done[t], (done - 1) & 1, ctl))) break;
+                tc_fence_after();
+              }
+            }
+            const uint32_t p_addr = L::SPLIT_P && g4 >= 2 ? lane_base + L::P_COL(t, 1) : s_addr + 32 * (g4 >> 1);
+            tmem_st16(p_addr + 16 * (g4 & 1), packed);
+          }
+          if (!ok) break;
+          l += acc.x + acc.y;
+          tmem_wait_st();
           tc_fence_before();
           __syncwarp();
-          if (lane == 0) mbar_arrive(&o_free[t]);
+          if (lane == 0) mbar_arrive(&p_full[t]);
+        } else if (more && lane == 0) {
+          mbar_arrive(&p_half[t]);
+          mbar_arrive(&p_full[t]);
         }
-        if (idle || 32 * c >= p.d) continue;
-        float v[32];
-#pragma unroll
-        for (int k = 0; k < 32; ++k) v[k] = nonzero ? __uint_as_float(r[k]) * inv_l : 0.f;
-        if (p.num_splits == 1) {
-          // 32 rows of 64 bytes with the 64-byte swizzle: 16-byte chunk k of row i at
-          // k ^ ((i >> 1) & 3).  The map clips rows and columns past the caller's.
-          uint8_t* stg = smem + L::OFF_BOX + (2 * warp + box) * L::BOX_BYTES;
-          box ^= 1;
-          if (lane == 0) bulk_wait_read<1>();  // the TMA unit has read this box
-          __syncwarp();
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            *reinterpret_cast<uint4*>(stg + lane * 64 + ((k ^ ((lane >> 1) & 3)) << 4)) =
-                make_uint4(pack_bf16x2(v[8 * k], v[8 * k + 1]), pack_bf16x2(v[8 * k + 2], v[8 * k + 3]),
-                           pack_bf16x2(v[8 * k + 4], v[8 * k + 5]), pack_bf16x2(v[8 * k + 6], v[8 * k + 7]));
-          fence_proxy_async_smem();
-          __syncwarp();
-          if (lane == 0) {
-            tma_store_3d(&tm_o, stg, 32 * c, row - lane, w.bh);
-            bulk_commit_group();
+        if constexpr (!L::DEFER) {
+          pw = w;
+          pm = m_used;
+          pl = l;
+        }
+        if (L::DEFER ? i == 0 && pending : i + 1 == w.n) {
+          // ---- a block's O: a loop of 32 columns a turn (it runs once a block, and
+          // what runs once waits for its instructions: unrolled, it took longer)
+          if (!(ok = warp_wait(&pv_done[t], (L::DEFER ? done - 1 : begun) & 1, ctl))) break;
+          ++begun;
+          tc_fence_after();
+          if constexpr (L::SUM_MMA) {
+            uint32_t h[16];
+            tmem_ld16(o_addr + DM, h);
+            tmem_wait_ld();
+            pl = __uint_as_float(h[0]);
           }
-        } else if (row < p.M) {
-          float4* dst = reinterpret_cast<float4*>(
-              p.o_part + (static_cast<size_t>(w.split) * p.BH * p.M + at) * D + 32 * c);
+          const int prow = pw.r0 + row_local;
+          const bool pidle = prow - lane >= p.M;
+          const bool nonzero = pl > 0.f;
+          const float inv_l = nonzero ? 1.f / pl : 0.f;
+          const size_t at = static_cast<size_t>(pw.bh) * p.M + prow;
+          constexpr int kChunks = (DM + 31) / 32;
+#pragma unroll 1
+          for (int c = 0; c < kChunks; ++c) {
+            uint32_t r[32];  // (the last chunk's columns past the caller's are not stored)
+            tmem_ld32(o_addr + 32 * c, r);
+            tmem_wait_ld();
+            if (c == kChunks - 1) {
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(&o_free[t]);
+            }
+            if (pidle || 32 * c >= p.d) continue;
+            float v[32];
 #pragma unroll
-          for (int k = 0; k < 8; ++k) dst[k] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+            for (int k = 0; k < 32; ++k) v[k] = nonzero ? __uint_as_float(r[k]) * inv_l : 0.f;
+            if (p.num_splits == 1) {
+              // 32 rows of 64 bytes with the 64-byte swizzle: 16-byte chunk k of row i at
+              // k ^ ((i >> 1) & 3).  The map clips rows and columns past the caller's.
+              uint8_t* stg = smem + L::OFF_BOX + (2 * warp + box) * L::BOX_BYTES;
+              box ^= 1;
+              if (lane == 0) bulk_wait_read<1>();  // the TMA unit has read this box
+              __syncwarp();
+#pragma unroll
+              for (int k = 0; k < 4; ++k)
+                *reinterpret_cast<uint4*>(stg + lane * 64 + ((k ^ ((lane >> 1) & 3)) << 4)) =
+                    make_uint4(pack_bf16x2(v[8 * k], v[8 * k + 1]), pack_bf16x2(v[8 * k + 2], v[8 * k + 3]),
+                               pack_bf16x2(v[8 * k + 4], v[8 * k + 5]), pack_bf16x2(v[8 * k + 6], v[8 * k + 7]));
+              fence_proxy_async_smem();
+              __syncwarp();
+              if (lane == 0) {
+                tma_store_3d(&tm_o, stg, 32 * c, prow - lane, pw.bh);
+                bulk_commit_group();
+              }
+            } else if (prow < p.M) {
+              float4* dst = reinterpret_cast<float4*>(
+                  p.o_part + (static_cast<size_t>(pw.split) * p.BH * p.M + at) * D + 32 * c);
+#pragma unroll
+              for (int k = 0; k < 8; ++k) dst[k] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+            }
+            __syncwarp();
+          }
+          if (prow < p.M) {
+            const float m_eff = pm == -INFINITY ? 0.f : pm;
+            store_lse(pw, prow, nonzero ? (m_eff + __log2f(pl)) * 0.69314718055994530942f : -INFINITY);
+          }
+          __syncwarp();
+          pending = false;
         }
-        __syncwarp();
+        // (a warp without rows not a tile ahead of the others: their arrivals for this
+        // one count first)
+        if (L::SPLIT_P && idle && more && !(ok = warp_wait(&pv_done[t], done & 1, ctl))) break;
       }
-      if (row < p.M) {
-        const float m_eff = m_used == -INFINITY ? 0.f : m_used;
-        store_lse(w, row, nonzero ? (m_eff + __log2f(l)) * 0.69314718055994530942f : -INFINITY);
+      if (!ok || !more) break;
+      if constexpr (L::DEFER) {
+        pending = true;
+        pw = w;
+        pm = m_used;
+        pl = l;
+        pblock = blocks;
       }
-      __syncwarp();
       ++blocks;
     }
-    if (!ok && *abort_flag) {
+    if (*abort_flag) {
       // a wait gave up: this query tile's rows of the blocks left get a defined result
-      for (int x = blockIdx.x + blocks * gridDim.x; x < p.items; x += gridDim.x) {
+      for (int x = blockIdx.x + (pending ? pblock : blocks) * gridDim.x; x < p.items; x += gridDim.x) {
         const Block b = block_of(p, x);
         if (b.r0 + row_local < p.M) store_nothing(b, b.r0 + row_local);
       }
