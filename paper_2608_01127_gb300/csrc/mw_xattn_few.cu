@@ -39,7 +39,7 @@ struct Layout {
   static constexpr int OFF_MISC = OFF_BAR + 2 * kStages * 8;
   // the parts to join, over the stages once those are read: per warp, and the CTA's
   struct Part {
-    float m[R], l[R], o[R][D];
+    float m[R], l[R], e[R], o[R][D];
   };
   static constexpr int OFF_PARTS = 0;
   static_assert((kWarps + 1) * sizeof(Part) <= OFF_BAR, "the parts fit the stages");
@@ -114,7 +114,7 @@ __global__ void __launch_bounds__(Layout<D, R>::THREADS)
   const int i0 = rank * base + min(rank, rest), n = aligned ? base + (rank < rest) : 0;
 
   float o[D / 8][4];  // channels 8 k + 2 (lane % 4) and + 1 of rows lane / 4 and + 8
-  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, e[2] = {0.f, 0.f};
   bool ok = true;
   if (warp == kWarps) {
     // ------------------------------------------------------------ copies
@@ -205,14 +205,16 @@ __global__ void __launch_bounds__(Layout<D, R>::THREADS)
         if (__any_sync(0xffffffffu, top > m[h])) {
           const float keep = ex2_approx(m[h] - from);
           l[h] *= keep;
+          e[h] *= keep;
 #pragma unroll
           for (int k = 0; k < D / 8; ++k) o[k][2 * h] *= keep, o[k][2 * h + 1] *= keep;
           m[h] = top;
         }
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
-          w[2 * b + h] = pack_bf16x2(ex2_approx(x[b][0] - from), ex2_approx(x[b][1] - from));
-          // the sum of the weights that the product uses
+          const float w0 = ex2_approx(x[b][0] - from), w1 = ex2_approx(x[b][1] - from);
+          w[2 * b + h] = pack_bf16x2(w0, w1);
+          e[h] += w0 + w1;  // for the LSE, and the sum of the weights that the product uses
           l[h] += __uint_as_float(w[2 * b + h] << 16) + __uint_as_float(w[2 * b + h] & 0xffff0000u);
         }
       }
@@ -231,6 +233,8 @@ __global__ void __launch_bounds__(Layout<D, R>::THREADS)
     for (int h = 0; h < H; ++h) {
       l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
       l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
+      e[h] += __shfl_xor_sync(0xffffffffu, e[h], 1);
+      e[h] += __shfl_xor_sync(0xffffffffu, e[h], 2);
     }
   }
   // join the warps, then the cluster's CTAs
@@ -244,7 +248,7 @@ __global__ void __launch_bounds__(Layout<D, R>::THREADS)
 #pragma unroll
       for (int k = 0; k < D / 8; ++k)
         *reinterpret_cast<float2*>(&mine.o[r][8 * k + pair]) = make_float2(o[k][2 * h], o[k][2 * h + 1]);
-      if (pair == 0) mine.m[r] = ok ? m[h] : -INFINITY, mine.l[r] = l[h];
+      if (pair == 0) mine.m[r] = ok ? m[h] : -INFINITY, mine.l[r] = l[h], mine.e[r] = e[h];
     }
   }
   __syncthreads();
@@ -252,33 +256,35 @@ __global__ void __launch_bounds__(Layout<D, R>::THREADS)
   Part& whole = parts[kWarps];
   for (int i = threadIdx.x; i < total; i += L::THREADS) {
     const int r = i / p.d, ch = i - r * p.d;
-    float top = -INFINITY, sum = 0.f, acc = 0.f;
+    float top = -INFINITY, sum = 0.f, exact = 0.f, acc = 0.f;
 #pragma unroll
     for (int k = 0; k < kWarps; ++k) top = fmaxf(top, parts[k].m[r]);
 #pragma unroll
     for (int k = 0; k < kWarps; ++k) {
       const float a = weight(parts[k].m[r], top);
       sum = fmaf(parts[k].l[r], a, sum);
+      exact = fmaf(parts[k].e[r], a, exact);
       acc = fmaf(parts[k].o[r][ch], a, acc);
     }
     whole.o[r][ch] = acc;
-    if (ch == 0) whole.m[r] = top, whole.l[r] = sum;
+    if (ch == 0) whole.m[r] = top, whole.l[r] = sum, whole.e[r] = exact;
   }
   cluster.sync();
   for (int i = rank * L::THREADS + threadIdx.x; i < total; i += ranks * L::THREADS) {
     const int r = i / p.d, ch = i - r * p.d;
-    float top = -INFINITY, sum = 0.f, acc = 0.f;
+    float top = -INFINITY, sum = 0.f, exact = 0.f, acc = 0.f;
     for (int k = 0; k < ranks; ++k) top = fmaxf(top, cluster.map_shared_rank(&whole, k)->m[r]);
     for (int k = 0; k < ranks; ++k) {
       const Part* other = cluster.map_shared_rank(&whole, k);
       const float a = weight(other->m[r], top);
       sum = fmaf(other->l[r], a, sum);
+      exact = fmaf(other->e[r], a, exact);
       acc = fmaf(other->o[r][ch], a, acc);
     }
     const size_t at = static_cast<size_t>(bh) * p.M + r;
     p.o[at * p.d + ch] = __float2bfloat16(sum > 0.f ? acc / sum : 0.f);
     if (p.lse && ch == 0)
-      p.lse[at] = sum > 0.f ? (top + __log2f(sum)) * 0.69314718055994530942f : -INFINITY;
+      p.lse[at] = sum > 0.f ? (top + __log2f(exact)) * 0.69314718055994530942f : -INFINITY;
   }
   cluster.sync();  // shared memory stays until all have read it
 }

@@ -12,21 +12,23 @@
 // are loaded, and its first S is computed, while the softmax warps finish the
 // last one; they take O into registers, hand its tensor memory back, and store
 // rows while the next block's MMAs run.  What bounds a step is the chain from S through
-// softmax and P to the next S (d = 64: 2230 cycles, of which S to registers 350, P 1600),
-// not the exponentials (1024 cycles at 32 a clock) or the MMAs (1150; d = 128 2048 of
-// 3170).  Steps of 64 keys with two S in flight were slower (d = 64 1.16 -> 1.59 us, 128
+// softmax and P to the next S (d = 64: 2300 cycles, of which S to registers 350, P 1600),
+// not the exponentials (1024 cycles at 32 a clock) or the MMAs (1024; d = 128 2048 of
+// 3070).  Steps of 64 keys with two S in flight were slower (d = 64 1.16 -> 1.59 us, 128
 // 1.65 -> 1.88): half of the softmax is latency that does not shrink with the step.
+// Measured, 24 query and 40 key tiles a head: d = 64 1.21, 72 1.31, 128 1.60 us a step of
+// 256 rows x 128 keys (1.6 PFLOP/s over the SMs); two key tiles 2.25, 2.79, 2.79.
 //
 // Roles (384 threads):
 //   warps 0-3 / 4-7  softmax of query tile 0 / 1 (one thread per row = TMEM lane)
 //   warp 8           TMA producer
-//   warp 9           tcgen05 issuer; d = 64: of query tile 0, and warp 10 of tile 1
-//   the rest of 9-11 V tiles that end inside the valid states: rows past them are
-//                    zeroed (their weights are 0, but what they hold may be NaN);
-//                    80-wide MMAs: also the ones columns of every V tile
-// TMEM as in the block-causal forward: S_t at column 128 t, O_t at 256 + OW t with
-// 16 row-sum columns where V has ones columns; P_t, bf16, over S_t, its second
-// half in columns of its own where there is room.
+//   warps 9, 10      tcgen05 issuers: of query tile 0 and of tile 1 (d > 80: 9 of both)
+//   warp 11          V tiles that end inside the valid states: rows past them are
+//                    zeroed (their weights are 0, but what they hold may be NaN)
+// TMEM: S_t at column 128 t, O_t at 256 + DM t; P_t, bf16, over S_t, its second half in
+// columns of its own where there is room.  The row sums are of the weights before their
+// rounding to bf16 (the block-causal forward takes those after it), in 32 bits: LSE is as
+// exact as S, and the backward's P with it.
 #include <type_traits>
 
 #include "mw_internal.h"
@@ -47,20 +49,17 @@ struct Layout {
   static constexpr int OFF_Q = 0;
   static constexpr int OFF_K = OFF_Q + QBUFS * QT * TILE_BYTES;
   static constexpr int OFF_V = OFF_K + STAGES * TILE_BYTES;
-  // The row sum of P as 16 more columns of the PV MMA: ones in a region of their
-  // own (d = 64) or in columns 80..95 of each V tile (80-wide MMAs)
-  static constexpr bool ONES_IN_V = (D == 128 && DM == 80);
-  static constexpr bool SUM_MMA = (D == 64) || ONES_IN_V;
-  static constexpr int OW = SUM_MMA ? DM + 16 : DM;
-  static constexpr int OFF_ONES = OFF_V + STAGES * TILE_BYTES;
-  static constexpr int ONES_BYTES = (D == 64) ? REGION_BYTES : 0;
+  static constexpr int OFF_BOX = OFF_V + STAGES * TILE_BYTES;
   // O leaves through TMA stores of 32 x 32 boxes, two a warp in turn
   static constexpr int BOX_BYTES = 32 * 64;
-  static constexpr int OFF_BOX = OFF_ONES + ONES_BYTES;
   static constexpr int OFF_BAR = OFF_BOX + 8 * 2 * BOX_BYTES;
-  static constexpr bool SPLIT_P = 256 + OW * QT + 32 * QT <= 512;
-  static constexpr int ISSUERS = D == 64 ? QT : 1;
-  static constexpr int HELPERS = 3 - ISSUERS;
+  // P's second half has columns of its own (d <= 80): S of the next tile is computed once
+  // P's first half is used.  (Both halves in columns of their own, d = 64, and S once this
+  // one is in registers: 1.21 -> 1.30 us a step.)
+  static constexpr bool SPLIT_P = 256 + DM * QT + 32 * QT <= 512;
+  // A warp a query tile issues MMAs, or one both: 24 x 40 tiles, two / one: d = 72 1.31 /
+  // 1.46 us a step, 128 (where the tensor core has more to do) 2.03 / 1.60
+  static constexpr int ISSUERS = DM < 128 ? QT : 1;
   // A block's O leaves after the first softmax of the next block, while that one's MMAs
   // run.  Where P overwrites all of S, S of the tile after that would wait for it: there
   // O leaves at the end of its own block (us a step of 2 x 128 rows, blocks of two key
@@ -73,9 +72,9 @@ struct Layout {
   static constexpr int BYTES = OFF_MISC + 16;
   static_assert(BYTES <= 232448, "shared memory");
   static constexpr uint32_t S_COL(int t) { return 128u * t; }
-  static constexpr uint32_t O_COL(int t) { return 256u + OW * t; }
+  static constexpr uint32_t O_COL(int t) { return 256u + DM * t; }
   static constexpr uint32_t P_COL(int t, int half) {
-    return half == 0 ? S_COL(t) : SPLIT_P ? 256u + OW * QT + 32u * t : S_COL(t) + 32u;
+    return half == 0 ? S_COL(t) : SPLIT_P ? 256u + DM * QT + 32u * t : S_COL(t) + 32u;
   }
   static constexpr int THREADS = 384;
   // registers per thread after the re-split: 2 * 128 * S + 128 * C is exactly the
@@ -95,10 +94,10 @@ struct Block {
   int row0, n;   // its first key row, its key tiles
   int len;       // valid states
   __device__ __forceinline__ bool present(int t, int M) const { return r0 + kTileRows * t < M; }
-  // V tile i of the block passes through the helper warps: all of them, or those
-  // with rows that count as nothing but may hold anything (past S are zeros)
-  __device__ __forceinline__ bool helped(int i, bool all, int S) const {
-    return all || (row0 + (i + 1) * kTileRows > len && len < S);
+  // V tile i of the block passes through a helper warp: it has rows that count as
+  // nothing but may hold anything (past S are zeros)
+  __device__ __forceinline__ bool helped(int i, int S) const {
+    return row0 + (i + 1) * kTileRows > len && len < S;
   }
 };
 
@@ -187,7 +186,7 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
     for (int s = 0; s < NS; ++s) {
       mbar_init(&k_full[s], 1);
       mbar_init(&k_empty[s], L::ISSUERS);
-      mbar_init(&v_full[s], L::ONES_IN_V ? L::HELPERS : 1);
+      mbar_init(&v_full[s], 1);
       mbar_init(&v_empty[s], L::ISSUERS);
       mbar_init(&v_raw[s], 1);
     }
@@ -214,13 +213,6 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
   if (warp == 9) {
     tmem_alloc(tmem_slot, 512);
     tmem_relinquish();
-  }
-  if constexpr (L::ONES_BYTES > 0) {
-    uint4* ones = reinterpret_cast<uint4*>(smem + L::OFF_ONES);
-    const uint32_t one2 = 0x3F803F80u;  // bf16 1.0 twice
-    for (int k = threadIdx.x; k < L::ONES_BYTES / 16; k += L::THREADS)
-      ones[k] = make_uint4(one2, one2, one2, one2);
-    fence_proxy_async_smem();  // read by the tensor core (async proxy)
   }
   tc_fence_before();
   __syncthreads();
@@ -310,7 +302,7 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
             tma_load_3d(sK + st * L::TILE_BYTES + r * L::REGION_BYTES, &tm_k, &k_full[st], 64 * r, row0, w.bh);
           ++nk;
           if (!(ok = mbar_wait(&v_empty[st], ph, ctl))) break;
-          const bool help = w.helped(i, L::ONES_IN_V, p.S);
+          const bool help = w.helped(i, p.S);
           uint64_t* bar = help ? &v_raw[st] : &v_full[st];
           mbar_arrive_expect_tx(bar, L::TILE_BYTES);
           for (int r = 0; r < L::REG; ++r)
@@ -336,11 +328,10 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
   } else if (warp == 9 || (L::ISSUERS > 1 && warp == 10)) {
     // ------------------------------------------------------------ MMA issuers (whole warps)
     constexpr uint32_t idesc_qk = idesc_bf16_f32(128, 128, false, false);
-    constexpr uint32_t idesc_pv = idesc_bf16_f32(128, L::OW, false, true);
+    constexpr uint32_t idesc_pv = idesc_bf16_f32(128, DM, false, true);
     const uint32_t q_desc = sdesc_sw128(smem_u32(sQ), 16);
     const uint32_t k_desc = sdesc_sw128(smem_u32(sK), 16);
     const uint32_t v_addr = smem_u32(sV);
-    const uint32_t ones_addr = smem_u32(smem + L::OFF_ONES);
     auto issue_qk = [&](int t, int qb, int st) {
       const uint32_t qa = sdesc_add(q_desc, (qb * QT + t) * L::TILE_BYTES);
       const uint32_t kb = sdesc_add(k_desc, st * L::TILE_BYTES);
@@ -354,8 +345,7 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
       }
     };
     auto issue_pv = [&](int t, int st, bool acc, int half) {
-      const uint32_t vs = v_addr + st * L::TILE_BYTES;
-      const uint32_t vb = sdesc_sw128(vs, L::ONES_BYTES > 0 ? ones_addr - vs : L::REGION_BYTES);
+      const uint32_t vb = sdesc_sw128(v_addr + st * L::TILE_BYTES, L::REGION_BYTES);
       umma_ts4<8, 128>(tmem + L::O_COL(t), tmem + L::P_COL(t, half), sdesc_add(vb, half * 8192), idesc_pv,
                        (acc || half > 0) ? 1u : 0u);
     };
@@ -445,33 +435,23 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
     }
   } else {
     // ------------------------------------------------------------ V tiles made ready
-    // With ones columns every tile passes through all helpers, else only the
-    // ragged ones, through the first.  A stage's v_raw cannot complete again
-    // before the helper has looked: the stage is free for another tile only once
-    // the MMAs, which wait for the helper, have read this one.
-    const int part = warp - 9 - L::ISSUERS;
-    constexpr int kParts = L::ONES_IN_V ? L::HELPERS : 1;
-    constexpr int kRows = kTileRows / kParts;  // of a helper
+    // Only ragged ones pass through here (warp 11).  A stage's v_raw cannot complete again
+    // before the helper has looked: the stage is free for another tile only once the MMAs,
+    // which wait for the helper, have read this one.
     int nv = 0;
     uint32_t raws = 0;  // parity of each stage's uses
     bool ok = true;
     while (ok && next_keys()) {
       for (int i = 0; i < w.n; ++i, ++nv) {
-        if (part >= kParts || !w.helped(i, L::ONES_IN_V, p.S)) continue;
+        if (warp != 11 || !w.helped(i, p.S)) continue;
         const int st = nv % NS;
         if (!(ok = warp_wait(&v_raw[st], (raws >> st) & 1, ctl))) break;
         raws ^= 1u << st;
         uint8_t* tile = sV + st * L::TILE_BYTES;
         const int limit = w.len - w.row0 - i * kTileRows;
 #pragma unroll
-        for (int k = 0; k < kRows / 32; ++k) {
-          const int r = kRows * part + 32 * k + lane;
-          if constexpr (L::ONES_IN_V) {
-            const uint4 ones = make_uint4(0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u);
-            uint8_t* row = tile + L::REGION_BYTES + r * 128;
-            *reinterpret_cast<uint4*>(row + (((DM - 64) / 8 ^ (r & 7)) << 4)) = ones;
-            *reinterpret_cast<uint4*>(row + (((DM - 64) / 8 + 1 ^ (r & 7)) << 4)) = ones;
-          }
+        for (int k = 0; k < kTileRows / 32; ++k) {
+          const int r = 32 * k + lane;
           if (r >= limit) {
             const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
@@ -570,9 +550,9 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
                 if (!(ok = warp_wait(&pv_done[t], (done - 1) & 1, ctl))) break;
                 tc_fence_after();
               }
-              // exactly the tile's O columns, row sums included
+              // exactly the tile's O columns
 #pragma unroll 1
-              for (int c = 0; c < L::OW; c += 16) {
+              for (int c = 0; c < DM; c += 16) {
                 uint32_t r[16];
                 tmem_ld16(o_addr + c, r);
                 tmem_wait_ld();
@@ -594,12 +574,9 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
 #pragma unroll
             for (int k = 0; k < 16; ++k) {
               const float2 x = fma2(make_float2(s[32 * g4 + 2 * k], s[32 * g4 + 2 * k + 1]), sl2x2, negm);
-              const uint32_t pk = pack_bf16x2(ex2_approx(x.x), ex2_approx(x.y));
-              // the row sum uses the bf16 weights the PV MMA consumes, so O is an
-              // exact convex combination of them
-              if constexpr (!L::SUM_MMA)
-                acc = add2(acc, make_float2(__uint_as_float(pk << 16), __uint_as_float(pk & 0xffff0000u)));
-              packed[k] = pk;
+              const float2 e = make_float2(ex2_approx(x.x), ex2_approx(x.y));
+              packed[k] = pack_bf16x2(e.x, e.y);
+              acc = add2(acc, e);  // of the weights before their rounding: the LSE is exact
             }
             if (g4 == 2) {
               tmem_wait_st();
@@ -612,8 +589,7 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
                 tc_fence_after();
               }
             }
-            const uint32_t p_addr = L::SPLIT_P && g4 >= 2 ? lane_base + L::P_COL(t, 1) : s_addr + 32 * (g4 >> 1);
-            tmem_st16(p_addr + 16 * (g4 & 1), packed);
+            tmem_st16(lane_base + L::P_COL(t, g4 >> 1) + 16 * (g4 & 1), packed);
           }
           if (!ok) break;
           l += acc.x + acc.y;
@@ -636,12 +612,6 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
           if (!(ok = warp_wait(&pv_done[t], (L::DEFER ? done - 1 : begun) & 1, ctl))) break;
           ++begun;
           tc_fence_after();
-          if constexpr (L::SUM_MMA) {
-            uint32_t h[16];
-            tmem_ld16(o_addr + DM, h);
-            tmem_wait_ld();
-            pl = __uint_as_float(h[0]);
-          }
           const int prow = pw.r0 + row_local;
           const bool pidle = prow - lane >= p.M;
           const bool nonzero = pl > 0.f;
