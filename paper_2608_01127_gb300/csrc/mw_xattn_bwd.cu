@@ -174,6 +174,19 @@ struct Plan {
   __device__ __forceinline__ bool step() { return ++w.kt < k_end || (p.key_major ? key_piece() : query_piece()); }
 };
 
+// After a wait gave up: zeros for gradients that are written whole.  Other CTAs' rows as
+// well, which the call's status makes no worse: each CTA's own from its plan took 8 KB of
+// code next to this path's 1.
+__device__ __forceinline__ void leave_zeros(const XattnBwdParams& p, unsigned thread, unsigned threads) {
+#pragma unroll 1
+  for (int a = 0; a < 3; ++a) {
+    const unsigned n = static_cast<unsigned>(p.BH) * (a == 0 ? p.M : p.S);
+    uint4* out = reinterpret_cast<uint4*>(a == 0 ? p.dq : a == 1 ? p.dk : p.dv);
+#pragma unroll 1
+    for (size_t i = thread; i < static_cast<size_t>(n) * (p.d / 8); i += threads) out[i] = make_uint4(0u, 0u, 0u, 0u);
+  }
+}
+
 template <int D, int DM>
 __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
     xattn_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
@@ -190,9 +203,10 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
   constexpr int NB = L::DS_BUFS;
   extern __shared__ __align__(1024) uint8_t smem[];
   if ((smem_u32(smem) & 1023u) != 0u) {
-    // nothing runs without aligned shared memory: report it (the accumulators
-    // keep the zeros they start with)
+    // nothing runs without aligned shared memory: report it, and leave zeros (the
+    // accumulators start with them)
     if (threadIdx.x == 0) atomicOr(p.status, kDevMisaligned);
+    if (blockIdx.x == 0) leave_zeros(p, threadIdx.x, L::THREADS);
     return;  // uniform across the CTA, before any barrier or TMEM use
   }
   constexpr int NK = L::KBUFS;
@@ -910,6 +924,8 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
     // every copy has completed before the CTA's shared memory goes away
     if (lane == 0 && !ok && loads > 0) drain_wait(&acc_full[wq], (loads - 1) & 1, p.budget_ns);
     if (lane == 0) bulk_wait_all();
+    __syncwarp();
+    if (*abort_flag) leave_zeros(p, 32 * wq + lane, 128);
     __syncwarp();
   }
 
