@@ -925,8 +925,6 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
     if (lane == 0 && !ok && loads > 0) drain_wait(&acc_full[wq], (loads - 1) & 1, p.budget_ns);
     if (lane == 0) bulk_wait_all();
     __syncwarp();
-    if (*abort_flag) leave_zeros(p, 32 * wq + lane, 128);
-    __syncwarp();
   }
 
   __syncwarp();
@@ -936,6 +934,7 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
     tc_fence_after();
     tmem_dealloc(tmem, 512);
   }
+  if (*abort_flag) leave_zeros(p, threadIdx.x, L::THREADS);
 }
 
 // D_i = <dO_i, O_i> and LSE_i log2(e) (padding rows 0 and +inf, so that their P is

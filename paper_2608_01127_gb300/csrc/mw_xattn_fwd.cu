@@ -150,15 +150,20 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
     store_lse(w, row, -INFINITY);
   };
 
-  if ((smem_u32(smem) & 1023u) != 0u) {
-    // nothing runs without aligned shared memory: report it, and give this CTA's
-    // rows a defined result
-    if (threadIdx.x == 0) atomicOr(p.status, kDevMisaligned);
+  auto leave_nothing = [&]() {  // in all blocks of this CTA
+#pragma unroll 1
     for (int x = blockIdx.x; x < p.items; x += gridDim.x) {
       const Block w = block_of(p, x);
       const int row = w.r0 + static_cast<int>(threadIdx.x);
       if (threadIdx.x < kFwdBlockRows && row < p.M) store_nothing(w, row);
     }
+  };
+
+  if ((smem_u32(smem) & 1023u) != 0u) {
+    // nothing runs without aligned shared memory: report it, and give this CTA's
+    // rows a defined result
+    if (threadIdx.x == 0) atomicOr(p.status, kDevMisaligned);
+    leave_nothing();
     return;  // uniform across the CTA, before any barrier or TMEM use
   }
   uint64_t* q_full = reinterpret_cast<uint64_t*>(smem + L::OFF_BAR);
@@ -475,7 +480,6 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
     const uint32_t s_addr = lane_base + L::S_COL(t);
     const uint32_t o_addr = lane_base + L::O_COL(t);
     const float sl2 = p.scale_log2;
-    int blocks = 0;  // blocks dealt with
     int begun = 0;   // blocks of this query tile whose O is out
     int done = 0;    // key tiles of this query tile
     int box = 0;     // the staging box whose turn it is
@@ -483,7 +487,6 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
     bool pending = false;
     Block pw;
     float pm = 0.f, pl = 0.f;
-    int pblock = 0;
     while (true) {
       bool ok = true;
       const bool more = next_block();  // (at the end one more turn, for the last block's O)
@@ -492,13 +495,9 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
       if (more && w.n == 0) {  // no keys
         if (row < p.M) store_nothing(w, row);
         __syncwarp();
-        ++blocks;
         continue;
       }
-      if (more && !w.present(t, p.M)) {
-        ++blocks;
-        continue;
-      }
+      if (more && !w.present(t, p.M)) continue;
       if (!more) w.n = 1;
       float m_used = -INFINITY;
       float l = 0.f;
@@ -675,19 +674,12 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
         pw = w;
         pm = m_used;
         pl = l;
-        pblock = blocks;
       }
-      ++blocks;
     }
-    if (*abort_flag) {
-      // a wait gave up: this query tile's rows of the blocks left get a defined result
-      for (int x = blockIdx.x + (pending ? pblock : blocks) * gridDim.x; x < p.items; x += gridDim.x) {
-        const Block b = block_of(p, x);
-        if (b.r0 + row_local < p.M) store_nothing(b, b.r0 + row_local);
-      }
-      __syncwarp();
+    if (lane == 0) {
+      if (*abort_flag) bulk_wait_all();  // (these rows are written once more below)
+      bulk_wait_read<0>();               // the boxes are read before shared memory goes
     }
-    if (lane == 0) bulk_wait_read<0>();  // the boxes are read before shared memory goes
     __syncwarp();
     pdl_trigger();  // the next kernel (the split combine) may be scheduled now
   }
@@ -699,6 +691,7 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
     tc_fence_after();
     tmem_dealloc(tmem, 512);
   }
+  if (*abort_flag) leave_nothing();  // a wait gave up: the rows get a defined result
 }
 
 template <int D, int DM>
