@@ -40,8 +40,8 @@ mw_status make_map(CUtensorMap* m, const void* ptr, int rows, int BH, int d, con
                    int box_rows = kTileRows, bool f32 = false, int cols = 0);
 // Map over the backward's bias rows [BH, N_pad, 8] f32.
 mw_status encode_bias_map(CUtensorMap* m, const float* bias, int N_pad, int BH, int box_rows);
-// Map over bf16 rows [BH, rows, d] in boxes of 32 columns x 32 rows, with the 64-byte
-// swizzle or without.
+// Map over bf16 rows [BH, rows, d] in boxes of 32 rows: x 64 columns with the 128-byte
+// swizzle, or x 32 without.
 mw_status encode_rows_map(CUtensorMap* m, void* ptr, int rows, int BH, int d, bool swizzle);
 
 // The device status word of the current device `dev`.

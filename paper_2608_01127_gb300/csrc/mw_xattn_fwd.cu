@@ -16,8 +16,8 @@
 // not the exponentials (1024 cycles at 32 a clock) or the MMAs (1024; d = 128 2048 of
 // 3070).  Steps of 64 keys with two S in flight were slower (d = 64 1.16 -> 1.59 us, 128
 // 1.65 -> 1.88): half of the softmax is latency that does not shrink with the step.
-// Measured, 24 query and 40 key tiles a head: d = 64 1.21, 72 1.31, 128 1.60 us a step of
-// 256 rows x 128 keys (1.6 PFLOP/s over the SMs); two key tiles 2.25, 2.79, 2.79.
+// Measured, 24 query and 40 key tiles a head: d = 64 1.21, 72 1.31, 128 1.59 us a step of
+// 256 rows x 128 keys (128: 1.6 PFLOP/s over the SMs); two key tiles 2.07, 2.70, 2.74.
 //
 // Roles (384 threads):
 //   warps 0-3 / 4-7  softmax of query tile 0 / 1 (one thread per row = TMEM lane)
@@ -50,9 +50,8 @@ struct Layout {
   static constexpr int OFF_K = OFF_Q + QBUFS * QT * TILE_BYTES;
   static constexpr int OFF_V = OFF_K + STAGES * TILE_BYTES;
   static constexpr int OFF_BOX = OFF_V + STAGES * TILE_BYTES;
-  // O leaves through TMA stores of 32 x 32 boxes, two a warp in turn
-  static constexpr int BOX_BYTES = 32 * 64;
-  static constexpr int OFF_BAR = OFF_BOX + 8 * 2 * BOX_BYTES;
+  static constexpr int BOX_BYTES = 32 * 128;  // O leaves through TMA stores, 32 x 64 a warp
+  static constexpr int OFF_BAR = OFF_BOX + 8 * BOX_BYTES;
   // P's second half has columns of its own (d <= 80): S of the next tile is computed once
   // P's first half is used.  (Both halves in columns of their own, d = 64, and S once this
   // one is in registers: 1.21 -> 1.30 us a step.)
@@ -482,7 +481,6 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
     const float sl2 = p.scale_log2;
     int begun = 0;   // blocks of this query tile whose O is out
     int done = 0;    // key tiles of this query tile
-    int box = 0;     // the staging box whose turn it is
     // the block whose O has to leave, and its statistics
     bool pending = false;
     Block pw;
@@ -606,8 +604,10 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
           pl = l;
         }
         if (L::DEFER ? i == 0 && pending : i + 1 == w.n) {
-          // ---- a block's O: a loop of 32 columns a turn (it runs once a block, and
-          // what runs once waits for its instructions: unrolled, it took longer)
+          // ---- a block's O, 64 columns a turn.  It runs once a block, and what runs once
+          // waits for its instructions: unrolled it took longer, and with turns of 32
+          // columns too (blocks of two key tiles, us a step: d = 64 2.23 -> 2.07, 72 2.83 ->
+          // 2.70, 128 2.87 -> 2.74).
           if (!(ok = warp_wait(&pv_done[t], (L::DEFER ? done - 1 : begun) & 1, ctl))) break;
           ++begun;
           tc_fence_after();
@@ -616,44 +616,52 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
           const bool nonzero = pl > 0.f;
           const float inv_l = nonzero ? 1.f / pl : 0.f;
           const size_t at = static_cast<size_t>(pw.bh) * p.M + prow;
-          constexpr int kChunks = (DM + 31) / 32;
+          constexpr int kChunks = (DM + 63) / 64;
+          const bool all_nonzero = __all_sync(0xffffffffu, nonzero);
 #pragma unroll 1
           for (int c = 0; c < kChunks; ++c) {
-            uint32_t r[32];  // (the last chunk's columns past the caller's are not stored)
-            tmem_ld32(o_addr + 32 * c, r);
+            uint32_t r[2][32];  // (the last chunk's columns past the caller's are not stored)
+            tmem_ld32(o_addr + 64 * c, r[0]);
+            tmem_ld32(o_addr + 64 * c + 32, r[1]);
             tmem_wait_ld();
             if (c == kChunks - 1) {
               tc_fence_before();
               __syncwarp();
               if (lane == 0) mbar_arrive(&o_free[t]);
             }
-            if (pidle || 32 * c >= p.d) continue;
-            float v[32];
+            if (pidle || 64 * c >= p.d) continue;
+            float2 v[32];
 #pragma unroll
-            for (int k = 0; k < 32; ++k) v[k] = nonzero ? __uint_as_float(r[k]) * inv_l : 0.f;
+            for (int k = 0; k < 32; ++k)
+              v[k] = mul2(make_float2(__uint_as_float(r[k >> 4][2 * k & 31]), __uint_as_float(r[k >> 4][(2 * k & 31) + 1])),
+                          make_float2(inv_l, inv_l));
+            if (!all_nonzero && !nonzero) {
+#pragma unroll
+              for (int k = 0; k < 32; ++k) v[k] = make_float2(0.f, 0.f);
+            }
             if (p.num_splits == 1) {
-              // 32 rows of 64 bytes with the 64-byte swizzle: 16-byte chunk k of row i at
-              // k ^ ((i >> 1) & 3).  The map clips rows and columns past the caller's.
-              uint8_t* stg = smem + L::OFF_BOX + (2 * warp + box) * L::BOX_BYTES;
-              box ^= 1;
-              if (lane == 0) bulk_wait_read<1>();  // the TMA unit has read this box
+              // 32 rows of 128 bytes with the 128-byte swizzle: 16-byte chunk k of row i at
+              // k ^ (i & 7).  The map clips rows and columns past the caller's.
+              uint8_t* stg = smem + L::OFF_BOX + warp * L::BOX_BYTES;
+              if (lane == 0) bulk_wait_read<0>();  // the TMA unit has read the box
               __syncwarp();
 #pragma unroll
-              for (int k = 0; k < 4; ++k)
-                *reinterpret_cast<uint4*>(stg + lane * 64 + ((k ^ ((lane >> 1) & 3)) << 4)) =
-                    make_uint4(pack_bf16x2(v[8 * k], v[8 * k + 1]), pack_bf16x2(v[8 * k + 2], v[8 * k + 3]),
-                               pack_bf16x2(v[8 * k + 4], v[8 * k + 5]), pack_bf16x2(v[8 * k + 6], v[8 * k + 7]));
+              for (int k = 0; k < 8; ++k)
+                *reinterpret_cast<uint4*>(stg + lane * 128 + ((k ^ (lane & 7)) << 4)) =
+                    make_uint4(pack_bf16x2(v[4 * k].x, v[4 * k].y), pack_bf16x2(v[4 * k + 1].x, v[4 * k + 1].y),
+                               pack_bf16x2(v[4 * k + 2].x, v[4 * k + 2].y), pack_bf16x2(v[4 * k + 3].x, v[4 * k + 3].y));
               fence_proxy_async_smem();
               __syncwarp();
               if (lane == 0) {
-                tma_store_3d(&tm_o, stg, 32 * c, prow - lane, pw.bh);
+                tma_store_3d(&tm_o, stg, 64 * c, prow - lane, pw.bh);
                 bulk_commit_group();
               }
             } else if (prow < p.M) {
               float4* dst = reinterpret_cast<float4*>(
-                  p.o_part + (static_cast<size_t>(pw.split) * p.BH * p.M + at) * D + 32 * c);
+                  p.o_part + (static_cast<size_t>(pw.split) * p.BH * p.M + at) * D + 64 * c);
 #pragma unroll
-              for (int k = 0; k < 8; ++k) dst[k] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+              for (int k = 0; k < 16; ++k)
+                dst[k] = make_float4(v[2 * k].x, v[2 * k].y, v[2 * k + 1].x, v[2 * k + 1].y);
             }
             __syncwarp();
           }
