@@ -240,7 +240,7 @@ struct XattnTcParams {
   unsigned long long budget_ns;
   int debug_skip_q;    // test hook: never load Q, so the issuers' wait expires
 };
-// d, dm: tile and MMA width as for launch_fwd; to: o in 32 x 32 boxes with the 64-byte
+// d, dm: tile and MMA width as for launch_fwd; to: o in 32 x 64 boxes with the 128-byte
 // swizzle; sms: CTAs at most
 cudaError_t launch_xattn_tc(int d, int dm, const CUtensorMap& tq, const CUtensorMap& tk,
                             const CUtensorMap& tv, const CUtensorMap& to, const XattnTcParams& p, int dev, int sms,

@@ -146,9 +146,7 @@ constexpr int max_threads(int VEC, int V) { return VEC == 1 && V > 8 ? 512 : 256
 constexpr int fwd_blocks(int VEC, int V, int x) {
   return VEC == 1 ? (V <= 4 ? 5 : V <= 8 ? 3 : 1) : V <= 2 ? 4 : V <= 4 ? 3 : V <= 6 && x == 2 ? 3 : 2;
 }
-constexpr int bwd_blocks(int VEC, int V, int x) {
-  return VEC == 1 ? (V <= 4 ? 3 : V <= 8 ? 2 : 1) : V == 1 ? 3 : V == 2 && x == 2 ? 2 : 1;
-}
+constexpr int bwd_blocks(int V) { return V <= 4 ? 3 : V <= 8 ? 2 : 1; }
 
 // Rows that a team of the forward works on at once: their loads, sums and barriers
 // overlap, and they share what a group's weight and bias cost (read from L1 for every
@@ -285,9 +283,20 @@ __global__ void __launch_bounds__(max_threads(VEC, V), fwd_blocks(VEC, V, sizeof
   }
 }
 
+// A block's sums of dw and db over its rows: its partial, or the result.
+__device__ __forceinline__ void write_params(const NormParams& p, size_t g, const float* sums) {
+  for (int c = threadIdx.x; c < 2 * p.C; c += blockDim.x) {
+    if (p.parts > 1)
+      p.partial[static_cast<size_t>(blockIdx.x) * 2 * p.C + c] = sums[c];
+    else if (c < p.C ? p.dweight != nullptr : p.dbias != nullptr)
+      store_param(c < p.C ? p.dweight : p.dbias, p.param_f32, g + (c < p.C ? c : c - p.C), sums[c]);
+  }
+}
+
 // Block (part, group): rows [part n / parts, (part + 1) n / parts) of the group.
-template <class TX, class TY, int VEC, int V>
-__global__ void __launch_bounds__(max_threads(VEC, V), bwd_blocks(VEC, V, sizeof(TX))) norm_bwd_kernel(const NormParams p) {
+template <class TX, class TY, int V>
+__global__ void __launch_bounds__(max_threads(1, V), bwd_blocks(V)) norm_bwd_kernel(const NormParams p) {
+  constexpr int VEC = 1;
   __shared__ Sums<2> red[2][16];
   extern __shared__ float sums[];  // [2][C]
   const Team team(p.W);
@@ -371,12 +380,184 @@ __global__ void __launch_bounds__(max_threads(VEC, V), bwd_blocks(VEC, V, sizeof
     }
     __syncthreads();
   }
-  for (int c = threadIdx.x; c < 2 * p.C; c += blockDim.x) {
-    if (p.parts > 1)
-      p.partial[static_cast<size_t>(blockIdx.x) * 2 * p.C + c] = sums[c];
-    else if (c < p.C ? p.dweight != nullptr : p.dbias != nullptr)
-      store_param(c < p.C ? p.dweight : p.dbias, p.param_f32, g + (c < p.C ? c : c - p.C), sums[c]);
+  write_params(p, g, sums);
+}
+
+// N sums over a warp at once, N = 2, 4 or 8: halves of the values change sides until one is
+// left, so 9 shuffles do for 8; lane l ends with value l / (32 / N).
+template <int N>
+__device__ __forceinline__ float warp_sums(float (&v)[N]) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int h = N / 2, m = 16; m > 0; h /= 2, m /= 2) {
+    if (h > 0) {
+#pragma unroll
+      for (int i = 0; i < N / 2; ++i) {
+        if (i >= h) continue;
+        const bool up = lane & m;
+        const float mine = up ? v[i + h] : v[i], other = up ? v[i] : v[i + h];
+        v[i] = mine + __shfl_xor_sync(0xffffffffu, other, m);
+      }
+    } else {
+      v[0] += __shfl_xor_sync(0xffffffffu, v[0], m);
+    }
   }
+  return v[0];
+}
+
+// The same with rows in 16-byte pieces.  A team takes kBatch rows at a time, and every
+// thread copies its own columns of the next ones to shared memory meanwhile (no barrier:
+// nobody else reads them): the copies keep HBM busy while a batch waits for its sums, of
+// which there is one barrier a batch, and the registers hold sums alone.
+constexpr int kBatch = 4;
+template <class TX, class TY>
+constexpr int kPieces = (sizeof(TX) + sizeof(TY)) / 2;  // of x and dy, a thread's 8 columns
+template <class TX, class TY, int V>
+constexpr int kRowsOf = kBatch / V / (kPieces<TX, TY> > 2 ? 2 : 1);
+
+template <class TX, class TY, int V>
+__global__ void __maxnreg__(V == 1 ? 80 : 128) norm_bwd_rows_kernel(const NormParams p) {
+  constexpr int R = kRowsOf<TX, TY, V>, N = 2 * R;
+  constexpr int PX = sizeof(TX) / 2, PY = sizeof(TY) / 2;  // pieces of x and dy
+  __shared__ float red[2][16][N];
+  extern __shared__ __align__(16) uint8_t ring[];  // [2][R][V][PX + PY][threads] pieces; then [2][C] sums
+  const Team team(p.W);
+  const TX* x = static_cast<const TX*>(p.x);
+  const TY* dy = static_cast<const TY*>(p.dy);
+  TX* dx = static_cast<TX*>(p.dx);
+  const int lane = threadIdx.x & 31;
+  const float inv_c = 1.f / static_cast<float>(p.C);
+  const int part = blockIdx.x % p.parts;
+  const long long group = blockIdx.x / p.parts;
+  const long long n = p.rows_per_group;
+  const long long r0 = group * n + part * n / p.parts, r1 = group * n + (part + 1) * n / p.parts;
+  const size_t g = static_cast<size_t>(group) * p.C;
+  auto column = [&](int k) { return (k * team.W * 32 + team.t) * 8; };
+  const uint32_t mine = smem_u32(ring) + 16 * threadIdx.x;
+  const uint32_t piece = 16 * blockDim.x;
+  auto at = [&](int stage, int r, int k, int i) {
+    return mine + piece * (((stage * R + r) * V + k) * (PX + PY) + i);
+  };
+  pdl_wait();
+  pdl_trigger();
+  float mean[R], rstd[R], next_mean[R], next_rstd[R];
+  auto fetch = [&](long long row, int stage) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      if (row + r >= r1) continue;
+      next_mean[r] = p.mean[row + r];
+      next_rstd[r] = p.rstd[row + r];
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        if (column(k) >= p.C) continue;
+        const size_t from = static_cast<size_t>(row + r) * p.C + column(k);
+#pragma unroll
+        for (int i = 0; i < PX; ++i) copy_16b(at(stage, r, k, i), reinterpret_cast<const uint4*>(x + from) + i);
+#pragma unroll
+        for (int i = 0; i < PY; ++i) copy_16b(at(stage, r, k, PX + i), reinterpret_cast<const uint4*>(dy + from) + i);
+      }
+    }
+  };
+  long long row = r0 + static_cast<long long>(team.index) * R;
+  const long long step = static_cast<long long>(team.count) * R;
+#pragma unroll
+  for (int r = 0; r < R; ++r) next_mean[r] = next_rstd[r] = 0.f;
+  fetch(row, 0);
+  copy_commit();
+  float w[V][8], aw[V][8], ab[V][8];
+#pragma unroll
+  for (int k = 0; k < V; ++k) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) aw[k][e] = ab[k][e] = 0.f, w[k][e] = 1.f;
+    if (p.weight && column(k) < p.C) load_param<8>(p.weight, p.param_f32, g + column(k), w[k]);
+  }
+  // x and dy of a row's columns, as fp32
+  auto read = [&](int stage, int r, int k, float (&vx)[8], float (&vy)[8]) {
+    Raw<TX, 8> rx;
+    Raw<TY, 8> ry;
+#pragma unroll
+    for (int i = 0; i < PX; ++i) reinterpret_cast<uint4*>(&rx)[i] = shared_16b(at(stage, r, k, i));
+#pragma unroll
+    for (int i = 0; i < PY; ++i) reinterpret_cast<uint4*>(&ry)[i] = shared_16b(at(stage, r, k, PX + i));
+    rx.get(vx);
+    ry.get(vy);
+  };
+  for (int turn = 0; row < r1; row += step, turn ^= 1) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) mean[r] = next_mean[r], rstd[r] = next_rstd[r];
+    fetch(row + step, turn ^ 1);
+    copy_commit();
+    copy_wait<1>();
+    float s[N];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      s[2 * r] = s[2 * r + 1] = 0.f;
+      if (row + r >= r1) continue;
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        if (column(k) >= p.C) continue;
+        float xh[8], gr[8];
+        read(turn, r, k, xh, gr);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          xh[e] = (xh[e] - mean[r]) * rstd[r];
+          aw[k][e] = fmaf(gr[e], xh[e], aw[k][e]);
+          ab[k][e] += gr[e];
+          gr[e] *= w[k][e];
+          s[2 * r] += gr[e];
+          s[2 * r + 1] = fmaf(gr[e], xh[e], s[2 * r + 1]);
+        }
+      }
+    }
+    float sum = warp_sums<N>(s);
+    constexpr int kShare = 32 / N;  // lanes of a value
+    int from = kShare;
+    if (p.W > 1) {
+      if (lane % kShare == 0) red[turn][team.index * p.W + team.warp][lane / kShare] = sum;
+      asm volatile("bar.sync %0, %1;" ::"r"(team.index + 1), "r"(p.W * 32) : "memory");
+      sum = 0.f;
+      for (int i = lane / N; i < p.W; i += kShare) sum += red[turn][team.index * p.W + i][lane % N];
+#pragma unroll
+      for (int m = N; m < 32; m *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, m);
+      from = 1;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) s[i] = __shfl_sync(0xffffffffu, sum, i * from) * inv_c;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      if (row + r >= r1) continue;
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        if (column(k) >= p.C) continue;
+        float xh[8], gr[8];
+        read(turn, r, k, xh, gr);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          gr[e] = rstd[r] * (gr[e] * w[k][e] - s[2 * r] - (xh[e] - mean[r]) * rstd[r] * s[2 * r + 1]);
+        store<8>(dx + static_cast<size_t>(row + r) * p.C + column(k), gr);
+      }
+    }
+  }
+  if (!p.dweight && !p.dbias) return;
+  copy_wait<0>();
+  __syncthreads();  // the ring is read
+  float* sums = reinterpret_cast<float*>(ring);
+  for (int t = 0; t < team.count; ++t) {
+    if (team.index == t) {
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        const int c = column(k);
+        if (c >= p.C) continue;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          sums[c + e] = t == 0 ? aw[k][e] : sums[c + e] + aw[k][e];
+          sums[p.C + c + e] = t == 0 ? ab[k][e] : sums[p.C + c + e] + ab[k][e];
+        }
+      }
+    }
+    __syncthreads();
+  }
+  write_params(p, g, sums);
 }
 
 // dw and db of a group from its blocks' partials: `split` threads a column, each an
@@ -409,28 +590,40 @@ __global__ void __launch_bounds__(256) norm_params_kernel(const NormParams p, in
   }
 }
 
-// Warps a row and accesses a thread.  VEC = 8: forward the fewest warps that hold the
-// row in ten accesses; backward, which holds three times as much a column and sums
-// over rows, the fewest slots with two accesses a thread (four of the widest rows).
-// VEC = 1: the fewest slots with 8 accesses, 16 of the widest rows.
+// The row kernel's shape: 8 or 16 columns a thread, W warps a row, teams up to 256 threads;
+// blocks of an SM up to 768 threads (their registers, and 256 bytes of the ring each).
+struct RowsShape {
+  int W, V, threads, blocks;
+};
+RowsShape rows_shape(int C) {
+  RowsShape s{};
+  s.V = C <= 4096 ? 1 : 2;
+  s.W = (C + 256 * s.V - 1) / (256 * s.V);
+  s.threads = 32 * s.W * (s.W < 8 ? 8 / s.W : 1);
+  s.blocks = 768 / (s.threads * s.V) < 1 ? 1 : 768 / (s.threads * s.V);
+  return s;
+}
+
+// Warps a row and accesses a thread of the other kernels.  VEC = 8 (forward): the fewest
+// warps that hold the row in ten accesses.  VEC = 1: the fewest slots with 8 accesses, 16
+// of the widest rows.
 struct Shape {
   int W, V, threads;
 };
-int form(int V, bool vec, bool backward) {  // the least V that is compiled
+int form(int V, bool vec) {  // the least V that is compiled
   if (!vec) return V <= 2 ? 2 : V <= 4 ? 4 : V <= 8 ? 8 : V <= 16 ? 16 : 99;
-  if (backward) return V <= 4 ? V : 99;
   return V <= 4 ? V : V <= 6 ? 6 : V <= 10 ? 10 : 99;
 }
 // Few rows (forward): all SMs' warps for them, a thread's part of a row as short as can be.
-Shape shape_of(int C, bool vec, bool backward, bool few) {
+Shape shape_of(int C, bool vec, bool few) {
   const int elems = vec ? 256 : 32;
-  const int max_v = vec ? (!backward && !few ? 10 : C <= 4096 ? 2 : 4) : (C <= 2048 ? 8 : 16);
+  const int max_v = vec ? (!few ? 10 : C <= 4096 ? 2 : 4) : (C <= 2048 ? 8 : 16);
   const int max_w = vec || C <= 2048 ? 8 : 16;
   Shape best{0, 0, 0};
   for (int W = 1; W <= max_w; ++W) {
-    const int V = form((C + elems * W - 1) / (elems * W), vec, backward);
+    const int V = form((C + elems * W - 1) / (elems * W), vec);
     if (V > max_v) continue;
-    if (best.W == 0 || (W * V < best.W * best.V && (backward || few || !vec))) best = {W, V, 0};
+    if (best.W == 0 || (W * V < best.W * best.V && (few || !vec))) best = {W, V, 0};
   }
   best.threads = 32 * best.W * (best.W < 8 ? 8 / best.W : 1);
   return best;
@@ -439,12 +632,11 @@ Shape shape_of(int C, bool vec, bool backward, bool few) {
 template <class X, class Y, int VEC, int V>
 struct Kernels {
   static constexpr auto fwd() { return norm_fwd_kernel<X, Y, VEC, V>; }
-  static constexpr auto bwd() { return norm_bwd_kernel<X, Y, VEC, V>; }
   static constexpr int blocks = fwd_blocks(VEC, V, sizeof(X));
 };
 
 // f of the kernels for these types and accesses a thread.
-template <bool BACKWARD, class F>
+template <class F>
 cudaError_t by_shape(const NormParams& p, bool vec, int V, F&& f) {
   auto types = [&](auto tx, auto ty) {
     using X = decltype(tx);
@@ -453,10 +645,8 @@ cudaError_t by_shape(const NormParams& p, bool vec, int V, F&& f) {
       if (V == 1) return f(Kernels<X, Y, 8, 1>{});
       if (V == 2) return f(Kernels<X, Y, 8, 2>{});
       if (V == 3) return f(Kernels<X, Y, 8, 3>{});
-      if constexpr (!BACKWARD) {
-        if (V == 6) return f(Kernels<X, Y, 8, 6>{});
-        if (V == 10) return f(Kernels<X, Y, 8, 10>{});
-      }
+      if (V == 6) return f(Kernels<X, Y, 8, 6>{});
+      if (V == 10) return f(Kernels<X, Y, 8, 10>{});
       return f(Kernels<X, Y, 8, 4>{});
     }
     if (V == 2) return f(Kernels<X, Y, 1, 2>{});
@@ -469,24 +659,43 @@ cudaError_t by_shape(const NormParams& p, bool vec, int V, F&& f) {
   return types(float{}, float{});
 }
 
+// The backward's shared memory: the rows' ring, or the sums of the widest row.
+constexpr int kNormMaxSmem = 512 * 256;
+static_assert(kNormMaxSmem >= 2 * kNormMaxC * static_cast<int>(sizeof(float)), "the sums fit");
+
+template <auto kKernel>
+cudaError_t run_bwd(const NormParams& p, unsigned blocks, int threads, size_t smem, int dev, cudaStream_t s) {
+  static OncePerDevice prepared;
+  const cudaError_t e = prepared(
+      dev, [] { return cudaFuncSetAttribute(kKernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kNormMaxSmem); });
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg;
+  cudaLaunchAttribute attr;
+  pdl_config(cfg, attr, dim3(blocks), dim3(threads), smem, s);
+  return cudaLaunchKernelEx(&cfg, kKernel, p);
+}
+
 }  // namespace
 
 int norm_parts(long long rows_per_group, int C, int groups) {
   // as many blocks as the SMs hold, by the form that aligned rows take
-  const bool vec = C % 8 == 0;
-  const Shape sh = shape_of(C, vec, true, false);
-  long long parts = static_cast<long long>(kNormSms) * bwd_blocks(vec ? 8 : 1, sh.V, 2) * max_threads(vec ? 8 : 1, sh.V) /
-                    sh.threads / groups;
+  long long parts;
+  if (C % 8 == 0) {
+    parts = static_cast<long long>(kNormSms) * rows_shape(C).blocks / groups;
+  } else {
+    const Shape sh = shape_of(C, false, false);
+    parts = static_cast<long long>(kNormSms) * bwd_blocks(sh.V) * max_threads(1, sh.V) / sh.threads / groups;
+  }
   if (parts > rows_per_group) parts = rows_per_group;
   return parts < 1 ? 1 : static_cast<int>(parts);
 }
 
 cudaError_t launch_norm_fwd(NormParams p, bool vec, int sms, cudaStream_t s) {
-  const Shape sh = shape_of(p.C, vec, false, p.rows <= 8ll * sms);
+  const Shape sh = shape_of(p.C, vec, p.rows <= 8ll * sms);
   p.W = sh.W;
   const int teams = sh.threads / 32 / sh.W;
   const long long blocks = (p.rows + teams - 1) / teams;
-  return by_shape<false>(p, vec, sh.V, [&](auto k) {
+  return by_shape(p, vec, sh.V, [&](auto k) {
     // as many blocks as the SMs hold (of fewer threads, more)
     const long long most = static_cast<long long>(sms) * decltype(k)::blocks * 256 / sh.threads;
     cudaLaunchConfig_t cfg;
@@ -497,28 +706,46 @@ cudaError_t launch_norm_fwd(NormParams p, bool vec, int sms, cudaStream_t s) {
 }
 
 cudaError_t launch_norm_bwd(NormParams p, bool vec, int dev, cudaStream_t s) {
-  const Shape sh = shape_of(p.C, vec, true, false);
-  p.W = sh.W;
-  const size_t smem = static_cast<size_t>(2) * p.C * sizeof(float);
-  cudaLaunchConfig_t cfg;
-  cudaLaunchAttribute attr;
-  pdl_config(cfg, attr, dim3(static_cast<unsigned>(p.groups) * p.parts), dim3(sh.threads), smem, s);
-  const cudaError_t e = by_shape<true>(p, vec, sh.V, [&](auto k) {
-    constexpr auto bwd = decltype(k)::bwd();
-    if (smem > 48 * 1024) {
-      static OncePerDevice prepared;
-      const cudaError_t e0 = prepared(dev, [&] {
-        return cudaFuncSetAttribute(bwd, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                    2 * kNormMaxC * static_cast<int>(sizeof(float)));
-      });
-      if (e0 != cudaSuccess) return e0;
-    }
-    return cudaLaunchKernelEx(&cfg, bwd, p);
-  });
+  const size_t sums = static_cast<size_t>(2) * p.C * sizeof(float);
+  const unsigned blocks = static_cast<unsigned>(p.groups) * p.parts;
+  cudaError_t e;
+  auto types = [&](auto f) {
+    if (!p.x_f32) return f(bf16{}, bf16{});
+    if (!p.y_f32) return f(float{}, bf16{});
+    return f(float{}, float{});
+  };
+  if (vec) {
+    const RowsShape sh = rows_shape(p.C);
+    p.W = sh.W;
+    e = types([&](auto tx, auto ty) {
+      using X = decltype(tx);
+      using Y = decltype(ty);
+      auto smem = [&](int rows) {
+        const size_t ring = static_cast<size_t>(2) * rows * sh.V * kPieces<X, Y> * 16 * sh.threads;
+        return ring > sums ? ring : sums;
+      };
+      return sh.V == 1
+                 ? run_bwd<norm_bwd_rows_kernel<X, Y, 1>>(p, blocks, sh.threads, smem(kRowsOf<X, Y, 1>), dev, s)
+                 : run_bwd<norm_bwd_rows_kernel<X, Y, 2>>(p, blocks, sh.threads, smem(kRowsOf<X, Y, 2>), dev, s);
+    });
+  } else {
+    const Shape sh = shape_of(p.C, false, false);
+    p.W = sh.W;
+    e = types([&](auto tx, auto ty) {
+      using X = decltype(tx);
+      using Y = decltype(ty);
+      if (sh.V == 2) return run_bwd<norm_bwd_kernel<X, Y, 2>>(p, blocks, sh.threads, sums, dev, s);
+      if (sh.V == 4) return run_bwd<norm_bwd_kernel<X, Y, 4>>(p, blocks, sh.threads, sums, dev, s);
+      if (sh.V == 8) return run_bwd<norm_bwd_kernel<X, Y, 8>>(p, blocks, sh.threads, sums, dev, s);
+      return run_bwd<norm_bwd_kernel<X, Y, 16>>(p, blocks, sh.threads, sums, dev, s);
+    });
+  }
   if (e != cudaSuccess || p.parts == 1 || (!p.dweight && !p.dbias)) return e;
   int split = 1;
   while (split < 32 && p.parts >= 16 * split) split *= 2;
   const int columns = 256 / split;
+  cudaLaunchConfig_t cfg;
+  cudaLaunchAttribute attr;
   pdl_config(cfg, attr, dim3((2 * p.C + columns - 1) / columns, p.groups < 65535 ? p.groups : 65535), dim3(256), 0, s);
   return cudaLaunchKernelEx(&cfg, norm_params_kernel, p, split);
 }

@@ -498,6 +498,21 @@ __device__ __forceinline__ float ex2_approx(float x) {
   return y;
 }
 
+// 16 bytes from global to shared memory, asynchronously, and back into registers.
+__device__ __forceinline__ void copy_16b(uint32_t to, const void* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ uint4 shared_16b(uint32_t from) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(from) : "memory");
+  return v;
+}
+
 // Programmatic dependent launch: a kernel launched with programmatic
 // stream serialization may start while the previous kernel in the stream
 // finishes; pdl_wait blocks until that kernel has completed and its memory
