@@ -326,7 +326,8 @@ mw_status mw_bca_cache_fwd_noalloc(const void* q, const void* k_new, const void*
  * int32, the valid states of each sample (the first kv_len[b]; below 0 counts as
  * 0, above S as S), or NULL: all S.  What K and V hold in the other places does
  * not matter (NaN included).  A row that sees no state has O = 0, LSE = -inf.
- * lse (fp32 [B, H, M]) may be NULL.  M = 0 and S = 0 are valid.
+ * lse (fp32 [B, H, M]) may be NULL; it is summed in fp32 from the weights before
+ * their rounding to bf16.  M = 0 and S = 0 are valid.
  * workspace: mw_xattn_workspace_size() bytes, 256-byte aligned (NULL if 0).
  */
 size_t mw_xattn_workspace_size(int B, int H, int Hkv, int M, int S, int d);
@@ -338,7 +339,9 @@ mw_status mw_xattn_fwd(const void* q, const void* k, const void* v, const int* k
  * Its gradients: with D_i = <dO_i, O_i> and dS = P (dO V^T - D),
  *     dV = P^T dO,   dK = scale dS^T Q,   dQ = scale dS K,
  * those of K and V summed over the query heads that share them, and 0 in the
- * places past kv_len.  o and lse are the forward's.
+ * places past kv_len.  o and lse are the forward's: D carries the rounding of o to
+ * bf16, whose share of dQ is proportional to the row's mean key (dQ itself depends
+ * on the keys' differences only).
  */
 size_t mw_xattn_bwd_workspace_size(int B, int H, int Hkv, int M, int S, int d);
 mw_status mw_xattn_bwd(const void* q, const void* k, const void* v, const int* kv_len, const void* o,
@@ -393,7 +396,8 @@ mw_status mw_device_status(void* stream, int clear);
  *                      (the workspace size follows this setting)
  *   "wait_budget_ms"   time limit of every bounded wait inside the kernels
  *                      (default 2000)
- *   "debug_skip_q_load" non-zero: the forward and backward kernels never
+ *   "debug_skip_q_load" non-zero: the forward and backward kernels (cross
+ *                      attention's of more than 16 rows a head too) never
  *                      load Q, so their first wait expires; for testing the
  *                      timeout path only
  *   "fwd_group_waves"  forward CTAs per head group, in multiples of the SM
@@ -404,9 +408,9 @@ mw_status mw_device_status(void* stream, int clear);
  *                      bytes within 48 MB, taken where list scheduling
  *                      predicts a 1% shorter launch); 1 = one head after
  *                      another; head dims over 80 always run head by head
- *   "pdl"              0 launches the forward, the split combine and the
- *                      commit without programmatic dependent launch
- *                      (default 1)
+ *   "pdl"              0 launches the forwards, the split combine, the
+ *                      commit and the layer norm's kernels without
+ *                      programmatic dependent launch (default 1)
  * Returns MW_ERR_INVALID_ARG for an unknown name or a negative value.
  */
 mw_status mw_set_option(const char* name, long long value);

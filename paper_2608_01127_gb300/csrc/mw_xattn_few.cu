@@ -11,7 +11,8 @@
 // with eight; tcgen05 with its 128 rows 40 us, one warp's softmax a key tile).  The
 // keys of a head are shared by up to 16 CTAs, one thread-block cluster, which join
 // their maxima, sums and outputs through distributed shared memory: one launch, no
-// workspace.
+// workspace.  Measured: 8 x 20 rows on 8 x 4 heads of 128, 8192 keys each (134 MB) 25 us
+// (5.4 TB/s, of which some 6 us are the start, the first loads and the join).
 #include <cooperative_groups.h>
 
 #include "mw_internal.h"
