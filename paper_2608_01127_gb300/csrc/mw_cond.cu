@@ -341,7 +341,6 @@ mw_status mw_xattn_bwd(const void* q, const void* k, const void* v, const int* k
   p.pieces = p.key_major ? z.BH * p.ranges * p.k_tiles : 0;
   p.dkv_whole = ws.dkv_whole;
   p.zero_dq = p.key_major;
-  p.wide_dq = wide_rows(dq, d);
   p.wide_dkv = wide_rows(dk, d) && wide_rows(dv, d);
   p.scale = scale;
   p.scale_log2 = scale * 1.4426950408889634f;
@@ -367,10 +366,8 @@ mw_status mw_xattn_bwd(const void* q, const void* k, const void* v, const int* k
     MW_TRY(make_map(&m.dv, p.dkv_acc + static_cast<size_t>(z.BH) * ws.S_pad * D, ws.S_pad, z.BH, D, "dv_acc", 32,
                     true, d));
   }
-  if (D == 64)
-    MW_TRY(encode_bias_map(&m.bias, p.bias, ws.M_pad, z.BH, kTileRows));
-  else
-    MW_TRY(encode_rows_map(&m.dq_out, dq, z.rows, z.BH, d, false));
+  if (D == 64) MW_TRY(encode_bias_map(&m.bias, p.bias, ws.M_pad, z.BH, kTileRows));
+  MW_TRY(encode_rows_map(&m.dq_out, dq, z.rows, z.BH, d, D == 64));
   return launch_status(launch_xattn_bwd(D, mma_d(d), m, p, scope.device(), std::min(sm_count(), kXattnMaxCtas), s),
                        "cross attention backward launch");
 }

@@ -283,7 +283,7 @@ struct XattnBwdParams {
   int pieces;          // key-major: BH * ranges * k_tiles
   bool dkv_whole;      // one sweep makes all of a key tile's dK and dV
   bool zero_dq;        // dq_acc is only added to
-  bool wide_dq, wide_dkv;  // every row of the outputs starts at a multiple of 32 bytes
+  bool wide_dkv;  // every row of dK and dV starts at a multiple of 32 bytes
   float scale, scale_log2;
   float* lse2;         // [BH, M_pad] (d = 64: unused, as delta)
   float* delta;        // [BH, M_pad]

@@ -777,8 +777,10 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
         if (lane == 0) {
           uint8_t* stg = smem + L::OFF_STG + L::BOXES * wq * L::BOX_BYTES;
           mbar_arrive_expect_tx(&acc_full[wq], 2 * L::BOX_BYTES);
-          for (int c = 0; c < 2; ++c)
+          for (int c = 1; c >= 0; --c) {
+            if (c == 0) bulk_wait_read<0>();  // the rows of the step before have left it
             tma_load_3d(stg + c * L::BOX_BYTES, &tm_dq, &acc_full[wq], 32 * c, (w.q0 + j) * QN + 32 * wq, w.bh);
+          }
         }
         ++loads;
       };
@@ -854,12 +856,24 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
           // lanes = query rows
           static_assert(D == 64 || L::DQT, "the drain below covers two 32-column boxes");
           const int row = q0 + wq * 32;
-          auto store_rows = [&](const uint32_t (&r)[32], int c) {
-            float v[32];
+          // bf16 rows of 128 bytes, 16-byte chunk k of row i at k ^ (i & 7); the map clips
+          // rows past the caller's
+          auto store_rows = [&](const uint32_t (&r)[2][32], uint8_t* stg) {
 #pragma unroll
-            for (int k = 0; k < 32; ++k) v[k] = __uint_as_float(r[k]) * p.scale;
-            if (row + lane < p.M)
-              store_row32(p.dq + (static_cast<size_t>(w.bh) * p.M + row + lane) * D + 32 * c, v, 4, p.wide_dq);
+            for (int k = 0; k < 8; ++k) {
+              uint32_t v[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                v[i] = pack_bf16x2(__uint_as_float(r[k >> 2][8 * (k & 3) + 2 * i]) * p.scale,
+                                   __uint_as_float(r[k >> 2][8 * (k & 3) + 2 * i + 1]) * p.scale);
+              *reinterpret_cast<uint4*>(stg + lane * 128 + ((k ^ (lane & 7)) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+              tma_store_3d(&tm_dqo, stg, 0, row, w.bh);
+              bulk_commit_group();
+            }
           };
           uint32_t r[2][32];
           tmem_ld32(lane_base + L::DQ_COL, r[0]);
@@ -882,16 +896,18 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
                 r[c][4 * i + 2] = __float_as_uint(__uint_as_float(r[c][4 * i + 2]) + x.z);
                 r[c][4 * i + 3] = __float_as_uint(__uint_as_float(r[c][4 * i + 3]) + x.w);
               }
-            fence_proxy_async_smem();  // the boxes are read before the next copy into them
-            __syncwarp();
+            store_rows(r, smem + L::OFF_STG + L::BOXES * wq * L::BOX_BYTES);
+            box = 1;  // (the first one is being read)
             if (j + 1 < w.n_q) load_acc(j + 1);
-          }
+          } else if (whole) {
+            uint8_t* stg = smem + L::OFF_STG + (L::BOXES * wq + box) * L::BOX_BYTES;
+            box ^= 1;
+            if (lane == 0) bulk_wait_read<1>();  // the TMA unit has read this box
+            __syncwarp();
+            store_rows(r, stg);
+          } else {
 #pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            if (whole || finish)
-              store_rows(r[c], c);
-            else
-              put_rows(&tm_dq, r[c], 32 * c, row, add);
+            for (int c = 0; c < 2; ++c) put_rows(&tm_dq, r[c], 32 * c, row, add);
           }
           __syncwarp();
         }
