@@ -52,28 +52,29 @@ struct Layout {
   static constexpr int QTILE = REG * QREGION;
   static constexpr int QSTAGES = (D == 64) ? 3 : 2;
   static constexpr int DOSTAGES = (D == 64) ? 3 : 1;
-  static constexpr int KBUFS = (D == 64) ? 2 : 1;    // K tiles: the next sweep's S while dQ ends this one
   static constexpr int DS_BYTES = (QN / 64) * KREGION;  // dS^T: 128 key rows x QN columns
-  static constexpr int DS_BUFS = 1;
   static constexpr int BOX_BYTES = 32 * 32 * 4;
-  static constexpr int BOXES = 2;                    // staging boxes per drain warp
+  // staging boxes per drain warp: two for sums, d = 64 a third that dQ in bf16 leaves from
+  static constexpr int BOXES = 2;
+  static constexpr int OUT_BYTES = (D == 64) ? 4 * BOX_BYTES : 0;
   static constexpr bool FOLD = (D == 64);            // LSE and D through tf32 MMAs
   static constexpr int BIAS_BYTES = FOLD ? QN * 32 : 0;
   static constexpr int QSTRIDE = QTILE + BIAS_BYTES;
   static constexpr int VEC_BYTES = FOLD ? 0 : QN * 4;
   static constexpr int ONES_BYTES = FOLD ? 512 : 0;
   static constexpr int OFF_K = 0;
-  static constexpr int OFF_V = OFF_K + KBUFS * KTILE;
+  static constexpr int OFF_V = OFF_K + KTILE;
   static constexpr int OFF_Q = OFF_V + KTILE;
   static constexpr int OFF_DO = OFF_Q + QSTAGES * QSTRIDE;
   static constexpr int OFF_DS = OFF_DO + DOSTAGES * QTILE;
-  static constexpr int OFF_STG = OFF_DS + DS_BUFS * DS_BYTES;
-  static constexpr int OFF_LSE = OFF_STG + BOXES * 4 * BOX_BYTES;
+  static constexpr int OFF_STG = OFF_DS + DS_BYTES;
+  static constexpr int OFF_OUT = OFF_STG + BOXES * 4 * BOX_BYTES;
+  static constexpr int OFF_LSE = OFF_OUT + OUT_BYTES;
   static constexpr int OFF_DELTA = OFF_LSE + QSTAGES * VEC_BYTES;
   static constexpr int OFF_ONES = OFF_DELTA + 2 * VEC_BYTES;
   static constexpr int OFF_BAR = OFF_ONES + ONES_BYTES;
   static constexpr int SLOTS = 4;  // sweeps announced ahead
-  static constexpr int NBAR = 3 * KBUFS + 3 + 2 * (QSTAGES + DOSTAGES) + 9 + 2 * DS_BUFS + 2 * SLOTS + 4;
+  static constexpr int NBAR = 6 + 2 * (QSTAGES + DOSTAGES) + 11 + 2 * SLOTS + 4;
   static constexpr int OFF_SLOTS = (OFF_BAR + NBAR * 8 + 15) / 16 * 16;
   static constexpr int OFF_MISC = OFF_SLOTS + SLOTS * 32;
   static constexpr int BYTES = OFF_MISC + 16;
@@ -207,7 +208,6 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
   constexpr int ND = L::DOSTAGES;
   constexpr int QN = L::QN;
   constexpr int CW = L::CW;
-  constexpr int NB = L::DS_BUFS;
   extern __shared__ __align__(1024) uint8_t smem[];
   if ((smem_u32(smem) & 1023u) != 0u) {
     // nothing runs without aligned shared memory: report it, and leave zeros (the
@@ -216,11 +216,10 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
     if (blockIdx.x == 0) leave_zeros(p, threadIdx.x, L::THREADS);
     return;  // uniform across the CTA, before any barrier or TMEM use
   }
-  constexpr int NK = L::KBUFS;
   uint64_t* k_full = reinterpret_cast<uint64_t*>(smem + L::OFF_BAR);
-  uint64_t* k_raw = k_full + NK;   // a K tile that warp 15 makes ready, then k_full
-  uint64_t* k_empty = k_raw + NK;
-  uint64_t* v_full = k_empty + NK;
+  uint64_t* k_raw = k_full + 1;    // a K tile that warp 15 makes ready, then k_full
+  uint64_t* k_empty = k_raw + 1;
+  uint64_t* v_full = k_empty + 1;
   uint64_t* v_raw = v_full + 1;
   uint64_t* v_empty = v_raw + 1;
   uint64_t* q_full = v_empty + 1;
@@ -237,8 +236,8 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
   uint64_t* dkv_full = dq_free + 1;
   uint64_t* dkv_free = dkv_full + 1;
   uint64_t* p_ready = dkv_free + 1;
-  uint64_t* ds_free = p_ready + NB;
-  uint64_t* w_full = ds_free + NB;         // a sweep is announced, and
+  uint64_t* ds_free = p_ready + 1;
+  uint64_t* w_full = ds_free + 1;          // a sweep is announced, and
   uint64_t* w_empty = w_full + L::SLOTS;   // read by all roles
   uint64_t* acc_full = w_empty + L::SLOTS;  // dQ so far, for a drain warp each
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + L::OFF_MISC);
@@ -257,11 +256,9 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
     }
   }
   if (threadIdx.x == 0) {
-    for (int b = 0; b < NK; ++b) {
-      mbar_init(&k_full[b], 1);
-      mbar_init(&k_raw[b], 1);
-      mbar_init(&k_empty[b], 2);
-    }
+    mbar_init(k_full, 1);
+    mbar_init(k_raw, 1);
+    mbar_init(k_empty, 2);
     for (int b = 0; b < L::SLOTS; ++b) {
       mbar_init(&w_full[b], 1);
       mbar_init(&w_empty[b], 15);  // the other warps
@@ -287,10 +284,8 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
     mbar_init(dq_free, 4);
     mbar_init(dkv_full, 2);
     mbar_init(dkv_free, 4);
-    for (int b = 0; b < NB; ++b) {
-      mbar_init(&p_ready[b], 8);
-      mbar_init(&ds_free[b], 1);
-    }
+    mbar_init(p_ready, 8);
+    mbar_init(ds_free, 1);
     *abort_flag = 0;
     fence_mbar_init();
   }
@@ -340,8 +335,8 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
       prefetch_tmap(&tm_do);
       int sw = 0, raws = 0, n_q = 0, n_do = 0;  // K tiles, V tiles through warp 15, Q and dO tiles so far
       int n_v = 0;                              // V tiles (one a sweep, loaded ahead of K)
-      uint32_t k_raws = 0, k_was_raw = 0;       // per K buffer: parity of those through warp 15; the last one was
-      bool ok = true, raw = false;
+      int k_raws = 0;                           // K tiles through warp 15
+      bool ok = true, raw = false, k_was_raw = false;
       Plan plan(p);
       auto load_q = [&](int q) {
         const int st = n_q % NQ;
@@ -380,45 +375,31 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
         mbar_arrive(&w_full[slot]);  // (releases the stores above)
         if (!more) break;
         raw = w.ragged(p.S);
-        const int kb = sw % NK;
-        // Q, dO and V of the sweep's first step; K (one buffer) waits for the last dQ of
-        // the sweep before
+        // Q, dO and V of the sweep's first step; K waits for the last dQ of the sweep before
         if (!(ok = load_q(w.query_row(0, p.key_major)))) break;
         auto load_tile = [&](uint8_t* dst, const CUtensorMap* map, uint64_t* bar) {
           mbar_arrive_expect_tx(bar, L::KTILE);
           for (int r = 0; r < L::REG; ++r)
             tma_load_3d(dst + r * L::KREGION, map, bar, 64 * r, w.kt * kTileRows, w.bh);
         };
-        auto load_k = [&]() {
-          if (!mbar_wait(&k_empty[kb], ((sw / NK) & 1) ^ 1, ctl)) return false;
-          load_tile(sK + kb * L::KTILE, &tm_k, raw ? &k_raw[kb] : &k_full[kb]);
-          if (raw) k_raws ^= 1u << kb;
-          k_was_raw = (k_was_raw & ~(1u << kb)) | (raw ? 1u << kb : 0u);
-          ++sw;
-          return true;
-        };
-        if (NK > 1 && !(ok = load_k())) break;
         if (!(ok = mbar_wait(v_empty, (n_v & 1) ^ 1, ctl))) break;
         load_tile(sV, &tm_v, raw ? v_raw : v_full);
         ++n_v;
         raws += raw;
         if (!(ok = load_do(w.query_row(0, p.key_major)))) break;
-        if (NK == 1 && !(ok = load_k())) break;
+        if (!(ok = mbar_wait(k_empty, (sw & 1) ^ 1, ctl))) break;
+        load_tile(sK, &tm_k, raw ? k_raw : k_full);
+        k_raws += raw;
+        k_was_raw = raw;
+        ++sw;
         for (int j = 1; ok && j < w.n_q; ++j)
           ok = load_q(w.query_row(j, p.key_major)) && load_do(w.query_row(j, p.key_major));
         if (!ok) break;
       }
       if (*abort_flag || !ok) {
         // let every copy this CTA started land before shared memory goes away
-        for (int i = max(0, sw - NK); i < sw; ++i) {
-          const int kb = i % NK;
-          if ((k_was_raw >> kb) & 1)
-            drain_wait(&k_raw[kb], ((k_raws >> kb) & 1) ^ 1, p.budget_ns);
-          else
-            drain_wait(&k_full[kb], (i / NK) & 1, p.budget_ns);
-        }
-        // (a sweep whose V is not loaded yet leaves the one before, which has been read)
-        if (n_v > 0 && (NK == 1 || n_v == sw)) drain_wait(raw ? v_raw : v_full, ((raw ? raws : n_v) - 1) & 1, p.budget_ns);
+        if (sw > 0) drain_wait(k_was_raw ? k_raw : k_full, ((k_was_raw ? k_raws : sw) - 1) & 1, p.budget_ns);
+        if (n_v > 0) drain_wait(raw ? v_raw : v_full, ((raw ? raws : n_v) - 1) & 1, p.budget_ns);
         for (int j = max(0, n_q - NQ); j < n_q; ++j) drain_wait(&q_full[j % NQ], (j / NQ) & 1, p.budget_ns);
         for (int j = max(0, n_do - ND); j < n_do; ++j) drain_wait(&do_full[j % ND], (j / ND) & 1, p.budget_ns);
       }
@@ -438,8 +419,8 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
     const uint32_t do_kmaj0 = sdesc_sw128(smem_u32(sDO), 16);
     const uint32_t q_mn0 = sdesc_sw128(smem_u32(sQ), L::QREGION);
     const uint32_t do_mn0 = sdesc_sw128(smem_u32(sDO), L::QREGION);
-    const uint32_t ds_mn0 = sdesc_sw128(smem_u32(sDS), L::KREGION);
-    const uint32_t ds_kmaj0 = sdesc_sw128(smem_u32(sDS), 16);
+    const uint32_t ds_mn = sdesc_sw128(smem_u32(sDS), L::KREGION);
+    const uint32_t ds_kmaj = sdesc_sw128(smem_u32(sDS), 16);
     const uint64_t ones_l = sdesc_sw32(smem_u32(smem + L::OFF_ONES), 0);
     const uint64_t ones_d = sdesc_sw32(smem_u32(smem + L::OFF_ONES + 256), 0);
     const uint64_t bias0 = sdesc_sw32(smem_u32(sQ + L::QTILE), 256);
@@ -457,8 +438,8 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
         umma_ss(tmem + d_col, sdesc_add(a, L::KREGION), sdesc_add(b, L::QREGION), idesc_s, 1u);
       }
     };
-    auto issue_s = [&](int g, uint32_t k_off) {
-      issue_kmajor(L::S_COL, sdesc_add(k_kmaj, k_off), sdesc_add(q_kmaj0, (g % NQ) * L::QSTRIDE));
+    auto issue_s = [&](int g) {
+      issue_kmajor(L::S_COL, k_kmaj, sdesc_add(q_kmaj0, (g % NQ) * L::QSTRIDE));
       add_bias(L::S_COL, ones_l, g % NQ);
       umma_commit(s_full);
     };
@@ -478,26 +459,22 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
                          (acc || r > 0) ? 1u : 0u);
     };
     auto issue_dk = [&](int g, bool acc) {  // dK += dS^T Q
-      const uint32_t ds_kmaj = sdesc_add(ds_kmaj0, (g % NB) * L::DS_BYTES);
       const uint32_t q_mn = sdesc_add(q_mn0, (g % NQ) * L::QSTRIDE);
 #pragma unroll
       for (int r = 0; r < QN / 64; ++r)
         umma_ss4<2, 128>(tmem + L::DK_COL, sdesc_add(ds_kmaj, r * L::KREGION), sdesc_add(q_mn, r * 8192), idesc_tn,
                          (acc || r > 0) ? 1u : 0u);
     };
-    auto issue_dq = [&](int g, uint32_t k_off) {
-      const uint32_t k_mn0 = sdesc_add(k_mn, k_off);
-      const uint32_t ds_mn = sdesc_add(ds_mn0, (g % NB) * L::DS_BYTES);
+    auto issue_dq = [&]() {
 #pragma unroll
       for (int r = 0; r < kTileRows / 64; ++r)
-        umma_ss4<128, 128>(tmem + L::DQ_COL, sdesc_add(L::DQT ? k_mn0 : ds_mn, r * 8192),
-                           sdesc_add(L::DQT ? ds_mn : k_mn0, r * 8192), idesc_dq, r > 0 ? 1u : 0u);
+        umma_ss4<128, 128>(tmem + L::DQ_COL, sdesc_add(L::DQT ? k_mn : ds_mn, r * 8192),
+                           sdesc_add(L::DQT ? ds_mn : k_mn, r * 8192), idesc_dq, r > 0 ? 1u : 0u);
     };
     bool ok = true;
     int g = 0, sw = 0;  // steps and sweeps so far
     while (ok && next_sweep()) {
-      const uint32_t k_off = (sw % NK) * L::KTILE;  // this sweep's K
-      if (!(ok = warp_wait(&k_full[sw % NK], (sw / NK) & 1, ctl))) break;
+      if (!(ok = warp_wait(k_full, sw & 1, ctl))) break;
       // the last sweep's dK and dV are out of tensor memory
       auto wait_dkv = [&]() { return sw == 0 || warp_wait(dkv_free, (sw - 1) & 1, ctl); };
       if (role_a) {
@@ -526,7 +503,7 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
             if (!(ok = warp_wait(&q_full[g % NQ], (g / NQ) & 1, ctl))) break;
             if (g > 0 && !(ok = warp_wait(s_free, (g - 1) & 1, ctl))) break;
             tc_fence_after();
-            issue_s(g++, k_off);
+            issue_s(g++);
           }
           if (j >= 0) {
             const int x = L::PAIRED || !more ? g - 1 : g - 2;  // the step in work
@@ -540,7 +517,7 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
           if constexpr (L::PAIRED) {
             if (!(ok = warp_wait(&q_full[g % NQ], (g / NQ) & 1, ctl))) break;
             tc_fence_after();
-            issue_s(g++, k_off);
+            issue_s(g++);
           } else {
             if (j < 0 && !(ok = warp_wait(v_full, sw & 1, ctl))) break;
             if (!(ok = next_dp(g - 1))) break;
@@ -550,12 +527,12 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
       } else {
         for (int j = 0; j < w.n_q; ++j, ++g) {
           // dS is in shared memory (and so dP in registers)
-          if (!(ok = warp_wait(&p_ready[g % NB], (g / NB) & 1, ctl))) break;
+          if (!(ok = warp_wait(p_ready, g & 1, ctl))) break;
           // dQ first, so the drain starts while dK runs
           if constexpr (!L::PAIRED)
             if (g > 0 && !(ok = warp_wait(dq_free, (g - 1) & 1, ctl))) break;
           tc_fence_after();
-          issue_dq(g, k_off);
+          issue_dq();
           umma_commit(dq_full);
           if (j == 0) {
             if (!(ok = wait_dkv())) break;
@@ -563,36 +540,32 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
           }
           issue_dk(g, j > 0);
           umma_commit(&q_empty[g % NQ]);
-          umma_commit(&ds_free[g % NB]);
+          umma_commit(ds_free);
         }
       }
       if (!ok) break;
       umma_commit(dkv_full);  // one arrival per issuing warp
-      umma_commit(&k_empty[sw % NK]);
+      umma_commit(k_empty);
       ++sw;
     }
   } else {
     // ------------------------------------------------------------ ragged K and V tiles
-    int v_raws = 0, sw = 0;
-    uint32_t k_raws = 0;
+    int raws = 0;
     bool ok = true;
-    for (; ok && next_sweep(); ++sw) {
+    while (ok && next_sweep()) {
       if (!w.ragged(p.S)) continue;
-      const int kb = sw % NK;
       const int limit = w.len - w.kt * kTileRows;
       for (int m = 0; ok && m < 2; ++m) {  // in the order of the loads
-        const bool is_k = (m == 0) == (NK > 1);
-        if (!(ok = is_k ? warp_wait(&k_raw[kb], (k_raws >> kb) & 1, ctl) : warp_wait(v_raw, v_raws & 1, ctl))) break;
-        uint8_t* tile = is_k ? sK + kb * L::KTILE : sV;
+        if (!(ok = warp_wait(m == 0 ? v_raw : k_raw, raws & 1, ctl))) break;
+        uint8_t* tile = m == 0 ? sV : sK;
         for (int i = limit * 8 + lane; i < kTileRows * 8; i += 32)
           for (int r = 0; r < L::REG; ++r)
             *reinterpret_cast<uint4*>(tile + r * L::KREGION + i * 16) = make_uint4(0u, 0u, 0u, 0u);
         fence_proxy_async_smem();  // the tensor core reads the tile next
         __syncwarp();
-        if (lane == 0) mbar_arrive(is_k ? &k_full[kb] : v_full);
+        if (lane == 0) mbar_arrive(m == 0 ? v_full : k_full);
       }
-      k_raws ^= 1u << kb;
-      ++v_raws;
+      ++raws;
     }
   }
   } else if (warp < 8) {
@@ -685,8 +658,7 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
         tmem_ld32(dp_addr, r);
       }
       // the wait for the dS^T buffer passes while dP^T loads
-      const int buf = g % NB;
-      if (g >= NB && !(ok = warp_wait(&ds_free[buf], ((g / NB) - 1) & 1, ctl))) break;
+      if (g > 0 && !(ok = warp_wait(ds_free, (g - 1) & 1, ctl))) break;
       uint32_t dk[CW / 2];
 #pragma unroll
       for (int h = 0; h < CW / 32; ++h) {
@@ -715,7 +687,7 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
         }
       }
       // dS^T row segment -> shared memory (swizzled like a TMA 128-byte tile)
-      uint8_t* ds_row = sDS + buf * L::DS_BYTES + ds_off;
+      uint8_t* ds_row = sDS + ds_off;
 #pragma unroll
       for (int q = 0; q < CW / 8; ++q)
         *reinterpret_cast<uint4*>(ds_row + (((chunk0 + q) ^ sw) << 4)) =
@@ -723,7 +695,7 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
       fence_proxy_async_smem();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(&p_ready[buf]);
+      if (lane == 0) mbar_arrive(p_ready);
     }
     }
   } else {
@@ -777,10 +749,8 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
         if (lane == 0) {
           uint8_t* stg = smem + L::OFF_STG + L::BOXES * wq * L::BOX_BYTES;
           mbar_arrive_expect_tx(&acc_full[wq], 2 * L::BOX_BYTES);
-          for (int c = 1; c >= 0; --c) {
-            if (c == 0) bulk_wait_read<0>();  // the rows of the step before have left it
+          for (int c = 0; c < 2; ++c)
             tma_load_3d(stg + c * L::BOX_BYTES, &tm_dq, &acc_full[wq], 32 * c, (w.q0 + j) * QN + 32 * wq, w.bh);
-          }
         }
         ++loads;
       };
@@ -858,7 +828,10 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
           const int row = q0 + wq * 32;
           // bf16 rows of 128 bytes, 16-byte chunk k of row i at k ^ (i & 7); the map clips
           // rows past the caller's
-          auto store_rows = [&](const uint32_t (&r)[2][32], uint8_t* stg) {
+          auto store_rows = [&](const uint32_t (&r)[2][32]) {
+            uint8_t* stg = smem + L::OFF_OUT + wq * L::BOX_BYTES;
+            if (lane == 0) bulk_wait_read<0>();  // the TMA unit has read the box
+            __syncwarp();
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
               uint32_t v[4];
@@ -896,15 +869,12 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
                 r[c][4 * i + 2] = __float_as_uint(__uint_as_float(r[c][4 * i + 2]) + x.z);
                 r[c][4 * i + 3] = __float_as_uint(__uint_as_float(r[c][4 * i + 3]) + x.w);
               }
-            store_rows(r, smem + L::OFF_STG + L::BOXES * wq * L::BOX_BYTES);
-            box = 1;  // (the first one is being read)
-            if (j + 1 < w.n_q) load_acc(j + 1);
-          } else if (whole) {
-            uint8_t* stg = smem + L::OFF_STG + (L::BOXES * wq + box) * L::BOX_BYTES;
-            box ^= 1;
-            if (lane == 0) bulk_wait_read<1>();  // the TMA unit has read this box
+            fence_proxy_async_smem();  // the boxes are read before the next copy into them
             __syncwarp();
-            store_rows(r, stg);
+            if (j + 1 < w.n_q) load_acc(j + 1);
+          }
+          if (finish || whole) {
+            store_rows(r);
           } else {
 #pragma unroll
             for (int c = 0; c < 2; ++c) put_rows(&tm_dq, r[c], 32 * c, row, add);
