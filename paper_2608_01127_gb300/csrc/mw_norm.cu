@@ -648,7 +648,7 @@ Shape shape_of(int C, bool vec, bool few) {
   Shape best{0, 0, 0};
   for (int W = 1; W <= max_w; ++W) {
     const int V = form((C + elems * W - 1) / (elems * W), vec);
-    if (V > max_v) continue;
+    if (V > max_v || 32 * W > max_threads(vec ? 8 : 1, V)) continue;
     if (best.W == 0 || (W * V < best.W * best.V && (few || !vec))) best = {W, V, 0};
   }
   best.threads = 32 * best.W * (best.W < 8 ? 8 / best.W : 1);

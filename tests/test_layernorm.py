@@ -150,6 +150,14 @@ def test_sizes(mw, R, C):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("C", [2047, 2049, 2305, 3001, 4095, 4097, 6143, 8191])
+@pytest.mark.parametrize("R", [3, 1300])
+def test_wide_rows_of_odd_width(mw, R, C):
+    run(mw, R, C)
+    run(mw, R, C, x_dtype=F32, y_dtype=F32)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("types", [(BF16, BF16), (F32, BF16), (F32, F32)])
 @pytest.mark.parametrize("p_dtype", [F32, BF16])
 @pytest.mark.parametrize("C", [768, 771, 2560, 8192, 7001])
@@ -192,6 +200,38 @@ def test_shapes_and_no_rows(mw):
     y, mean, rstd = mw.mw_layernorm_fwd(e, w[0].contiguous(), w[0].contiguous())
     dx, dw, db = mw.mw_layernorm_bwd(e, e, mean, rstd, w[0].contiguous(), w[0].contiguous())
     assert y.shape == dx.shape == (0, 64) and torch.count_nonzero(dw) == 0 and torch.count_nonzero(db) == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("C", [2056, 2049])
+def test_arrays_past_32_bits(mw, C):
+    """More than 2^31 elements, rows in pieces of 16 bytes and single elements: the last rows,
+    and the parameters' gradients over all of them.  An element is rounded to bf16 once
+    (2^-8 of itself; dx is a difference of terms up to 4 times its size in fp32); the sums
+    over a million rows by sqrt(R / blocks) 2^-24 of sqrt(R) terms: far below 1e-4."""
+    R = (1 << 20) + 3
+    x, dy = (torch.empty(R, C, dtype=BF16, device="cuda") for _ in range(2))
+    assert x.numel() > 1 << 31
+    for i, t in enumerate((x, dy)):
+        t.normal_(generator=torch.Generator("cuda").manual_seed(40 + i))
+    w, b = rnd(42, C).cuda(), rnd(43, C).cuda()
+    y, mean, rstd = mw.mw_layernorm_fwd(x, w, b)
+    dx, dw, db = mw.mw_layernorm_bwd(dy, x, mean, rstd, w, b)
+    ref_w, ref_b = (torch.zeros(C, dtype=torch.float64, device="cuda") for _ in range(2))
+    for i in range(0, R, 1 << 16):
+        v, g = x[i:i + (1 << 16)].double(), dy[i:i + (1 << 16)].double()
+        var, mu = torch.var_mean(v, -1, correction=0, keepdim=True)
+        xh = (v - mu) / (var + 1e-5).sqrt()
+        ref_w += (g * xh).sum(0)
+        ref_b += g.sum(0)
+    gw = g * w.double()
+    last = (gw - gw.mean(-1, keepdim=True) - xh * (gw * xh).mean(-1, keepdim=True)) / (var + 1e-5).sqrt()
+    want = xh * w.double() + b.double()
+    n = xh.shape[0]
+    assert float(((y[-n:].double() - want).abs() - 2.0 ** -8 * want.abs()).max()) <= 1e-4
+    assert float(((dx[-n:].double() - last).abs() - 2.0 ** -8 * last.abs()).max()) <= 1e-4
+    for got, ref in ((dw, ref_w), (db, ref_b)):
+        assert float((got.double() - ref).norm()) <= 1e-4 * float(ref.norm())
 
 
 @pytest.mark.gpu

@@ -301,6 +301,83 @@ def test_lse_is_of_the_weights_before_their_rounding(mw, M, S, d):
     assert float(err.max()) <= 2e-5
 
 
+def reference(q, k, v, do, scale):
+    """(O, LSE, dQ, dK, dV) of one head in 64 bits, on the inputs' device."""
+    q, k, v, do = (t.double() for t in (q, k, v, do))
+    s = q @ k.T * scale
+    lse = torch.logsumexp(s, -1)
+    p = (s - lse[:, None]).exp()
+    o = p @ v
+    ds = p * (do @ v.T - (do * o).sum(-1, keepdim=True))
+    return o, lse, scale * ds @ k, scale * ds.T @ q, p.T @ do
+
+
+def near(got, ref, tol):
+    return float((got.double() - ref).norm()) <= tol * float(ref.norm())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M,S", [(4000, 200), (8000, 300)])
+def test_many_rows_and_few_states(mw, M, S):
+    """d = 64, enough tiles of rows that the backward takes them through two and three key
+    tiles a run at a time: dK and dV in accumulators."""
+    B, H, d = 4, 12, 64
+    lens = [S, 130, 0, 7]
+    q, k, v, do = (bf(30 + i, B, H, n, d).cuda() for i, n in enumerate((M, S, S, M)))
+    kv_len = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    padded = [-(-n // 128) * 128 for n in (M, S)]
+    assert mw.mw_xattn_bwd_workspace_size(B, H, H, M, S, d) >= B * H * (padded[0] + 2 * padded[1]) * d * 4
+    o, lse = mw.mw_xattn_fwd(q, k, v, kv_len)
+    dq, dk, dv = mw.mw_xattn_bwd(q, k, v, o, lse, do, kv_len)
+    for b, n in enumerate(lens):
+        if n == 0:
+            for t in (o, dq, dk, dv):
+                assert torch.count_nonzero(t[b]) == 0
+            continue
+        assert torch.count_nonzero(dk[b, :, n:]) == 0 and torch.count_nonzero(dv[b, :, n:]) == 0
+        for h in (0, 5, 11):
+            ref = reference(q[b, h], k[b, h, :n], v[b, h, :n], do[b, h], 0.125)
+            assert near(o[b, h], ref[0], 5e-3)
+            assert float((lse[b, h].double() - ref[1]).abs().max()) <= 1e-3
+            for got, r in ((dq[b, h], ref[2]), (dk[b, h, :n], ref[3]), (dv[b, h, :n], ref[4])):
+                assert near(got, r, 1e-2), (b, h)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M", [1, 40])
+def test_states_past_32_bits(mw, M):
+    """K and V of more than 2^31 elements: the last head's."""
+    B, H, S, d = 1, 17, (1 << 20) + 5, 128
+    k, v = (torch.empty(B, H, S, d, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    assert k.numel() > 1 << 31
+    for t in (k, v):
+        t.normal_(generator=torch.Generator("cuda").manual_seed(4))
+    q = bf(5, B, H, M, d).cuda()
+    o, lse = mw.mw_xattn_fwd(q, k, v)
+    ref = reference(q[0, -1], k[0, -1], v[0, -1], q[0, -1], d ** -0.5)
+    # (a mean of a million states: its own size is 2^-8 of theirs)
+    assert near(o[0, -1], ref[0], 1e-2)
+    assert float((lse[0, -1].double() - ref[1]).abs().max()) <= 2e-5 * float(ref[1].abs().max())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("S", [100, 130])
+def test_rows_past_32_bits(mw, S):
+    """Q, O and their gradients of more than 2^31 elements."""
+    B, H, M, d = 1, 16, (1 << 20) + 77, 128
+    q, do = (torch.empty(B, H, M, d, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    assert q.numel() > 1 << 31
+    for i, t in enumerate((q, do)):
+        t.normal_(generator=torch.Generator("cuda").manual_seed(6 + i))
+    k, v = bf(8, B, H, S, d).cuda(), bf(9, B, H, S, d).cuda()
+    o, lse = mw.mw_xattn_fwd(q, k, v)
+    dq, dk, dv = mw.mw_xattn_bwd(q, k, v, o, lse, do)
+    ref = reference(q[0, -1], k[0, -1], v[0, -1], do[0, -1], d ** -0.5)
+    for got, r, tol in zip((o, dq, dk, dv), (ref[0],) + ref[2:], (5e-3, 1e-2, 1e-2, 1e-2)):
+        assert near(got[0, -1], r, tol)
+    assert float((lse[0, -1].double() - ref[1]).abs().max()) <= 1e-3
+
+
 @pytest.mark.gpu
 def test_autograd_and_shared_heads(mw):
     """The gradients of shared heads are the sums over the query heads that share
