@@ -64,12 +64,12 @@ size_t xattn_ws(const XattnSizes& z, int S, int d) {
 // The order of the backward's work, from a model of the time (us): steps of t and a
 // sweep's start and end; key-major also two passes and a quarter over dQ in HBM (zeroed,
 // read, bf16 written; written once in bf16 query-major).  Query-major a run ends after
-// few tiles, and its dQ waits for copies: a step costs more, and the first ones 6 us.  Heads x query tiles x key
-// tiles, us of all kernels, query-/key-major: d = 64 48 x 110 x 2 186 / 216, 152 x 40 x 2
-// 213 / 218, 100 x 24 x 5 202 / 190, 16 x 110 x 9 231 / 186, 64 x 3 x 2 28 / 20; d = 128,
-// where dQ could not leave with the last sweep (no shared memory for it): 48 x 110 x 2
-// 420 / 420, 152 x 40 x 2 522 / 424, 16 x 110 x 9 395 / 305, so that it is key-major from
-// two key tiles on.
+// few tiles, and its dQ is read back: a step costs more, and the first ones 6 us.  Heads x
+// query tiles x key tiles at d = 64, us of all kernels, query-/key-major: 48 x 110 x 2 181 /
+// 223, 152 x 40 x 2 204 / 231, 100 x 24 x 5 195 / 183, 16 x 110 x 9 220 / 177, 64 x 3 x 2 28 /
+// 21.  d = 128, where dQ cannot leave with the last sweep (no shared memory for it), was
+// slower query-major (152 x 40 x 2 522 / 424, 16 x 110 x 9 395 / 305, 48 x 110 x 2 420 each):
+// key-major from two key tiles on.
 struct XattnBwdPlan {
   bool key_major = false;
   int ranges = 1;  // key-major: of a head's query tiles
@@ -78,7 +78,7 @@ struct XattnBwdPlan {
 
 XattnBwdPlan xattn_bwd_plan(int BH, int q_tiles, int k_tiles, int D) {
   XattnBwdPlan best;
-  best.run = 16;  // 48 x 110 x 2: runs of 4 227, of 8 201, of 16 186 us
+  best.run = 16;  // 48 x 110 x 2: runs of 4 227, of 8 201, of 16 186, of 20 182 us
   if (k_tiles == 1) return best;
   const double t = D == 64 ? 1.55 : 2.25, sweep = D == 64 ? 1.0 : 2.0;
   const double acc = 4e-6 * BH * static_cast<double>(q_tiles) * kTileRows * D / 6.5;  // us a pass
