@@ -72,7 +72,8 @@ size_t xattn_ws(const XattnSizes& z, int S, int d) {
 // key-major from two key tiles on.
 struct XattnBwdPlan {
   bool key_major = false;
-  int ranges = 1;  // key-major: of a head's query tiles
+  int ranges = 1;  // key-major: of a head's query tiles (more than one: the number is worked
+                   // out again on the device, for the states that the samples have)
   int run = 1;     // query-major: query tiles of a run, so that the dQ of all runs in work stays in L2
 };
 
@@ -80,18 +81,20 @@ XattnBwdPlan xattn_bwd_plan(int BH, int q_tiles, int k_tiles, int D) {
   XattnBwdPlan best;
   best.run = 16;  // 48 x 110 x 2: runs of 4 227, of 8 201, of 16 186, of 20 182 us
   if (k_tiles == 1) return best;
-  const double t = D == 64 ? 1.55 : 2.25, sweep = D == 64 ? 1.0 : 2.0;
   const double acc = 4e-6 * BH * static_cast<double>(q_tiles) * kTileRows * D / 6.5;  // us a pass
   double best_cost = D == 64 ? ceil_div(static_cast<long long>(BH) * q_tiles, kNormSms) * k_tiles * 2.05 + 6 : INFINITY;
-  for (int r = 1; r <= q_tiles && r <= 64; ++r) {
-    const double cost = ceil_div(static_cast<long long>(BH) * r * k_tiles, kNormSms) * (ceil_div(q_tiles, r) * t + sweep) +
-                        2.25 * acc;
-    if (cost < best_cost) {
-      best_cost = cost;
+  const double acc_kv = 8e-6 * BH * static_cast<double>(k_tiles) * kTileRows * D / 6.5;  // of dK's and dV's
+  auto cost = [&](int r) {
+    return ceil_div(static_cast<long long>(BH) * r * k_tiles, kNormSms) * (ceil_div(q_tiles, r) * xattn_step_us(D) + xattn_sweep_us(D)) +
+           2.25 * (acc + (r > 1 ? acc_kv : 0));
+  };
+  const int most = q_tiles < kXattnMaxRanges ? q_tiles : kXattnMaxRanges;
+  for (int r = 1; r <= most; ++r)
+    if (cost(r) < best_cost) {
+      best_cost = cost(r);
       best.key_major = true;
       best.ranges = r;
     }
-  }
   return best;
 }
 
@@ -335,10 +338,6 @@ mw_status mw_xattn_bwd(const void* q, const void* k, const void* v, const int* k
   p.k_tiles = ws.S_pad / kTileRows;
   p.key_major = ws.plan.key_major;
   p.run = ws.plan.run;
-  p.ranges = ws.plan.ranges;
-  p.range_tiles = p.q_tiles / p.ranges;
-  p.range_rest = p.q_tiles % p.ranges;
-  p.pieces = p.key_major ? z.BH * p.ranges * p.k_tiles : 0;
   p.dkv_whole = ws.dkv_whole;
   p.zero_dq = p.key_major;
   p.wide_dkv = wide_rows(dk, d) && wide_rows(dv, d);

@@ -265,6 +265,10 @@ cudaError_t launch_xattn_few(int d, const CUtensorMap& tk, const CUtensorMap& tv
 
 // Backward on tensor cores (mw_xattn_bwd.cu).
 constexpr int kXattnMaxCtas = 1023;
+constexpr int kXattnMaxRanges = 64;
+// Key-major, us: a step, and what a sweep's start and end add (24 x 40, 12 x 8 tiles).
+constexpr float xattn_step_us(int D) { return D == 64 ? 1.55f : 2.25f; }
+constexpr float xattn_sweep_us(int D) { return D == 64 ? 1.f : 2.f; }
 struct XattnBwdParams {
   const int* kv_len;
   const __nv_bfloat16* o;
@@ -278,17 +282,15 @@ struct XattnBwdParams {
   int q_tiles, k_tiles;  // of a head's rows; of S states
   bool key_major;      // a piece of work is one key tile, else a run of query tiles
   int run;             // query-major: query tiles of a run at most
-  int ranges;          // key-major: ranges of a head's query tiles,
-  int range_tiles, range_rest;  // of range_tiles each, one more in the first range_rest
-  int pieces;          // key-major: BH * ranges * k_tiles
-  bool dkv_whole;      // one sweep makes all of a key tile's dK and dV
+  bool dkv_whole;      // key-major: one sweep makes all of a key tile's dK and dV
   bool zero_dq;        // dq_acc is only added to
   bool wide_dkv;  // every row of dK and dV starts at a multiple of 32 bytes
   float scale, scale_log2;
   float* lse2;         // [BH, M_pad] (d = 64: unused, as delta)
   float* delta;        // [BH, M_pad]
   float* bias;         // [BH, M_pad, 8] (d = 64)
-  int2* shares;        // query-major: where each CTA's share begins, and the end (sample, unit)
+  int2* shares;        // query-major: where each CTA's share begins, and the end (sample, unit);
+                       // key-major: [0].x ranges of a head's query tiles
   float* dq_acc;       // [BH, M_pad, D]
   float* dkv_acc;      // [2, BH, S_pad, D] unless dkv_whole: dK, then dV
   long long dkv_float4s;  // its size

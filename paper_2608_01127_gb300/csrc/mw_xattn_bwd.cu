@@ -135,9 +135,12 @@ struct Plan {
   // query-major: the CTA's share of all units (query tiles of a sample's heads) goes
   // from unit `unit` of sample `sample` up to unit `last` of sample `last_sample`
   int sample = 0, unit = 0, last_sample = 0, last = 0;
-  int next;          // key-major: index of the next (head, range, key tile)
+  int next;          // key-major: index of the next (head, range, key tile), and those
+  int before = 0;    // of the samples before `sample`
+  int ranges;        // of a head's query tiles
   __device__ explicit Plan(const XattnBwdParams& p_) : p(p_), next(blockIdx.x) {
     w.kt = 0;
+    ranges = p.shares[0].x;
     if (p.key_major) return;
     const int2 a = p.shares[blockIdx.x], b = p.shares[blockIdx.x + 1];
     sample = a.x, unit = a.y, last_sample = b.x, last = b.y;
@@ -162,22 +165,31 @@ struct Plan {
       return true;
     }
   }
+  // (pieces of key tiles that a sample does not have are not counted, so that the CTAs'
+  // numbers of pieces differ by one at most: 8 x 12 heads of 3520 rows of 64, 256 to 1024
+  // states, 285 -> 230 us for all kernels)
   __device__ __forceinline__ bool key_piece() {
-    while (next < p.pieces) {
-      int x = next;
-      next += gridDim.x;
-      w.kt = x % p.k_tiles;
-      x /= p.k_tiles;
-      w.bh = x / p.ranges;
-      const int r = x - w.bh * p.ranges;
-      w.q0 = r * p.range_tiles + min(r, p.range_rest);
-      w.n_q = p.range_tiles + (r < p.range_rest);
-      w.len = valid_states(p, w.bh / p.heads);
-      w.n_kt = (w.len + kTileRows - 1) / kTileRows;
-      k_end = w.kt + 1;
-      if (w.kt < w.n_kt) return true;
+    int x = next;
+    next += gridDim.x;
+    for (; sample < p.samples; ++sample) {
+      w.n_kt = key_tiles(p, sample);
+      const int count = p.heads * ranges * w.n_kt;
+      if (x - before < count) break;
+      before += count;
     }
-    return false;
+    if (sample == p.samples) return false;
+    x -= before;
+    const int h = x / w.n_kt;
+    w.kt = x - h * w.n_kt;
+    w.bh = h / ranges;
+    const int r = h - w.bh * ranges;
+    w.bh += sample * p.heads;
+    const int tiles = p.q_tiles / ranges, rest = p.q_tiles - tiles * ranges;
+    w.q0 = r * tiles + min(r, rest);  // (the first ones have one more)
+    w.n_q = tiles + (r < rest);
+    w.len = valid_states(p, sample);
+    k_end = w.kt + 1;
+    return true;
   }
   __device__ __forceinline__ bool step() { return ++w.kt < k_end || (p.key_major ? key_piece() : query_piece()); }
 };
@@ -936,7 +948,7 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
 // Also zeroes what is only added to, and the gradients that no sweep writes: dQ of
 // samples without states here; in the blocks after the rows' the accumulators of dK
 // and dV or, where each key tile's one sweep writes them whole, their rows past a
-// sample's key tiles.  The last block divides the work (query-major).
+// sample's key tiles.  The last block divides the work.
 constexpr int kPreRows = 4;
 template <int D>
 __global__ void __launch_bounds__(256) xattn_pre_kernel(const XattnBwdParams p, long long row_blocks, int ctas) {
@@ -944,7 +956,28 @@ __global__ void __launch_bounds__(256) xattn_pre_kernel(const XattnBwdParams p, 
   constexpr int kGroups = 256 / G;
   const int d_io = (D == 64) ? D : p.d;
   if (blockIdx.x == gridDim.x - 1) {
-    if (p.key_major) return;
+    if (p.key_major) {
+      // the ranges that take the least rounds of the CTAs through the samples' key tiles
+      // (2 x 4 heads of 22000 rows of 128, 1500 and 600 states: those for 1500 each 300 us
+      // for all kernels, these 239)
+      __shared__ float us[kXattnMaxRanges];
+      const int r = threadIdx.x + 1;
+      if (r <= kXattnMaxRanges) {
+        long long pieces = 0;
+        for (int b = 0; b < p.samples; ++b) pieces += static_cast<long long>(p.heads) * r * key_tiles(p, b);
+        us[r - 1] = static_cast<float>((pieces + ctas - 1) / ctas) *
+                    (static_cast<float>((p.q_tiles + r - 1) / r) * xattn_step_us(D) + xattn_sweep_us(D));
+      }
+      __syncthreads();
+      if (threadIdx.x == 0) {
+        int best = 1;
+        if (!p.dkv_whole)
+          for (int k = 2; k <= min(p.q_tiles, kXattnMaxRanges); ++k)
+            if (us[k - 1] < us[best - 1]) best = k;
+        p.shares[0] = make_int2(best, 0);
+      }
+      return;
+    }
     // share c begins where c / ctas of all steps are done: units of a sample count as its
     // key tiles
     long long total = 0;
@@ -1096,7 +1129,9 @@ cudaError_t launch(const XattnBwdMaps& m, const XattnBwdParams& p, int dev, int 
     return cudaFuncSetAttribute(xattn_bwd_kernel<D, DM>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::BYTES);
   });
   if (e != cudaSuccess) return e;
-  const long long work = p.key_major ? p.pieces : static_cast<long long>(p.BH) * p.q_tiles;
+  const long long work = !p.key_major  ? static_cast<long long>(p.BH) * p.q_tiles
+                         : p.dkv_whole ? static_cast<long long>(p.BH) * p.k_tiles
+                                       : sms;
   const unsigned grid = static_cast<unsigned>(work < sms ? work : sms);
   constexpr int kBlockRows = kPreRows * 256 / (D / 8);
   const long long row_blocks = (static_cast<long long>(p.BH) * p.M_pad + kBlockRows - 1) / kBlockRows;

@@ -344,6 +344,32 @@ def test_many_rows_and_few_states(mw, M, S):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 72, 128])
+@pytest.mark.parametrize("M,lens", [(900, [700, 1, 300, 0]), (2500, [0, 640, 0, 129]), (1100, [0, 0, 0, 5]),
+                                    (600, [0, 0, 0, 0])])
+def test_ragged_lengths_over_many_tiles(mw, d, M, lens):
+    """The backward divides key tiles that are there among the SMs, in ranges of rows."""
+    B, H, Hkv, S = 4, 4, 2, 700
+    q, k, v, do = (bf(50 + i, B, h, n, d).cuda() for i, (h, n) in enumerate(((H, M), (Hkv, S), (Hkv, S), (H, M))))
+    kv_len = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    o, lse = mw.mw_xattn_fwd(q, k, v, kv_len)
+    dq, dk, dv = mw.mw_xattn_bwd(q, k, v, o, lse, do, kv_len)
+    for b, n in enumerate(lens):
+        if n == 0:
+            for t in (o, dq, dk, dv):
+                assert torch.count_nonzero(t[b]) == 0
+            continue
+        assert torch.count_nonzero(dk[b, :, n:]) == 0 and torch.count_nonzero(dv[b, :, n:]) == 0
+        for h in range(Hkv):
+            rows = lambda t: t[b, 2 * h:2 * h + 2].reshape(2 * M, d)  # noqa: E731
+            ref = reference(rows(q), k[b, h, :n], v[b, h, :n], rows(do), d ** -0.5)
+            assert near(rows(o), ref[0], 5e-3)
+            assert near(dv[b, h, :n], ref[4], 1e-2)
+            if n > 1:  # (one state: dS = 0)
+                assert near(rows(dq), ref[2], 1e-2) and near(dk[b, h, :n], ref[3], 1e-2)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("M", [1, 40])
 def test_states_past_32_bits(mw, M):
     """K and V of more than 2^31 elements: the last head's."""
