@@ -341,7 +341,7 @@ mw_status mw_xattn_fwd(const void* q, const void* k, const void* v, const int* k
  * those of K and V summed over the query heads that share them, and 0 in the
  * places past kv_len.  o and lse are the forward's: D carries the rounding of o to
  * bf16, whose share of dQ is proportional to the row's mean key (dQ itself depends
- * on the keys' differences only).
+ * on the keys' differences only); of samples with 2 to 8 states D is summed again.
  */
 size_t mw_xattn_bwd_workspace_size(int B, int H, int Hkv, int M, int S, int d);
 mw_status mw_xattn_bwd(const void* q, const void* k, const void* v, const int* kv_len, const void* o,

@@ -319,6 +319,9 @@ mw_status mw_xattn_bwd(const void* q, const void* k, const void* v, const int* k
   XattnBwdParams p{};
   MW_TRY(status_ptr(scope.device(), &p.status));
   p.kv_len = kv_len;
+  p.q = static_cast<const __nv_bfloat16*>(q);
+  p.k = static_cast<const __nv_bfloat16*>(k);
+  p.v = static_cast<const __nv_bfloat16*>(v);
   p.o = static_cast<const __nv_bfloat16*>(o);
   p.dout = static_cast<const __nv_bfloat16*>(dout);
   p.lse = lse;

@@ -271,6 +271,9 @@ constexpr float xattn_step_us(int D) { return D == 64 ? 1.55f : 2.25f; }
 constexpr float xattn_sweep_us(int D) { return D == 64 ? 1.f : 2.f; }
 struct XattnBwdParams {
   const int* kv_len;
+  const __nv_bfloat16* q;
+  const __nv_bfloat16* k;
+  const __nv_bfloat16* v;
   const __nv_bfloat16* o;
   const __nv_bfloat16* dout;
   const float* lse;

@@ -949,9 +949,15 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
 // samples without states here; in the blocks after the rows' the accumulators of dK
 // and dV or, where each key tile's one sweep writes them whole, their rows past a
 // sample's key tiles.  The last block divides the work.
+// Of few states D is summed from P and dP again instead: P is near 0 or 1 there, dP - D a
+// small difference, and what O lost in bf16 was up to 1e-2 of dQ and dK (two states, q and k
+// twice the usual size; of 11700 calls of 2 and more states 6% were off by over 5e-3, all but
+// one with fewer than 16; with this one in 7500).  Five blocks an SM: 48 x 14080 rows of 64
+// 44 -> 41 us.
 constexpr int kPreRows = 4;
+constexpr int kFewStates = 8;
 template <int D>
-__global__ void __launch_bounds__(256) xattn_pre_kernel(const XattnBwdParams p, long long row_blocks, int ctas) {
+__global__ void __launch_bounds__(256, 5) xattn_pre_kernel(const XattnBwdParams p, long long row_blocks, int ctas) {
   constexpr int G = D / 8;
   constexpr int kGroups = 256 / G;
   const int d_io = (D == 64) ? D : p.d;
@@ -1025,23 +1031,23 @@ __global__ void __launch_bounds__(256) xattn_pre_kernel(const XattnBwdParams p, 
   const int bh = static_cast<int>(min(row0, rows - 1) / p.M_pad);
   const int i0 = static_cast<int>(row0 - static_cast<long long>(bh) * p.M_pad);
   const bool valid = row0 < rows;
-  const bool no_keys = p.kv_len && valid_states(p, bh / p.heads) == 0;
-  uint4 a[kPreRows], b[kPreRows];
+  const int keys = valid_states(p, bh / p.heads);
+  auto dot = [](const uint4& x, const uint4& y) {  // over the row's lanes
+    const uint32_t xv[4] = {x.x, x.y, x.z, x.w}, yv[4] = {y.x, y.y, y.z, y.w};
+    float sum = 0.f;
 #pragma unroll
-  for (int r = 0; r < kPreRows; ++r) {
-    a[r] = b[r] = make_uint4(0u, 0u, 0u, 0u);
-    if (valid && i0 + r < p.M && 8 * sub < d_io) {
-      const size_t off = (static_cast<size_t>(bh) * p.M + i0 + r) * d_io + 8 * sub;
-      if (no_keys) {
-        *reinterpret_cast<uint4*>(p.dq + off) = a[r];
-      } else {
-        a[r] = *reinterpret_cast<const uint4*>(p.o + off);
-        b[r] = *reinterpret_cast<const uint4*>(p.dout + off);
-      }
+    for (int k = 0; k < 4; ++k) {
+      sum = fmaf(__uint_as_float(xv[k] << 16), __uint_as_float(yv[k] << 16), sum);
+      sum = fmaf(__uint_as_float(xv[k] & 0xffff0000u), __uint_as_float(yv[k] & 0xffff0000u), sum);
     }
-  }
 #pragma unroll
-  for (int r = 0; r < kPreRows; ++r) {
+    for (int s = G / 2; s > 0; s >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, s);
+    return sum;
+  };
+  auto piece = [&](const __nv_bfloat16* base, size_t row) {
+    return 8 * sub < d_io ? *reinterpret_cast<const uint4*>(base + row * d_io + 8 * sub) : make_uint4(0u, 0u, 0u, 0u);
+  };
+  auto finish = [&](int r, float sum) {
     const long long gr = row0 + r;
     if (valid && p.zero_dq) {
       float4* acc = reinterpret_cast<float4*>(p.dq_acc + gr * D);
@@ -1049,15 +1055,6 @@ __global__ void __launch_bounds__(256) xattn_pre_kernel(const XattnBwdParams p, 
       for (int k = 0; k < 2; ++k)
         if (4 * (sub + k * G) < d_io) acc[sub + k * G] = make_float4(0.f, 0.f, 0.f, 0.f);
     }
-    const uint32_t av[4] = {a[r].x, a[r].y, a[r].z, a[r].w}, bv[4] = {b[r].x, b[r].y, b[r].z, b[r].w};
-    float sum = 0.f;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      sum = fmaf(__uint_as_float(av[k] << 16), __uint_as_float(bv[k] << 16), sum);
-      sum = fmaf(__uint_as_float(av[k] & 0xffff0000u), __uint_as_float(bv[k] & 0xffff0000u), sum);
-    }
-#pragma unroll
-    for (int s = G / 2; s > 0; s >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, s);
     if (valid && sub == 0) {
       const float lse = i0 + r < p.M ? p.lse[static_cast<size_t>(bh) * p.M + i0 + r] : INFINITY;
       if constexpr (D == 64) {
@@ -1072,7 +1069,40 @@ __global__ void __launch_bounds__(256) xattn_pre_kernel(const XattnBwdParams p, 
         p.lse2[gr] = lse * 1.4426950408889634f;
       }
     }
+  };
+  if (keys > 1 && keys <= kFewStates) {  // (of one state O is exact, V itself)
+#pragma unroll 1
+    for (int r = 0; r < kPreRows; ++r) {  // (a warp's lanes see the same sample)
+      const bool there = valid && i0 + r < p.M;
+      const size_t row = static_cast<size_t>(bh) * p.M + (there ? i0 + r : 0);
+      const uint4 q = piece(p.q, row), g = piece(p.dout, row);
+      const float lse2 = p.lse[row] * 1.4426950408889634f;
+      float sum = 0.f;
+#pragma unroll 1
+      for (int j = 0; j < keys; ++j) {
+        const size_t state = static_cast<size_t>(bh) * p.S + j;
+        sum = fmaf(ex2_approx(fmaf(dot(q, piece(p.k, state)), p.scale_log2, -lse2)), dot(g, piece(p.v, state)), sum);
+      }
+      finish(r, there ? sum : 0.f);
+    }
+    return;
   }
+  uint4 a[kPreRows], b[kPreRows];
+#pragma unroll
+  for (int r = 0; r < kPreRows; ++r) {
+    a[r] = b[r] = make_uint4(0u, 0u, 0u, 0u);
+    if (valid && i0 + r < p.M && 8 * sub < d_io) {
+      const size_t off = (static_cast<size_t>(bh) * p.M + i0 + r) * d_io + 8 * sub;
+      if (keys == 0) {
+        *reinterpret_cast<uint4*>(p.dq + off) = a[r];
+      } else {
+        a[r] = *reinterpret_cast<const uint4*>(p.o + off);
+        b[r] = *reinterpret_cast<const uint4*>(p.dout + off);
+      }
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < kPreRows; ++r) finish(r, dot(a[r], b[r]));
 }
 
 // bf16 rows from the accumulators: dQ of samples with several key tiles (the others'
