@@ -85,7 +85,8 @@ XattnBwdPlan xattn_bwd_plan(int BH, int q_tiles, int k_tiles, int D) {
   double best_cost = D == 64 ? ceil_div(static_cast<long long>(BH) * q_tiles, kNormSms) * k_tiles * 2.05 + 6 : INFINITY;
   const double acc_kv = 8e-6 * BH * static_cast<double>(k_tiles) * kTileRows * D / 6.5;  // of dK's and dV's
   auto cost = [&](int r) {
-    return ceil_div(static_cast<long long>(BH) * r * k_tiles, kNormSms) * (ceil_div(q_tiles, r) * xattn_step_us(D) + xattn_sweep_us(D)) +
+    return ceil_div(static_cast<long long>(BH) * r * k_tiles, kNormSms) *
+               (ceil_div(q_tiles, r) * xattn_step_us(D) + xattn_sweep_us(D)) +
            2.25 * (acc + (r > 1 ? acc_kv : 0));
   };
   const int most = q_tiles < kXattnMaxRanges ? q_tiles : kXattnMaxRanges;

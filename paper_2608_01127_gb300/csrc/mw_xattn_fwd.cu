@@ -725,8 +725,8 @@ cudaError_t launch(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorM
 
 }  // namespace
 
-cudaError_t launch_xattn_tc(int d, int dm, const CUtensorMap& tq, const CUtensorMap& tk,
-                            const CUtensorMap& tv, const CUtensorMap& to, const XattnTcParams& p, int dev, int sms, cudaStream_t s) {
+cudaError_t launch_xattn_tc(int d, int dm, const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv,
+                            const CUtensorMap& to, const XattnTcParams& p, int dev, int sms, cudaStream_t s) {
   if (d == 64) return launch<64, 64>(tq, tk, tv, to, p, dev, sms, s);
   if (dm == 80) return launch<128, 80>(tq, tk, tv, to, p, dev, sms, s);
   return launch<128, 128>(tq, tk, tv, to, p, dev, sms, s);
