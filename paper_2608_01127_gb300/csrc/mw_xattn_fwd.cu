@@ -16,8 +16,8 @@
 // not the exponentials (1024 cycles at 32 a clock) or the MMAs (1024; d = 128 2048 of
 // 3070).  Steps of 64 keys with two S in flight were slower (d = 64 1.16 -> 1.59 us, 128
 // 1.65 -> 1.88): half of the softmax is latency that does not shrink with the step.
-// Measured, 24 query and 40 key tiles a head: d = 64 1.21, 72 1.31, 128 1.59 us a step of
-// 256 rows x 128 keys (128: 1.6 PFLOP/s over the SMs); two key tiles 2.07, 2.70, 2.74.
+// Measured, 24 query and 40 key tiles a head: d = 64 1.17, 72 1.24, 128 1.58 us a step of
+// 256 rows x 128 keys (128: 1.6 PFLOP/s over the SMs); two key tiles 2.02, 2.62, 2.69.
 //
 // Roles (384 threads):
 //   warps 0-3 / 4-7  softmax of query tile 0 / 1 (one thread per row = TMEM lane)
@@ -506,13 +506,13 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
         if (!idle) {
           tc_fence_after();
           float s[128];
+          {
+            uint32_t r[4][32];
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            uint32_t r[32];
-            tmem_ld32(s_addr + 32 * c, r);
+            for (int c = 0; c < 4; ++c) tmem_ld32(s_addr + 32 * c, r[c]);
             tmem_wait_ld();
 #pragma unroll
-            for (int k = 0; k < 32; ++k) s[32 * c + k] = __uint_as_float(r[k]);
+            for (int c = 0; c < 128; ++c) s[c] = __uint_as_float(r[c >> 5][c & 31]);
           }
           const int limit = w.len - w.row0 - i * kTileRows;
           if (limit < kTileRows) {
@@ -563,8 +563,9 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
           const float m_eff = m_used == -INFINITY ? 0.f : m_used;
           const float2 sl2x2 = make_float2(sl2, sl2), negm = make_float2(-m_eff, -m_eff);
           float2 acc = make_float2(0.f, 0.f);
-          // P in four 32-key groups, each stored as soon as it is packed; the first
-          // two are announced while the third is stored
+          // P in halves of 64 keys, each stored as a whole; the first is announced while the
+          // second is computed
+          uint32_t held[16];
 #pragma unroll
           for (int g4 = 0; g4 < 4; ++g4) {
             uint32_t packed[16];
@@ -586,7 +587,15 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
                 tc_fence_after();
               }
             }
-            tmem_st16(lane_base + L::P_COL(t, g4 >> 1) + 16 * (g4 & 1), packed);
+            if (g4 & 1) {
+              uint32_t half[32];
+#pragma unroll
+              for (int k = 0; k < 16; ++k) half[k] = held[k], half[16 + k] = packed[k];
+              tmem_st32(lane_base + L::P_COL(t, g4 >> 1), half);
+            } else {
+#pragma unroll
+              for (int k = 0; k < 16; ++k) held[k] = packed[k];
+            }
           }
           if (!ok) break;
           l += acc.x + acc.y;
