@@ -646,13 +646,13 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
           if (!k_valid) pr[c] = 0.f;
       }
       // P^T (bf16 pairs) -> TMEM right away, so that dV starts while dS is computed
-      uint32_t r[32];  // 32 columns of dP^T
+      uint32_t r[CW / 32][32];  // dP^T
       if constexpr (!L::PAIRED) {
         // dP^T is issued after the last dV: once it is there, that has read P^T.
         // Its first half loads while P^T is stored.
         if (!(ok = warp_wait(dp_full, g & 1, ctl))) break;
         tc_fence_after();
-        tmem_ld32(dp_addr, r);
+        tmem_ld32(dp_addr, r[0]);
       }
       {
         uint32_t pe[CW / 2];
@@ -667,29 +667,30 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
       if constexpr (L::PAIRED) {
         if (!(ok = warp_wait(dp_full, g & 1, ctl))) break;
         tc_fence_after();
-        tmem_ld32(dp_addr, r);
+        tmem_ld32(dp_addr, r[0]);
       }
+#pragma unroll
+      for (int h = 1; h < CW / 32; ++h) tmem_ld32(dp_addr + 32 * h, r[h]);
       // the wait for the dS^T buffer passes while dP^T loads
       if (g > 0 && !(ok = warp_wait(ds_free, (g - 1) & 1, ctl))) break;
+      tmem_wait_ld();
+      if constexpr (!L::PAIRED) {
+        // dP^T is in registers: its columns can take the next step's
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(dp_free);
+      }
       uint32_t dk[CW / 2];
 #pragma unroll
       for (int h = 0; h < CW / 32; ++h) {
-        if (h > 0) tmem_ld32(dp_addr + 32 * h, r);
-        tmem_wait_ld();
-        if (!L::PAIRED && h == CW / 32 - 1) {
-          // dP^T is in registers: its columns can take the next step's
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(dp_free);
-        }
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
           // d = 64: the MMA already subtracted D
           const float4 dv = L::FOLD ? make_float4(0.f, 0.f, 0.f, 0.f)
                                     : reinterpret_cast<const float4*>(delta)[8 * h + k];
           const int c = 32 * h + 4 * k;
-          const float2 dp0 = make_float2(__uint_as_float(r[4 * k]), __uint_as_float(r[4 * k + 1]));
-          const float2 dp1 = make_float2(__uint_as_float(r[4 * k + 2]), __uint_as_float(r[4 * k + 3]));
+          const float2 dp0 = make_float2(__uint_as_float(r[h][4 * k]), __uint_as_float(r[h][4 * k + 1]));
+          const float2 dp1 = make_float2(__uint_as_float(r[h][4 * k + 2]), __uint_as_float(r[h][4 * k + 3]));
           const float2 t0 = L::FOLD ? dp0 : add2(dp0, make_float2(-dv.x, -dv.y));
           const float2 t1 = L::FOLD ? dp1 : add2(dp1, make_float2(-dv.z, -dv.w));
           const float2 s0 = mul2(make_float2(pr[c], pr[c + 1]), t0);
