@@ -325,7 +325,8 @@ mw_status mw_bca_cache_fwd_noalloc(const void* q, const void* k_new, const void*
  * h H/Hkv ... (h+1) H/Hkv - 1 share head h of K and V.  kv_len: device array of B
  * int32, the valid states of each sample (the first kv_len[b]; below 0 counts as
  * 0, above S as S), or NULL: all S.  What K and V hold in the other places does
- * not matter (NaN included).  A row that sees no state has O = 0, LSE = -inf.
+ * not matter (NaN included).  A row that sees no state, or only scores of -inf, has
+ * O = 0, LSE = -inf; one with a score of NaN or +inf has NaN in both.
  * lse (fp32 [B, H, M]) may be NULL; it is summed in fp32 from the weights before
  * their rounding to bf16.  M = 0 and S = 0 are valid.
  * workspace: mw_xattn_workspace_size() bytes, 256-byte aligned (NULL if 0).

@@ -925,13 +925,13 @@ __global__ void __launch_bounds__(256) combine_kernel(const float* __restrict__ 
         if (s < n) m = fmaxf(m, ls[s]);
     }
     // a split whose LSE is -inf saw no key of the row: its O part is skipped
-    // (never multiplied: it may hold anything)
+    // (never multiplied: it may hold anything); a NaN makes the row one
 #pragma unroll
     for (int k = 0; k < kChunk; ++k) {
       if (s0 + k >= n) break;
       const float w = ls[s0 + k] == -INFINITY ? 0.f : __expf(ls[s0 + k] - m);
       wsum += w;
-      if (w > 0.f) {
+      if (!(w == 0.f)) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           acc[4 * h] += w * x[k][h].x;
@@ -943,11 +943,11 @@ __global__ void __launch_bounds__(256) combine_kernel(const float* __restrict__ 
     }
   }
   if (row >= n_rows) return;
-  const float inv = wsum > 0.f ? 1.f / wsum : 0.f;
+  const float inv = wsum == 0.f ? 0.f : 1.f / wsum;
   *reinterpret_cast<uint4*>(o + static_cast<size_t>(row) * d_io + 8 * sub) =
       make_uint4(pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv),
                  pack_bf16x2(acc[4] * inv, acc[5] * inv), pack_bf16x2(acc[6] * inv, acc[7] * inv));
-  if (lse && sub == 0) lse[row] = wsum > 0.f ? m + __logf(wsum) : -INFINITY;
+  if (lse && sub == 0) lse[row] = wsum == 0.f ? -INFINITY : m + __logf(wsum);
 }
 
 template <int D, int DM, bool ROPE, bool SPLIT>

@@ -283,9 +283,10 @@ __global__ void __launch_bounds__(Layout<D, R>::THREADS)
       acc = fmaf(other->o[r][ch], a, acc);
     }
     const size_t at = static_cast<size_t>(bh) * p.M + r;
-    p.o[at * p.d + ch] = __float2bfloat16(sum > 0.f ? acc / sum : 0.f);
+    // (a NaN is a result, not a row without states)
+    p.o[at * p.d + ch] = __float2bfloat16(sum == 0.f ? 0.f : acc / sum);
     if (p.lse && ch == 0)
-      p.lse[at] = sum > 0.f ? (top + __log2f(exact)) * 0.69314718055994530942f : -INFINITY;
+      p.lse[at] = sum == 0.f ? -INFINITY : (top + __log2f(exact)) * 0.69314718055994530942f;
   }
   cluster.sync();  // shared memory stays until all have read it
 }

@@ -622,7 +622,7 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
           tc_fence_after();
           const int prow = pw.r0 + row_local;
           const bool pidle = prow - lane >= p.M;
-          const bool nonzero = pl > 0.f;
+          const bool nonzero = !(pl == 0.f);  // (a NaN is a result, not a row without states)
           const float inv_l = nonzero ? 1.f / pl : 0.f;
           const size_t at = static_cast<size_t>(pw.bh) * p.M + prow;
           constexpr int kChunks = (DM + 63) / 64;
