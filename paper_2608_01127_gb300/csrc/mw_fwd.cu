@@ -775,7 +775,7 @@ __global__ void __launch_bounds__(FwdLayout<D, DM>::THREADS, 1)
         l = __uint_as_float(r[0]);
       }
     }
-    const bool nonzero = have && l > 0.f;
+    const bool nonzero = have && !(l == 0.f);  // (a NaN is a result, not a row without keys)
     const float inv_l = nonzero ? 1.f / l : 0.f;
     const float m_eff = (m_used == -INFINITY) ? 0.f : m_used;
     const float lse = nonzero ? (m_eff + __log2f(l)) * 0.69314718055994530942f : -INFINITY;
