@@ -97,3 +97,32 @@ def test_scores_of_minus_infinity(mw, M, S, d):
     assert float((o[:, :1].double().cpu() - o_ref).norm()) <= 5e-3 * float(o_ref.norm())
     assert float((lse[:, :1].double().cpu() - lse_ref).abs().max()) <= 1e-4 * max(1.0, float(lse_ref.abs().max()))
     assert torch.count_nonzero(o[0, 1]) == 0 and bool((lse[0, 1] == -INF).all())
+
+
+@pytest.mark.parametrize("d", [64, 72, 128])
+@pytest.mark.parametrize("M,S,lens", [(40, 200, [130, 70]), (700, 700, [300, 650]), (9000, 300, [5, 290])])
+def test_a_gradient_of_one_row(mw, M, S, lens, d):
+    """A gradient with NaN in one row: it reaches that row's dQ and its heads' valid keys, and
+    nothing in padded places, other rows or other heads."""
+    B, H, Hkv = 2, 4, 2
+    q, k, v, do = (t.cuda() for t in (bf(4, B, H, M, d), bf(5, B, Hkv, S, d), bf(6, B, Hkv, S, d), bf(7, B, H, M, d)))
+    kv_len = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    o, lse = mw.mw_xattn_fwd(q, k, v, kv_len)
+    good = mw.mw_xattn_bwd(q, k, v, o, lse, do, kv_len)
+    bad = do.clone()
+    bad[1, 3, M // 2, 4] = math.nan
+    dq, dk, dv = mw.mw_xattn_bwd(q, k, v, o, lse, bad, kv_len)
+    torch.cuda.synchronize()
+    assert mw.mw_device_status() == 0
+    for b, n in enumerate(lens):
+        assert torch.count_nonzero(dk[b, :, n:]) == 0 and torch.count_nonzero(dv[b, :, n:]) == 0
+    n = lens[1]
+    assert bool(dq[1, 3, M // 2].isnan().all())
+    assert bool(dk[1, 1, :n].isnan().all()) and bool(dv[1, 1, :n, 4].isnan().all())
+    dq[1, 3, M // 2] = good[0][1, 3, M // 2]
+    for got, ref in zip((dq, dk, dv), good):
+        got, ref = got.double(), ref.double()
+        if got.shape[2] == S:  # but for the head that the row shares
+            got, ref = (torch.cat([t[0].flatten(), t[1, 0].flatten()]) for t in (got, ref))
+        # (sums of several tiles come in any order)
+        assert bool(torch.isfinite(got).all()) and float((got - ref).norm()) <= 4e-3 * float(ref.norm())
