@@ -740,8 +740,30 @@ class RingState:
         return slot
 
 
+class _FirstDerivatives(torch.autograd.Function):
+    """Gradients that were asked for with a graph of their own: there is no second
+    derivative, and without this node it would be left out silently."""
+
+    @staticmethod
+    def forward(ctx, what, compute, *inputs):
+        ctx.what = what
+        return compute(*inputs)
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise RuntimeError(f"{ctx.what} has no second derivative")
+
+
+def _first_derivatives(what: str, compute, *inputs):
+    """compute(*inputs), the gradients of a function that depend on these tensors."""
+    if torch.is_grad_enabled():
+        return _FirstDerivatives.apply(what, compute, *inputs)
+    return compute(*inputs)
+
+
 class BlockCausalAttention(torch.autograd.Function):
-    """Autograd wrapper: O = block-causal attention(q, k, v) with chunks of T_chunk."""
+    """Autograd wrapper: O = block-causal attention(q, k, v) with chunks of T_chunk.  A second
+    derivative is refused."""
 
     @staticmethod
     def forward(ctx, q, k, v, T_chunk: int, scale: Optional[float] = None):
@@ -753,13 +775,15 @@ class BlockCausalAttention(torch.autograd.Function):
     @staticmethod
     def backward(ctx, do):
         q, k, v, o, lse = ctx.saved_tensors
-        dq, dk, dv = mw_bca_bwd(q, k, v, o, lse, do.contiguous(), ctx.T_chunk, ctx.scale)
-        return dq, dk, dv, None, None
+        grads = _first_derivatives(
+            "BlockCausalAttention",
+            lambda q, k, v, do: mw_bca_bwd(q, k, v, o, lse, do.contiguous(), ctx.T_chunk, ctx.scale), q, k, v, do)
+        return (*grads, None, None)
 
 
 class CrossAttention(torch.autograd.Function):
     """Autograd wrapper: O = cross attention(q, k, v) over the first kv_len states of
-    each sample (None: all)."""
+    each sample (None: all).  A second derivative is refused."""
 
     @classmethod
     def apply(cls, q, k, v, kv_len: Optional[torch.Tensor] = None,
@@ -781,13 +805,15 @@ class CrossAttention(torch.autograd.Function):
     @staticmethod
     def backward(ctx, do):
         q, k, v, o, lse, kv_len = ctx.saved_tensors
-        dq, dk, dv = mw_xattn_bwd(q, k, v, o, lse, do.contiguous(), kv_len, ctx.scale)
-        return dq, dk, dv, None, None
+        grads = _first_derivatives(
+            "CrossAttention",
+            lambda q, k, v, do: mw_xattn_bwd(q, k, v, o, lse, do.contiguous(), kv_len, ctx.scale), q, k, v, do)
+        return (*grads, None, None)
 
 
 class LayerNorm(torch.autograd.Function):
     """Autograd wrapper: y = layer norm(x) * weight + bias, weight and bias [C], one of
-    each for every group of rows ([groups, C]), or None."""
+    each for every group of rows ([groups, C]), or None.  A second derivative is refused."""
 
     @classmethod
     def apply(cls, x, weight: Optional[torch.Tensor] = None,
@@ -810,5 +836,7 @@ class LayerNorm(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dy):
         x, weight, bias, mean, rstd = ctx.saved_tensors
-        dx, dw, db = mw_layernorm_bwd(dy.contiguous(), x, mean, rstd, weight, bias)
-        return dx, dw, db, None, None
+        grads = _first_derivatives(
+            "LayerNorm",
+            lambda x, weight, dy: mw_layernorm_bwd(dy.contiguous(), x, mean, rstd, weight, bias), x, weight, dy)
+        return (*grads, None, None)

@@ -702,6 +702,25 @@ at::Tensor plain_gradient(const at::Tensor& g, const at::Tensor& like, at::Scala
   return g.contiguous();
 }
 
+// Stands behind first derivatives that were asked for with a graph of their own: there is
+// no second one, and a gradient without a graph would leave it out silently.
+struct NoSecondDerivative : public torch::autograd::Node {
+  std::string what;
+  std::string name() const override { return "NoSecondDerivative"; }
+  variable_list apply(variable_list&&) override { TORCH_CHECK(false, what, " has no second derivative"); }
+};
+
+// For gradients that depend on `inputs`, with grad mode as the engine set it.
+template <class... T>
+void first_only(const char* what, const variable_list& grads, const T&... inputs) {
+  if (!torch::autograd::compute_requires_grad(inputs...)) return;
+  auto node = std::shared_ptr<NoSecondDerivative>(new NoSecondDerivative(), torch::autograd::deleteNode);
+  node->what = what;
+  node->set_next_edges(torch::autograd::collect_next_edges(inputs...));
+  for (const at::Tensor& g : grads)
+    if (g.defined()) torch::autograd::set_history(g, node);
+}
+
 struct CrossAttentionBackward : public torch::autograd::Node {
   SavedVariable q, k, v, o, lse, len;
   float scale = 0.f;
@@ -714,10 +733,18 @@ struct CrossAttentionBackward : public torch::autograd::Node {
   variable_list apply(variable_list&& grads) override {
     variable_list out(3);
     if (!grads[0].defined()) return out;
-    const at::NoGradGuard no_grad;
     const at::Tensor tq = q.unpack(), tk = k.unpack(), tv = v.unpack(), to = o.unpack(shared_from_this());
     const at::Tensor tl = lse.unpack(), tn = len.unpack();
-    const at::Tensor dout = plain_gradient(grads[0], tq, at::kBFloat16);
+    gradients(grads[0], tq, tk, tv, to, tl, tn, &out);
+    first_only("CrossAttention", out, tq, tk, tv, grads[0]);
+    return out;
+  }
+
+ private:
+  void gradients(const at::Tensor& grad, const at::Tensor& tq, const at::Tensor& tk, const at::Tensor& tv,
+                 const at::Tensor& to, const at::Tensor& tl, const at::Tensor& tn, variable_list* out) {
+    const at::NoGradGuard no_grad;
+    const at::Tensor dout = plain_gradient(grad, tq, at::kBFloat16);
     for (const at::Tensor* t : {&tq, &tk, &tv, &to, &tl})
       TORCH_CHECK(is_real(*t) && t->is_contiguous(), "a saved tensor is no plain CUDA tensor any more");
     const int* lens = tn.defined() ? static_cast<const int*>(tn.const_data_ptr()) : nullptr;
@@ -726,8 +753,7 @@ struct CrossAttentionBackward : public torch::autograd::Node {
     TORCH_CHECK(xattn_gradients(tq, tk, tv, lens, to, tl, dout, scale, dev, &g, &s), "no plain CUDA tensors");
     if (s != MW_OK) raise(s);
     for (size_t i = 0; i < 3; ++i)
-      if (task_should_compute_output(i)) out[i] = g[i];
-    return out;
+      if (task_should_compute_output(i)) (*out)[i] = g[i];
   }
 };
 
@@ -777,9 +803,17 @@ struct LayerNormBackward : public torch::autograd::Node {
   variable_list apply(variable_list&& grads) override {
     variable_list out(3);
     if (!grads[0].defined()) return out;
-    const at::NoGradGuard no_grad;
     const at::Tensor tx = x.unpack(), tw = weight.unpack(), tm = mean.unpack(), tr = rstd.unpack();
-    const at::Tensor dy = plain_gradient(grads[0], tx, z.yt == MW_F32 ? at::kFloat : at::kBFloat16);
+    gradients(grads[0], tx, tw, tm, tr, &out);
+    first_only("LayerNorm", out, tx, tw, grads[0]);
+    return out;
+  }
+
+ private:
+  void gradients(const at::Tensor& grad, const at::Tensor& tx, const at::Tensor& tw, const at::Tensor& tm,
+                 const at::Tensor& tr, variable_list* out) {
+    const at::NoGradGuard no_grad;
+    const at::Tensor dy = plain_gradient(grad, tx, z.yt == MW_F32 ? at::kFloat : at::kBFloat16);
     for (const at::Tensor* t : {&tx, &tm, &tr})
       TORCH_CHECK(is_real(*t) && t->is_contiguous(), "a saved tensor is no plain CUDA tensor any more");
     // (gradients of parameters that nothing asks for are left out)
@@ -792,8 +826,7 @@ struct LayerNormBackward : public torch::autograd::Node {
                 "no plain CUDA tensors");
     if (s != MW_OK) raise(s);
     for (size_t i = 0; i < 3; ++i)
-      if (g[i].defined() && task_should_compute_output(i)) out[i] = g[i];
-    return out;
+      if (g[i].defined() && task_should_compute_output(i)) (*out)[i] = g[i];
   }
 };
 
