@@ -540,6 +540,7 @@ PyObject* xattn_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 // Type codes of the layer norm's arrays (-1: another type).
 int norm_type(at::ScalarType t) { return t == at::kBFloat16 ? MW_BF16 : t == at::kFloat ? MW_F32 : -1; }
+at::ScalarType torch_type(int t) { return t == MW_F32 ? at::kFloat : at::kBFloat16; }
 
 // A layer norm call: its tensors and sizes, and the results of its forward.
 struct Norm {
@@ -702,6 +703,15 @@ at::Tensor plain_gradient(const at::Tensor& g, const at::Tensor& like, at::Scala
   return g.contiguous();
 }
 
+// A saved tensor as the forward left it: a hook may have put another in its place, and the
+// kernels get its address.
+void check_saved(const at::Tensor& t, const char* name, at::ScalarType type, at::IntArrayRef sizes,
+                 c10::DeviceIndex dev) {
+  TORCH_CHECK(t.defined() && is_real(t) && t.is_contiguous() && t.scalar_type() == type && t.sizes() == sizes &&
+                  t.get_device() == dev,
+              "the saved ", name, " is not the plain CUDA tensor that was saved");
+}
+
 // Stands behind first derivatives that were asked for with a graph of their own: there is
 // no second one, and a gradient without a graph would leave it out silently.
 struct NoSecondDerivative : public torch::autograd::Node {
@@ -723,6 +733,8 @@ void first_only(const char* what, const variable_list& grads, const T&... inputs
 
 struct CrossAttentionBackward : public torch::autograd::Node {
   SavedVariable q, k, v, o, lse, len;
+  Shape q_sizes{}, k_sizes{};
+  bool lengths = false;
   float scale = 0.f;
   c10::DeviceIndex dev = 0;
 
@@ -744,10 +756,14 @@ struct CrossAttentionBackward : public torch::autograd::Node {
   void gradients(const at::Tensor& grad, const at::Tensor& tq, const at::Tensor& tk, const at::Tensor& tv,
                  const at::Tensor& to, const at::Tensor& tl, const at::Tensor& tn, variable_list* out) {
     const at::NoGradGuard no_grad;
+    check_saved(tq, "q", at::kBFloat16, q_sizes, dev);
+    check_saved(tk, "k", at::kBFloat16, k_sizes, dev);
+    check_saved(tv, "v", at::kBFloat16, k_sizes, dev);
+    check_saved(to, "o", at::kBFloat16, q_sizes, dev);
+    check_saved(tl, "lse", at::kFloat, at::IntArrayRef(q_sizes.data(), 3), dev);
+    if (lengths) check_saved(tn, "kv_len", at::kInt, at::IntArrayRef(q_sizes.data(), 1), dev);
     const at::Tensor dout = plain_gradient(grad, tq, at::kBFloat16);
-    for (const at::Tensor* t : {&tq, &tk, &tv, &to, &tl})
-      TORCH_CHECK(is_real(*t) && t->is_contiguous(), "a saved tensor is no plain CUDA tensor any more");
-    const int* lens = tn.defined() ? static_cast<const int*>(tn.const_data_ptr()) : nullptr;
+    const int* lens = lengths ? static_cast<const int*>(tn.const_data_ptr()) : nullptr;
     std::array<at::Tensor, 3> g;
     mw_status s = MW_OK;
     TORCH_CHECK(xattn_gradients(tq, tk, tv, lens, to, tl, dout, scale, dev, &g, &s), "no plain CUDA tensors");
@@ -782,6 +798,9 @@ PyObject* xattn_apply(PyObject*, PyObject* const* a, Py_ssize_t n) {
     node->v = SavedVariable(v, false);
     node->lse = SavedVariable(x.lse, false);
     if (x.st.len) node->len = SavedVariable(*x.st.len, false);
+    node->lengths = x.st.len != nullptr;
+    node->q_sizes = shape(q);
+    node->k_sizes = shape(k);
     node->scale = x.scale;
     node->dev = x.dev;
     torch::autograd::set_history(x.o, node);
@@ -794,6 +813,7 @@ PyObject* xattn_apply(PyObject*, PyObject* const* a, Py_ssize_t n) {
 struct LayerNormBackward : public torch::autograd::Node {
   SavedVariable x, weight, mean, rstd;
   NormSizes z{};
+  std::vector<int64_t> sizes;  // of x
   c10::DeviceIndex dev = 0;
 
   std::string name() const override { return "LayerNormBackward"; }
@@ -813,16 +833,19 @@ struct LayerNormBackward : public torch::autograd::Node {
   void gradients(const at::Tensor& grad, const at::Tensor& tx, const at::Tensor& tw, const at::Tensor& tm,
                  const at::Tensor& tr, variable_list* out) {
     const at::NoGradGuard no_grad;
-    const at::Tensor dy = plain_gradient(grad, tx, z.yt == MW_F32 ? at::kFloat : at::kBFloat16);
-    for (const at::Tensor* t : {&tx, &tm, &tr})
-      TORCH_CHECK(is_real(*t) && t->is_contiguous(), "a saved tensor is no plain CUDA tensor any more");
+    const at::IntArrayRef lead(sizes.data(), sizes.size() - 1);
+    check_saved(tx, "x", torch_type(z.xt), sizes, dev);
+    check_saved(tm, "mean", at::kFloat, lead, dev);
+    check_saved(tr, "rstd", at::kFloat, lead, dev);
+    if (z.w) check_saved(tw, "weight", torch_type(z.pt), z.params, dev);
+    const at::Tensor dy = plain_gradient(grad, tx, torch_type(z.yt));
     // (gradients of parameters that nothing asks for are left out)
     NormSizes need = z;
     need.w = z.w && task_should_compute_output(1);
     need.b = z.b && task_should_compute_output(2);
     std::array<at::Tensor, 3> g;
     mw_status s = MW_OK;
-    TORCH_CHECK(norm_gradients(dy, tx, tm, tr, tw.defined() ? tw.const_data_ptr() : nullptr, need, dev, &g, &s),
+    TORCH_CHECK(norm_gradients(dy, tx, tm, tr, z.w ? tw.const_data_ptr() : nullptr, need, dev, &g, &s),
                 "no plain CUDA tensors");
     if (s != MW_OK) raise(s);
     for (size_t i = 0; i < 3; ++i)
@@ -856,6 +879,7 @@ PyObject* norm_apply(PyObject*, PyObject* const* a, Py_ssize_t n) {
     node->mean = SavedVariable(t.mean, false);
     node->rstd = SavedVariable(t.rstd, false);
     node->z = norm_sizes(t, yt);
+    node->sizes = x.sizes().vec();
     node->dev = t.dev;
     torch::autograd::set_history(t.y, node);
   }
