@@ -262,6 +262,7 @@ mw_status mw_xattn_fwd(const void* q, const void* k, const void* v, const int* k
   p.sms = sm_count();
   p.scale_log2 = scale * 1.4426950408889634f;
   p.budget_ns = budget_ns();
+  p.debug_skip_q = debug_skip_q();
   return launch_status(launch_xattn_few(kernel_d(d), tk, tv, p, scope.device(), s),
                        "cross attention forward launch");
 }

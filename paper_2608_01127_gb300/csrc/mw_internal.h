@@ -258,6 +258,7 @@ struct XattnFewParams {
   float scale_log2;
   unsigned* status;
   unsigned long long budget_ns;
+  int debug_skip_q;    // test hook: never load K and V
 };
 // d: tile width (64 or 128); without states any maps
 cudaError_t launch_xattn_few(int d, const CUtensorMap& tk, const CUtensorMap& tv, const XattnFewParams& p, int dev,

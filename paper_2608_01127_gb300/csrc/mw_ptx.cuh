@@ -64,6 +64,10 @@ struct WaitCtl {
   uint64_t budget_ns;      // per wait
 };
 
+// The test hook of cross attention's forward: 1, no CTA loads what its first wait is for;
+// 2, the odd ones do not.
+__device__ __forceinline__ bool skips_loads(int hook) { return hook == 1 || (hook == 2 && (blockIdx.x & 1)); }
+
 // Waits for the phase with the given parity; gives up after the budget (or
 // when another role of the CTA already gave up), records the timeout in the
 // status word and returns false.  Never traps.  The abort flag and the clock

@@ -15,6 +15,8 @@
 // (5.4 TB/s, of which some 6 us are the start, the first loads and the join).
 #include <cooperative_groups.h>
 
+#include <cfloat>
+
 #include "mw_internal.h"
 #include "mw_ptx.cuh"
 
@@ -73,8 +75,9 @@ __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint3
 // The weight of a part whose maximum is m once the whole's is top (-inf: no keys).
 __device__ __forceinline__ float weight(float m, float top) { return m == -INFINITY ? 0.f : ex2_approx(m - top); }
 
-// Cluster: a head's rows; CTA: a share of its stages of keys.
-template <int D, int R>
+// Cluster: a head's rows; CTA: a share of its stages of keys.  HOOK: with the test option, in
+// a kernel of its own (a look at it in the copying warp cost 0.1 of 3.5 us).
+template <int D, int R, bool HOOK>
 __global__ void __launch_bounds__(Layout<D, R>::THREADS)
     xattn_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                      const XattnFewParams p) {
@@ -121,7 +124,8 @@ __global__ void __launch_bounds__(Layout<D, R>::THREADS)
     // ------------------------------------------------------------ copies
     if (lane == 0) {
       int issued = 0;
-      for (; issued < n; ++issued) {
+      const int copies = HOOK && skips_loads(p.debug_skip_q) ? 0 : n;
+      for (; issued < copies; ++issued) {
         const int st = issued % kStages;
         if (!mbar_wait(&empty[st], ((issued / kStages) & 1) ^ 1, ctl)) break;
         mbar_arrive_expect_tx(&full[st], 2 * L::TILE_BYTES);
@@ -249,7 +253,12 @@ __global__ void __launch_bounds__(Layout<D, R>::THREADS)
 #pragma unroll
       for (int k = 0; k < D / 8; ++k)
         *reinterpret_cast<float2*>(&mine.o[r][8 * k + pair]) = make_float2(o[k][2 * h], o[k][2 * h + 1]);
-      if (pair == 0) mine.m[r] = ok ? m[h] : -INFINITY, mine.l[r] = l[h], mine.e[r] = e[h];
+      if (pair == 0) {
+        // a warp whose wait ran out: a part that outweighs all others and makes the sum -inf
+        mine.m[r] = ok ? m[h] : FLT_MAX;
+        mine.l[r] = ok ? l[h] : -INFINITY;
+        mine.e[r] = e[h];
+      }
     }
   }
   __syncthreads();
@@ -283,15 +292,15 @@ __global__ void __launch_bounds__(Layout<D, R>::THREADS)
       acc = fmaf(other->o[r][ch], a, acc);
     }
     const size_t at = static_cast<size_t>(bh) * p.M + r;
-    // (a NaN is a result, not a row without states)
-    p.o[at * p.d + ch] = __float2bfloat16(sum == 0.f ? 0.f : acc / sum);
+    // 0: no states; -inf: a wait ran out, and what the others read is no result either (a NaN is)
+    p.o[at * p.d + ch] = __float2bfloat16(sum <= 0.f ? 0.f : acc / sum);
     if (p.lse && ch == 0)
-      p.lse[at] = sum == 0.f ? -INFINITY : (top + __log2f(exact)) * 0.69314718055994530942f;
+      p.lse[at] = sum <= 0.f ? -INFINITY : (top + __log2f(exact)) * 0.69314718055994530942f;
   }
   cluster.sync();  // shared memory stays until all have read it
 }
 
-template <int D, int R>
+template <int D, int R, bool HOOK = false>
 cudaError_t launch(const CUtensorMap& tk, const CUtensorMap& tv, const XattnFewParams& p, int dev, cudaStream_t s) {
   using L = Layout<D, R>;
   // CTAs a head: as many as the SMs hold at once (their shared memory: two, or four of
@@ -302,9 +311,9 @@ cudaError_t launch(const CUtensorMap& tk, const CUtensorMap& tv, const XattnFewP
   static OncePerDevice prepared;
   const cudaError_t e = prepared(dev, [] {
     const cudaError_t e0 =
-        cudaFuncSetAttribute(xattn_few_kernel<D, R>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::BYTES);
+        cudaFuncSetAttribute(xattn_few_kernel<D, R, HOOK>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::BYTES);
     if (e0 != cudaSuccess) return e0;
-    return cudaFuncSetAttribute(xattn_few_kernel<D, R>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    return cudaFuncSetAttribute(xattn_few_kernel<D, R, HOOK>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
   });
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg{};
@@ -320,13 +329,14 @@ cudaError_t launch(const CUtensorMap& tk, const CUtensorMap& tv, const XattnFewP
   cfg.stream = s;
   cfg.attrs = attr;
   cfg.numAttrs = g_pdl_enabled ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, xattn_few_kernel<D, R>, tk, tv, p);
+  return cudaLaunchKernelEx(&cfg, xattn_few_kernel<D, R, HOOK>, tk, tv, p);
 }
 
 }  // namespace
 
 cudaError_t launch_xattn_few(int d, const CUtensorMap& tk, const CUtensorMap& tv, const XattnFewParams& p, int dev,
                              cudaStream_t s) {
+  if (p.debug_skip_q) return d == 64 ? launch<64, 16, true>(tk, tv, p, dev, s) : launch<128, 16, true>(tk, tv, p, dev, s);
   if (d == 64) return p.M <= 8 ? launch<64, 8>(tk, tv, p, dev, s) : launch<64, 16>(tk, tv, p, dev, s);
   return p.M <= 8 ? launch<128, 8>(tk, tv, p, dev, s) : launch<128, 16>(tk, tv, p, dev, s);
 }

@@ -1,0 +1,70 @@
+"""Waits of cross attention's forward that run out in some CTAs only, where several share a
+head's states: the rows get O = 0 and LSE = -inf, not a softmax over the states that the others
+read; heads that none of those CTAs works on keep their results, and so does the context."""
+import pytest
+import torch
+
+import oracle
+
+pytestmark = pytest.mark.gpu
+
+OK, TIMEOUT = 0, 4
+
+
+@pytest.fixture(scope="module")
+def mw():
+    import paper_2608_01127_gb300 as pkg
+    pkg.library()
+    assert pkg.mw_device_status(clear=True) == OK
+    return pkg
+
+
+def bf(seed, *shape):
+    return torch.randn(*shape, generator=torch.Generator().manual_seed(seed)).to(torch.bfloat16)
+
+
+def run(mw, hook, M, S, d, lens, lost):
+    """lost: samples whose rows are given up."""
+    q, k, v = bf(0, 2, 2, M, d), bf(1, 2, 2, S, d), bf(2, 2, 2, S, d)
+    args = [t.cuda() for t in (q, k, v)] + [torch.tensor(lens, dtype=torch.int32, device="cuda")]
+    out = torch.full_like(args[0], float("nan")), torch.full((2, 2, M), float("nan"), device="cuda")
+    workspace = torch.empty(max(256, mw.mw_xattn_workspace_size(2, 2, 2, M, S, d)), dtype=torch.uint8, device="cuda")
+    mw.mw_set_option("wait_budget_ms", 100)
+    mw.mw_set_option("debug_skip_q_load", hook)
+    try:
+        mw.mw_xattn_fwd(*args, workspace=workspace, out=out)
+        status = mw.mw_device_status(clear=True)
+    finally:
+        mw.mw_set_option("debug_skip_q_load", 0)
+        mw.mw_set_option("wait_budget_ms", 2000)
+    assert status == (TIMEOUT if lost else OK)
+    ref, lse_ref = oracle.xattn_fwd(q, k, v, lens, d ** -0.5)
+
+    def right(o, lse, b):
+        if lens[b] == 0:
+            return torch.count_nonzero(o[b]) == 0 and bool((lse[b] == -float("inf")).all())
+        return (float((o[b].double().cpu() - ref[b]).norm()) <= 5e-3 * float(ref[b].norm()) and
+                float((lse[b].double().cpu() - lse_ref[b]).abs().max()) <= 1e-3)
+
+    for b in range(2):
+        if b in lost:
+            assert torch.count_nonzero(out[0][b]) == 0 and bool((out[1][b] == -float("inf")).all()), b
+        else:
+            assert right(*out, b), b
+    again = mw.mw_xattn_fwd(*args)
+    torch.cuda.synchronize()
+    assert mw.mw_device_status() == OK
+    assert right(*again, 0) and right(*again, 1)
+
+
+@pytest.mark.parametrize("d", [64, 72, 128])
+@pytest.mark.parametrize("M", [1, 8, 9, 16])
+@pytest.mark.parametrize("hook,S,lens,lost", [
+    (1, 50, [50, 0], [0]),           # one CTA a head
+    (1, 2000, [2000, 1000], [0, 1]),  # a cluster a head
+    (2, 2000, [2000, 1000], [0, 1]),  # every other CTA of a cluster
+    (2, 2000, [60, 2000], [1]),      # (60 states are the first CTA's alone)
+    (2, 2000, [0, 100], [1]),
+])
+def test_few_rows(mw, hook, S, lens, lost, M, d):
+    run(mw, hook, M, S, d, lens, lost)
