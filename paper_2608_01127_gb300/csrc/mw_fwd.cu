@@ -925,7 +925,8 @@ __global__ void __launch_bounds__(256) combine_kernel(const float* __restrict__ 
         if (s < n) m = fmaxf(m, ls[s]);
     }
     // a split whose LSE is -inf saw no key of the row: its O part is skipped
-    // (never multiplied: it may hold anything); a NaN makes the row one
+    // (never multiplied: it may hold anything); a NaN makes the row one; +inf,
+    // which no sum of weights has: a split that was given up, and the row with it
 #pragma unroll
     for (int k = 0; k < kChunk; ++k) {
       if (s0 + k >= n) break;
@@ -943,6 +944,11 @@ __global__ void __launch_bounds__(256) combine_kernel(const float* __restrict__ 
     }
   }
   if (row >= n_rows) return;
+  if (m == INFINITY) {
+    wsum = 0.f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) acc[k] = 0.f;
+  }
   const float inv = wsum == 0.f ? 0.f : 1.f / wsum;
   *reinterpret_cast<uint4*>(o + static_cast<size_t>(row) * d_io + 8 * sub) =
       make_uint4(pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv),

@@ -231,7 +231,7 @@ struct XattnTcParams {
   __nv_bfloat16* o;
   float* lse;          // nullable
   float* o_part;       // [num_splits, BH * M, D] where num_splits > 1
-  float* lse_part;     // [num_splits, BH * M]
+  float* lse_part;     // [num_splits, BH * M]; +inf: its range was given up
   int BH, heads, M, S, d;
   int n_qblocks, num_splits;
   int items;           // BH * n_qblocks * num_splits

@@ -141,20 +141,21 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
     else if (p.lse)
       p.lse[at] = lse;
   };
-  auto store_nothing = [&](const Block& w, int row) {
-    if (p.num_splits == 1) {  // (the combine skips a split whose LSE is -inf)
+  auto store_nothing = [&](const Block& w, int row, float lse) {
+    if (p.num_splits == 1) {  // (the combine does not read O of a split that saw nothing)
       uint4* dst = reinterpret_cast<uint4*>(p.o + (static_cast<size_t>(w.bh) * p.M + row) * p.d);
       for (int c = 0; c < p.d / 8; ++c) dst[c] = make_uint4(0u, 0u, 0u, 0u);
     }
-    store_lse(w, row, -INFINITY);
+    store_lse(w, row, lse);
   };
 
-  auto leave_nothing = [&]() {  // in all blocks of this CTA
+  // in all blocks of this CTA; a range of a row's keys takes the others along (+inf)
+  auto leave_nothing = [&]() {
 #pragma unroll 1
     for (int x = blockIdx.x; x < p.items; x += gridDim.x) {
       const Block w = block_of(p, x);
       const int row = w.r0 + static_cast<int>(threadIdx.x);
-      if (threadIdx.x < kFwdBlockRows && row < p.M) store_nothing(w, row);
+      if (threadIdx.x < kFwdBlockRows && row < p.M) store_nothing(w, row, p.num_splits > 1 ? INFINITY : -INFINITY);
     }
   };
 
@@ -287,7 +288,7 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
         if (w.n == 0) continue;
         const int qb = nq % NQ;
         if (!(ok = mbar_wait(&q_empty[qb], ((nq / NQ) & 1) ^ 1, ctl))) break;
-        if (!p.debug_skip_q) {
+        if (!skips_loads(p.debug_skip_q)) {
           const int tiles = w.present(1, p.M) ? QT : 1;
           mbar_arrive_expect_tx(&q_full[qb], tiles * L::TILE_BYTES);
           for (int t = 0; t < tiles; ++t)
@@ -491,7 +492,7 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
       if (!more && (*abort_flag || !pending)) break;
       const int row = w.r0 + row_local;
       if (more && w.n == 0) {  // no keys
-        if (row < p.M) store_nothing(w, row);
+        if (row < p.M) store_nothing(w, row, -INFINITY);
         __syncwarp();
         continue;
       }

@@ -68,3 +68,12 @@ def run(mw, hook, M, S, d, lens, lost):
 ])
 def test_few_rows(mw, hook, S, lens, lost, M, d):
     run(mw, hook, M, S, d, lens, lost)
+
+
+@pytest.mark.parametrize("d", [64, 72, 128])
+@pytest.mark.parametrize("hook,lens,lost", [(1, [1500, 700], [0, 1]), (2, [1500, 700], [0, 1]), (2, [1500, 100], [0]),
+                                            (2, [0, 1400], [1])])
+def test_key_ranges_joined_in_another_kernel(mw, hook, lens, lost, d):
+    """40 rows of 1500 states: a key tile a range, the odd ones given up."""
+    assert mw.mw_xattn_workspace_size(2, 2, 2, 40, 1500, d) >= 12 * 4 * 40 * (64 if d == 64 else 128) * 4
+    run(mw, hook, 40, 1500, d, lens, lost)
