@@ -399,8 +399,8 @@ mw_status mw_device_status(void* stream, int clear);
  *                      (default 2000)
  *   "debug_skip_q_load" non-zero: the forward and backward kernels never
  *                      load Q (cross attention's forward of at most 16 rows a
- *                      head: K and V), so their first wait expires; 2: of
- *                      cross attention's forward the odd CTAs only; for
+ *                      head: K and V), so their first wait expires; 2: where
+ *                      CTAs share a head's keys, the odd ones only; for
  *                      testing the timeout path only
  *   "fwd_group_waves"  forward CTAs per head group, in multiples of the SM
  *                      count (default 3; 0 restores it): the query blocks of

@@ -202,8 +202,8 @@ __global__ void __launch_bounds__(FwdLayout<D, DM>::THREADS, 1)
   const int r0 = qb * kFwdBlockRows;
   if ((smem_u32(smem) & 1023u) != 0u) {
     // nothing runs without aligned shared memory: report it, and give this
-    // CTA's rows a defined result (O = 0, LSE = -inf; as split partials, a
-    // -inf LSE that the combine skips) instead of leaving stale values behind
+    // CTA's rows a defined result (O = 0, LSE = -inf; as split partials, an
+    // LSE of +inf, which makes the combine do so) instead of leaving stale values behind
     if (threadIdx.x == 0) atomicOr(p.status, kDevMisaligned);
     const int row = r0 + static_cast<int>(threadIdx.x);
     if (threadIdx.x < kFwdBlockRows && row < p.rows_q) {
@@ -214,7 +214,7 @@ __global__ void __launch_bounds__(FwdLayout<D, DM>::THREADS, 1)
         for (int c = 0; c < d_io / 8; ++c) dst[c] = make_uint4(0u, 0u, 0u, 0u);
         if (p.lse) p.lse[row_off] = -INFINITY;
       } else {
-        p.lse_part[static_cast<size_t>(split) * p.BH * p.rows_q + row_off] = -INFINITY;
+        p.lse_part[static_cast<size_t>(split) * p.BH * p.rows_q + row_off] = INFINITY;
       }
     }
     return;  // uniform across the CTA, before any barrier or TMEM use
@@ -332,7 +332,7 @@ __global__ void __launch_bounds__(FwdLayout<D, DM>::THREADS, 1)
     if (lane == 0 && n_local > 0) {
       if (!SPLIT) prefetch_maps();
       bool q_issued = false;
-      if (!p.debug_skip_q) {
+      if (!(SPLIT ? skips_loads(p.debug_skip_q) : p.debug_skip_q != 0)) {
         mbar_arrive_expect_tx(q_full, QT * L::TILE_BYTES);
         for (int t = 0; t < QT; ++t)
           for (int r = 0; r < L::REG; ++r)
@@ -842,7 +842,8 @@ __global__ void __launch_bounds__(FwdLayout<D, DM>::THREADS, 1)
       if constexpr (!SPLIT) {
         if (p.lse) p.lse[row_off] = lse;
       } else {
-        p.lse_part[static_cast<size_t>(split) * p.BH * p.rows_q + row_off] = lse;
+        // (+inf: a range that was given up takes its rows along)
+        p.lse_part[static_cast<size_t>(split) * p.BH * p.rows_q + row_off] = have || n_steps == 0 ? lse : INFINITY;
       }
     }
   }

@@ -50,7 +50,7 @@ mw_status status_ptr(int dev, unsigned** out);
 int sm_count();
 // Budget of a kernel's wait (option wait_budget_ms).
 unsigned long long budget_ns();
-// Test hook (option debug_skip_q_load).
+// Test hook (option debug_skip_q_load): bit 0 for the even CTAs, bit 1 for the odd ones.
 int debug_skip_q();
 
 inline size_t align256(size_t x) { return (x + 255) & ~size_t(255); }

@@ -64,9 +64,9 @@ struct WaitCtl {
   uint64_t budget_ns;      // per wait
 };
 
-// The test hook of cross attention's forward: 1, no CTA loads what its first wait is for;
-// 2, the odd ones do not.
-__device__ __forceinline__ bool skips_loads(int hook) { return hook == 1 || (hook == 2 && (blockIdx.x & 1)); }
+// The test hook where CTAs share a head's keys: bit 0, the even CTAs do not load what
+// their first wait is for; bit 1, the odd ones.
+__device__ __forceinline__ bool skips_loads(int hook) { return (hook >> (blockIdx.x & 1)) & 1; }
 
 // Waits for the phase with the given parity; gives up after the budget (or
 // when another role of the CTA already gave up), records the timeout in the
