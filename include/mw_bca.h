@@ -343,6 +343,10 @@ mw_status mw_xattn_fwd(const void* q, const void* k, const void* v, const int* k
  * places past kv_len.  o and lse are the forward's: D carries the rounding of o to
  * bf16, whose share of dQ is proportional to the row's mean key (dQ itself depends
  * on the keys' differences only); of samples with 2 to 8 states D is summed again.
+ * Where several CTAs add to a sum (by the sizes, dQ or dK and dV of more than 128
+ * states, or dK and dV of fewer), fp32 parts come in any order, and the last place may
+ * differ between calls.  After a wait that ran out (MW_ERR_TIMEOUT) gradients are not to
+ * be used: CTAs that gave up write zeros, the others' parts may be there.
  */
 size_t mw_xattn_bwd_workspace_size(int B, int H, int Hkv, int M, int S, int d);
 mw_status mw_xattn_bwd(const void* q, const void* k, const void* v, const int* kv_len, const void* o,

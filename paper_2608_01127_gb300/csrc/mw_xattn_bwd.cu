@@ -23,7 +23,7 @@
 // bf16 for their products, D comes from O in bf16; all sums are fp32.
 //
 // Bound by the chain S -> P -> dS -> dK, dQ of a step, and at d = 64 by instructions that
-// have to be fetched (2.8 stalls an issue), at 128 by the tensor core's share of 47%
+// have to be fetched (3.0 stalls an issue), at 128 by the tensor core's share of 49%
 // besides.  Measured, us a step and an SM, 24 query x 40 key tiles a head (key-major):
 // d = 64 1.35, 72 2.03, 128 2.21, where the products alone take 0.84, 1.05 and 1.68 at the
 // measured tensor rate; 40 x 2 tiles 1.94 (query-major), 2.16, 2.67.

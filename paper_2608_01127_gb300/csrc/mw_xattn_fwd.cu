@@ -28,7 +28,10 @@
 // TMEM: S_t at column 128 t, O_t at 256 + DM t; P_t, bf16, over S_t, its second half in
 // columns of its own where there is room.  The row sums are of the weights before their
 // rounding to bf16 (the block-causal forward takes those after it), in 32 bits: LSE is as
-// exact as S, and the backward's P with it.
+// exact as S, and the backward's P with it.  O is divided by the same sum, so that the mean
+// rounding of a row's weights, 2^-9 at most and less over many states, scales what its values
+// have in common: within O's own rounding to bf16.  (The form for few rows keeps both sums:
+// a second one here would lengthen the chain that bounds a step.)
 #include <type_traits>
 
 #include "mw_internal.h"
