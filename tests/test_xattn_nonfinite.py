@@ -126,3 +126,41 @@ def test_a_gradient_of_one_row(mw, M, S, lens, d):
             got, ref = (torch.cat([t[0].flatten(), t[1, 0].flatten()]) for t in (got, ref))
         # (sums of several tiles come in any order)
         assert bool(torch.isfinite(got).all()) and float((got - ref).norm()) <= 4e-3 * float(ref.norm())
+
+
+@pytest.mark.parametrize("d", [64, 72, 128])
+@pytest.mark.parametrize("M,S,lens", [(4, 90, [30, 90]), (40, 200, [130, 70]), (700, 700, [300, 650]), (9000, 300, [5, 290])])
+@pytest.mark.parametrize("where", ["q", "key"])
+def test_gradients_of_inputs_with_a_nan(mw, M, S, lens, d, where):
+    """Forward and backward: a NaN in a row of Q reaches that row's dQ and its heads' valid
+    keys, one in a key all rows of the heads that share it; padded places, and the heads and
+    rows that do not see it, keep their gradients."""
+    B, H, Hkv = 2, 4, 2
+    q, k, v, do = (t.cuda() for t in (bf(20, B, H, M, d), bf(21, B, Hkv, S, d), bf(22, B, Hkv, S, d), bf(23, B, H, M, d)))
+    kv_len = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    o, lse = mw.mw_xattn_fwd(q, k, v, kv_len)
+    good = mw.mw_xattn_bwd(q, k, v, o, lse, do, kv_len)
+    n = lens[1]
+    lost = torch.zeros(B, H, M, dtype=torch.bool, device="cuda")
+    if where == "q":
+        q[1, 3, M // 2, 2] = NAN
+        lost[1, 3, M // 2] = True
+    else:
+        k[1, 1, n - 1, 2] = NAN
+        lost[1, 2:] = True
+    o, lse = mw.mw_xattn_fwd(q, k, v, kv_len)
+    assert torch.equal(o.isnan(), lost[..., None].expand_as(o)) and torch.equal(lse.isnan(), lost)
+    dq, dk, dv = mw.mw_xattn_bwd(q, k, v, o, lse, do, kv_len)
+    torch.cuda.synchronize()
+    assert mw.mw_device_status() == 0
+    for b, m in enumerate(lens):
+        assert torch.count_nonzero(dk[b, :, m:]) == 0 and torch.count_nonzero(dv[b, :, m:]) == 0
+    assert torch.equal(dq.isnan(), lost[..., None].expand_as(dq))
+    assert bool(dk[1, 1, :n].isnan().all()) and bool(dv[1, 1, :n].isnan().all())
+    for i, got in enumerate((dq, dk, dv)):
+        keep = ~lost if i == 0 else torch.ones(B, Hkv, S, dtype=torch.bool, device="cuda")
+        if i > 0:
+            keep[1, 1] = False
+        got, ref = got[keep].double(), good[i][keep].double()
+        # (sums of several tiles come in any order)
+        assert bool(torch.isfinite(got).all()) and float((got - ref).norm()) <= 4e-3 * float(ref.norm())
