@@ -342,7 +342,8 @@ mw_status mw_xattn_fwd(const void* q, const void* k, const void* v, const int* k
  * those of K and V summed over the query heads that share them, and 0 in the
  * places past kv_len.  o and lse are the forward's: D carries the rounding of o to
  * bf16, whose share of dQ is proportional to the row's mean key (dQ itself depends
- * on the keys' differences only); of samples with 2 to 8 states D is summed again.
+ * on the keys' differences only) and which grows where rows put nearly all their weight
+ * on one state; of samples with 2 to 8 states D is summed again.
  * Where several CTAs add to a sum (by the sizes, dQ or dK and dV of more than 128
  * states, or dK and dV of fewer), fp32 parts come in any order, and the last place may
  * differ between calls.  After a wait that ran out (MW_ERR_TIMEOUT) gradients are not to
