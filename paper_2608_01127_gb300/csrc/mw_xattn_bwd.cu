@@ -914,9 +914,11 @@ __global__ void __launch_bounds__(Layout<D, DM>::THREADS, 1)
         }
         if (32 * c >= p.d) continue;
         // past the valid states: weights of 0, but a NaN or an infinity of dO or D times them is NaN
-        const uint32_t keep = row + lane < w.len ? 0xffffffffu : 0u;
+        if (row + 32 > w.len) {
+          const uint32_t keep = row + lane < w.len ? 0xffffffffu : 0u;
 #pragma unroll
-        for (int k = 0; k < 32; ++k) r[k] &= keep;
+          for (int k = 0; k < 32; ++k) r[k] &= keep;
+        }
         if (!p.dkv_whole) {
           put_rows(is_dk ? &tm_dk : &tm_dv, r, 32 * c, row, true);
         } else if (row + lane < p.S) {
