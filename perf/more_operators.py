@@ -283,12 +283,12 @@ def run(state):
         dx, dw = torch.autograd.grad(y, (s["x"], s["w"]), s["dy"])
         return {"y": y.detach(), "dx": dx, "dw": dw}
     if kind == "mm":
-        return {"y": lib.mw_fp8_matmul(s["xq"], s["xs"], s["wq"], s["ws"])}
+        return {"y": lib.mw_scaled_matmul(s["xq"], s["xs"], s["wq"], s["ws"])}
     if kind == "out":
-        q, scale = lib.mw_fp8_quantize(s["x"], (1, 128))
-        return {"y": lib.mw_fp8_matmul(q, scale, s["wq"], s["ws"])}
-    q, scale, h, _ = lib.mw_rmsnorm_fp8(s["x"], s["weight"], s["residual"], EPS, need_stats=False)
-    return {"h": h, "y": lib.mw_fp8_matmul(q, scale, s["wq"], s["ws"])}
+        q, scale = lib.mw_quantize(s["x"], (1, 128))
+        return {"y": lib.mw_scaled_matmul(q, scale, s["wq"], s["ws"])}
+    q, scale, h, _ = lib.mw_rmsnorm_quantize(s["x"], s["weight"], s["residual"], EPS, need_stats=False)
+    return {"h": h, "y": lib.mw_scaled_matmul(q, scale, s["wq"], s["ws"])}
 
 
 # ------------------------------------------------------------------ the same in 64 bits
