@@ -383,6 +383,74 @@ mw_status mw_layernorm_bwd(const void* dy, const void* x, const float* mean, con
                            size_t ws_bytes, long long rows, int C, int groups, int x_dtype,
                            int y_dtype, int param_dtype, void* stream);
 
+/* ---- Projections in 8 bits: RMS norm in front, the form, the product ---- */
+
+/*
+ * Root-mean-square norm over the C <= 8192 channels of each of `rows` rows, with the
+ * residual's addition in front:
+ *     h = x + residual, rounded to x's type (x itself where residual is NULL),
+ *     rstd = 1 / sqrt(sum h^2 / C + eps),   y = h rstd w_g
+ * with one weight for each of `groups` equal groups of consecutive rows (weight [groups, C];
+ * NULL: 1).  x, residual and h have one type, bf16 or fp32; y that one or bf16, or MW_E4M3:
+ * the 8-bit form of y in MW_FP8_ROWS (below), y codes and y_scale [rows, ceil(C / 128)]
+ * (then C is a multiple of 16, and x, residual, weight, y and h are 16-byte aligned).
+ * h is written where there is a residual, y_scale with MW_E4M3, rstd (fp32 [rows], for the
+ * backward) where it is not NULL.  Otherwise pointers need the alignment of their elements
+ * only; with C a multiple of 8 and all of them 16-byte aligned, memory is accessed 16 bytes
+ * at a time.
+ */
+enum { MW_E4M3 = 2 };
+mw_status mw_rmsnorm_fwd(const void* x, const void* residual, const void* weight, void* y, void* y_scale, void* h,
+                         float* rstd, long long rows, int C, int groups, float eps, int x_dtype, int y_dtype,
+                         int param_dtype, void* stream);
+
+/*
+ * Its gradients, from h (x where there was no residual), rstd, dy in y's type (bf16 or
+ * fp32) and dh, what comes down to h besides (x's type; NULL: nothing): dx in x's type is the
+ * gradient of x and of the residual alike; dweight (NULL: left out) in the weight's, summed
+ * over each group's rows in fp32 in a fixed order.
+ */
+size_t mw_rmsnorm_bwd_workspace_size(long long rows, int C, int groups);
+mw_status mw_rmsnorm_bwd(const void* dy, const void* h, const float* rstd, const void* weight, const void* dh,
+                         void* dx, void* dweight, void* workspace, size_t ws_bytes, long long rows, int C, int groups,
+                         int x_dtype, int y_dtype, int param_dtype, void* stream);
+
+/*
+ * The 8-bit form of a matrix x [rows, C]: codes q (e4m3) and, for every block of 128
+ * elements, a scale (e8m0, an exponent byte) that is the least power of two s with
+ * max |x| <= 448 s in the block (at least 2^-127):  q = e4m3(x / s), to nearest even, and
+ * x is about q s.  Blocks end where the matrix does.
+ *   MW_FP8_ROWS              q, scale [rows, ceil(C / 128)]: blocks of a row's elements
+ *   MW_FP8_COLUMNS           q_columns, scale_columns [ceil(rows / 128), C]: of a column's
+ *   MW_FP8_TILES             q, scale [ceil(rows / 128), ceil(C / 128)]: of 128 x 128
+ *   MW_FP8_ROWS_AND_COLUMNS  both of the first two, x read once
+ * Codes lie as x does.  A block with a NaN or an infinity has the scale NaN (0xff) and the
+ * codes NaN.  C: a multiple of 16, at most 2^24; x (bf16 or fp32), codes and scale_columns
+ * 16-byte aligned; the arrays that a form does not name may be NULL.
+ */
+enum { MW_FP8_ROWS = 0, MW_FP8_COLUMNS = 1, MW_FP8_TILES = 2, MW_FP8_ROWS_AND_COLUMNS = 3 };
+mw_status mw_quantize(const void* x, void* q, void* scale, void* q_columns, void* scale_columns, long long rows,
+                          int C, int form, int x_dtype, void* stream);
+
+/*
+ * The product of two of them, c = A B^T, summed in fp32 on tensor cores that apply the
+ * scales themselves:
+ *     c[m, n] = sum_k a[m, k] sa[m, k / 128] b[n, k] sb[n, k / 128]
+ *   a : codes [M, K] with scales of the form ROWS, or of TILES (a_tiles != 0); with
+ *       a_transposed != 0 codes [K, M] with scales of the form COLUMNS, or of TILES
+ *   b : the same with N in the place of M
+ *   c : [M, N], bf16 or fp32 (c_dtype), aligned to its elements
+ * So that for y = x W^T, x in ROWS and W [N, K] in TILES: y = (x, W), dx = (dy in ROWS,
+ * W transposed), dW = (dy in COLUMNS transposed, x in COLUMNS transposed).
+ * Codes 16-byte aligned, their rows multiples of 16 (K, or M or N where transposed); 0 <=
+ * M, N, K <= 2^24, at most 2^27 tiles of 128 x 128 results.  K = 0 gives zeros.  Scales of 0xff
+ * and codes of NaN give NaN.  The order of sums is fixed by the sizes.  After a wait that
+ * ran out (MW_ERR_TIMEOUT) the results are not to be used.
+ */
+mw_status mw_scaled_matmul(const void* a, const void* a_scale, int a_tiles, int a_transposed, const void* b,
+                        const void* b_scale, int b_tiles, int b_transposed, void* c, int M, int N, int K, int c_dtype,
+                        void* stream);
+
 /* Human-readable name of a status code (static string). */
 const char* mw_status_string(mw_status s);
 

@@ -18,6 +18,11 @@ Entry points (same names as the C ABI, taking torch tensors):
   mw_xattn_bwd(q, k, v, o, lse, dout, kv_len=None, scale=None) -> (dq, dk, dv)
   mw_layernorm_fwd(x, weight=None, bias=None, eps=1e-5) -> (y, mean, rstd)
   mw_layernorm_bwd(dy, x, mean, rstd, weight, bias) -> (dx, dweight, dbias)
+  mw_rmsnorm_fwd(x, weight=None, residual=None, eps=1e-5) -> (y, h, rstd)
+  mw_rmsnorm_quantize(x, weight=None, residual=None, eps=1e-5) -> (q, scale, h, rstd)
+  mw_rmsnorm_bwd(dy, h, rstd, weight=None, dh=None) -> (dx, dweight)
+  mw_quantize(x, block=(1, 128)) -> (q, scale), mw_quantize_both(x)
+  mw_scaled_matmul(a, a_scale, b, b_scale, out_dtype=bf16) -> a b^T of two 8-bit forms
   mw_device_status(clear=True), mw_set_option(name, value)
 Attention tensors are contiguous bf16 [B, H, rows, d] on the current CUDA device.
 """
@@ -42,7 +47,9 @@ __all__ = [
     "mw_device_status", "mw_set_option", "mw_qkv_rope_split", "BlockCausalAttention",
     "mw_xattn_fwd", "mw_xattn_bwd", "mw_xattn_workspace_size", "mw_xattn_bwd_workspace_size",
     "mw_layernorm_fwd", "mw_layernorm_bwd", "mw_layernorm_bwd_workspace_size", "CrossAttention",
-    "LayerNorm",
+    "LayerNorm", "mw_rmsnorm_fwd", "mw_rmsnorm_quantize", "mw_rmsnorm_bwd",
+    "mw_rmsnorm_bwd_workspace_size", "mw_quantize", "mw_quantize_both", "mw_scaled_matmul",
+    "RMSNorm", "Fp8Linear",
     "EXPORTED_SYMBOLS",
     "RingState",
 ]
@@ -59,6 +66,8 @@ EXPORTED_SYMBOLS = (
     "mw_bca_cache_fwd_rope", "mw_qkv_rope_split", "mw_bca_cache_step", "mw_bca_bwd_head_groups",
     "mw_xattn_workspace_size", "mw_xattn_fwd", "mw_xattn_bwd_workspace_size", "mw_xattn_bwd",
     "mw_layernorm_fwd", "mw_layernorm_bwd_workspace_size", "mw_layernorm_bwd",
+    "mw_rmsnorm_fwd", "mw_rmsnorm_bwd_workspace_size", "mw_rmsnorm_bwd", "mw_quantize",
+    "mw_scaled_matmul",
 )
 
 STATUS = {0: "MW_OK", 1: "MW_ERR_INVALID_ARG", 2: "MW_ERR_UNSUPPORTED", 3: "MW_ERR_CUDA",
@@ -130,6 +139,11 @@ def library() -> ctypes.CDLL:
         "mw_layernorm_bwd_workspace_size": (_Z, [_L, _I, _I]),
         "mw_layernorm_bwd": (_I, [_P, _P, _P, _P, _P, _P, _P, _P, _P, _Z, _L, _I, _I,
                                   _I, _I, _I, _P]),
+        "mw_rmsnorm_fwd": (_I, [_P, _P, _P, _P, _P, _P, _P, _L, _I, _I, _F, _I, _I, _I, _P]),
+        "mw_rmsnorm_bwd_workspace_size": (_Z, [_L, _I, _I]),
+        "mw_rmsnorm_bwd": (_I, [_P, _P, _P, _P, _P, _P, _P, _P, _Z, _L, _I, _I, _I, _I, _I, _P]),
+        "mw_quantize": (_I, [_P, _P, _P, _P, _P, _L, _I, _I, _I, _P]),
+        "mw_scaled_matmul": (_I, [_P, _P, _I, _I, _P, _P, _I, _I, _P, _I, _I, _I, _I, _P]),
         "mw_status_string": (ctypes.c_char_p, [_I]),
         "mw_last_error": (ctypes.c_char_p, []),
         "mw_device_status": (_I, [_P, _I]),
@@ -707,6 +721,217 @@ def mw_layernorm_bwd(dy, x, mean, rstd, weight: Optional[torch.Tensor] = None,
     return dx, dw, db
 
 
+_E4M3, _E8M0 = torch.float8_e4m3fn, torch.float8_e8m0fnu
+def _rms_inputs(x, weight, residual):
+    xt = _norm_type(x, "x")
+    rows, C, groups, ptype = _norm_params(x, weight, None)
+    if residual is not None:
+        _expect(residual, "residual", tuple(x.shape), x.dtype)
+    return xt, rows, C, groups, ptype
+
+
+def mw_rmsnorm_fwd(x: torch.Tensor, weight: Optional[torch.Tensor] = None,
+                   residual: Optional[torch.Tensor] = None, eps: float = 1e-5,
+                   out_dtype: Optional[torch.dtype] = None, need_stats: bool = True,
+                   out: Optional[torch.Tensor] = None):
+    """Root-mean-square norm over the last dimension of h = x + residual (bf16 or fp32, the
+    sum rounded to x's type): y = h / sqrt(mean h^2 + eps) * weight.  Returns (y, h, rstd): h
+    is None without a residual (it is x then), rstd (fp32 [...], for the backward) None
+    without ``need_stats``.
+
+    ``weight``: [C], or [groups, C] with one for every one of ``groups`` equal runs of
+    consecutive rows (samples, frames), or None.  y has ``out_dtype`` (None: x's; fp32 only
+    with x in fp32)."""
+    if out is None and hasattr(_native, "rms_fwd"):
+        r = _native.rms_fwd(x, weight, residual, eps, out_dtype, need_stats)
+        if r is not None:
+            return r if type(r) is tuple else _check(r)
+    xt, rows, C, groups, ptype = _rms_inputs(x, weight, residual)
+    out_dtype = x.dtype if out_dtype is None else out_dtype
+    if out_dtype not in _NORM_TYPES:
+        raise TypeError(f"out_dtype must be bfloat16 or float32, got {out_dtype}")
+    if out is not None:
+        _expect(out, "out", tuple(x.shape), out_dtype)
+    _on_device(x, (("weight", weight), ("residual", residual), ("out", out)))
+    y = torch.empty(x.shape, dtype=out_dtype, device=x.device) if out is None else out
+    h = None if residual is None else torch.empty_like(x)
+    rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if need_stats else None
+    _no_alias((("out", y),), (("x", x), ("weight", weight), ("residual", residual)))
+    _check(library().mw_rmsnorm_fwd(_ptr(x), _ptr(residual), _ptr(weight), _ptr(y), None, _ptr(h), _ptr(rstd),
+                                    rows, C, groups, float(eps), xt, _NORM_TYPES[out_dtype], ptype, _stream()))
+    return y, h, rstd
+
+
+def mw_rmsnorm_quantize(x: torch.Tensor, weight: Optional[torch.Tensor] = None,
+                   residual: Optional[torch.Tensor] = None, eps: float = 1e-5, need_stats: bool = True):
+    """mw_rmsnorm_fwd with y as the product reads it: (q, scale, h, rstd) with y's 8-bit form
+    in blocks of (1, 128), as mw_quantize gives it (y itself is not rounded before).  C
+    must be a multiple of 16."""
+    if hasattr(_native, "rms_fp8"):
+        r = _native.rms_fp8(x, weight, residual, eps, need_stats)
+        if r is not None:
+            return r if type(r) is tuple else _check(r)
+    xt, rows, C, groups, ptype = _rms_inputs(x, weight, residual)
+    _fp8_source(x)
+    _on_device(x, (("weight", weight), ("residual", residual)))
+    q = torch.empty(x.shape, dtype=_E4M3, device=x.device)
+    scale = torch.empty((rows, _blocks(C)), dtype=_E8M0, device=x.device)
+    h = None if residual is None else torch.empty_like(x)
+    rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if need_stats else None
+    _check(library().mw_rmsnorm_fwd(_ptr(x), _ptr(residual), _ptr(weight), _ptr(q), _ptr(scale), _ptr(h),
+                                    _ptr(rstd), rows, C, groups, float(eps), xt, 2, ptype, _stream()))
+    return q, scale, h, rstd
+
+
+def mw_rmsnorm_bwd_workspace_size(rows: int, C: int, groups: int) -> int:
+    return int(library().mw_rmsnorm_bwd_workspace_size(rows, C, groups))
+
+
+def mw_rmsnorm_bwd(dy, h, rstd, weight: Optional[torch.Tensor] = None, dh: Optional[torch.Tensor] = None,
+                   workspace: Optional[torch.Tensor] = None):
+    """Gradients (dx, dweight) of sum(y * dy) + sum(h * dh) through mw_rmsnorm_fwd, from its
+    h (x where there was no residual) and rstd: dx is the gradient of x and of the residual
+    alike; dweight None without a weight."""
+    if workspace is None and hasattr(_native, "rms_bwd"):
+        r = _native.rms_bwd(dy, h, rstd, weight, dh)
+        if r is not None:
+            return r if type(r) is tuple else _check(r)
+    xt, yt = _norm_type(h, "h"), _norm_type(dy, "dy")
+    rows, C, groups, ptype = _norm_params(h, weight, None)
+    _expect(dy, "dy", tuple(h.shape), dy.dtype)
+    if dh is not None:
+        _expect(dh, "dh", tuple(h.shape), h.dtype)
+    _expect(rstd, "rstd", tuple(h.shape[:-1]), torch.float32)
+    _on_device(h, (("dy", dy), ("rstd", rstd), ("weight", weight), ("dh", dh), ("workspace", workspace)))
+    ws_bytes = mw_rmsnorm_bwd_workspace_size(rows, C, groups) if weight is not None else 0
+    workspace = _workspace(workspace, ws_bytes, h.device)
+    dx = torch.empty_like(h)
+    dw = None if weight is None else torch.empty_like(weight)
+    _no_alias((("workspace", workspace),), (("dy", dy), ("h", h), ("rstd", rstd), ("weight", weight), ("dh", dh)))
+    _check(library().mw_rmsnorm_bwd(_ptr(dy), _ptr(h), _ptr(rstd), _ptr(weight), _ptr(dh), _ptr(dx), _ptr(dw),
+                                    _ptr(workspace), ws_bytes, rows, C, groups, xt, yt, ptype, _stream()))
+    return dx, dw
+
+
+_FP8_FORMS = {(1, 128): 0, (128, 1): 1, (128, 128): 2}
+
+
+def _blocks(n: int) -> int:
+    return (n + 127) // 128
+
+
+def _fp8_source(x) -> Tuple[int, int, int]:
+    """Type code, rows and columns of a matrix that goes into 8 bits."""
+    xt = _norm_type(x, "x")
+    if x.dim() < 1 or not x.is_contiguous():
+        raise ValueError("x must be a contiguous [..., C] tensor")
+    C = x.shape[-1]
+    if C % 16:
+        raise ValueError(f"x has {C} columns: rows of 8-bit codes must be multiples of 16")
+    return xt, (x.numel() // C if C else 0), C
+
+
+def mw_quantize(x: torch.Tensor, block: Tuple[int, int] = (1, 128), out=None
+                    ) -> Tuple[torch.Tensor, torch.Tensor]:
+    """The 8-bit form of x [..., C] (bf16 or fp32), its rows taken as one matrix [R, C]:
+    codes in x's shape (float8_e4m3fn) and for every ``block`` -- (1, 128), (128, 1) or
+    (128, 128) elements -- a scale (float8_e8m0fnu), the least power of two s with
+    max |x| <= 448 s; x is about code * scale.  Returns (q, scale), scale
+    [ceil(R / rows), ceil(C / columns)] for blocks of rows x columns.  A block with a NaN
+    or an infinity is NaN.  C must be a multiple of 16.
+
+    ``out`` = (q, scale) reuses caller buffers."""
+    if out is None and hasattr(_native, 'fp8_form'):
+        r = _native.fp8_form(x, block)
+        if r is not None:
+            return r if type(r) is tuple else _check(r)
+    xt, rows, C = _fp8_source(x)
+    form = _FP8_FORMS.get(tuple(block))
+    if form is None:
+        raise ValueError(f"block must be (1, 128), (128, 1) or (128, 128), got {block}")
+    shape = tuple(n if b == 1 else _blocks(n) for n, b in zip((rows, C), block))
+    q, scale = out if out is not None else (None, None)
+    if out is not None:
+        _expect(q, "q", tuple(x.shape), _E4M3)
+        _expect(scale, "scale", shape, _E8M0)
+    _on_device(x, (("q", q), ("scale", scale)))
+    if out is None:
+        q = torch.empty(x.shape, dtype=_E4M3, device=x.device)
+        scale = torch.empty(shape, dtype=_E8M0, device=x.device)
+    else:
+        _no_alias((("q", q), ("scale", scale)), (("x", x),))
+    outs = (None, None, _ptr(q), _ptr(scale)) if form == 1 else (_ptr(q), _ptr(scale), None, None)
+    _check(library().mw_quantize(_ptr(x), *outs, rows, C, form, xt, _stream()))
+    return q, scale
+
+
+def mw_quantize_both(x: torch.Tensor):
+    """mw_quantize with blocks of (1, 128) and of (128, 1) elements, x read once:
+    (q, scale, q_columns, scale_columns)."""
+    if hasattr(_native, 'fp8_form'):
+        r = _native.fp8_form(x, None)
+        if r is not None:
+            return r if type(r) is tuple else _check(r)
+    xt, rows, C = _fp8_source(x)
+    _on_device(x, ())
+    q, qc = (torch.empty(x.shape, dtype=_E4M3, device=x.device) for _ in range(2))
+    scale, sc = (torch.empty(n, dtype=_E8M0, device=x.device)
+                 for n in ((rows, _blocks(C)), (_blocks(rows), C)))
+    _check(library().mw_quantize(_ptr(x), _ptr(q), _ptr(scale), _ptr(qc), _ptr(sc), rows, C, 3,
+                                     xt, _stream()))
+    return q, scale, qc, sc
+
+
+def _fp8_operand(t, scale, name: str, transposed: bool) -> Tuple[int, int, bool]:
+    """Rows, contraction and kind of scales (one for 128 rows) of an operand."""
+    for v, n, dtype in ((t, name, _E4M3), (scale, f"{name}_scale", _E8M0)):
+        if not isinstance(v, torch.Tensor):
+            raise TypeError(f"{n} must be a torch.Tensor, got {type(v).__name__}")
+        if v.dtype != dtype:
+            raise TypeError(f"{n} must be {dtype}, got {v.dtype}")
+        if v.dim() != 2 or not v.is_contiguous():
+            raise ValueError(f"{n} must be a contiguous matrix")
+    if t.shape[1] % 16:
+        raise ValueError(f"{name} has {t.shape[1]} columns: rows of 8-bit codes must be multiples of 16")
+    rows, K = reversed(t.shape) if transposed else t.shape
+    for n, tiles in ((rows, False), (_blocks(rows), True)):
+        want = (_blocks(K), n) if transposed else (n, _blocks(K))
+        if tuple(scale.shape) == want:
+            return rows, K, tiles
+    raise ValueError(f"{name}_scale {tuple(scale.shape)} does not fit {name} {tuple(t.shape)}: a scale for "
+                     f"every 128 of the contraction, and for every row or 128 of them")
+
+
+def mw_scaled_matmul(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_scale: torch.Tensor,
+                  out_dtype: torch.dtype = torch.bfloat16, a_transposed: bool = False,
+                  b_transposed: bool = False, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """c = A B^T of two 8-bit forms, [M, N] in ``out_dtype`` (bf16 or fp32), summed in fp32.
+
+    a: codes [M, K] with scales [M, ceil(K/128)] (blocks of (1, 128)) or [ceil(M/128),
+    ceil(K/128)] (of (128, 128)); with ``a_transposed`` codes [K, M] with scales
+    [ceil(K/128), M] (blocks of (128, 1)) or [ceil(K/128), ceil(M/128)].  b: the same with
+    N in the place of M.  ``out`` reuses a caller's buffer."""
+    if out is None and hasattr(_native, 'fp8_form'):
+        r = _native.fp8_matmul(a, a_scale, b, b_scale, out_dtype, a_transposed, b_transposed)
+        if r is not None:
+            return _check(r) if type(r) is int else r
+    M, K, a_tiles = _fp8_operand(a, a_scale, "a", a_transposed)
+    N, Kb, b_tiles = _fp8_operand(b, b_scale, "b", b_transposed)
+    if K != Kb:
+        raise ValueError(f"a has a contraction of {K}, b of {Kb}")
+    if out_dtype not in _NORM_TYPES:
+        raise TypeError(f"out_dtype must be bfloat16 or float32, got {out_dtype}")
+    if out is not None:
+        _expect(out, "out", (M, N), out_dtype)
+    _on_device(a, (("a_scale", a_scale), ("b", b), ("b_scale", b_scale), ("out", out)))
+    c = torch.empty((M, N), dtype=out_dtype, device=a.device) if out is None else out
+    _no_alias((("out", c),), (("a", a), ("a_scale", a_scale), ("b", b), ("b_scale", b_scale)))
+    _check(library().mw_scaled_matmul(_ptr(a), _ptr(a_scale), int(a_tiles), int(bool(a_transposed)), _ptr(b),
+                                   _ptr(b_scale), int(b_tiles), int(bool(b_transposed)), _ptr(c), M, N, K,
+                                   _NORM_TYPES[out_dtype], _stream()))
+    return c
+
+
 def mw_device_status(clear: bool = True) -> int:
     """Synchronises the current stream and returns the device status code."""
     return int(library().mw_device_status(_stream(), 1 if clear else 0))
@@ -840,3 +1065,104 @@ class LayerNorm(torch.autograd.Function):
             "LayerNorm",
             lambda x, weight, dy: mw_layernorm_bwd(dy.contiguous(), x, mean, rstd, weight, bias), x, weight, dy)
         return (*grads, None, None)
+
+
+class RMSNorm(torch.autograd.Function):
+    """Autograd wrapper: y = RMS norm(x) * weight, weight [C], one for every group of rows
+    ([groups, C]), or None; with a residual (y, h) of h = x + residual, through both of which
+    gradients come back.  A second derivative is refused."""
+
+    @classmethod
+    def apply(cls, x, weight: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None,
+              eps: float = 1e-5, out_dtype: Optional[torch.dtype] = None):
+        if hasattr(_native, "rms_apply"):
+            r = _native.rms_apply(x, weight, residual, eps, out_dtype)
+            if r is not None:
+                return _check(r) if type(r) is int else r
+        return super().apply(x, weight, residual, eps, out_dtype)
+
+    @staticmethod
+    def forward(ctx, x, weight: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None,
+                eps: float = 1e-5, out_dtype: Optional[torch.dtype] = None):
+        y, h, rstd = mw_rmsnorm_fwd(x, weight, residual, eps, out_dtype)
+        ctx.set_materialize_grads(False)
+        ctx.save_for_backward(x if h is None else h, weight, rstd)
+        ctx.residual, ctx.y_type = residual is not None, y.dtype
+        return y if h is None else (y, h)
+
+    @staticmethod
+    def backward(ctx, dy, dh=None):
+        h, weight, rstd = ctx.saved_tensors
+        if dy is None:  # only h was used
+            if dh is None:
+                return None, None, None, None, None
+            return dh, None, dh, None, None
+
+        def gradients(h, weight, dy, dh):
+            return mw_rmsnorm_bwd(dy.contiguous(), h, rstd, weight, None if dh is None else dh.contiguous())
+
+        dx, dw = _first_derivatives("RMSNorm", gradients, h, weight, dy, dh)
+        return dx, dw, dx if ctx.residual else None, None, None
+
+
+class Fp8Linear(torch.autograd.Function):
+    """Autograd wrapper: y = x W^T for x [..., K] (bf16 or fp32) and weight [N, K] (bf16 or
+    fp32), its three products in 8 bits, in the form of mw_quantize: x and dy in blocks
+    along what is summed (a row for y and dx, a column for dW), W in blocks of (128, 128).  y
+    has ``out_dtype`` (None: x's); gradients have their inputs' types.  K and N are multiples
+    of 16.  A second derivative is refused."""
+
+    @classmethod
+    def apply(cls, x, weight, out_dtype: Optional[torch.dtype] = None):
+        if hasattr(_native, "linear_apply"):
+            r = _native.linear_apply(x, weight, out_dtype)
+            if r is not None:
+                return _check(r) if type(r) is int else r
+        return super().apply(x, weight, out_dtype)
+
+    @staticmethod
+    def forward(ctx, x, weight, out_dtype: Optional[torch.dtype] = None):
+        _norm_type(x, "x")
+        _norm_type(weight, "weight")
+        if weight.dim() != 2 or x.dim() < 1 or x.shape[-1] != weight.shape[1]:
+            raise ValueError(f"x must be [..., K] and weight [N, K], got {tuple(x.shape)} and {tuple(weight.shape)}")
+        if weight.shape[0] % 16 or weight.shape[1] % 16 or 0 in weight.shape:
+            raise ValueError(f"weight is {tuple(weight.shape)}: N and K must be multiples of 16 above 0")
+        x, weight = x.contiguous(), weight.contiguous()
+        wq, ws = mw_quantize(weight, (128, 128))
+        xc = xcs = None
+        if ctx.needs_input_grad[1]:
+            xq, xs, xc, xcs = mw_quantize_both(x)
+        else:
+            xq, xs = mw_quantize(x)
+        y = mw_scaled_matmul(xq.view(-1, x.shape[-1]), xs, wq, ws, x.dtype if out_dtype is None else out_dtype)
+        ctx.save_for_backward(xc, xcs, wq, ws)
+        ctx.types, ctx.shape = (x.dtype, weight.dtype), x.shape
+        return y.view(*x.shape[:-1], weight.shape[0])
+
+    @staticmethod
+    def backward(ctx, dy):
+        xc, xcs, wq, ws = ctx.saved_tensors
+        need_x, need_w = ctx.needs_input_grad[:2]
+        K = ctx.shape[-1]
+
+        def gradients(dy):
+            g = dy.contiguous().view(-1, wq.shape[0])
+            gq = gs = gc = gcs = None
+            if need_x and need_w:
+                gq, gs, gc, gcs = mw_quantize_both(g)
+            elif need_x:
+                gq, gs = mw_quantize(g)
+            elif need_w:
+                gc, gcs = mw_quantize(g, (128, 1))
+            dx = dw = None
+            if need_x:
+                dx = mw_scaled_matmul(gq, gs, wq, ws, ctx.types[0], b_transposed=True).view(ctx.shape)
+            if need_w:
+                dw = mw_scaled_matmul(gc, gcs, xc.view(-1, K), xcs, ctx.types[1], a_transposed=True, b_transposed=True)
+            return dx, dw
+
+        # (what the gradients depend on besides is saved in 8 bits, without its graph: any
+        # input that wants a gradient stands for it)
+        stand_in = torch.empty(0, requires_grad=True) if torch.is_grad_enabled() else None
+        return (*_first_derivatives("Fp8Linear", lambda dy, _: gradients(dy), dy, stand_in), None)

@@ -126,42 +126,9 @@ XattnBwdWs xattn_bwd_ws(const XattnSizes& z, int S, int d) {
   return w;
 }
 
-mw_status check_f32(const void* p, const char* name) {
-  if (reinterpret_cast<uintptr_t>(p) & 3u)
-    return fail(MW_ERR_INVALID_ARG, "%s is not 4-byte aligned", name);
-  return MW_OK;
-}
-
 mw_status check_scale(float scale) {
   if (!(scale > 0.f) || !std::isfinite(scale))
     return fail(MW_ERR_INVALID_ARG, "scale must be > 0 and finite");
-  return MW_OK;
-}
-
-bool dtype_ok(int t) { return t == MW_BF16 || t == MW_F32; }
-
-mw_status norm_sizes(long long rows, int C, int groups, float eps) {
-  if (C < 1 || C > kNormMaxC)
-    return fail(MW_ERR_UNSUPPORTED, "C=%d channels (supported: 1 to %d)", C, kNormMaxC);
-  if (rows < 0 || rows > INT_MAX)
-    return fail(MW_ERR_INVALID_ARG, "rows=%lld out of range [0, 2^31)", rows);
-  if (groups < 1 || groups > (1 << 24) || rows % groups != 0)
-    return fail(MW_ERR_INVALID_ARG, "rows=%lld is not a multiple of groups=%d", rows, groups);
-  if (!(eps >= 0.f) || !std::isfinite(eps))
-    return fail(MW_ERR_INVALID_ARG, "eps must be >= 0 and finite");
-  return MW_OK;
-}
-
-// Every row of every array can be read and written 16 bytes at a time.
-template <class... P>
-bool vector_rows(int C, P... ptrs) {
-  return C % 8 == 0 && (aligned16(ptrs) && ...);
-}
-
-mw_status check_elems(const void* p, int dtype, const char* name) {
-  if (p == nullptr) return fail(MW_ERR_INVALID_ARG, "%s is NULL", name);
-  if (reinterpret_cast<uintptr_t>(p) & (dtype == MW_F32 ? 3u : 1u))
-    return fail(MW_ERR_INVALID_ARG, "%s is not aligned to its elements", name);
   return MW_OK;
 }
 

@@ -4,7 +4,11 @@
 
 #include <cuda.h>
 #include <cuda_runtime.h>
+#include <limits.h>
+#include <math.h>
 #include <stddef.h>
+
+#include <cmath>
 
 #include "mw_bca.h"
 #include "mw_internal.h"
@@ -43,6 +47,10 @@ mw_status encode_bias_map(CUtensorMap* m, const float* bias, int N_pad, int BH, 
 // Map over bf16 rows [BH, rows, d] in boxes of 32 rows: x 64 columns with the 128-byte
 // swizzle, or x 32 without.
 mw_status encode_rows_map(CUtensorMap* m, void* ptr, int rows, int BH, int d, bool swizzle);
+// 2-D map over rows of `cols` elements (1, 2 or 4 bytes: codes, bf16, fp32) at a pitch of
+// as many, in boxes of 128 bytes x box_rows with the 128-byte swizzle; from the cache.
+mw_status make_map_2d(CUtensorMap* m, const void* ptr, long long rows, long long cols, int elem, int box_rows,
+                      const char* name);
 
 // The device status word of the current device `dev`.
 mw_status status_ptr(int dev, unsigned** out);
@@ -88,6 +96,39 @@ class DeviceScope {
   int prev_ = -1, dev_ = 0;
   cudaError_t err_ = cudaSuccess;
 };
+
+inline mw_status check_f32(const void* p, const char* name) {
+  if (reinterpret_cast<uintptr_t>(p) & 3u)
+    return fail(MW_ERR_INVALID_ARG, "%s is not 4-byte aligned", name);
+  return MW_OK;
+}
+
+inline bool dtype_ok(int t) { return t == MW_BF16 || t == MW_F32; }
+
+inline mw_status norm_sizes(long long rows, int C, int groups, float eps) {
+  if (C < 1 || C > kNormMaxC)
+    return fail(MW_ERR_UNSUPPORTED, "C=%d channels (supported: 1 to %d)", C, kNormMaxC);
+  if (rows < 0 || rows > INT_MAX)
+    return fail(MW_ERR_INVALID_ARG, "rows=%lld out of range [0, 2^31)", rows);
+  if (groups < 1 || groups > (1 << 24) || rows % groups != 0)
+    return fail(MW_ERR_INVALID_ARG, "rows=%lld is not a multiple of groups=%d", rows, groups);
+  if (!(eps >= 0.f) || !std::isfinite(eps))
+    return fail(MW_ERR_INVALID_ARG, "eps must be >= 0 and finite");
+  return MW_OK;
+}
+
+// Every row of every array can be read and written 16 bytes at a time.
+template <class... P>
+bool vector_rows(int C, P... ptrs) {
+  return C % 8 == 0 && (aligned16(ptrs) && ...);
+}
+
+inline mw_status check_elems(const void* p, int dtype, const char* name) {
+  if (p == nullptr) return fail(MW_ERR_INVALID_ARG, "%s is NULL", name);
+  if (reinterpret_cast<uintptr_t>(p) & (dtype == MW_F32 ? 3u : 1u))
+    return fail(MW_ERR_INVALID_ARG, "%s is not aligned to its elements", name);
+  return MW_OK;
+}
 
 inline mw_status launch_status(cudaError_t e, const char* what) {
   if (e != cudaSuccess) return fail(MW_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));

@@ -221,6 +221,34 @@ int norm_parts(long long rows_per_group, int C, int groups);
 cudaError_t launch_norm_fwd(NormParams p, bool vec, int sms, cudaStream_t s);
 cudaError_t launch_norm_bwd(NormParams p, bool vec, int dev, cudaStream_t s);
 
+// RMS norm (mw_rms.cu).
+enum { kRmsBf16 = 0, kRmsF32 = 1, kRmsCodes = 2 };  // y
+struct RmsParams {
+  const void* x;         // [rows, C], bf16 or fp32
+  const void* residual;  // x's type, nullable
+  const void* weight;    // [groups, C] or null (all 1)
+  void* y;               // forward: [rows, C]
+  uint8_t* y_scale;      // [rows, ceil(C / 128)] with codes
+  void* h;               // x's type: the sum (forward: with a residual), the backward's rows
+  float* rstd;           // [rows]; forward: nullable
+  const void* dy;        // backward: y's type
+  const void* dh;        // x's type, nullable
+  void* dx;
+  void* dweight;         // the weight's type, nullable
+  float* partial;        // [groups * parts, C] where parts > 1
+  long long rows, rows_per_group;
+  int C, groups;
+  int parts;             // backward: blocks that share a group's rows
+  int W;                 // warps that share a row (set by the launcher)
+  float eps;
+  int y_type;
+  bool x_f32, param_f32;
+};
+int rms_parts(long long rows_per_group, int C, int groups);
+// vec: C is a multiple of 8 and every pointer 16-byte aligned
+cudaError_t launch_rms_fwd(RmsParams p, bool vec, int sms, cudaStream_t s);
+cudaError_t launch_rms_bwd(RmsParams p, bool vec, int dev, cudaStream_t s);
+
 // Cross attention: BH heads of K and V [BH, S, d], each with M rows of Q (those of all
 // the query heads that share it, which lie one after another); head bh belongs to
 // sample bh / heads, whose first kv_len[...] keys count (null: all S).
@@ -309,5 +337,50 @@ struct XattnBwdMaps {
 };
 cudaError_t launch_xattn_bwd(int d, int dm, const XattnBwdMaps& m, const XattnBwdParams& p, int dev, int sms,
                              cudaStream_t s);
+
+// Matrices in 8 bits (e4m3) with a scale (e8m0) for every block of 128: of a row's
+// elements (rows), of a column's (columns), or of both (tiles).
+constexpr int kFp8Block = 128;
+struct Fp8FormParams {
+  const void* x;         // [rows, C], bf16 or fp32
+  uint8_t* q;            // rows or tiles: [rows, C]
+  uint8_t* scale;        // [rows, ceil(C / 128)], tiles [ceil(rows / 128), ceil(C / 128)]
+  uint8_t* q_columns;    // columns: [rows, C]
+  uint8_t* scale_columns;  // [ceil(rows / 128), C]
+  long long rows;
+  int C;
+  bool x_f32;
+};
+enum class Fp8Form { kRows, kColumns, kTiles, kBoth };
+cudaError_t launch_fp8_form(const Fp8FormParams& p, Fp8Form form, cudaStream_t s);
+
+// Product of two of them (mw_fp8_mm.cu): rows_a x rows_b results over `blocks` of the contraction.
+struct Fp8Scales {
+  const uint8_t* p;
+  long long row, block;  // bytes from a row, and from a block of the contraction, to the next
+  bool tile;             // one for 128 rows
+  bool words;            // blocks lie together, rows at multiples of four bytes
+};
+struct Fp8MmParams {
+  Fp8Scales a_scales, b_scales;
+  void* out;             // bf16 or fp32, rows of ld
+  long long ld;
+  int rows_a, rows_b, blocks;
+  int tiles_p, tiles_q;  // of 128 rows of A, of bn rows of B
+  int splits;            // join: CTAs of a tile
+  int ctas;              // else: CTAs at most
+  bool a_columns, b_columns;  // rows of the operand lie across the contraction
+  bool swap;             // join: a row of the output is one of B
+  bool out_f32;
+  bool out_quads;        // groups of four elements from any multiple of four on are aligned
+  bool tma_out;          // tc is a map of the output
+  unsigned* status;
+  unsigned long long budget_ns;
+  int debug_skip_q;      // test hook: never load A and B
+};
+// bn: rows of B of a tile (join: 16, 32, 64 or 128; else 128 or 256); ta, tb: boxes of 128
+// bytes x 128 rows (tb: x bn rows where B runs along the contraction); tc: 32 rows x 128 bytes
+cudaError_t launch_fp8_mm(int bn, bool join, const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap& tc,
+                          const Fp8MmParams& p, int dev, cudaStream_t s);
 
 }  // namespace mw

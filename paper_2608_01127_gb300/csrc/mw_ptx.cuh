@@ -146,6 +146,23 @@ __device__ __forceinline__ void tma_prefetch_3d(const CUtensorMap* map, int c0, 
                : "memory");
 }
 
+// 2-D tiled load and store, as the 3-D ones.
+__device__ __forceinline__ void tma_load_2d(void* dst, const CUtensorMap* map, uint64_t* bar,
+                                            int c0, int c1) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%3, %4}], [%2];" ::"r"(smem_u32(dst)),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(bar)), "r"(c0), "r"(c1)
+      : "memory");
+}
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, const void* src, int c0, int c1) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];" ::"l"(
+          reinterpret_cast<uint64_t>(map)),
+      "r"(smem_u32(src)), "r"(c0), "r"(c1)
+      : "memory");
+}
+
 // 3-D tiled reduce-add of a shared-memory box into global memory (element
 // type and box from the map; here f32), tracked as a bulk async-group of the
 // issuing thread.  Coordinates must not be negative; c0 * element size must be
@@ -344,6 +361,56 @@ __device__ __forceinline__ void umma_ts4(uint32_t d_tmem, uint32_t a_tmem, uint3
       : "memory");
 }
 
+// Four MMAs D (+)= A B^T of 8-bit operands (kind::mxf8f6f4: e4m3, a power-of-two scale
+// for 32 of the contraction, K = 32 per instruction), descriptors a_step and b_step
+// (16 bytes) further each time; all of them take the same byte of the scale words in
+// tensor memory at sfa and sfb (chosen by idesc).
+__device__ __forceinline__ void umma_mx4(uint32_t d_tmem, uint32_t a_desc, uint32_t b_desc, uint32_t a_step,
+                                         uint32_t b_step, uint32_t idesc, uint32_t sfa, uint32_t sfb,
+                                         uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, e;\n\t.reg .b32 a1, a2, a3, b1, b2, b3;\n\t.reg .b64 da, db;\n\t"
+      "elect.sync _|e, 0xffffffff;\n\t"
+      "@!e bra OTHERS;\n\t"
+      "add.u32 a1, %1, %3;\n\t"
+      "add.u32 b1, %2, %4;\n\t"
+      "add.u32 a2, a1, %3;\n\t"
+      "add.u32 b2, b1, %4;\n\t"
+      "add.u32 a3, a2, %3;\n\t"
+      "add.u32 b3, b2, %4;\n\t"
+      "setp.ne.b32 p, %8, 0;\n\t"
+      "mov.b64 da, {%1, %9};\n\t"
+      "mov.b64 db, {%2, %9};\n\t"
+      "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], da, db, %5, [%6], [%7], p;\n\t"
+      "setp.eq.b32 p, %8, %8;\n\t"
+      "mov.b64 da, {a1, %9};\n\t"
+      "mov.b64 db, {b1, %9};\n\t"
+      "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], da, db, %5, [%6], [%7], p;\n\t"
+      "mov.b64 da, {a2, %9};\n\t"
+      "mov.b64 db, {b2, %9};\n\t"
+      "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], da, db, %5, [%6], [%7], p;\n\t"
+      "mov.b64 da, {a3, %9};\n\t"
+      "mov.b64 db, {b3, %9};\n\t"
+      "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], da, db, %5, [%6], [%7], p;\n"
+      "OTHERS:\n\t}\n" ::"r"(d_tmem),
+      "r"(a_desc), "r"(b_desc), "r"(a_step), "r"(b_step), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate),
+      "n"(kSw128Hi)
+      : "memory");
+}
+
+// 512 bytes of scale words from shared memory into four columns of tensor memory, the same
+// in each quarter of its lanes: lane l of a quarter gets the 16 bytes 16 l ...  Ordered
+// before the MMAs that the same thread issues after it.
+__device__ __forceinline__ void tmem_copy_scales(uint32_t d_tmem, uint32_t saddr) {
+  asm volatile(
+      "{\n\t.reg .pred e;\n\t.reg .b64 d;\n\t"
+      "elect.sync _|e, 0xffffffff;\n\t"
+      "mov.b64 d, {%1, %2};\n\t"
+      "@e tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], d;\n\t}\n" ::"r"(d_tmem),
+      "r"((saddr & 0x3FFFFu) >> 4), "n"((128u >> 4) | (1u << 14))  // 8 rows of 16 bytes: SBO 128; no swizzle
+      : "memory");
+}
+
 // Arrive (once) on `bar` when every tcgen05 op issued so far by the elected
 // lane has completed.
 __device__ __forceinline__ void umma_commit(uint64_t* bar) {
@@ -487,6 +554,15 @@ __host__ __device__ constexpr uint32_t idesc_bf16_f32(int M, int N, bool a_mn_ma
          ((b_mn_major ? 1u : 0u) << 16) | (static_cast<uint32_t>(N >> 3) << 17) |
          (static_cast<uint32_t>(M >> 4) << 24);
 }
+
+// Instruction descriptor for kind::mxf8f6f4: A and B e4m3 (0 in bits 7-9 and 10-12), the
+// majors in 15 and 16 as above, N >> 3 in 17-22, scales e8m0 (bit 23), M >> 7 in 27-28; the
+// byte of the scale words to take in bits 4-5 (B) and 29-30 (A).
+__host__ __device__ constexpr uint32_t idesc_mxf8(int M, int N, bool a_mn_major, bool b_mn_major) {
+  return ((a_mn_major ? 1u : 0u) << 15) | ((b_mn_major ? 1u : 0u) << 16) | (static_cast<uint32_t>(N >> 3) << 17) |
+         (1u << 23) | (static_cast<uint32_t>(M >> 7) << 27);
+}
+__host__ __device__ constexpr uint32_t idesc_scale_byte(uint32_t byte) { return (byte << 4) | (byte << 29); }
 
 // ------------------------------------------------------------------ math
 
