@@ -185,7 +185,8 @@ def _load_native(lib: ctypes.CDLL) -> None:
         "mw_bca_cache_fwd_rope", "mw_bca_cache_step", "mw_qkv_rope_split",
         "mw_xattn_workspace_size", "mw_xattn_fwd", "mw_xattn_bwd_workspace_size", "mw_xattn_bwd",
         "mw_layernorm_fwd", "mw_layernorm_bwd_workspace_size", "mw_layernorm_bwd",
-        "mw_last_error")), MWError)
+        "mw_rmsnorm_fwd", "mw_rmsnorm_bwd_workspace_size", "mw_rmsnorm_bwd", "mw_quantize",
+        "mw_scaled_matmul", "mw_last_error")), MWError)
     _native = module
 
 
@@ -742,7 +743,7 @@ def mw_rmsnorm_fwd(x: torch.Tensor, weight: Optional[torch.Tensor] = None,
     ``weight``: [C], or [groups, C] with one for every one of ``groups`` equal runs of
     consecutive rows (samples, frames), or None.  y has ``out_dtype`` (None: x's; fp32 only
     with x in fp32)."""
-    if out is None and hasattr(_native, "rms_fwd"):
+    if out is None and _native is not None:
         r = _native.rms_fwd(x, weight, residual, eps, out_dtype, need_stats)
         if r is not None:
             return r if type(r) is tuple else _check(r)
@@ -767,8 +768,8 @@ def mw_rmsnorm_quantize(x: torch.Tensor, weight: Optional[torch.Tensor] = None,
     """mw_rmsnorm_fwd with y as the product reads it: (q, scale, h, rstd) with y's 8-bit form
     in blocks of (1, 128), as mw_quantize gives it (y itself is not rounded before).  C
     must be a multiple of 16."""
-    if hasattr(_native, "rms_fp8"):
-        r = _native.rms_fp8(x, weight, residual, eps, need_stats)
+    if _native is not None:
+        r = _native.rms_quantize(x, weight, residual, eps, need_stats)
         if r is not None:
             return r if type(r) is tuple else _check(r)
     xt, rows, C, groups, ptype = _rms_inputs(x, weight, residual)
@@ -792,7 +793,7 @@ def mw_rmsnorm_bwd(dy, h, rstd, weight: Optional[torch.Tensor] = None, dh: Optio
     """Gradients (dx, dweight) of sum(y * dy) + sum(h * dh) through mw_rmsnorm_fwd, from its
     h (x where there was no residual) and rstd: dx is the gradient of x and of the residual
     alike; dweight None without a weight."""
-    if workspace is None and hasattr(_native, "rms_bwd"):
+    if workspace is None and _native is not None:
         r = _native.rms_bwd(dy, h, rstd, weight, dh)
         if r is not None:
             return r if type(r) is tuple else _check(r)
@@ -841,8 +842,8 @@ def mw_quantize(x: torch.Tensor, block: Tuple[int, int] = (1, 128), out=None
     or an infinity is NaN.  C must be a multiple of 16.
 
     ``out`` = (q, scale) reuses caller buffers."""
-    if out is None and hasattr(_native, 'fp8_form'):
-        r = _native.fp8_form(x, block)
+    if out is None and _native is not None:
+        r = _native.quantize(x, block)
         if r is not None:
             return r if type(r) is tuple else _check(r)
     xt, rows, C = _fp8_source(x)
@@ -868,8 +869,8 @@ def mw_quantize(x: torch.Tensor, block: Tuple[int, int] = (1, 128), out=None
 def mw_quantize_both(x: torch.Tensor):
     """mw_quantize with blocks of (1, 128) and of (128, 1) elements, x read once:
     (q, scale, q_columns, scale_columns)."""
-    if hasattr(_native, 'fp8_form'):
-        r = _native.fp8_form(x, None)
+    if _native is not None:
+        r = _native.quantize(x, None)
         if r is not None:
             return r if type(r) is tuple else _check(r)
     xt, rows, C = _fp8_source(x)
@@ -911,8 +912,8 @@ def mw_scaled_matmul(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_
     ceil(K/128)] (of (128, 128)); with ``a_transposed`` codes [K, M] with scales
     [ceil(K/128), M] (blocks of (128, 1)) or [ceil(K/128), ceil(M/128)].  b: the same with
     N in the place of M.  ``out`` reuses a caller's buffer."""
-    if out is None and hasattr(_native, 'fp8_form'):
-        r = _native.fp8_matmul(a, a_scale, b, b_scale, out_dtype, a_transposed, b_transposed)
+    if out is None and _native is not None:
+        r = _native.scaled_matmul(a, a_scale, b, b_scale, out_dtype, a_transposed, b_transposed)
         if r is not None:
             return _check(r) if type(r) is int else r
     M, K, a_tiles = _fp8_operand(a, a_scale, "a", a_transposed)
@@ -1075,7 +1076,7 @@ class RMSNorm(torch.autograd.Function):
     @classmethod
     def apply(cls, x, weight: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None,
               eps: float = 1e-5, out_dtype: Optional[torch.dtype] = None):
-        if hasattr(_native, "rms_apply"):
+        if _native is not None:
             r = _native.rms_apply(x, weight, residual, eps, out_dtype)
             if r is not None:
                 return _check(r) if type(r) is int else r
@@ -1114,7 +1115,7 @@ class Fp8Linear(torch.autograd.Function):
 
     @classmethod
     def apply(cls, x, weight, out_dtype: Optional[torch.dtype] = None):
-        if hasattr(_native, "linear_apply"):
+        if _native is not None:
             r = _native.linear_apply(x, weight, out_dtype)
             if r is not None:
                 return _check(r) if type(r) is int else r

@@ -53,6 +53,11 @@ decltype(&mw_xattn_bwd) p_xattn_bwd = nullptr;
 decltype(&mw_layernorm_fwd) p_norm = nullptr;
 decltype(&mw_layernorm_bwd_workspace_size) p_norm_bwd_ws = nullptr;
 decltype(&mw_layernorm_bwd) p_norm_bwd = nullptr;
+decltype(&mw_rmsnorm_fwd) p_rms = nullptr;
+decltype(&mw_rmsnorm_bwd_workspace_size) p_rms_bwd_ws = nullptr;
+decltype(&mw_rmsnorm_bwd) p_rms_bwd = nullptr;
+decltype(&mw_quantize) p_quantize = nullptr;
+decltype(&mw_scaled_matmul) p_matmul = nullptr;
 decltype(&mw_last_error) p_last_error = nullptr;
 PyObject* error_type = nullptr;  // MWError(code, message)
 
@@ -190,9 +195,9 @@ auto call(F&& f) {
 }
 
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  constexpr int kEntries = 15;
+  constexpr int kEntries = 20;
   if (n != kEntries + 1) {
-    PyErr_SetString(PyExc_TypeError, "bind takes 15 addresses and the error type");
+    PyErr_SetString(PyExc_TypeError, "bind takes 20 addresses and the error type");
     return nullptr;
   }
   void* p[kEntries];
@@ -217,7 +222,12 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
   p_norm = reinterpret_cast<decltype(p_norm)>(p[11]);
   p_norm_bwd_ws = reinterpret_cast<decltype(p_norm_bwd_ws)>(p[12]);
   p_norm_bwd = reinterpret_cast<decltype(p_norm_bwd)>(p[13]);
-  p_last_error = reinterpret_cast<decltype(p_last_error)>(p[14]);
+  p_rms = reinterpret_cast<decltype(p_rms)>(p[14]);
+  p_rms_bwd_ws = reinterpret_cast<decltype(p_rms_bwd_ws)>(p[15]);
+  p_rms_bwd = reinterpret_cast<decltype(p_rms_bwd)>(p[16]);
+  p_quantize = reinterpret_cast<decltype(p_quantize)>(p[17]);
+  p_matmul = reinterpret_cast<decltype(p_matmul)>(p[18]);
+  p_last_error = reinterpret_cast<decltype(p_last_error)>(p[19]);
   Py_XDECREF(error_type);
   error_type = Py_NewRef(a[kEntries]);
   Py_RETURN_NONE;
@@ -676,6 +686,262 @@ PyObject* norm_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// ---- projections in 8 bits
+
+constexpr auto kCodes = at::kFloat8_e4m3fn;
+constexpr auto kScales = at::kFloat8_e8m0fnu;
+int64_t blocks128(int64_t n) { return (n + 127) / 128; }
+
+// An RMS norm call: its tensors and sizes, and the results of its forward.
+struct Rms {
+  const at::Tensor *x = nullptr, *w = nullptr, *r = nullptr;
+  int xt = -1, pt = MW_F32, C = 0, groups = 1;
+  int64_t rows = 0;
+  c10::DeviceIndex dev = -1;
+  at::Tensor y, scale, h, rstd;
+  bool read(PyObject* xo, PyObject* wo, PyObject* ro) {
+    x = tensor(xo);
+    if (!x || x->dim() < 1 || (xt = norm_type(x->scalar_type())) < 0) return false;
+    const int64_t c = x->size(-1);
+    if (c < 1 || c > INT_MAX) return false;
+    C = static_cast<int>(c);
+    rows = x->numel() / c;
+    if (wo != Py_None) {
+      w = tensor(wo);
+      if (!w || (pt = norm_type(w->scalar_type())) < 0 || w->dim() < 1 || w->dim() > 2 || w->size(-1) != c) return false;
+      const int64_t g = w->dim() == 2 ? w->size(0) : 1;
+      if (g < 1 || g > INT_MAX) return false;
+      groups = static_cast<int>(g);
+    }
+    if (ro != Py_None) {
+      r = tensor(ro);
+      if (!r || r->scalar_type() != x->scalar_type() || r->sizes() != x->sizes()) return false;
+    }
+    return rows % groups == 0 && one_device({x, w, r}, &dev);
+  }
+  bool out_type(PyObject* o, int* yt) const {
+    *yt = xt;
+    if (o == Py_None) return true;
+    if (!THPDtype_Check(o)) return false;
+    *yt = norm_type(reinterpret_cast<THPDtype*>(o)->scalar_type);
+    return *yt >= 0;
+  }
+  bool forward(float eps, int yt, bool stats, mw_status* s) {
+    const at::TensorOptions options = x->options();
+    const std::vector<int64_t> full = x->sizes().vec();
+    const at::IntArrayRef lead(full.data(), full.size() - 1);
+    const void *px = x->const_data_ptr(), *pw = w ? w->const_data_ptr() : nullptr;
+    const void* pr = r ? r->const_data_ptr() : nullptr;
+    return call([&] {
+      y = at::empty(full, options.dtype(yt == MW_E4M3 ? kCodes : torch_type(yt)));
+      if (yt == MW_E4M3) scale = at::empty({rows, blocks128(C)}, options.dtype(kScales));
+      if (r) h = at::empty(full, options);
+      if (stats) rstd = at::empty(lead, options.dtype(at::kFloat));
+      for (const at::Tensor* t : {&y, &scale, &h, &rstd})
+        if (t->defined() && !is_real(*t)) return false;
+      *s = p_rms(px, pr, pw, y.mutable_data_ptr(), scale.defined() ? scale.mutable_data_ptr() : nullptr,
+                 r ? h.mutable_data_ptr() : nullptr, stats ? static_cast<float*>(rstd.mutable_data_ptr()) : nullptr,
+                 rows, C, groups, eps, xt, yt, pt, c10::cuda::getCurrentCUDAStream(dev).stream());
+      return true;
+    });
+  }
+};
+
+// rms_fwd(x, weight, residual, eps, out_dtype, need_stats) -> (y, h or None, rstd or None)
+PyObject* rms_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Rms t;
+  float eps;
+  int yt;
+  if (n != 6 || !p_rms || !t.read(a[0], a[1], a[2]) || !real_number(a[3], &eps) || !t.out_type(a[4], &yt) ||
+      !PyBool_Check(a[5]))
+    return none();
+  mw_status s = MW_OK;
+  if (!t.forward(eps, yt, a[5] == Py_True, &s)) return none();
+  if (s != MW_OK) return PyLong_FromLong(s);
+  return result({&t.y, &t.h, &t.rstd});
+  END_HANDLE_TH_ERRORS
+}
+
+// rms_quantize(x, weight, residual, eps, need_stats) -> (q, scale, h or None, rstd or None)
+PyObject* rms_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Rms t;
+  float eps;
+  if (n != 5 || !p_rms || !t.read(a[0], a[1], a[2]) || t.C % 16 || !real_number(a[3], &eps) || !PyBool_Check(a[4]))
+    return none();
+  mw_status s = MW_OK;
+  if (!t.forward(eps, MW_E4M3, a[4] == Py_True, &s)) return none();
+  if (s != MW_OK) return PyLong_FromLong(s);
+  return result({&t.y, &t.scale, &t.h, &t.rstd});
+  END_HANDLE_TH_ERRORS
+}
+
+// The gradients of an RMS norm into new tensors (of x, and of the weight where there is a
+// shape for it); false: not real ones.  Called without the interpreter lock.
+struct RmsSizes {
+  int64_t rows;
+  int C, groups, xt, yt, pt;
+  bool w;
+  std::vector<int64_t> params;  // shape of the weight
+};
+bool rms_gradients(const at::Tensor& dy, const at::Tensor& h, const at::Tensor& rstd, const void* weight,
+                   const at::Tensor* dh, const RmsSizes& z, c10::DeviceIndex dev, std::array<at::Tensor, 2>* grads,
+                   mw_status* s) {
+  const size_t bytes = z.w ? p_rms_bwd_ws(z.rows, z.C, z.groups) : 0;
+  const at::TensorOptions options = h.options();
+  at::Tensor ws;
+  if (bytes) ws = scratch(bytes, options);
+  (*grads)[0] = at::empty(h.sizes(), options);
+  if (z.w) (*grads)[1] = at::empty(z.params, options.dtype(torch_type(z.pt)));
+  if (bytes && !is_real(ws)) return false;
+  for (const at::Tensor& t : *grads)
+    if (t.defined() && !is_real(t)) return false;
+  *s = p_rms_bwd(dy.const_data_ptr(), h.const_data_ptr(), static_cast<const float*>(rstd.const_data_ptr()), weight,
+                 dh ? dh->const_data_ptr() : nullptr, (*grads)[0].mutable_data_ptr(),
+                 z.w ? (*grads)[1].mutable_data_ptr() : nullptr, bytes ? ws.mutable_data_ptr() : nullptr, bytes,
+                 z.rows, z.C, z.groups, z.xt, z.yt, z.pt, c10::cuda::getCurrentCUDAStream(dev).stream());
+  return true;
+}
+
+RmsSizes rms_sizes(const Rms& t, int yt) {
+  return {t.rows, t.C, t.groups, t.xt, yt, t.pt, t.w != nullptr, t.w ? t.w->sizes().vec() : std::vector<int64_t>()};
+}
+
+// rms_bwd(dy, h, rstd, weight, dh) -> (dx, dweight or None)
+PyObject* rms_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 5 || !p_rms_bwd) return none();
+  Rms t;
+  const at::Tensor *dy = tensor(a[0]), *rstd = tensor(a[2]);
+  c10::DeviceIndex dev;
+  if (!t.read(a[1], a[3], a[4]) || !dy || !rstd || dy->sizes() != t.x->sizes() ||
+      !one_device({t.x, dy, rstd}, &dev))
+    return none();
+  const int yt = norm_type(dy->scalar_type());
+  if (yt < 0 || rstd->scalar_type() != at::kFloat || rstd->sizes() != t.x->sizes().slice(0, t.x->dim() - 1))
+    return none();
+  const RmsSizes z = rms_sizes(t, yt);
+  const void* pw = t.w ? t.w->const_data_ptr() : nullptr;
+  std::array<at::Tensor, 2> g;
+  mw_status s = MW_OK;
+  if (!call([&] { return rms_gradients(*dy, *t.x, *rstd, pw, t.r, z, dev, &g, &s); })) return none();
+  if (s != MW_OK) return PyLong_FromLong(s);
+  return result({&g[0], &g[1]});
+  END_HANDLE_TH_ERRORS
+}
+
+// The 8-bit form of a matrix of `rows` rows: codes and scales of its form, and of its
+// columns where form is MW_FP8_ROWS_AND_COLUMNS.
+struct Form {
+  at::Tensor q, scale, qc, sc;
+};
+// Into new tensors; false: not real ones.  Called without the interpreter lock.
+bool make_form(const at::Tensor& x, int64_t rows, int form, int xt, c10::DeviceIndex dev, Form* f, mw_status* s) {
+  const at::TensorOptions codes = x.options().dtype(kCodes), scales = x.options().dtype(kScales);
+  const int64_t C = x.size(-1);
+  const bool r = form != MW_FP8_COLUMNS, c = form == MW_FP8_COLUMNS || form == MW_FP8_ROWS_AND_COLUMNS;
+  if (r) {
+    f->q = at::empty(x.sizes(), codes);
+    f->scale = at::empty({form == MW_FP8_TILES ? blocks128(rows) : rows, blocks128(C)}, scales);
+  }
+  if (c) {
+    f->qc = at::empty(x.sizes(), codes);
+    f->sc = at::empty({blocks128(rows), C}, scales);
+  }
+  for (const at::Tensor* t : {&f->q, &f->scale, &f->qc, &f->sc})
+    if (t->defined() && !is_real(*t)) return false;
+  auto at = [](at::Tensor& t) { return t.defined() ? t.mutable_data_ptr() : nullptr; };
+  *s = p_quantize(x.const_data_ptr(), at(f->q), at(f->scale), at(f->qc), at(f->sc), rows, static_cast<int>(C), form, xt,
+                  c10::cuda::getCurrentCUDAStream(dev).stream());
+  return true;
+}
+
+// quantize(x, block or None) -> (q, scale), or the forms of rows and of columns
+PyObject* quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 2 || !p_quantize) return none();
+  int form = MW_FP8_ROWS_AND_COLUMNS;
+  if (a[1] != Py_None) {
+    int r, c;
+    if (!PyTuple_CheckExact(a[1]) || PyTuple_GET_SIZE(a[1]) != 2 || !small_int(PyTuple_GET_ITEM(a[1], 0), &r) ||
+        !small_int(PyTuple_GET_ITEM(a[1], 1), &c))
+      return none();
+    if (r == 1 && c == 128)
+      form = MW_FP8_ROWS;
+    else if (r == 128 && c == 1)
+      form = MW_FP8_COLUMNS;
+    else if (r == 128 && c == 128)
+      form = MW_FP8_TILES;
+    else
+      return none();
+  }
+  const at::Tensor* x = tensor(a[0]);
+  c10::DeviceIndex dev;
+  if (!x || x->dim() < 1 || !one_device({x}, &dev)) return none();
+  const int xt = norm_type(x->scalar_type());
+  const int64_t C = x->size(-1);
+  if (xt < 0 || C < 16 || C % 16 || C > INT_MAX) return none();
+  Form f;
+  mw_status s = MW_OK;
+  if (!call([&] { return make_form(*x, x->numel() / C, form, xt, dev, &f, &s); })) return none();
+  if (s != MW_OK) return PyLong_FromLong(s);
+  if (form == MW_FP8_ROWS_AND_COLUMNS) return result({&f.q, &f.scale, &f.qc, &f.sc});
+  return form == MW_FP8_COLUMNS ? result({&f.qc, &f.sc}) : result({&f.q, &f.scale});
+  END_HANDLE_TH_ERRORS
+}
+
+// An operand of a product: codes [rows, K], or [K, rows] where transposed.
+struct Operand {
+  const at::Tensor *q = nullptr, *scale = nullptr;
+  bool transposed = false, tiles = false;
+  int64_t rows = 0, K = 0;
+  bool read(PyObject* qo, PyObject* so, PyObject* to) {
+    q = tensor(qo);
+    scale = tensor(so);
+    if (!PyBool_Check(to) || !q || !scale || q->scalar_type() != kCodes || scale->scalar_type() != kScales ||
+        q->dim() != 2 || scale->dim() != 2 || q->size(1) % 16 || q->size(0) > INT_MAX || q->size(1) > INT_MAX)
+      return false;
+    transposed = to == Py_True;
+    rows = q->size(transposed ? 1 : 0);
+    K = q->size(transposed ? 0 : 1);
+    const int64_t along = scale->size(transposed ? 0 : 1), across = scale->size(transposed ? 1 : 0);
+    if (along != blocks128(K)) return false;
+    tiles = across != rows;
+    return !tiles || across == blocks128(rows);
+  }
+};
+
+// scaled_matmul(a, a_scale, b, b_scale, out_dtype, a_transposed, b_transposed) -> c
+PyObject* scaled_matmul(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 7 || !p_matmul) return none();
+  Operand l, r;
+  c10::DeviceIndex dev;
+  if (!l.read(a[0], a[1], a[5]) || !r.read(a[2], a[3], a[6]) || l.K != r.K || !THPDtype_Check(a[4]) ||
+      !one_device({l.q, l.scale, r.q, r.scale}, &dev))
+    return none();
+  const int ct = norm_type(reinterpret_cast<THPDtype*>(a[4])->scalar_type);
+  if (ct < 0) return none();
+  const at::TensorOptions options = l.q->options().dtype(torch_type(ct));
+  const void *pa = l.q->const_data_ptr(), *psa = l.scale->const_data_ptr();
+  const void *pb = r.q->const_data_ptr(), *psb = r.scale->const_data_ptr();
+  at::Tensor c;
+  mw_status s = MW_OK;
+  const bool real = call([&] {
+    c = at::empty({l.rows, r.rows}, options);
+    if (!is_real(c)) return false;
+    s = p_matmul(pa, psa, l.tiles, l.transposed, pb, psb, r.tiles, r.transposed, c.mutable_data_ptr(),
+                 static_cast<int>(l.rows), static_cast<int>(r.rows), static_cast<int>(l.K), ct,
+                 c10::cuda::getCurrentCUDAStream(dev).stream());
+    return true;
+  });
+  if (!real) return none();
+  if (s != MW_OK) return PyLong_FromLong(s);
+  return THPVariable_Wrap(c);
+  END_HANDLE_TH_ERRORS
+}
+
 // ---- the same with gradients: nodes of PyTorch's graph, whose backward pass runs
 // without the interpreter (a Python function's takes 60 us on the autograd thread,
 // more than the kernels of many layers).
@@ -887,6 +1153,238 @@ PyObject* norm_apply(PyObject*, PyObject* const* a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+struct RMSNormBackward : public torch::autograd::Node {
+  SavedVariable rows, weight, rstd;  // rows: h, or x where there was no residual
+  RmsSizes z{};
+  std::vector<int64_t> sizes;  // of x
+  bool residual = false;
+  c10::DeviceIndex dev = 0;
+
+  std::string name() const override { return "RMSNormBackward"; }
+  void release_variables() override {
+    for (SavedVariable* s : {&rows, &weight, &rstd}) s->reset_data();
+  }
+  variable_list apply(variable_list&& grads) override {
+    variable_list out(3);
+    const at::Tensor dh = residual ? grads[1] : at::Tensor();
+    if (!grads[0].defined()) {  // only h was used
+      if (!dh.defined()) return out;
+      if (task_should_compute_output(0)) out[0] = dh;
+      if (task_should_compute_output(2)) out[2] = dh;
+      return out;
+    }
+    const at::Tensor th = residual ? rows.unpack(shared_from_this()) : rows.unpack();
+    const at::Tensor tw = weight.unpack(), tr = rstd.unpack();
+    gradients(grads[0], dh, th, tw, tr, &out);
+    first_only("RMSNorm", out, th, tw, grads[0], dh);
+    return out;
+  }
+
+ private:
+  void gradients(const at::Tensor& grad, const at::Tensor& dh, const at::Tensor& th, const at::Tensor& tw,
+                 const at::Tensor& tr, variable_list* out) {
+    const at::NoGradGuard no_grad;
+    check_saved(th, residual ? "h" : "x", torch_type(z.xt), sizes, dev);
+    check_saved(tr, "rstd", at::kFloat, at::IntArrayRef(sizes.data(), sizes.size() - 1), dev);
+    if (z.w) check_saved(tw, "weight", torch_type(z.pt), z.params, dev);
+    const at::Tensor dy = plain_gradient(grad, th, torch_type(z.yt));
+    at::Tensor add;
+    if (dh.defined()) add = plain_gradient(dh, th, torch_type(z.xt));
+    // (the weight's gradient is left out where nothing asks for it)
+    RmsSizes need = z;
+    need.w = z.w && task_should_compute_output(1);
+    std::array<at::Tensor, 2> g;
+    mw_status s = MW_OK;
+    TORCH_CHECK(rms_gradients(dy, th, tr, z.w ? tw.const_data_ptr() : nullptr, add.defined() ? &add : nullptr, need,
+                              dev, &g, &s),
+                "no plain CUDA tensors");
+    if (s != MW_OK) raise(s);
+    if (task_should_compute_output(0)) (*out)[0] = g[0];
+    if (need.w) (*out)[1] = g[1];
+    if (residual && task_should_compute_output(2)) (*out)[2] = g[0];
+  }
+};
+
+// rms_apply(x, weight, residual, eps, out_dtype) -> y, or (y, h) with a residual
+PyObject* rms_apply(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Rms t;
+  float eps;
+  int yt;
+  if (n != 5 || !p_rms || !t.read(a[0], a[1], a[2]) || !real_number(a[3], &eps) || !t.out_type(a[4], &yt) ||
+      dual(t.x) || dual(t.w) || dual(t.r))
+    return none();
+  const at::Tensor none_given;
+  const at::Tensor &x = *t.x, &w = t.w ? *t.w : none_given, &r = t.r ? *t.r : none_given;
+  const bool graph = torch::autograd::compute_requires_grad(x, w, r);
+  mw_status s = MW_OK;
+  {
+    const at::NoGradGuard no_grad;
+    if (!t.forward(eps, yt, graph, &s)) return none();
+  }
+  if (s != MW_OK) return PyLong_FromLong(s);
+  if (graph) {
+    auto node = std::shared_ptr<RMSNormBackward>(new RMSNormBackward(), torch::autograd::deleteNode);
+    node->set_next_edges(torch::autograd::collect_next_edges(x, w, r));
+    if (t.w) node->weight = SavedVariable(w, false);
+    node->rstd = SavedVariable(t.rstd, false);
+    node->z = rms_sizes(t, yt);
+    node->sizes = x.sizes().vec();
+    node->residual = t.r != nullptr;
+    node->dev = t.dev;
+    torch::autograd::set_history(t.y, node);
+    if (t.r) {
+      torch::autograd::set_history(t.h, node);
+      node->rows = SavedVariable(t.h, true);
+    } else {
+      node->rows = SavedVariable(x, false);
+    }
+  }
+  return t.r ? result({&t.y, &t.h}) : THPVariable_Wrap(t.y);
+  END_HANDLE_TH_ERRORS
+}
+
+struct Fp8LinearBackward : public torch::autograd::Node {
+  SavedVariable xc, xcs, wq, ws;  // x in columns, where the weight wants a gradient; the weight
+  std::vector<int64_t> x_sizes, y_sizes;
+  int64_t M = 0;
+  int K = 0, N = 0, xt = 0, yt = 0, wt = 0;
+  bool columns = false;
+  c10::DeviceIndex dev = 0;
+
+  std::string name() const override { return "Fp8LinearBackward"; }
+  void release_variables() override {
+    for (SavedVariable* s : {&xc, &xcs, &wq, &ws}) s->reset_data();
+  }
+  variable_list apply(variable_list&& grads) override {
+    variable_list out(2);
+    if (!grads[0].defined()) return out;
+    const at::Tensor tx = xc.unpack(), txs = xcs.unpack(), tw = wq.unpack(), tws = ws.unpack();
+    gradients(grads[0], tx, txs, tw, tws, &out);
+    // (what they depend on besides is saved in 8 bits, without its graph)
+    if (at::GradMode::is_enabled()) {
+      auto node = std::shared_ptr<NoSecondDerivative>(new NoSecondDerivative(), torch::autograd::deleteNode);
+      node->what = "Fp8Linear";
+      for (const at::Tensor& g : out)
+        if (g.defined()) torch::autograd::set_history(g, node);
+    }
+    return out;
+  }
+
+ private:
+  void gradients(const at::Tensor& grad, const at::Tensor& tx, const at::Tensor& txs, const at::Tensor& tw,
+                 const at::Tensor& tws, variable_list* out) {
+    const at::NoGradGuard no_grad;
+    const bool need_x = task_should_compute_output(0), need_w = columns && task_should_compute_output(1);
+    if (!need_x && !need_w) return;
+    const std::array<int64_t, 2> wsz{N, K}, wss{blocks128(N), blocks128(K)}, xss{blocks128(M), K};
+    check_saved(tw, "weight in 8 bits", kCodes, wsz, dev);
+    check_saved(tws, "weight's scales", kScales, wss, dev);
+    if (columns) {
+      check_saved(tx, "x in 8 bits", kCodes, x_sizes, dev);
+      check_saved(txs, "x's scales", kScales, xss, dev);
+    }
+    TORCH_CHECK(is_real(grad) && grad.scalar_type() == torch_type(yt) && grad.sizes() == y_sizes &&
+                    grad.get_device() == dev,
+                "the gradient must be a plain CUDA tensor like the output");
+    const at::Tensor dy = grad.contiguous();
+    Form f;
+    mw_status s = MW_OK;
+    TORCH_CHECK(make_form(dy, M, need_x && need_w ? MW_FP8_ROWS_AND_COLUMNS : need_x ? MW_FP8_ROWS : MW_FP8_COLUMNS, yt,
+                          dev, &f, &s),
+                "no plain CUDA tensors");
+    if (s != MW_OK) raise(s);
+    const auto stream = c10::cuda::getCurrentCUDAStream(dev).stream();
+    const int m = static_cast<int>(M);
+    if (need_x) {
+      at::Tensor dx = at::empty(x_sizes, dy.options().dtype(torch_type(xt)));
+      TORCH_CHECK(is_real(dx), "no plain CUDA tensors");
+      s = p_matmul(f.q.const_data_ptr(), f.scale.const_data_ptr(), 0, 0, tw.const_data_ptr(), tws.const_data_ptr(), 1, 1,
+                   dx.mutable_data_ptr(), m, K, N, xt, stream);
+      if (s != MW_OK) raise(s);
+      (*out)[0] = dx;
+    }
+    if (need_w) {
+      at::Tensor dw = at::empty(wsz, dy.options().dtype(torch_type(wt)));
+      TORCH_CHECK(is_real(dw), "no plain CUDA tensors");
+      s = p_matmul(f.qc.const_data_ptr(), f.sc.const_data_ptr(), 0, 1, tx.const_data_ptr(), txs.const_data_ptr(), 0, 1,
+                   dw.mutable_data_ptr(), N, K, m, wt, stream);
+      if (s != MW_OK) raise(s);
+      (*out)[1] = dw;
+    }
+  }
+};
+
+// linear_apply(x, weight, out_dtype) -> y
+PyObject* linear_apply(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 3 || !p_matmul || !p_quantize) return none();
+  const at::Tensor *px = tensor(a[0]), *pw = tensor(a[1]);
+  c10::DeviceIndex dev;
+  if (!px || !pw || px->dim() < 1 || pw->dim() != 2 || px->size(-1) != pw->size(1) || !one_device({px, pw}, &dev) ||
+      dual(px) || dual(pw))
+    return none();
+  const at::Tensor &x = *px, &w = *pw;
+  const int xt = norm_type(x.scalar_type()), wt = norm_type(w.scalar_type());
+  int yt = xt;
+  if (a[2] != Py_None) {
+    if (!THPDtype_Check(a[2])) return none();
+    yt = norm_type(reinterpret_cast<THPDtype*>(a[2])->scalar_type);
+  }
+  const int64_t K = w.size(1), N = w.size(0);
+  if (xt < 0 || wt < 0 || yt < 0 || K < 16 || N < 16 || K % 16 || N % 16 || K > INT_MAX || N > INT_MAX ||
+      x.numel() / K > INT_MAX)
+    return none();
+  const int64_t M = x.numel() / K;
+  const bool graph = torch::autograd::compute_requires_grad(x, w);
+  const bool columns = graph && w.requires_grad();
+  std::vector<int64_t> sizes = x.sizes().vec();
+  sizes.back() = N;
+  Form fx, fw;
+  at::Tensor y;
+  mw_status s = MW_OK;
+  {
+    const at::NoGradGuard no_grad;
+    const bool real = call([&] {
+      if (!make_form(w, N, MW_FP8_TILES, wt, dev, &fw, &s)) return false;
+      if (s != MW_OK) return true;
+      if (!make_form(x, M, columns ? MW_FP8_ROWS_AND_COLUMNS : MW_FP8_ROWS, xt, dev, &fx, &s)) return false;
+      if (s != MW_OK) return true;
+      y = at::empty(sizes, x.options().dtype(torch_type(yt)));
+      if (!is_real(y)) return false;
+      s = p_matmul(fx.q.const_data_ptr(), fx.scale.const_data_ptr(), 0, 0, fw.q.const_data_ptr(),
+                   fw.scale.const_data_ptr(), 1, 0, y.mutable_data_ptr(), static_cast<int>(M), static_cast<int>(N),
+                   static_cast<int>(K), yt, c10::cuda::getCurrentCUDAStream(dev).stream());
+      return true;
+    });
+    if (!real) return none();
+  }
+  if (s != MW_OK) return PyLong_FromLong(s);
+  if (graph) {
+    auto node = std::shared_ptr<Fp8LinearBackward>(new Fp8LinearBackward(), torch::autograd::deleteNode);
+    node->set_next_edges(torch::autograd::collect_next_edges(x, w));
+    if (columns) {
+      node->xc = SavedVariable(fx.qc, false);
+      node->xcs = SavedVariable(fx.sc, false);
+    }
+    node->wq = SavedVariable(fw.q, false);
+    node->ws = SavedVariable(fw.scale, false);
+    node->x_sizes = x.sizes().vec();
+    node->y_sizes = sizes;
+    node->M = M;
+    node->K = static_cast<int>(K);
+    node->N = static_cast<int>(N);
+    node->xt = xt;
+    node->yt = yt;
+    node->wt = wt;
+    node->columns = columns;
+    node->dev = dev;
+    torch::autograd::set_history(y, node);
+  }
+  return THPVariable_Wrap(y);
+  END_HANDLE_TH_ERRORS
+}
+
 #define MW_FAST(f) reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL
 PyMethodDef methods[] = {
     {"bind", MW_FAST(bind), "addresses of the C entry points"},
@@ -900,6 +1398,13 @@ PyMethodDef methods[] = {
     {"norm_bwd", MW_FAST(norm_bwd), "mw_layernorm_bwd"},
     {"xattn_apply", MW_FAST(xattn_apply), "CrossAttention.apply"},
     {"norm_apply", MW_FAST(norm_apply), "LayerNorm.apply"},
+    {"rms_fwd", MW_FAST(rms_fwd), "mw_rmsnorm_fwd"},
+    {"rms_quantize", MW_FAST(rms_quantize), "mw_rmsnorm_fwd with an output in 8 bits"},
+    {"rms_bwd", MW_FAST(rms_bwd), "mw_rmsnorm_bwd"},
+    {"quantize", MW_FAST(quantize), "mw_quantize"},
+    {"scaled_matmul", MW_FAST(scaled_matmul), "mw_scaled_matmul"},
+    {"rms_apply", MW_FAST(rms_apply), "RMSNorm.apply"},
+    {"linear_apply", MW_FAST(linear_apply), "Fp8Linear.apply"},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_mw_torch", nullptr, -1, methods,
                       nullptr, nullptr, nullptr, nullptr};
