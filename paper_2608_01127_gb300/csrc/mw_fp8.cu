@@ -29,14 +29,14 @@ mw_status check_size(long long n, const char* name) {
   return MW_OK;
 }
 
-// How a product is cut: tiles of 128 x bn, each by one CTA in turn or by a cluster of
+// How a product is cut: tiles of 256 x bn by pairs of CTAs, or of 128 x bn by clusters of
 // `splits` CTAs (join) that share its contraction.
 struct MmPlan {
   int bn = 128, splits = 1;
   bool join = false, swap = false;
 };
 
-MmPlan mm_plan(int M, int N, int blocks, bool a_columns, bool b_columns, int sms) {
+MmPlan mm_plan(int M, int N, int blocks, bool a_columns, bool b_columns, bool f32, int sms) {
   MmPlan best;
   const bool few_m = M <= 64 && !a_columns, few_n = N <= 64 && !b_columns;
   if (few_m || few_n) {
@@ -47,18 +47,16 @@ MmPlan mm_plan(int M, int N, int blocks, bool a_columns, bool b_columns, int sms
     best.splits = std::max(1, std::min({8, blocks, 2 * sms / tiles}));
     return best;
   }
-  // cycles: a stage (128 x bn x 128) at the tensor cores' rate, and what a tile adds
+  // cycles: a stage, what a tile adds, what a launch does
   double best_cost = INFINITY;
   auto consider = [&](int bn, bool join, int splits) {
-    const long long tiles = static_cast<long long>(ceil_div(M, 128)) * ceil_div(N, bn);
-    const double stage = 2.0 * bn;
     double cost;
     if (join) {
-      const long long waves = ceil_div(tiles * splits, sms);
-      cost = waves * (ceil_div(blocks, splits) * stage + 4000 + 12.0 * bn);
+      const long long tiles = static_cast<long long>(ceil_div(M, 128)) * ceil_div(N, bn);
+      cost = ceil_div(tiles * splits, sms) * (ceil_div(blocks, splits) * 560.0 + 9000) + 3000;
     } else {
-      const long long waves = ceil_div(tiles, sms);
-      cost = waves * (blocks * stage + (bn == 256 ? 300 : 50)) + 3000 + 6.0 * bn;
+      const long long tiles = static_cast<long long>(ceil_div(M, 256)) * ceil_div(N, bn);
+      cost = ceil_div(tiles, sms / 2) * (blocks * (bn == 256 ? 800.0 : 630.0) + 500) + 6000;
     }
     if (cost < best_cost) {
       best_cost = cost;
@@ -69,7 +67,8 @@ MmPlan mm_plan(int M, int N, int blocks, bool a_columns, bool b_columns, int sms
   };
   consider(256, false, 1);
   consider(128, false, 1);
-  for (int s = 2; s <= 8 && s <= blocks; ++s) consider(128, true, s);
+  for (int s = 1; s <= 8 && s <= blocks; ++s)
+    if (!f32 || ceil_div(blocks, s) <= kFp8Chunk) consider(128, true, s);
   return best;
 }
 
@@ -251,15 +250,18 @@ mw_status mw_scaled_matmul(const void* a, const void* a_scale, int a_tiles, int 
   Fp8MmParams p{};
   MW_TRY(status_ptr(scope.device(), &p.status));
   p.blocks = ceil_div(K, kFp8Block);
-  const MmPlan plan = mm_plan(M, N, p.blocks, a_transposed, b_transposed, sm_count());
+  const MmPlan plan = mm_plan(M, N, p.blocks, a_transposed, b_transposed, f32, sm_count());
   auto scales = [&](const void* at, int rows, bool transposed, bool tile) {
     Fp8Scales z{};
     z.p = static_cast<const uint8_t*>(at);
-    z.tile = tile;
     const long long n = tile ? ceil_div(rows, 128) : rows;
     z.row = transposed ? 1 : p.blocks;
     z.block = transposed ? n : 1;
-    z.words = z.block == 1 && z.row % 4 == 0 && (reinterpret_cast<uintptr_t>(at) & 3u) == 0;
+    const bool words = (reinterpret_cast<uintptr_t>(at) & 3u) == 0;
+    z.read = tile                                             ? Fp8Read::kTile
+             : transposed && words                            ? Fp8Read::kQuads  // (rows: a multiple of 16)
+             : !transposed && words && p.blocks % 4 == 0      ? Fp8Read::kWords
+                                                              : Fp8Read::kBytes;
     return z;
   };
   Fp8Scales sa = scales(a_scale, M, a_transposed, a_tiles), sb = scales(b_scale, N, b_transposed, b_tiles);
@@ -280,9 +282,11 @@ mw_status mw_scaled_matmul(const void* a, const void* a_scale, int a_tiles, int 
   p.b_columns = tb_cols;
   p.swap = plan.swap;
   p.splits = plan.splits;
-  p.tiles_p = ceil_div(rows_a, 128);
+  p.tiles_p = ceil_div(rows_a, plan.join ? 128 : 256);
   p.tiles_q = ceil_div(rows_b, plan.bn);
   p.ctas = sm_count();
+  // (whole words of scales)
+  p.chunk = f32 ? ceil_div(ceil_div(p.blocks, ceil_div(p.blocks, kFp8Chunk)), 4) * 4 : p.blocks;
   p.out = c;
   p.out_f32 = f32;
   p.out_quads = N % 4 == 0 && (reinterpret_cast<uintptr_t>(c) & (4 * elem - 1)) == 0;
@@ -294,7 +298,7 @@ mw_status mw_scaled_matmul(const void* a, const void* a_scale, int a_tiles, int 
     return columns ? make_map_2d(m, at, K, rows, 1, kFp8Block, name) : make_map_2d(m, at, rows, K, 1, box, name);
   };
   MW_TRY(operand(&ma, a, rows_a, p.a_columns, 128, "a"));
-  MW_TRY(operand(&mb, b, rows_b, p.b_columns, plan.bn, "b"));
+  MW_TRY(operand(&mb, b, rows_b, p.b_columns, plan.join ? plan.bn : plan.bn / 2, "b"));
   mc = ma;
   if (p.tma_out) MW_TRY(make_map_2d(&mc, c, M, N, static_cast<int>(elem), 32, "c"));
   return launch_status(launch_fp8_mm(plan.bn, plan.join, ma, mb, mc, p, scope.device(), s), "8-bit product launch");

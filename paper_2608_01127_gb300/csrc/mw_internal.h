@@ -341,6 +341,7 @@ cudaError_t launch_xattn_bwd(int d, int dm, const XattnBwdMaps& m, const XattnBw
 // Matrices in 8 bits (e4m3) with a scale (e8m0) for every block of 128: of a row's
 // elements (rows), of a column's (columns), or of both (tiles).
 constexpr int kFp8Block = 128;
+constexpr int kFp8Chunk = 64;  // blocks that an fp32 result sums in tensor memory at most
 struct Fp8FormParams {
   const void* x;         // [rows, C], bf16 or fp32
   uint8_t* q;            // rows or tiles: [rows, C]
@@ -355,20 +356,23 @@ enum class Fp8Form { kRows, kColumns, kTiles, kBoth };
 cudaError_t launch_fp8_form(const Fp8FormParams& p, Fp8Form form, cudaStream_t s);
 
 // Product of two of them (mw_fp8_mm.cu): rows_a x rows_b results over `blocks` of the contraction.
+// How the scales of a row's blocks are read: one for 128 rows; four blocks of a row as a word;
+// a block of four rows as a word; a byte each.
+enum class Fp8Read { kTile, kWords, kQuads, kBytes };
 struct Fp8Scales {
   const uint8_t* p;
-  long long row, block;  // bytes from a row, and from a block of the contraction, to the next
-  bool tile;             // one for 128 rows
-  bool words;            // blocks lie together, rows at multiples of four bytes
+  long long row, block;  // bytes from a row (kTile: from 128 rows), and from a block, to the next
+  Fp8Read read;
 };
 struct Fp8MmParams {
   Fp8Scales a_scales, b_scales;
   void* out;             // bf16 or fp32, rows of ld
   long long ld;
   int rows_a, rows_b, blocks;
-  int tiles_p, tiles_q;  // of 128 rows of A, of bn rows of B
+  int tiles_p, tiles_q;  // of 128 rows of A (pairs: 256), of bn rows of B
   int splits;            // join: CTAs of a tile
-  int ctas;              // else: CTAs at most
+  int ctas;              // pairs: CTAs at most
+  int chunk;             // pairs: blocks that are summed in tensor memory before the output takes them
   bool a_columns, b_columns;  // rows of the operand lie across the contraction
   bool swap;             // join: a row of the output is one of B
   bool out_f32;
@@ -378,8 +382,9 @@ struct Fp8MmParams {
   unsigned long long budget_ns;
   int debug_skip_q;      // test hook: never load A and B
 };
-// bn: rows of B of a tile (join: 16, 32, 64 or 128; else 128 or 256); ta, tb: boxes of 128
-// bytes x 128 rows (tb: x bn rows where B runs along the contraction); tc: 32 rows x 128 bytes
+// bn: rows of B of a tile (join: 16, 32, 64 or 128; pairs: 128 or 256); ta, tb: boxes of 128
+// bytes x 128 rows (join's tb, and pairs' of 128 rows: x bn and 64 rows where B runs along the
+// contraction); tc: 32 rows x 128 bytes
 cudaError_t launch_fp8_mm(int bn, bool join, const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap& tc,
                           const Fp8MmParams& p, int dev, cudaStream_t s);
 

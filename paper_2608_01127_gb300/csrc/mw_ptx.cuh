@@ -56,6 +56,30 @@ __device__ __forceinline__ bool mbar_try_wait(uint64_t* bar, uint32_t parity) {
   return ok != 0;
 }
 
+// The same where what the other CTA of a pair wrote is read next.
+__device__ __forceinline__ bool mbar_try_wait_cluster(uint64_t* bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}\n"
+      : "=r"(ok)
+      : "r"(smem_u32(bar)), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+
+// The shared-memory address `addr` of this CTA in CTA `rank` of the cluster.
+__device__ __forceinline__ uint32_t cluster_address(uint32_t addr, uint32_t rank) {
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+  return r;
+}
+
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr) {
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+
 // Shared abort state of one CTA: a flag that every bounded wait polls, so
 // that one expired wait releases all roles, plus the time budget.
 struct WaitCtl {
@@ -73,9 +97,10 @@ __device__ __forceinline__ bool skips_loads(int hook) { return (hook >> (blockId
 // status word and returns false.  Never traps.  The abort flag and the clock
 // are looked at only every 32nd poll (try_wait itself suspends the thread for
 // a while): a read of the clock before the first one delayed every wait.
+template <bool CLUSTER = false>
 __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, const WaitCtl& ctl) {
   uint64_t t0 = 0;
-  for (uint32_t spins = 1; !mbar_try_wait(bar, parity); ++spins) {
+  for (uint32_t spins = 1; !(CLUSTER ? mbar_try_wait_cluster(bar, parity) : mbar_try_wait(bar, parity)); ++spins) {
     if ((spins & 31u) != 0u) continue;
     if (*ctl.abort) return false;
     const uint64_t t = global_timer_ns();
@@ -93,9 +118,11 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, const 
 // that .sync.aligned tcgen05 instructions after it are never divergent.  The
 // loop itself is uniform (a vote a poll): a vote over mbar_wait's answers
 // took 104 cycles for a phase that was complete already, this form 59.
+template <bool CLUSTER = false>
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, const WaitCtl& ctl) {
   uint64_t t0 = 0;
-  for (uint32_t spins = 1; !__all_sync(0xffffffffu, mbar_try_wait(bar, parity)); ++spins) {
+  for (uint32_t spins = 1; !__all_sync(0xffffffffu, CLUSTER ? mbar_try_wait_cluster(bar, parity) : mbar_try_wait(bar, parity));
+       ++spins) {
     if ((spins & 31u) != 0u) continue;
     const uint64_t t = global_timer_ns();
     if (t0 == 0) t0 = t;
@@ -153,6 +180,22 @@ __device__ __forceinline__ void tma_load_2d(void* dst, const CUtensorMap* map, u
       "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
       " [%0], [%1, {%3, %4}], [%2];" ::"r"(smem_u32(dst)),
       "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(bar)), "r"(c0), "r"(c1)
+      : "memory");
+}
+// A load of one CTA of a pair that is counted by a barrier of either (its address in the cluster).
+__device__ __forceinline__ void tma_load_2d_pair(void* dst, const CUtensorMap* map, uint32_t cluster_bar, int c0,
+                                                 int c1) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2"
+      " [%0], [%1, {%3, %4}], [%2];" ::"r"(smem_u32(dst)),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(cluster_bar), "r"(c0), "r"(c1)
+      : "memory");
+}
+__device__ __forceinline__ void tma_reduce_add_2d(const CUtensorMap* map, const void* src, int c0, int c1) {
+  asm volatile(
+      "cp.reduce.async.bulk.tensor.2d.global.shared::cta.add.tile.bulk_group [%0, {%2, %3}], [%1];" ::"l"(
+          reinterpret_cast<uint64_t>(map)),
+      "r"(smem_u32(src)), "r"(c0), "r"(c1)
       : "memory");
 }
 __device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, const void* src, int c0, int c1) {
@@ -229,6 +272,17 @@ __device__ __forceinline__ void fence_proxy_async_smem() {
 }
 
 // ------------------------------------------------------------------ tcgen05
+
+// (_pair: both CTAs of a pair, one warp of each)
+__device__ __forceinline__ void tmem_alloc_pair(uint32_t* dst_smem, uint32_t ncols) {
+  asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(dst_smem)),
+               "r"(ncols)
+               : "memory");
+  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_dealloc_pair(uint32_t taddr, uint32_t ncols) {
+  asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(ncols) : "memory");
+}
 
 __device__ __forceinline__ void tmem_alloc(uint32_t* dst_smem, uint32_t ncols) {
   asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
@@ -364,51 +418,61 @@ __device__ __forceinline__ void umma_ts4(uint32_t d_tmem, uint32_t a_tmem, uint3
 // Four MMAs D (+)= A B^T of 8-bit operands (kind::mxf8f6f4: e4m3, a power-of-two scale
 // for 32 of the contraction, K = 32 per instruction), descriptors a_step and b_step
 // (16 bytes) further each time; all of them take the same byte of the scale words in
-// tensor memory at sfa and sfb (chosen by idesc).
+// tensor memory at sfa and sfb (chosen by idesc).  PAIR: of two CTAs, issued by the one of
+// rank 0: 128 rows of A and half of the rows of B in each one's shared memory, the results
+// of its rows of A in each one's tensor memory, with its rows' and all of B's scales.
+template <bool PAIR = false>
 __device__ __forceinline__ void umma_mx4(uint32_t d_tmem, uint32_t a_desc, uint32_t b_desc, uint32_t a_step,
                                          uint32_t b_step, uint32_t idesc, uint32_t sfa, uint32_t sfb,
                                          uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p, e;\n\t.reg .b32 a1, a2, a3, b1, b2, b3;\n\t.reg .b64 da, db;\n\t"
-      "elect.sync _|e, 0xffffffff;\n\t"
-      "@!e bra OTHERS;\n\t"
-      "add.u32 a1, %1, %3;\n\t"
-      "add.u32 b1, %2, %4;\n\t"
-      "add.u32 a2, a1, %3;\n\t"
-      "add.u32 b2, b1, %4;\n\t"
-      "add.u32 a3, a2, %3;\n\t"
-      "add.u32 b3, b2, %4;\n\t"
-      "setp.ne.b32 p, %8, 0;\n\t"
-      "mov.b64 da, {%1, %9};\n\t"
-      "mov.b64 db, {%2, %9};\n\t"
-      "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], da, db, %5, [%6], [%7], p;\n\t"
-      "setp.eq.b32 p, %8, %8;\n\t"
-      "mov.b64 da, {a1, %9};\n\t"
-      "mov.b64 db, {b1, %9};\n\t"
-      "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], da, db, %5, [%6], [%7], p;\n\t"
-      "mov.b64 da, {a2, %9};\n\t"
-      "mov.b64 db, {b2, %9};\n\t"
-      "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], da, db, %5, [%6], [%7], p;\n\t"
-      "mov.b64 da, {a3, %9};\n\t"
-      "mov.b64 db, {b3, %9};\n\t"
-      "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], da, db, %5, [%6], [%7], p;\n"
-      "OTHERS:\n\t}\n" ::"r"(d_tmem),
-      "r"(a_desc), "r"(b_desc), "r"(a_step), "r"(b_step), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate),
-      "n"(kSw128Hi)
-      : "memory");
+#define MW_MMA(group, a, b)          \
+  "mov.b64 da, {" a ", %9};\n\t"     \
+  "mov.b64 db, {" b ", %9};\n\t"     \
+  "tcgen05.mma.cta_group::" group ".kind::mxf8f6f4.block_scale.scale_vec::1X [%0], da, db, %5, [%6], [%7], p;\n\t"
+#define MW_MMA4(group)                                                                                       \
+  asm volatile(                                                                                              \
+      "{\n\t.reg .pred p, e;\n\t.reg .b32 a1, a2, a3, b1, b2, b3;\n\t.reg .b64 da, db;\n\t"                  \
+      "elect.sync _|e, 0xffffffff;\n\t"                                                                      \
+      "@!e bra OTHERS;\n\t"                                                                                  \
+      "add.u32 a1, %1, %3;\n\t"                                                                              \
+      "add.u32 b1, %2, %4;\n\t"                                                                              \
+      "add.u32 a2, a1, %3;\n\t"                                                                              \
+      "add.u32 b2, b1, %4;\n\t"                                                                              \
+      "add.u32 a3, a2, %3;\n\t"                                                                              \
+      "add.u32 b3, b2, %4;\n\t"                                                                              \
+      "setp.ne.b32 p, %8, 0;\n\t" MW_MMA(group, "%1", "%2") "setp.eq.b32 p, %8, %8;\n\t" MW_MMA(group, "a1", "b1") \
+          MW_MMA(group, "a2", "b2") MW_MMA(group, "a3", "b3") "\nOTHERS:\n\t}\n" ::"r"(d_tmem),              \
+      "r"(a_desc), "r"(b_desc), "r"(a_step), "r"(b_step), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate),   \
+      "n"(kSw128Hi)                                                                                          \
+      : "memory")
+  if constexpr (PAIR)
+    MW_MMA4("2");
+  else
+    MW_MMA4("1");
+#undef MW_MMA4
+#undef MW_MMA
 }
 
 // 512 bytes of scale words from shared memory into four columns of tensor memory, the same
 // in each quarter of its lanes: lane l of a quarter gets the 16 bytes 16 l ...  Ordered
-// before the MMAs that the same thread issues after it.
+// before the MMAs that the same thread issues after it.  PAIR: in each CTA of the pair, from
+// its own shared memory.
+template <bool PAIR = false>
 __device__ __forceinline__ void tmem_copy_scales(uint32_t d_tmem, uint32_t saddr) {
-  asm volatile(
-      "{\n\t.reg .pred e;\n\t.reg .b64 d;\n\t"
-      "elect.sync _|e, 0xffffffff;\n\t"
-      "mov.b64 d, {%1, %2};\n\t"
-      "@e tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], d;\n\t}\n" ::"r"(d_tmem),
-      "r"((saddr & 0x3FFFFu) >> 4), "n"((128u >> 4) | (1u << 14))  // 8 rows of 16 bytes: SBO 128; no swizzle
-      : "memory");
+#define MW_CP(group)                                                    \
+  asm volatile(                                                         \
+      "{\n\t.reg .pred e;\n\t.reg .b64 d;\n\t"                          \
+      "elect.sync _|e, 0xffffffff;\n\t"                                 \
+      "mov.b64 d, {%1, %2};\n\t"                                        \
+      "@e tcgen05.cp.cta_group::" group ".32x128b.warpx4 [%0], d;\n\t}\n" ::"r"(d_tmem), \
+      "r"((saddr & 0x3FFFFu) >> 4), "n"((128u >> 4) | (1u << 14))       \
+      : "memory")
+  // (descriptor: 8 rows of 16 bytes, then the next 8 at 128; no swizzle)
+  if constexpr (PAIR)
+    MW_CP("2");
+  else
+    MW_CP("1");
+#undef MW_CP
 }
 
 // Arrive (once) on `bar` when every tcgen05 op issued so far by the elected
@@ -419,6 +483,17 @@ __device__ __forceinline__ void umma_commit(uint64_t* bar) {
       "elect.sync _|e, 0xffffffff;\n\t"
       "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}\n" ::"r"(
           smem_u32(bar))
+      : "memory");
+}
+
+// The same on the barriers at `bar` of both CTAs of a pair.
+__device__ __forceinline__ void umma_commit_pair(uint64_t* bar) {
+  asm volatile(
+      "{\n\t.reg .pred e;\n\t"
+      "elect.sync _|e, 0xffffffff;\n\t"
+      "@e tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n\t}\n" ::"r"(
+          smem_u32(bar)),
+      "h"(static_cast<uint16_t>(3))
       : "memory");
 }
 
