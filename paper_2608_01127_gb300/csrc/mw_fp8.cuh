@@ -18,6 +18,13 @@ __device__ __forceinline__ uint8_t fp8_scale(uint32_t top) {
   return top >= 0x7f800000u ? kFp8NanScale : static_cast<uint8_t>(max(e, 0));
 }
 
+// The same of the two bf16 magnitudes of a word, in its halves.
+__device__ __forceinline__ uint32_t fp8_scale2(uint32_t tops) {
+  const uint32_t e = __vmaxu2(((tops + 0x001f001fu) >> 7) & 0x00ff00ffu, 0x00080008u) - 0x00080008u;
+  const uint32_t over = (tops + 0x00800080u) & 0x80008000u;  // not finite
+  return e | ((over >> 7) - (over >> 15));
+}
+
 // 1 / s (NaN for NaN): 7 <= 254 - scale <= 254, a normal number.
 __device__ __forceinline__ float fp8_inverse(uint8_t scale) {
   return __uint_as_float(scale == kFp8NanScale ? 0x7fffffffu : (254u - scale) << 23);
@@ -29,6 +36,9 @@ __device__ __forceinline__ uint32_t fp8_pair(float a, float b) {
   asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(b), "f"(a));
   return r;
 }
+
+// Four codes.
+__device__ __forceinline__ uint32_t fp8_four(float2 a, float2 b) { return fp8_pair(a.x, a.y) | fp8_pair(b.x, b.y) << 16; }
 
 // Eight codes of values already divided by the scale (NaN where that is NaN).
 __device__ __forceinline__ uint2 fp8_codes(const float (&v)[8], uint8_t scale) {

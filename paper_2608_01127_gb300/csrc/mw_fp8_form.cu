@@ -8,8 +8,10 @@
 // the scale NaN and the codes NaN: what it stands for is NaN, wherever it is read.
 //
 // Bound by HBM: an element is read once for all the forms asked for.  A block of 256
-// threads holds 128 x 128 elements in registers, a thread 8 columns of 8 rows; a row's
-// maximum is one over 16 lanes, a column's over the 16 groups of lanes.
+// threads holds 128 x 128 elements in registers, a thread 8 columns of 8 rows.  The scale
+// grows with the maximum, so that what lanes and warps put together are scale bytes, four to
+// a word: four shuffles for a thread's eight rows.  (With maxima in 32 bits, 32 shuffles and
+// a scale for every row in every lane: rows and columns of 14080 x 2560 bf16 46 us.)
 #include "mw_fp8.cuh"
 #include "mw_internal.h"
 #include "mw_ptx.cuh"
@@ -17,143 +19,172 @@
 namespace mw {
 namespace {
 
+// 8 columns of 8 rows of a thread as they lie in memory.
 template <class T>
-struct Eight;  // elements of a row as they lie in memory
+struct Held;
 template <>
-struct Eight<__nv_bfloat16> {
-  uint4 a;
-  __device__ __forceinline__ void load(const __nv_bfloat16* p) { a = *reinterpret_cast<const uint4*>(p); }
-  __device__ __forceinline__ void zero() { a = make_uint4(0, 0, 0, 0); }
-  __device__ __forceinline__ float get(int k) const {
-    const uint32_t w = k < 2 ? a.x : k < 4 ? a.y : k < 6 ? a.z : a.w;
-    return __uint_as_float(k & 1 ? w & 0xffff0000u : w << 16);
+struct Held<__nv_bfloat16> {
+  uint4 a[8];
+  __device__ __forceinline__ void load(int i, const __nv_bfloat16* p) { a[i] = *reinterpret_cast<const uint4*>(p); }
+  __device__ __forceinline__ void zero(int i) { a[i] = make_uint4(0, 0, 0, 0); }
+  __device__ __forceinline__ void get(int i, float2 (&v)[4]) const {
+    const uint32_t w[4] = {a[i].x, a[i].y, a[i].z, a[i].w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = make_float2(__uint_as_float(w[k] << 16), __uint_as_float(w[k] & 0xffff0000u));
+  }
+  // Scale bytes of the rows (byte i % 4 of word i / 4) and of the columns.
+  __device__ __forceinline__ void scales(uint32_t (&rows)[2], uint32_t (&columns)[2]) const {
+    uint32_t c[4] = {0u, 0u, 0u, 0u}, r[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t w[4] = {a[i].x & 0x7fff7fffu, a[i].y & 0x7fff7fffu, a[i].z & 0x7fff7fffu, a[i].w & 0x7fff7fffu};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) c[k] = __vmaxu2(c[k], w[k]);
+      r[i] = __vmaxu2(__vmaxu2(w[0], w[1]), __vmaxu2(w[2], w[3]));
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      columns[h] = __byte_perm(fp8_scale2(c[2 * h]), fp8_scale2(c[2 * h + 1]), 0x6420);
+      uint32_t pair[2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const uint32_t x = r[4 * h + 2 * k], y = r[4 * h + 2 * k + 1];
+        pair[k] = fp8_scale2(__vmaxu2(__byte_perm(x, y, 0x5410), __byte_perm(x, y, 0x7632)));
+      }
+      rows[h] = __byte_perm(pair[0], pair[1], 0x6420);
+    }
   }
 };
 template <>
-struct Eight<float> {
-  float4 a, b;
-  __device__ __forceinline__ void load(const float* p) {
-    a = reinterpret_cast<const float4*>(p)[0];
-    b = reinterpret_cast<const float4*>(p)[1];
+struct Held<float> {
+  float4 a[8], b[8];
+  __device__ __forceinline__ void load(int i, const float* p) {
+    a[i] = reinterpret_cast<const float4*>(p)[0];
+    b[i] = reinterpret_cast<const float4*>(p)[1];
   }
-  __device__ __forceinline__ void zero() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
-  __device__ __forceinline__ float get(int k) const {
-    return k == 0 ? a.x : k == 1 ? a.y : k == 2 ? a.z : k == 3 ? a.w : k == 4 ? b.x : k == 5 ? b.y : k == 6 ? b.z : b.w;
+  __device__ __forceinline__ void zero(int i) { a[i] = b[i] = make_float4(0.f, 0.f, 0.f, 0.f); }
+  __device__ __forceinline__ void get(int i, float2 (&v)[4]) const {
+    v[0] = make_float2(a[i].x, a[i].y), v[1] = make_float2(a[i].z, a[i].w);
+    v[2] = make_float2(b[i].x, b[i].y), v[3] = make_float2(b[i].z, b[i].w);
+  }
+  __device__ __forceinline__ void scales(uint32_t (&rows)[2], uint32_t (&columns)[2]) const {
+    uint32_t c[8] = {};
+    rows[0] = rows[1] = columns[0] = columns[1] = 0u;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      float2 v[4];
+      get(i, v);
+      uint32_t r = 0u;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint32_t x = fp8_magnitude(v[k].x), y = fp8_magnitude(v[k].y);
+        c[2 * k] = max(c[2 * k], x);
+        c[2 * k + 1] = max(c[2 * k + 1], y);
+        r = max(r, max(x, y));
+      }
+      rows[i / 4] |= static_cast<uint32_t>(fp8_scale(r)) << (8 * (i % 4));
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) columns[k / 4] |= static_cast<uint32_t>(fp8_scale(c[k])) << (8 * (k % 4));
   }
 };
 
+__device__ __forceinline__ uint8_t byte_of(const uint32_t (&w)[2], int i) {
+  return static_cast<uint8_t>(w[i / 4] >> (8 * (i % 4)));
+}
+
 template <class T, Fp8Form FORM>
-__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) fp8_form_kernel(const Fp8FormParams p, int tiles_c) {
+__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 4 : 2) fp8_form_kernel(const Fp8FormParams p, int tiles_c) {
   constexpr bool ROWS = FORM == Fp8Form::kRows || FORM == Fp8Form::kBoth;
   constexpr bool COLUMNS = FORM == Fp8Form::kColumns || FORM == Fp8Form::kBoth;
   constexpr bool TILES = FORM == Fp8Form::kTiles;
-  __shared__ uint32_t tops[COLUMNS ? 8 * 128 : 8];
+  __shared__ uint2 tops[COLUMNS ? 8 * 16 : 1];
+  __shared__ uint32_t whole[8];
   const int tile_c = blockIdx.x % tiles_c;
   const long long tile_r = blockIdx.x / tiles_c;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int part = threadIdx.x & 15, ry = threadIdx.x >> 4;
   const int c = tile_c * 128 + part * 8;
   const long long r0 = tile_r * 128 + ry;
+  // rows r0, r0 + 16, ... that there are, and of this thread's columns
+  const int all = static_cast<int>(min(8ll, max(0ll, (p.rows - r0 + 15) / 16))), n = c < p.C ? all : 0;
   const T* x = static_cast<const T*>(p.x) + r0 * p.C + c;
+  const size_t pitch = static_cast<size_t>(16) * p.C;
   pdl_wait();
   pdl_trigger();
-  Eight<T> e[8];
+  Held<T> e;
+  if (n == 8) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    if (c < p.C && r0 + 16 * i < p.rows)
-      e[i].load(x + static_cast<long long>(16 * i) * p.C);
-    else
-      e[i].zero();
+    for (int i = 0; i < 8; ++i) e.load(i, x + i * pitch);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (i < n)
+        e.load(i, x + i * pitch);
+      else
+        e.zero(i);
+    }
   }
-  uint32_t column[8];  // largest magnitudes of the thread's columns
+  uint32_t rows[2], columns[2];
+  e.scales(rows, columns);
+  if constexpr (ROWS) {
+    // the largest over 16 lanes: halves of the rows change sides, then four bytes go on
+    const uint32_t other = __shfl_xor_sync(0xffffffffu, lane & 8 ? rows[0] : rows[1], 8);
+    uint32_t r = __vmaxu4(lane & 8 ? rows[1] : rows[0], other);
 #pragma unroll
-  for (int k = 0; k < 8; ++k) column[k] = 0u;
-  uint32_t tile = 0u;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    uint32_t top = 0u;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const uint32_t m = fp8_magnitude(e[i].get(k));
-      if (COLUMNS) column[k] = max(column[k], m);
-      top = max(top, m);
-    }
-    if constexpr (ROWS) {
-#pragma unroll
-      for (int s = 8; s > 0; s >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, s));
-      const uint8_t scale = fp8_scale(top);
-      const long long row = r0 + 16 * i;
-      if (row < p.rows && c < p.C) {
-        const float inv = fp8_inverse(scale);
-        float v[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = e[i].get(k) * inv;
-        *reinterpret_cast<uint2*>(p.q + row * p.C + c) = fp8_codes(v, scale);
-        if (part == 0) p.scale[row * tiles_c + tile_c] = scale;
-      }
-    }
-    tile = max(tile, top);
+    for (int s = 4; s > 0; s >>= 1) r = __vmaxu4(r, __shfl_xor_sync(0xffffffffu, r, s));
+    rows[0] = __shfl_sync(0xffffffffu, r, lane & 16);
+    rows[1] = __shfl_sync(0xffffffffu, r, (lane & 16) + 8);
+    if (part < all) p.scale[(r0 + 16 * part) * tiles_c + tile_c] = byte_of(rows, part);
   }
   if constexpr (COLUMNS) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) column[k] = max(column[k], __shfl_xor_sync(0xffffffffu, column[k], 16));
-    if (lane < 16) {
-      uint4* to = reinterpret_cast<uint4*>(tops + warp * 128 + part * 8);
-      to[0] = make_uint4(column[0], column[1], column[2], column[3]);
-      to[1] = make_uint4(column[4], column[5], column[6], column[7]);
-    }
+    for (int h = 0; h < 2; ++h) columns[h] = __vmaxu4(columns[h], __shfl_xor_sync(0xffffffffu, columns[h], 16));
+    if (lane < 16) tops[warp * 16 + part] = make_uint2(columns[0], columns[1]);
     __syncthreads();
-    uint32_t bytes[2] = {0u, 0u};
-    float inv[8];
-    bool bad[8];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      uint4 m = make_uint4(0, 0, 0, 0);
-#pragma unroll
-      for (int w = 0; w < 8; ++w) {
-        const uint4 o = reinterpret_cast<const uint4*>(tops + w * 128 + part * 8)[h];
-        m.x = max(m.x, o.x), m.y = max(m.y, o.y), m.z = max(m.z, o.z), m.w = max(m.w, o.w);
-      }
-      const uint32_t top[4] = {m.x, m.y, m.z, m.w};
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const uint8_t scale = fp8_scale(top[k]);
-        bytes[h] |= static_cast<uint32_t>(scale) << (8 * k);
-        inv[4 * h + k] = fp8_inverse(scale);
-        bad[4 * h + k] = scale == kFp8NanScale;
-      }
+    for (int w = 0; w < 8; ++w) {
+      const uint2 o = tops[w * 16 + part];
+      columns[0] = __vmaxu4(columns[0], o.x);
+      columns[1] = __vmaxu4(columns[1], o.y);
     }
-    if (c < p.C) {
-      if (ry == 0) *reinterpret_cast<uint2*>(p.scale_columns + tile_r * p.C + c) = make_uint2(bytes[0], bytes[1]);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const long long row = r0 + 16 * i;
-        if (row >= p.rows) continue;
-        float v[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = bad[k] ? __uint_as_float(0x7fffffffu) : e[i].get(k) * inv[k];
-        *reinterpret_cast<uint2*>(p.q_columns + row * p.C + c) = fp8_codes(v, 0);
-      }
-    }
+    if (ry == 0 && c < p.C)
+      *reinterpret_cast<uint2*>(p.scale_columns + tile_r * p.C + c) = make_uint2(columns[0], columns[1]);
   }
+  uint8_t tile = 0;
   if constexpr (TILES) {
-    tile = __reduce_max_sync(0xffffffffu, tile);
-    if (lane == 0) tops[warp] = tile;
+    uint32_t t = __vmaxu4(rows[0], rows[1]);
+    t = __vmaxu4(t, t >> 16);
+    t = max(t & 0xffu, t >> 8 & 0xffu);
+    t = __reduce_max_sync(0xffffffffu, t);
+    if (lane == 0) whole[warp] = t;
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < 8; ++w) tile = max(tile, tops[w]);
-    const uint8_t scale = fp8_scale(tile);
-    const float inv = fp8_inverse(scale);
-    if (threadIdx.x == 0) p.scale[tile_r * tiles_c + tile_c] = scale;
+    for (int w = 0; w < 8; ++w) t = max(t, whole[w]);
+    tile = static_cast<uint8_t>(t);
+    if (threadIdx.x == 0) p.scale[tile_r * tiles_c + tile_c] = tile;
+  }
+  [[maybe_unused]] float2 inv[4];  // of the columns
+  if constexpr (COLUMNS) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const long long row = r0 + 16 * i;
-      if (row >= p.rows || c >= p.C) continue;
-      float v[8];
+    for (int k = 0; k < 4; ++k)
+      inv[k] = make_float2(fp8_inverse(byte_of(columns, 2 * k)), fp8_inverse(byte_of(columns, 2 * k + 1)));
+  }
+  const size_t out = static_cast<size_t>(r0) * p.C + c;
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = e[i].get(k) * inv;
-      *reinterpret_cast<uint2*>(p.q + row * p.C + c) = fp8_codes(v, scale);
+  for (int i = 0; i < 8; ++i) {
+    if (i >= n) continue;
+    float2 v[4];
+    e.get(i, v);
+    if constexpr (ROWS || TILES) {
+      const float s = fp8_inverse(ROWS ? byte_of(rows, i) : tile);
+      const float2 by = make_float2(s, s);
+      *reinterpret_cast<uint2*>(p.q + out + i * pitch) =
+          make_uint2(fp8_four(mul2(v[0], by), mul2(v[1], by)), fp8_four(mul2(v[2], by), mul2(v[3], by)));
     }
+    if constexpr (COLUMNS)
+      *reinterpret_cast<uint2*>(p.q_columns + out + i * pitch) = make_uint2(
+          fp8_four(mul2(v[0], inv[0]), mul2(v[1], inv[1])), fp8_four(mul2(v[2], inv[2]), mul2(v[3], inv[3])));
   }
 }
 
