@@ -121,7 +121,7 @@ mw_status mw_rmsnorm_fwd(const void* x, const void* residual, const void* weight
   p.x_f32 = x_dtype == MW_F32;
   p.y_type = codes ? kRmsCodes : y_dtype == MW_F32 ? kRmsF32 : kRmsBf16;
   p.param_f32 = param_dtype == MW_F32;
-  return launch_status(launch_rms_fwd(p, vector_rows(C, x, residual, weight, y, p.h), sm_count(), s),
+  return launch_status(launch_rms_fwd(p, vector_rows(C, x, residual, weight, y, p.h), scope.device(), sm_count(), s),
                        "RMS norm forward launch");
 }
 

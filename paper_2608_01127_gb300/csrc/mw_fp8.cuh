@@ -41,8 +41,7 @@ __device__ __forceinline__ uint32_t fp8_pair(float a, float b) {
 __device__ __forceinline__ uint32_t fp8_four(float2 a, float2 b) { return fp8_pair(a.x, a.y) | fp8_pair(b.x, b.y) << 16; }
 
 // Eight codes of values already divided by the scale (NaN where that is NaN).
-__device__ __forceinline__ uint2 fp8_codes(const float (&v)[8], uint8_t scale) {
-  if (scale == kFp8NanScale) return make_uint2(0x7f7f7f7fu, 0x7f7f7f7fu);
+__device__ __forceinline__ uint2 fp8_codes(const float (&v)[8]) {
   return make_uint2(fp8_pair(v[0], v[1]) | fp8_pair(v[2], v[3]) << 16, fp8_pair(v[4], v[5]) | fp8_pair(v[6], v[7]) << 16);
 }
 

@@ -238,7 +238,7 @@ struct RmsParams {
   float* partial;        // [groups * parts, C] where parts > 1
   long long rows, rows_per_group;
   int C, groups;
-  int parts;             // backward: blocks that share a group's rows
+  int parts;             // blocks that share a group's rows (forward: set by the launcher)
   int W;                 // warps that share a row (set by the launcher)
   float eps;
   int y_type;
@@ -246,7 +246,7 @@ struct RmsParams {
 };
 int rms_parts(long long rows_per_group, int C, int groups);
 // vec: C is a multiple of 8 and every pointer 16-byte aligned
-cudaError_t launch_rms_fwd(RmsParams p, bool vec, int sms, cudaStream_t s);
+cudaError_t launch_rms_fwd(RmsParams p, bool vec, int dev, int sms, cudaStream_t s);
 cudaError_t launch_rms_bwd(RmsParams p, bool vec, int dev, cudaStream_t s);
 
 // Cross attention: BH heads of K and V [BH, S, d], each with M rows of Q (those of all

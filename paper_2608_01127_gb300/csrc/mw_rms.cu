@@ -31,16 +31,16 @@ __device__ __forceinline__ void store_y(void* base, size_t at, const float (&v)[
 __device__ __forceinline__ float rounded(float v, const float*) { return v; }
 __device__ __forceinline__ float rounded(float v, const bf16*) { return __bfloat162float(__float2bfloat16(v)); }
 
-constexpr int fwd_blocks(int VEC, int V, int x, bool res) {
-  return VEC == 1 ? (V <= 4 ? 5 : V <= 8 ? 3 : 1) : V <= 2 ? 4 : V <= 4 ? 3 : V <= 6 && x == 2 && !res ? 3 : 2;
+constexpr int fwd_blocks(int VEC, int V, int x) {
+  return VEC == 1 ? (V <= 4 ? 5 : V <= 8 ? 3 : 1) : V <= 2 ? 4 : x == 2 ? 3 : 2;
 }
 
 // Each team takes a run of rows, R at once where they are short in registers.
 template <class TX, class TY, int VEC, int V, bool RES>
-__global__ void __launch_bounds__(max_threads(VEC, V), fwd_blocks(VEC, V, sizeof(TX), RES))
+__global__ void __launch_bounds__(max_threads(VEC, V), fwd_blocks(VEC, V, sizeof(TX)))
     rms_fwd_kernel(const RmsParams p) {
   constexpr bool CODES = std::is_same_v<TY, E4m3>;
-  constexpr int R = VEC == 8 && V >= 3 && sizeof(TX) == 2 && !RES ? 2 : 1;
+  constexpr int R = VEC == 8 && V >= 3 && sizeof(TX) == 2 && !RES && !CODES ? 2 : 1;
   __shared__ Sums<R> red[2][16];
   const Team team(p.W);
   const TX* x = static_cast<const TX*>(p.x);
@@ -99,43 +99,60 @@ __global__ void __launch_bounds__(max_threads(VEC, V), fwd_blocks(VEC, V, sizeof
     rstd = team.sum(rstd, red[turn]);
 #pragma unroll
     for (int r = 0; r < R; ++r) rstd.v[r] = rsqrtf(rstd.v[r] * inv_c + p.eps);
+    if constexpr (CODES) {
+      // scale bytes of four of a thread's blocks to a word: 16 lanes hold a block, and the
+      // largest of them is found for four at once (lanes past the row's end hold zeros)
+      float v[V][VEC];
+      uint32_t bytes[(V + 3) / 4];
 #pragma unroll
-    for (int k = 0; k < V; ++k) {
-      const bool in = column(k) < p.C;
-      if (!CODES && !in) continue;
-      float w[VEC];
+      for (int k = 0; k < V; ++k) {
+        uint32_t top = 0u;
+        if (column(k) < p.C) {
+          float w[VEC];
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) w[e] = 1.f;
-      if (in && p.weight) load_param<VEC>(p.weight, p.param_f32, params + column(k), w);
+          for (int e = 0; e < VEC; ++e) w[e] = 1.f;
+          if (p.weight) load_param<VEC>(p.weight, p.param_f32, params + column(k), w);
+          raw[0][k].get(v[k]);
 #pragma unroll
-      for (int r = 0; r < R; ++r) {
-        if (r >= n) continue;
-        float v[VEC];
+          for (int e = 0; e < VEC; ++e) {
+            v[k][e] = v[k][e] * rstd.v[0] * w[e];
+            top = max(top, fp8_magnitude(v[k][e]));
+          }
+        }
+        const uint32_t byte = static_cast<uint32_t>(fp8_scale(top)) << (8 * (k % 4));
+        bytes[k / 4] = k % 4 == 0 ? byte : bytes[k / 4] | byte;
+      }
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) v[e] = 0.f;
-        if (in) {
+      for (int s = 8; s > 0; s >>= 1)
+#pragma unroll
+        for (int i = 0; i < (V + 3) / 4; ++i)
+          bytes[i] = __vmaxu4(bytes[i], __shfl_xor_sync(0xffffffffu, bytes[i], s));
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        if (column(k) >= p.C) continue;
+        const uint8_t scale = static_cast<uint8_t>(bytes[k / 4] >> (8 * (k % 4)));
+        const float inv = fp8_inverse(scale);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) v[k][e] *= inv;
+        *reinterpret_cast<uint2*>(static_cast<uint8_t*>(p.y) + row * p.C + column(k)) = fp8_codes(v[k]);
+        if ((team.t & 15) == 0) p.y_scale[row * ((p.C + 127) / 128) + (column(k) >> 7)] = scale;
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        if (column(k) >= p.C) continue;
+        float w[VEC];
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) w[e] = 1.f;
+        if (p.weight) load_param<VEC>(p.weight, p.param_f32, params + column(k), w);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          if (r >= n) continue;
+          float v[VEC];
           raw[r][k].get(v);
 #pragma unroll
           for (int e = 0; e < VEC; ++e) v[e] = v[e] * rstd.v[r] * w[e];
-        }
-        const size_t at = static_cast<size_t>(row + r) * p.C + column(k);
-        if constexpr (CODES) {
-          // (warps are whole here: a row's lanes past its end hold zeros)
-          uint32_t top = 0u;
-#pragma unroll
-          for (int e = 0; e < VEC; ++e) top = max(top, fp8_magnitude(v[e]));
-#pragma unroll
-          for (int s = 8; s > 0; s >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, s));
-          const uint8_t scale = fp8_scale(top);
-          const float inv = fp8_inverse(scale);
-#pragma unroll
-          for (int e = 0; e < VEC; ++e) v[e] *= inv;
-          if (in) {
-            *reinterpret_cast<uint2*>(static_cast<uint8_t*>(p.y) + at) = fp8_codes(v, scale);
-            if ((team.t & 15) == 0) p.y_scale[(row + r) * ((p.C + 127) / 128) + (column(k) >> 7)] = scale;
-          }
-        } else {
-          store_y<TY, VEC>(p.y, at, v);
+          store_y<TY, VEC>(p.y, static_cast<size_t>(row + r) * p.C + column(k), v);
         }
       }
     }
@@ -147,6 +164,210 @@ __global__ void __launch_bounds__(max_threads(VEC, V), fwd_blocks(VEC, V, sizeof
     if (p.groups > 1 && left == 0) {
       left = p.rows_per_group;
       params += p.C;
+    }
+  }
+}
+
+// A thread's ring in shared memory, of the rows kernels: [2][R][V] slots of `pieces` 16-byte
+// pieces for each thread of the block.  The 32 lanes of a warp copy the 8 columns of each of
+// them together, 512 bytes at a time (in fp32 a lane's own 32 bytes would make every copy
+// fetch half of each sector), so a warp waits for all of its lanes before it reads or copies.
+struct Ring {
+  uint32_t base;     // of the block
+  uint32_t threads, warp, lane;
+  int columns;       // of a row
+  int slots_k, pieces, rows;
+  template <class T>
+  __device__ __forceinline__ void copy(int stage, int r, int k, int from_piece, const T* row, int at_column) const {
+    constexpr int P = sizeof(T) / 2;
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const int c = at_column + (i * 32 + lane) * (16 / static_cast<int>(sizeof(T)));
+      if (c < columns) copy_16b(at<T>(stage, r, k, from_piece) + (i * 32 + lane) * 16, row + c);
+    }
+  }
+  template <class T>
+  __device__ __forceinline__ Raw<T, 8> read(int stage, int r, int k, int from_piece) const {
+    constexpr int P = sizeof(T) / 2;
+    Raw<T, 8> raw;
+#pragma unroll
+    for (int i = 0; i < P; ++i)
+      reinterpret_cast<uint4*>(&raw)[i] = shared_16b(at<T>(stage, r, k, from_piece) + (lane * P + i) * 16);
+    return raw;
+  }
+
+ private:
+  template <class T>
+  __device__ __forceinline__ uint32_t at(int stage, int r, int k, int from_piece) const {
+    constexpr int P = sizeof(T) / 2;
+    return base + 16 * threads * (((stage * rows + r) * slots_k + k) * pieces + from_piece) + warp * 512 * P;
+  }
+};
+
+// Many rows in 16-byte pieces, as the backward below: a team takes R rows at a time, every
+// thread copies its columns of the next ones to shared memory meanwhile, one barrier a
+// batch.  Block (part, group): rows [part n / parts, (part + 1) n / parts) of the group, whose
+// weight stays in registers.  Pieces of a thread's 8 columns: of x and the residual.
+template <class TX, bool RES>
+constexpr int kFwdPieces = sizeof(TX) / 2 * (RES ? 2 : 1);
+template <class TX, int V, bool RES>
+constexpr int kFwdRows = 4 / V / (kFwdPieces<TX, RES> > 2 ? 2 : 1);
+
+template <class TX, class TY, int V, bool RES>
+__global__ void __maxnreg__(V == 1 ? 80 : 128) rms_fwd_rows_kernel(const RmsParams p) {
+  constexpr bool CODES = std::is_same_v<TY, E4m3>;
+  constexpr int R = kFwdRows<TX, V, RES>, PX = sizeof(TX) / 2, PIECES = kFwdPieces<TX, RES>;
+  __shared__ float red[2][16][R];
+  extern __shared__ __align__(16) uint8_t ring[];  // [2][R][V][PIECES][threads] pieces
+  const Team team(p.W);
+  const TX* x = static_cast<const TX*>(p.x);
+  [[maybe_unused]] const TX* res = static_cast<const TX*>(p.residual);
+  [[maybe_unused]] TX* hs = static_cast<TX*>(p.h);
+  const int lane = threadIdx.x & 31;
+  const float inv_c = 1.f / static_cast<float>(p.C);
+  const int part = blockIdx.x % p.parts;
+  const long long group = blockIdx.x / p.parts;
+  const long long n = p.rows_per_group;
+  const long long r0 = group * n + part * n / p.parts, r1 = group * n + (part + 1) * n / p.parts;
+  const size_t g = static_cast<size_t>(group) * p.C;
+  auto column = [&](int k) { return (k * team.W * 32 + team.t) * 8; };
+  const Ring slots{smem_u32(ring), blockDim.x, threadIdx.x >> 5, threadIdx.x & 31, p.C, V, PIECES, R};
+  auto warp_column = [&](int k) { return (k * team.W + team.warp) * 256; };
+  pdl_wait();
+  pdl_trigger();
+  auto fetch = [&](long long row, int stage) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      if (row + r >= r1) continue;
+      const size_t from = static_cast<size_t>(row + r) * p.C;
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        slots.copy(stage, r, k, 0, x + from, warp_column(k));
+        if constexpr (RES) slots.copy(stage, r, k, PX, res + from, warp_column(k));
+      }
+    }
+  };
+  long long row = r0 + static_cast<long long>(team.index) * R;
+  const long long step = static_cast<long long>(team.count) * R;
+  fetch(row, 0);
+  copy_commit();
+  float2 w[V][4];
+#pragma unroll
+  for (int k = 0; k < V; ++k) {
+    float one[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
+    if (p.weight && column(k) < p.C) load_param<8>(p.weight, p.param_f32, g + column(k), one);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[k][e] = make_float2(one[2 * e], one[2 * e + 1]);
+  }
+  for (int turn = 0; row < r1; row += step, turn ^= 1) {
+    __syncwarp();
+    fetch(row + step, turn ^ 1);
+    copy_commit();
+    copy_wait<1>();
+    __syncwarp();
+    Raw<TX, 8> held[R][V];
+    float s[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      s[r] = 0.f;
+      if (row + r >= r1) continue;
+      float2 s2 = make_float2(0.f, 0.f);
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        if (column(k) >= p.C) continue;
+        held[r][k] = slots.read<TX>(turn, r, k, 0);
+        float v[8];
+        held[r][k].get(v);
+        if constexpr (RES) {
+          float a[8];
+          slots.read<TX>(turn, r, k, PX).get(a);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] += a[e];
+          held[r][k].put(v);
+          held[r][k].get(v);
+          store<8>(hs + static_cast<size_t>(row + r) * p.C + column(k), v);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float2 u = make_float2(v[2 * e], v[2 * e + 1]);
+          s2 = fma2(u, u, s2);
+        }
+      }
+      s[r] = s2.x + s2.y;
+    }
+    float sum = warp_sums<R>(s);
+    constexpr int kShare = 32 / R;  // lanes of a value
+    int from = kShare;
+    if (p.W > 1) {
+      if (lane % kShare == 0) red[turn][team.index * p.W + team.warp][lane / kShare] = sum;
+      asm volatile("bar.sync %0, %1;" ::"r"(team.index + 1), "r"(p.W * 32) : "memory");
+      sum = 0.f;
+      for (int i = lane / R; i < p.W; i += kShare) sum += red[turn][team.index * p.W + i][lane % R];
+#pragma unroll
+      for (int m = R; m < 32; m *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, m);
+      from = 1;
+    }
+    sum = rsqrtf(sum * inv_c + p.eps);
+    float rstd[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) rstd[r] = __shfl_sync(0xffffffffu, sum, r * from);
+    if (team.t == 0 && p.rstd) {
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+        if (row + r < r1) p.rstd[row + r] = rstd[r];
+    }
+    // y of a row's columns
+    auto result = [&](int r, int k, float2 (&y)[4]) {
+      float v[8];
+      held[r][k].get(v);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        y[e] = mul2(mul2(make_float2(v[2 * e], v[2 * e + 1]), make_float2(rstd[r], rstd[r])), w[k][e]);
+    };
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      const bool in = column(k) < p.C;
+      if constexpr (CODES) {
+        // scale bytes of the rows: 16 lanes hold a block, and the largest is found for all rows
+        // at once (lanes past the row's end hold zeros)
+        // (y is worked out twice: held for all rows it spilled, 14080 x 2560 bf16 43 -> 55 us)
+        uint32_t bytes = 0u;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          if (!in || row + r >= r1) continue;
+          float2 y[4];
+          result(r, k, y);
+          uint32_t top = 0u;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) top = max(top, max(fp8_magnitude(y[e].x), fp8_magnitude(y[e].y)));
+          bytes |= static_cast<uint32_t>(fp8_scale(top)) << (8 * r);
+        }
+#pragma unroll
+        for (int i = 8; i > 0; i >>= 1) bytes = __vmaxu4(bytes, __shfl_xor_sync(0xffffffffu, bytes, i));
+        if (!in) continue;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          if (row + r >= r1) continue;
+          float2 y[4];
+          result(r, k, y);
+          const uint8_t scale = static_cast<uint8_t>(bytes >> (8 * r));
+          const float inv = fp8_inverse(scale);
+          const float2 by = make_float2(inv, inv);
+          *reinterpret_cast<uint2*>(static_cast<uint8_t*>(p.y) + (row + r) * p.C + column(k)) =
+              make_uint2(fp8_four(mul2(y[0], by), mul2(y[1], by)), fp8_four(mul2(y[2], by), mul2(y[3], by)));
+          if ((team.t & 15) == 0) p.y_scale[(row + r) * ((p.C + 127) / 128) + (column(k) >> 7)] = scale;
+        }
+      } else {
+        if (!in) continue;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          if (row + r >= r1) continue;
+          float2 y[4];
+          result(r, k, y);
+          const float v[8] = {y[0].x, y[0].y, y[1].x, y[1].y, y[2].x, y[2].y, y[3].x, y[3].y};
+          store_y<TY, 8>(p.y, static_cast<size_t>(row + r) * p.C + column(k), v);
+        }
+      }
     }
   }
 }
@@ -273,9 +494,8 @@ __global__ void __maxnreg__(V == 1 ? 80 : 128) rms_bwd_rows_kernel(const RmsPara
   const long long r0 = group * n + part * n / p.parts, r1 = group * n + (part + 1) * n / p.parts;
   const size_t g = static_cast<size_t>(group) * p.C;
   auto column = [&](int k) { return (k * team.W * 32 + team.t) * 8; };
-  const uint32_t mine = smem_u32(ring) + 16 * threadIdx.x;
-  const uint32_t piece = 16 * blockDim.x;
-  auto at = [&](int stage, int r, int k, int i) { return mine + piece * (((stage * R + r) * V + k) * PIECES + i); };
+  const Ring slots{smem_u32(ring), blockDim.x, threadIdx.x >> 5, threadIdx.x & 31, p.C, V, PIECES, R};
+  auto warp_column = [&](int k) { return (k * team.W + team.warp) * 256; };
   pdl_wait();
   pdl_trigger();
   float rstd[R], next_rstd[R];
@@ -284,19 +504,12 @@ __global__ void __maxnreg__(V == 1 ? 80 : 128) rms_bwd_rows_kernel(const RmsPara
     for (int r = 0; r < R; ++r) {
       if (row + r >= r1) continue;
       next_rstd[r] = p.rstd[row + r];
+      const size_t from = static_cast<size_t>(row + r) * p.C;
 #pragma unroll
       for (int k = 0; k < V; ++k) {
-        if (column(k) >= p.C) continue;
-        const size_t from = static_cast<size_t>(row + r) * p.C + column(k);
-#pragma unroll
-        for (int i = 0; i < PX; ++i) copy_16b(at(stage, r, k, i), reinterpret_cast<const uint4*>(h + from) + i);
-#pragma unroll
-        for (int i = 0; i < PY; ++i) copy_16b(at(stage, r, k, PX + i), reinterpret_cast<const uint4*>(dy + from) + i);
-        if constexpr (DH) {
-#pragma unroll
-          for (int i = 0; i < PX; ++i)
-            copy_16b(at(stage, r, k, PX + PY + i), reinterpret_cast<const uint4*>(dh + from) + i);
-        }
+        slots.copy(stage, r, k, 0, h + from, warp_column(k));
+        slots.copy(stage, r, k, PX, dy + from, warp_column(k));
+        if constexpr (DH) slots.copy(stage, r, k, PX + PY, dh + from, warp_column(k));
       }
     }
   };
@@ -320,13 +533,8 @@ __global__ void __maxnreg__(V == 1 ? 80 : 128) rms_bwd_rows_kernel(const RmsPara
   }
   // 8 columns of a row as fp32, from piece `first` on
   auto read = [&](auto like, int stage, int r, int k, int first, float2 (&v)[4]) {
-    using T = decltype(like);
-    Raw<T, 8> raw;
-#pragma unroll
-    for (int i = 0; i < static_cast<int>(sizeof(T)) / 2; ++i)
-      reinterpret_cast<uint4*>(&raw)[i] = shared_16b(at(stage, r, k, first + i));
     float f[8];
-    raw.get(f);
+    slots.read<decltype(like)>(stage, r, k, first).get(f);
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] = make_float2(f[2 * e], f[2 * e + 1]);
   };
@@ -334,9 +542,11 @@ __global__ void __maxnreg__(V == 1 ? 80 : 128) rms_bwd_rows_kernel(const RmsPara
   for (int turn = 0; row < r1; row += step, turn ^= 1) {
 #pragma unroll
     for (int r = 0; r < R; ++r) rstd[r] = next_rstd[r];
+    __syncwarp();
     fetch(row + step, turn ^ 1);
     copy_commit();
     copy_wait<1>();
+    __syncwarp();
     float s[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
@@ -444,16 +654,35 @@ __global__ void __launch_bounds__(256) rms_weight_kernel(const RmsParams p, int 
   }
 }
 
+// The rows kernels' shared memory: the rows' ring (of 512 threads in fp32 with dh: two stages of
+// two times six pieces), or the sums of the widest row.
+constexpr int kRmsMaxSmem = 2 * 2 * 6 * 16 * 512;
+static_assert(kRmsMaxSmem >= kNormMaxC * static_cast<int>(sizeof(float)), "the sums fit");
+
 template <class X, class Y, int VEC, int V, bool RES>
 cudaError_t run_fwd(const RmsParams& p, const Shape& sh, int sms, cudaStream_t s) {
   const int teams = sh.threads / 32 / sh.W;
   const long long blocks = (p.rows + teams - 1) / teams;
   // as many blocks as the SMs hold (of fewer threads, more)
-  const long long most = static_cast<long long>(sms) * fwd_blocks(VEC, V, sizeof(X), RES) * 256 / sh.threads;
+  const long long most = static_cast<long long>(sms) * fwd_blocks(VEC, V, sizeof(X)) * 256 / sh.threads;
   cudaLaunchConfig_t cfg;
   cudaLaunchAttribute attr;
   pdl_config(cfg, attr, dim3(static_cast<unsigned>(blocks < most ? blocks : most)), dim3(sh.threads), 0, s);
   return cudaLaunchKernelEx(&cfg, rms_fwd_kernel<X, Y, VEC, V, RES>, p);
+}
+
+template <class X, class Y, int V, bool RES>
+cudaError_t run_fwd_rows(const RmsParams& p, const RowsShape& sh, int dev, cudaStream_t s) {
+  constexpr auto kKernel = rms_fwd_rows_kernel<X, Y, V, RES>;
+  const size_t ring = static_cast<size_t>(2) * kFwdRows<X, V, RES> * V * kFwdPieces<X, RES> * 16 * sh.threads;
+  static OncePerDevice prepared;
+  const cudaError_t e = prepared(
+      dev, [] { return cudaFuncSetAttribute(kKernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRmsMaxSmem); });
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg;
+  cudaLaunchAttribute attr;
+  pdl_config(cfg, attr, dim3(static_cast<unsigned>(p.groups) * p.parts), dim3(sh.threads), ring, s);
+  return cudaLaunchKernelEx(&cfg, kKernel, p);
 }
 
 template <class X, class Y, bool RES>
@@ -462,9 +691,7 @@ cudaError_t run_fwd_shape(const RmsParams& p, bool vec, const Shape& sh, int sms
     if (sh.V == 1) return run_fwd<X, Y, 8, 1, RES>(p, sh, sms, s);
     if (sh.V == 2) return run_fwd<X, Y, 8, 2, RES>(p, sh, sms, s);
     if (sh.V == 3) return run_fwd<X, Y, 8, 3, RES>(p, sh, sms, s);
-    if (sh.V == 4) return run_fwd<X, Y, 8, 4, RES>(p, sh, sms, s);
-    if (sh.V == 6) return run_fwd<X, Y, 8, 6, RES>(p, sh, sms, s);
-    return run_fwd<X, Y, 8, 10, RES>(p, sh, sms, s);
+    return run_fwd<X, Y, 8, 4, RES>(p, sh, sms, s);
   }
   if constexpr (!std::is_same_v<Y, E4m3>) {
     if (sh.V == 2) return run_fwd<X, Y, 1, 2, RES>(p, sh, sms, s);
@@ -474,11 +701,6 @@ cudaError_t run_fwd_shape(const RmsParams& p, bool vec, const Shape& sh, int sms
   }
   return cudaErrorInvalidValue;  // (codes are written in pieces of eight)
 }
-
-// The backward's shared memory: the rows' ring (of 512 threads in fp32 with dh: two stages of
-// two times six pieces), or the sums of the widest row.
-constexpr int kRmsMaxSmem = 2 * 2 * 6 * 16 * 512;
-static_assert(kRmsMaxSmem >= kNormMaxC * static_cast<int>(sizeof(float)), "the sums fit");
 
 template <auto kKernel>
 cudaError_t run_bwd(const RmsParams& p, unsigned blocks, int threads, size_t smem, int dev, cudaStream_t s) {
@@ -515,19 +737,31 @@ int rms_parts(long long rows_per_group, int C, int groups) {
   return parts < 1 ? 1 : static_cast<int>(parts);
 }
 
-cudaError_t launch_rms_fwd(RmsParams p, bool vec, int sms, cudaStream_t s) {
-  const Shape sh = shape_of(p.C, vec, p.rows <= 8ll * sms);
-  p.W = sh.W;
-  auto types = [&](auto res) {
-    constexpr bool RES = decltype(res)::value;
-    if (p.y_type == kRmsCodes)
-      return p.x_f32 ? run_fwd_shape<float, E4m3, RES>(p, vec, sh, sms, s)
-                     : run_fwd_shape<bf16, E4m3, RES>(p, vec, sh, sms, s);
-    if (!p.x_f32) return run_fwd_shape<bf16, bf16, RES>(p, vec, sh, sms, s);
-    if (p.y_type == kRmsF32) return run_fwd_shape<float, float, RES>(p, vec, sh, sms, s);
-    return run_fwd_shape<float, bf16, RES>(p, vec, sh, sms, s);
+cudaError_t launch_rms_fwd(RmsParams p, bool vec, int dev, int sms, cudaStream_t s) {
+  auto types = [&](auto f) {
+    if (p.y_type == kRmsCodes) return p.x_f32 ? f(float{}, E4m3{}) : f(bf16{}, E4m3{});
+    if (!p.x_f32) return f(bf16{}, bf16{});
+    return p.y_type == kRmsF32 ? f(float{}, float{}) : f(float{}, bf16{});
   };
-  return p.residual ? types(std::true_type{}) : types(std::false_type{});
+  if (vec && p.rows > 8ll * sms) {
+    const RowsShape sh = rows_shape(p.C);
+    p.W = sh.W;
+    p.parts = rms_parts(p.rows_per_group, p.C, p.groups);
+    return types([&](auto tx, auto ty) {
+      using X = decltype(tx);
+      using Y = decltype(ty);
+      if (sh.V == 1)
+        return p.residual ? run_fwd_rows<X, Y, 1, true>(p, sh, dev, s) : run_fwd_rows<X, Y, 1, false>(p, sh, dev, s);
+      return p.residual ? run_fwd_rows<X, Y, 2, true>(p, sh, dev, s) : run_fwd_rows<X, Y, 2, false>(p, sh, dev, s);
+    });
+  }
+  const Shape sh = shape_of(p.C, vec, true);
+  p.W = sh.W;
+  return types([&](auto tx, auto ty) {
+    using X = decltype(tx);
+    using Y = decltype(ty);
+    return p.residual ? run_fwd_shape<X, Y, true>(p, vec, sh, sms, s) : run_fwd_shape<X, Y, false>(p, vec, sh, sms, s);
+  });
 }
 
 cudaError_t launch_rms_bwd(RmsParams p, bool vec, int dev, cudaStream_t s) {
