@@ -36,39 +36,44 @@ struct MmPlan {
   bool join = false, swap = false;
 };
 
+// Clusters of r CTAs that run at once, a CTA an SM: eight groups of SMs, each of which holds
+// whole clusters.
+int clusters_at_once(int r, int sms) { return std::max(1, 8 * (sms / 8 / r)); }
+
 MmPlan mm_plan(int M, int N, int blocks, bool a_columns, bool b_columns, bool f32, int sms) {
   MmPlan best;
+  const int most = std::min(kFp8Splits, blocks);
+  double best_cost = INFINITY;
   const bool few_m = M <= 64 && !a_columns, few_n = N <= 64 && !b_columns;
   if (few_m || few_n) {
     const int few = few_m ? M : N, tiles = ceil_div(few_m ? N : M, 128);
     best.swap = few_m;
     best.join = true;
     best.bn = few <= 16 ? 16 : few <= 32 ? 32 : 64;
-    best.splits = std::max(1, std::min({8, blocks, 2 * sms / tiles}));
+    // blocks that a CTA goes through; clusters past those that run at once share SMs, which
+    // costs more than their number (us for 1 to 8 CTAs: 8 x 2560 x 10240 21.2 12.7 10.2 8.6 8.0
+    // 7.9 8.3 8.3; 16 x 7680 x 2560 8.8 7.4 7.6 7.2 11.2 11.5 12.1 12.4)
+    for (int r = 1; r <= most; ++r) {
+      const double load = std::max(1.0, static_cast<double>(tiles) / clusters_at_once(r, sms));
+      const double cost = ceil_div(blocks, r) * load * load;
+      if (cost < best_cost) best_cost = cost, best.splits = r;
+    }
     return best;
   }
-  // cycles: a stage, what a tile adds, what a launch does
-  double best_cost = INFINITY;
-  auto consider = [&](int bn, bool join, int splits) {
-    double cost;
-    if (join) {
-      const long long tiles = static_cast<long long>(ceil_div(M, 128)) * ceil_div(N, bn);
-      cost = ceil_div(tiles * splits, sms) * (ceil_div(blocks, splits) * 560.0 + 9000) + 3000;
-    } else {
-      const long long tiles = static_cast<long long>(ceil_div(M, 256)) * ceil_div(N, bn);
-      cost = ceil_div(tiles, sms / 2) * (blocks * (bn == 256 ? 800.0 : 630.0) + 500) + 6000;
-    }
-    if (cost < best_cost) {
-      best_cost = cost;
-      best.bn = bn;
-      best.join = join;
-      best.splits = splits;
-    }
+  // us, fitted to 14 sizes: what a launch takes, a block of the contraction, a tile
+  auto take = [&](int bn, bool join, int splits, double cost) {
+    if (cost < best_cost) best_cost = cost, best.bn = bn, best.join = join, best.splits = splits;
   };
-  consider(256, false, 1);
-  consider(128, false, 1);
-  for (int s = 1; s <= 8 && s <= blocks; ++s)
-    if (!f32 || ceil_div(blocks, s) <= kFp8Chunk) consider(128, true, s);
+  auto tiles = [&](int rows, int bn) { return static_cast<long long>(ceil_div(M, rows)) * ceil_div(N, bn); };
+  take(256, false, 1, 4.8 + ceil_div(tiles(256, 256), sms / 2) * (0.265 * blocks + 1.0));
+  take(128, false, 1, 4.0 + ceil_div(tiles(256, 128), sms / 2) * (0.26 * blocks + 0.5));
+  for (int r = 1; r <= most; ++r) {
+    const int share = ceil_div(blocks, r);
+    if (f32 && share > kFp8Chunk) continue;
+    const double load = static_cast<double>(tiles(128, 128)) / clusters_at_once(r, sms);
+    const bool once = load <= 1.15 && tiles(128, 128) * r <= sms;
+    take(128, true, r, (once ? 1.0 : std::max(2.0, std::ceil(load))) * (7.1 + 0.225 * share));
+  }
   return best;
 }
 

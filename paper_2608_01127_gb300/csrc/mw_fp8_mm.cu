@@ -367,15 +367,16 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         for (int k = 0; k < n_boxes; ++k) {
           const int c0 = half * (BN / 2) + (backwards ? n_boxes - 1 - k : k) * per;
           uint32_t w[32], v[32];
+          const bool free_now = frees && (L::OVERLAP ? k == 0 : k == n_boxes - 1);
           if (ok) {
-            tmem_ld32(acc + c0, w);
             if (!p.out_f32) tmem_ld32(acc + c0 + 32, v);
+            tmem_ld32(acc + c0, w);
             tmem_wait_ld();
           } else {
 #pragma unroll
             for (int e = 0; e < 32; ++e) w[e] = v[e] = 0u;
           }
-          if (frees && (L::OVERLAP ? k == 0 : k == n_boxes - 1)) {  // (a box covers the overlap's 32 columns)
+          if (free_now) {  // (a box covers the overlap's 32 columns)
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster(freed + 8 * (j & 1));
@@ -442,31 +443,36 @@ __global__ void __launch_bounds__(kPairThreads, 1)
 //
 // Few rows of one operand (16, 32 or 64 of them are the B of 128 of the other's: a token's
 // product reads weights), or few tiles and a long contraction: the CTAs of a cluster take
-// each a share of the blocks, and add their parts up through each other's shared memory, in
-// the order of their ranks.
+// each a share of the blocks, and each adds up a share of the tile in the order of the ranks.
+// Up to 16 rows (SEND) a CTA owns a share of the tile's rows, and all send it their parts of
+// these.  More than that is left where it was made and read from there, 16 bytes at a time,
+// which takes two more trips through the cluster but moves parts faster (us, sent / read: one
+// token x 2304 x 768 3.1 / 3.5; 64 x 7680 x 2560 16.3 / 13.8).
 
 template <int BN>
 struct JoinLayout {
+  static constexpr bool SEND = BN == 16;
   static constexpr int B = BN * kBlock;  // (columns of B: 128 at a time, so BN = 128 there)
   static constexpr int STAGE = kA + B;
   static constexpr int ATOMS = 2;
   static constexpr int SETS = 4;
-  static constexpr int STAGES = BN == 128 ? 6 : 4;
-  static constexpr int OFF_SCALE = STAGES * STAGE;
+  static constexpr int STAGES = BN == 128 ? 6 : SEND ? 5 : 4;
+  // SEND: parts of the CTA's rows, [ranks][BN][rows] at an odd pitch: 128 to 138 floats a
+  // column; else the CTA's part, in the stages' place
+  static constexpr int PARTS = SEND ? BN * 138 * 4 : 0;
+  static constexpr int OFF_PARTS = SEND ? STAGES * STAGE : 0;
+  static constexpr int OFF_SCALE = STAGES * STAGE + (PARTS + 511) / 512 * 512;
   static constexpr int OFF_BAR = OFF_SCALE + SETS * ATOMS * 512;
   static constexpr int N_BAR = 2 * STAGES + 2 * SETS + 2;
   static constexpr int OFF_MISC = OFF_BAR + N_BAR * 8;
   static constexpr int SMEM = OFF_MISC + 16;
-  static_assert(SMEM <= 232448, "shared memory of a CTA");
+  static_assert(SMEM <= (BN <= 64 ? 233472 / 2 - 1024 : 232448), "shared memory of a CTA, of which an SM holds two up to 64");
   static constexpr int SCALES = BN;      // columns of tensor memory: the accumulator, the scale words
   static constexpr int WORDS = 4 * ATOMS;
   static constexpr int USED = SCALES + SETS * WORDS;
   static constexpr int COLS = USED <= 64 ? 64 : USED <= 128 ? 128 : 256;
-  // the parts that a cluster adds up: rows of a padded pitch
-  static constexpr int PART = ((BN + 4) * 128 > 132 * BN ? (BN + 4) * 128 : 132 * BN) * 4;
-  static_assert(PART <= STAGES * STAGE, "the parts take the stages' place");
+  static_assert(((BN + 4) * 128 > 132 * BN ? (BN + 4) * 128 : 132 * BN) * 4 <= STAGES * STAGE, "a part fits");
 };
-
 // Four results in a row of the output, of which n count.
 __device__ __forceinline__ void store_four(const Fp8MmParams& p, long long at, float4 v, int n) {
   if (n >= 4 && p.out_quads) {
@@ -487,6 +493,13 @@ __device__ __forceinline__ void store_four(const Fp8MmParams& p, long long at, f
       static_cast<__nv_bfloat16*>(p.out)[at + i] = __float2bfloat16(e[i]);
   }
 }
+
+// The rows [r0, r1) of 128 that a rank owns, and their pitch.
+struct OwnRows {
+  int r0, r1;
+  __device__ __forceinline__ OwnRows(int rank, int ranks) : r0(128 * rank / ranks), r1(128 * (rank + 1) / ranks) {}
+  __device__ __forceinline__ int pitch() const { return (r1 - r0) | 1; }
+};
 
 template <int BN>
 __global__ void __launch_bounds__(kThreads, BN <= 64 ? 2 : 1)
@@ -524,14 +537,14 @@ __global__ void __launch_bounds__(kThreads, BN <= 64 ? 2 : 1)
   tc_fence_after();
   const uint32_t tmem = *tmem_at;
   const WaitCtl ctl{abort_flag, p.status, p.budget_ns};
-  pdl_wait();
-  pdl_trigger();
-
+  cluster_arrive();  // (this CTA is there)
   cg::cluster_group cluster = cg::this_cluster();
   const int rank = static_cast<int>(cluster.block_rank()), ranks = static_cast<int>(cluster.num_blocks());
   int tp, tq;
   tile_at(p, blockIdx.x / ranks, &tp, &tq);
   const int kb0 = p.blocks * rank / ranks, kb1 = p.blocks * (rank + 1) / ranks;
+  pdl_wait();
+  pdl_trigger();
 
   if (warp == 0) {
     // ------------------------------------------------------------ tiles of A and B
@@ -612,12 +625,19 @@ __global__ void __launch_bounds__(kThreads, BN <= 64 ? 2 : 1)
   } else if (warp >= 4) {
     // ------------------------------------------------------------ this CTA's part
     const int row = (warp - 4) * 32 + lane;
+    int owner = row * ranks / 128;
+    if (OwnRows(owner, ranks).r1 <= row) ++owner;
+    const OwnRows own(owner, ranks);
+    [[maybe_unused]] const uint32_t to = cluster_address(smem_u32(smem + L::OFF_PARTS), owner) +
+                                         4 * (rank * BN * own.pitch() + row - own.r0);
+    [[maybe_unused]] float* part = reinterpret_cast<float*>(smem);
+    const int n = min(BN, p.rows_b - tq * BN);
     const bool ok = aligned && warp_wait(acc_full, 0, ctl);
     tc_fence_after();
     const uint32_t acc = tmem + (static_cast<uint32_t>((warp - 4) * 32) << 16);
-    float* part = reinterpret_cast<float*>(smem);
+    cluster_wait();  // all CTAs are there
 #pragma unroll 1
-    for (int c = 0; c < BN; c += 16) {
+    for (int c = 0; c < n; c += 16) {
       uint32_t v[16];
       if (ok) {
         tmem_ld16(acc + c, v);
@@ -626,7 +646,11 @@ __global__ void __launch_bounds__(kThreads, BN <= 64 ? 2 : 1)
 #pragma unroll
         for (int k = 0; k < 16; ++k) v[k] = 0u;
       }
-      if (p.swap) {
+      if constexpr (L::SEND) {
+#pragma unroll
+        for (int k = 0; k < 16; ++k)
+          if (c + k < n) store_cluster(to + 4 * (c + k) * own.pitch(), v[k]);
+      } else if (p.swap) {
 #pragma unroll
         for (int k = 0; k < 16; ++k) part[(c + k) * 132 + row] = __uint_as_float(v[k]);
       } else {
@@ -637,12 +661,32 @@ __global__ void __launch_bounds__(kThreads, BN <= 64 ? 2 : 1)
     }
     __syncwarp();
   }
+  if (warp < 4) cluster_wait();
 
-  // ------------------------------------------------------------ every CTA adds up a share of the tile
+  // ------------------------------------------------------------ the sums of this CTA's share
   tc_fence_before();
-  cluster.sync();
-  {
+  cluster_arrive();
+  cluster_wait();
+  if constexpr (L::SEND) {
+    const OwnRows own(rank, ranks);
+    const int pitch = own.pitch(), rows = min(own.r1, p.rows_a - tp * 128) - own.r0, n = min(BN, p.rows_b - tq * BN);
+    const float* parts = reinterpret_cast<const float*>(smem + L::OFF_PARTS);
     // swapped: a row of the output is a row of B, and runs over A's rows
+    const int inner = p.swap ? rows : n, outer = p.swap ? n : rows;
+    const long long o0 = p.swap ? tq * BN : tp * 128 + own.r0, i0 = p.swap ? tp * 128 + own.r0 : tq * BN;
+    const int wide = inner > 32 ? 64 : 32;  // threads to a row of the output
+    for (int o = threadIdx.x / wide; o < outer; o += kThreads / wide)
+      for (int i = threadIdx.x % wide; i < inner; i += wide) {
+        const float* at = parts + (p.swap ? o : i) * pitch + (p.swap ? i : o);
+        float s = at[0];
+        for (int r = 1; r < ranks; ++r) s += at[r * BN * pitch];
+        const long long dst = (o0 + o) * p.ld + i0 + i;
+        if (p.out_f32)
+          static_cast<float*>(p.out)[dst] = s;
+        else
+          static_cast<__nv_bfloat16*>(p.out)[dst] = __float2bfloat16(s);
+      }
+  } else {
     const int inner = p.swap ? 128 : BN, pitch = inner + 4;
     const int o0 = p.swap ? tq * BN : tp * 128, i0 = p.swap ? tp * 128 : tq * BN;
     const int outer = min(p.swap ? BN : 128, (p.swap ? p.rows_b : p.rows_a) - o0);
@@ -652,15 +696,21 @@ __global__ void __launch_bounds__(kThreads, BN <= 64 ? 2 : 1)
     float* part = reinterpret_cast<float*>(smem);
     for (int e = q0 + threadIdx.x; e < q1; e += kThreads) {
       const int o = e / (inner / 4), i = e % (inner / 4) * 4;
-      float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (int r = 0; r < ranks; ++r) {
-        const float4 v = *reinterpret_cast<const float4*>(cluster.map_shared_rank(part, r) + o * pitch + i);
-        s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
-      }
-      if (i < in_n) store_four(p, static_cast<long long>(o0 + o) * p.ld + i0 + i, s, in_n - i);
+      if (i >= in_n) continue;
+      // (all on their way at once: one after another, eight of them took 5 us)
+      float4 v[kFp8Splits];
+#pragma unroll
+      for (int r = 0; r < kFp8Splits; ++r)
+        if (r < ranks) v[r] = *reinterpret_cast<const float4*>(cluster.map_shared_rank(part, r) + o * pitch + i);
+      float4 s = v[0];
+#pragma unroll
+      for (int r = 1; r < kFp8Splits; ++r)
+        if (r < ranks) s.x += v[r].x, s.y += v[r].y, s.z += v[r].z, s.w += v[r].w;
+      store_four(p, static_cast<long long>(o0 + o) * p.ld + i0 + i, s, in_n - i);
     }
+    cluster_arrive();  // shared memory stays until all have read it
+    cluster_wait();
   }
-  cluster.sync();  // shared memory stays until all have read it
   if (warp == 1) {
     tc_fence_after();
     tmem_dealloc(tmem, L::COLS);

@@ -341,6 +341,7 @@ cudaError_t launch_xattn_bwd(int d, int dm, const XattnBwdMaps& m, const XattnBw
 // Matrices in 8 bits (e4m3) with a scale (e8m0) for every block of 128: of a row's
 // elements (rows), of a column's (columns), or of both (tiles).
 constexpr int kFp8Block = 128;
+constexpr int kFp8Splits = 8;  // CTAs that share a contraction at most
 constexpr int kFp8Chunk = 64;  // blocks that an fp32 result sums in tensor memory at most
 struct Fp8FormParams {
   const void* x;         // [rows, C], bf16 or fp32

@@ -56,25 +56,21 @@ __device__ __forceinline__ bool mbar_try_wait(uint64_t* bar, uint32_t parity) {
   return ok != 0;
 }
 
-// The same where what the other CTA of a pair wrote is read next.
-__device__ __forceinline__ bool mbar_try_wait_cluster(uint64_t* bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}\n"
-      : "=r"(ok)
-      : "r"(smem_u32(bar)), "r"(parity)
-      : "memory");
-  return ok != 0;
-}
-
 // The shared-memory address `addr` of this CTA in CTA `rank` of the cluster.
 __device__ __forceinline__ uint32_t cluster_address(uint32_t addr, uint32_t rank) {
   uint32_t r;
   asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
   return r;
 }
+
+// A value into a CTA's shared memory, wherever in the cluster.
+__device__ __forceinline__ void store_cluster(uint32_t cluster_addr, uint32_t v) {
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(cluster_addr), "r"(v) : "memory");
+}
+
+// The cluster's barrier in halves, for threads on ways of their own.
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
@@ -97,10 +93,9 @@ __device__ __forceinline__ bool skips_loads(int hook) { return (hook >> (blockId
 // status word and returns false.  Never traps.  The abort flag and the clock
 // are looked at only every 32nd poll (try_wait itself suspends the thread for
 // a while): a read of the clock before the first one delayed every wait.
-template <bool CLUSTER = false>
 __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, const WaitCtl& ctl) {
   uint64_t t0 = 0;
-  for (uint32_t spins = 1; !(CLUSTER ? mbar_try_wait_cluster(bar, parity) : mbar_try_wait(bar, parity)); ++spins) {
+  for (uint32_t spins = 1; !mbar_try_wait(bar, parity); ++spins) {
     if ((spins & 31u) != 0u) continue;
     if (*ctl.abort) return false;
     const uint64_t t = global_timer_ns();
@@ -118,11 +113,9 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, const 
 // that .sync.aligned tcgen05 instructions after it are never divergent.  The
 // loop itself is uniform (a vote a poll): a vote over mbar_wait's answers
 // took 104 cycles for a phase that was complete already, this form 59.
-template <bool CLUSTER = false>
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, const WaitCtl& ctl) {
   uint64_t t0 = 0;
-  for (uint32_t spins = 1; !__all_sync(0xffffffffu, CLUSTER ? mbar_try_wait_cluster(bar, parity) : mbar_try_wait(bar, parity));
-       ++spins) {
+  for (uint32_t spins = 1; !__all_sync(0xffffffffu, mbar_try_wait(bar, parity)); ++spins) {
     if ((spins & 31u) != 0u) continue;
     const uint64_t t = global_timer_ns();
     if (t0 == 0) t0 = t;
