@@ -1244,23 +1244,70 @@ PyObject* rms_apply(PyObject*, PyObject* const* a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
-struct Fp8LinearBackward : public torch::autograd::Node {
-  SavedVariable xc, xcs, wq, ws;  // x in columns, where the weight wants a gradient; the weight
-  std::vector<int64_t> x_sizes, y_sizes;
-  int64_t M = 0;
-  int K = 0, N = 0, xt = 0, yt = 0, wt = 0;
+// Arrays that lie one after another in one allocation (one of its own each would take as
+// long as a launch).
+struct Pack {
+  int64_t bytes = 0;
+  int64_t add(int64_t n) {  // where it starts
+    const int64_t at = bytes;
+    bytes += (n + 255) / 256 * 256;
+    return at;
+  }
+};
+// An 8-bit form in a pack: rows (or tiles), and columns.
+struct PackedForm {
+  int64_t q = 0, scale = 0, qc = 0, sc = 0;
+  PackedForm() = default;
+  PackedForm(Pack* to, int64_t rows, int64_t C, int form) {
+    if (form != MW_FP8_COLUMNS) {
+      q = to->add(rows * C);
+      scale = to->add((form == MW_FP8_TILES ? blocks128(rows) : rows) * blocks128(C));
+    }
+    if (form == MW_FP8_COLUMNS || form == MW_FP8_ROWS_AND_COLUMNS) {
+      qc = to->add(rows * C);
+      sc = to->add(blocks128(rows) * C);
+    }
+  }
+};
+
+// y = x W^T with K, N multiples of 16.  Kept for the backward: W's form, and x's in columns
+// where W wants a gradient; x's in rows lives as long as the call.
+struct Linear {
+  int64_t M = 0, K = 0, N = 0;
+  int xt = -1, wt = -1, yt = -1;
   bool columns = false;
+  PackedForm w, x, xc;
+  Pack kept, scratch;
+  void plan() {
+    w = PackedForm(&kept, N, K, MW_FP8_TILES);
+    if (columns) xc = PackedForm(&kept, M, K, MW_FP8_COLUMNS);
+    x = PackedForm(&scratch, M, K, MW_FP8_ROWS);
+  }
+  mw_status forward(const void* px, const void* pw, char* keep, char* temp, void* y, cudaStream_t stream) const {
+    mw_status s = p_quantize(pw, keep + w.q, keep + w.scale, nullptr, nullptr, N, static_cast<int>(K), MW_FP8_TILES, wt,
+                             stream);
+    if (s != MW_OK) return s;
+    s = p_quantize(px, temp + x.q, temp + x.scale, columns ? keep + xc.qc : nullptr, columns ? keep + xc.sc : nullptr, M,
+                   static_cast<int>(K), columns ? MW_FP8_ROWS_AND_COLUMNS : MW_FP8_ROWS, xt, stream);
+    if (s != MW_OK) return s;
+    return p_matmul(temp + x.q, temp + x.scale, 0, 0, keep + w.q, keep + w.scale, 1, 0, y, static_cast<int>(M),
+                    static_cast<int>(N), static_cast<int>(K), yt, stream);
+  }
+};
+
+struct Fp8LinearBackward : public torch::autograd::Node {
+  SavedVariable kept;
+  Linear z;
+  std::vector<int64_t> x_sizes, y_sizes;
   c10::DeviceIndex dev = 0;
 
   std::string name() const override { return "Fp8LinearBackward"; }
-  void release_variables() override {
-    for (SavedVariable* s : {&xc, &xcs, &wq, &ws}) s->reset_data();
-  }
+  void release_variables() override { kept.reset_data(); }
   variable_list apply(variable_list&& grads) override {
     variable_list out(2);
     if (!grads[0].defined()) return out;
-    const at::Tensor tx = xc.unpack(), txs = xcs.unpack(), tw = wq.unpack(), tws = ws.unpack();
-    gradients(grads[0], tx, txs, tw, tws, &out);
+    const at::Tensor keep = kept.unpack();
+    gradients(grads[0], keep, &out);
     // (what they depend on besides is saved in 8 bits, without its graph)
     if (at::GradMode::is_enabled()) {
       auto node = std::shared_ptr<NoSecondDerivative>(new NoSecondDerivative(), torch::autograd::deleteNode);
@@ -1272,46 +1319,37 @@ struct Fp8LinearBackward : public torch::autograd::Node {
   }
 
  private:
-  void gradients(const at::Tensor& grad, const at::Tensor& tx, const at::Tensor& txs, const at::Tensor& tw,
-                 const at::Tensor& tws, variable_list* out) {
+  void gradients(const at::Tensor& grad, const at::Tensor& keep, variable_list* out) {
     const at::NoGradGuard no_grad;
-    const bool need_x = task_should_compute_output(0), need_w = columns && task_should_compute_output(1);
+    const bool need_x = task_should_compute_output(0), need_w = z.columns && task_should_compute_output(1);
     if (!need_x && !need_w) return;
-    const std::array<int64_t, 2> wsz{N, K}, wss{blocks128(N), blocks128(K)}, xss{blocks128(M), K};
-    check_saved(tw, "weight in 8 bits", kCodes, wsz, dev);
-    check_saved(tws, "weight's scales", kScales, wss, dev);
-    if (columns) {
-      check_saved(tx, "x in 8 bits", kCodes, x_sizes, dev);
-      check_saved(txs, "x's scales", kScales, xss, dev);
-    }
-    TORCH_CHECK(is_real(grad) && grad.scalar_type() == torch_type(yt) && grad.sizes() == y_sizes &&
+    check_saved(keep, "operands in 8 bits", at::kByte, {z.kept.bytes}, dev);
+    TORCH_CHECK(is_real(grad) && grad.scalar_type() == torch_type(z.yt) && grad.sizes() == y_sizes &&
                     grad.get_device() == dev,
                 "the gradient must be a plain CUDA tensor like the output");
     const at::Tensor dy = grad.contiguous();
-    Form f;
-    mw_status s = MW_OK;
-    TORCH_CHECK(make_form(dy, M, need_x && need_w ? MW_FP8_ROWS_AND_COLUMNS : need_x ? MW_FP8_ROWS : MW_FP8_COLUMNS, yt,
-                          dev, &f, &s),
-                "no plain CUDA tensors");
-    if (s != MW_OK) raise(s);
+    const int form = need_x && need_w ? MW_FP8_ROWS_AND_COLUMNS : need_x ? MW_FP8_ROWS : MW_FP8_COLUMNS;
+    Pack pack;
+    const PackedForm g(&pack, z.M, z.N, form);
+    const at::TensorOptions options = dy.options();
+    at::Tensor temp = scratch(pack.bytes, options), dx, dw;
+    if (need_x) dx = at::empty(x_sizes, options.dtype(torch_type(z.xt)));
+    if (need_w) dw = at::empty({z.N, z.K}, options.dtype(torch_type(z.wt)));
+    for (const at::Tensor* t : {&temp, &dx, &dw}) TORCH_CHECK(!t->defined() || is_real(*t), "no plain CUDA tensors");
     const auto stream = c10::cuda::getCurrentCUDAStream(dev).stream();
-    const int m = static_cast<int>(M);
-    if (need_x) {
-      at::Tensor dx = at::empty(x_sizes, dy.options().dtype(torch_type(xt)));
-      TORCH_CHECK(is_real(dx), "no plain CUDA tensors");
-      s = p_matmul(f.q.const_data_ptr(), f.scale.const_data_ptr(), 0, 0, tw.const_data_ptr(), tws.const_data_ptr(), 1, 1,
-                   dx.mutable_data_ptr(), m, K, N, xt, stream);
-      if (s != MW_OK) raise(s);
-      (*out)[0] = dx;
-    }
-    if (need_w) {
-      at::Tensor dw = at::empty(wsz, dy.options().dtype(torch_type(wt)));
-      TORCH_CHECK(is_real(dw), "no plain CUDA tensors");
-      s = p_matmul(f.qc.const_data_ptr(), f.sc.const_data_ptr(), 0, 1, tx.const_data_ptr(), txs.const_data_ptr(), 0, 1,
-                   dw.mutable_data_ptr(), N, K, m, wt, stream);
-      if (s != MW_OK) raise(s);
-      (*out)[1] = dw;
-    }
+    char* p = pack.bytes ? static_cast<char*>(temp.mutable_data_ptr()) : nullptr;
+    const char* k = static_cast<const char*>(keep.const_data_ptr());
+    const int M = static_cast<int>(z.M), K = static_cast<int>(z.K), N = static_cast<int>(z.N);
+    mw_status s = p_quantize(dy.const_data_ptr(), p + g.q, p + g.scale, p + g.qc, p + g.sc, z.M, N, form, z.yt, stream);
+    if (s == MW_OK && need_x)
+      s = p_matmul(p + g.q, p + g.scale, 0, 0, k + z.w.q, k + z.w.scale, 1, 1, dx.mutable_data_ptr(), M, K, N, z.xt,
+                   stream);
+    if (s == MW_OK && need_w)
+      s = p_matmul(p + g.qc, p + g.sc, 0, 1, k + z.xc.qc, k + z.xc.sc, 0, 1, dw.mutable_data_ptr(), N, K, M, z.wt,
+                   stream);
+    if (s != MW_OK) raise(s);
+    (*out)[0] = dx;
+    (*out)[1] = dw;
   }
 };
 
@@ -1325,36 +1363,39 @@ PyObject* linear_apply(PyObject*, PyObject* const* a, Py_ssize_t n) {
       dual(px) || dual(pw))
     return none();
   const at::Tensor &x = *px, &w = *pw;
-  const int xt = norm_type(x.scalar_type()), wt = norm_type(w.scalar_type());
-  int yt = xt;
+  Linear z;
+  z.xt = z.yt = norm_type(x.scalar_type());
+  z.wt = norm_type(w.scalar_type());
   if (a[2] != Py_None) {
     if (!THPDtype_Check(a[2])) return none();
-    yt = norm_type(reinterpret_cast<THPDtype*>(a[2])->scalar_type);
+    z.yt = norm_type(reinterpret_cast<THPDtype*>(a[2])->scalar_type);
   }
-  const int64_t K = w.size(1), N = w.size(0);
-  if (xt < 0 || wt < 0 || yt < 0 || K < 16 || N < 16 || K % 16 || N % 16 || K > INT_MAX || N > INT_MAX ||
-      x.numel() / K > INT_MAX)
+  z.K = w.size(1);
+  z.N = w.size(0);
+  if (z.xt < 0 || z.wt < 0 || z.yt < 0 || z.K < 16 || z.N < 16 || z.K % 16 || z.N % 16 || z.K > INT_MAX ||
+      z.N > INT_MAX || x.numel() / z.K > INT_MAX)
     return none();
-  const int64_t M = x.numel() / K;
+  z.M = x.numel() / z.K;
   const bool graph = torch::autograd::compute_requires_grad(x, w);
-  const bool columns = graph && w.requires_grad();
+  z.columns = graph && w.requires_grad();
+  z.plan();
   std::vector<int64_t> sizes = x.sizes().vec();
-  sizes.back() = N;
-  Form fx, fw;
-  at::Tensor y;
+  sizes.back() = z.N;
+  const at::TensorOptions options = x.options();
+  const void *dx = x.const_data_ptr(), *dw = w.const_data_ptr();
+  at::Tensor y, kept, temp;
   mw_status s = MW_OK;
   {
     const at::NoGradGuard no_grad;
     const bool real = call([&] {
-      if (!make_form(w, N, MW_FP8_TILES, wt, dev, &fw, &s)) return false;
-      if (s != MW_OK) return true;
-      if (!make_form(x, M, columns ? MW_FP8_ROWS_AND_COLUMNS : MW_FP8_ROWS, xt, dev, &fx, &s)) return false;
-      if (s != MW_OK) return true;
-      y = at::empty(sizes, x.options().dtype(torch_type(yt)));
-      if (!is_real(y)) return false;
-      s = p_matmul(fx.q.const_data_ptr(), fx.scale.const_data_ptr(), 0, 0, fw.q.const_data_ptr(),
-                   fw.scale.const_data_ptr(), 1, 0, y.mutable_data_ptr(), static_cast<int>(M), static_cast<int>(N),
-                   static_cast<int>(K), yt, c10::cuda::getCurrentCUDAStream(dev).stream());
+      kept = scratch(z.kept.bytes, options);
+      temp = scratch(z.scratch.bytes, options);
+      y = at::empty(sizes, options.dtype(torch_type(z.yt)));
+      for (const at::Tensor* t : {&kept, &temp, &y})
+        if (!is_real(*t)) return false;
+      s = z.forward(dx, dw, static_cast<char*>(kept.mutable_data_ptr()),
+                    z.scratch.bytes ? static_cast<char*>(temp.mutable_data_ptr()) : nullptr, y.mutable_data_ptr(),
+                    c10::cuda::getCurrentCUDAStream(dev).stream());
       return true;
     });
     if (!real) return none();
@@ -1363,21 +1404,10 @@ PyObject* linear_apply(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (graph) {
     auto node = std::shared_ptr<Fp8LinearBackward>(new Fp8LinearBackward(), torch::autograd::deleteNode);
     node->set_next_edges(torch::autograd::collect_next_edges(x, w));
-    if (columns) {
-      node->xc = SavedVariable(fx.qc, false);
-      node->xcs = SavedVariable(fx.sc, false);
-    }
-    node->wq = SavedVariable(fw.q, false);
-    node->ws = SavedVariable(fw.scale, false);
+    node->kept = SavedVariable(kept, false);
+    node->z = z;
     node->x_sizes = x.sizes().vec();
-    node->y_sizes = sizes;
-    node->M = M;
-    node->K = static_cast<int>(K);
-    node->N = static_cast<int>(N);
-    node->xt = xt;
-    node->yt = yt;
-    node->wt = wt;
-    node->columns = columns;
+    node->y_sizes = std::move(sizes);
     node->dev = dev;
     torch::autograd::set_history(y, node);
   }
