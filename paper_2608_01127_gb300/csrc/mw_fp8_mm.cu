@@ -367,19 +367,35 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         for (int k = 0; k < n_boxes; ++k) {
           const int c0 = half * (BN / 2) + (backwards ? n_boxes - 1 - k : k) * per;
           uint32_t w[32], v[32];
-          const bool free_now = frees && (L::OVERLAP ? k == 0 : k == n_boxes - 1);
-          if (ok) {
-            if (!p.out_f32) tmem_ld32(acc + c0 + 32, v);
-            tmem_ld32(acc + c0, w);
-            tmem_wait_ld();
-          } else {
-#pragma unroll
-            for (int e = 0; e < 32; ++e) w[e] = v[e] = 0u;
-          }
-          if (free_now) {  // (a box covers the overlap's 32 columns)
+          auto give_back = [&] {
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster(freed + 8 * (j & 1));
+          };
+          if (!ok) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) w[e] = v[e] = 0u;
+            if (frees && k == (L::OVERLAP ? 0 : n_boxes - 1)) give_back();
+          } else if (L::OVERLAP && frees && k == 0) {
+            // the overlap's 32 columns, which the next tile's MMAs wait for, before the others
+            if (p.out_f32 || !backwards)
+              tmem_ld32(acc + c0, w);
+            else
+              tmem_ld32(acc + c0 + 32, v);
+            tmem_wait_ld();
+            give_back();
+            if (!p.out_f32) {
+              if (backwards)
+                tmem_ld32(acc + c0, w);
+              else
+                tmem_ld32(acc + c0 + 32, v);
+              tmem_wait_ld();
+            }
+          } else {
+            tmem_ld32(acc + c0, w);
+            if (!p.out_f32) tmem_ld32(acc + c0 + 32, v);
+            tmem_wait_ld();
+            if (!L::OVERLAP && k == n_boxes - 1) give_back();
           }
           if (!p.out_f32) {
 #pragma unroll
