@@ -829,7 +829,7 @@ def _fp8_source(x) -> Tuple[int, int, int]:
     C = x.shape[-1]
     if C % 16:
         raise ValueError(f"x has {C} columns: rows of 8-bit codes must be multiples of 16")
-    return xt, (x.numel() // C if C else 0), C
+    return xt, math.prod(x.shape[:-1]), C
 
 
 def mw_quantize(x: torch.Tensor, block: Tuple[int, int] = (1, 128), out=None

@@ -1167,14 +1167,15 @@ struct RMSNormBackward : public torch::autograd::Node {
   variable_list apply(variable_list&& grads) override {
     variable_list out(3);
     const at::Tensor dh = residual ? grads[1] : at::Tensor();
-    if (!grads[0].defined()) {  // only h was used
+    const at::Tensor tr = rstd.unpack();  // (a second time through the graph ends here)
+    if (!grads[0].defined()) {            // only h was used
       if (!dh.defined()) return out;
       if (task_should_compute_output(0)) out[0] = dh;
       if (task_should_compute_output(2)) out[2] = dh;
       return out;
     }
     const at::Tensor th = residual ? rows.unpack(shared_from_this()) : rows.unpack();
-    const at::Tensor tw = weight.unpack(), tr = rstd.unpack();
+    const at::Tensor tw = weight.unpack();
     gradients(grads[0], dh, th, tw, tr, &out);
     first_only("RMSNorm", out, th, tw, grads[0], dh);
     return out;
