@@ -189,9 +189,10 @@ namespace {
 struct MapKey2d {
   const void* ptr = nullptr;
   long long rows = 0, cols = 0;
-  int elem = 0, box_rows = 0;
+  int elem = 0, box_rows = 0, box_bytes = 0;
   bool operator==(const MapKey2d& o) const {
-    return ptr == o.ptr && rows == o.rows && cols == o.cols && elem == o.elem && box_rows == o.box_rows;
+    return ptr == o.ptr && rows == o.rows && cols == o.cols && elem == o.elem && box_rows == o.box_rows &&
+           box_bytes == o.box_bytes;
   }
 };
 thread_local MapKey2d t_map_keys_2d[kMapCache];
@@ -200,8 +201,8 @@ thread_local int t_map_next_2d = 0;
 }  // namespace
 
 mw_status make_map_2d(CUtensorMap* m, const void* ptr, long long rows, long long cols, int elem, int box_rows,
-                      const char* name) {
-  const MapKey2d key{ptr, rows, cols, elem, box_rows};
+                      const char* name, int box_bytes) {
+  const MapKey2d key{ptr, rows, cols, elem, box_rows, box_bytes};
   for (int i = 0; i < kMapCache; ++i)
     if (t_map_keys_2d[i].ptr != nullptr && t_map_keys_2d[i] == key) {
       *m = t_maps_2d[i];
@@ -211,14 +212,14 @@ mw_status make_map_2d(CUtensorMap* m, const void* ptr, long long rows, long long
   if (!fn) return fail(MW_ERR_CUDA, "cuTensorMapEncodeTiled is unavailable (no CUDA driver?)");
   cuuint64_t dims[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)};
   cuuint64_t strides[1] = {static_cast<cuuint64_t>(cols) * elem};
-  cuuint32_t box[2] = {static_cast<cuuint32_t>(128 / elem), static_cast<cuuint32_t>(box_rows)};
+  cuuint32_t box[2] = {static_cast<cuuint32_t>(box_bytes / elem), static_cast<cuuint32_t>(box_rows)};
   cuuint32_t estr[2] = {1, 1};
   const CUresult r = fn(m,
                         elem == 1   ? CU_TENSOR_MAP_DATA_TYPE_UINT8
                         : elem == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
                                     : CU_TENSOR_MAP_DATA_TYPE_FLOAT32,
                         2, const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                        CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                        box_bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS) return fail(MW_ERR_CUDA, "cuTensorMapEncodeTiled(%s) failed: %d", name, (int)r);
   t_map_keys_2d[t_map_next_2d] = key;

@@ -305,7 +305,7 @@ mw_status mw_scaled_matmul(const void* a, const void* a_scale, int a_tiles, int 
   MW_TRY(operand(&ma, a, rows_a, p.a_columns, 128, "a"));
   MW_TRY(operand(&mb, b, rows_b, p.b_columns, plan.join ? plan.bn : plan.bn / 2, "b"));
   mc = ma;
-  if (p.tma_out) MW_TRY(make_map_2d(&mc, c, M, N, static_cast<int>(elem), 32, "c"));
+  if (p.tma_out) MW_TRY(make_map_2d(&mc, c, M, N, static_cast<int>(elem), 32, "c", 64));
   return launch_status(launch_fp8_mm(plan.bn, plan.join, ma, mb, mc, p, scope.device(), s), "8-bit product launch");
 }
 

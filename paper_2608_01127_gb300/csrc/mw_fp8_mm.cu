@@ -135,6 +135,7 @@ __device__ __forceinline__ void tile_at(const Fp8MmParams& p, int t, int* tp, in
 
 constexpr int kPairThreads = 384;
 constexpr int kPairEpiWarps = 8;  // two for a quarter of the rows, half of the columns each
+constexpr int kBoxBytes = 32 * 64;
 
 template <int BN>
 struct PairLayout {
@@ -143,9 +144,9 @@ struct PairLayout {
   static constexpr int STAGE = kA + B;
   static constexpr int ATOMS = 1 + BN / 128;   // of scale words, 512 bytes each
   static constexpr int SETS = BN == 256 ? 2 : 4;  // groups of scales in shared and tensor memory
-  static constexpr int STAGES = 5;
-  static constexpr int OFF_STORE = STAGES * STAGE;  // a box of 32 rows x 128 bytes a warp
-  static constexpr int OFF_SCALE = OFF_STORE + kPairEpiWarps * 4096;
+  static constexpr int STAGES = 6;                  // (5: 2% more time)
+  static constexpr int OFF_STORE = STAGES * STAGE;  // a box of 32 rows x 64 bytes a warp
+  static constexpr int OFF_SCALE = OFF_STORE + kPairEpiWarps * kBoxBytes;
   static constexpr int OFF_BAR = OFF_SCALE + SETS * ATOMS * 512;
   static constexpr int N_BAR = 2 * STAGES + 2 * SETS + 5;
   static constexpr int OFF_MISC = OFF_BAR + N_BAR * 8;
@@ -342,11 +343,10 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     // ------------------------------------------------------------ results
     const int quarter = warp & 3, half = (warp - 4) >> 2;
     const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
-    uint8_t* to = smem + L::OFF_STORE + (warp - 4) * 4096;
+    uint8_t* to = smem + L::OFF_STORE + (warp - 4) * kBoxBytes;
     const uint32_t freed = cluster_address(smem_u32(&acc_free[0]), 0);
-    const int per = p.out_f32 ? 32 : 64;  // columns of a box
-    constexpr int kMine = BN / 64;        // boxes of 32 columns of a warp
-    const int n_boxes = p.out_f32 ? kMine : kMine / 2;
+    const int per = p.out_f32 ? 16 : 32;  // columns of a box
+    const int n_boxes = BN / 2 / per;     // of a warp
     bool ok = aligned;
     int j = 0;
     for (int t = tile0; t < n_tiles; t += tile_step) {
@@ -360,58 +360,41 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         const bool add = first > 0;
         if (add && lane == 0) bulk_wait_all();  // the part before is in the output
         __syncwarp();
-        // accumulator 0 ends in the overlap, 1 begins with it
+        // accumulator 0 ends in the overlap, 1 begins with it: its 32 columns are read first, and
+        // then the next tile's MMAs go on
         const bool backwards = L::OVERLAP && (j & 1) == 0;
-        const bool frees = !L::OVERLAP || (half == 1) == backwards;
+        const int frees = !L::OVERLAP ? n_boxes - 1 : (half == 1) == backwards ? L::OVERLAP / per - 1 : -1;
 #pragma unroll 1
         for (int k = 0; k < n_boxes; ++k) {
           const int c0 = half * (BN / 2) + (backwards ? n_boxes - 1 - k : k) * per;
-          uint32_t w[32], v[32];
-          auto give_back = [&] {
+          uint32_t w[16];
+          if (!ok) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) w[e] = 0u;
+          } else if (p.out_f32) {
+            tmem_ld16(acc + c0, w);
+            tmem_wait_ld();
+          } else {
+            uint32_t v[32];
+            tmem_ld32(acc + c0, v);
+            tmem_wait_ld();
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+              w[e] = pack_bf16x2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1]));
+          }
+          if (k == frees) {
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster(freed + 8 * (j & 1));
-          };
-          if (!ok) {
-#pragma unroll
-            for (int e = 0; e < 32; ++e) w[e] = v[e] = 0u;
-            if (frees && k == (L::OVERLAP ? 0 : n_boxes - 1)) give_back();
-          } else if (L::OVERLAP && frees && k == 0) {
-            // the overlap's 32 columns, which the next tile's MMAs wait for, before the others
-            if (p.out_f32 || !backwards)
-              tmem_ld32(acc + c0, w);
-            else
-              tmem_ld32(acc + c0 + 32, v);
-            tmem_wait_ld();
-            give_back();
-            if (!p.out_f32) {
-              if (backwards)
-                tmem_ld32(acc + c0, w);
-              else
-                tmem_ld32(acc + c0 + 32, v);
-              tmem_wait_ld();
-            }
-          } else {
-            tmem_ld32(acc + c0, w);
-            if (!p.out_f32) tmem_ld32(acc + c0 + 32, v);
-            tmem_wait_ld();
-            if (!L::OVERLAP && k == n_boxes - 1) give_back();
-          }
-          if (!p.out_f32) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e)
-              w[e] = pack_bf16x2(__uint_as_float(w[2 * e]), __uint_as_float(w[2 * e + 1]));
-#pragma unroll
-            for (int e = 0; e < 16; ++e)
-              w[16 + e] = pack_bf16x2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1]));
           }
           const int col0 = tq * BN + c0;
           if (col0 >= p.rows_b || row0 >= p.rows_a) continue;
           if (lane == 0) bulk_wait_read<0>();
           __syncwarp();
+          // (the 64-byte swizzle: 16-byte piece e of row r at e ^ (r / 2 % 4))
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            *reinterpret_cast<uint4*>(to + lane * 128 + ((e ^ (lane & 7)) << 4)) =
+          for (int e = 0; e < 4; ++e)
+            *reinterpret_cast<uint4*>(to + lane * 64 + ((e ^ ((lane >> 1) & 3)) << 4)) =
                 make_uint4(w[4 * e], w[4 * e + 1], w[4 * e + 2], w[4 * e + 3]);
           if (p.tma_out) {
             fence_proxy_async_smem();
@@ -426,10 +409,10 @@ __global__ void __launch_bounds__(kPairThreads, 1)
           } else {  // rows that do not start at 16 bytes: single elements, a row a turn
             __syncwarp();
             for (int r = 0; r < 32 && row0 + r < p.rows_a; ++r)
-              for (int c = lane; c < per && col0 + c < p.rows_b; c += 32) {
-                const int at = p.out_f32 ? c * 4 : c * 2;
-                const uint8_t* from = to + r * 128 + (((at >> 4) ^ (r & 7)) << 4) + (at & 15);
-                const long long dst = static_cast<long long>(row0 + r) * p.ld + col0 + c;
+              if (lane < per && col0 + lane < p.rows_b) {
+                const int at = p.out_f32 ? lane * 4 : lane * 2;
+                const uint8_t* from = to + r * 64 + (((at >> 4) ^ ((r >> 1) & 3)) << 4) + (at & 15);
+                const long long dst = static_cast<long long>(row0 + r) * p.ld + col0 + lane;
                 if (p.out_f32) {
                   float* o = static_cast<float*>(p.out) + dst;
                   const float v = *reinterpret_cast<const float*>(from);

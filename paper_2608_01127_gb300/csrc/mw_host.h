@@ -48,9 +48,10 @@ mw_status encode_bias_map(CUtensorMap* m, const float* bias, int N_pad, int BH, 
 // swizzle, or x 32 without.
 mw_status encode_rows_map(CUtensorMap* m, void* ptr, int rows, int BH, int d, bool swizzle);
 // 2-D map over rows of `cols` elements (1, 2 or 4 bytes: codes, bf16, fp32) at a pitch of
-// as many, in boxes of 128 bytes x box_rows with the 128-byte swizzle; from the cache.
+// as many, in boxes of box_bytes (128 or 64) x box_rows with the swizzle of as many bytes;
+// from the cache.
 mw_status make_map_2d(CUtensorMap* m, const void* ptr, long long rows, long long cols, int elem, int box_rows,
-                      const char* name);
+                      const char* name, int box_bytes = 128);
 
 // The device status word of the current device `dev`.
 mw_status status_ptr(int dev, unsigned** out);

@@ -385,7 +385,7 @@ struct Fp8MmParams {
 };
 // bn: rows of B of a tile (join: 16, 32, 64 or 128; pairs: 128 or 256); ta, tb: boxes of 128
 // bytes x 128 rows (join's tb, and pairs' of 128 rows: x bn and 64 rows where B runs along the
-// contraction); tc: 32 rows x 128 bytes
+// contraction); tc: 32 rows x 64 bytes
 cudaError_t launch_fp8_mm(int bn, bool join, const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap& tc,
                           const Fp8MmParams& p, int dev, cudaStream_t s);
 
