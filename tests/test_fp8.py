@@ -248,6 +248,15 @@ def test_product_of_columns(mw, M, N, K, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("M,N,K,across", [(2560, 2562, 8320, False), (2561, 2560, 16640, False),
+                                          (2560, 2560, 8300, True)])
+def test_long_sums_in_fp32(mw, M, N, K, across):
+    """More blocks than one part of a sum: the parts are added in the output, through copies or
+    (rows that do not start at 16 bytes) element by element."""
+    check_product(mw, M, N, K, across, across, False, not across, F32)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("M,N,K", [(1, 768, 2304), (31, 1152, 160), (65, 272, 144), (300, 1152, 1152), (4403, 64, 1152)])
 @pytest.mark.parametrize("b_tiles", [True, False])
 def test_product_with_b_across(mw, M, N, K, b_tiles):
@@ -403,6 +412,20 @@ def test_linear(mw, M, K, N, x_dtype, w_dtype):
     for got, (ref, terms, n) in zip((y, dx, dw), linear_reference(x, w, dy)):
         bound = (n / 32 + 8) * 2.0 ** -22 * terms + (2.0 ** -8 * ref.abs() if got.dtype == BF16 else 0.0) + 1e-30
         assert got.shape == ref.shape and float(((got.detach().double().cpu() - ref).abs() / bound).max()) <= 1.0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("x_dtype,out_dtype", [(F32, BF16), (BF16, F32)])
+def test_linear_output_of_another_type(mw, x_dtype, out_dtype):
+    M, K, N = 150, 272, 160
+    x, w, dy = rnd(1, M, K, dtype=x_dtype), rnd(2, N, K), rnd(3, M, N, dtype=out_dtype)
+    lx, lw = x.cuda().requires_grad_(True), w.cuda().requires_grad_(True)
+    y = mw.Fp8Linear.apply(lx, lw, out_dtype)
+    dx, dw = torch.autograd.grad(y, (lx, lw), dy.cuda())
+    assert y.dtype == out_dtype and dx.dtype == x_dtype and dw.dtype == F32
+    for got, (ref, terms, n) in zip((y, dx, dw), linear_reference(x, w, dy)):
+        bound = (n / 32 + 8) * 2.0 ** -22 * terms + (2.0 ** -8 * ref.abs() if got.dtype == BF16 else 0.0) + 1e-30
+        assert float(((got.detach().double().cpu() - ref).abs() / bound).max()) <= 1.0
 
 
 @pytest.mark.gpu
