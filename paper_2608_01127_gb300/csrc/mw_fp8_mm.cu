@@ -182,7 +182,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
   if (threadIdx.x == 0) {
     for (int s = 0; s < L::STAGES; ++s) mbar_init(&full[s], 1), mbar_init(&empty[s], 1);
     for (int s = 0; s < L::SETS; ++s) mbar_init(&sc_full[s], 2), mbar_init(&sc_empty[s], 1);
-    for (int s = 0; s < 2; ++s) mbar_init(&acc_full[s], 1), mbar_init(&acc_free[s], L::OVERLAP ? kPairEpiWarps : 2 * kPairEpiWarps);
+    for (int s = 0; s < 2; ++s) mbar_init(&acc_full[s], 1), mbar_init(&acc_free[s], 2 * kPairEpiWarps);
     mbar_init(done, 1);
     *abort_flag = aligned ? 0 : 1;
     fence_mbar_init();
@@ -255,8 +255,8 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       for (int t = tile0; t < n_tiles && ok; t += tile_step) {
         for (int first = 0; first < p.blocks && ok; first += p.chunk, ++j) {
           const uint32_t acc = tmem + (j & 1) * (BN - L::OVERLAP);
-          // this accumulator's columns have been read: of the chunk before (their overlap) or
-          // of the one before that
+          // this accumulator's columns have been read: of the chunk before (their overlap, and
+          // by then all of the one before that) or of the one before that
           const int wait = L::OVERLAP ? j - 1 : j - 2;
           if (wait >= 0) ok = warp_wait(&acc_free[wait & 1], (wait >> 1) & 1, ctl);
           tc_fence_after();
@@ -361,9 +361,16 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         if (add && lane == 0) bulk_wait_all();  // the part before is in the output
         __syncwarp();
         // accumulator 0 ends in the overlap, 1 begins with it: its 32 columns are read first, and
-        // then the next tile's MMAs go on
+        // then the next tile's MMAs go on, into what the chunk before left.  The warps without a
+        // part in the overlap say that they are through with that one: they may be far behind the
+        // others, where the half of a tile at the edge left these nothing to write.
         const bool backwards = L::OVERLAP && (j & 1) == 0;
         const int frees = !L::OVERLAP ? n_boxes - 1 : (half == 1) == backwards ? L::OVERLAP / per - 1 : -1;
+        if (frees < 0) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_cluster(freed + 8 * (j & 1));
+        }
 #pragma unroll 1
         for (int k = 0; k < n_boxes; ++k) {
           const int c0 = half * (BN / 2) + (backwards ? n_boxes - 1 - k : k) * per;

@@ -257,6 +257,16 @@ def test_long_sums_in_fp32(mw, M, N, K, across):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("M,N,K", [(5984, 4705, 16), (5984, 4705, 288), (6000, 4704, 128), (20000, 1300, 640),
+                                   (12000, 2305, 128)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_many_tiles_of_few_blocks(mw, M, N, K, dtype):
+    """The tile at the edge leaves half of the warps that write results little or nothing to do, and
+    the others fall behind them: by single elements, more than a tile's MMAs take."""
+    check_product(mw, M, N, K, dtype=dtype)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("M,N,K", [(1, 768, 2304), (31, 1152, 160), (65, 272, 144), (300, 1152, 1152), (4403, 64, 1152)])
 @pytest.mark.parametrize("b_tiles", [True, False])
 def test_product_with_b_across(mw, M, N, K, b_tiles):
