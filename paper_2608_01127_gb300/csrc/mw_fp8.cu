@@ -29,18 +29,17 @@ mw_status check_size(long long n, const char* name) {
   return MW_OK;
 }
 
-// How a product is cut: tiles of 256 x bn by pairs of CTAs, or of 128 x bn by clusters of
-// `splits` CTAs (join) that share its contraction.
+// How a product is cut: tiles of 256 x bn by pairs of CTAs, of which `splits` share a tile's
+// contraction (bn = 256), or of 128 x bn by clusters of `splits` CTAs (join) that do.
 struct MmPlan {
   int bn = 128, splits = 1;
   bool join = false, swap = false;
 };
 
-// Clusters of r CTAs that run at once, a CTA an SM: eight groups of SMs, each of which holds
-// whole clusters.
-int clusters_at_once(int r, int sms) { return std::max(1, 8 * (sms / 8 / r)); }
+// Blocks of each of r pairs that share a contraction: whole words of scales.
+int pair_share(int blocks, int r) { return ceil_div(ceil_div(blocks, r), 4) * 4; }
 
-MmPlan mm_plan(int M, int N, int blocks, bool a_columns, bool b_columns, bool f32, int sms) {
+MmPlan mm_plan(int M, int N, int blocks, bool a_columns, bool b_columns, bool f32, int sms, int dev) {
   MmPlan best;
   const int most = std::min(kFp8Splits, blocks);
   double best_cost = INFINITY;
@@ -54,13 +53,13 @@ MmPlan mm_plan(int M, int N, int blocks, bool a_columns, bool b_columns, bool f3
     // costs more than their number (us for 1 to 8 CTAs: 8 x 2560 x 10240 21.2 12.7 10.2 8.6 8.0
     // 7.9 8.3 8.3; 16 x 7680 x 2560 8.8 7.4 7.6 7.2 11.2 11.5 12.1 12.4)
     for (int r = 1; r <= most; ++r) {
-      const double load = std::max(1.0, static_cast<double>(tiles) / clusters_at_once(r, sms));
+      const double load = std::max(1.0, static_cast<double>(tiles) / fp8_clusters(r, dev));
       const double cost = ceil_div(blocks, r) * load * load;
       if (cost < best_cost) best_cost = cost, best.splits = r;
     }
     return best;
   }
-  // us, fitted to 14 sizes: what a launch takes, a block of the contraction, a tile
+  // us, fitted to 22 sizes: what a launch takes, a block of the contraction, a tile
   auto take = [&](int bn, bool join, int splits, double cost) {
     if (cost < best_cost) best_cost = cost, best.bn = bn, best.join = join, best.splits = splits;
   };
@@ -70,9 +69,15 @@ MmPlan mm_plan(int M, int N, int blocks, bool a_columns, bool b_columns, bool f3
   for (int r = 1; r <= most; ++r) {
     const int share = ceil_div(blocks, r);
     if (f32 && share > kFp8Chunk) continue;
-    const double load = static_cast<double>(tiles(128, 128)) / clusters_at_once(r, sms);
-    const bool once = load <= 1.15 && tiles(128, 128) * r <= sms;
-    take(128, true, r, (once ? 1.0 : std::max(2.0, std::ceil(load))) * (7.1 + 0.225 * share));
+    const double load = static_cast<double>(tiles(128, 128)) / fp8_clusters(r, dev);
+    take(128, true, r, std::ceil(load) * (7.1 + 0.225 * share));
+  }
+  // (one round of clusters: a second one starts from nothing)
+  for (int r = 2; 2 * r <= kFp8Splits && tiles(256, 256) * 2 * r <= sms; ++r) {
+    const int share = pair_share(blocks, r);
+    if ((f32 && share > kFp8Chunk) || share * (r - 1) >= blocks) continue;
+    const double cost = 9.5 + 0.272 * share;
+    if (cost < best_cost && tiles(256, 256) <= fp8_clusters(2 * r, dev)) take(256, false, r, cost);
   }
   return best;
 }
@@ -255,7 +260,7 @@ mw_status mw_scaled_matmul(const void* a, const void* a_scale, int a_tiles, int 
   Fp8MmParams p{};
   MW_TRY(status_ptr(scope.device(), &p.status));
   p.blocks = ceil_div(K, kFp8Block);
-  const MmPlan plan = mm_plan(M, N, p.blocks, a_transposed, b_transposed, f32, sm_count());
+  const MmPlan plan = mm_plan(M, N, p.blocks, a_transposed, b_transposed, f32, sm_count(), scope.device());
   auto scales = [&](const void* at, int rows, bool transposed, bool tile) {
     Fp8Scales z{};
     z.p = static_cast<const uint8_t*>(at);
@@ -291,11 +296,13 @@ mw_status mw_scaled_matmul(const void* a, const void* a_scale, int a_tiles, int 
   p.tiles_q = ceil_div(rows_b, plan.bn);
   p.ctas = sm_count();
   // (whole words of scales)
-  p.chunk = f32 ? ceil_div(ceil_div(p.blocks, ceil_div(p.blocks, kFp8Chunk)), 4) * 4 : p.blocks;
+  p.chunk = !plan.join && plan.splits > 1 ? pair_share(p.blocks, plan.splits)
+            : f32                            ? pair_share(p.blocks, ceil_div(p.blocks, kFp8Chunk))
+                                             : p.blocks;
   p.out = c;
   p.out_f32 = f32;
   p.out_quads = N % 4 == 0 && (reinterpret_cast<uintptr_t>(c) & (4 * elem - 1)) == 0;
-  p.tma_out = !plan.join && aligned16(c) && N * elem % 16 == 0;
+  p.tma_out = !plan.join && plan.splits == 1 && aligned16(c) && N * elem % 16 == 0;
   p.budget_ns = budget_ns();
   p.debug_skip_q = debug_skip_q();
   CUtensorMap ma, mb, mc;

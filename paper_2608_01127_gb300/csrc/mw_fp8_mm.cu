@@ -21,6 +21,8 @@
 // and clusters that share the contraction of a tile, for few.
 #include <cooperative_groups.h>
 
+#include <atomic>
+
 #include "mw_internal.h"
 #include "mw_ptx.cuh"
 
@@ -122,6 +124,55 @@ __device__ __forceinline__ void tile_at(const Fp8MmParams& p, int t, int* tp, in
   *tq = i / n;
 }
 
+// ------------------------------------------------------------------ parts
+
+// Four results in a row of the output, of which n count.
+__device__ __forceinline__ void store_four(const Fp8MmParams& p, long long at, float4 v, int n) {
+  if (n >= 4 && p.out_quads) {
+    if (p.out_f32)
+      *reinterpret_cast<float4*>(static_cast<float*>(p.out) + at) = v;
+    else
+      *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.out) + at) =
+          make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
+    return;
+  }
+  const float e[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (i >= n) continue;
+    if (p.out_f32)
+      static_cast<float*>(p.out)[at + i] = e[i];
+    else
+      static_cast<__nv_bfloat16*>(p.out)[at + i] = __float2bfloat16(e[i]);
+  }
+}
+
+// The sum of the parts that `ranks` CTAs have in shared memory at `part`, [outer][inner] at a
+// pitch of inner + 4 floats, in the order of the ranks: this one, `rank`, does its share of
+// them.  CTA r of these is cta(r) of the cluster.  To row o0 and column i0 of the output, of which in_n
+// columns are left.
+template <class Cta>
+__device__ __forceinline__ void join_parts(const Fp8MmParams& p, float* part, int outer, int inner, long long o0,
+                                           int i0, int in_n, int rank, int ranks, int threads, Cta cta) {
+  cg::cluster_group cluster = cg::this_cluster();
+  const int quads = outer * (inner / 4), pitch = inner + 4;
+  const int q0 = quads * rank / ranks, q1 = quads * (rank + 1) / ranks;
+  for (int e = q0 + threadIdx.x; e < q1; e += threads) {
+    const int o = e / (inner / 4), i = e % (inner / 4) * 4;
+    if (i >= in_n) continue;
+    // (all on their way at once: one after another, eight of them took 5 us)
+    float4 v[kFp8Splits];
+#pragma unroll
+    for (int r = 0; r < kFp8Splits; ++r)
+      if (r < ranks) v[r] = *reinterpret_cast<const float4*>(cluster.map_shared_rank(part, cta(r)) + o * pitch + i);
+    float4 s = v[0];
+#pragma unroll
+    for (int r = 1; r < kFp8Splits; ++r)
+      if (r < ranks) s.x += v[r].x, s.y += v[r].y, s.z += v[r].z, s.w += v[r].w;
+    store_four(p, (o0 + o) * p.ld + i0 + i, s, in_n - i);
+  }
+}
+
 // ------------------------------------------------------------------ pairs of CTAs
 //
 // Two CTAs (of one pair of SMs) take a tile of 256 x BN: each copies 128 rows of A and half of
@@ -132,6 +183,11 @@ __device__ __forceinline__ void tile_at(const Fp8MmParams& p, int t, int* tp, in
 // Sums of more than `chunk` blocks leave tensor memory in parts, which the output adds up in
 // fp32: the tensor cores cut, not round, what falls below a sum's last place, and 440 such
 // additions (14080 tokens) came to 1e-6 of the result.
+//
+// JOIN: few tiles and a long contraction, as a weight's gradient has: a cluster of up to four
+// pairs shares the blocks of a tile, and each CTA adds up a share of its rows' parts, which takes
+// 4 us and saves half of the blocks or more (gradient of 2304 x 768 over 14080: 35.6 to
+// 24.9 us, by 27 x 2 pairs of 76).
 
 constexpr int kPairThreads = 384;
 constexpr int kPairEpiWarps = 8;  // two for a quarter of the rows, half of the columns each
@@ -152,6 +208,7 @@ struct PairLayout {
   static constexpr int OFF_MISC = OFF_BAR + N_BAR * 8;
   static constexpr int SMEM = OFF_MISC + 16;
   static_assert(SMEM <= 232448, "shared memory of a CTA");
+  static_assert((BN + 4) * 128 * 4 <= OFF_STORE, "a part fits");
   // Tensor memory: two accumulators; of 256 columns they overlap in 32, which are read first
   static constexpr int OVERLAP = BN == 256 ? 32 : 0;
   static constexpr int SCALES = 2 * BN - OVERLAP;
@@ -159,7 +216,7 @@ struct PairLayout {
   static_assert(SCALES + SETS * WORDS <= 512, "tensor memory");
 };
 
-template <int BN>
+template <int BN, bool JOIN>
 __global__ void __launch_bounds__(kPairThreads, 1)
     fp8_mm_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b,
                        const __grid_constant__ CUtensorMap tm_c, const Fp8MmParams p) {
@@ -177,8 +234,9 @@ __global__ void __launch_bounds__(kPairThreads, 1)
   uint32_t* tmem_at = reinterpret_cast<uint32_t*>(smem + L::OFF_MISC + 8);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   cg::cluster_group cluster = cg::this_cluster();
-  const uint32_t rank = cluster.block_rank();
-  const bool aligned = (smem_u32(smem) & 1023u) == 0u;  // (the same in both)
+  // of the pair, whose first CTA is `leader` of the cluster
+  const uint32_t rank = cluster.block_rank() & 1u, leader = cluster.block_rank() & ~1u;
+  const bool aligned = (smem_u32(smem) & 1023u) == 0u;  // (the same in all)
   if (threadIdx.x == 0) {
     for (int s = 0; s < L::STAGES; ++s) mbar_init(&full[s], 1), mbar_init(&empty[s], 1);
     for (int s = 0; s < L::SETS; ++s) mbar_init(&sc_full[s], 2), mbar_init(&sc_empty[s], 1);
@@ -202,7 +260,10 @@ __global__ void __launch_bounds__(kPairThreads, 1)
   pdl_trigger();
 
   const int n_tiles = p.tiles_p * p.tiles_q;
-  const int tile0 = blockIdx.x / 2, tile_step = gridDim.x / 2;
+  const int pairs = JOIN ? p.splits : 1;  // of a tile
+  const int tile0 = blockIdx.x / (2 * pairs), tile_step = gridDim.x / (2 * pairs);
+  // this pair's blocks (JOIN: a chunk of them, and one tile a cluster)
+  const int k0 = JOIN ? static_cast<int>(leader / 2) * p.chunk : 0, k1 = JOIN ? min(k0 + p.chunk, p.blocks) : p.blocks;
 
   if (warp == 0) {
     // ------------------------------------------------------------ tiles of A and B
@@ -215,7 +276,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         int tp, tq;
         tile_at(p, t, &tp, &tq);
         const int row_a = tp * 256 + rank * 128, row_b = tq * BN + rank * (BN / 2);
-        for (int kb = 0; kb < p.blocks; ++kb, ++i) {
+        for (int kb = k0; kb < k1; ++kb, ++i) {
           const int st = i % L::STAGES;
           if (!mbar_wait(&empty[st], ((i / L::STAGES) & 1) ^ 1, ctl)) {
             ok = false;
@@ -223,7 +284,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
           }
           if (skip) continue;
           uint8_t* a = smem + st * L::STAGE;
-          const uint32_t bar = cluster_address(smem_u32(&full[st]), 0);
+          const uint32_t bar = cluster_address(smem_u32(&full[st]), leader);
           if (rank == 0) mbar_arrive_expect_tx(&full[st], 2 * bytes);
           if (p.a_columns)
             tma_load_2d_pair(a, &tm_a, bar, row_a, kb * kBlock);
@@ -253,14 +314,14 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       bool ok = aligned;
       int i = 0, g = 0, j = 0;  // stages, scale groups, chunks
       for (int t = tile0; t < n_tiles && ok; t += tile_step) {
-        for (int first = 0; first < p.blocks && ok; first += p.chunk, ++j) {
+        for (int first = k0; first < k1 && ok; first += p.chunk, ++j) {
           const uint32_t acc = tmem + (j & 1) * (BN - L::OVERLAP);
           // this accumulator's columns have been read: of the chunk before (their overlap, and
           // by then all of the one before that) or of the one before that
           const int wait = L::OVERLAP ? j - 1 : j - 2;
           if (wait >= 0) ok = warp_wait(&acc_free[wait & 1], (wait >> 1) & 1, ctl);
           tc_fence_after();
-          const int end = min(first + p.chunk, p.blocks);
+          const int end = min(first + p.chunk, k1);
           for (int kb = first; kb < end && ok; ++kb, ++i) {
             const int in = (kb - first) % kGroup, set = g % L::SETS;
             const uint32_t words = tmem + L::SCALES + set * L::WORDS;
@@ -279,17 +340,17 @@ __global__ void __launch_bounds__(kPairThreads, 1)
             const uint32_t a = a0 + st * (L::STAGE >> 4);
             umma_mx4<true>(acc, a, a + (kA >> 4), a_step, b_step, idesc | idesc_scale_byte(in), words, words + 4,
                            kb > first);
-            umma_commit_pair(&empty[st]);
+            umma_commit_pair(&empty[st], leader);
             if (in == kGroup - 1 || kb + 1 == end) {
-              umma_commit_pair(&sc_empty[set]);
+              umma_commit_pair(&sc_empty[set], leader);
               ++g;
             }
           }
-          if (ok) umma_commit_pair(&acc_full[j & 1]);
+          if (ok) umma_commit_pair(&acc_full[j & 1], leader);
         }
       }
       if (!ok) {  // what was issued ends before the CTAs go
-        umma_commit_pair(done);
+        umma_commit_pair(done, leader);
         drain_wait(done, 0, p.budget_ns);
       }
     }
@@ -306,21 +367,21 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         // the group after (t, first, kb)
         auto advance = [&](int* t, int* first, int* kb) {
           *kb += kGroup;
-          if (*kb < min(*first + p.chunk, p.blocks)) return;
+          if (*kb < min(*first + p.chunk, k1)) return;
           *first += p.chunk;
-          if (*first >= p.blocks) *first = 0, *t += tile_step;
+          if (*first >= k1) *first = k0, *t += tile_step;
           *kb = *first;
         };
         auto load = [&](Raw* to, int t, int first, int kb) {
           if (t >= n_tiles) return;
           int tp, tq;
           tile_at(p, t, &tp, &tq);
-          const int end = min(first + p.chunk, p.blocks);
+          const int end = min(first + p.chunk, k1);
           to->a.load(p.a_scales, tp * 256 + rank * 128, p.rows_a, kb, end);
 #pragma unroll
           for (int a = 0; a < L::ATOMS - 1; ++a) to->b[a].load(p.b_scales, tq * BN + a * 128, p.rows_b, kb, end);
         };
-        int t = aligned ? tile0 : n_tiles, first = 0, kb = 0;
+        int t = aligned ? tile0 : n_tiles, first = k0, kb = k0;
         load(&raw, t, first, kb);
         for (int g = 0; t < n_tiles; ++g) {
           const int set = g % L::SETS;
@@ -333,18 +394,40 @@ __global__ void __launch_bounds__(kPairThreads, 1)
           for (int a = 0; a < L::ATOMS - 1; ++a) raw.b[a].store(to + (a + 1) * 512);
           fence_proxy_async_smem();
           __syncwarp();
-          if (lane == 0) mbar_arrive_cluster(cluster_address(smem_u32(&sc_full[set]), 0));
+          if (lane == 0) mbar_arrive_cluster(cluster_address(smem_u32(&sc_full[set]), leader));
           raw = next;
         }
       });
     });
     __syncwarp();
-  } else if (warp >= 4) {
+  } else if (JOIN && warp >= 4) {
+    // ------------------------------------------------------------ this CTA's part, in the stages' place
+    const int quarter = warp & 3, half = (warp - 4) >> 2;
+    const bool ok = aligned && warp_wait(acc_full, 0, ctl);
+    tc_fence_after();
+    const uint32_t acc = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
+    float* part = reinterpret_cast<float*>(smem) + (quarter * 32 + lane) * (BN + 4);
+#pragma unroll 1
+    for (int c = half * (BN / 2); c < (half + 1) * (BN / 2); c += 16) {
+      uint32_t v[16];
+      if (ok) {
+        tmem_ld16(acc + c, v);
+        tmem_wait_ld();
+      } else {
+#pragma unroll
+        for (int k = 0; k < 16; ++k) v[k] = 0u;
+      }
+#pragma unroll
+      for (int k = 0; k < 16; k += 4)
+        *reinterpret_cast<uint4*>(part + c + k) = make_uint4(v[k], v[k + 1], v[k + 2], v[k + 3]);
+    }
+    __syncwarp();
+  } else if (!JOIN && warp >= 4) {
     // ------------------------------------------------------------ results
     const int quarter = warp & 3, half = (warp - 4) >> 2;
     const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
     uint8_t* to = smem + L::OFF_STORE + (warp - 4) * kBoxBytes;
-    const uint32_t freed = cluster_address(smem_u32(&acc_free[0]), 0);
+    const uint32_t freed = cluster_address(smem_u32(&acc_free[0]), leader);
     const int per = p.out_f32 ? 16 : 32;  // columns of a box
     const int n_boxes = BN / 2 / per;     // of a warp
     bool ok = aligned;
@@ -438,7 +521,15 @@ __global__ void __launch_bounds__(kPairThreads, 1)
   }
   tc_fence_before();
   __syncthreads();
-  cluster.sync();  // neither's shared memory is in use any more
+  if constexpr (JOIN) {
+    cluster.sync();  // all parts are there
+    int tp, tq;
+    tile_at(p, tile0, &tp, &tq);
+    const int row0 = tp * 256 + rank * 128;
+    join_parts(p, reinterpret_cast<float*>(smem), max(0, min(128, p.rows_a - row0)), BN, row0, tq * BN, p.rows_b - tq * BN,
+               leader / 2, pairs, kPairThreads, [&](int r) { return 2 * r + static_cast<int>(rank); });
+  }
+  cluster.sync();  // nobody's shared memory is in use any more
   if (warp == 1) {
     tc_fence_after();
     tmem_dealloc_pair(tmem, 512);
@@ -472,33 +563,13 @@ struct JoinLayout {
   static constexpr int N_BAR = 2 * STAGES + 2 * SETS + 2;
   static constexpr int OFF_MISC = OFF_BAR + N_BAR * 8;
   static constexpr int SMEM = OFF_MISC + 16;
-  static_assert(SMEM <= (BN <= 64 ? 233472 / 2 - 1024 : 232448), "shared memory of a CTA, of which an SM holds two up to 64");
+  static_assert(SMEM <= (BN <= 64 ? 233472 / 2 - 1024 : 232448), "shared memory (up to 64: of two CTAs an SM)");
   static constexpr int SCALES = BN;      // columns of tensor memory: the accumulator, the scale words
   static constexpr int WORDS = 4 * ATOMS;
   static constexpr int USED = SCALES + SETS * WORDS;
   static constexpr int COLS = USED <= 64 ? 64 : USED <= 128 ? 128 : 256;
   static_assert(((BN + 4) * 128 > 132 * BN ? (BN + 4) * 128 : 132 * BN) * 4 <= STAGES * STAGE, "a part fits");
 };
-// Four results in a row of the output, of which n count.
-__device__ __forceinline__ void store_four(const Fp8MmParams& p, long long at, float4 v, int n) {
-  if (n >= 4 && p.out_quads) {
-    if (p.out_f32)
-      *reinterpret_cast<float4*>(static_cast<float*>(p.out) + at) = v;
-    else
-      *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.out) + at) =
-          make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
-    return;
-  }
-  const float e[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if (i >= n) continue;
-    if (p.out_f32)
-      static_cast<float*>(p.out)[at + i] = e[i];
-    else
-      static_cast<__nv_bfloat16*>(p.out)[at + i] = __float2bfloat16(e[i]);
-  }
-}
 
 // The rows [r0, r1) of 128 that a rank owns, and their pitch.
 struct OwnRows {
@@ -693,27 +764,12 @@ __global__ void __launch_bounds__(kThreads, BN <= 64 ? 2 : 1)
           static_cast<__nv_bfloat16*>(p.out)[dst] = __float2bfloat16(s);
       }
   } else {
-    const int inner = p.swap ? 128 : BN, pitch = inner + 4;
+    const int inner = p.swap ? 128 : BN;
     const int o0 = p.swap ? tq * BN : tp * 128, i0 = p.swap ? tp * 128 : tq * BN;
     const int outer = min(p.swap ? BN : 128, (p.swap ? p.rows_b : p.rows_a) - o0);
     const int in_n = (p.swap ? p.rows_a : p.rows_b) - i0;
-    const int quads = outer * (inner / 4);
-    const int q0 = quads * rank / ranks, q1 = quads * (rank + 1) / ranks;
-    float* part = reinterpret_cast<float*>(smem);
-    for (int e = q0 + threadIdx.x; e < q1; e += kThreads) {
-      const int o = e / (inner / 4), i = e % (inner / 4) * 4;
-      if (i >= in_n) continue;
-      // (all on their way at once: one after another, eight of them took 5 us)
-      float4 v[kFp8Splits];
-#pragma unroll
-      for (int r = 0; r < kFp8Splits; ++r)
-        if (r < ranks) v[r] = *reinterpret_cast<const float4*>(cluster.map_shared_rank(part, r) + o * pitch + i);
-      float4 s = v[0];
-#pragma unroll
-      for (int r = 1; r < kFp8Splits; ++r)
-        if (r < ranks) s.x += v[r].x, s.y += v[r].y, s.z += v[r].z, s.w += v[r].w;
-      store_four(p, static_cast<long long>(o0 + o) * p.ld + i0 + i, s, in_n - i);
-    }
+    join_parts(p, reinterpret_cast<float*>(smem), outer, inner, o0, i0, in_n, rank, ranks, kThreads,
+               [](int r) { return r; });
     cluster_arrive();  // shared memory stays until all have read it
     cluster_wait();
   }
@@ -725,6 +781,20 @@ __global__ void __launch_bounds__(kThreads, BN <= 64 ? 2 : 1)
 
 // ------------------------------------------------------------------ launches
 
+// The attributes of a launch in clusters of `ranks` CTAs.
+struct ClusterConfig {
+  cudaLaunchConfig_t cfg;
+  cudaLaunchAttribute attr[2];
+  ClusterConfig(int blocks, int threads, int ranks, int smem, cudaStream_t s) {
+    pdl_config(cfg, attr[0], dim3(blocks), dim3(threads), smem, s);
+    cudaLaunchAttribute& c = attr[cfg.numAttrs++];
+    c.id = cudaLaunchAttributeClusterDimension;
+    c.val.clusterDim.x = ranks;
+    c.val.clusterDim.y = c.val.clusterDim.z = 1;
+  }
+  ClusterConfig(const ClusterConfig&) = delete;  // (cfg points into it)
+};
+
 // ranks: CTAs of a cluster
 template <class Kernel, class... Args>
 cudaError_t launch(Kernel kernel, OncePerDevice& prepared, int dev, int blocks, int threads, int ranks, int smem,
@@ -732,23 +802,17 @@ cudaError_t launch(Kernel kernel, OncePerDevice& prepared, int dev, int blocks, 
   const cudaError_t e = prepared(
       dev, [&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem); });
   if (e != cudaSuccess) return e;
-  cudaLaunchConfig_t cfg;
-  cudaLaunchAttribute attr[2];
-  pdl_config(cfg, attr[0], dim3(blocks), dim3(threads), smem, s);
-  cudaLaunchAttribute& c = attr[cfg.numAttrs++];
-  c.id = cudaLaunchAttributeClusterDimension;
-  c.val.clusterDim.x = ranks;
-  c.val.clusterDim.y = c.val.clusterDim.z = 1;
-  return cudaLaunchKernelEx(&cfg, kernel, args...);
+  const ClusterConfig c(blocks, threads, ranks, smem, s);
+  return cudaLaunchKernelEx(&c.cfg, kernel, args...);
 }
 
-template <int BN>
+template <int BN, bool JOIN>
 cudaError_t run_pair(const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap& tc, const Fp8MmParams& p, int dev,
                      cudaStream_t s) {
   static OncePerDevice prepared;
-  const int tiles = p.tiles_p * p.tiles_q, most = p.ctas / 2;
-  return launch(fp8_mm_pair_kernel<BN>, prepared, dev, 2 * (tiles < most ? tiles : most), kPairThreads, 2,
-                PairLayout<BN>::SMEM, s, ta, tb, tc, p);
+  const int tiles = p.tiles_p * p.tiles_q, most = p.ctas / 2, pairs = JOIN ? p.splits : 1;
+  return launch(fp8_mm_pair_kernel<BN, JOIN>, prepared, dev, 2 * (JOIN ? tiles * pairs : tiles < most ? tiles : most),
+                kPairThreads, 2 * pairs, PairLayout<BN>::SMEM, s, ta, tb, tc, p);
 }
 
 template <int BN>
@@ -760,6 +824,24 @@ cudaError_t run_join(const CUtensorMap& ta, const CUtensorMap& tb, const Fp8MmPa
 
 }  // namespace
 
+int fp8_clusters(int r, int dev) {
+  static std::atomic<int> known[kMaxDevices][kFp8Splits + 1];
+  if (dev < 0 || dev >= kMaxDevices) return 1;
+  std::atomic<int>& here = known[dev][r];
+  if (const int n = here.load(std::memory_order_relaxed)) return n;
+  const auto kernel = fp8_mm_join_kernel<128>;
+  constexpr int smem = JoinLayout<128>::SMEM;
+  const ClusterConfig c(r, kThreads, r, smem, nullptr);
+  int n = 0;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess ||
+      cudaOccupancyMaxActiveClusters(&n, kernel, &c.cfg) != cudaSuccess || n < 1) {
+    cudaGetLastError();
+    n = 1;
+  }
+  here.store(n, std::memory_order_relaxed);
+  return n;
+}
+
 cudaError_t launch_fp8_mm(int bn, bool join, const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap& tc,
                           const Fp8MmParams& p, int dev, cudaStream_t s) {
   if (join) {
@@ -768,8 +850,9 @@ cudaError_t launch_fp8_mm(int bn, bool join, const CUtensorMap& ta, const CUtens
     if (bn == 64) return run_join<64>(ta, tb, p, dev, s);
     return run_join<128>(ta, tb, p, dev, s);
   }
-  if (bn == 128) return run_pair<128>(ta, tb, tc, p, dev, s);
-  return run_pair<256>(ta, tb, tc, p, dev, s);
+  if (bn == 128) return run_pair<128, false>(ta, tb, tc, p, dev, s);
+  if (p.splits > 1) return run_pair<256, true>(ta, tb, tc, p, dev, s);
+  return run_pair<256, false>(ta, tb, tc, p, dev, s);
 }
 
 }  // namespace mw

@@ -371,9 +371,10 @@ struct Fp8MmParams {
   long long ld;
   int rows_a, rows_b, blocks;
   int tiles_p, tiles_q;  // of 128 rows of A (pairs: 256), of bn rows of B
-  int splits;            // join: CTAs of a tile
+  int splits;            // join: CTAs of a tile; pairs: pairs of a tile
   int ctas;              // pairs: CTAs at most
-  int chunk;             // pairs: blocks that are summed in tensor memory before the output takes them
+  int chunk;             // pairs: blocks that are summed in tensor memory before the output takes them,
+                         // or a pair's share of a tile's blocks
   bool a_columns, b_columns;  // rows of the operand lie across the contraction
   bool swap;             // join: a row of the output is one of B
   bool out_f32;
@@ -383,6 +384,9 @@ struct Fp8MmParams {
   unsigned long long budget_ns;
   int debug_skip_q;      // test hook: never load A and B
 };
+// Clusters of r CTAs (1 to kFp8Splits), a CTA an SM, that device dev, the current one, runs at once.
+// Its groups of SMs are not alike (152 SMs: 76 clusters of 2, 46 of 3, 36 of 4, 23 of 6, 15 of 8).
+int fp8_clusters(int r, int dev);
 // bn: rows of B of a tile (join: 16, 32, 64 or 128; pairs: 128 or 256); ta, tb: boxes of 128
 // bytes x 128 rows (join's tb, and pairs' of 128 rows: x bn and 64 rows where B runs along the
 // contraction); tc: 32 rows x 64 bytes

@@ -480,13 +480,13 @@ __device__ __forceinline__ void umma_commit(uint64_t* bar) {
 }
 
 // The same on the barriers at `bar` of both CTAs of a pair.
-__device__ __forceinline__ void umma_commit_pair(uint64_t* bar) {
+// (leader: the first CTA's rank in the cluster)
+__device__ __forceinline__ void umma_commit_pair(uint64_t* bar, uint32_t leader) {
   asm volatile(
       "{\n\t.reg .pred e;\n\t"
       "elect.sync _|e, 0xffffffff;\n\t"
-      "@e tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n\t}\n" ::"r"(
-          smem_u32(bar)),
-      "h"(static_cast<uint16_t>(3))
+      "@e tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n\t}\n"
+      ::"r"(smem_u32(bar)), "h"(static_cast<uint16_t>(3u << leader))
       : "memory");
 }
 

@@ -267,6 +267,20 @@ def test_many_tiles_of_few_blocks(mw, M, N, K, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("M,N,K,aT,bT", [
+    (1152, 1152, 14077, True, True), (2304, 768, 14080, True, True), (1104, 1104, 9000, True, True),
+    (1536, 1280, 16000, True, True), (1024, 768, 14080, True, True), (512, 2560, 10240, False, False),
+    (1100, 1101, 9008, False, False), (516, 2512, 12304, False, True), (1040, 1030, 9008, True, False)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_few_tiles_and_a_long_contraction(mw, M, N, K, aT, bT, dtype):
+    """Two to four pairs of CTAs share the contraction of a tile of 256 x 256; tiles' second
+    halves without rows; rows that start anywhere; what lies behind the results stays."""
+    whole = torch.full((M * N + 64,), 7.0, dtype=dtype, device="cuda")
+    check_product(mw, M, N, K, aT, bT, not aT and N % 2 == 0, not bT, dtype, out=whole[:M * N].view(M, N))
+    assert bool((whole[M * N:] == 7).all())
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("M,N,K", [(1, 768, 2304), (31, 1152, 160), (65, 272, 144), (300, 1152, 1152), (4403, 64, 1152)])
 @pytest.mark.parametrize("b_tiles", [True, False])
 def test_product_with_b_across(mw, M, N, K, b_tiles):
@@ -395,6 +409,22 @@ def test_a_wait_that_runs_out_is_told(mw, M):
         mw.mw_set_option("debug_skip_q_load", 0)
         mw.mw_set_option("wait_budget_ms", 2000)
     assert torch.equal(mw.mw_scaled_matmul(a, sa, b, sb), good) and mw.mw_device_status() == 0
+
+
+@pytest.mark.gpu
+def test_a_wait_that_runs_out_in_joined_pairs(mw):
+    a, sa, _ = operand(mw, 1, 1152, 8192, True, False)
+    b, sb, _ = operand(mw, 2, 1152, 8192, True, False)
+    good = mw.mw_scaled_matmul(a, sa, b, sb, F32, True, True)
+    mw.mw_set_option("wait_budget_ms", 50)
+    mw.mw_set_option("debug_skip_q_load", 1)
+    try:
+        mw.mw_scaled_matmul(a, sa, b, sb, F32, True, True)
+        assert mw.mw_device_status() == 4
+    finally:
+        mw.mw_set_option("debug_skip_q_load", 0)
+        mw.mw_set_option("wait_budget_ms", 2000)
+    assert torch.equal(mw.mw_scaled_matmul(a, sa, b, sb, F32, True, True), good) and mw.mw_device_status() == 0
 
 
 # ------------------------------------------------------------------ the linear layer
