@@ -11,6 +11,13 @@ constexpr uint8_t kFp8NanScale = 0xff;
 // A magnitude's bits, which order as the magnitudes do, infinities and NaN above.
 __device__ __forceinline__ uint32_t fp8_magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 
+// The largest magnitude of three, NaN where one is (one instruction).
+__device__ __forceinline__ float fp8_largest(float a, float b, float c) {
+  float r;
+  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+
 // The exponent byte of the least power of two s with top <= 448 s: 448 = 1.75 x 2^8, so the
 // exponent is top's less 8, or less 7 for a fraction over 1.75 (the sum carries into it).
 __device__ __forceinline__ uint8_t fp8_scale(uint32_t top) {
@@ -38,11 +45,14 @@ __device__ __forceinline__ uint32_t fp8_pair(float a, float b) {
 }
 
 // Four codes.
-__device__ __forceinline__ uint32_t fp8_four(float2 a, float2 b) { return fp8_pair(a.x, a.y) | fp8_pair(b.x, b.y) << 16; }
+__device__ __forceinline__ uint32_t fp8_four(float2 a, float2 b) {
+  return fp8_pair(a.x, a.y) | fp8_pair(b.x, b.y) << 16;
+}
 
 // Eight codes of values already divided by the scale (NaN where that is NaN).
 __device__ __forceinline__ uint2 fp8_codes(const float (&v)[8]) {
-  return make_uint2(fp8_pair(v[0], v[1]) | fp8_pair(v[2], v[3]) << 16, fp8_pair(v[4], v[5]) | fp8_pair(v[6], v[7]) << 16);
+  return make_uint2(fp8_four(make_float2(v[0], v[1]), make_float2(v[2], v[3])),
+                    fp8_four(make_float2(v[4], v[5]), make_float2(v[6], v[7])));
 }
 
 }  // namespace mw

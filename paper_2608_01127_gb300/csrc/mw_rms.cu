@@ -337,10 +337,10 @@ __global__ void __maxnreg__(V == 1 ? 80 : 128) rms_fwd_rows_kernel(const RmsPara
           if (!in || row + r >= r1) continue;
           float2 y[4];
           result(r, k, y);
-          uint32_t top = 0u;
+          float top = 0.f;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) top = max(top, max(fp8_magnitude(y[e].x), fp8_magnitude(y[e].y)));
-          bytes |= static_cast<uint32_t>(fp8_scale(top)) << (8 * r);
+          for (int e = 0; e < 4; ++e) top = fp8_largest(top, y[e].x, y[e].y);
+          bytes |= static_cast<uint32_t>(fp8_scale(__float_as_uint(top))) << (8 * r);
         }
 #pragma unroll
         for (int i = 8; i > 0; i >>= 1) bytes = __vmaxu4(bytes, __shfl_xor_sync(0xffffffffu, bytes, i));
