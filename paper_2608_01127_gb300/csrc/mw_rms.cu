@@ -10,6 +10,8 @@
 // the layer norm's (mw_norm.cu): W warps to a row, 16-byte accesses where rows allow them.
 // 128 columns of a row lie in 16 lanes, whose maximum gives the scale without leaving the
 // registers.
+#include <algorithm>
+#include <atomic>
 #include <type_traits>
 
 #include "mw_fp8.cuh"
@@ -672,13 +674,30 @@ cudaError_t run_fwd(const RmsParams& p, const Shape& sh, int sms, cudaStream_t s
 }
 
 template <class X, class Y, int V, bool RES>
-cudaError_t run_fwd_rows(const RmsParams& p, const RowsShape& sh, int dev, cudaStream_t s) {
+cudaError_t run_fwd_rows(RmsParams p, const RowsShape& sh, int dev, int sms, cudaStream_t s) {
   constexpr auto kKernel = rms_fwd_rows_kernel<X, Y, V, RES>;
   const size_t ring = static_cast<size_t>(2) * kFwdRows<X, V, RES> * V * kFwdPieces<X, RES> * 16 * sh.threads;
   static OncePerDevice prepared;
   const cudaError_t e = prepared(
       dev, [] { return cudaFuncSetAttribute(kKernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRmsMaxSmem); });
   if (e != cudaSuccess) return e;
+  // A group's rows are in parts for as many blocks as the backward has, or, where instructions
+  // and not HBM bound the time, as many as the SMs hold (14080 x 5120 bf16, one block of 320 threads and
+  // two: to 8 bits 87 and 60 us, with the residual 102 and 84; bf16 58 and 46, but with the residual 88
+  // and 95).
+  p.parts = rms_parts(p.rows_per_group, p.C, p.groups);
+  if constexpr (std::is_same_v<Y, E4m3> || !RES) {
+    static std::atomic<int> held[kMaxDevices][kNormMaxC / 256 + 1];
+    std::atomic<int>& here = held[dev][sh.W];
+    int blocks = here.load(std::memory_order_relaxed);
+    if (blocks == 0) {
+      const cudaError_t o = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&blocks, kKernel, sh.threads, ring);
+      if (o != cudaSuccess) return o;
+      here.store(blocks, std::memory_order_relaxed);
+    }
+    const long long parts = std::min(static_cast<long long>(sms) * blocks / p.groups, p.rows_per_group);
+    p.parts = static_cast<int>(std::max(parts, 1ll));
+  }
   cudaLaunchConfig_t cfg;
   cudaLaunchAttribute attr;
   pdl_config(cfg, attr, dim3(static_cast<unsigned>(p.groups) * p.parts), dim3(sh.threads), ring, s);
@@ -746,13 +765,14 @@ cudaError_t launch_rms_fwd(RmsParams p, bool vec, int dev, int sms, cudaStream_t
   if (vec && p.rows > 8ll * sms) {
     const RowsShape sh = rows_shape(p.C);
     p.W = sh.W;
-    p.parts = rms_parts(p.rows_per_group, p.C, p.groups);
     return types([&](auto tx, auto ty) {
       using X = decltype(tx);
       using Y = decltype(ty);
       if (sh.V == 1)
-        return p.residual ? run_fwd_rows<X, Y, 1, true>(p, sh, dev, s) : run_fwd_rows<X, Y, 1, false>(p, sh, dev, s);
-      return p.residual ? run_fwd_rows<X, Y, 2, true>(p, sh, dev, s) : run_fwd_rows<X, Y, 2, false>(p, sh, dev, s);
+        return p.residual ? run_fwd_rows<X, Y, 1, true>(p, sh, dev, sms, s)
+                          : run_fwd_rows<X, Y, 1, false>(p, sh, dev, sms, s);
+      return p.residual ? run_fwd_rows<X, Y, 2, true>(p, sh, dev, sms, s)
+                        : run_fwd_rows<X, Y, 2, false>(p, sh, dev, sms, s);
     });
   }
   const Shape sh = shape_of(p.C, vec, true);
