@@ -836,7 +836,7 @@ int fp8_clusters(int r, int dev) {
   if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess ||
       cudaOccupancyMaxActiveClusters(&n, kernel, &c.cfg) != cudaSuccess || n < 1) {
     cudaGetLastError();
-    n = 1;
+    return 1;
   }
   here.store(n, std::memory_order_relaxed);
   return n;

@@ -427,6 +427,30 @@ def test_a_wait_that_runs_out_in_joined_pairs(mw):
     assert torch.equal(mw.mw_scaled_matmul(a, sa, b, sb, F32, True, True), good) and mw.mw_device_status() == 0
 
 
+@pytest.mark.gpu
+def test_products_on_streams_at_once(mw):
+    """Every kind of product, and the 8-bit form, side by side on the device: as one after another."""
+    jobs = []
+    for i, (M, N, K, T) in enumerate([(1152, 1152, 9008, True), (3, 2304, 768, False), (64, 512, 4096, False),
+                                      (4403, 768, 640, False), (700, 640, 2304, False)]):
+        a, sa, _ = operand(mw, 10 + i, M, K, T, False)
+        b, sb, _ = operand(mw, 30 + i, N, K, T, False)
+        jobs.append(lambda a=a, sa=sa, b=b, sb=sb, T=T: mw.mw_scaled_matmul(a, sa, b, sb, F32, T, T))
+    x = rnd(50, 4403, 2304, dtype=BF16).cuda()
+    jobs.append(lambda: bits(mw.mw_quantize(x, (128, 128))[0]))
+    want = [job() for job in jobs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    for turn in range(12):
+        got = []
+        for i, job in enumerate(jobs):
+            with torch.cuda.stream(streams[(i * 5 + turn) % 3]):
+                got.append(job())
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(got, want))
+    assert mw.mw_device_status() == 0
+
+
 # ------------------------------------------------------------------ the linear layer
 
 def linear_reference(x, w, dy):
