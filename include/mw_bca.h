@@ -430,7 +430,7 @@ mw_status mw_rmsnorm_bwd(const void* dy, const void* h, const float* rstd, const
  */
 enum { MW_FP8_ROWS = 0, MW_FP8_COLUMNS = 1, MW_FP8_TILES = 2, MW_FP8_ROWS_AND_COLUMNS = 3 };
 mw_status mw_quantize(const void* x, void* q, void* scale, void* q_columns, void* scale_columns, long long rows,
-                          int C, int form, int x_dtype, void* stream);
+                      int C, int form, int x_dtype, void* stream);
 
 /*
  * The product of two of them, c = A B^T, summed in fp32 on tensor cores that apply the
@@ -448,8 +448,8 @@ mw_status mw_quantize(const void* x, void* q, void* scale, void* q_columns, void
  * ran out (MW_ERR_TIMEOUT) the results are not to be used.
  */
 mw_status mw_scaled_matmul(const void* a, const void* a_scale, int a_tiles, int a_transposed, const void* b,
-                        const void* b_scale, int b_tiles, int b_transposed, void* c, int M, int N, int K, int c_dtype,
-                        void* stream);
+                           const void* b_scale, int b_tiles, int b_transposed, void* c, int M, int N, int K,
+                           int c_dtype, void* stream);
 
 /* Human-readable name of a status code (static string). */
 const char* mw_status_string(mw_status s);

@@ -195,7 +195,7 @@ mw_status mw_rmsnorm_bwd(const void* dy, const void* h, const float* rstd, const
 }
 
 mw_status mw_quantize(const void* x, void* q, void* scale, void* q_columns, void* scale_columns, long long rows,
-                          int C, int form, int x_dtype, void* stream) {
+                      int C, int form, int x_dtype, void* stream) {
   if (form < MW_FP8_ROWS || form > MW_FP8_ROWS_AND_COLUMNS)
     return fail(MW_ERR_INVALID_ARG, "form=%d is none of MW_FP8_ROWS ... MW_FP8_ROWS_AND_COLUMNS", form);
   MW_TRY(check_type(x_dtype, "x_dtype"));
@@ -231,8 +231,8 @@ mw_status mw_quantize(const void* x, void* q, void* scale, void* q_columns, void
 }
 
 mw_status mw_scaled_matmul(const void* a, const void* a_scale, int a_tiles, int a_transposed, const void* b,
-                        const void* b_scale, int b_tiles, int b_transposed, void* c, int M, int N, int K, int c_dtype,
-                        void* stream) {
+                           const void* b_scale, int b_tiles, int b_transposed, void* c, int M, int N, int K,
+                           int c_dtype, void* stream) {
   MW_TRY(check_size(M, "M"));
   MW_TRY(check_size(N, "N"));
   MW_TRY(check_size(K, "K"));

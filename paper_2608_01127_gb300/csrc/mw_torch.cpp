@@ -708,7 +708,8 @@ struct Rms {
     rows = x->numel() / c;
     if (wo != Py_None) {
       w = tensor(wo);
-      if (!w || (pt = norm_type(w->scalar_type())) < 0 || w->dim() < 1 || w->dim() > 2 || w->size(-1) != c) return false;
+      if (!w || (pt = norm_type(w->scalar_type())) < 0 || w->dim() < 1 || w->dim() > 2 || w->size(-1) != c)
+        return false;
       const int64_t g = w->dim() == 2 ? w->size(0) : 1;
       if (g < 1 || g > INT_MAX) return false;
       groups = static_cast<int>(g);
