@@ -297,6 +297,7 @@ mw_status mw_scaled_matmul(const void* a, const void* a_scale, int a_tiles, int 
   p.ctas = sm_count();
   // (whole words of scales)
   p.chunk = !plan.join && plan.splits > 1 ? pair_share(p.blocks, plan.splits)
+            : plan.join && f32               ? kFp8Chunk
             : f32                            ? pair_share(p.blocks, ceil_div(p.blocks, kFp8Chunk))
                                              : p.blocks;
   p.out = c;

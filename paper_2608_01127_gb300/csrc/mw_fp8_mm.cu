@@ -545,8 +545,14 @@ __global__ void __launch_bounds__(kPairThreads, 1)
 // these.  More than that is left where it was made and read from there, 16 bytes at a time,
 // which takes two more trips through the cluster but moves parts faster (us, sent / read: one
 // token x 2304 x 768 3.1 / 3.5; 64 x 7680 x 2560 16.3 / 13.8).
+//
+// LONG: a CTA's share of more than `chunk` blocks is summed in parts here too.  Two accumulators
+// take turns, and while the MMAs go on with one, the warps that read results add the other to a
+// sum in tensor memory beside them, which takes no time of its own (16 x 19456 x 16384 in fp32, 128
+// blocks: 56.5 us in two parts and in one).  A kernel of its own, for what the code costs where
+// there is one part (one token x 2304 x 768 3.2 us, with it 3.5).
 
-template <int BN>
+template <int BN, bool LONG>
 struct JoinLayout {
   static constexpr bool SEND = BN == 16;
   static constexpr int B = BN * kBlock;  // (columns of B: 128 at a time, so BN = 128 there)
@@ -560,14 +566,18 @@ struct JoinLayout {
   static constexpr int OFF_PARTS = SEND ? STAGES * STAGE : 0;
   static constexpr int OFF_SCALE = STAGES * STAGE + (PARTS + 511) / 512 * 512;
   static constexpr int OFF_BAR = OFF_SCALE + SETS * ATOMS * 512;
-  static constexpr int N_BAR = 2 * STAGES + 2 * SETS + 2;
+  static constexpr int ACCS = LONG ? 2 : 1;
+  static constexpr int N_BAR = 2 * STAGES + 2 * SETS + 2 * ACCS + 1;
   static constexpr int OFF_MISC = OFF_BAR + N_BAR * 8;
   static constexpr int SMEM = OFF_MISC + 16;
   static_assert(SMEM <= (BN <= 64 ? 233472 / 2 - 1024 : 232448), "shared memory (up to 64: of two CTAs an SM)");
-  static constexpr int SCALES = BN;      // columns of tensor memory: the accumulator, the scale words
+  // columns of tensor memory: the accumulators, the scale words, the sum
+  static constexpr int SCALES = ACCS * BN;
   static constexpr int WORDS = 4 * ATOMS;
-  static constexpr int USED = SCALES + SETS * WORDS;
-  static constexpr int COLS = USED <= 64 ? 64 : USED <= 128 ? 128 : 256;
+  static constexpr int SUM = SCALES + SETS * WORDS;
+  static constexpr int USED = SUM + (LONG ? BN : 0);
+  static constexpr int COLS = USED <= 64 ? 64 : USED <= 128 ? 128 : USED <= 256 ? 256 : 512;
+  static_assert(COLS * (BN <= 64 ? 2 : 1) <= 512, "tensor memory (up to 64: of two CTAs an SM)");
   static_assert(((BN + 4) * 128 > 132 * BN ? (BN + 4) * 128 : 132 * BN) * 4 <= STAGES * STAGE, "a part fits");
 };
 
@@ -578,18 +588,19 @@ struct OwnRows {
   __device__ __forceinline__ int pitch() const { return (r1 - r0) | 1; }
 };
 
-template <int BN>
+template <int BN, bool LONG>
 __global__ void __launch_bounds__(kThreads, BN <= 64 ? 2 : 1)
     fp8_mm_join_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b,
                        const Fp8MmParams p) {
-  using L = JoinLayout<BN>;
+  using L = JoinLayout<BN, LONG>;
   extern __shared__ __align__(1024) uint8_t smem[];
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::OFF_BAR);
   uint64_t* empty = full + L::STAGES;
   uint64_t* sc_full = empty + L::STAGES;
   uint64_t* sc_empty = sc_full + L::SETS;
-  uint64_t* acc_full = sc_empty + L::SETS;
-  uint64_t* done = acc_full + 1;
+  uint64_t* acc_full = sc_empty + L::SETS;  // [ACCS]
+  uint64_t* acc_free = acc_full + L::ACCS;  // [ACCS]
+  uint64_t* done = acc_free + L::ACCS;
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + L::OFF_MISC);
   uint32_t* tmem_at = reinterpret_cast<uint32_t*>(smem + L::OFF_MISC + 8);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -597,7 +608,9 @@ __global__ void __launch_bounds__(kThreads, BN <= 64 ? 2 : 1)
   if (threadIdx.x == 0) {
     for (int s = 0; s < L::STAGES; ++s) mbar_init(&full[s], 1), mbar_init(&empty[s], 1);
     for (int s = 0; s < L::SETS; ++s) mbar_init(&sc_full[s], 1), mbar_init(&sc_empty[s], 1);
-    mbar_init(acc_full, 1);
+    for (int s = 0; s < L::ACCS; ++s) mbar_init(&acc_full[s], 1);
+    if constexpr (LONG)
+      for (int s = 0; s < L::ACCS; ++s) mbar_init(&acc_free[s], 4);
     mbar_init(done, 1);
     *abort_flag = aligned ? 0 : 1;
     fence_mbar_init();
@@ -654,7 +667,19 @@ __global__ void __launch_bounds__(kThreads, BN <= 64 ? 2 : 1)
     const uint32_t a0 = sdesc_sw128(smem_u32(smem), 128 * kBlock);
     const uint32_t sc0 = smem_u32(smem + L::OFF_SCALE);
     bool ok = aligned;
+    int part = 0, first = 0;  // and the block that it begins with
     for (int i = 0; i < kb1 - kb0; ++i) {
+      if constexpr (LONG) {
+        if (i - first == p.chunk) {
+          umma_commit(&acc_full[part & 1]);
+          ++part;
+          first = i;
+          // this accumulator's part of two before has been read
+          if (part > 1) ok = warp_wait(&acc_free[part & 1], ((part >> 1) - 1) & 1, ctl);
+          if (!ok) break;
+          tc_fence_after();
+        }
+      }
       const int in = i % kGroup, g = i / kGroup, set = g % L::SETS;
       const uint32_t words = tmem + L::SCALES + set * L::WORDS;
       if (in == 0) {
@@ -669,11 +694,12 @@ __global__ void __launch_bounds__(kThreads, BN <= 64 ? 2 : 1)
       if (!ok) break;
       tc_fence_after();
       const uint32_t a = a0 + st * (L::STAGE >> 4);
-      umma_mx4(tmem, a, a + (kA >> 4), a_step, b_step, idesc | idesc_scale_byte(in), words, words + 4, i > 0);
+      umma_mx4(tmem + (part & 1) * BN, a, a + (kA >> 4), a_step, b_step, idesc | idesc_scale_byte(in), words, words + 4,
+               i > first);
       umma_commit(&empty[st]);
       if (in == kGroup - 1) umma_commit(&sc_empty[set]);
     }
-    umma_commit(ok ? acc_full : done);
+    umma_commit(ok ? &acc_full[part & 1] : done);
     if (!ok) drain_wait(done, 0, p.budget_ns);  // what was issued ends before the CTA goes
     __syncwarp();
   } else if (warp == 2) {
@@ -709,16 +735,45 @@ __global__ void __launch_bounds__(kThreads, BN <= 64 ? 2 : 1)
                                          4 * (rank * BN * own.pitch() + row - own.r0);
     [[maybe_unused]] float* part = reinterpret_cast<float*>(smem);
     const int n = min(BN, p.rows_b - tq * BN);
-    const bool ok = aligned && warp_wait(acc_full, 0, ctl);
-    tc_fence_after();
     const uint32_t acc = tmem + (static_cast<uint32_t>((warp - 4) * 32) << 16);
+    const int last = LONG ? (kb1 - kb0 - 1) / p.chunk : 0;
+    // 16 columns of part k, with the sum of those before it
+    auto read = [&](int k, int c, uint32_t (&v)[16]) {
+      tmem_ld16(acc + (k & 1) * BN + c, v);
+      if (!LONG || k == 0) {
+        tmem_wait_ld();
+        return;
+      }
+      uint32_t s[16];
+      tmem_ld16(acc + L::SUM + c, s);
+      tmem_wait_ld();
+#pragma unroll
+      for (int e = 0; e < 16; ++e) v[e] = __float_as_uint(__uint_as_float(s[e]) + __uint_as_float(v[e]));
+    };
+    bool ok = aligned;
+    for (int k = 0; k < last && ok; ++k) {
+      ok = warp_wait(&acc_full[k & 1], (k >> 1) & 1, ctl);
+      if (!ok) break;
+      tc_fence_after();
+#pragma unroll 1
+      for (int c = 0; c < n; c += 16) {
+        uint32_t v[16];
+        read(k, c, v);
+        tmem_st16(acc + L::SUM + c, v);
+      }
+      tmem_wait_st();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&acc_free[k & 1]);
+    }
+    ok = ok && warp_wait(&acc_full[last & 1], (last >> 1) & 1, ctl);
+    tc_fence_after();
     cluster_wait();  // all CTAs are there
 #pragma unroll 1
     for (int c = 0; c < n; c += 16) {
       uint32_t v[16];
       if (ok) {
-        tmem_ld16(acc + c, v);
-        tmem_wait_ld();
+        read(last, c, v);
       } else {
 #pragma unroll
         for (int k = 0; k < 16; ++k) v[k] = 0u;
@@ -815,11 +870,11 @@ cudaError_t run_pair(const CUtensorMap& ta, const CUtensorMap& tb, const CUtenso
                 kPairThreads, 2 * pairs, PairLayout<BN>::SMEM, s, ta, tb, tc, p);
 }
 
-template <int BN>
+template <int BN, bool LONG>
 cudaError_t run_join(const CUtensorMap& ta, const CUtensorMap& tb, const Fp8MmParams& p, int dev, cudaStream_t s) {
   static OncePerDevice prepared;
-  return launch(fp8_mm_join_kernel<BN>, prepared, dev, p.tiles_p * p.tiles_q * p.splits, kThreads, p.splits,
-                JoinLayout<BN>::SMEM, s, ta, tb, p);
+  return launch(fp8_mm_join_kernel<BN, LONG>, prepared, dev, p.tiles_p * p.tiles_q * p.splits, kThreads, p.splits,
+                JoinLayout<BN, LONG>::SMEM, s, ta, tb, p);
 }
 
 }  // namespace
@@ -829,8 +884,8 @@ int fp8_clusters(int r, int dev) {
   if (dev < 0 || dev >= kMaxDevices) return 1;
   std::atomic<int>& here = known[dev][r];
   if (const int n = here.load(std::memory_order_relaxed)) return n;
-  const auto kernel = fp8_mm_join_kernel<128>;
-  constexpr int smem = JoinLayout<128>::SMEM;
+  const auto kernel = fp8_mm_join_kernel<128, false>;
+  constexpr int smem = JoinLayout<128, false>::SMEM;
   const ClusterConfig c(r, kThreads, r, smem, nullptr);
   int n = 0;
   if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess ||
@@ -845,10 +900,11 @@ int fp8_clusters(int r, int dev) {
 cudaError_t launch_fp8_mm(int bn, bool join, const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap& tc,
                           const Fp8MmParams& p, int dev, cudaStream_t s) {
   if (join) {
-    if (bn == 16) return run_join<16>(ta, tb, p, dev, s);
-    if (bn == 32) return run_join<32>(ta, tb, p, dev, s);
-    if (bn == 64) return run_join<64>(ta, tb, p, dev, s);
-    return run_join<128>(ta, tb, p, dev, s);
+    const bool parts = (p.blocks + p.splits - 1) / p.splits > p.chunk;
+    if (bn == 16) return parts ? run_join<16, true>(ta, tb, p, dev, s) : run_join<16, false>(ta, tb, p, dev, s);
+    if (bn == 32) return parts ? run_join<32, true>(ta, tb, p, dev, s) : run_join<32, false>(ta, tb, p, dev, s);
+    if (bn == 64) return parts ? run_join<64, true>(ta, tb, p, dev, s) : run_join<64, false>(ta, tb, p, dev, s);
+    return run_join<128, false>(ta, tb, p, dev, s);
   }
   if (bn == 128) return run_pair<128, false>(ta, tb, tc, p, dev, s);
   if (p.splits > 1) return run_pair<256, true>(ta, tb, tc, p, dev, s);

@@ -373,8 +373,8 @@ struct Fp8MmParams {
   int tiles_p, tiles_q;  // of 128 rows of A (pairs: 256), of bn rows of B
   int splits;            // join: CTAs of a tile; pairs: pairs of a tile
   int ctas;              // pairs: CTAs at most
-  int chunk;             // pairs: blocks that are summed in tensor memory before the output takes them,
-                         // or a pair's share of a tile's blocks
+  int chunk;             // blocks (whole words of scales) that are summed in tensor memory at once, before the
+                         // output takes them (pairs) or a sum beside them (join); or a pair's share of a tile's
   bool a_columns, b_columns;  // rows of the operand lie across the contraction
   bool swap;             // join: a row of the output is one of B
   bool out_f32;
