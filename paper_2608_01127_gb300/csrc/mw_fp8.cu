@@ -64,8 +64,13 @@ MmPlan mm_plan(int M, int N, int blocks, bool a_columns, bool b_columns, bool f3
     if (cost < best_cost) best_cost = cost, best.bn = bn, best.join = join, best.splits = splits;
   };
   auto tiles = [&](int rows, int bn) { return static_cast<long long>(ceil_div(M, rows)) * ceil_div(N, bn); };
-  take(256, false, 1, 4.8 + ceil_div(tiles(256, 256), sms / 2) * (0.265 * blocks + 1.0));
-  take(128, false, 1, 4.0 + ceil_div(tiles(256, 128), sms / 2) * (0.26 * blocks + 0.5));
+  // (parts of a pair's sum are added up in the output, which bf16 cannot take; clusters keep them
+  // in tensor memory: 2048 x 2048 x 524288 in 2.1 ms, by pairs in one part 1.1 ms)
+  const int limit = f32 ? kFp8Chunk : kFp8ChunkBf16;
+  if (f32 || blocks <= limit) {
+    take(256, false, 1, 4.8 + ceil_div(tiles(256, 256), sms / 2) * (0.265 * blocks + 1.0));
+    take(128, false, 1, 4.0 + ceil_div(tiles(256, 128), sms / 2) * (0.26 * blocks + 0.5));
+  }
   for (int r = 1; r <= most; ++r) {
     const int share = ceil_div(blocks, r);
     if (f32 && share > kFp8Chunk) continue;
@@ -75,7 +80,7 @@ MmPlan mm_plan(int M, int N, int blocks, bool a_columns, bool b_columns, bool f3
   // (one round of clusters: a second one starts from nothing)
   for (int r = 2; 2 * r <= kFp8Splits && tiles(256, 256) * 2 * r <= sms; ++r) {
     const int share = pair_share(blocks, r);
-    if ((f32 && share > kFp8Chunk) || share * (r - 1) >= blocks) continue;
+    if (share > limit || share * (r - 1) >= blocks) continue;
     const double cost = 9.5 + 0.272 * share;
     if (cost < best_cost && tiles(256, 256) <= fp8_clusters(2 * r, dev)) take(256, false, r, cost);
   }
@@ -296,10 +301,10 @@ mw_status mw_scaled_matmul(const void* a, const void* a_scale, int a_tiles, int 
   p.tiles_q = ceil_div(rows_b, plan.bn);
   p.ctas = sm_count();
   // (whole words of scales)
-  p.chunk = !plan.join && plan.splits > 1 ? pair_share(p.blocks, plan.splits)
-            : plan.join && f32               ? kFp8Chunk
-            : f32                            ? pair_share(p.blocks, ceil_div(p.blocks, kFp8Chunk))
-                                             : p.blocks;
+  const int limit = f32 ? kFp8Chunk : kFp8ChunkBf16;
+  p.chunk = plan.join         ? limit
+            : plan.splits > 1 ? pair_share(p.blocks, plan.splits)
+                              : pair_share(p.blocks, ceil_div(p.blocks, limit));
   p.out = c;
   p.out_f32 = f32;
   p.out_quads = N % 4 == 0 && (reinterpret_cast<uintptr_t>(c) & (4 * elem - 1)) == 0;

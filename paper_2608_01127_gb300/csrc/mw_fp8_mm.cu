@@ -904,7 +904,7 @@ cudaError_t launch_fp8_mm(int bn, bool join, const CUtensorMap& ta, const CUtens
     if (bn == 16) return parts ? run_join<16, true>(ta, tb, p, dev, s) : run_join<16, false>(ta, tb, p, dev, s);
     if (bn == 32) return parts ? run_join<32, true>(ta, tb, p, dev, s) : run_join<32, false>(ta, tb, p, dev, s);
     if (bn == 64) return parts ? run_join<64, true>(ta, tb, p, dev, s) : run_join<64, false>(ta, tb, p, dev, s);
-    return run_join<128, false>(ta, tb, p, dev, s);
+    return parts ? run_join<128, true>(ta, tb, p, dev, s) : run_join<128, false>(ta, tb, p, dev, s);
   }
   if (bn == 128) return run_pair<128, false>(ta, tb, tc, p, dev, s);
   if (p.splits > 1) return run_pair<256, true>(ta, tb, tc, p, dev, s);

@@ -10,6 +10,7 @@ import torch
 
 BF16, F32, E4M3, E8M0 = torch.bfloat16, torch.float32, torch.float8_e4m3fn, torch.float8_e8m0fnu
 PART = 64 * 4  # instructions in a row of an fp32 result: 64 blocks
+PART_BF16 = 2048 * 4
 
 
 @pytest.fixture(scope="module")
@@ -56,14 +57,15 @@ def reference(a, sa, b, sb):
     return out
 
 
-def deviations(mw, M, N, K, dtype, few=256):
-    """(result - exact) / exact of up to `few` rows and columns."""
+def deviations(mw, M, N, K, dtype, rounding=None, few=256):
+    """(result - exact) / exact of up to `few` rows and columns; sizes less the last rounding's."""
     a, sa = positive(1, M, K)
     b, sb = positive(2, N, K)
     c = mw.mw_scaled_matmul(a, sa, b, sb, dtype)
     assert mw.mw_device_status() == 0
     ref = reference(a[-few:], sa[-few:], b[-few:], sb[-few:])
-    return (c[-few:, -few:].double() - ref) / ref
+    off = c[-few:, -few:].double() - ref
+    return off / ref if rounding is None else (off.abs() - rounding(ref)) / ref
 
 
 @pytest.mark.gpu
@@ -92,6 +94,39 @@ def test_parts_of_whole_numbers_are_exact(mw, M, N, K):
     assert torch.equal(c.double(), reference(a, sa, b, sb))
     assert bool((everything[M * N:] == 7).all())
     assert torch.equal(mw.mw_scaled_matmul(a, sa, b, sb, F32), c)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M,N,K", [(16, 640, 1 << 22), (200, 40, 1 << 22), (300, 300, 1 << 22), (1024, 1024, 1 << 21),
+                                   (2600, 2304, 1 << 19)])
+def test_what_bf16_results_lose_does_not_grow(mw, M, N, K):
+    """Less the last rounding, half a step at most.  Of thousands of instructions the sum grows
+    evenly, within a twentieth, at every element: a half again, not at the mean alone."""
+    off = deviations(mw, M, N, K, BF16, lambda ref: torch.exp2(torch.floor(torch.log2(ref)) - 8))
+    assert float(off.max()) <= 1.05 * PART_BF16 / 2 * 2.0 ** -22
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M,N,K", [(2, 19456, 1 << 18), (7, 2000, 262144 * 7 + 48), (300, 257, 262144 * 9 + 16),
+                                   (1500, 1300, 262144 + 128), (1200, 1100, 262144 * 2 + 112)])
+def test_bf16_parts_of_whole_numbers_are_exact(mw, M, N, K):
+    a, sa = whole(1, M, K)
+    b, sb = whole(2, N, K)
+    c = mw.mw_scaled_matmul(a, sa, b, sb)
+    assert mw.mw_device_status() == 0
+    assert torch.equal(c, reference(a, sa, b, sb).float().to(BF16))
+
+
+@pytest.mark.gpu
+def test_columns_of_a_long_contraction(mw):
+    """Both operands across it: the weight's gradient over half a million rows."""
+    K = (1 << 19) + 3
+    (a, sa), (b, sb) = whole(1, 640, K), whole(2, 512, K)
+    ones = torch.full((-(-K // 128), 640), 127, dtype=torch.uint8, device="cuda").view(E8M0)
+    for dtype in (BF16, F32):
+        c = mw.mw_scaled_matmul(a.T.contiguous(), ones, b.T.contiguous(), ones[:, :512].contiguous(), dtype, True, True)
+        want = sum(a[:, k:k + 65536].double() @ b[:, k:k + 65536].double().T for k in range(0, K, 65536))
+        assert torch.equal(c, want.float().to(dtype))
 
 
 @pytest.mark.gpu
