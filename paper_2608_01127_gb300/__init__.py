@@ -987,6 +987,13 @@ def _first_derivatives(what: str, compute, *inputs):
     return compute(*inputs)
 
 
+def _aligned_gradient(g: torch.Tensor) -> torch.Tensor:
+    """A gradient as 16-byte accesses and copies need it: autograd may deliver a view that
+    starts anywhere."""
+    g = g.contiguous()
+    return g if g.data_ptr() % 16 == 0 else g.clone()
+
+
 class BlockCausalAttention(torch.autograd.Function):
     """Autograd wrapper: O = block-causal attention(q, k, v) with chunks of T_chunk.  A second
     derivative is refused."""
@@ -1148,7 +1155,7 @@ class Fp8Linear(torch.autograd.Function):
         K = ctx.shape[-1]
 
         def gradients(dy):
-            g = dy.contiguous().view(-1, wq.shape[0])
+            g = _aligned_gradient(dy).view(-1, wq.shape[0])
             gq = gs = gc = gcs = None
             if need_x and need_w:
                 gq, gs, gc, gcs = mw_quantize_both(g)

@@ -970,6 +970,13 @@ at::Tensor plain_gradient(const at::Tensor& g, const at::Tensor& like, at::Scala
   return g.contiguous();
 }
 
+// A gradient as 16-byte accesses and copies need it: autograd may deliver a view that starts
+// anywhere.
+at::Tensor aligned_gradient(const at::Tensor& g) {
+  const at::Tensor c = g.contiguous();
+  return reinterpret_cast<uintptr_t>(c.const_data_ptr()) % 16 == 0 ? c : c.clone();
+}
+
 // A saved tensor as the forward left it: a hook may have put another in its place, and the
 // kernels get its address.
 void check_saved(const at::Tensor& t, const char* name, at::ScalarType type, at::IntArrayRef sizes,
@@ -1329,7 +1336,7 @@ struct Fp8LinearBackward : public torch::autograd::Node {
     TORCH_CHECK(is_real(grad) && grad.scalar_type() == torch_type(z.yt) && grad.sizes() == y_sizes &&
                     grad.get_device() == dev,
                 "the gradient must be a plain CUDA tensor like the output");
-    const at::Tensor dy = grad.contiguous();
+    const at::Tensor dy = aligned_gradient(grad);
     const int form = need_x && need_w ? MW_FP8_ROWS_AND_COLUMNS : need_x ? MW_FP8_ROWS : MW_FP8_COLUMNS;
     Pack pack;
     const PackedForm g(&pack, z.M, z.N, form);
