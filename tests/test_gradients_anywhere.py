@@ -52,3 +52,18 @@ def test_linear(mw, way, dtype, needs):
         check(lambda t: mw.Fp8Linear.apply(t, w), (x,), 3)
     else:
         check(lambda t: mw.Fp8Linear.apply(x, t), (w,), 7 if dtype == BF16 else 2)
+
+
+def test_norms(mw, way):
+    """(Read element by element then, with sums in another order: fp32's rounding, 2^-24 for
+    each of the 96 terms at most, and the result's.)"""
+    for call in (lambda x, w: mw.LayerNorm.apply(x, w), lambda x, w: mw.RMSNorm.apply(x, w)):
+        x, w = (t.requires_grad_(True) for t in (rnd(1, 30, 96), rnd(2, 96, dtype=torch.float32)))
+        y = call(x, w)
+        dy = rnd(3, 30, 96)
+        want = torch.autograd.grad(y, (x, w), dy, retain_graph=True)
+        whole = torch.cat([torch.zeros(1, dtype=BF16, device="cuda", requires_grad=True), y.flatten()])
+        got = torch.autograd.grad(whole, (x, w), torch.cat([torch.zeros(1, dtype=BF16, device="cuda"), dy.flatten()]))
+        for a, b, last in zip(got, want, (2.0 ** -7, 0.0)):
+            size = b.double().abs().max()
+            assert bool(((a.double() - b.double()).abs() <= last * b.double().abs() + 96 * 2.0 ** -24 * size).all())
