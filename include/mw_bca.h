@@ -444,8 +444,9 @@ mw_status mw_quantize(const void* x, void* q, void* scale, void* q_columns, void
  * W transposed), dW = (dy in COLUMNS transposed, x in COLUMNS transposed).
  * Codes 16-byte aligned, their rows multiples of 16 (K, or M or N where transposed); 0 <=
  * M, N, K <= 2^24, at most 2^27 tiles of 128 x 128 results.  K = 0 gives zeros.  Scales of 0xff
- * and codes of NaN give NaN.  The order of sums is fixed by the sizes.  After a wait that
- * ran out (MW_ERR_TIMEOUT) the results are not to be used.
+ * and codes of NaN give NaN.  The order of sums is fixed by the sizes, the layouts, c_dtype and
+ * the device, which is asked once how many clusters it runs (MW_ERR_CUDA where it does not
+ * tell).  After a wait that ran out (MW_ERR_TIMEOUT) the results are not to be used.
  */
 mw_status mw_scaled_matmul(const void* a, const void* a_scale, int a_tiles, int a_transposed, const void* b,
                            const void* b_scale, int b_tiles, int b_transposed, void* c, int M, int N, int K,

@@ -39,9 +39,15 @@ struct MmPlan {
 // Blocks of each of r pairs that share a contraction: whole words of scales.
 int pair_share(int blocks, int r) { return ceil_div(ceil_div(blocks, r), 4) * 4; }
 
-MmPlan mm_plan(int M, int N, int blocks, bool a_columns, bool b_columns, bool f32, int sms, int dev) {
-  MmPlan best;
+// A device that does not tell how many clusters it runs is an error: with a guess in its place a
+// call's sums would be made in another order than the next one's.
+mw_status mm_plan(int M, int N, int blocks, bool a_columns, bool b_columns, bool f32, int sms, int dev, MmPlan* plan) {
+  MmPlan& best = *plan;
   const int most = std::min(kFp8Splits, blocks);
+  int clusters[kFp8Splits + 1] = {};
+  for (int r = 1; r <= most; ++r)
+    MW_TRY(launch_status(fp8_clusters(r, dev, &clusters[r]), "asking for the clusters of a device"));
+  if (clusters[1] < 1) return fail(MW_ERR_CUDA, "the device has no SM with the shared memory of a product");
   double best_cost = INFINITY;
   const bool few_m = M <= 64 && !a_columns, few_n = N <= 64 && !b_columns;
   if (few_m || few_n) {
@@ -53,11 +59,12 @@ MmPlan mm_plan(int M, int N, int blocks, bool a_columns, bool b_columns, bool f3
     // costs more than their number (us for 1 to 8 CTAs: 8 x 2560 x 10240 21.2 12.7 10.2 8.6 8.0
     // 7.9 8.3 8.3; 16 x 7680 x 2560 8.8 7.4 7.6 7.2 11.2 11.5 12.1 12.4)
     for (int r = 1; r <= most; ++r) {
-      const double load = std::max(1.0, static_cast<double>(tiles) / fp8_clusters(r, dev));
+      if (clusters[r] == 0) continue;
+      const double load = std::max(1.0, static_cast<double>(tiles) / clusters[r]);
       const double cost = ceil_div(blocks, r) * load * load;
       if (cost < best_cost) best_cost = cost, best.splits = r;
     }
-    return best;
+    return MW_OK;
   }
   // us, fitted to 22 sizes: what a launch takes, a block of the contraction, a tile
   auto take = [&](int bn, bool join, int splits, double cost) {
@@ -73,8 +80,8 @@ MmPlan mm_plan(int M, int N, int blocks, bool a_columns, bool b_columns, bool f3
   }
   for (int r = 1; r <= most; ++r) {
     const int share = ceil_div(blocks, r);
-    if (f32 && share > kFp8Chunk) continue;
-    const double load = static_cast<double>(tiles(128, 128)) / fp8_clusters(r, dev);
+    if ((f32 && share > kFp8Chunk) || clusters[r] == 0) continue;
+    const double load = static_cast<double>(tiles(128, 128)) / clusters[r];
     take(128, true, r, std::ceil(load) * (7.1 + 0.225 * share));
   }
   // (one round of clusters: a second one starts from nothing)
@@ -82,9 +89,9 @@ MmPlan mm_plan(int M, int N, int blocks, bool a_columns, bool b_columns, bool f3
     const int share = pair_share(blocks, r);
     if (share > limit || share * (r - 1) >= blocks) continue;
     const double cost = 9.5 + 0.272 * share;
-    if (cost < best_cost && tiles(256, 256) <= fp8_clusters(2 * r, dev)) take(256, false, r, cost);
+    if (cost < best_cost && tiles(256, 256) <= clusters[2 * r]) take(256, false, r, cost);
   }
-  return best;
+  return MW_OK;
 }
 
 }  // namespace
@@ -265,7 +272,8 @@ mw_status mw_scaled_matmul(const void* a, const void* a_scale, int a_tiles, int 
   Fp8MmParams p{};
   MW_TRY(status_ptr(scope.device(), &p.status));
   p.blocks = ceil_div(K, kFp8Block);
-  const MmPlan plan = mm_plan(M, N, p.blocks, a_transposed, b_transposed, f32, sm_count(), scope.device());
+  MmPlan plan;
+  MW_TRY(mm_plan(M, N, p.blocks, a_transposed, b_transposed, f32, sm_count(), scope.device(), &plan));
   auto scales = [&](const void* at, int rows, bool transposed, bool tile) {
     Fp8Scales z{};
     z.p = static_cast<const uint8_t*>(at);

@@ -879,22 +879,22 @@ cudaError_t run_join(const CUtensorMap& ta, const CUtensorMap& tb, const Fp8MmPa
 
 }  // namespace
 
-int fp8_clusters(int r, int dev) {
-  static std::atomic<int> known[kMaxDevices][kFp8Splits + 1];
-  if (dev < 0 || dev >= kMaxDevices) return 1;
+cudaError_t fp8_clusters(int r, int dev, int* n) {
+  static std::atomic<int> known[kMaxDevices][kFp8Splits + 1];  // one more than there are
+  if (dev < 0 || dev >= kMaxDevices) return cudaErrorInvalidDevice;
   std::atomic<int>& here = known[dev][r];
-  if (const int n = here.load(std::memory_order_relaxed)) return n;
+  *n = here.load(std::memory_order_relaxed) - 1;
+  if (*n >= 0) return cudaSuccess;
   const auto kernel = fp8_mm_join_kernel<128, false>;
   constexpr int smem = JoinLayout<128, false>::SMEM;
   const ClusterConfig c(r, kThreads, r, smem, nullptr);
-  int n = 0;
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess ||
-      cudaOccupancyMaxActiveClusters(&n, kernel, &c.cfg) != cudaSuccess || n < 1) {
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e == cudaSuccess) e = cudaOccupancyMaxActiveClusters(n, kernel, &c.cfg);
+  if (e == cudaSuccess)
+    here.store(*n + 1, std::memory_order_relaxed);
+  else
     cudaGetLastError();
-    return 1;
-  }
-  here.store(n, std::memory_order_relaxed);
-  return n;
+  return e;
 }
 
 cudaError_t launch_fp8_mm(int bn, bool join, const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap& tc,

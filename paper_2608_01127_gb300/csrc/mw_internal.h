@@ -388,7 +388,8 @@ struct Fp8MmParams {
 };
 // Clusters of r CTAs (1 to kFp8Splits), a CTA an SM, that device dev, the current one, runs at once.
 // Its groups of SMs are not alike (152 SMs: 76 clusters of 2, 46 of 3, 36 of 4, 23 of 6, 15 of 8).
-int fp8_clusters(int r, int dev);
+// Asked of the device once.
+cudaError_t fp8_clusters(int r, int dev, int* n);
 // bn: rows of B of a tile (join: 16, 32, 64 or 128; pairs: 128 or 256); ta, tb: boxes of 128
 // bytes x 128 rows (join's tb, and pairs' of 128 rows: x bn and 64 rows where B runs along the
 // contraction); tc: 32 rows x 64 bytes
