@@ -147,6 +147,22 @@ def test_a_wait_that_runs_out_with_parts_to_come(mw, M):
 
 
 @pytest.mark.gpu
+def test_a_wait_that_runs_out_with_bf16_parts_to_come(mw):
+    a, sa = whole(1, 300, 1 << 22)
+    b, sb = whole(2, 260, 1 << 22)
+    good = mw.mw_scaled_matmul(a, sa, b, sb)
+    mw.mw_set_option("wait_budget_ms", 50)
+    mw.mw_set_option("debug_skip_q_load", 1)
+    try:
+        mw.mw_scaled_matmul(a, sa, b, sb)
+        assert mw.mw_device_status() == 4
+    finally:
+        mw.mw_set_option("debug_skip_q_load", 0)
+        mw.mw_set_option("wait_budget_ms", 2000)
+    assert torch.equal(mw.mw_scaled_matmul(a, sa, b, sb), good) and mw.mw_device_status() == 0
+
+
+@pytest.mark.gpu
 def test_parts_on_streams_at_once(mw):
     """Two CTAs an SM take turns with accumulators; other products beside them."""
     jobs = []
