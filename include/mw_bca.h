@@ -443,7 +443,10 @@ mw_status mw_quantize(const void* x, void* q, void* scale, void* q_columns, void
  * So that for y = x W^T, x in ROWS and W [N, K] in TILES: y = (x, W), dx = (dy in ROWS,
  * W transposed), dW = (dy in COLUMNS transposed, x in COLUMNS transposed).
  * Codes 16-byte aligned, their rows multiples of 16 (K, or M or N where transposed); 0 <=
- * M, N, K <= 2^24, at most 2^27 tiles of 128 x 128 results.  K = 0 gives zeros.  Scales of 0xff
+ * M, N, K <= 2^24, at most 2^27 tiles of 128 x 128 results.  K = 0 gives zeros.  Scales are
+ * exponent bytes, powers of two; a matrix with scales of any value has to be put into this form.
+ * The tensor cores cut what falls below a sum's last place, so that sums are made in parts: of
+ * 8192 of the contraction at most for fp32 results, of 262144 for bf16.  Scales of 0xff
  * and codes of NaN give NaN.  The order of sums is fixed by the sizes, the layouts, c_dtype and
  * the device, which is asked once how many clusters it runs (MW_ERR_CUDA where it does not
  * tell).  After a wait that ran out (MW_ERR_TIMEOUT) the results are not to be used.

@@ -723,6 +723,8 @@ def mw_layernorm_bwd(dy, x, mean, rstd, weight: Optional[torch.Tensor] = None,
 
 
 _E4M3, _E8M0 = torch.float8_e4m3fn, torch.float8_e8m0fnu
+
+
 def _rms_inputs(x, weight, residual):
     xt = _norm_type(x, "x")
     rows, C, groups, ptype = _norm_params(x, weight, None)
@@ -764,7 +766,7 @@ def mw_rmsnorm_fwd(x: torch.Tensor, weight: Optional[torch.Tensor] = None,
 
 
 def mw_rmsnorm_quantize(x: torch.Tensor, weight: Optional[torch.Tensor] = None,
-                   residual: Optional[torch.Tensor] = None, eps: float = 1e-5, need_stats: bool = True):
+                        residual: Optional[torch.Tensor] = None, eps: float = 1e-5, need_stats: bool = True):
     """mw_rmsnorm_fwd with y as the product reads it: (q, scale, h, rstd) with y's 8-bit form
     in blocks of (1, 128), as mw_quantize gives it (y itself is not rounded before).  C
     must be a multiple of 16."""
@@ -832,8 +834,7 @@ def _fp8_source(x) -> Tuple[int, int, int]:
     return xt, math.prod(x.shape[:-1]), C
 
 
-def mw_quantize(x: torch.Tensor, block: Tuple[int, int] = (1, 128), out=None
-                    ) -> Tuple[torch.Tensor, torch.Tensor]:
+def mw_quantize(x: torch.Tensor, block: Tuple[int, int] = (1, 128), out=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """The 8-bit form of x [..., C] (bf16 or fp32), its rows taken as one matrix [R, C]:
     codes in x's shape (float8_e4m3fn) and for every ``block`` -- (1, 128), (128, 1) or
     (128, 128) elements -- a scale (float8_e8m0fnu), the least power of two s with
@@ -878,8 +879,7 @@ def mw_quantize_both(x: torch.Tensor):
     q, qc = (torch.empty(x.shape, dtype=_E4M3, device=x.device) for _ in range(2))
     scale, sc = (torch.empty(n, dtype=_E8M0, device=x.device)
                  for n in ((rows, _blocks(C)), (_blocks(rows), C)))
-    _check(library().mw_quantize(_ptr(x), _ptr(q), _ptr(scale), _ptr(qc), _ptr(sc), rows, C, 3,
-                                     xt, _stream()))
+    _check(library().mw_quantize(_ptr(x), _ptr(q), _ptr(scale), _ptr(qc), _ptr(sc), rows, C, 3, xt, _stream()))
     return q, scale, qc, sc
 
 
@@ -904,14 +904,19 @@ def _fp8_operand(t, scale, name: str, transposed: bool) -> Tuple[int, int, bool]
 
 
 def mw_scaled_matmul(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_scale: torch.Tensor,
-                  out_dtype: torch.dtype = torch.bfloat16, a_transposed: bool = False,
-                  b_transposed: bool = False, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+                     out_dtype: torch.dtype = torch.bfloat16, a_transposed: bool = False,
+                     b_transposed: bool = False, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """c = A B^T of two 8-bit forms, [M, N] in ``out_dtype`` (bf16 or fp32), summed in fp32.
 
     a: codes [M, K] with scales [M, ceil(K/128)] (blocks of (1, 128)) or [ceil(M/128),
     ceil(K/128)] (of (128, 128)); with ``a_transposed`` codes [K, M] with scales
     [ceil(K/128), M] (blocks of (128, 1)) or [ceil(K/128), ceil(M/128)].  b: the same with
-    N in the place of M.  ``out`` reuses a caller's buffer."""
+    N in the place of M.  ``out`` reuses a caller's buffer.
+
+    Scales are powers of two (float8_e8m0fnu), as mw_quantize makes them.  A matrix that comes
+    with scales of any value (fp32) has to be multiplied out and put into this form.  An fp32
+    result sums 8192 of the contraction at most in one tensor-core accumulator, one in bf16
+    262144, and longer ones in parts."""
     if out is None and _native is not None:
         r = _native.scaled_matmul(a, a_scale, b, b_scale, out_dtype, a_transposed, b_transposed)
         if r is not None:
@@ -928,8 +933,8 @@ def mw_scaled_matmul(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_
     c = torch.empty((M, N), dtype=out_dtype, device=a.device) if out is None else out
     _no_alias((("out", c),), (("a", a), ("a_scale", a_scale), ("b", b), ("b_scale", b_scale)))
     _check(library().mw_scaled_matmul(_ptr(a), _ptr(a_scale), int(a_tiles), int(bool(a_transposed)), _ptr(b),
-                                   _ptr(b_scale), int(b_tiles), int(bool(b_transposed)), _ptr(c), M, N, K,
-                                   _NORM_TYPES[out_dtype], _stream()))
+                                      _ptr(b_scale), int(b_tiles), int(bool(b_transposed)), _ptr(c), M, N, K,
+                                      _NORM_TYPES[out_dtype], _stream()))
     return c
 
 
@@ -1118,7 +1123,9 @@ class Fp8Linear(torch.autograd.Function):
     fp32), its three products in 8 bits, in the form of mw_quantize: x and dy in blocks
     along what is summed (a row for y and dx, a column for dW), W in blocks of (128, 128).  y
     has ``out_dtype`` (None: x's); gradients have their inputs' types.  K and N are multiples
-    of 16.  A second derivative is refused."""
+    of 16; x and weight start at 16 bytes (gradients may start anywhere).  W's form is made at
+    each call: a program whose weights stay keeps mw_quantize(W, (128, 128)) and calls
+    mw_scaled_matmul.  A second derivative is refused."""
 
     @classmethod
     def apply(cls, x, weight, out_dtype: Optional[torch.dtype] = None):

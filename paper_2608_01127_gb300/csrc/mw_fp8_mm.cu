@@ -180,9 +180,10 @@ __device__ __forceinline__ void join_parts(const Fp8MmParams& p, float* part, in
 // L2 for 128 x 256 x 128 products, not 48 (a CTA alone with 128 x 256: 14080 x 10240 x 2560 in
 // 322 us, held by L2 at 13 TB/s).  Both have the scales of all of B's rows.
 //
-// Sums of more than `chunk` blocks leave tensor memory in parts, which the output adds up in
-// fp32: the tensor cores cut, not round, what falls below a sum's last place, and 440 such
-// additions (14080 tokens) came to 1e-6 of the result.
+// fp32 sums of more than `chunk` blocks leave tensor memory in parts, which the output adds up:
+// the tensor cores cut, not round, what falls below a sum's last place, and 440 such additions
+// (14080 tokens) came to 1e-6 of the result, of positive terms to 2^-23.6 for each addition.  (bf16
+// results of more are left to clusters of CTAs, below, which add up in tensor memory.)
 //
 // JOIN: few tiles and a long contraction, as a weight's gradient has: a cluster of up to four
 // pairs shares the blocks of a tile, and each CTA adds up a share of its rows' parts, which takes
@@ -526,8 +527,9 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     int tp, tq;
     tile_at(p, tile0, &tp, &tq);
     const int row0 = tp * 256 + rank * 128;
-    join_parts(p, reinterpret_cast<float*>(smem), max(0, min(128, p.rows_a - row0)), BN, row0, tq * BN, p.rows_b - tq * BN,
-               leader / 2, pairs, kPairThreads, [&](int r) { return 2 * r + static_cast<int>(rank); });
+    join_parts(p, reinterpret_cast<float*>(smem), max(0, min(128, p.rows_a - row0)), BN, row0, tq * BN,
+               p.rows_b - tq * BN, leader / 2, pairs, kPairThreads,
+               [&](int r) { return 2 * r + static_cast<int>(rank); });
   }
   cluster.sync();  // nobody's shared memory is in use any more
   if (warp == 1) {

@@ -682,13 +682,15 @@ cudaError_t run_fwd_rows(RmsParams p, const RowsShape& sh, int dev, int sms, cud
       dev, [] { return cudaFuncSetAttribute(kKernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRmsMaxSmem); });
   if (e != cudaSuccess) return e;
   // A group's rows are in parts for as many blocks as the backward has, or, where instructions
-  // and not HBM bound the time, as many as the SMs hold (14080 x 5120 bf16, one block of 320 threads and
-  // two: to 8 bits 87 and 60 us, with the residual 102 and 84; bf16 58 and 46, but with the residual 88
-  // and 95).
+  // and not HBM bound the time, as many as the SMs hold.  The two differ at 14080 x 5120, one block of 320
+  // threads and two (us): bf16 58 and 46, with the residual 89 and 95; to 8 bits 87 and 60, with the
+  // residual 103 and 84; fp32 98 and 98, with the residual 175 and 197, to 8 bits 83 and 83, but with the
+  // residual, where the rule is wrong, 153 and 163.  At 768, 1536, 2560, 4096 and 8192 channels, all types,
+  // they are within 1%.
   p.parts = rms_parts(p.rows_per_group, p.C, p.groups);
   if constexpr (std::is_same_v<Y, E4m3> || !RES) {
     static std::atomic<int> held[kMaxDevices][kNormMaxC / 256 + 1];
-    std::atomic<int>& here = held[dev][sh.W];
+    std::atomic<int>& here = held[dev][sh.W];  // (dev is one that `prepared` has taken)
     int blocks = here.load(std::memory_order_relaxed);
     if (blocks == 0) {
       const cudaError_t o = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&blocks, kKernel, sh.threads, ring);
@@ -762,6 +764,9 @@ cudaError_t launch_rms_fwd(RmsParams p, bool vec, int dev, int sms, cudaStream_t
     if (!p.x_f32) return f(bf16{}, bf16{});
     return p.y_type == kRmsF32 ? f(float{}, float{}) : f(float{}, bf16{});
   };
+  // Rows that a warp or few hold are started sooner than copied ahead.  us of rms_fwd_kernel and of this
+  // one, cold, bf16: 1216 x 768 2.2 and 2.6, 1824 x 768 4.9 and 3.1 (fp32 with the residual 4.3 and 4.3, 7.3 and
+  // 5.3).  Of wide rows fewer would do: 608 x 2560 3.1 and 3.1, but 1216 x 2560 7.1 and 4.4.
   if (vec && p.rows > 8ll * sms) {
     const RowsShape sh = rows_shape(p.C);
     p.W = sh.W;
